@@ -195,11 +195,13 @@ def _dense(tokens, values, V):
 
 
 def _teacher(d):
-    """The teacher's log-probs and probabilities, and what its list leaves of 1 (a small difference: in 64 bits)."""
+    """The teacher's log-probs and probabilities, and what its list leaves of 1 (a small difference: in 64 bits; what fp32
+    log-probs of whole rows may be off by, 2^-20, counts as nothing)."""
     there = d["teacher_tokens"] >= 0
     l = torch.where(there, d["teacher_logp"], -math.inf)
     if d["case"]["tail"]:
-        return l, l.exp(), (1.0 - l.double().exp().sum(dim=1, keepdim=True)).clamp(min=0.0).float()
+        rest = 1.0 - l.double().exp().sum(dim=1, keepdim=True)
+        return l, l.exp(), torch.where(rest < 2.0 ** -20, torch.zeros_like(rest), rest).float()
     top = l.amax(dim=1, keepdim=True)
     e = (l - torch.where(top == -math.inf, torch.zeros_like(top), top)).exp()
     q = e / torch.where(top == -math.inf, torch.ones_like(top), e.sum(dim=1, keepdim=True))
@@ -311,7 +313,8 @@ def _exact_rows(c, d, s):
     l = l.masked_fill(tok < 0, -math.inf)
     some = (tok >= 0).any(dim=1, keepdim=True)
     if c["tail"]:
-        rest = (1.0 - l.exp().sum(dim=1, keepdim=True)).clamp(min=0.0)
+        rest = 1.0 - l.exp().sum(dim=1, keepdim=True)
+        rest = rest.masked_fill(rest < 2.0 ** -20, 0.0)
     else:
         l = torch.where(some, l - torch.logsumexp(l, dim=1, keepdim=True), l)
         rest = torch.zeros_like(lse)
