@@ -58,6 +58,14 @@ enum pb_select_mode {
   PB_SELECT_TWO_STAGE_CTC = 2 /* the same with the CTC rule for repeated labels (Sec. II-C)             */
 };
 
+enum pb_dtype { PB_F32 = 0, PB_F16 = 1, PB_BF16 = 2 }; /* element type of logits and of their gradient */
+
+enum pb_distill_mode {
+  PB_DISTILL_RENORM = 0, /* the teacher's probabilities are those of its entries, scaled to sum to 1    */
+  PB_DISTILL_TAIL = 1    /* the entries are log-probs over the whole vocabulary; what they leave of 1 is
+                            one more class, held against the student's mass on all other tokens         */
+};
+
 typedef struct {
   int32_t vocab_size;         /* V > 0                                                                  */
   int32_t blank_id;           /* in [0, V), or -1 for a blank-free vocabulary                           */
@@ -296,6 +304,79 @@ int pb_fuse_step_beam_forest(const pb_forest* forest, const float* d_logp, int64
                              const int32_t* d_tree_ids, const float* d_hyp_scores, const int32_t* d_states_in,
                              float alpha, int32_t U, int32_t K, int32_t* d_tokens, int32_t* d_parents,
                              int32_t* d_states_out, float* d_scores_out, void* hip_stream);
+
+/*
+ * Rows of logits before and after the tree: how sure a model was of the tokens a decoder emitted, what else it had in
+ * mind, and the two losses that train on such lists.  Not in the paper.  These calls need no tree.
+ *   d_logits: rows x V elements of `dtype` (enum pb_dtype), row r at d_logits + r * row_stride elements (row_stride >= V),
+ *   at any alignment of its elements.  Log-probs of the decoders above are logits as well.  Arithmetic is fp32 for every
+ *   type.  With z_j = x_j / temperature:
+ *     log p(t) = z_t - log sum_j exp(z_j),   p_j = exp(log p(j)),   H = -sum_j p_j log p(j)   (p_j = 0 adds nothing).
+ *   A logit of -inf is a masked token (p = 0).  A row of nothing but -inf has log p = -inf, H = 0 and gradient 0.  A row
+ *   that holds a NaN or +inf is marked: NaN scores, -1 ids.  A token id outside [0, V) is absent: see each call.
+ *   The calls take the device that is current and d_logits lies on; they allocate nothing, synchronise nothing and may be
+ *   captured.  `d_workspace`: device memory of at least ..._workspace_bytes(...) bytes, 16-byte aligned, used only during
+ *   the call (contents before and after mean nothing; calls that may overlap in time, two graphs among them, need one each);
+ *   null where that is 0.  The size functions return PB_EINVAL, PB_EUNSUPPORTED as the call itself would.
+ *   PB_EINVAL: rows < 0, V < 1, an unknown dtype or mode, a stride below V, a pointer that is null but needed or not aligned
+ *   to its elements, nothing to write, a workspace that is null, too small or misaligned when one is needed.  PB_ERANGE: a
+ *   temperature outside [1e-4, 1e4].  PB_EUNSUPPORTED: V > 524288, or more than 64 tokens, alternatives or entries a row.
+ *   rows == 0 is a no-op.  Outputs are contiguous and lie apart from the inputs, except where a gradient takes the place of
+ *   the logits.  Results do not depend on other rows of the call and are the same bits every time.
+ *
+ * pb_token_logprobs -- any of, for every row:
+ *   d_logp[rows, n_tokens]       log p of the tokens d_tokens[rows, n_tokens] (NaN for an id outside [0, V)); null, with
+ *                                d_tokens, if and only if n_tokens == 0
+ *   d_entropy[rows]              H; may be null
+ *   d_top_tokens, d_top_logp     [rows, n_top]: the n_top <= V tokens that come first by (logit descending, id ascending)
+ *                                and their log p, in that order; null if and only if n_top == 0
+ *   d_stats[rows, 3]             what pb_token_logprobs_backward needs: max_j x_j, log sum_j exp(z_j - max z), H (-inf, 0, 0
+ *                                for a row of nothing but -inf); may be null
+ */
+int64_t pb_token_logprobs_workspace_bytes(int32_t dtype, int32_t rows, int32_t vocab_size, int32_t n_top);
+int pb_token_logprobs(const void* d_logits, int32_t dtype, int64_t row_stride, int32_t rows, int32_t vocab_size,
+                      float temperature, const int32_t* d_tokens, int32_t n_tokens, int32_t n_top, float* d_logp,
+                      float* d_entropy, int32_t* d_top_tokens, float* d_top_logp, float* d_stats, void* d_workspace,
+                      int64_t workspace_bytes, void* hip_stream);
+
+/*
+ * pb_token_logprobs_backward -- gradient of sum_k g_k log p(t_k) + h H of every row, g = d_grad_logp[rows, n_tokens],
+ * h = d_grad_entropy[rows] (either may be null: 0; both: PB_EINVAL), from the logits and the d_stats that
+ * pb_token_logprobs left for the same rows and temperature:
+ *     d_grad_logits[r * grad_stride + j] = (sum_k g_k ([j = t_k] - p_j) - h p_j (log p(j) + H)) / temperature
+ *   in the logits' type, rounded once.  A token id outside [0, V) takes no gradient and its g is not looked at; the same
+ *   token several times adds up.  A row whose incoming gradients are all 0 gets zeros, whatever it holds (padding).
+ *   n_tokens == 0 with null d_tokens and d_grad_logp: the entropy alone.  d_grad_logits may be d_logits with the same stride.
+ */
+int pb_token_logprobs_backward(const void* d_logits, int32_t dtype, int64_t row_stride, int32_t rows, int32_t vocab_size,
+                               float temperature, const float* d_stats, const int32_t* d_tokens, int32_t n_tokens,
+                               const float* d_grad_logp, const float* d_grad_entropy, void* d_grad_logits,
+                               int64_t grad_stride, void* hip_stream);
+
+/*
+ * pb_distill_topk -- distillation from the alternatives that were kept of a teacher (for instance of boosted rows, by
+ * pb_token_logprobs at the same temperature): K tokens t_k = d_teacher_tokens[rows, K] and values l_k = d_teacher_logp of
+ * every row, against the student's p over all V tokens.
+ *   PB_DISTILL_RENORM  q = softmax(l):   L = sum_k q_k (log q_k - log p(t_k))
+ *   PB_DISTILL_TAIL    q_k = exp(l_k), q' = 1 - sum_k q_k, p' = sum of p_j over the tokens not listed:
+ *                      L = sum_k q_k (log q_k - log p(t_k)) + q' (log q' - log p')
+ *                      (q' below 2^-20 counts as 0: fp32 log-probs of whole rows do not add up to 1 more exactly, and a
+ *                      list that holds all that a mask has left must not have its rounding held against no mass at all)
+ *   d_loss[rows] = L, and the gradient of w L with w = d_row_grads[r] (null: 1) in the logits' type, rounded once:
+ *     d_grad_logits[r * grad_stride + j] = w / temperature * ((sum_k q_k + q') p_j - sum over t_k = j of q_k
+ *                                                             - [j not listed] q' p_j / p')
+ *   Either output may be null, not both: loss and gradient in one call where the weights of the rows are known, the loss
+ *   first and the gradient of the same inputs when they are.  (No factor temperature^2: it belongs in the weights.)
+ *   An id outside [0, V) is an absent entry (lists may be shorter than K); a token listed twice counts with the sum of its
+ *   q; p' below the smallest normal fp32 number counts as 0.  A row without entries (or, PB_DISTILL_RENORM, with none above -inf) has loss 0 and gradient 0, whatever it holds; a
+ *   row of weight 0 has gradient 0.  Where q is positive and p is 0 the loss is +inf, the gradient finite; a student's row of
+ *   nothing but -inf has gradient 0.  1 <= K <= 64.  d_grad_logits may be d_logits with the same stride.
+ */
+int64_t pb_distill_topk_workspace_bytes(int32_t dtype, int32_t rows, int32_t vocab_size, int32_t K);
+int pb_distill_topk(const void* d_logits, int32_t dtype, int64_t row_stride, int32_t rows, int32_t vocab_size,
+                    float temperature, const int32_t* d_teacher_tokens, const float* d_teacher_logp, int32_t K, int32_t mode,
+                    const float* d_row_grads, float* d_loss, void* d_grad_logits, int64_t grad_stride, void* d_workspace,
+                    int64_t workspace_bytes, void* hip_stream);
 
 /*
  * pb_validate -- debug aid (host-side, O(N + V)): bounds-checks every index the kernels follow in the compiled

@@ -17,13 +17,16 @@ from . import build as _build
 PB_OK, PB_EINVAL, PB_ERANGE, PB_ENOMEM, PB_EHIP, PB_EUNSUPPORTED = 0, -1, -2, -3, -4, -5
 PB_W_UNIFORM, PB_W_LOGDEPTH, PB_W_UNIFORM_FINAL = 0, 1, 2
 PB_SELECT_FUSED, PB_SELECT_TWO_STAGE, PB_SELECT_TWO_STAGE_CTC = 0, 1, 2
+PB_F32, PB_F16, PB_BF16 = 0, 1, 2
+PB_DISTILL_RENORM, PB_DISTILL_TAIL = 0, 1
 
 EXPORTS = ["pb_build", "pb_free", "pb_info", "pb_host_arrays", "pb_state_prefix", "pb_score", "pb_fuse_step",
            "pb_fuse_frames", "pb_fuse_step_select", "pb_fuse_frames_select", "pb_fuse_frames_plan",
            "pb_fuse_frames_workspace_bytes",
            "pb_fuse_frames_ws", "pb_fuse_frames_static", "pb_fuse_step_beam", "pb_forest_build", "pb_forest_free", "pb_score_forest",
            "pb_fuse_step_forest", "pb_fuse_frames_forest", "pb_fuse_step_beam_forest", "pb_validate",
-           "pb_validate_states", "pb_strerror"]
+           "pb_validate_states", "pb_strerror", "pb_token_logprobs", "pb_token_logprobs_workspace_bytes",
+           "pb_token_logprobs_backward", "pb_distill_topk", "pb_distill_topk_workspace_bytes"]
 
 
 class PbError(RuntimeError):
@@ -57,8 +60,10 @@ class pb_host_view(C.Structure):
 HOT = ["pb_score", "pb_fuse_step", "pb_fuse_frames", "pb_fuse_step_select", "pb_fuse_frames_select", "pb_fuse_frames_ws",
        "pb_fuse_frames_static", "pb_fuse_step_beam", "pb_score_forest", "pb_fuse_step_forest", "pb_fuse_frames_forest",
        "pb_fuse_step_beam_forest"]  # called once per decoding step: they go through _pbcall (see pb_python.cpp)
+ROW_CALLS = ["pb_token_logprobs", "pb_token_logprobs_backward", "pb_distill_topk"]  # the same without a handle
 
 _lib = None
+_rows = None  # the ROW_CALLS, like _hot
 _hot = None  # the HOT entry points, taking device buffers as they come and returning a status code
 
 
@@ -132,10 +137,33 @@ def load():
     lib.pb_validate_states.argtypes = [vp, i32p, C.c_int64, i64p]
     lib.pb_strerror.restype = C.c_char_p
     lib.pb_strerror.argtypes = [C.c_int]
-    global _hot
+    i32, i64, f32 = C.c_int32, C.c_int64, C.c_float
+    lib.pb_token_logprobs_workspace_bytes.restype = i64
+    lib.pb_token_logprobs_workspace_bytes.argtypes = [i32, i32, i32, i32]
+    lib.pb_token_logprobs.restype = C.c_int
+    lib.pb_token_logprobs.argtypes = [vp, i32, i64, i32, i32, f32, vp, i32, i32, vp, vp, vp, vp, vp, vp, i64, vp]
+    lib.pb_token_logprobs_backward.restype = C.c_int
+    lib.pb_token_logprobs_backward.argtypes = [vp, i32, i64, i32, i32, f32, vp, vp, i32, vp, vp, vp, i64, vp]
+    lib.pb_distill_topk_workspace_bytes.restype = i64
+    lib.pb_distill_topk_workspace_bytes.argtypes = [i32, i32, i32, i32]
+    lib.pb_distill_topk.restype = C.c_int
+    lib.pb_distill_topk.argtypes = [vp, i32, i64, i32, i32, f32, vp, vp, i32, i32, vp, vp, vp, i64, vp, i64, vp]
+    global _hot, _rows
     _hot = _bind_hot(lib)
+    _rows = _bind_rows(lib)
     _lib = lib
     return lib
+
+
+def _bind_rows(lib):
+    calls = _CtypesCalls(lib, ROW_CALLS, 0)
+    try:
+        from . import _pbcall
+        for name in ROW_CALLS:
+            _pbcall.bind(name, C.cast(getattr(lib, name), C.c_void_p).value, getattr(calls, name))
+    except (ImportError, ValueError):  # not built (_bind_hot has said so), or built before these calls were there
+        return calls
+    return _pbcall
 
 
 def _bind_hot(lib):
@@ -153,15 +181,15 @@ def _bind_hot(lib):
 
 class _CtypesCalls:
     """The same calls through ctypes: where the extension module has not been built, and for arguments it leaves alone.
-    The first argument is the handle, the last the stream; the other pointers are device buffers."""
+    The first `handles` pointers are handles, the last the stream; the others are device buffers."""
 
-    def __init__(self, lib):
-        for name in HOT:
-            setattr(self, name, self._call(getattr(lib, name)))
+    def __init__(self, lib, names=HOT, handles=1):
+        for name in names:
+            setattr(self, name, self._call(getattr(lib, name), handles))
 
     @staticmethod
-    def _call(fn):
-        buffers = [i for i, t in enumerate(fn.argtypes) if t is C.c_void_p][1:-1]
+    def _call(fn, handles):
+        buffers = [i for i, t in enumerate(fn.argtypes) if t is C.c_void_p][handles:-1]
 
         def call(*args):
             a = list(args)
@@ -405,3 +433,46 @@ def pb_fuse_step_beam_forest(forest: Forest, d_logp, row_stride: int, d_tree_ids
     _check((_hot or _load_hot()).pb_fuse_step_beam_forest(
         forest.handle, d_logp, row_stride, d_tree_ids, d_hyp_scores, d_states_in, alpha, U, K, d_tokens,
         d_parents, d_states_out, d_scores_out, stream), "pb_fuse_step_beam_forest")
+
+
+def _load_rows():
+    load()
+    return _rows
+
+
+def _bytes(n: int, where: str) -> int:
+    if n < 0:
+        raise PbError(n, where)
+    return n
+
+
+def pb_token_logprobs_workspace_bytes(dtype: int, rows: int, vocab_size: int, n_top: int) -> int:
+    return _bytes(int(load().pb_token_logprobs_workspace_bytes(dtype, rows, vocab_size, n_top)), "pb_token_logprobs_workspace_bytes")
+
+
+def pb_token_logprobs(d_logits, dtype: int, row_stride: int, rows: int, vocab_size: int, temperature: float, d_tokens,
+                      n_tokens: int, n_top: int, d_logp, d_entropy, d_top_tokens, d_top_logp, d_stats, d_workspace,
+                      workspace_bytes: int, stream: int = 0):
+    _check((_rows or _load_rows()).pb_token_logprobs(
+        d_logits, dtype, row_stride, rows, vocab_size, temperature, d_tokens, n_tokens, n_top, d_logp, d_entropy,
+        d_top_tokens, d_top_logp, d_stats, d_workspace, workspace_bytes, stream), "pb_token_logprobs")
+
+
+def pb_token_logprobs_backward(d_logits, dtype: int, row_stride: int, rows: int, vocab_size: int, temperature: float,
+                               d_stats, d_tokens, n_tokens: int, d_grad_logp, d_grad_entropy, d_grad_logits,
+                               grad_stride: int, stream: int = 0):
+    _check((_rows or _load_rows()).pb_token_logprobs_backward(
+        d_logits, dtype, row_stride, rows, vocab_size, temperature, d_stats, d_tokens, n_tokens, d_grad_logp,
+        d_grad_entropy, d_grad_logits, grad_stride, stream), "pb_token_logprobs_backward")
+
+
+def pb_distill_topk_workspace_bytes(dtype: int, rows: int, vocab_size: int, K: int) -> int:
+    return _bytes(int(load().pb_distill_topk_workspace_bytes(dtype, rows, vocab_size, K)), "pb_distill_topk_workspace_bytes")
+
+
+def pb_distill_topk(d_logits, dtype: int, row_stride: int, rows: int, vocab_size: int, temperature: float, d_teacher_tokens,
+                    d_teacher_logp, K: int, mode: int, d_row_grads, d_loss, d_grad_logits, grad_stride: int, d_workspace,
+                    workspace_bytes: int, stream: int = 0):
+    _check((_rows or _load_rows()).pb_distill_topk(
+        d_logits, dtype, row_stride, rows, vocab_size, temperature, d_teacher_tokens, d_teacher_logp, K, mode, d_row_grads,
+        d_loss, d_grad_logits, grad_stride, d_workspace, workspace_bytes, stream), "pb_distill_topk")

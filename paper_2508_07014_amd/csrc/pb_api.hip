@@ -13,6 +13,7 @@
 
 #include "pb.h"
 #include "pb_kernels.hpp"
+#include "pb_logits.hpp"
 #include "pb_tree.hpp"
 
 namespace {
@@ -521,6 +522,140 @@ int pb_fuse_step_beam_forest(const pb_forest* forest, const float* d_logp, int64
   const pb::TreePick pick{forest->d_table, d_tree_ids, forest->count};
   return launch_beam_step(forest->proto, pick, d_logp, row_stride, d_hyp_scores, d_states_in, alpha, U, K, d_tokens, d_parents,
                           d_states_out, d_scores_out, hip_stream);
+}
+
+}  // extern "C"
+
+namespace {
+
+int64_t element_bytes(int32_t dtype) { return dtype == PB_F32 ? 4 : 2; }
+bool aligned(const void* p, int64_t bytes) { return (reinterpret_cast<uintptr_t>(p) & static_cast<uintptr_t>(bytes - 1)) == 0; }
+
+// What all calls on rows of logits check of their shape, `most` the largest number of list entries a row.
+int check_logits(int32_t dtype, int32_t rows, int32_t V, int32_t most) {
+  if (dtype != PB_F32 && dtype != PB_F16 && dtype != PB_BF16) return PB_EINVAL;
+  if (rows < 0 || V < 1) return PB_EINVAL;
+  if (V > pb::kLogitsMaxV || most > pb::kMaxGiven) return PB_EUNSUPPORTED;
+  return PB_OK;
+}
+int check_temperature(float t) { return t >= 1e-4f && t <= 1e4f ? PB_OK : PB_ERANGE; }  // (false for NaN)
+int check_workspace(int64_t need, const void* d_workspace, int64_t bytes) {
+  return need > 0 && (!d_workspace || bytes < need || !aligned(d_workspace, 16)) ? PB_EINVAL : PB_OK;
+}
+
+template <typename T>
+void advance(T*& p, int64_t n) {
+  if (p) p += n;
+}
+pb::LogitRows rows_from(const pb::LogitRows& in, int32_t dtype, size_t at, int32_t n) {
+  pb::LogitRows r = in;
+  r.x = static_cast<const char*>(in.x) + static_cast<int64_t>(at) * in.stride * element_bytes(dtype);
+  r.rows = n;
+  return r;
+}
+
+}  // namespace
+
+extern "C" {
+
+int64_t pb_token_logprobs_workspace_bytes(int32_t dtype, int32_t rows, int32_t vocab_size, int32_t n_top) {
+  if (n_top < 0 || n_top > vocab_size) return PB_EINVAL;
+  const int rc = check_logits(dtype, rows, vocab_size, n_top);
+  return rc != PB_OK ? rc : 0;
+}
+
+int pb_token_logprobs(const void* d_logits, int32_t dtype, int64_t row_stride, int32_t rows, int32_t vocab_size,
+                      float temperature, const int32_t* d_tokens, int32_t n_tokens, int32_t n_top, float* d_logp,
+                      float* d_entropy, int32_t* d_top_tokens, float* d_top_logp, float* d_stats, void* d_workspace,
+                      int64_t workspace_bytes, void* hip_stream) {
+  if (n_tokens < 0 || n_top < 0 || n_top > vocab_size || workspace_bytes < 0) return PB_EINVAL;
+  int rc = check_logits(dtype, rows, vocab_size, std::max(n_tokens, n_top));
+  if (rc == PB_OK) rc = check_temperature(temperature);
+  if (rc != PB_OK) return rc;
+  if (row_stride < vocab_size) return PB_EINVAL;
+  if (n_tokens == 0 && n_top == 0 && !d_entropy && !d_stats) return PB_EINVAL;
+  if (rows == 0) return PB_OK;
+  if (!d_logits || !aligned(d_logits, element_bytes(dtype))) return PB_EINVAL;
+  if ((n_tokens > 0) != (d_tokens != nullptr) || (n_tokens > 0) != (d_logp != nullptr)) return PB_EINVAL;
+  if ((n_top > 0) != (d_top_tokens != nullptr) || (n_top > 0) != (d_top_logp != nullptr)) return PB_EINVAL;
+  for (const void* p : {static_cast<const void*>(d_tokens), static_cast<const void*>(d_logp), static_cast<const void*>(d_entropy),
+                        static_cast<const void*>(d_top_tokens), static_cast<const void*>(d_top_logp), static_cast<const void*>(d_stats)})
+    if (!aligned(p, 4)) return PB_EINVAL;
+  if (check_workspace(pb_token_logprobs_workspace_bytes(dtype, rows, vocab_size, n_top), d_workspace, workspace_bytes) != PB_OK) return PB_EINVAL;
+  pb::LogprobArgs a{{d_logits, row_stride, rows, vocab_size, 1.0f / temperature}, d_tokens, n_tokens, n_top, d_logp, d_entropy, d_top_tokens, d_top_logp, d_stats};
+  return in_slices(rows, pb::kMaxWorkgroups, [&](size_t at, int32_t n) {
+    pb::LogprobArgs s = a;
+    s.in = rows_from(a.in, dtype, at, n);
+    advance(s.tokens, at * n_tokens);
+    advance(s.logp, at * n_tokens);
+    advance(s.entropy, at);
+    advance(s.top_tokens, at * n_top);
+    advance(s.top_logp, at * n_top);
+    advance(s.stats, at * 3);
+    return pb::launch_token_logprobs(dtype, s, static_cast<hipStream_t>(hip_stream));
+  });
+}
+
+int pb_token_logprobs_backward(const void* d_logits, int32_t dtype, int64_t row_stride, int32_t rows, int32_t vocab_size,
+                               float temperature, const float* d_stats, const int32_t* d_tokens, int32_t n_tokens,
+                               const float* d_grad_logp, const float* d_grad_entropy, void* d_grad_logits,
+                               int64_t grad_stride, void* hip_stream) {
+  if (n_tokens < 0) return PB_EINVAL;
+  int rc = check_logits(dtype, rows, vocab_size, n_tokens);
+  if (rc == PB_OK) rc = check_temperature(temperature);
+  if (rc != PB_OK) return rc;
+  if (row_stride < vocab_size || grad_stride < vocab_size) return PB_EINVAL;
+  if (rows == 0) return PB_OK;
+  const int64_t es = element_bytes(dtype);
+  if (!d_logits || !d_stats || !d_grad_logits || !aligned(d_logits, es) || !aligned(d_grad_logits, es)) return PB_EINVAL;
+  if ((!d_grad_logp && !d_grad_entropy) || (n_tokens > 0) != (d_tokens != nullptr) || (d_grad_logp && n_tokens == 0)) return PB_EINVAL;
+  if (!aligned(d_stats, 4) || !aligned(d_tokens, 4) || !aligned(d_grad_logp, 4) || !aligned(d_grad_entropy, 4)) return PB_EINVAL;
+  if (d_grad_logits == d_logits && grad_stride != row_stride) return PB_EINVAL;
+  pb::LogprobGradArgs a{{d_logits, row_stride, rows, vocab_size, 1.0f / temperature}, d_stats, d_tokens, n_tokens, d_grad_logp, d_grad_entropy, d_grad_logits, grad_stride};
+  return in_slices(rows, pb::kMaxWorkgroups, [&](size_t at, int32_t n) {
+    pb::LogprobGradArgs s = a;
+    s.in = rows_from(a.in, dtype, at, n);
+    advance(s.stats, at * 3);
+    advance(s.tokens, at * n_tokens);
+    advance(s.grad_logp, at * n_tokens);
+    advance(s.grad_entropy, at);
+    s.grad = static_cast<char*>(a.grad) + static_cast<int64_t>(at) * grad_stride * es;
+    return pb::launch_token_logprobs_backward(dtype, s, static_cast<hipStream_t>(hip_stream));
+  });
+}
+
+int64_t pb_distill_topk_workspace_bytes(int32_t dtype, int32_t rows, int32_t vocab_size, int32_t K) {
+  if (K < 1) return PB_EINVAL;
+  const int rc = check_logits(dtype, rows, vocab_size, K);
+  return rc != PB_OK ? rc : 0;
+}
+
+int pb_distill_topk(const void* d_logits, int32_t dtype, int64_t row_stride, int32_t rows, int32_t vocab_size,
+                    float temperature, const int32_t* d_teacher_tokens, const float* d_teacher_logp, int32_t K, int32_t mode,
+                    const float* d_row_grads, float* d_loss, void* d_grad_logits, int64_t grad_stride, void* d_workspace,
+                    int64_t workspace_bytes, void* hip_stream) {
+  if (K < 1 || workspace_bytes < 0 || (mode != PB_DISTILL_RENORM && mode != PB_DISTILL_TAIL)) return PB_EINVAL;
+  int rc = check_logits(dtype, rows, vocab_size, K);
+  if (rc == PB_OK) rc = check_temperature(temperature);
+  if (rc != PB_OK) return rc;
+  if (row_stride < vocab_size || (d_grad_logits && grad_stride < vocab_size) || (!d_loss && !d_grad_logits)) return PB_EINVAL;
+  if (rows == 0) return PB_OK;
+  const int64_t es = element_bytes(dtype);
+  if (!d_logits || !d_teacher_tokens || !d_teacher_logp || !aligned(d_logits, es) || !aligned(d_grad_logits, es)) return PB_EINVAL;
+  if (!aligned(d_teacher_tokens, 4) || !aligned(d_teacher_logp, 4) || !aligned(d_row_grads, 4) || !aligned(d_loss, 4)) return PB_EINVAL;
+  if (d_grad_logits == d_logits && grad_stride != row_stride) return PB_EINVAL;
+  if (check_workspace(pb_distill_topk_workspace_bytes(dtype, rows, vocab_size, K), d_workspace, workspace_bytes) != PB_OK) return PB_EINVAL;
+  pb::DistillArgs a{{d_logits, row_stride, rows, vocab_size, 1.0f / temperature}, d_teacher_tokens, d_teacher_logp, K, mode == PB_DISTILL_TAIL, d_row_grads, d_loss, d_grad_logits, grad_stride};
+  return in_slices(rows, pb::kMaxWorkgroups, [&](size_t at, int32_t n) {
+    pb::DistillArgs s = a;
+    s.in = rows_from(a.in, dtype, at, n);
+    advance(s.tokens, at * K);
+    advance(s.logp, at * K);
+    advance(s.row_grads, at);
+    advance(s.loss, at);
+    if (a.grad) s.grad = static_cast<char*>(a.grad) + static_cast<int64_t>(at) * grad_stride * es;
+    return pb::launch_distill_topk(dtype, s, static_cast<hipStream_t>(hip_stream));
+  });
 }
 
 int pb_validate(const pb_tree* tree) {
