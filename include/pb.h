@@ -320,9 +320,10 @@ int pb_fuse_step_beam_forest(const pb_forest* forest, const float* d_logp, int64
  *   null where that is 0.  The size functions return PB_EINVAL, PB_EUNSUPPORTED as the call itself would.
  *   PB_EINVAL: rows < 0, V < 1, an unknown dtype or mode, a stride below V, a pointer that is null but needed or not aligned
  *   to its elements, nothing to write, a workspace that is null, too small or misaligned when one is needed.  PB_ERANGE: a
- *   temperature outside [1e-4, 1e4].  PB_EUNSUPPORTED: V > 524288, or more than 64 tokens, alternatives or entries a row.
+ *   temperature outside [1e-4, 1e4].  PB_EUNSUPPORTED: V > 393216, or more than 64 tokens, alternatives or entries a row.
  *   rows == 0 is a no-op.  Outputs are contiguous and lie apart from the inputs, except where a gradient takes the place of
- *   the logits.  Results do not depend on other rows of the call and are the same bits every time.
+ *   the logits.  A call gives the same bits every time; the order of its sums depends on the shape of the call and on the
+ *   alignment of a row, not on what other rows hold.
  *
  * pb_token_logprobs -- any of, for every row:
  *   d_logp[rows, n_tokens]       log p of the tokens d_tokens[rows, n_tokens] (NaN for an id outside [0, V)); null, with

@@ -561,7 +561,7 @@ extern "C" {
 int64_t pb_token_logprobs_workspace_bytes(int32_t dtype, int32_t rows, int32_t vocab_size, int32_t n_top) {
   if (n_top < 0 || n_top > vocab_size) return PB_EINVAL;
   const int rc = check_logits(dtype, rows, vocab_size, n_top);
-  return rc != PB_OK ? rc : 0;
+  return rc != PB_OK ? rc : pb::token_logprobs_workspace(dtype, rows, vocab_size);
 }
 
 int pb_token_logprobs(const void* d_logits, int32_t dtype, int64_t row_stride, int32_t rows, int32_t vocab_size,
@@ -592,7 +592,7 @@ int pb_token_logprobs(const void* d_logits, int32_t dtype, int64_t row_stride, i
     advance(s.top_tokens, at * n_top);
     advance(s.top_logp, at * n_top);
     advance(s.stats, at * 3);
-    return pb::launch_token_logprobs(dtype, s, static_cast<hipStream_t>(hip_stream));
+    return pb::launch_token_logprobs(dtype, s, d_workspace, static_cast<hipStream_t>(hip_stream));
   });
 }
 
@@ -612,7 +612,8 @@ int pb_token_logprobs_backward(const void* d_logits, int32_t dtype, int64_t row_
   if (!aligned(d_stats, 4) || !aligned(d_tokens, 4) || !aligned(d_grad_logp, 4) || !aligned(d_grad_entropy, 4)) return PB_EINVAL;
   if (d_grad_logits == d_logits && grad_stride != row_stride) return PB_EINVAL;
   pb::LogprobGradArgs a{{d_logits, row_stride, rows, vocab_size, 1.0f / temperature}, d_stats, d_tokens, n_tokens, d_grad_logp, d_grad_entropy, d_grad_logits, grad_stride};
-  return in_slices(rows, pb::kMaxWorkgroups, [&](size_t at, int32_t n) {
+  // (a workgroup per 4096 fp32 or 8192 other elements of a row, see pb_logprobs.hip)
+  return in_slices(rows, pb::kMaxWorkgroups / (1 + vocab_size / 4096), [&](size_t at, int32_t n) {
     pb::LogprobGradArgs s = a;
     s.in = rows_from(a.in, dtype, at, n);
     advance(s.stats, at * 3);
@@ -627,7 +628,7 @@ int pb_token_logprobs_backward(const void* d_logits, int32_t dtype, int64_t row_
 int64_t pb_distill_topk_workspace_bytes(int32_t dtype, int32_t rows, int32_t vocab_size, int32_t K) {
   if (K < 1) return PB_EINVAL;
   const int rc = check_logits(dtype, rows, vocab_size, K);
-  return rc != PB_OK ? rc : 0;
+  return rc != PB_OK ? rc : pb::distill_topk_workspace(dtype, rows, vocab_size);
 }
 
 int pb_distill_topk(const void* d_logits, int32_t dtype, int64_t row_stride, int32_t rows, int32_t vocab_size,
@@ -654,7 +655,7 @@ int pb_distill_topk(const void* d_logits, int32_t dtype, int64_t row_stride, int
     advance(s.row_grads, at);
     advance(s.loss, at);
     if (a.grad) s.grad = static_cast<char*>(a.grad) + static_cast<int64_t>(at) * grad_stride * es;
-    return pb::launch_distill_topk(dtype, s, static_cast<hipStream_t>(hip_stream));
+    return pb::launch_distill_topk(dtype, s, d_workspace, static_cast<hipStream_t>(hip_stream));
   });
 }
 

@@ -1,0 +1,424 @@
+// pb_distill_topk (gfx950): the loss and the gradient of a row in one go, the row held in registers between the two.
+#include <hip/hip_runtime.h>
+
+#include "pb_kernels.hpp"
+#include "pb_logit_rows.hpp"
+
+namespace pb {
+namespace lr {
+namespace {
+
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double dpp_add(double v) {
+  const long long b = __double_as_longlong(v);
+  const unsigned lo = static_cast<unsigned>(__builtin_amdgcn_update_dpp(0, static_cast<int>(b), CTRL, ROWS, 0xf, false));
+  const unsigned hi = static_cast<unsigned>(__builtin_amdgcn_update_dpp(0, static_cast<int>(b >> 32), CTRL, ROWS, 0xf, false));
+  return v + __longlong_as_double((static_cast<long long>(hi) << 32) | lo);
+}
+__device__ __forceinline__ double wave_sum(double v) {
+  v = dpp_add<0x111, 0xf>(v);
+  v = dpp_add<0x112, 0xf>(v);
+  v = dpp_add<0x114, 0xf>(v);
+  v = dpp_add<0x118, 0xf>(v);
+  v = dpp_add<0x142, 0xa>(v);
+  v = dpp_add<0x143, 0xc>(v);
+  const long long b = __double_as_longlong(v);
+  const unsigned lo = __builtin_amdgcn_readlane(static_cast<int>(b), 63), hi = __builtin_amdgcn_readlane(static_cast<int>(b >> 32), 63);
+  return __longlong_as_double((static_cast<long long>(hi) << 32) | lo);
+}
+
+// The teacher's list of a row, an entry a lane.
+struct Entry {
+  int token;    // -1: absent
+  float x;      // the student's logit
+  float log_q, q;
+};
+struct List {   // the same in every lane
+  float rest;   // what the entries leave of 1
+  float Q;      // sum of q and rest
+  float shift;  // log q = l - shift
+  int any;      // there is something to learn from
+};
+template <typename E, bool TAIL>
+__device__ __forceinline__ List load_list(const DistillArgs& a, int64_t r, const Row<E>& row, int lane, Entry& e) {
+  e = Entry{-1, 0.0f, -INFINITY, 0.0f};
+  if (lane < a.K) {
+    const int t = a.tokens[r * a.K + lane];
+    if (static_cast<unsigned>(t) < static_cast<unsigned>(row.V)) {
+      e.token = t;
+      e.x = E::up(row.x[t]);
+      e.log_q = a.logp[r * a.K + lane];
+    }
+  }
+  List l;
+  if constexpr (TAIL) {
+    // (1 - sum q in 64 bits: where the list holds nearly everything, fp32 would leave nothing of it)
+    const double q = exp(static_cast<double>(e.log_q)), left = 1.0 - wave_sum(q);
+    e.q = static_cast<float>(q);
+    l.rest = left < 0x1p-20 ? 0.0f : static_cast<float>(left);  // (NaN stays)
+    l.any = __ballot(e.token >= 0) != 0 ? 1 : 0;
+    l.shift = 0.0f;
+  } else {
+    const float top = wave_max(e.log_q);
+    l.any = top != -INFINITY ? 1 : 0;
+    const float part = e.token >= 0 ? exp2_fast((e.log_q - (l.any ? top : 0.0f)) * kLog2e) : 0.0f;
+    const float sum = wave_sum(part);
+    l.rest = 0.0f;
+    l.shift = top + logf(sum);
+    e.log_q -= l.shift;
+    e.q = part / sum;
+  }
+  l.Q = wave_sum(e.q) + l.rest;
+  return l;
+}
+
+struct Student {
+  float S;       // sum over all tokens
+  float p_rest;  // what the student leaves to the tokens that are not listed
+  float A;       // their gradient, a unit of exp((x - base) / T)
+};
+template <bool TAIL>
+__device__ __forceinline__ Student student(const RowSums& sums, const List& list, float w, float inv) {
+  Student s{TAIL ? sums.S + sums.X : sums.S, 0.0f, 0.0f};
+  float share = list.Q;
+  if constexpr (TAIL) {
+    s.p_rest = sums.m == -INFINITY ? 0.0f : sums.S / s.S;
+    if (s.p_rest < 0x1p-126f) s.p_rest = 0.0f;  // (NaN stays)
+    if (list.rest > 0.0f && s.p_rest > 0.0f) share -= list.rest / s.p_rest;
+  }
+  s.A = share * w * inv / s.S;
+  return s;
+}
+// By one wave: the row's loss, and the gradient on the lane's listed token.
+template <bool TAIL>
+__device__ __forceinline__ float loss_and_own(const DistillArgs& a, int64_t r, int lane, const Entry& e, const List& list, const RowSums& sums,
+                                              const Student& st, float w, float inv) {
+  // (terms that cancel, and log-probs of masked tokens that may pass the fp32 range: in 64 bits)
+  const double lp = (static_cast<double>(e.x) - sums.base) * inv - (sums.m == -INFINITY ? 0.0 : log(static_cast<double>(st.S)));
+  if (a.loss) {
+    double loss = wave_sum(e.q > 0.0f ? e.q * (e.log_q - lp) : static_cast<double>(e.q));  // (0, or NaN)
+    if (TAIL && list.rest != 0.0f) loss += list.rest * static_cast<double>(logf(list.rest / st.p_rest));
+    if (lane == 0) a.loss[r] = sums.bad ? NAN : static_cast<float>(loss);
+  }
+  float mass = 0.0f;  // (a token may be listed more than once)
+  for (int k = 0; k < a.K; ++k)
+    if (__builtin_amdgcn_readlane(e.token, k) == e.token) mass += __int_as_float(__builtin_amdgcn_readlane(__float_as_int(e.q), k));
+  return (expf(static_cast<float>(lp)) * list.Q - mass) * w * inv;
+}
+
+// One row, by a wave (four rows a workgroup) or a workgroup.  Thread t holds vectors t, t + NT, ... of the row, HELD of them
+// in registers; what a row has beyond HELD * NT vectors is read a second time for the gradient (from cache: only the rows
+// at work are in between).  With TAIL the tokens that are not listed have a sum of their own, so that little mass does not
+// vanish in a difference: bits in LDS say which elements are listed, and most vectors have none.
+template <typename E, int NT, int HELD, bool TAIL>
+__global__ __launch_bounds__(NT == 64 ? 256 : NT) void distill_kernel(DistillArgs a, int mark_bytes) {
+  constexpr int ROWS = NT == 64 ? 4 : 1, SECOND = TAIL ? kListed : kAlone;
+  extern __shared__ __align__(16) unsigned char s_all[];
+  __shared__ float s_sums[ROWS][3 * NT / 64];
+  __shared__ List s_list;
+  __shared__ unsigned s_edge[ROWS];
+  const int sub = NT == 64 ? uniform_i(threadIdx.x >> 6) : 0, tid = NT == 64 ? threadIdx.x & 63 : threadIdx.x;
+  const int64_t r = static_cast<int64_t>(blockIdx.x) * ROWS + sub;
+  if (ROWS > 1 && r >= a.in.rows) return;
+  const Row<E> row = row_at<E>(a.in.x, a.in.stride, r, a.in.V);
+  unsigned char* marks = s_all + sub * mark_bytes;
+  v4u held[HELD];  // (behind the row's end: its last vector again; loads under conditions took 230 registers instead of 50)
+  if (row.nv > 0) {
+#pragma unroll
+    for (int u = 0; u < HELD; ++u) held[u] = row.vec(min(u * NT + tid, row.nv - 1));
+  }
+  float edge = -INFINITY;
+  if (tid < row.edges) edge = E::up(row.x[row.edge_token(tid)]);
+  const float w = a.row_grads ? a.row_grads[r] : 1.0f, inv = a.in.inv_temp, c = inv * kLog2e, room = kRoom / c;
+  const bool lister = NT == 64 || tid < 64;
+  if constexpr (TAIL) {
+    for (int i = tid; i < mark_bytes / 4; i += NT) reinterpret_cast<unsigned*>(marks)[i] = 0u;
+    if (tid == 0) s_edge[sub] = 0u;
+  }
+  Entry e{-1, 0.0f, 0.0f, 0.0f};
+  List list{0.0f, 0.0f, 0.0f, 0};
+  if (lister) list = load_list<E, TAIL>(a, r, row, tid & 63, e);
+  if constexpr (NT > 64) {
+    if (tid == 0) s_list = list;
+  }
+  if constexpr (TAIL || NT > 64) row_sync<NT>();
+  if constexpr (NT > 64) list = s_list;
+  if constexpr (TAIL) {
+    if (lister && e.token >= 0) {
+      const int at = e.token - row.head, v = at / E::N;
+      if (at < 0 || v >= row.nv) {
+        atomicOr(&s_edge[sub], 1u << (at < 0 ? e.token : e.token - row.nv * E::N));
+      } else {
+        atomicOr(&reinterpret_cast<unsigned*>(marks)[at >> 5], 1u << (at & 31));
+      }
+    }
+    row_sync<NT>();
+  }
+  typename E::type* out = a.grad ? static_cast<typename E::type*>(a.grad) + r * a.grad_stride : nullptr;
+  auto zeros = [&] {
+    const v4u z = {0u, 0u, 0u, 0u};
+    for (int v = tid; v < row.nv; v += NT) store_vector<E>(out + row.token(v, 0), z);
+    if (tid < row.edges) out[row.edge_token(tid)] = E::down(0.0f);
+  };
+  if (!uniform_i(list.any)) {
+    if (a.loss && tid == 0) a.loss[r] = 0.0f;
+    if (out) zeros();
+    return;
+  }
+  Sums s(kFar / c);
+  auto listed = [&](int v) -> unsigned { return !TAIL ? 0u : E::N == 8 ? marks[v] : (marks[v >> 1] >> (4 * (v & 1))) & 15u; };
+  auto edge_listed = [&](int t) -> bool { return TAIL && ((s_edge[sub] >> t) & 1u); };
+  auto one = [&](const v4u& raw, int v) {
+    float x[E::N];
+    E::unpack(raw, x);
+    const float vm = vec_max(x);
+    s.m = fmaxf(s.m, vm);
+    add_vector<SECOND>(s, x, vm, c, room, listed(v));
+  };
+#pragma unroll
+  for (int u = 0; u < HELD; ++u)
+    if (u * NT + tid < row.nv) one(held[u], u * NT + tid);
+  for (int v = HELD * NT + tid; v < row.nv; v += NT) one(row.vec(v), v);
+  if (tid < row.edges) {
+    const float x[1] = {edge};
+    s.m = fmaxf(s.m, edge);
+    add_vector<SECOND>(s, x, edge, c, room, edge_listed(tid) ? 1u : 0u);
+  }
+  const Part part = wave_part<SECOND>(s, c, [&](auto&& add) {
+    for (int v = tid; v < row.nv; v += NT) {
+      float x[E::N];
+      E::unpack(row.vec(v), x);
+      const unsigned on = listed(v);
+#pragma unroll
+      for (int i = 0; i < E::N; ++i) add(x[i], (on >> i) & 1u);
+    }
+    if (tid < row.edges) add(edge, edge_listed(tid));
+  });
+  const RowSums sums = join_waves<NT, SECOND>(part, tid, c, s_sums[sub]);
+  const bool empty = sums.m == -INFINITY;
+  const Student st = student<TAIL>(sums, list, w, inv);
+  float own = 0.0f;  // the gradient of the lane's listed token
+  if (lister) own = loss_and_own<TAIL>(a, r, tid, e, list, sums, st, w, inv);
+  if (!out) return;
+  if (empty || w == 0.0f) {
+    if constexpr (NT > 64) __syncthreads();  // (the gradient may take the logits' place: all of them have been read)
+    zeros();
+    return;
+  }
+  auto grad = [&](float x) { return exp2_fast((x - sums.base) * c) * st.A; };
+  auto put = [&](const v4u& raw, int v) {
+    float x[E::N];
+    E::unpack(raw, x);
+#pragma unroll
+    for (int i = 0; i < E::N; ++i) x[i] = grad(x[i]);
+    store_vector<E>(out + row.token(v, 0), E::pack(x));
+  };
+  if constexpr (NT > 64) __syncthreads();
+#pragma unroll
+  for (int u = 0; u < HELD; ++u) asm volatile("" : "+v"(held[u]));  // (unpacked again, not kept unpacked: 80 registers -> 50)
+#pragma unroll
+  for (int u = 0; u < HELD; ++u)
+    if (u * NT + tid < row.nv) put(held[u], u * NT + tid);
+  for (int v = HELD * NT + tid; v < row.nv; v += NT) put(row.vec(v), v);
+  if (tid < row.edges) out[row.edge_token(tid)] = E::down(grad(edge));
+  row_sync<NT>();
+  if (lister && e.token >= 0) out[e.token] = E::down(own);
+}
+
+// Few long rows, and rows too long for the registers of a workgroup: every wave takes 64 * `each` vectors of a row and
+// leaves their part of the sums in the workspace (the first one also the list's, and the student's logits on it, since the
+// gradient may take the logits' place); the second kernel joins the parts and writes the gradient.
+struct DistillSpace {
+  float4* parts;  // [rows, parts]
+  List* lists;    // [rows]
+  float* x;       // [rows, 64]
+};
+template <typename E, bool TAIL>
+__global__ __launch_bounds__(256) void distill_parts_kernel(DistillArgs a, int parts, int each, DistillSpace ws) {
+  constexpr int SECOND = TAIL ? kListed : kAlone;
+  __shared__ unsigned s_marks[4][64 * kMaxEach / 4];  // a byte per vector
+  __shared__ unsigned s_edge[4];
+  const int sub = uniform_i(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int64_t at = static_cast<int64_t>(blockIdx.x) * 4 + sub;
+  const int64_t r = at / parts;
+  if (r >= a.in.rows) return;
+  const int begin = static_cast<int>(at - r * parts) * 64 * each;
+  const Row<E> row = row_at<E>(a.in.x, a.in.stride, r, a.in.V);
+  const float c = a.in.inv_temp * kLog2e, room = kRoom / c;
+  const int end = min(begin + 64 * each, row.nv);
+  if (begin == 0) {
+    Entry e;
+    const List l = load_list<E, TAIL>(a, r, row, lane, e);
+    if (lane == 0) ws.lists[r] = l;
+    ws.x[r * 64 + lane] = e.x;
+  }
+  if constexpr (TAIL) {
+    if (lane < 16 * each) s_marks[sub][lane] = 0u;
+    if (16 * each > 64 && lane < 16 * each - 64) s_marks[sub][64 + lane] = 0u;
+    if (lane == 0) s_edge[sub] = 0u;
+    row_sync<64>();
+    if (lane < a.K) {
+      const int t = a.tokens[r * a.K + lane], e = t - row.head, v = e / E::N;
+      if (static_cast<unsigned>(t) < static_cast<unsigned>(a.in.V)) {
+        if (e < 0 || v >= row.nv)
+          atomicOr(&s_edge[sub], 1u << (e < 0 ? t : t - row.nv * E::N));
+        else if (v >= begin && v < end)
+          atomicOr(&s_marks[sub][(v - begin) >> 2], 1u << (8 * ((v - begin) & 3) + e % E::N));
+      }
+    }
+    row_sync<64>();
+  }
+  auto listed = [&](int v) -> unsigned { return TAIL ? reinterpret_cast<const unsigned char*>(s_marks[sub])[v - begin] : 0u; };
+  Sums s(kFar / c);
+  for (int v = begin + lane; v < end; v += 64) {
+    float x[E::N];
+    E::unpack(row.vec(v), x);
+    const float vm = vec_max(x);
+    s.m = fmaxf(s.m, vm);
+    add_vector<SECOND>(s, x, vm, c, room, listed(v));
+  }
+  const bool has_edge = begin == 0 && lane < row.edges;
+  const bool on_edge = TAIL && has_edge && ((s_edge[sub] >> lane) & 1u);
+  float edge = -INFINITY;
+  if (has_edge) {
+    edge = E::up(row.x[row.edge_token(lane)]);
+    const float x[1] = {edge};
+    s.m = fmaxf(s.m, edge);
+    add_vector<SECOND>(s, x, edge, c, room, on_edge ? 1u : 0u);
+  }
+  const Part p = wave_part<SECOND>(s, c, [&](auto&& add) {
+    for (int v = begin + lane; v < end; v += 64) {
+      float x[E::N];
+      E::unpack(row.vec(v), x);
+      const unsigned on = listed(v);
+#pragma unroll
+      for (int i = 0; i < E::N; ++i) add(x[i], (on >> i) & 1u);
+    }
+    if (has_edge) add(edge, on_edge);
+  });
+  if (lane == 0) ws.parts[at] = make_float4(p.m, p.S, p.X, 0.0f);
+}
+
+constexpr int kGradUnroll = 4;
+template <typename E, bool TAIL>
+__global__ __launch_bounds__(256) void distill_grad_kernel(DistillArgs a, int parts, int blocks, DistillSpace ws) {
+  constexpr int SECOND = TAIL ? kListed : kAlone, BLOCK = 256 * kGradUnroll;
+  const int64_t r = blockIdx.x / blocks;
+  const int block = blockIdx.x % blocks, tid = threadIdx.x, lane = tid & 63;
+  const Row<E> row = row_at<E>(a.in.x, a.in.stride, r, a.in.V);
+  typename E::type* out = a.grad ? static_cast<typename E::type*>(a.grad) + r * a.grad_stride : nullptr;
+  v4u raw[kGradUnroll];
+  if (out) {  // (a row behind its end: its last vector again)
+#pragma unroll
+    for (int u = 0; u < kGradUnroll; ++u) raw[u] = row.vec(min(block * BLOCK + u * 256 + tid, row.nv - 1));
+  }
+  const bool has_edge = block == 0 && tid < row.edges;
+  float edge = 0.0f;
+  if (has_edge) edge = E::up(row.x[row.edge_token(tid)]);
+  const float w = a.row_grads ? a.row_grads[r] : 1.0f, inv = a.in.inv_temp, c = inv * kLog2e;
+  const List list = ws.lists[r];
+  Part p{-INFINITY, 0.0f, 0.0f};
+#pragma unroll
+  for (int i = 0; i < kMaxParts / 64; ++i)
+    if (64 * i + lane < parts) {
+      const float4 q = ws.parts[r * parts + 64 * i + lane];
+      p = join<SECOND>(p, Part{q.x, q.y, q.z}, c);
+    }
+  const RowSums sums = join_waves<64, SECOND>(join_lanes<SECOND>(p, c), lane, c, nullptr);
+  const Student st = student<TAIL>(sums, list, w, inv);
+  const bool learn = list.any != 0, none = !learn || sums.m == -INFINITY || w == 0.0f;
+  Entry e{-1, 0.0f, -INFINITY, 0.0f};
+  bool mine = false;  // the lane's listed token lies in this block, whose first wave writes it after the other stores
+  float own = 0.0f;
+  if (tid < 64) {
+    if (learn && tid < a.K) {
+      const int t = a.tokens[r * a.K + tid];
+      if (static_cast<unsigned>(t) < static_cast<unsigned>(a.in.V)) {
+        e.token = t;
+        e.x = ws.x[r * 64 + tid];
+        e.log_q = a.logp[r * a.K + tid] - list.shift;
+        e.q = exp2_fast(e.log_q * kLog2e);
+        mine = block == (t < row.head || t >= row.head + row.nv * E::N ? 0 : (t - row.head) / E::N / BLOCK);
+      }
+    }
+    if (!learn && block == 0 && a.loss && tid == 0) a.loss[r] = 0.0f;
+    DistillArgs loss_of = a;
+    if (block != 0 || !learn) loss_of.loss = nullptr;
+    if (loss_of.loss || __ballot(mine) != 0) own = loss_and_own<TAIL>(loss_of, r, tid, e, list, sums, st, w, inv);
+  }
+  if (!out) return;
+#pragma unroll
+  for (int u = 0; u < kGradUnroll; ++u) {
+    const int v = block * BLOCK + u * 256 + tid;
+    if (v < row.nv) {
+      float x[E::N];
+      E::unpack(raw[u], x);
+#pragma unroll
+      for (int i = 0; i < E::N; ++i) x[i] = none ? 0.0f : exp2_fast((x[i] - sums.base) * c) * st.A;
+      store_vector<E>(out + row.token(v, 0), E::pack(x));
+    }
+  }
+  if (has_edge) out[row.edge_token(tid)] = E::down(none ? 0.0f : exp2_fast((edge - sums.base) * c) * st.A);
+  __syncthreads();
+  if (mine && !none) out[e.token] = E::down(own);
+}
+
+DistillSpace space_in(void* p, int32_t rows, int parts) {
+  DistillSpace ws;
+  ws.parts = static_cast<float4*>(p);
+  ws.lists = reinterpret_cast<List*>(ws.parts + static_cast<int64_t>(rows) * parts);
+  ws.x = reinterpret_cast<float*>(ws.lists + rows);
+  return ws;
+}
+
+template <typename E>
+int distill_split(const DistillArgs& a, const RowSplit& split, void* workspace, hipStream_t stream) {
+  const DistillSpace ws = space_in(workspace, a.in.rows, split.parts);
+  const int grid = static_cast<int>((static_cast<int64_t>(a.in.rows) * split.parts + 3) / 4);
+  const int blocks = a.grad ? (a.in.V / E::N + 256 * kGradUnroll - 1) / (256 * kGradUnroll) : 1;
+  auto go = [&](auto tail) {
+    constexpr bool TAIL = decltype(tail)::value;
+    distill_parts_kernel<E, TAIL><<<grid, 256, 0, stream>>>(a, split.parts, split.each, ws);
+    if (hipGetLastError() != hipSuccess) return PB_EHIP;
+    distill_grad_kernel<E, TAIL><<<a.in.rows * blocks, 256, 0, stream>>>(a, split.parts, blocks, ws);
+    return hipGetLastError() == hipSuccess ? PB_OK : PB_EHIP;
+  };
+  return a.tail ? go(std::true_type{}) : go(std::false_type{});
+}
+
+template <typename E>
+int distill(const DistillArgs& a, void* workspace, hipStream_t stream) {
+  const RowSplit split = row_split(a.in.V / E::N, a.in.rows);
+  if (split.parts > 0) return distill_split<E>(a, split, workspace, stream);
+  const int nv = a.in.V / E::N, mark_bytes = (a.in.V + 127) / 128 * 16;  // (a bit per element behind the head)
+  auto go = [&](auto nt, auto held) {
+    constexpr int NT = decltype(nt)::value, HELD = decltype(held)::value, ROWS = NT == 64 ? 4 : 1, THREADS = NT == 64 ? 256 : NT;
+    const int grid = (a.in.rows + ROWS - 1) / ROWS;
+    if (a.tail)
+      distill_kernel<E, NT, HELD, true><<<grid, THREADS, ROWS * mark_bytes, stream>>>(a, mark_bytes);
+    else
+      distill_kernel<E, NT, HELD, false><<<grid, THREADS, 0, stream>>>(a, 0);
+    return hipGetLastError() == hipSuccess ? PB_OK : PB_EHIP;
+  };
+  using std::integral_constant;
+  if (nv <= 512) return go(integral_constant<int, 64>{}, integral_constant<int, 8>{});
+  if (nv <= 2048) return go(integral_constant<int, 256>{}, integral_constant<int, 8>{});
+  if (nv <= 4096) return go(integral_constant<int, 512>{}, integral_constant<int, 8>{});
+  return go(integral_constant<int, 1024>{}, integral_constant<int, 8>{});
+}
+
+}  // namespace
+}  // namespace lr
+
+int64_t distill_topk_workspace(int dtype, int32_t rows, int32_t V) {
+  const RowSplit split = row_split(V / (dtype == PB_F32 ? lr::F32::N : lr::F16::N), rows);
+  if (split.parts == 0) return 0;
+  return static_cast<int64_t>(rows) * (split.parts * static_cast<int64_t>(sizeof(float4)) + sizeof(lr::List) + 64 * sizeof(float));
+}
+int launch_distill_topk(int dtype, const DistillArgs& a, void* workspace, hipStream_t stream) {
+  return dtype == PB_F32   ? lr::distill<lr::F32>(a, workspace, stream)
+         : dtype == PB_F16 ? lr::distill<lr::F16>(a, workspace, stream)
+                           : lr::distill<lr::BF16>(a, workspace, stream);
+}
+
+}  // namespace pb

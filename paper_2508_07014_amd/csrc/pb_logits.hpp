@@ -1,5 +1,5 @@
 // Log-probs, entropy and alternatives of rows of logits, and distillation from a teacher's alternatives: arguments of the
-// calls as the kernels get them, and the launch wrappers (pb_logits.hip).
+// calls as the kernels get them, and the launch wrappers (pb_logprobs.hip, pb_distill.hip).
 #pragma once
 #include <hip/hip_runtime.h>
 
@@ -9,7 +9,7 @@
 
 namespace pb {
 
-constexpr int kLogitsMaxV = 1 << 19;   // widest row: a bit per token fits in LDS
+constexpr int kLogitsMaxV = 3 << 17;   // widest row: a bit per token fits in 64 KiB of LDS with room to spare
 constexpr int kMaxGiven = 64;          // tokens scored, alternatives kept or teacher's entries a row: one lane each
 
 struct LogitRows {
@@ -52,8 +52,23 @@ struct DistillArgs {
   int64_t grad_stride;
 };
 
-int launch_token_logprobs(int dtype, const LogprobArgs& a, hipStream_t stream);
+// Few long rows are split over the chip: `parts` waves a row, each with 64 * `each` vectors of 16 bytes (0: not split).
+// At most kMaxParts, so that one workgroup can join them.
+constexpr int kWaveVectors = 512;  // longest row that one wave takes, in vectors
+constexpr int kMaxParts = 256, kMaxEach = (kLogitsMaxV / 4 + 64 * kMaxParts - 1) / (64 * kMaxParts);
+struct RowSplit {
+  int parts, each;
+};
+inline RowSplit row_split(int vectors, int32_t rows) {
+  if (vectors < 5120 || rows >= 256) return RowSplit{0, 0};
+  const int each = (vectors + 64 * kMaxParts - 1) / (64 * kMaxParts);
+  return RowSplit{(vectors + 64 * each - 1) / (64 * each), each};
+}
+
+int64_t token_logprobs_workspace(int dtype, int32_t rows, int32_t V);
+int64_t distill_topk_workspace(int dtype, int32_t rows, int32_t V);
+int launch_token_logprobs(int dtype, const LogprobArgs& a, void* workspace, hipStream_t stream);
 int launch_token_logprobs_backward(int dtype, const LogprobGradArgs& a, hipStream_t stream);
-int launch_distill_topk(int dtype, const DistillArgs& a, hipStream_t stream);
+int launch_distill_topk(int dtype, const DistillArgs& a, void* workspace, hipStream_t stream);
 
 }  // namespace pb

@@ -1,0 +1,561 @@
+// pb_token_logprobs and its gradient (gfx950): rows read once, in 16-byte vectors, by a wave or a workgroup each.
+#include <hip/hip_runtime.h>
+
+#include "pb_kernels.hpp"
+#include "pb_logit_rows.hpp"
+
+namespace pb {
+namespace lr {
+namespace {
+
+constexpr int kUnroll = 4;            // vectors of a thread in flight
+constexpr int kGroups = 256;          // parts of a row whose maxima bound the alternatives
+
+// The alternatives.  Every lane keeps the largest element of its vectors (m1), the first vector that holds it (k1) and the
+// largest element of its other vectors (m2).  The N-th largest of the lanes' (or, past 256 threads, of 256 groups of
+// lanes') m1 is a bound that N elements reach; hardly more than those lie above it (with G groups G ln(G / (G - N)) are
+// expected), and all lie in vectors k1, except where an m2 reaches it too.  So after one pass over the row a few vectors
+// are read a second time, from cache, and a list of N and some candidates is put in order by counting.
+template <int N>
+constexpr int list_size() { return 64 * N + 64; }
+struct Tops {
+  float m1 = -INFINITY, m2 = -INFINITY;
+  int k1 = 0;
+  __device__ __forceinline__ void add(float vm, int k) {
+    k1 = vm > m1 ? k : k1;
+    m2 = __builtin_amdgcn_fmed3f(vm, m1, m2);  // (m2 <= m1)
+    m1 = fmaxf(m1, vm);
+  }
+};
+
+__device__ __forceinline__ unsigned order32(float x) { return ukey(__fadd_rn(x, 0.0f)); }  // (-0.0 as 0.0)
+__device__ __forceinline__ u64 order64(unsigned key, int token) { return (static_cast<u64>(key) << 32) | static_cast<unsigned>(~token); }
+
+template <int NT, int N>
+struct TopLds {
+  unsigned group[NT == 64 ? 1 : NT];
+  int first[NT == 64 ? 1 : NT];
+  u64 list[list_size<N>()];
+  u64 best;
+  int count;
+};
+
+// The largest b that at least `n` keys of the row's groups reach (0: there are fewer); a wave holds them all, PER per lane.
+template <int PER>
+__device__ __forceinline__ int how_many(const unsigned (&key)[PER], unsigned b) {
+  int n = 0;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) n += __builtin_popcountll(__ballot(key[i] >= b));
+  return n;
+}
+template <int PER>
+__device__ __forceinline__ unsigned bound_of(const unsigned (&key)[PER], int n) {
+  unsigned b = 0;
+  for (int bit = 31; bit >= 0; --bit) {
+    const unsigned t = b | (1u << bit);
+    const int got = how_many(key, t);
+    if (got >= n) b = t;
+    if (got == n) break;
+  }
+  return b;
+}
+
+// Candidates into the list: the elements of vector v that the bound admits.
+template <typename E, int NT>
+__device__ __forceinline__ void push_vector(const Row<E>& row, const float (&x)[E::N], int v, unsigned b, int last, TopLds<NT, E::N>& lds) {
+  unsigned take = 0;
+#pragma unroll
+  for (int i = 0; i < E::N; ++i) {
+    const unsigned k = order32(x[i]);
+    take |= (k > b || (k == b && v <= last)) ? 1u << i : 0u;
+  }
+  if (take) {
+    int at = atomicAdd(&lds.count, __builtin_popcount(take));
+#pragma unroll
+    for (int i = 0; i < E::N; ++i)
+      if ((take >> i) & 1u) {
+        if (at < list_size<E::N>()) lds.list[at] = order64(order32(x[i]), row.token(v, i));
+        ++at;
+      }
+  }
+}
+template <typename E, int NT>
+__device__ __forceinline__ void push_edge(const Row<E>& row, int tid, float edge, unsigned b, TopLds<NT, E::N>& lds) {
+  if (tid < row.edges && order32(edge) >= b) {
+    const int at = atomicAdd(&lds.count, 1);
+    if (at < list_size<E::N>()) lds.list[at] = order64(order32(edge), row.edge_token(tid));
+  }
+}
+
+struct TopOut {
+  int n;
+  float base, inv, logs;
+  int32_t* tokens;
+  float* logp;
+  __device__ __forceinline__ void write(int rank, u64 k) const {
+    tokens[rank] = static_cast<int32_t>(~static_cast<unsigned>(k));
+    logp[rank] = (ukey_val(static_cast<unsigned>(k >> 32)) - base) * inv - logs;
+  }
+};
+// The list in order.  Where there were more candidates than it holds (the largest values crowd in a few groups): one
+// alternative after the other, each a pass over the row.
+template <typename E, int NT>
+__device__ __forceinline__ void write_list(const Row<E>& row, int tid, float edge, const TopOut& out, TopLds<NT, E::N>& lds) {
+  row_sync<NT>();
+  const int count = uniform_i(lds.count);
+  if (count <= list_size<E::N>()) {
+    for (int i = tid; i < count; i += NT) {
+      const u64 k = lds.list[i];
+      int rank = 0;
+      for (int j = 0; j < count; ++j) rank += lds.list[j] > k ? 1 : 0;
+      if (rank < out.n) out.write(rank, k);
+    }
+    return;
+  }
+  u64 before = ~0ull;
+  for (int n = 0; n < out.n; ++n) {
+    u64 best = 0;
+    auto take = [&](float x, int token) {
+      const u64 k = order64(order32(x), token);
+      best = k < before && k > best ? k : best;
+    };
+    for (int v = tid; v < row.nv; v += NT) {
+      float x[E::N];
+      E::unpack(row.vec(v), x);
+#pragma unroll
+      for (int i = 0; i < E::N; ++i) take(x[i], row.token(v, i));
+    }
+    if (tid < row.edges) take(edge, row.edge_token(tid));
+    if (tid == 0) lds.best = 0;
+    row_sync<NT>();
+    atomicMax(&lds.best, best);
+    row_sync<NT>();
+    before = lds.best;
+    if (tid == 0) out.write(n, before);
+    row_sync<NT>();
+  }
+}
+
+template <typename E, int NT>
+__device__ __forceinline__ void write_alternatives(const Row<E>& row, int tid, const Tops& tops, float edge, const TopOut& out,
+                                                   TopLds<NT, E::N>& lds) {
+  constexpr int PER = NT == 64 ? 1 : kGroups / 64, PARTS = NT == 64 ? 1 : NT / kGroups;
+  const int lane = tid & 63;
+  const bool some = tid < row.nv;
+  const unsigned own = some ? order32(tops.m1) : 0u;
+  if (tid == 0) lds.count = 0;
+  unsigned key[PER];
+  if constexpr (NT == 64) {
+    key[0] = own;
+  } else {
+    lds.group[tid] = own;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      key[i] = 0u;
+#pragma unroll
+      for (int p = 0; p < PARTS; ++p) key[i] = max(key[i], lds.group[kGroups * p + 64 * i + lane]);
+    }
+  }
+  const unsigned b = bound_of(key, out.n);
+  // Elements equal to the bound count in the order of their tokens.  Where many groups have it for their maximum (masked
+  // rows with fewer tokens left than alternatives wanted, flat rows), only those up to vector `last` are wanted: the groups
+  // above it are not enough by `need`, and the `need` lowest vectors in which a group has its maximum hold so many.
+  int last = INT_MAX;
+  if (b != 0u && how_many(key, b) > out.n + 16) {
+    int first[PER];
+    if constexpr (NT == 64) {
+      first[0] = tops.k1 * NT + tid;
+    } else {
+      lds.first[tid] = tops.k1 * NT + tid;
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        first[i] = INT_MAX;
+#pragma unroll
+        for (int p = 0; p < PARTS; ++p) {
+          const int at = kGroups * p + 64 * i + lane;
+          if (lds.group[at] == b) first[i] = min(first[i], lds.first[at]);
+        }
+      }
+    }
+    unsigned place[PER];  // (the need-th smallest is the need-th largest of the complements)
+#pragma unroll
+    for (int i = 0; i < PER; ++i) place[i] = key[i] == b ? static_cast<unsigned>(INT_MAX - first[i]) : 0u;
+    last = INT_MAX - static_cast<int>(bound_of(place, out.n - how_many(key, b + 1)));
+  }
+  row_sync<NT>();
+  const int v1 = tops.k1 * NT + tid;
+  if (some && (own > b || (own == b && v1 <= last))) {
+    float x[E::N];
+    E::unpack(row.vec(v1), x);
+    push_vector<E, NT>(row, x, v1, b, last, lds);
+    if (row.nv > NT && order32(tops.m2) >= b)
+      for (int v = tid; v < row.nv; v += NT)
+        if (v != v1) {
+          E::unpack(row.vec(v), x);
+          push_vector<E, NT>(row, x, v, b, last, lds);
+        }
+  }
+  push_edge<E, NT>(row, tid, edge, b, lds);
+  write_list<E, NT>(row, tid, edge, out, lds);
+}
+
+// What a row's sums say, and the scores of the given tokens.
+__device__ __forceinline__ float write_scores(const LogprobArgs& a, int64_t r, int tid, const RowSums& sums, int given, float given_x) {
+  const bool empty = sums.m == -INFINITY;
+  const float logs = sums.bad ? NAN : empty ? 0.0f : logf(sums.S);
+  if (tid < a.n_tokens) a.logp[r * a.n_tokens + tid] = given < 0 ? NAN : (given_x - sums.base) * a.in.inv_temp - logs;
+  if (tid == 0) {
+    const float H = sums.bad ? NAN : empty ? 0.0f : logs - sums.X * kLn2 / sums.S;
+    if (a.entropy) a.entropy[r] = H;
+    if (a.stats) {
+      a.stats[3 * r + 0] = sums.bad ? NAN : sums.m;
+      a.stats[3 * r + 1] = logs;
+      a.stats[3 * r + 2] = H;
+    }
+  }
+  if (sums.bad && tid < a.n_top) {
+    a.top_tokens[r * a.n_top + tid] = -1;
+    a.top_logp[r * a.n_top + tid] = NAN;
+  }
+  return logs;
+}
+template <typename E>
+__device__ __forceinline__ int load_given(const LogprobArgs& a, int64_t r, const Row<E>& row, int tid, float& x) {
+  x = 0.0f;
+  if (tid >= a.n_tokens) return -1;
+  const int t = a.tokens[r * a.n_tokens + tid];
+  if (static_cast<unsigned>(t) >= static_cast<unsigned>(row.V)) return -1;
+  x = E::up(row.x[t]);
+  return t;
+}
+
+// One row.  NT == 64: a wave of its own, kThreads / 64 of them in a workgroup.
+template <typename E, int NT, bool ENT, bool TOP>
+__global__ __launch_bounds__(NT == 64 ? 256 : NT) void logprobs_kernel(LogprobArgs a) {
+  constexpr int ROWS = NT == 64 ? 4 : 1, SECOND = ENT ? kEntropy : kAlone;
+  __shared__ float s_sums[ROWS][3 * NT / 64];
+  __shared__ TopLds<TOP ? NT : 64, TOP ? E::N : 1> s_top[TOP ? ROWS : 1];
+  const int sub = NT == 64 ? uniform_i(threadIdx.x >> 6) : 0, tid = NT == 64 ? threadIdx.x & 63 : threadIdx.x;
+  const int64_t r = static_cast<int64_t>(blockIdx.x) * ROWS + sub;
+  if (ROWS > 1 && r >= a.in.rows) return;
+  const Row<E> row = row_at<E>(a.in.x, a.in.stride, r, a.in.V);
+  const float inv = a.in.inv_temp, c = inv * kLog2e, room = kRoom / c;
+  float given_x;  // (on its way during the pass)
+  const int given = load_given<E>(a, r, row, tid, given_x);
+  Sums s(kFar / c);
+  Tops tops;
+  const int whole = row.nv / (kUnroll * NT);
+  auto one = [&](const v4u& raw, int k) {
+    float x[E::N];
+    E::unpack(raw, x);
+    const float vm = vec_max(x);
+    if constexpr (TOP) tops.add(vm, k);
+    else s.m = fmaxf(s.m, vm);
+    add_vector<SECOND>(s, x, vm, c, room);
+  };
+  for (int b = 0; b < whole; ++b) {
+    v4u raw[kUnroll];
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) raw[u] = row.vec((b * kUnroll + u) * NT + tid);
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) one(raw[u], b * kUnroll + u);
+  }
+  {
+    v4u raw[kUnroll];
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u)
+      if ((whole * kUnroll + u) * NT + tid < row.nv) raw[u] = row.vec((whole * kUnroll + u) * NT + tid);
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u)
+      if ((whole * kUnroll + u) * NT + tid < row.nv) one(raw[u], whole * kUnroll + u);
+  }
+  float edge = -INFINITY;
+  if (tid < row.edges) {
+    edge = E::up(row.x[row.edge_token(tid)]);
+    const float x[1] = {edge};
+    add_vector<SECOND>(s, x, edge, c, room);
+  }
+  s.m = fmaxf(TOP ? tops.m1 : s.m, edge);
+  const Part part = wave_part<SECOND>(s, c, [&](auto&& add) {
+    for (int v = tid; v < row.nv; v += NT) {
+      float x[E::N];
+      E::unpack(row.vec(v), x);
+#pragma unroll
+      for (int i = 0; i < E::N; ++i) add(x[i], false);
+    }
+    if (tid < row.edges) add(edge, false);
+  });
+  const RowSums sums = join_waves<NT, SECOND>(part, tid, c, s_sums[sub]);
+  const float logs = write_scores(a, r, tid, sums, given, given_x);
+  if constexpr (TOP) {
+    if (!sums.bad)
+      write_alternatives<E, NT>(row, tid, tops, edge, TopOut{a.n_top, sums.base, inv, logs, a.top_tokens + r * a.n_top, a.top_logp + r * a.n_top},
+                                s_top[sub]);
+  }
+}
+
+// Few long rows: every wave takes 64 * `each` vectors of a row and leaves their part (the maximum and the sums) in the
+// workspace; a workgroup per row joins them.  The parts' maxima bound the alternatives as the lanes' do above, and the
+// parts that reach the bound are read again.
+template <typename E, bool ENT>
+__global__ __launch_bounds__(256) void logprobs_parts_kernel(LogprobArgs a, int parts, int each, float4* __restrict__ out) {
+  constexpr int SECOND = ENT ? kEntropy : kAlone;
+  const int64_t at = static_cast<int64_t>(blockIdx.x) * 4 + uniform_i(threadIdx.x >> 6);
+  const int64_t r = at / parts;
+  if (r >= a.in.rows) return;
+  const int lane = threadIdx.x & 63, begin = static_cast<int>(at - r * parts) * 64 * each;
+  const Row<E> row = row_at<E>(a.in.x, a.in.stride, r, a.in.V);
+  const float c = a.in.inv_temp * kLog2e, room = kRoom / c;
+  const int end = min(begin + 64 * each, row.nv);
+  Sums s(kFar / c);
+  for (int v = begin + lane; v < end; v += 64) {
+    float x[E::N];
+    E::unpack(row.vec(v), x);
+    const float vm = vec_max(x);
+    s.m = fmaxf(s.m, vm);
+    add_vector<SECOND>(s, x, vm, c, room);
+  }
+  const bool has_edge = begin == 0 && lane < row.edges;  // (the first part has the edge as well)
+  float edge = -INFINITY;
+  if (has_edge) {
+    edge = E::up(row.x[row.edge_token(lane)]);
+    const float x[1] = {edge};
+    s.m = fmaxf(s.m, edge);
+    add_vector<SECOND>(s, x, edge, c, room);
+  }
+  const Part p = wave_part<SECOND>(s, c, [&](auto&& add) {
+    for (int v = begin + lane; v < end; v += 64) {
+      float x[E::N];
+      E::unpack(row.vec(v), x);
+#pragma unroll
+      for (int i = 0; i < E::N; ++i) add(x[i], false);
+    }
+    if (has_edge) add(edge, false);
+  });
+  if (lane == 0) out[at] = make_float4(p.m, p.S, p.X, 0.0f);
+}
+
+constexpr int kJoinThreads = 1024;
+template <typename E, bool ENT, bool TOP>
+__global__ __launch_bounds__(kJoinThreads) void logprobs_join_kernel(LogprobArgs a, int parts, int each, const float4* __restrict__ in) {
+  constexpr int SECOND = ENT ? kEntropy : kAlone, NT = kJoinThreads, W = NT / 64;
+  __shared__ float s_sums[3 * W];
+  __shared__ TopLds<TOP ? NT : 64, TOP ? E::N : 1> lds;
+  __shared__ int s_found[W];
+  const int64_t r = blockIdx.x;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const Row<E> row = row_at<E>(a.in.x, a.in.stride, r, a.in.V);
+  const float c = a.in.inv_temp * kLog2e;
+  float given_x;
+  const int given = load_given<E>(a, r, row, tid, given_x);
+  Part p{-INFINITY, 0.0f, 0.0f};
+  if (tid < parts) {
+    const float4 q = in[r * parts + tid];
+    p = Part{q.x, q.y, q.z};
+  }
+  const bool some = tid < parts && (tid == 0 || tid * 64 * each < row.nv);  // (a row's head may leave its last part empty)
+  const unsigned own = some ? order32(p.m) : 0u;
+  float edge = -INFINITY;
+  if (tid < row.edges) edge = E::up(row.x[row.edge_token(tid)]);
+  const RowSums sums = join_waves<NT, SECOND>(join_lanes<SECOND>(p, c), tid, c, s_sums);
+  const float logs = write_scores(a, r, tid, sums, given, given_x);
+  if constexpr (TOP) {
+    if (sums.bad) return;
+    const TopOut out{a.n_top, sums.base, a.in.inv_temp, logs, a.top_tokens + r * a.n_top, a.top_logp + r * a.n_top};
+    if (tid == 0) lds.count = lds.first[kGroups] = 0;
+    if (tid < kGroups) lds.group[tid] = own;
+    __syncthreads();
+    unsigned key[kGroups / 64];
+#pragma unroll
+    for (int i = 0; i < kGroups / 64; ++i) key[i] = lds.group[64 * i + lane];
+    const unsigned b = bound_of(key, out.n);
+    const bool ties = b != 0u && how_many(key, b) > out.n + 16;  // (then the elements equal to the bound are looked for in order)
+    if (own > b || (own == b && some && !ties)) lds.first[atomicAdd(&lds.first[kGroups], 1)] = tid;
+    __syncthreads();
+    const int n = uniform_i(lds.first[kGroups]), last = ties ? -1 : INT_MAX;
+    for (int i = tid >> 6; i < n; i += W) {
+      const int begin = uniform_i(lds.first[i]) * 64 * each;
+      for (int v = begin + lane; v < min(begin + 64 * each, row.nv); v += 64) {
+        float x[E::N];
+        E::unpack(row.vec(v), x);
+        push_vector<E, NT>(row, x, v, b, last, lds);
+      }
+    }
+    push_edge<E, NT>(row, tid, edge, b, lds);
+    if (ties) {
+      // n_top elements equal to the bound, the first ones (some may fall behind larger elements of the list)
+      for (int before = 0, at = 0; at < row.nv && before < out.n; at += NT) {
+        unsigned equal = 0;
+        float x[E::N];
+        if (at + tid < row.nv) {
+          E::unpack(row.vec(at + tid), x);
+#pragma unroll
+          for (int i = 0; i < E::N; ++i) equal |= order32(x[i]) == b ? 1u << i : 0u;
+        }
+        int mine = 0, wave = 0;  // equal elements of the wave's lanes before this one, and of all
+#pragma unroll
+        for (int i = 0; i < E::N; ++i) {
+          const u64 who = __ballot((equal >> i) & 1u);
+          mine += __builtin_amdgcn_mbcnt_hi(static_cast<unsigned>(who >> 32), __builtin_amdgcn_mbcnt_lo(static_cast<unsigned>(who), 0u));
+          wave += __builtin_popcountll(who);
+        }
+        if (lane == 0) s_found[tid >> 6] = wave;
+        __syncthreads();
+        int total = 0;
+        for (int w = 0; w < W; ++w) {
+          if (w < (tid >> 6)) mine += s_found[w];
+          total += s_found[w];
+        }
+        unsigned take = 0;
+        mine += before;
+#pragma unroll
+        for (int i = 0; i < E::N; ++i)
+          if ((equal >> i) & 1u) {
+            if (mine < out.n) take |= 1u << i;
+            ++mine;
+          }
+        if (take) {
+          int to = atomicAdd(&lds.count, __builtin_popcount(take));
+#pragma unroll
+          for (int i = 0; i < E::N; ++i)
+            if ((take >> i) & 1u) {
+              if (to < list_size<E::N>()) lds.list[to] = order64(b, row.token(at + tid, i));
+              ++to;
+            }
+        }
+        before += total;
+        __syncthreads();
+      }
+    }
+    write_list<E, NT>(row, tid, edge, out, lds);
+  }
+}
+
+// Gradient: p (A + B log2 p) with A = -(G + h H) / T, B = -h ln(2) / T for all tokens, plus what the given ones take.  A
+// workgroup takes kUnroll vectors a thread of one row (a wave, four rows a workgroup, where those hold the row).  The
+// gradients on the given tokens are computed before anything is written and stored behind the rest.
+template <typename E, int NT>
+__global__ __launch_bounds__(256) void logprobs_backward_kernel(LogprobGradArgs a, int parts) {
+  constexpr int ROWS = 256 / NT, PART = NT * kUnroll;
+  const int sub = ROWS > 1 ? uniform_i(threadIdx.x / NT) : 0, tid = threadIdx.x % NT;
+  const int64_t r = ROWS > 1 ? static_cast<int64_t>(blockIdx.x) * ROWS + sub : blockIdx.x / parts;
+  const int part = ROWS > 1 ? 0 : blockIdx.x % parts;
+  if (ROWS > 1 && r >= a.in.rows) return;
+  const Row<E> row = row_at<E>(a.in.x, a.in.stride, r, a.in.V);
+  typename E::type* out = static_cast<typename E::type*>(a.grad) + r * a.grad_stride;
+  v4u raw[kUnroll];
+#pragma unroll
+  for (int u = 0; u < kUnroll; ++u)
+    if (part * PART + u * NT + tid < row.nv) raw[u] = row.vec(part * PART + u * NT + tid);
+  const bool has_edge = part == 0 && tid < row.edges;
+  float edge = 0.0f;
+  if (has_edge) edge = E::up(row.x[row.edge_token(tid)]);
+  const float inv = a.in.inv_temp, c = inv * kLog2e;
+  const float m = a.stats[3 * r], logs = a.stats[3 * r + 1], H = a.stats[3 * r + 2];
+  const float h = a.grad_entropy ? a.grad_entropy[r] : 0.0f;
+  const int lane = threadIdx.x & 63;
+  int given = -1;
+  bool mine = false;  // the token lies in this part, which writes it, after its other stores
+  float g = 0.0f, given_x = 0.0f;
+  if (lane < a.n_tokens && a.grad_logp) {
+    given = a.tokens[r * a.n_tokens + lane];
+    if (static_cast<unsigned>(given) < static_cast<unsigned>(a.in.V)) {
+      g = a.grad_logp[r * a.n_tokens + lane];
+      mine = part == (given < row.head || given >= row.head + row.nv * E::N ? 0 : (given - row.head) / E::N / PART);
+      if (mine) given_x = E::up(row.x[given]);
+    } else {
+      given = -1;
+    }
+  }
+  const float G = wave_sum(g);
+  const bool none = (__ballot(g != 0.0f) == 0 && h == 0.0f) || m == -INFINITY;
+  const float A = none ? 0.0f : m != m ? NAN : -(G + h * H) * inv, B = none ? 0.0f : -h * kLn2 * inv, log2s = logs * kLog2e;
+  auto pull = [&](float x) {
+    const float d = fmaxf(__builtin_fmaf(x - m, c, -log2s), -1000.0f);
+    return exp2_fast(d) * __builtin_fmaf(B, d, A);
+  };
+  float onto = g;  // what the given token takes, listed once or several times
+  if (a.n_tokens > 1 && a.grad_logp) {
+    onto = 0.0f;
+    for (int k = 0; k < a.n_tokens; ++k)
+      if (__builtin_amdgcn_readlane(given, k) == given) onto += __int_as_float(__builtin_amdgcn_readlane(__float_as_int(g), k));
+  }
+  const float taken = pull(given_x) + onto * inv;
+  if constexpr (NT > 64) __syncthreads();
+#pragma unroll
+  for (int u = 0; u < kUnroll; ++u) {
+    const int v = part * PART + u * NT + tid;
+    if (v < row.nv) {
+      float x[E::N];
+      E::unpack(raw[u], x);
+#pragma unroll
+      for (int i = 0; i < E::N; ++i) x[i] = none ? 0.0f : pull(x[i]);
+      store_vector<E>(out + row.token(v, 0), E::pack(x));
+    }
+  }
+  if (has_edge) out[row.edge_token(tid)] = E::down(none ? 0.0f : pull(edge));
+  row_sync<NT>();
+  if (threadIdx.x % NT < 64 && mine && !none) out[given] = E::down(taken);
+}
+
+template <typename E>
+int forward(const LogprobArgs& a, void* workspace, hipStream_t stream) {
+  const bool ent = a.entropy || a.stats, top = a.n_top > 0;
+  auto done = [] { return hipGetLastError() == hipSuccess ? PB_OK : PB_EHIP; };
+  const RowSplit split = row_split(a.in.V / E::N, a.in.rows);
+  if (split.parts > 0) {
+    float4* ws = static_cast<float4*>(workspace);
+    const int grid = static_cast<int>((static_cast<int64_t>(a.in.rows) * split.parts + 3) / 4);
+    if (ent) logprobs_parts_kernel<E, true><<<grid, 256, 0, stream>>>(a, split.parts, split.each, ws);
+    else logprobs_parts_kernel<E, false><<<grid, 256, 0, stream>>>(a, split.parts, split.each, ws);
+    if (done() != PB_OK) return PB_EHIP;
+    auto finish = [&](auto kernel) { kernel<<<a.in.rows, kJoinThreads, 0, stream>>>(a, split.parts, split.each, ws); return done(); };
+    if (ent && top) return finish(logprobs_join_kernel<E, true, true>);
+    if (ent) return finish(logprobs_join_kernel<E, true, false>);
+    if (top) return finish(logprobs_join_kernel<E, false, true>);
+    return finish(logprobs_join_kernel<E, false, false>);
+  }
+  auto pick = [&](auto nt) {
+    constexpr int NT = decltype(nt)::value;
+    constexpr int ROWS = NT == 64 ? 4 : 1, THREADS = NT == 64 ? 256 : NT;
+    auto go = [&](auto kernel) { kernel<<<(a.in.rows + ROWS - 1) / ROWS, THREADS, 0, stream>>>(a); return done(); };
+    if (ent && top) return go(logprobs_kernel<E, NT, true, true>);
+    if (ent) return go(logprobs_kernel<E, NT, true, false>);
+    if (top) return go(logprobs_kernel<E, NT, false, true>);
+    return go(logprobs_kernel<E, NT, false, false>);
+  };
+  if (a.in.V / E::N <= kWaveVectors) return pick(std::integral_constant<int, 64>{});
+  if (a.in.rows >= 1024) return pick(std::integral_constant<int, 256>{});
+  return pick(std::integral_constant<int, 1024>{});
+}
+
+template <typename E>
+int backward(const LogprobGradArgs& a, hipStream_t stream) {
+  const int64_t nv = a.in.V / E::N;
+  if (nv <= 64 * kUnroll) {
+    logprobs_backward_kernel<E, 64><<<(a.in.rows + 3) / 4, 256, 0, stream>>>(a, 1);
+  } else {
+    const int parts = static_cast<int>((nv + 256 * kUnroll - 1) / (256 * kUnroll));
+    logprobs_backward_kernel<E, 256><<<a.in.rows * parts, 256, 0, stream>>>(a, parts);
+  }
+  return hipGetLastError() == hipSuccess ? PB_OK : PB_EHIP;
+}
+
+}  // namespace
+}  // namespace lr
+
+int64_t token_logprobs_workspace(int dtype, int32_t rows, int32_t V) {
+  return static_cast<int64_t>(rows) * row_split(V / (dtype == PB_F32 ? lr::F32::N : lr::F16::N), rows).parts * static_cast<int64_t>(sizeof(float4));
+}
+int launch_token_logprobs(int dtype, const LogprobArgs& a, void* workspace, hipStream_t stream) {
+  return dtype == PB_F32   ? lr::forward<lr::F32>(a, workspace, stream)
+         : dtype == PB_F16 ? lr::forward<lr::F16>(a, workspace, stream)
+                           : lr::forward<lr::BF16>(a, workspace, stream);
+}
+int launch_token_logprobs_backward(int dtype, const LogprobGradArgs& a, hipStream_t stream) {
+  return dtype == PB_F32 ? lr::backward<lr::F32>(a, stream) : dtype == PB_F16 ? lr::backward<lr::F16>(a, stream) : lr::backward<lr::BF16>(a, stream);
+}
+
+}  // namespace pb

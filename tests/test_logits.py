@@ -35,7 +35,7 @@ COMMON = [(dict(rows=-1), pb.PB_EINVAL), (dict(vocab_size=0, row_stride=16), pb.
           (dict(d_logits=P + ODD, dtype=pb.PB_BF16), pb.PB_EINVAL),
           (dict(temperature=0.0), pb.PB_ERANGE), (dict(temperature=-1.0), pb.PB_ERANGE), (dict(temperature=float("nan")), pb.PB_ERANGE),
           (dict(temperature=float("inf")), pb.PB_ERANGE), (dict(temperature=1e-5), pb.PB_ERANGE), (dict(temperature=1e5), pb.PB_ERANGE),
-          (dict(vocab_size=524289, row_stride=1 << 20, grad_stride=1 << 20), pb.PB_EUNSUPPORTED), (dict(rows=0), pb.PB_OK)]
+          (dict(vocab_size=393217, row_stride=1 << 20, grad_stride=1 << 20), pb.PB_EUNSUPPORTED), (dict(rows=0), pb.PB_OK)]
 
 
 @pytest.mark.parametrize("change,want", COMMON + [
@@ -77,14 +77,14 @@ def test_workspaces():
     for size, last in ((lp, 5), (di, 5)):
         assert size(pb.PB_BF16, 0, 1000, last) == 0
         for bad, want in (((3, 1, 10, last), pb.PB_EINVAL), ((0, -1, 10, last), pb.PB_EINVAL), ((0, 1, 0, last), pb.PB_EINVAL),
-                          ((0, 1, 524289, last), pb.PB_EUNSUPPORTED), ((0, 1, 1000, 65), pb.PB_EUNSUPPORTED)):
+                          ((0, 1, 393217, last), pb.PB_EUNSUPPORTED), ((0, 1, 1000, 65), pb.PB_EUNSUPPORTED)):
             with pytest.raises(pb.PbError) as e:
                 size(*bad)
             assert e.value.code == want
     for call, base, size in ((pb.pb_token_logprobs, LP, lp), (pb.pb_distill_topk, DIST, di)):
         for kind in (pb.PB_F32, pb.PB_F16, pb.PB_BF16):
             for rows in (1, 7, 100, 2000):
-                for V in (100, 5000, 131072, 524288):
+                for V in (100, 5000, 131072, 393216):
                     need = size(kind, rows, V, base.get("n_top", 2))
                     assert 0 <= need <= 64 << 20
                     if need:  # too little, none, misaligned: refused before anything is launched
