@@ -8,6 +8,130 @@ namespace pb {
 namespace lr {
 namespace {
 
+// Maximum and sums of exponentials in one pass.  With c = log2(e) / T every term is e = exp2(d), d = x c - rc; the reference
+// rc is the lane's own and is moved, with the sums, only when an element exceeds it by more than 2^kRoom: the first vector
+// sets it, after that a lane hardly ever comes back (one fused multiply-add and one exponential a term, no running maximum
+// in the chain).  d is rounded once; what rc itself was rounded by is the same for all terms of the lane, and is made up for
+// at the end (wave_part).  Elements below -kFar / c are masks of a lowest value: nothing beside any ordinary logit.
+// With LISTED a second sum takes the terms of listed tokens, which the first one then lacks.
+constexpr float kRoom = 30.0f;
+
+// (S, X) seen from a reference that lies `apart` = rc - new rc higher.
+template <bool LISTED>
+__device__ __forceinline__ void rebase(float& S, float& X, float apart) {
+  const float f = exp2_fast(apart);  // (may be infinite where the sums are 0)
+  if constexpr (LISTED) X = X == 0.0f ? 0.0f : f * X;
+  S = S == 0.0f ? 0.0f : f * S;
+}
+struct Sums {
+  float rc = 0.0f, thr, S = 0.0f, X = 0.0f, m = -INFINITY;
+  __device__ __forceinline__ explicit Sums(float far) : thr(-far) {}
+};
+// A vector into the sums; `vm` its largest element, `listed` a bit per element that goes to the second sum.
+template <bool LISTED, int N>
+__device__ __forceinline__ void add_vector(Sums& s, const float (&x)[N], float vm, float c, float room, unsigned listed = 0u) {
+  if (__ballot(vm > s.thr) != 0) {  // (of the wave: a branch, not selects in every vector)
+    if (vm > s.thr) {
+      const float next = vm * c;
+      rebase<LISTED>(s.S, s.X, s.rc - next);
+      s.rc = next;
+      s.thr = vm + room;
+    }
+  }
+  float e[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) e[i] = exp2_fast(__builtin_fmaf(x[i], c, -s.rc));
+  if (LISTED && listed != 0u) {
+    float on[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      on[i] = (listed >> i) & 1u ? e[i] : 0.0f;
+      e[i] = (listed >> i) & 1u ? 0.0f : e[i];
+    }
+    s.X += vec_sum(on);
+  }
+  s.S += vec_sum(e);
+}
+
+// Sums of a part of a row, seen from its maximum: d = (x - m) c.  A part of nothing but -inf has sums of 0.
+struct Part {
+  float m, S, X;
+};
+// The part of a wave from its lanes', the same in every lane.  again(add) goes over the wave's elements a second time, with
+// add(x, listed): where the maximum lies so far from 0 that x c and m c no longer resolve what is between them, the
+// difference does.
+template <bool LISTED, typename Again>
+__device__ __forceinline__ Part wave_part(const Sums& s, float c, Again&& again) {
+  Part p{wave_max(s.m), s.S, s.X};
+  const float mc = p.m * c;
+  rebase<LISTED>(p.S, p.X, s.rc - mc);
+  p.S = wave_sum(p.S);
+  if constexpr (LISTED) p.X = wave_sum(p.X);
+  rebase<LISTED>(p.S, p.X, -__builtin_fmaf(p.m, c, -mc));  // (from the rounded m c to m c)
+  if (!(fabsf(mc) <= kFar) && fabsf(p.m) != INFINITY) {
+    float S = 0.0f, X = 0.0f;
+    again([&](float x, bool on) {
+      const float d = (x - p.m) * c, e = exp2_fast(d);
+      S += LISTED && on ? 0.0f : e;
+          if constexpr (LISTED) X += on ? e : 0.0f;
+    });
+    p.S = wave_sum(S);
+    if constexpr (LISTED) p.X = wave_sum(X);
+  }
+  return p;
+}
+template <bool LISTED>
+__device__ __forceinline__ Part see_from(Part p, float m, float c) {
+  rebase<LISTED>(p.S, p.X, (p.m - m) * c);
+  p.m = m;
+  return p;
+}
+// Two parts, or the parts that the lanes of a wave hold, as one.
+template <bool LISTED>
+__device__ __forceinline__ Part join(const Part& p, const Part& q, float c) {
+  const float m = fmaxf(p.m, q.m);
+  const Part a = see_from<LISTED>(p, m, c), b = see_from<LISTED>(q, m, c);
+  return Part{m, a.S + b.S, a.X + b.X};
+}
+template <bool LISTED>
+__device__ __forceinline__ Part join_lanes(const Part& p, float c) {
+  const Part q = see_from<LISTED>(p, wave_max(p.m), c);
+  return Part{q.m, wave_sum(q.S), LISTED ? wave_sum(q.X) : 0.0f};
+}
+
+struct RowSums {  // the same in every thread of the row
+  float m;        // maximum, -inf for a row of nothing but -inf
+  float base;     // m, 0 for such a row
+  float S, X;     // the sums, d = (x - base) c
+  bool bad;       // the row holds a NaN or +inf
+};
+// The row from its waves' parts (`lds`: 3 * NT / 64 floats).
+template <int NT, bool LISTED>
+__device__ __forceinline__ RowSums join_waves(Part p, int tid, float c, float* lds) {
+  constexpr int W = NT / 64;
+  if constexpr (W > 1) {
+    if ((tid & 63) == 0) {
+      lds[tid >> 6] = p.m;
+      lds[W + (tid >> 6)] = p.S;
+      lds[2 * W + (tid >> 6)] = p.X;
+    }
+    __syncthreads();
+    float M = lds[0], S = 0.0f, X = 0.0f;
+#pragma unroll
+    for (int w = 1; w < W; ++w) M = fmaxf(M, lds[w]);
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+      const Part q = see_from<LISTED>(Part{lds[w], lds[W + w], lds[2 * W + w]}, M, c);
+      S += q.S;
+      X += q.X;
+    }
+    p = Part{uniform_f(M), uniform_f(S), uniform_f(X)};
+  }
+  RowSums r{p.m, p.m == -INFINITY ? 0.0f : p.m, p.S, p.X, false};
+  r.bad = r.S != r.S || r.X != r.X || r.m == INFINITY;
+  return r;
+}
+
 template <int CTRL, int ROWS>
 __device__ __forceinline__ double dpp_add(double v) {
   const long long b = __double_as_longlong(v);
@@ -112,7 +236,7 @@ __device__ __forceinline__ float loss_and_own(const DistillArgs& a, int64_t r, i
 // vanish in a difference: bits in LDS say which elements are listed, and most vectors have none.
 template <typename E, int NT, int HELD, bool TAIL>
 __global__ __launch_bounds__(NT == 64 ? 256 : NT) void distill_kernel(DistillArgs a, int mark_bytes) {
-  constexpr int ROWS = NT == 64 ? 4 : 1, SECOND = TAIL ? kListed : kAlone;
+  constexpr int ROWS = NT == 64 ? 4 : 1;
   extern __shared__ __align__(16) unsigned char s_all[];
   __shared__ float s_sums[ROWS][3 * NT / 64];
   __shared__ List s_list;
@@ -173,7 +297,7 @@ __global__ __launch_bounds__(NT == 64 ? 256 : NT) void distill_kernel(DistillArg
     E::unpack(raw, x);
     const float vm = vec_max(x);
     s.m = fmaxf(s.m, vm);
-    add_vector<SECOND>(s, x, vm, c, room, listed(v));
+    add_vector<TAIL>(s, x, vm, c, room, listed(v));
   };
 #pragma unroll
   for (int u = 0; u < HELD; ++u)
@@ -182,9 +306,9 @@ __global__ __launch_bounds__(NT == 64 ? 256 : NT) void distill_kernel(DistillArg
   if (tid < row.edges) {
     const float x[1] = {edge};
     s.m = fmaxf(s.m, edge);
-    add_vector<SECOND>(s, x, edge, c, room, edge_listed(tid) ? 1u : 0u);
+    add_vector<TAIL>(s, x, edge, c, room, edge_listed(tid) ? 1u : 0u);
   }
-  const Part part = wave_part<SECOND>(s, c, [&](auto&& add) {
+  const Part part = wave_part<TAIL>(s, c, [&](auto&& add) {
     for (int v = tid; v < row.nv; v += NT) {
       float x[E::N];
       E::unpack(row.vec(v), x);
@@ -194,7 +318,7 @@ __global__ __launch_bounds__(NT == 64 ? 256 : NT) void distill_kernel(DistillArg
     }
     if (tid < row.edges) add(edge, edge_listed(tid));
   });
-  const RowSums sums = join_waves<NT, SECOND>(part, tid, c, s_sums[sub]);
+  const RowSums sums = join_waves<NT, TAIL>(part, tid, c, s_sums[sub]);
   const bool empty = sums.m == -INFINITY;
   const Student st = student<TAIL>(sums, list, w, inv);
   float own = 0.0f;  // the gradient of the lane's listed token
@@ -235,7 +359,6 @@ struct DistillSpace {
 };
 template <typename E, bool TAIL>
 __global__ __launch_bounds__(256) void distill_parts_kernel(DistillArgs a, int parts, int each, DistillSpace ws) {
-  constexpr int SECOND = TAIL ? kListed : kAlone;
   __shared__ unsigned s_marks[4][64 * kMaxEach / 4];  // a byte per vector
   __shared__ unsigned s_edge[4];
   const int sub = uniform_i(threadIdx.x >> 6), lane = threadIdx.x & 63;
@@ -275,7 +398,7 @@ __global__ __launch_bounds__(256) void distill_parts_kernel(DistillArgs a, int p
     E::unpack(row.vec(v), x);
     const float vm = vec_max(x);
     s.m = fmaxf(s.m, vm);
-    add_vector<SECOND>(s, x, vm, c, room, listed(v));
+    add_vector<TAIL>(s, x, vm, c, room, listed(v));
   }
   const bool has_edge = begin == 0 && lane < row.edges;
   const bool on_edge = TAIL && has_edge && ((s_edge[sub] >> lane) & 1u);
@@ -284,9 +407,9 @@ __global__ __launch_bounds__(256) void distill_parts_kernel(DistillArgs a, int p
     edge = E::up(row.x[row.edge_token(lane)]);
     const float x[1] = {edge};
     s.m = fmaxf(s.m, edge);
-    add_vector<SECOND>(s, x, edge, c, room, on_edge ? 1u : 0u);
+    add_vector<TAIL>(s, x, edge, c, room, on_edge ? 1u : 0u);
   }
-  const Part p = wave_part<SECOND>(s, c, [&](auto&& add) {
+  const Part p = wave_part<TAIL>(s, c, [&](auto&& add) {
     for (int v = begin + lane; v < end; v += 64) {
       float x[E::N];
       E::unpack(row.vec(v), x);
@@ -302,7 +425,7 @@ __global__ __launch_bounds__(256) void distill_parts_kernel(DistillArgs a, int p
 constexpr int kGradUnroll = 4;
 template <typename E, bool TAIL>
 __global__ __launch_bounds__(256) void distill_grad_kernel(DistillArgs a, int parts, int blocks, DistillSpace ws) {
-  constexpr int SECOND = TAIL ? kListed : kAlone, BLOCK = 256 * kGradUnroll;
+  constexpr int BLOCK = 256 * kGradUnroll;
   const int64_t r = blockIdx.x / blocks;
   const int block = blockIdx.x % blocks, tid = threadIdx.x, lane = tid & 63;
   const Row<E> row = row_at<E>(a.in.x, a.in.stride, r, a.in.V);
@@ -322,9 +445,9 @@ __global__ __launch_bounds__(256) void distill_grad_kernel(DistillArgs a, int pa
   for (int i = 0; i < kMaxParts / 64; ++i)
     if (64 * i + lane < parts) {
       const float4 q = ws.parts[r * parts + 64 * i + lane];
-      p = join<SECOND>(p, Part{q.x, q.y, q.z}, c);
+      p = join<TAIL>(p, Part{q.x, q.y, q.z}, c);
     }
-  const RowSums sums = join_waves<64, SECOND>(join_lanes<SECOND>(p, c), lane, c, nullptr);
+  const RowSums sums = join_waves<64, TAIL>(join_lanes<TAIL>(p, c), lane, c, nullptr);
   const Student st = student<TAIL>(sums, list, w, inv);
   const bool learn = list.any != 0, none = !learn || sums.m == -INFINITY || w == 0.0f;
   Entry e{-1, 0.0f, -INFINITY, 0.0f};

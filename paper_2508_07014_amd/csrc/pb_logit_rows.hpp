@@ -147,28 +147,10 @@ __device__ __forceinline__ void store_vector(typename E::type* p, const v4u& r) 
   *reinterpret_cast<typename E::any4*>(p) = r;
 }
 
-// max and sums of exponentials in one pass.  With c = log2(e) / T every term is e = exp2(d), d = x c - rc; the reference rc
-// is the lane's own and is moved, with the sums, only when an element exceeds it by more than 2^kRoom: the first vector
-// sets it, after that a lane hardly ever comes back (one fused multiply-add and one exponential a term, no running maximum
-// in the chain).  d is rounded once; what rc itself was rounded by is the same for all terms of the lane, and is made up for
-// at the end (row_sums).  Elements below -kFar / c are masks of a lowest value: nothing beside any ordinary logit.  A row whose
-// maximum lies beyond +-kFar / c is summed again from differences (row_sums).
-// A second sum goes along: of e d (for the entropy), or of the terms of listed tokens, which the first one then lacks.
-constexpr float kRoom = 30.0f, kFar = 1048576.0f;
-enum Second : int { kAlone = 0, kEntropy = 1, kListed = 2 };
+// Elements further than kFar / c from 0 (c = log2(e) / T): there x c is too coarse for the differences between them, and a
+// row's sums are formed from (x - max) c instead.
+constexpr float kFar = 1048576.0f;
 
-// (S, X) seen from a reference that lies `apart` = rc - new rc higher.
-template <int SECOND>
-__device__ __forceinline__ void rebase(float& S, float& X, float apart) {
-  const float f = exp2_fast(apart);  // (may be infinite where the sums are 0)
-  if constexpr (SECOND == kEntropy) X = S == 0.0f ? 0.0f : f * __builtin_fmaf(apart, S, X);
-  if constexpr (SECOND == kListed) X = X == 0.0f ? 0.0f : f * X;
-  S = S == 0.0f ? 0.0f : f * S;
-}
-struct Sums {
-  float rc = 0.0f, thr, S = 0.0f, X = 0.0f, m = -INFINITY;
-  __device__ __forceinline__ explicit Sums(float far) : thr(-far) {}
-};
 template <int N>
 __device__ __forceinline__ float vec_max(const float (&x)[N]) {
   if constexpr (N == 1) return x[0];
@@ -178,113 +160,13 @@ __device__ __forceinline__ float vec_max(const float (&x)[N]) {
   if constexpr (N % 2 == 0) m = fmaxf(m, x[N - 1]);
   return m;
 }
-// A vector into the sums; `vm` its largest element, `listed` a bit per element that goes to the second sum (kListed).
-template <int SECOND, int N>
-__device__ __forceinline__ void add_vector(Sums& s, const float (&x)[N], float vm, float c, float room, unsigned listed = 0u) {
-  if (__ballot(vm > s.thr) != 0) {  // (of the wave: a branch, not selects in every vector)
-    if (vm > s.thr) {
-      const float next = vm * c;
-      rebase<SECOND>(s.S, s.X, s.rc - next);
-      s.rc = next;
-      s.thr = vm + room;
-    }
-  }
-  if (SECOND == kListed && listed != 0u) {
+template <int N>
+__device__ __forceinline__ float vec_sum(float (&x)[N]) {  // (in pairs: fewer roundings in a row)
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const float e = exp2_fast(__builtin_fmaf(x[i], c, -s.rc));
-      const bool on = (listed >> i) & 1u;
-      s.S += on ? 0.0f : e;
-      s.X += on ? e : 0.0f;
-    }
-    return;
-  }
+  for (int n = N / 2; n > 0; n /= 2)
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    const float d = __builtin_fmaf(x[i], c, -s.rc), e = exp2_fast(d);
-    s.S += e;
-    if constexpr (SECOND == kEntropy) s.X = __builtin_fmaf(e, fmaxf(d, -1000.0f), s.X);  // (-inf: nothing)
-  }
-}
-
-// Sums of a part of a row, seen from its maximum: d = (x - m) c.  A part of nothing but -inf has sums of 0.
-struct Part {
-  float m, S, X;
-};
-// The part of a wave from its lanes', the same in every lane.  again(add) goes over the wave's elements a second time, with
-// add(x, listed): where the maximum lies so far from 0 that x c and m c no longer resolve what is between them, the
-// difference does.
-template <int SECOND, typename Again>
-__device__ __forceinline__ Part wave_part(const Sums& s, float c, Again&& again) {
-  Part p{wave_max(s.m), s.S, s.X};
-  const float mc = p.m * c;
-  rebase<SECOND>(p.S, p.X, s.rc - mc);
-  p.S = wave_sum(p.S);
-  if constexpr (SECOND != kAlone) p.X = wave_sum(p.X);
-  rebase<SECOND>(p.S, p.X, -__builtin_fmaf(p.m, c, -mc));  // (from the rounded m c to m c)
-  if (!(fabsf(mc) <= kFar) && fabsf(p.m) != INFINITY) {
-    float S = 0.0f, X = 0.0f;
-    again([&](float x, bool on) {
-      const float d = (x - p.m) * c, e = exp2_fast(d);
-      S += SECOND == kListed && on ? 0.0f : e;
-      if constexpr (SECOND == kEntropy) X = __builtin_fmaf(e, fmaxf(d, -1000.0f), X);
-      if constexpr (SECOND == kListed) X += on ? e : 0.0f;
-    });
-    p.S = wave_sum(S);
-    if constexpr (SECOND != kAlone) p.X = wave_sum(X);
-  }
-  return p;
-}
-template <int SECOND>
-__device__ __forceinline__ Part see_from(Part p, float m, float c) {
-  rebase<SECOND>(p.S, p.X, (p.m - m) * c);
-  p.m = m;
-  return p;
-}
-// Two parts, or the parts that the lanes of a wave hold, as one.
-template <int SECOND>
-__device__ __forceinline__ Part join(const Part& p, const Part& q, float c) {
-  const float m = fmaxf(p.m, q.m);
-  const Part a = see_from<SECOND>(p, m, c), b = see_from<SECOND>(q, m, c);
-  return Part{m, a.S + b.S, a.X + b.X};
-}
-template <int SECOND>
-__device__ __forceinline__ Part join_lanes(const Part& p, float c) {
-  const Part q = see_from<SECOND>(p, wave_max(p.m), c);
-  return Part{q.m, wave_sum(q.S), SECOND != kAlone ? wave_sum(q.X) : 0.0f};
-}
-
-struct RowSums {  // the same in every thread of the row
-  float m;        // maximum, -inf for a row of nothing but -inf
-  float base;     // m, 0 for such a row
-  float S, X;     // the sums, d = (x - base) c
-  bool bad;       // the row holds a NaN or +inf
-};
-// The row from its waves' parts (`lds`: 3 * NT / 64 floats).
-template <int NT, int SECOND>
-__device__ __forceinline__ RowSums join_waves(Part p, int tid, float c, float* lds) {
-  constexpr int W = NT / 64;
-  if constexpr (W > 1) {
-    if ((tid & 63) == 0) {
-      lds[tid >> 6] = p.m;
-      lds[W + (tid >> 6)] = p.S;
-      lds[2 * W + (tid >> 6)] = p.X;
-    }
-    __syncthreads();
-    float M = lds[0], S = 0.0f, X = 0.0f;
-#pragma unroll
-    for (int w = 1; w < W; ++w) M = fmaxf(M, lds[w]);
-#pragma unroll
-    for (int w = 0; w < W; ++w) {
-      const Part q = see_from<SECOND>(Part{lds[w], lds[W + w], lds[2 * W + w]}, M, c);
-      S += q.S;
-      X += q.X;
-    }
-    p = Part{uniform_f(M), uniform_f(S), uniform_f(X)};
-  }
-  RowSums r{p.m, p.m == -INFINITY ? 0.0f : p.m, p.S, p.X, false};
-  r.bad = r.S != r.S || r.X != r.X || r.m == INFINITY;
-  return r;
+    for (int i = 0; i < n; ++i) x[i] += x[i + n];
+  return x[0];
 }
 
 }  // namespace lr

@@ -11,6 +11,139 @@ namespace {
 constexpr int kUnroll = 4;            // vectors of a thread in flight
 constexpr int kGroups = 256;          // parts of a row whose maxima bound the alternatives
 
+// Maximum, sum of exponentials and entropy in one pass.  With c = log2(e) / T every term is e = exp2(d), d = x c - rc, and the
+// reference rc = m c, m the largest element that the lane has seen: batch by batch (kUnroll vectors), since a move costs an
+// exponential and a product a sum.  So e <= 1, and the sum X of e d holds no term of the maximum's size that the entropy
+// would have to cancel.  The sum of the batch in which the maximum lies, P, is kept apart from the others', S, down to the
+// logarithm: log(P + S) = log1p((P - 1) + S), so that what lies beside a near-certain token is not rounded to its unit
+// (entropies of such rows: errors of 5e-6 without, 1e-7 with it).  d is rounded once; what rc was rounded by is the same for all terms and
+// comes off at the end.  Elements below -kFar / c are masks of a lowest value: nothing beside any ordinary logit.
+struct Sums {
+  float m = -INFINITY, thr, rc = 0.0f, P = 0.0f, S = 0.0f, X = 0.0f;
+  __device__ __forceinline__ explicit Sums(float far) : thr(-far) {}
+};
+// (S, X) seen from a reference that lies `apart` = rc - new rc higher.
+template <bool ENT>
+__device__ __forceinline__ void rebase(float& S, float& X, float apart) {
+  const float f = exp2_fast(apart);  // (may be infinite, or none, where the sums are 0)
+  if constexpr (ENT) X = S == 0.0f ? 0.0f : f * __builtin_fmaf(apart, S, X);
+  S = S == 0.0f ? 0.0f : f * S;
+}
+template <bool ENT, int U, int N>
+__device__ __forceinline__ void add_batch(Sums& s, const float (&x)[U][N], float m, float c) {
+  const bool up = m > s.thr;
+  if (__ballot(up) != 0) {
+    if (up) {
+      const float next = m * c;
+      s.S += s.P;
+      rebase<ENT>(s.S, s.X, s.rc - next);
+      s.rc = next;
+      s.thr = m;
+    }
+  }
+  float sum = 0.0f, sum_x = 0.0f;
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    float e[N], ed[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const float d = __builtin_fmaf(x[u][i], c, -s.rc);
+      e[i] = exp2_fast(d);
+      if constexpr (ENT) ed[i] = e[i] * fmaxf(d, -1000.0f);  // (-inf: nothing)
+    }
+    if constexpr (ENT) sum_x += vec_sum(ed);
+    sum += vec_sum(e);
+  }
+  s.P = up ? sum : s.P;
+  s.S += up ? 0.0f : sum;
+  if constexpr (ENT) s.X += sum_x;
+}
+
+// Sums of a part of a row, as above, with rc = m c (rounded; where m lies far from 0: d = (x - m) c).  A part of nothing but
+// -inf has sums of 0.
+struct Part {
+  float m, P, S, X;
+};
+// The parts that the lanes of a wave hold as one, the same in every lane: one lane's P stays apart.
+template <bool ENT>
+__device__ __forceinline__ Part join_lanes(float m, float rc, float P, float S, float X, float c) {
+  Part p;
+  p.m = wave_max(m);
+  const int first = wv::first_lane(__ballot(m == p.m) | (1ull << 63));
+  p.P = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(P), first));
+  if (static_cast<int>(threadIdx.x & 63) != first) {
+    S += P;
+    rebase<ENT>(S, X, fabsf(p.m) * c <= kFar ? rc - p.m * c : (m - p.m) * c);
+  }
+  p.S = wave_sum(S);
+  p.X = ENT ? wave_sum(X) : 0.0f;
+  return p;
+}
+// again(add) goes over the wave's elements a second time, where the maximum lies far from 0.
+template <bool ENT, typename Again>
+__device__ __forceinline__ Part wave_part(const Sums& s, float c, Again&& again) {
+  Part p = join_lanes<ENT>(s.m, s.rc, s.P, s.S, s.X, c);
+  if (!(fabsf(p.m) * c <= kFar) && fabsf(p.m) != INFINITY) {
+    float S = 0.0f, X = 0.0f;
+    again([&](float x) {
+      const float d = (x - p.m) * c, e = exp2_fast(d);
+      S += e;
+      if constexpr (ENT) X = __builtin_fmaf(e, fmaxf(d, -1000.0f), X);
+    });
+    p.P = wave_sum(S);
+    p.S = 0.0f;
+    p.X = ENT ? wave_sum(X) : 0.0f;
+  }
+  return p;
+}
+
+struct RowSums {  // the same in every thread of the row
+  float base;     // the maximum, 0 for a row of nothing but -inf
+  float m;        // the maximum
+  float log_s;    // log of the sum of exp((x - base) / T), 0 for such a row
+  float H;        // entropy
+  bool bad;       // the row holds a NaN or +inf
+};
+// The row from its waves' parts (`lds`: 4 * NT / 64 floats).
+template <int NT, bool ENT>
+__device__ __forceinline__ RowSums join_waves(Part p, int tid, float c, float* lds) {
+  constexpr int W = NT / 64;
+  if constexpr (W > 1) {
+    if ((tid & 63) == 0) {
+      lds[tid >> 6] = p.m;
+      lds[W + (tid >> 6)] = p.P;
+      lds[2 * W + (tid >> 6)] = p.S;
+      lds[3 * W + (tid >> 6)] = p.X;
+    }
+    __syncthreads();
+    p = Part{lds[0], 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int w = 1; w < W; ++w) p.m = fmaxf(p.m, lds[w]);
+    bool taken = false;
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+      const bool top = !taken && lds[w] == p.m;
+      float S = lds[2 * W + w] + (top ? 0.0f : lds[W + w]), X = lds[3 * W + w];
+      if (!top) rebase<ENT>(S, X, fabsf(p.m) * c <= kFar ? lds[w] * c - p.m * c : (lds[w] - p.m) * c);
+      p.P = top ? lds[W + w] : p.P;
+      p.S += S;
+      p.X += X;
+      taken = taken || top;
+    }
+    p = Part{uniform_f(p.m), uniform_f(p.P), uniform_f(p.S), uniform_f(p.X)};
+  }
+  const bool empty = p.m == -INFINITY;
+  const float S = p.P + p.S, mc = p.m * c, rounded = fabsf(mc) <= kFar ? __builtin_fmaf(p.m, c, -mc) : 0.0f;
+  const float log_s = log1pf((p.P - 1.0f) + p.S);
+  RowSums r;
+  r.bad = S != S || p.m == INFINITY;
+  r.m = r.bad ? NAN : p.m;
+  r.base = empty ? 0.0f : p.m;
+  r.log_s = r.bad ? NAN : empty ? 0.0f : log_s - rounded * kLn2;
+  r.H = r.bad ? NAN : empty ? 0.0f : log_s - p.X * kLn2 / S;
+  return r;
+}
+
 // The alternatives.  Every lane keeps the largest element of its vectors (m1), the first vector that holds it (k1) and the
 // largest element of its other vectors (m2).  The N-th largest of the lanes' (or, past 256 threads, of 256 groups of
 // lanes') m1 is a bound that N elements reach; hardly more than those lie above it (with G groups G ln(G / (G - N)) are
@@ -202,24 +335,20 @@ __device__ __forceinline__ void write_alternatives(const Row<E>& row, int tid, c
 }
 
 // What a row's sums say, and the scores of the given tokens.
-__device__ __forceinline__ float write_scores(const LogprobArgs& a, int64_t r, int tid, const RowSums& sums, int given, float given_x) {
-  const bool empty = sums.m == -INFINITY;
-  const float logs = sums.bad ? NAN : empty ? 0.0f : logf(sums.S);
-  if (tid < a.n_tokens) a.logp[r * a.n_tokens + tid] = given < 0 ? NAN : (given_x - sums.base) * a.in.inv_temp - logs;
+__device__ __forceinline__ void write_scores(const LogprobArgs& a, int64_t r, int tid, const RowSums& sums, int given, float given_x) {
+  if (tid < a.n_tokens) a.logp[r * a.n_tokens + tid] = given < 0 ? NAN : (given_x - sums.base) * a.in.inv_temp - sums.log_s;
   if (tid == 0) {
-    const float H = sums.bad ? NAN : empty ? 0.0f : logs - sums.X * kLn2 / sums.S;
-    if (a.entropy) a.entropy[r] = H;
+    if (a.entropy) a.entropy[r] = sums.H;
     if (a.stats) {
-      a.stats[3 * r + 0] = sums.bad ? NAN : sums.m;
-      a.stats[3 * r + 1] = logs;
-      a.stats[3 * r + 2] = H;
+      a.stats[3 * r + 0] = sums.m;
+      a.stats[3 * r + 1] = sums.log_s;
+      a.stats[3 * r + 2] = sums.H;
     }
   }
   if (sums.bad && tid < a.n_top) {
     a.top_tokens[r * a.n_top + tid] = -1;
     a.top_logp[r * a.n_top + tid] = NAN;
   }
-  return logs;
 }
 template <typename E>
 __device__ __forceinline__ int load_given(const LogprobArgs& a, int64_t r, const Row<E>& row, int tid, float& x) {
@@ -234,33 +363,39 @@ __device__ __forceinline__ int load_given(const LogprobArgs& a, int64_t r, const
 // One row.  NT == 64: a wave of its own, kThreads / 64 of them in a workgroup.
 template <typename E, int NT, bool ENT, bool TOP>
 __global__ __launch_bounds__(NT == 64 ? 256 : NT) void logprobs_kernel(LogprobArgs a) {
-  constexpr int ROWS = NT == 64 ? 4 : 1, SECOND = ENT ? kEntropy : kAlone;
-  __shared__ float s_sums[ROWS][3 * NT / 64];
+  constexpr int ROWS = NT == 64 ? 4 : 1;
+  __shared__ float s_sums[ROWS][4 * NT / 64];
   __shared__ TopLds<TOP ? NT : 64, TOP ? E::N : 1> s_top[TOP ? ROWS : 1];
   const int sub = NT == 64 ? uniform_i(threadIdx.x >> 6) : 0, tid = NT == 64 ? threadIdx.x & 63 : threadIdx.x;
   const int64_t r = static_cast<int64_t>(blockIdx.x) * ROWS + sub;
   if (ROWS > 1 && r >= a.in.rows) return;
   const Row<E> row = row_at<E>(a.in.x, a.in.stride, r, a.in.V);
-  const float inv = a.in.inv_temp, c = inv * kLog2e, room = kRoom / c;
+  const float inv = a.in.inv_temp, c = inv * kLog2e;
   float given_x;  // (on its way during the pass)
   const int given = load_given<E>(a, r, row, tid, given_x);
   Sums s(kFar / c);
   Tops tops;
   const int whole = row.nv / (kUnroll * NT);
-  auto one = [&](const v4u& raw, int k) {
-    float x[E::N];
-    E::unpack(raw, x);
-    const float vm = vec_max(x);
-    if constexpr (TOP) tops.add(vm, k);
-    else s.m = fmaxf(s.m, vm);
-    add_vector<SECOND>(s, x, vm, c, room);
+  auto batch = [&](auto& x, int k) {  // (vectors k, k + 1, ... of the thread)
+    constexpr int U = sizeof(x) / sizeof(x[0]);
+    float m = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const float vm = vec_max(x[u]);
+      if constexpr (TOP) tops.add(vm, k + u);
+      m = fmaxf(m, vm);
+    }
+    s.m = fmaxf(s.m, m);
+    add_batch<ENT>(s, x, m, c);
   };
   for (int b = 0; b < whole; ++b) {
     v4u raw[kUnroll];
+    float x[kUnroll][E::N];
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) raw[u] = row.vec((b * kUnroll + u) * NT + tid);
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) one(raw[u], b * kUnroll + u);
+    for (int u = 0; u < kUnroll; ++u) E::unpack(raw[u], x[u]);
+    batch(x, b * kUnroll);
   }
   {
     v4u raw[kUnroll];
@@ -269,29 +404,33 @@ __global__ __launch_bounds__(NT == 64 ? 256 : NT) void logprobs_kernel(LogprobAr
       if ((whole * kUnroll + u) * NT + tid < row.nv) raw[u] = row.vec((whole * kUnroll + u) * NT + tid);
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u)
-      if ((whole * kUnroll + u) * NT + tid < row.nv) one(raw[u], whole * kUnroll + u);
+      if ((whole * kUnroll + u) * NT + tid < row.nv) {
+        float x[1][E::N];
+        E::unpack(raw[u], x[0]);
+        batch(x, whole * kUnroll + u);
+      }
   }
   float edge = -INFINITY;
   if (tid < row.edges) {
     edge = E::up(row.x[row.edge_token(tid)]);
-    const float x[1] = {edge};
-    add_vector<SECOND>(s, x, edge, c, room);
+    const float x[1][1] = {{edge}};
+    s.m = fmaxf(s.m, edge);
+    add_batch<ENT>(s, x, edge, c);
   }
-  s.m = fmaxf(TOP ? tops.m1 : s.m, edge);
-  const Part part = wave_part<SECOND>(s, c, [&](auto&& add) {
+  const Part part = wave_part<ENT>(s, c, [&](auto&& add) {
     for (int v = tid; v < row.nv; v += NT) {
       float x[E::N];
       E::unpack(row.vec(v), x);
 #pragma unroll
-      for (int i = 0; i < E::N; ++i) add(x[i], false);
+      for (int i = 0; i < E::N; ++i) add(x[i]);
     }
-    if (tid < row.edges) add(edge, false);
+    if (tid < row.edges) add(edge);
   });
-  const RowSums sums = join_waves<NT, SECOND>(part, tid, c, s_sums[sub]);
-  const float logs = write_scores(a, r, tid, sums, given, given_x);
+  const RowSums sums = join_waves<NT, ENT>(part, tid, c, s_sums[sub]);
+  write_scores(a, r, tid, sums, given, given_x);
   if constexpr (TOP) {
     if (!sums.bad)
-      write_alternatives<E, NT>(row, tid, tops, edge, TopOut{a.n_top, sums.base, inv, logs, a.top_tokens + r * a.n_top, a.top_logp + r * a.n_top},
+      write_alternatives<E, NT>(row, tid, tops, edge, TopOut{a.n_top, sums.base, inv, sums.log_s, a.top_tokens + r * a.n_top, a.top_logp + r * a.n_top},
                                 s_top[sub]);
   }
 }
@@ -301,47 +440,46 @@ __global__ __launch_bounds__(NT == 64 ? 256 : NT) void logprobs_kernel(LogprobAr
 // parts that reach the bound are read again.
 template <typename E, bool ENT>
 __global__ __launch_bounds__(256) void logprobs_parts_kernel(LogprobArgs a, int parts, int each, float4* __restrict__ out) {
-  constexpr int SECOND = ENT ? kEntropy : kAlone;
   const int64_t at = static_cast<int64_t>(blockIdx.x) * 4 + uniform_i(threadIdx.x >> 6);
   const int64_t r = at / parts;
   if (r >= a.in.rows) return;
   const int lane = threadIdx.x & 63, begin = static_cast<int>(at - r * parts) * 64 * each;
   const Row<E> row = row_at<E>(a.in.x, a.in.stride, r, a.in.V);
-  const float c = a.in.inv_temp * kLog2e, room = kRoom / c;
+  const float c = a.in.inv_temp * kLog2e;
   const int end = min(begin + 64 * each, row.nv);
   Sums s(kFar / c);
   for (int v = begin + lane; v < end; v += 64) {
-    float x[E::N];
-    E::unpack(row.vec(v), x);
-    const float vm = vec_max(x);
+    float x[1][E::N];
+    E::unpack(row.vec(v), x[0]);
+    const float vm = vec_max(x[0]);
     s.m = fmaxf(s.m, vm);
-    add_vector<SECOND>(s, x, vm, c, room);
+    add_batch<ENT>(s, x, vm, c);
   }
   const bool has_edge = begin == 0 && lane < row.edges;  // (the first part has the edge as well)
   float edge = -INFINITY;
   if (has_edge) {
     edge = E::up(row.x[row.edge_token(lane)]);
-    const float x[1] = {edge};
+    const float x[1][1] = {{edge}};
     s.m = fmaxf(s.m, edge);
-    add_vector<SECOND>(s, x, edge, c, room);
+    add_batch<ENT>(s, x, edge, c);
   }
-  const Part p = wave_part<SECOND>(s, c, [&](auto&& add) {
+  const Part p = wave_part<ENT>(s, c, [&](auto&& add) {
     for (int v = begin + lane; v < end; v += 64) {
       float x[E::N];
       E::unpack(row.vec(v), x);
 #pragma unroll
-      for (int i = 0; i < E::N; ++i) add(x[i], false);
+      for (int i = 0; i < E::N; ++i) add(x[i]);
     }
-    if (has_edge) add(edge, false);
+    if (has_edge) add(edge);
   });
-  if (lane == 0) out[at] = make_float4(p.m, p.S, p.X, 0.0f);
+  if (lane == 0) out[at] = make_float4(p.m, p.P, p.S, p.X);
 }
 
 constexpr int kJoinThreads = 1024;
 template <typename E, bool ENT, bool TOP>
 __global__ __launch_bounds__(kJoinThreads) void logprobs_join_kernel(LogprobArgs a, int parts, int each, const float4* __restrict__ in) {
-  constexpr int SECOND = ENT ? kEntropy : kAlone, NT = kJoinThreads, W = NT / 64;
-  __shared__ float s_sums[3 * W];
+  constexpr int NT = kJoinThreads, W = NT / 64;
+  __shared__ float s_sums[4 * W];
   __shared__ TopLds<TOP ? NT : 64, TOP ? E::N : 1> lds;
   __shared__ int s_found[W];
   const int64_t r = blockIdx.x;
@@ -350,20 +488,20 @@ __global__ __launch_bounds__(kJoinThreads) void logprobs_join_kernel(LogprobArgs
   const float c = a.in.inv_temp * kLog2e;
   float given_x;
   const int given = load_given<E>(a, r, row, tid, given_x);
-  Part p{-INFINITY, 0.0f, 0.0f};
+  Part p{-INFINITY, 0.0f, 0.0f, 0.0f};
   if (tid < parts) {
     const float4 q = in[r * parts + tid];
-    p = Part{q.x, q.y, q.z};
+    p = Part{q.x, q.y, q.z, q.w};
   }
   const bool some = tid < parts && (tid == 0 || tid * 64 * each < row.nv);  // (a row's head may leave its last part empty)
   const unsigned own = some ? order32(p.m) : 0u;
   float edge = -INFINITY;
   if (tid < row.edges) edge = E::up(row.x[row.edge_token(tid)]);
-  const RowSums sums = join_waves<NT, SECOND>(join_lanes<SECOND>(p, c), tid, c, s_sums);
-  const float logs = write_scores(a, r, tid, sums, given, given_x);
+  const RowSums sums = join_waves<NT, ENT>(join_lanes<ENT>(p.m, p.m * c, p.P, p.S, p.X, c), tid, c, s_sums);
+  write_scores(a, r, tid, sums, given, given_x);
   if constexpr (TOP) {
     if (sums.bad) return;
-    const TopOut out{a.n_top, sums.base, a.in.inv_temp, logs, a.top_tokens + r * a.n_top, a.top_logp + r * a.n_top};
+    const TopOut out{a.n_top, sums.base, a.in.inv_temp, sums.log_s, a.top_tokens + r * a.n_top, a.top_logp + r * a.n_top};
     if (tid == 0) lds.count = lds.first[kGroups] = 0;
     if (tid < kGroups) lds.group[tid] = own;
     __syncthreads();
