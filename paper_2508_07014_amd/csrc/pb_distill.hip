@@ -8,15 +8,12 @@ namespace pb {
 namespace lr {
 namespace {
 
-// Maximum and sums of exponentials in one pass.  With c = log2(e) / T every term is e = exp2(d), d = x c - rc; the reference
-// rc is the lane's own and is moved, with the sums, only when an element exceeds it by more than 2^kRoom: the first vector
-// sets it, after that a lane hardly ever comes back (one fused multiply-add and one exponential a term, no running maximum
-// in the chain).  d is rounded once; what rc itself was rounded by is the same for all terms of the lane, and is made up for
-// at the end (wave_part).  Elements below -kFar / c are masks of a lowest value: nothing beside any ordinary logit.
-// With LISTED a second sum takes the terms of listed tokens, which the first one then lacks.
-constexpr float kRoom = 30.0f;
-
-// (S, X) seen from a reference that lies `apart` = rc - new rc higher.
+// Sums of exponentials: every term is e = exp2(d), d = x c - rc with c = log2(e) / T and the reference rc = m c, m the largest
+// element that the lane has seen (a reference below the maximum would add its distance to the rounding of d).  d is rounded
+// once; what rc itself was rounded by is the same for all terms of the lane and is made up for at the end (wave_part).
+// Elements below -kFar / c are masks of a lowest value: nothing beside any ordinary logit.  With LISTED a second sum, X,
+// takes the terms of listed tokens, which S then lacks.
+// (S, X) seen from a reference that lies `apart` = rc - new rc higher:
 template <bool LISTED>
 __device__ __forceinline__ void rebase(float& S, float& X, float apart) {
   const float f = exp2_fast(apart);  // (may be infinite where the sums are 0)
@@ -27,17 +24,21 @@ struct Sums {
   float rc = 0.0f, thr, S = 0.0f, X = 0.0f, m = -INFINITY;
   __device__ __forceinline__ explicit Sums(float far) : thr(-far) {}
 };
-// A vector into the sums; `vm` its largest element, `listed` a bit per element that goes to the second sum.
-template <bool LISTED, int N>
-__device__ __forceinline__ void add_vector(Sums& s, const float (&x)[N], float vm, float c, float room, unsigned listed = 0u) {
-  if (__ballot(vm > s.thr) != 0) {  // (of the wave: a branch, not selects in every vector)
-    if (vm > s.thr) {
-      const float next = vm * c;
+// Moves the reference to `m`, the largest of the elements that are about to be added, if they exceed it.
+template <bool LISTED>
+__device__ __forceinline__ void look_at(Sums& s, float m, float c) {
+  s.m = fmaxf(s.m, m);
+  if (__ballot(m > s.thr) != 0) {  // (of the wave: a branch, not selects)
+    if (m > s.thr) {
+      const float next = m * c;
       rebase<LISTED>(s.S, s.X, s.rc - next);
       s.rc = next;
-      s.thr = vm + room;
+      s.thr = m;
     }
   }
+}
+template <bool LISTED, int N>
+__device__ __forceinline__ void add_vector(Sums& s, const float (&x)[N], float c, unsigned listed) {  // (a bit per element)
   float e[N];
 #pragma unroll
   for (int i = 0; i < N; ++i) e[i] = exp2_fast(__builtin_fmaf(x[i], c, -s.rc));
@@ -73,7 +74,7 @@ __device__ __forceinline__ Part wave_part(const Sums& s, float c, Again&& again)
     again([&](float x, bool on) {
       const float d = (x - p.m) * c, e = exp2_fast(d);
       S += LISTED && on ? 0.0f : e;
-          if constexpr (LISTED) X += on ? e : 0.0f;
+      if constexpr (LISTED) X += on ? e : 0.0f;
     });
     p.S = wave_sum(S);
     if constexpr (LISTED) p.X = wave_sum(X);
@@ -230,6 +231,13 @@ __device__ __forceinline__ float loss_and_own(const DistillArgs& a, int64_t r, i
   return (expf(static_cast<float>(lp)) * list.Q - mass) * w * inv;
 }
 
+// Has the compiler unpack held vectors again, rather than keep them unpacked in twice the registers.
+template <int HELD>
+__device__ __forceinline__ void reload(v4u (&held)[HELD]) {
+#pragma unroll
+  for (int u = 0; u < HELD; ++u) asm volatile("" : "+v"(held[u]));
+}
+
 // One row, by a wave (four rows a workgroup) or a workgroup.  Thread t holds vectors t, t + NT, ... of the row, HELD of them
 // in registers; what a row has beyond HELD * NT vectors is read a second time for the gradient (from cache: only the rows
 // at work are in between).  With TAIL the tokens that are not listed have a sum of their own, so that little mass does not
@@ -253,7 +261,7 @@ __global__ __launch_bounds__(NT == 64 ? 256 : NT) void distill_kernel(DistillArg
   }
   float edge = -INFINITY;
   if (tid < row.edges) edge = E::up(row.x[row.edge_token(tid)]);
-  const float w = a.row_grads ? a.row_grads[r] : 1.0f, inv = a.in.inv_temp, c = inv * kLog2e, room = kRoom / c;
+  const float w = a.row_grads ? a.row_grads[r] : 1.0f, inv = a.in.inv_temp, c = inv * kLog2e;
   const bool lister = NT == 64 || tid < 64;
   if constexpr (TAIL) {
     for (int i = tid; i < mark_bytes / 4; i += NT) reinterpret_cast<unsigned*>(marks)[i] = 0u;
@@ -292,21 +300,32 @@ __global__ __launch_bounds__(NT == 64 ? 256 : NT) void distill_kernel(DistillArg
   Sums s(kFar / c);
   auto listed = [&](int v) -> unsigned { return !TAIL ? 0u : E::N == 8 ? marks[v] : (marks[v >> 1] >> (4 * (v & 1))) & 15u; };
   auto edge_listed = [&](int t) -> bool { return TAIL && ((s_edge[sub] >> t) & 1u); };
-  auto one = [&](const v4u& raw, int v) {
-    float x[E::N];
-    E::unpack(raw, x);
-    const float vm = vec_max(x);
-    s.m = fmaxf(s.m, vm);
-    add_vector<TAIL>(s, x, vm, c, room, listed(v));
-  };
+  float most = edge;
 #pragma unroll
   for (int u = 0; u < HELD; ++u)
-    if (u * NT + tid < row.nv) one(held[u], u * NT + tid);
-  for (int v = HELD * NT + tid; v < row.nv; v += NT) one(row.vec(v), v);
+    if (u * NT + tid < row.nv) {
+      float x[E::N];
+      E::unpack(held[u], x);
+      most = fmaxf(most, vec_max(x));
+    }
+  look_at<TAIL>(s, most, c);
+  reload(held);
+#pragma unroll
+  for (int u = 0; u < HELD; ++u)
+    if (u * NT + tid < row.nv) {
+      float x[E::N];
+      E::unpack(held[u], x);
+      add_vector<TAIL>(s, x, c, listed(u * NT + tid));
+    }
   if (tid < row.edges) {
     const float x[1] = {edge};
-    s.m = fmaxf(s.m, edge);
-    add_vector<TAIL>(s, x, edge, c, room, edge_listed(tid) ? 1u : 0u);
+    add_vector<TAIL>(s, x, c, edge_listed(tid) ? 1u : 0u);
+  }
+  for (int v = HELD * NT + tid; v < row.nv; v += NT) {
+    float x[E::N];
+    E::unpack(row.vec(v), x);
+    look_at<TAIL>(s, vec_max(x), c);
+    add_vector<TAIL>(s, x, c, listed(v));
   }
   const Part part = wave_part<TAIL>(s, c, [&](auto&& add) {
     for (int v = tid; v < row.nv; v += NT) {
@@ -338,8 +357,7 @@ __global__ __launch_bounds__(NT == 64 ? 256 : NT) void distill_kernel(DistillArg
     store_vector<E>(out + row.token(v, 0), E::pack(x));
   };
   if constexpr (NT > 64) __syncthreads();
-#pragma unroll
-  for (int u = 0; u < HELD; ++u) asm volatile("" : "+v"(held[u]));  // (unpacked again, not kept unpacked: 80 registers -> 50)
+  reload(held);
 #pragma unroll
   for (int u = 0; u < HELD; ++u)
     if (u * NT + tid < row.nv) put(held[u], u * NT + tid);
@@ -367,7 +385,7 @@ __global__ __launch_bounds__(256) void distill_parts_kernel(DistillArgs a, int p
   if (r >= a.in.rows) return;
   const int begin = static_cast<int>(at - r * parts) * 64 * each;
   const Row<E> row = row_at<E>(a.in.x, a.in.stride, r, a.in.V);
-  const float c = a.in.inv_temp * kLog2e, room = kRoom / c;
+  const float c = a.in.inv_temp * kLog2e;
   const int end = min(begin + 64 * each, row.nv);
   if (begin == 0) {
     Entry e;
@@ -396,9 +414,8 @@ __global__ __launch_bounds__(256) void distill_parts_kernel(DistillArgs a, int p
   for (int v = begin + lane; v < end; v += 64) {
     float x[E::N];
     E::unpack(row.vec(v), x);
-    const float vm = vec_max(x);
-    s.m = fmaxf(s.m, vm);
-    add_vector<TAIL>(s, x, vm, c, room, listed(v));
+    look_at<TAIL>(s, vec_max(x), c);
+    add_vector<TAIL>(s, x, c, listed(v));
   }
   const bool has_edge = begin == 0 && lane < row.edges;
   const bool on_edge = TAIL && has_edge && ((s_edge[sub] >> lane) & 1u);
@@ -406,8 +423,8 @@ __global__ __launch_bounds__(256) void distill_parts_kernel(DistillArgs a, int p
   if (has_edge) {
     edge = E::up(row.x[row.edge_token(lane)]);
     const float x[1] = {edge};
-    s.m = fmaxf(s.m, edge);
-    add_vector<TAIL>(s, x, edge, c, room, on_edge ? 1u : 0u);
+    look_at<TAIL>(s, edge, c);
+    add_vector<TAIL>(s, x, c, on_edge ? 1u : 0u);
   }
   const Part p = wave_part<TAIL>(s, c, [&](auto&& add) {
     for (int v = begin + lane; v < end; v += 64) {
