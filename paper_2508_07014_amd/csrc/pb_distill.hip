@@ -367,6 +367,8 @@ __global__ __launch_bounds__(NT == 64 ? 256 : NT) void distill_kernel(DistillArg
   if (lister && e.token >= 0) out[e.token] = E::down(own);
 }
 
+constexpr int kGradUnroll = 4;
+
 // Few long rows, and rows too long for the registers of a workgroup: every wave takes 64 * `each` vectors of a row and
 // leaves their part of the sums in the workspace (the first one also the list's, and the student's logits on it, since the
 // gradient may take the logits' place); the second kernel joins the parts and writes the gradient.
@@ -411,11 +413,19 @@ __global__ __launch_bounds__(256) void distill_parts_kernel(DistillArgs a, int p
   }
   auto listed = [&](int v) -> unsigned { return TAIL ? reinterpret_cast<const unsigned char*>(s_marks[sub])[v - begin] : 0u; };
   Sums s(kFar / c);
-  for (int v = begin + lane; v < end; v += 64) {
-    float x[E::N];
-    E::unpack(row.vec(v), x);
-    look_at<TAIL>(s, vec_max(x), c);
-    add_vector<TAIL>(s, x, c, listed(v));
+  for (int v0 = begin + lane; v0 < end; v0 += 64 * kGradUnroll) {
+    v4u raw[kGradUnroll];
+#pragma unroll
+    for (int u = 0; u < kGradUnroll; ++u)
+      if (v0 + 64 * u < end) raw[u] = row.vec(v0 + 64 * u);
+#pragma unroll
+    for (int u = 0; u < kGradUnroll; ++u)
+      if (v0 + 64 * u < end) {
+        float x[E::N];
+        E::unpack(raw[u], x);
+        look_at<TAIL>(s, vec_max(x), c);
+        add_vector<TAIL>(s, x, c, listed(v0 + 64 * u));
+      }
   }
   const bool has_edge = begin == 0 && lane < row.edges;
   const bool on_edge = TAIL && has_edge && ((s_edge[sub] >> lane) & 1u);
@@ -439,7 +449,6 @@ __global__ __launch_bounds__(256) void distill_parts_kernel(DistillArgs a, int p
   if (lane == 0) ws.parts[at] = make_float4(p.m, p.S, p.X, 0.0f);
 }
 
-constexpr int kGradUnroll = 4;
 template <typename E, bool TAIL>
 __global__ __launch_bounds__(256) void distill_grad_kernel(DistillArgs a, int parts, int blocks, DistillSpace ws) {
   constexpr int BLOCK = 256 * kGradUnroll;
@@ -469,7 +478,6 @@ __global__ __launch_bounds__(256) void distill_grad_kernel(DistillArgs a, int pa
   const bool learn = list.any != 0, none = !learn || sums.m == -INFINITY || w == 0.0f;
   Entry e{-1, 0.0f, -INFINITY, 0.0f};
   bool mine = false;  // the lane's listed token lies in this block, whose first wave writes it after the other stores
-  float own = 0.0f;
   if (tid < 64) {
     if (learn && tid < a.K) {
       const int t = a.tokens[r * a.K + tid];
@@ -481,24 +489,32 @@ __global__ __launch_bounds__(256) void distill_grad_kernel(DistillArgs a, int pa
         mine = block == (t < row.head || t >= row.head + row.nv * E::N ? 0 : (t - row.head) / E::N / BLOCK);
       }
     }
-    if (!learn && block == 0 && a.loss && tid == 0) a.loss[r] = 0.0f;
-    DistillArgs loss_of = a;
-    if (block != 0 || !learn) loss_of.loss = nullptr;
-    if (loss_of.loss || __ballot(mine) != 0) own = loss_and_own<TAIL>(loss_of, r, tid, e, list, sums, st, w, inv);
   }
-  if (!out) return;
+  if (out) {
 #pragma unroll
-  for (int u = 0; u < kGradUnroll; ++u) {
-    const int v = block * BLOCK + u * 256 + tid;
-    if (v < row.nv) {
-      float x[E::N];
-      E::unpack(raw[u], x);
+    for (int u = 0; u < kGradUnroll; ++u) {
+      const int v = block * BLOCK + u * 256 + tid;
+      if (v < row.nv) {
+        float x[E::N];
+        E::unpack(raw[u], x);
 #pragma unroll
-      for (int i = 0; i < E::N; ++i) x[i] = none ? 0.0f : exp2_fast((x[i] - sums.base) * c) * st.A;
-      store_vector<E>(out + row.token(v, 0), E::pack(x));
+        for (int i = 0; i < E::N; ++i) x[i] = none ? 0.0f : exp2_fast((x[i] - sums.base) * c) * st.A;
+        store_vector<E>(out + row.token(v, 0), E::pack(x));
+      }
+    }
+    if (has_edge) out[row.edge_token(tid)] = E::down(none ? 0.0f : exp2_fast((edge - sums.base) * c) * st.A);
+  }
+  float own = 0.0f;
+  if (tid < 64) {
+    const bool first = block == 0 && a.loss;
+    if (first && !learn && tid == 0) a.loss[r] = 0.0f;
+    if (learn && (first || __ballot(mine) != 0)) {
+      DistillArgs b = a;
+      if (!first) b.loss = nullptr;
+      own = loss_and_own<TAIL>(b, r, tid, e, list, sums, st, w, inv);
     }
   }
-  if (has_edge) out[row.edge_token(tid)] = E::down(none ? 0.0f : exp2_fast((edge - sums.base) * c) * st.A);
+  if (!out) return;
   __syncthreads();
   if (mine && !none) out[e.token] = E::down(own);
 }

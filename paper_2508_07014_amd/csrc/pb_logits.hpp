@@ -53,15 +53,20 @@ struct DistillArgs {
 };
 
 // Few long rows are split over the chip: `parts` waves a row, each with 64 * `each` vectors of 16 bytes (0: not split).
-// At most kMaxParts, so that one workgroup can join them.
+// At most kMaxParts, so that one wave can join them; at least kLeastParts, whose maxima are to bound 64 alternatives; and
+// about kSplitWaves in all, four vectors a lane where there is so much.
 constexpr int kWaveVectors = 512;  // longest row that one wave takes, in vectors
-constexpr int kMaxParts = 256, kMaxEach = (kLogitsMaxV / 4 + 64 * kMaxParts - 1) / (64 * kMaxParts);
+constexpr int kMaxParts = 256, kLeastParts = 80, kSplitWaves = 4096, kSplitRows = 256;
+constexpr int kMaxEach = 8;  // (the marks of a part's listed tokens lie in LDS)
+static_assert(kMaxEach * 64 * kMaxParts >= kLogitsMaxV / 4, "the widest row is split");
 struct RowSplit {
   int parts, each;
 };
 inline RowSplit row_split(int vectors, int32_t rows) {
-  if (vectors < 5120 || rows >= 256) return RowSplit{0, 0};
-  const int each = (vectors + 64 * kMaxParts - 1) / (64 * kMaxParts);
+  if (vectors < 64 * kLeastParts || rows >= kSplitRows) return RowSplit{0, 0};
+  const int least = (vectors + 64 * kMaxParts - 1) / (64 * kMaxParts), most = vectors / (64 * kLeastParts) < kMaxEach ? vectors / (64 * kLeastParts) : kMaxEach;
+  const int64_t want = static_cast<int64_t>(rows) * vectors / (64 * kSplitWaves);
+  const int each = static_cast<int>(want < least ? least : want > most ? (most > least ? most : least) : want);
   return RowSplit{(vectors + 64 * each - 1) / (64 * each), each};
 }
 

@@ -61,7 +61,7 @@ __device__ __forceinline__ void add_batch(Sums& s, const float (&x)[U][N], float
 
 // Sums of a part of a row, as above, with rc = m c (rounded; where m lies far from 0: d = (x - m) c).  A part of nothing but
 // -inf has sums of 0.
-struct Part {
+struct __align__(16) Part {
   float m, P, S, X;
 };
 // The parts that the lanes of a wave hold as one, the same in every lane: one lane's P stays apart.
@@ -97,6 +97,27 @@ __device__ __forceinline__ Part wave_part(const Sums& s, float c, Again&& again)
   return p;
 }
 
+// W parts as one.
+template <bool ENT, int W>
+__device__ __forceinline__ Part join_set(const Part (&q)[W], float c) {
+  Part p{q[0].m, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+  for (int w = 1; w < W; ++w) p.m = fmaxf(p.m, q[w].m);
+  bool taken = false;
+#pragma unroll
+  for (int w = 0; w < W; ++w) {
+    const bool top = !taken && q[w].m == p.m;
+    float S = q[w].S + (top ? 0.0f : q[w].P), X = q[w].X;
+    float S1 = S, X1 = X;
+    rebase<ENT>(S1, X1, fabsf(p.m) * c <= kFar ? q[w].m * c - p.m * c : (q[w].m - p.m) * c);
+    p.P = top ? q[w].P : p.P;
+    p.S += top ? S : S1;
+    p.X += top ? X : X1;
+    taken = taken || top;
+  }
+  return p;
+}
+
 struct RowSums {  // the same in every thread of the row
   float base;     // the maximum, 0 for a row of nothing but -inf
   float m;        // the maximum
@@ -104,34 +125,7 @@ struct RowSums {  // the same in every thread of the row
   float H;        // entropy
   bool bad;       // the row holds a NaN or +inf
 };
-// The row from its waves' parts (`lds`: 4 * NT / 64 floats).
-template <int NT, bool ENT>
-__device__ __forceinline__ RowSums join_waves(Part p, int tid, float c, float* lds) {
-  constexpr int W = NT / 64;
-  if constexpr (W > 1) {
-    if ((tid & 63) == 0) {
-      lds[tid >> 6] = p.m;
-      lds[W + (tid >> 6)] = p.P;
-      lds[2 * W + (tid >> 6)] = p.S;
-      lds[3 * W + (tid >> 6)] = p.X;
-    }
-    __syncthreads();
-    p = Part{lds[0], 0.0f, 0.0f, 0.0f};
-#pragma unroll
-    for (int w = 1; w < W; ++w) p.m = fmaxf(p.m, lds[w]);
-    bool taken = false;
-#pragma unroll
-    for (int w = 0; w < W; ++w) {
-      const bool top = !taken && lds[w] == p.m;
-      float S = lds[2 * W + w] + (top ? 0.0f : lds[W + w]), X = lds[3 * W + w];
-      if (!top) rebase<ENT>(S, X, fabsf(p.m) * c <= kFar ? lds[w] * c - p.m * c : (lds[w] - p.m) * c);
-      p.P = top ? lds[W + w] : p.P;
-      p.S += S;
-      p.X += X;
-      taken = taken || top;
-    }
-    p = Part{uniform_f(p.m), uniform_f(p.P), uniform_f(p.S), uniform_f(p.X)};
-  }
+__device__ __forceinline__ RowSums finish(const Part& p, float c) {
   const bool empty = p.m == -INFINITY;
   const float S = p.P + p.S, mc = p.m * c, rounded = fabsf(mc) <= kFar ? __builtin_fmaf(p.m, c, -mc) : 0.0f;
   const float log_s = log1pf((p.P - 1.0f) + p.S);
@@ -142,6 +136,24 @@ __device__ __forceinline__ RowSums join_waves(Part p, int tid, float c, float* l
   r.log_s = r.bad ? NAN : empty ? 0.0f : log_s - rounded * kLn2;
   r.H = r.bad ? NAN : empty ? 0.0f : log_s - p.X * kLn2 / S;
   return r;
+}
+
+// The row from its waves' parts (`lds`: NT / 64 of them).
+template <int NT, bool ENT>
+__device__ __forceinline__ RowSums join_waves(const Part& p, int tid, float c, Part* lds) {
+  constexpr int W = NT / 64;
+  if constexpr (W == 1) return finish(p, c);
+  if ((tid & 63) == 0) lds[tid >> 6] = p;
+  __syncthreads();
+  if constexpr (W <= 4) {
+    Part q[W];
+#pragma unroll
+    for (int w = 0; w < W; ++w) q[w] = lds[w];
+    return finish(join_set<ENT, W>(q, c), c);
+  }
+  // (a lane each: the waves of one row share a CU, and sixteen joins one after the other took longer than the reductions)
+  const Part q = (tid & 63) < W ? lds[tid & 63] : Part{-INFINITY, 0.0f, 0.0f, 0.0f};
+  return finish(join_lanes<ENT>(q.m, q.m * c, q.P, q.S, q.X, c), c);
 }
 
 // The alternatives.  Every lane keeps the largest element of its vectors (m1), the first vector that holds it (k1) and the
@@ -181,16 +193,25 @@ __device__ __forceinline__ int how_many(const unsigned (&key)[PER], unsigned b) 
   for (int i = 0; i < PER; ++i) n += __builtin_popcountll(__ballot(key[i] >= b));
   return n;
 }
+// Halving between 0 .. the largest key: about ln2(groups) steps until exactly n reach the middle, 32 at most (equal keys).
 template <int PER>
 __device__ __forceinline__ unsigned bound_of(const unsigned (&key)[PER], int n) {
-  unsigned b = 0;
-  for (int bit = 31; bit >= 0; --bit) {
-    const unsigned t = b | (1u << bit);
-    const int got = how_many(key, t);
-    if (got >= n) b = t;
-    if (got == n) break;
+  if (how_many(key, 1u) < n) return 0u;
+  unsigned most = key[0], least = key[0] - 1u;  // (a key of 0 is none)
+#pragma unroll
+  for (int i = 1; i < PER; ++i) {
+    most = max(most, key[i]);
+    least = min(least, key[i] - 1u);
   }
-  return b;
+  unsigned lo = ~wv::wave_max_u(~least) + 1u, hi = wv::wave_max_u(most);  // n keys or more reach lo, fewer reach hi + 1
+  while (lo < hi) {
+    const unsigned mid = lo + (hi - lo) / 2 + 1;
+    const int got = how_many(key, mid);
+    if (got == n) return mid;
+    if (got > n) lo = mid;
+    else hi = mid - 1;
+  }
+  return lo;
 }
 
 // Candidates into the list: the elements of vector v that the bound admits.
@@ -217,6 +238,47 @@ __device__ __forceinline__ void push_edge(const Row<E>& row, int tid, float edge
   if (tid < row.edges && order32(edge) >= b) {
     const int at = atomicAdd(&lds.count, 1);
     if (at < list_size<E::N>()) lds.list[at] = order64(order32(edge), row.edge_token(tid));
+  }
+}
+
+// The first n elements of the vectors that equal the bound (some may fall behind larger elements of the list).
+template <typename E, int NT>
+__device__ __forceinline__ void push_equal(const Row<E>& row, int tid, unsigned b, int n, int* found, TopLds<NT, E::N>& lds) {
+  constexpr int W = NT / 64;
+  for (int before = 0, at = 0; at < row.nv && before < n; at += NT) {
+    unsigned equal = 0;
+    float x[E::N];
+    if (at + tid < row.nv) {
+      E::unpack(row.vec(at + tid), x);
+#pragma unroll
+      for (int i = 0; i < E::N; ++i) equal |= order32(x[i]) == b ? 1u << i : 0u;
+    }
+    int mine = 0, wave = 0;  // equal elements of the wave's lanes before this one, and of all
+#pragma unroll
+    for (int i = 0; i < E::N; ++i) {
+      const u64 who = __ballot((equal >> i) & 1u);
+      mine += __builtin_amdgcn_mbcnt_hi(static_cast<unsigned>(who >> 32), __builtin_amdgcn_mbcnt_lo(static_cast<unsigned>(who), 0u));
+      wave += __builtin_popcountll(who);
+    }
+    if ((tid & 63) == 0) found[tid >> 6] = wave;
+    __syncthreads();
+    int total = 0;
+    for (int w = 0; w < W; ++w) {
+      if (w < (tid >> 6)) mine += found[w];
+      total += found[w];
+    }
+    mine += before;
+#pragma unroll
+    for (int i = 0; i < E::N; ++i)
+      if ((equal >> i) & 1u) {
+        if (mine < n) {
+          const int to = atomicAdd(&lds.count, 1);
+          if (to < list_size<E::N>()) lds.list[to] = order64(b, row.token(at + tid, i));
+        }
+        ++mine;
+      }
+    before += total;
+    __syncthreads();
   }
 }
 
@@ -364,7 +426,7 @@ __device__ __forceinline__ int load_given(const LogprobArgs& a, int64_t r, const
 template <typename E, int NT, bool ENT, bool TOP>
 __global__ __launch_bounds__(NT == 64 ? 256 : NT) void logprobs_kernel(LogprobArgs a) {
   constexpr int ROWS = NT == 64 ? 4 : 1;
-  __shared__ float s_sums[ROWS][4 * NT / 64];
+  __shared__ Part s_sums[ROWS][NT / 64];
   __shared__ TopLds<TOP ? NT : 64, TOP ? E::N : 1> s_top[TOP ? ROWS : 1];
   const int sub = NT == 64 ? uniform_i(threadIdx.x >> 6) : 0, tid = NT == 64 ? threadIdx.x & 63 : threadIdx.x;
   const int64_t r = static_cast<int64_t>(blockIdx.x) * ROWS + sub;
@@ -439,7 +501,7 @@ __global__ __launch_bounds__(NT == 64 ? 256 : NT) void logprobs_kernel(LogprobAr
 // workspace; a workgroup per row joins them.  The parts' maxima bound the alternatives as the lanes' do above, and the
 // parts that reach the bound are read again.
 template <typename E, bool ENT>
-__global__ __launch_bounds__(256) void logprobs_parts_kernel(LogprobArgs a, int parts, int each, float4* __restrict__ out) {
+__global__ __launch_bounds__(256) void logprobs_parts_kernel(LogprobArgs a, int parts, int each, Part* __restrict__ out) {
   const int64_t at = static_cast<int64_t>(blockIdx.x) * 4 + uniform_i(threadIdx.x >> 6);
   const int64_t r = at / parts;
   if (r >= a.in.rows) return;
@@ -448,12 +510,20 @@ __global__ __launch_bounds__(256) void logprobs_parts_kernel(LogprobArgs a, int 
   const float c = a.in.inv_temp * kLog2e;
   const int end = min(begin + 64 * each, row.nv);
   Sums s(kFar / c);
-  for (int v = begin + lane; v < end; v += 64) {
-    float x[1][E::N];
-    E::unpack(row.vec(v), x[0]);
-    const float vm = vec_max(x[0]);
-    s.m = fmaxf(s.m, vm);
-    add_batch<ENT>(s, x, vm, c);
+  for (int v0 = begin + lane; v0 < end; v0 += 64 * kUnroll) {
+    v4u raw[kUnroll];
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u)
+      if (v0 + 64 * u < end) raw[u] = row.vec(v0 + 64 * u);
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u)
+      if (v0 + 64 * u < end) {
+        float x[1][E::N];
+        E::unpack(raw[u], x[0]);
+        const float vm = vec_max(x[0]);
+        s.m = fmaxf(s.m, vm);
+        add_batch<ENT>(s, x, vm, c);
+      }
   }
   const bool has_edge = begin == 0 && lane < row.edges;  // (the first part has the edge as well)
   float edge = -INFINITY;
@@ -472,49 +542,58 @@ __global__ __launch_bounds__(256) void logprobs_parts_kernel(LogprobArgs a, int 
     }
     if (has_edge) add(edge);
   });
-  if (lane == 0) out[at] = make_float4(p.m, p.P, p.S, p.X);
+  if (lane == 0) out[at] = p;
 }
 
-constexpr int kJoinThreads = 1024;
+// Every wave joins all parts by itself (a few instructions, no barrier); the parts that reach the bound are dealt out to the
+// waves.
+constexpr int kJoinThreads = 512;
 template <typename E, bool ENT, bool TOP>
-__global__ __launch_bounds__(kJoinThreads) void logprobs_join_kernel(LogprobArgs a, int parts, int each, const float4* __restrict__ in) {
-  constexpr int NT = kJoinThreads, W = NT / 64;
-  __shared__ float s_sums[4 * W];
+__global__ __launch_bounds__(kJoinThreads) void logprobs_join_kernel(LogprobArgs a, int parts, int each, const Part* __restrict__ in) {
+  constexpr int NT = kJoinThreads, W = NT / 64, PER = kMaxParts / 64;
   __shared__ TopLds<TOP ? NT : 64, TOP ? E::N : 1> lds;
   __shared__ int s_found[W];
+  __shared__ short s_part[W][kMaxParts];
   const int64_t r = blockIdx.x;
-  const int tid = threadIdx.x, lane = tid & 63;
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform_i(tid >> 6);
+  if constexpr (TOP) {
+    if (tid == 0) lds.count = 0;
+    __syncthreads();
+  }
   const Row<E> row = row_at<E>(a.in.x, a.in.stride, r, a.in.V);
   const float c = a.in.inv_temp * kLog2e;
-  float given_x;
-  const int given = load_given<E>(a, r, row, tid, given_x);
-  Part p{-INFINITY, 0.0f, 0.0f, 0.0f};
-  if (tid < parts) {
-    const float4 q = in[r * parts + tid];
-    p = Part{q.x, q.y, q.z, q.w};
+  Part p[PER];
+  unsigned key[PER];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int at = 64 * i + lane;
+    p[i] = at < parts ? in[r * parts + at] : Part{-INFINITY, 0.0f, 0.0f, 0.0f};
+    // (a row's head may leave its last part empty)
+    key[i] = at < parts && (at == 0 || at * 64 * each < row.nv) ? order32(p[i].m) : 0u;
   }
-  const bool some = tid < parts && (tid == 0 || tid * 64 * each < row.nv);  // (a row's head may leave its last part empty)
-  const unsigned own = some ? order32(p.m) : 0u;
-  float edge = -INFINITY;
+  float given_x, edge = -INFINITY;
+  const int given = load_given<E>(a, r, row, tid, given_x);
   if (tid < row.edges) edge = E::up(row.x[row.edge_token(tid)]);
-  const RowSums sums = join_waves<NT, ENT>(join_lanes<ENT>(p.m, p.m * c, p.P, p.S, p.X, c), tid, c, s_sums);
-  write_scores(a, r, tid, sums, given, given_x);
+  const Part all = join_set<ENT, PER>(p, c);
+  const RowSums sums = finish(join_lanes<ENT>(all.m, all.m * c, all.P, all.S, all.X, c), c);
+  if (wave == 0) write_scores(a, r, tid, sums, given, given_x);
   if constexpr (TOP) {
     if (sums.bad) return;
     const TopOut out{a.n_top, sums.base, a.in.inv_temp, sums.log_s, a.top_tokens + r * a.n_top, a.top_logp + r * a.n_top};
-    if (tid == 0) lds.count = lds.first[kGroups] = 0;
-    if (tid < kGroups) lds.group[tid] = own;
-    __syncthreads();
-    unsigned key[kGroups / 64];
-#pragma unroll
-    for (int i = 0; i < kGroups / 64; ++i) key[i] = lds.group[64 * i + lane];
     const unsigned b = bound_of(key, out.n);
     const bool ties = b != 0u && how_many(key, b) > out.n + 16;  // (then the elements equal to the bound are looked for in order)
-    if (own > b || (own == b && some && !ties)) lds.first[atomicAdd(&lds.first[kGroups], 1)] = tid;
-    __syncthreads();
-    const int n = uniform_i(lds.first[kGroups]), last = ties ? -1 : INT_MAX;
-    for (int i = tid >> 6; i < n; i += W) {
-      const int begin = uniform_i(lds.first[i]) * 64 * each;
+    const int last = ties ? -1 : INT_MAX;
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const bool take = key[i] > b || (key[i] == b && key[i] != 0u && !ties);
+      const u64 who = __ballot(take);
+      if (take) s_part[wave][n + __builtin_amdgcn_mbcnt_hi(static_cast<unsigned>(who >> 32), __builtin_amdgcn_mbcnt_lo(static_cast<unsigned>(who), 0u))] = static_cast<short>(64 * i + lane);
+      n += __builtin_popcountll(who);
+    }
+    row_sync<64>();
+    for (int i = wave; i < n; i += W) {
+      const int begin = uniform_i(s_part[wave][i]) * 64 * each;
       for (int v = begin + lane; v < min(begin + 64 * each, row.nv); v += 64) {
         float x[E::N];
         E::unpack(row.vec(v), x);
@@ -522,51 +601,7 @@ __global__ __launch_bounds__(kJoinThreads) void logprobs_join_kernel(LogprobArgs
       }
     }
     push_edge<E, NT>(row, tid, edge, b, lds);
-    if (ties) {
-      // n_top elements equal to the bound, the first ones (some may fall behind larger elements of the list)
-      for (int before = 0, at = 0; at < row.nv && before < out.n; at += NT) {
-        unsigned equal = 0;
-        float x[E::N];
-        if (at + tid < row.nv) {
-          E::unpack(row.vec(at + tid), x);
-#pragma unroll
-          for (int i = 0; i < E::N; ++i) equal |= order32(x[i]) == b ? 1u << i : 0u;
-        }
-        int mine = 0, wave = 0;  // equal elements of the wave's lanes before this one, and of all
-#pragma unroll
-        for (int i = 0; i < E::N; ++i) {
-          const u64 who = __ballot((equal >> i) & 1u);
-          mine += __builtin_amdgcn_mbcnt_hi(static_cast<unsigned>(who >> 32), __builtin_amdgcn_mbcnt_lo(static_cast<unsigned>(who), 0u));
-          wave += __builtin_popcountll(who);
-        }
-        if (lane == 0) s_found[tid >> 6] = wave;
-        __syncthreads();
-        int total = 0;
-        for (int w = 0; w < W; ++w) {
-          if (w < (tid >> 6)) mine += s_found[w];
-          total += s_found[w];
-        }
-        unsigned take = 0;
-        mine += before;
-#pragma unroll
-        for (int i = 0; i < E::N; ++i)
-          if ((equal >> i) & 1u) {
-            if (mine < out.n) take |= 1u << i;
-            ++mine;
-          }
-        if (take) {
-          int to = atomicAdd(&lds.count, __builtin_popcount(take));
-#pragma unroll
-          for (int i = 0; i < E::N; ++i)
-            if ((take >> i) & 1u) {
-              if (to < list_size<E::N>()) lds.list[to] = order64(b, row.token(at + tid, i));
-              ++to;
-            }
-        }
-        before += total;
-        __syncthreads();
-      }
-    }
+    if (ties) push_equal<E, NT>(row, tid, b, out.n, s_found, lds);
     write_list<E, NT>(row, tid, edge, out, lds);
   }
 }
@@ -644,7 +679,7 @@ int forward(const LogprobArgs& a, void* workspace, hipStream_t stream) {
   auto done = [] { return hipGetLastError() == hipSuccess ? PB_OK : PB_EHIP; };
   const RowSplit split = row_split(a.in.V / E::N, a.in.rows);
   if (split.parts > 0) {
-    float4* ws = static_cast<float4*>(workspace);
+    Part* ws = static_cast<Part*>(workspace);
     const int grid = static_cast<int>((static_cast<int64_t>(a.in.rows) * split.parts + 3) / 4);
     if (ent) logprobs_parts_kernel<E, true><<<grid, 256, 0, stream>>>(a, split.parts, split.each, ws);
     else logprobs_parts_kernel<E, false><<<grid, 256, 0, stream>>>(a, split.parts, split.each, ws);
@@ -685,7 +720,7 @@ int backward(const LogprobGradArgs& a, hipStream_t stream) {
 }  // namespace lr
 
 int64_t token_logprobs_workspace(int dtype, int32_t rows, int32_t V) {
-  return static_cast<int64_t>(rows) * row_split(V / (dtype == PB_F32 ? lr::F32::N : lr::F16::N), rows).parts * static_cast<int64_t>(sizeof(float4));
+  return static_cast<int64_t>(rows) * row_split(V / (dtype == PB_F32 ? lr::F32::N : lr::F16::N), rows).parts * static_cast<int64_t>(sizeof(lr::Part));
 }
 int launch_token_logprobs(int dtype, const LogprobArgs& a, void* workspace, hipStream_t stream) {
   return dtype == PB_F32   ? lr::forward<lr::F32>(a, workspace, stream)
