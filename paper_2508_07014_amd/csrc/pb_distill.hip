@@ -214,21 +214,38 @@ __device__ __forceinline__ Student student(const RowSums& sums, const List& list
   s.A = share * w * inv / s.S;
   return s;
 }
-// By one wave: the row's loss, and the gradient on the lane's listed token.
-template <bool TAIL>
-__device__ __forceinline__ float loss_and_own(const DistillArgs& a, int64_t r, int lane, const Entry& e, const List& list, const RowSums& sums,
-                                              const Student& st, float w, float inv) {
-  // (terms that cancel, and log-probs of masked tokens that may pass the fp32 range: in 64 bits)
-  const double lp = (static_cast<double>(e.x) - sums.base) * inv - (sums.m == -INFINITY ? 0.0 : log(static_cast<double>(st.S)));
-  if (a.loss) {
-    double loss = wave_sum(e.q > 0.0f ? e.q * (e.log_q - lp) : static_cast<double>(e.q));  // (0, or NaN)
-    if (TAIL && list.rest != 0.0f) loss += list.rest * static_cast<double>(logf(list.rest / st.p_rest));
-    if (lane == 0) a.loss[r] = sums.bad ? NAN : static_cast<float>(loss);
+// Sum of q over the entries of the lane's token (it may be listed more than once).  By one wave; `table`, kHashBits bits of
+// LDS, tells whether any two tokens can be the same (6 % of lists of 32 different ones are taken for such), which they
+// hardly ever are: 64 comparisons of every lane took 1.5 us.
+constexpr int kHashBits = 8192;
+__device__ __forceinline__ float mass_of(const Entry& e, int K, unsigned* table) {
+  const v4u none = {0u, 0u, 0u, 0u};
+#pragma unroll
+  for (int i = 0; i < kHashBits / 128; i += 64) reinterpret_cast<v4u*>(table)[i + (threadIdx.x & 63)] = none;
+  row_sync<64>();
+  unsigned seen = 0u;
+  if (e.token >= 0) {
+    const unsigned h = static_cast<unsigned>(e.token) * 2654435761u >> 19;
+    seen = atomicOr(&table[h >> 5], 1u << (h & 31)) >> (h & 31) & 1u;
   }
-  float mass = 0.0f;  // (a token may be listed more than once)
-  for (int k = 0; k < a.K; ++k)
+  if (__ballot(seen != 0u) == 0) return e.q;
+  float mass = 0.0f;
+  for (int k = 0; k < K; ++k)
     if (__builtin_amdgcn_readlane(e.token, k) == e.token) mass += __int_as_float(__builtin_amdgcn_readlane(__float_as_int(e.q), k));
-  return (expf(static_cast<float>(lp)) * list.Q - mass) * w * inv;
+  return mass;
+}
+// By one wave: the row's loss.  Terms that cancel, and log-probs of masked tokens that may pass the fp32 range: in 64 bits.
+template <bool TAIL>
+__device__ __forceinline__ void write_loss(const DistillArgs& a, int64_t r, int lane, const Entry& e, const List& list, const RowSums& sums,
+                                           const Student& st, float inv) {
+  const double lp = (static_cast<double>(e.x) - sums.base) * inv - (sums.m == -INFINITY ? 0.0 : log(static_cast<double>(st.S)));
+  double loss = wave_sum(e.q > 0.0f ? e.q * (e.log_q - lp) : static_cast<double>(e.q));  // (0, or NaN)
+  if (TAIL && list.rest != 0.0f) loss += list.rest * static_cast<double>(logf(list.rest / st.p_rest));
+  if (lane == 0) a.loss[r] = sums.bad ? NAN : static_cast<float>(loss);
+}
+// The gradient on a listed token.
+__device__ __forceinline__ float listed_grad(float x, float mass, const List& list, const RowSums& sums, const Student& st, float c, float w, float inv) {
+  return (exp2_fast((x - sums.base) * c) / st.S * list.Q - mass) * w * inv;
 }
 
 // Has the compiler unpack held vectors again, rather than keep them unpacked in twice the registers.
@@ -249,6 +266,7 @@ __global__ __launch_bounds__(NT == 64 ? 256 : NT) void distill_kernel(DistillArg
   __shared__ float s_sums[ROWS][3 * NT / 64];
   __shared__ List s_list;
   __shared__ unsigned s_edge[ROWS];
+  __shared__ __align__(16) unsigned s_table[ROWS][kHashBits / 32];
   const int sub = NT == 64 ? uniform_i(threadIdx.x >> 6) : 0, tid = NT == 64 ? threadIdx.x & 63 : threadIdx.x;
   const int64_t r = static_cast<int64_t>(blockIdx.x) * ROWS + sub;
   if (ROWS > 1 && r >= a.in.rows) return;
@@ -269,7 +287,11 @@ __global__ __launch_bounds__(NT == 64 ? 256 : NT) void distill_kernel(DistillArg
   }
   Entry e{-1, 0.0f, 0.0f, 0.0f};
   List list{0.0f, 0.0f, 0.0f, 0};
-  if (lister) list = load_list<E, TAIL>(a, r, row, tid & 63, e);
+  float mass = 0.0f;
+  if (lister) {
+    list = load_list<E, TAIL>(a, r, row, tid & 63, e);
+    if (a.grad) mass = mass_of(e, a.K, s_table[sub]);
+  }
   if constexpr (NT > 64) {
     if (tid == 0) s_list = list;
   }
@@ -340,8 +362,7 @@ __global__ __launch_bounds__(NT == 64 ? 256 : NT) void distill_kernel(DistillArg
   const RowSums sums = join_waves<NT, TAIL>(part, tid, c, s_sums[sub]);
   const bool empty = sums.m == -INFINITY;
   const Student st = student<TAIL>(sums, list, w, inv);
-  float own = 0.0f;  // the gradient of the lane's listed token
-  if (lister) own = loss_and_own<TAIL>(a, r, tid, e, list, sums, st, w, inv);
+  if (lister && a.loss) write_loss<TAIL>(a, r, tid, e, list, sums, st, inv);
   if (!out) return;
   if (empty || w == 0.0f) {
     if constexpr (NT > 64) __syncthreads();  // (the gradient may take the logits' place: all of them have been read)
@@ -363,6 +384,7 @@ __global__ __launch_bounds__(NT == 64 ? 256 : NT) void distill_kernel(DistillArg
     if (u * NT + tid < row.nv) put(held[u], u * NT + tid);
   for (int v = HELD * NT + tid; v < row.nv; v += NT) put(row.vec(v), v);
   if (tid < row.edges) out[row.edge_token(tid)] = E::down(grad(edge));
+  const float own = lister ? listed_grad(e.x, mass, list, sums, st, c, w, inv) : 0.0f;
   row_sync<NT>();
   if (lister && e.token >= 0) out[e.token] = E::down(own);
 }
@@ -370,30 +392,34 @@ __global__ __launch_bounds__(NT == 64 ? 256 : NT) void distill_kernel(DistillArg
 constexpr int kGradUnroll = 4;
 
 // Few long rows, and rows too long for the registers of a workgroup: every wave takes 64 * `each` vectors of a row and
-// leaves their part of the sums in the workspace (the first one also the list's, and the student's logits on it, since the
+// leaves their part of the sums in the workspace, and one more wave the list's (with the student's logits on it, since the
 // gradient may take the logits' place); the second kernel joins the parts and writes the gradient.
 struct DistillSpace {
   float4* parts;  // [rows, parts]
   List* lists;    // [rows]
   float* x;       // [rows, 64]
+  float* mass;    // [rows, 64]
 };
 template <typename E, bool TAIL>
 __global__ __launch_bounds__(256) void distill_parts_kernel(DistillArgs a, int parts, int each, DistillSpace ws) {
   __shared__ unsigned s_marks[4][64 * kMaxEach / 4];  // a byte per vector
   __shared__ unsigned s_edge[4];
+  __shared__ __align__(16) unsigned s_table[kHashBits / 32];  // (of the one list wave that a workgroup has at most)
   const int sub = uniform_i(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int64_t at = static_cast<int64_t>(blockIdx.x) * 4 + sub;
-  const int64_t r = at / parts;
+  const int64_t r = at / (parts + 1);
   if (r >= a.in.rows) return;
-  const int begin = static_cast<int>(at - r * parts) * 64 * each;
+  const int part = static_cast<int>(at - r * (parts + 1)), begin = part * 64 * each;
   const Row<E> row = row_at<E>(a.in.x, a.in.stride, r, a.in.V);
   const float c = a.in.inv_temp * kLog2e;
   const int end = min(begin + 64 * each, row.nv);
-  if (begin == 0) {
+  if (part == parts) {
     Entry e;
     const List l = load_list<E, TAIL>(a, r, row, lane, e);
     if (lane == 0) ws.lists[r] = l;
     ws.x[r * 64 + lane] = e.x;
+    ws.mass[r * 64 + lane] = mass_of(e, a.K, s_table);
+    return;
   }
   if constexpr (TAIL) {
     if (lane < 16 * each) s_marks[sub][lane] = 0u;
@@ -446,7 +472,7 @@ __global__ __launch_bounds__(256) void distill_parts_kernel(DistillArgs a, int p
     }
     if (has_edge) add(edge, on_edge);
   });
-  if (lane == 0) ws.parts[at] = make_float4(p.m, p.S, p.X, 0.0f);
+  if (lane == 0) ws.parts[r * parts + part] = make_float4(p.m, p.S, p.X, 0.0f);
 }
 
 template <typename E, bool TAIL>
@@ -477,6 +503,7 @@ __global__ __launch_bounds__(256) void distill_grad_kernel(DistillArgs a, int pa
   const Student st = student<TAIL>(sums, list, w, inv);
   const bool learn = list.any != 0, none = !learn || sums.m == -INFINITY || w == 0.0f;
   Entry e{-1, 0.0f, -INFINITY, 0.0f};
+  float mass = 0.0f;
   bool mine = false;  // the lane's listed token lies in this block, whose first wave writes it after the other stores
   if (tid < 64) {
     if (learn && tid < a.K) {
@@ -484,6 +511,7 @@ __global__ __launch_bounds__(256) void distill_grad_kernel(DistillArgs a, int pa
       if (static_cast<unsigned>(t) < static_cast<unsigned>(a.in.V)) {
         e.token = t;
         e.x = ws.x[r * 64 + tid];
+        mass = ws.mass[r * 64 + tid];
         e.log_q = a.logp[r * a.K + tid] - list.shift;
         e.q = exp2_fast(e.log_q * kLog2e);
         mine = block == (t < row.head || t >= row.head + row.nv * E::N ? 0 : (t - row.head) / E::N / BLOCK);
@@ -504,19 +532,13 @@ __global__ __launch_bounds__(256) void distill_grad_kernel(DistillArgs a, int pa
     }
     if (has_edge) out[row.edge_token(tid)] = E::down(none ? 0.0f : exp2_fast((edge - sums.base) * c) * st.A);
   }
-  float own = 0.0f;
-  if (tid < 64) {
-    const bool first = block == 0 && a.loss;
-    if (first && !learn && tid == 0) a.loss[r] = 0.0f;
-    if (learn && (first || __ballot(mine) != 0)) {
-      DistillArgs b = a;
-      if (!first) b.loss = nullptr;
-      own = loss_and_own<TAIL>(b, r, tid, e, list, sums, st, w, inv);
-    }
+  if (block == 0 && tid < 64 && a.loss) {
+    if (learn) write_loss<TAIL>(a, r, tid, e, list, sums, st, inv);
+    else if (tid == 0) a.loss[r] = 0.0f;
   }
   if (!out) return;
   __syncthreads();
-  if (mine && !none) out[e.token] = E::down(own);
+  if (mine && !none) out[e.token] = E::down(listed_grad(e.x, mass, list, sums, st, c, w, inv));
 }
 
 DistillSpace space_in(void* p, int32_t rows, int parts) {
@@ -524,13 +546,14 @@ DistillSpace space_in(void* p, int32_t rows, int parts) {
   ws.parts = static_cast<float4*>(p);
   ws.lists = reinterpret_cast<List*>(ws.parts + static_cast<int64_t>(rows) * parts);
   ws.x = reinterpret_cast<float*>(ws.lists + rows);
+  ws.mass = ws.x + static_cast<int64_t>(rows) * 64;
   return ws;
 }
 
 template <typename E>
 int distill_split(const DistillArgs& a, const RowSplit& split, void* workspace, hipStream_t stream) {
   const DistillSpace ws = space_in(workspace, a.in.rows, split.parts);
-  const int grid = static_cast<int>((static_cast<int64_t>(a.in.rows) * split.parts + 3) / 4);
+  const int grid = static_cast<int>((static_cast<int64_t>(a.in.rows) * (split.parts + 1) + 3) / 4);
   const int blocks = a.grad ? (a.in.V / E::N + 256 * kGradUnroll - 1) / (256 * kGradUnroll) : 1;
   auto go = [&](auto tail) {
     constexpr bool TAIL = decltype(tail)::value;
@@ -569,7 +592,7 @@ int distill(const DistillArgs& a, void* workspace, hipStream_t stream) {
 int64_t distill_topk_workspace(int dtype, int32_t rows, int32_t V) {
   const RowSplit split = row_split(V / (dtype == PB_F32 ? lr::F32::N : lr::F16::N), rows);
   if (split.parts == 0) return 0;
-  return static_cast<int64_t>(rows) * (split.parts * static_cast<int64_t>(sizeof(float4)) + sizeof(lr::List) + 64 * sizeof(float));
+  return static_cast<int64_t>(rows) * (split.parts * static_cast<int64_t>(sizeof(float4)) + sizeof(lr::List) + 2 * 64 * sizeof(float));
 }
 int launch_distill_topk(int dtype, const DistillArgs& a, void* workspace, hipStream_t stream) {
   return dtype == PB_F32   ? lr::distill<lr::F32>(a, workspace, stream)
