@@ -582,7 +582,7 @@ int pb_token_logprobs(const void* d_logits, int32_t dtype, int64_t row_stride, i
                         static_cast<const void*>(d_top_tokens), static_cast<const void*>(d_top_logp), static_cast<const void*>(d_stats)})
     if (!aligned(p, 4)) return PB_EINVAL;
   if (check_workspace(pb_token_logprobs_workspace_bytes(dtype, rows, vocab_size, n_top), d_workspace, workspace_bytes) != PB_OK) return PB_EINVAL;
-  pb::LogprobArgs a{{d_logits, row_stride, rows, vocab_size, 1.0f / temperature}, d_tokens, n_tokens, n_top, d_logp, d_entropy, d_top_tokens, d_top_logp, d_stats};
+  pb::LogprobArgs a{pb::logit_rows(d_logits, row_stride, rows, vocab_size, temperature), d_tokens, n_tokens, n_top, d_logp, d_entropy, d_top_tokens, d_top_logp, d_stats};
   return in_slices(rows, pb::kMaxWorkgroups, [&](size_t at, int32_t n) {
     pb::LogprobArgs s = a;
     s.in = rows_from(a.in, dtype, at, n);
@@ -611,7 +611,7 @@ int pb_token_logprobs_backward(const void* d_logits, int32_t dtype, int64_t row_
   if ((!d_grad_logp && !d_grad_entropy) || (n_tokens > 0) != (d_tokens != nullptr) || (d_grad_logp && n_tokens == 0)) return PB_EINVAL;
   if (!aligned(d_stats, 4) || !aligned(d_tokens, 4) || !aligned(d_grad_logp, 4) || !aligned(d_grad_entropy, 4)) return PB_EINVAL;
   if (d_grad_logits == d_logits && grad_stride != row_stride) return PB_EINVAL;
-  pb::LogprobGradArgs a{{d_logits, row_stride, rows, vocab_size, 1.0f / temperature}, d_stats, d_tokens, n_tokens, d_grad_logp, d_grad_entropy, d_grad_logits, grad_stride};
+  pb::LogprobGradArgs a{pb::logit_rows(d_logits, row_stride, rows, vocab_size, temperature), d_stats, d_tokens, n_tokens, d_grad_logp, d_grad_entropy, d_grad_logits, grad_stride};
   // (a workgroup per 4096 fp32 or 8192 other elements of a row, see pb_logprobs.hip)
   return in_slices(rows, pb::kMaxWorkgroups / (1 + vocab_size / 4096), [&](size_t at, int32_t n) {
     pb::LogprobGradArgs s = a;
@@ -646,7 +646,7 @@ int pb_distill_topk(const void* d_logits, int32_t dtype, int64_t row_stride, int
   if (!aligned(d_teacher_tokens, 4) || !aligned(d_teacher_logp, 4) || !aligned(d_row_grads, 4) || !aligned(d_loss, 4)) return PB_EINVAL;
   if (d_grad_logits == d_logits && grad_stride != row_stride) return PB_EINVAL;
   if (check_workspace(pb_distill_topk_workspace_bytes(dtype, rows, vocab_size, K), d_workspace, workspace_bytes) != PB_OK) return PB_EINVAL;
-  pb::DistillArgs a{{d_logits, row_stride, rows, vocab_size, 1.0f / temperature}, d_teacher_tokens, d_teacher_logp, K, mode == PB_DISTILL_TAIL, d_row_grads, d_loss, d_grad_logits, grad_stride};
+  pb::DistillArgs a{pb::logit_rows(d_logits, row_stride, rows, vocab_size, temperature), d_teacher_tokens, d_teacher_logp, K, mode == PB_DISTILL_TAIL, d_row_grads, d_loss, d_grad_logits, grad_stride};
   return in_slices(rows, pb::kMaxWorkgroups, [&](size_t at, int32_t n) {
     pb::DistillArgs s = a;
     s.in = rows_from(a.in, dtype, at, n);

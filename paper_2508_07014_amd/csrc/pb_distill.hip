@@ -259,31 +259,31 @@ __device__ __forceinline__ void reload(v4u (&held)[HELD]) {
 // in registers; what a row has beyond HELD * NT vectors is read a second time for the gradient (from cache: only the rows
 // at work are in between).  With TAIL the tokens that are not listed have a sum of their own, so that little mass does not
 // vanish in a difference: bits in LDS say which elements are listed, and most vectors have none.
-template <typename E, int NT, int HELD, bool TAIL>
+template <typename E, int NT, int HELD, bool TAIL, bool STREAM>
 __global__ __launch_bounds__(NT == 64 ? 256 : NT) void distill_kernel(DistillArgs a, int mark_bytes) {
   constexpr int ROWS = NT == 64 ? 4 : 1;
   extern __shared__ __align__(16) unsigned char s_all[];
   __shared__ float s_sums[ROWS][3 * NT / 64];
   __shared__ List s_list;
-  __shared__ unsigned s_edge[ROWS];
+  __shared__ u64 s_edge[ROWS];
   __shared__ __align__(16) unsigned s_table[ROWS][kHashBits / 32];
   const int sub = NT == 64 ? uniform_i(threadIdx.x >> 6) : 0, tid = NT == 64 ? threadIdx.x & 63 : threadIdx.x;
   const int64_t r = static_cast<int64_t>(blockIdx.x) * ROWS + sub;
   if (ROWS > 1 && r >= a.in.rows) return;
-  const Row<E> row = row_at<E>(a.in.x, a.in.stride, r, a.in.V);
+  const Row<E> row = row_at<E, NT == 64 ? 16 : 64>(a.in.x, a.in.stride, r, a.in.V);
   unsigned char* marks = s_all + sub * mark_bytes;
   v4u held[HELD];  // (behind the row's end: its last vector again; loads under conditions took 230 registers instead of 50)
   if (row.nv > 0) {
 #pragma unroll
-    for (int u = 0; u < HELD; ++u) held[u] = row.vec(min(u * NT + tid, row.nv - 1));
+    for (int u = 0; u < HELD; ++u) held[u] = row.template vec_once<STREAM>(min(u * NT + tid, row.nv - 1));
   }
   float edge = -INFINITY;
   if (tid < row.edges) edge = E::up(row.x[row.edge_token(tid)]);
-  const float w = a.row_grads ? a.row_grads[r] : 1.0f, inv = a.in.inv_temp, c = inv * kLog2e;
+  const float w = a.row_grads ? a.row_grads[r] : 1.0f, inv = a.in.inv_temp, c = a.in.c;
   const bool lister = NT == 64 || tid < 64;
   if constexpr (TAIL) {
     for (int i = tid; i < mark_bytes / 4; i += NT) reinterpret_cast<unsigned*>(marks)[i] = 0u;
-    if (tid == 0) s_edge[sub] = 0u;
+    if (tid == 0) s_edge[sub] = 0;
   }
   Entry e{-1, 0.0f, 0.0f, 0.0f};
   List list{0.0f, 0.0f, 0.0f, 0};
@@ -301,7 +301,7 @@ __global__ __launch_bounds__(NT == 64 ? 256 : NT) void distill_kernel(DistillArg
     if (lister && e.token >= 0) {
       const int at = e.token - row.head, v = at / E::N;
       if (at < 0 || v >= row.nv) {
-        atomicOr(&s_edge[sub], 1u << (at < 0 ? e.token : e.token - row.nv * E::N));
+        atomicOr(&s_edge[sub], 1ull << (at < 0 ? e.token : e.token - row.nv * E::N));
       } else {
         atomicOr(&reinterpret_cast<unsigned*>(marks)[at >> 5], 1u << (at & 31));
       }
@@ -319,7 +319,7 @@ __global__ __launch_bounds__(NT == 64 ? 256 : NT) void distill_kernel(DistillArg
     if (out) zeros();
     return;
   }
-  Sums s(kFar / c);
+  Sums s(a.in.far);
   auto listed = [&](int v) -> unsigned { return !TAIL ? 0u : E::N == 8 ? marks[v] : (marks[v >> 1] >> (4 * (v & 1))) & 15u; };
   auto edge_listed = [&](int t) -> bool { return TAIL && ((s_edge[sub] >> t) & 1u); };
   float most = edge;
@@ -375,7 +375,8 @@ __global__ __launch_bounds__(NT == 64 ? 256 : NT) void distill_kernel(DistillArg
     E::unpack(raw, x);
 #pragma unroll
     for (int i = 0; i < E::N; ++i) x[i] = grad(x[i]);
-    store_vector<E>(out + row.token(v, 0), E::pack(x));
+    if constexpr (NT > 64 && E::N == 8) stream_vector<E>(out + row.token(v, 0), E::pack(x));
+    else store_vector<E>(out + row.token(v, 0), E::pack(x));
   };
   if constexpr (NT > 64) __syncthreads();
   reload(held);
@@ -403,7 +404,7 @@ struct DistillSpace {
 template <typename E, bool TAIL>
 __global__ __launch_bounds__(256) void distill_parts_kernel(DistillArgs a, int parts, int each, DistillSpace ws) {
   __shared__ unsigned s_marks[4][64 * kMaxEach / 4];  // a byte per vector
-  __shared__ unsigned s_edge[4];
+  __shared__ u64 s_edge[4];
   __shared__ __align__(16) unsigned s_table[kHashBits / 32];  // (of the one list wave that a workgroup has at most)
   const int sub = uniform_i(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int64_t at = static_cast<int64_t>(blockIdx.x) * 4 + sub;
@@ -411,7 +412,7 @@ __global__ __launch_bounds__(256) void distill_parts_kernel(DistillArgs a, int p
   if (r >= a.in.rows) return;
   const int part = static_cast<int>(at - r * (parts + 1)), begin = part * 64 * each;
   const Row<E> row = row_at<E>(a.in.x, a.in.stride, r, a.in.V);
-  const float c = a.in.inv_temp * kLog2e;
+  const float c = a.in.c;
   const int end = min(begin + 64 * each, row.nv);
   if (part == parts) {
     Entry e;
@@ -424,13 +425,13 @@ __global__ __launch_bounds__(256) void distill_parts_kernel(DistillArgs a, int p
   if constexpr (TAIL) {
     if (lane < 16 * each) s_marks[sub][lane] = 0u;
     if (16 * each > 64 && lane < 16 * each - 64) s_marks[sub][64 + lane] = 0u;
-    if (lane == 0) s_edge[sub] = 0u;
+    if (lane == 0) s_edge[sub] = 0;
     row_sync<64>();
     if (lane < a.K) {
       const int t = a.tokens[r * a.K + lane], e = t - row.head, v = e / E::N;
       if (static_cast<unsigned>(t) < static_cast<unsigned>(a.in.V)) {
         if (e < 0 || v >= row.nv)
-          atomicOr(&s_edge[sub], 1u << (e < 0 ? t : t - row.nv * E::N));
+          atomicOr(&s_edge[sub], 1ull << (e < 0 ? t : t - row.nv * E::N));
         else if (v >= begin && v < end)
           atomicOr(&s_marks[sub][(v - begin) >> 2], 1u << (8 * ((v - begin) & 3) + e % E::N));
       }
@@ -438,7 +439,7 @@ __global__ __launch_bounds__(256) void distill_parts_kernel(DistillArgs a, int p
     row_sync<64>();
   }
   auto listed = [&](int v) -> unsigned { return TAIL ? reinterpret_cast<const unsigned char*>(s_marks[sub])[v - begin] : 0u; };
-  Sums s(kFar / c);
+  Sums s(a.in.far);
   for (int v0 = begin + lane; v0 < end; v0 += 64 * kGradUnroll) {
     v4u raw[kGradUnroll];
 #pragma unroll
@@ -490,7 +491,7 @@ __global__ __launch_bounds__(256) void distill_grad_kernel(DistillArgs a, int pa
   const bool has_edge = block == 0 && tid < row.edges;
   float edge = 0.0f;
   if (has_edge) edge = E::up(row.x[row.edge_token(tid)]);
-  const float w = a.row_grads ? a.row_grads[r] : 1.0f, inv = a.in.inv_temp, c = inv * kLog2e;
+  const float w = a.row_grads ? a.row_grads[r] : 1.0f, inv = a.in.inv_temp, c = a.in.c;
   const List list = ws.lists[r];
   Part p{-INFINITY, 0.0f, 0.0f};
 #pragma unroll
@@ -527,7 +528,7 @@ __global__ __launch_bounds__(256) void distill_grad_kernel(DistillArgs a, int pa
         E::unpack(raw[u], x);
 #pragma unroll
         for (int i = 0; i < E::N; ++i) x[i] = none ? 0.0f : exp2_fast((x[i] - sums.base) * c) * st.A;
-        store_vector<E>(out + row.token(v, 0), E::pack(x));
+        stream_vector<E>(out + row.token(v, 0), E::pack(x));
       }
     }
     if (has_edge) out[row.edge_token(tid)] = E::down(none ? 0.0f : exp2_fast((edge - sums.base) * c) * st.A);
@@ -570,13 +571,22 @@ int distill(const DistillArgs& a, void* workspace, hipStream_t stream) {
   const RowSplit split = row_split(a.in.V / E::N, a.in.rows);
   if (split.parts > 0) return distill_split<E>(a, split, workspace, stream);
   const int nv = a.in.V / E::N, mark_bytes = (a.in.V + 127) / 128 * 16;  // (a bit per element behind the head)
+  // (logits of 16 bits that do not fit in the last cache with their gradient, in long rows, are not kept there either:
+  // 8192 x 32001 195 -> 191 us, 16384 x 16000 201 -> 190; 32768 x 8193 207 against 213, 1024 x 32001, which fits, 28 against 30.
+  // The gradient of such types goes past the caches (there 36 -> 28 us; fp32 8192 x 32000 397 us against 420).)
+  const bool large = E::N == 8 && nv > 2048 && 4 * static_cast<int64_t>(a.in.rows) * a.in.V > (256ll << 20);
   auto go = [&](auto nt, auto held) {
     constexpr int NT = decltype(nt)::value, HELD = decltype(held)::value, ROWS = NT == 64 ? 4 : 1, THREADS = NT == 64 ? 256 : NT;
-    const int grid = (a.in.rows + ROWS - 1) / ROWS;
-    if (a.tail)
-      distill_kernel<E, NT, HELD, true><<<grid, THREADS, ROWS * mark_bytes, stream>>>(a, mark_bytes);
-    else
-      distill_kernel<E, NT, HELD, false><<<grid, THREADS, 0, stream>>>(a, 0);
+    constexpr bool CAN = E::N == 8 && NT >= 512;
+    const int grid = (a.in.rows + ROWS - 1) / ROWS, lds = a.tail ? ROWS * mark_bytes : 0;
+    auto launch = [&](auto kernel) { kernel<<<grid, THREADS, lds, stream>>>(a, a.tail ? mark_bytes : 0); };
+    if (a.tail) {
+      if (CAN && large) launch(distill_kernel<E, NT, HELD, true, CAN>);
+      else launch(distill_kernel<E, NT, HELD, true, false>);
+    } else {
+      if (CAN && large) launch(distill_kernel<E, NT, HELD, false, CAN>);
+      else launch(distill_kernel<E, NT, HELD, false, false>);
+    }
     return hipGetLastError() == hipSuccess ? PB_OK : PB_EHIP;
   };
   using std::integral_constant;

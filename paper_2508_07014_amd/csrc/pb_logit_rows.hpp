@@ -87,8 +87,8 @@ struct BF16 {
   static __device__ __forceinline__ __bf16 down(float v) { return static_cast<__bf16>(v); }
 };
 
-// A row of V elements at any alignment: up to N - 1 elements before the first 16-byte boundary and as many behind the last
-// one (the edge, one lane each), `nv` aligned vectors between them.  Nothing outside the row is touched.
+// A row of V elements at any alignment: the elements before the first boundary and the fewer than N behind the last vector
+// (the edge, one lane each), `nv` aligned vectors between them.  Nothing outside the row is touched.
 template <typename E>
 struct Row {
   const typename E::type* x;
@@ -97,15 +97,22 @@ struct Row {
   __device__ __forceinline__ v4u vec(int v) const {  // (a 32-bit offset from a uniform base)
     return *reinterpret_cast<const v4u*>(reinterpret_cast<const char*>(body) + static_cast<unsigned>(v) * 16u);
   }
+  template <bool STREAM>
+  __device__ __forceinline__ v4u vec_once(int v) const {  // (STREAM: past the caches)
+    if constexpr (!STREAM) return vec(v);
+    return __builtin_nontemporal_load(reinterpret_cast<const v4u*>(reinterpret_cast<const char*>(body) + static_cast<unsigned>(v) * 16u));
+  }
   __device__ __forceinline__ int edge_token(int t) const { return t + (t >= head ? nv * E::N : 0); }
   __device__ __forceinline__ int token(int v, int i) const { return head + v * E::N + i; }
 };
-template <typename E>
+// ALIGN: the boundary that the vectors begin at, 16, or 64, so that a wave's stores fill whole cache lines but for the first
+// and last (odd rows of bf16 in one pass over 2 x 500 MB: 192 -> 188 us; the longer edge costs short rows 5 %).
+template <typename E, unsigned ALIGN = 16>
 __device__ __forceinline__ Row<E> row_at(const void* base, int64_t stride, int64_t row, int V) {
   Row<E> r;
   r.x = static_cast<const typename E::type*>(base) + row * stride;
   r.V = V;
-  r.head = min(V, static_cast<int>((0u - static_cast<unsigned>(reinterpret_cast<uintptr_t>(r.x))) & 15u) / static_cast<int>(sizeof(typename E::type)));
+  r.head = min(V, static_cast<int>((0u - static_cast<unsigned>(reinterpret_cast<uintptr_t>(r.x))) & (ALIGN - 1u)) / static_cast<int>(sizeof(typename E::type)));
   r.nv = (V - r.head) / E::N;
   r.edges = V - r.nv * E::N;
   r.body = reinterpret_cast<const v4u*>(r.x + r.head);
@@ -141,24 +148,36 @@ __device__ __forceinline__ void row_sync() {
   }
 }
 
-// 16 bytes to any element of a row.
+// 16 bytes to any element of a row, and the same past the caches.
+template <typename E>
+__device__ __forceinline__ void stream_vector(typename E::type* p, const v4u& r) {
+  __builtin_nontemporal_store(r, reinterpret_cast<typename E::any4*>(p));
+}
 template <typename E>
 __device__ __forceinline__ void store_vector(typename E::type* p, const v4u& r) {
   *reinterpret_cast<typename E::any4*>(p) = r;
 }
 
-// Elements further than kFar / c from 0 (c = log2(e) / T): there x c is too coarse for the differences between them, and a
-// row's sums are formed from (x - max) c instead.
-constexpr float kFar = 1048576.0f;
-
+// The larger of three (a NaN is passed over, as by fmaxf, which would first quiet each operand by an instruction of its own).
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
 template <int N>
 __device__ __forceinline__ float vec_max(const float (&x)[N]) {
   if constexpr (N == 1) return x[0];
-  float m = x[0];
+  float m = max3(x[0], x[1], x[2]);
 #pragma unroll
-  for (int i = 1; i + 1 < N; i += 2) m = fmaxf(fmaxf(m, x[i]), x[i + 1]);
-  if constexpr (N % 2 == 0) m = fmaxf(m, x[N - 1]);
+  for (int i = 3; i + 1 < N; i += 2) m = max3(m, x[i], x[i + 1]);
+  if constexpr (N % 2 == 0) m = max3(m, x[N - 1], x[N - 1]);
   return m;
+}
+// log(1 + r), r > -1/2: the logarithm of u = 1 + r, rounded, by what u lacks of r (Kahan).
+__device__ __forceinline__ float log_1p(float r) {
+  const float u = 1.0f + r, d = u - 1.0f;
+  const float l = __builtin_amdgcn_logf(u) * kLn2;  // (base 2)
+  return d == 0.0f ? r : fabsf(d) < 0.5f ? l * (r / d) : l;
 }
 template <int N>
 __device__ __forceinline__ float vec_sum(float (&x)[N]) {  // (in pairs: fewer roundings in a row)

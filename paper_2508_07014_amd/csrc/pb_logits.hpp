@@ -16,8 +16,17 @@ struct LogitRows {
   const void* x;       // [rows, stride], enum pb_dtype
   int64_t stride;      // in elements
   int32_t rows, V;
-  float inv_temp;
+  float inv_temp;      // 1 / T
+  float c;             // log2(e) / T
+  float far;           // logits further from 0 than this: see kFar
 };
+// Elements further than kFar / c from 0: there x c is too coarse for the differences between them, and a row's sums are
+// formed from (x - max) c instead.
+constexpr float kFar = 1048576.0f;
+inline LogitRows logit_rows(const void* x, int64_t stride, int32_t rows, int32_t V, float temperature) {
+  const double c = 1.44269504088896340736 / temperature;
+  return LogitRows{x, stride, rows, V, static_cast<float>(1.0 / temperature), static_cast<float>(c), static_cast<float>(kFar / c)};
+}
 
 struct LogprobArgs {
   LogitRows in;

@@ -33,6 +33,7 @@ template <bool ENT, int U, int N>
 __device__ __forceinline__ void add_batch(Sums& s, const float (&x)[U][N], float m, float c) {
   const bool up = m > s.thr;
   if (__ballot(up) != 0) {
+    asm volatile("");  // (a branch: selects would take the move's exponential in every batch)
     if (up) {
       const float next = m * c;
       s.S += s.P;
@@ -128,7 +129,7 @@ struct RowSums {  // the same in every thread of the row
 __device__ __forceinline__ RowSums finish(const Part& p, float c) {
   const bool empty = p.m == -INFINITY;
   const float S = p.P + p.S, mc = p.m * c, rounded = fabsf(mc) <= kFar ? __builtin_fmaf(p.m, c, -mc) : 0.0f;
-  const float log_s = log1pf((p.P - 1.0f) + p.S);
+  const float log_s = log_1p((p.P - 1.0f) + p.S);
   RowSums r;
   r.bad = S != S || p.m == INFINITY;
   r.m = r.bad ? NAN : p.m;
@@ -169,7 +170,7 @@ struct Tops {
   __device__ __forceinline__ void add(float vm, int k) {
     k1 = vm > m1 ? k : k1;
     m2 = __builtin_amdgcn_fmed3f(vm, m1, m2);  // (m2 <= m1)
-    m1 = fmaxf(m1, vm);
+    m1 = max3(m1, vm, vm);
   }
 };
 
@@ -217,12 +218,10 @@ __device__ __forceinline__ unsigned bound_of(const unsigned (&key)[PER], int n) 
 // Candidates into the list: the elements of vector v that the bound admits.
 template <typename E, int NT>
 __device__ __forceinline__ void push_vector(const Row<E>& row, const float (&x)[E::N], int v, unsigned b, int last, TopLds<NT, E::N>& lds) {
+  const float least = ukey_val(v <= last ? b : b + 1);  // (an order as good as that of the keys, -0.0 as 0.0)
   unsigned take = 0;
 #pragma unroll
-  for (int i = 0; i < E::N; ++i) {
-    const unsigned k = order32(x[i]);
-    take |= (k > b || (k == b && v <= last)) ? 1u << i : 0u;
-  }
+  for (int i = 0; i < E::N; ++i) take |= b == 0u || x[i] >= least ? 1u << i : 0u;
   if (take) {
     int at = atomicAdd(&lds.count, __builtin_popcount(take));
 #pragma unroll
@@ -432,46 +431,39 @@ __global__ __launch_bounds__(NT == 64 ? 256 : NT) void logprobs_kernel(LogprobAr
   const int64_t r = static_cast<int64_t>(blockIdx.x) * ROWS + sub;
   if (ROWS > 1 && r >= a.in.rows) return;
   const Row<E> row = row_at<E>(a.in.x, a.in.stride, r, a.in.V);
-  const float inv = a.in.inv_temp, c = inv * kLog2e;
+  const float inv = a.in.inv_temp, c = a.in.c;
   float given_x;  // (on its way during the pass)
   const int given = load_given<E>(a, r, row, tid, given_x);
-  Sums s(kFar / c);
+  Sums s(a.in.far);
   Tops tops;
   const int whole = row.nv / (kUnroll * NT);
-  auto batch = [&](auto& x, int k) {  // (vectors k, k + 1, ... of the thread)
-    constexpr int U = sizeof(x) / sizeof(x[0]);
-    float m = -INFINITY;
+  auto batch = [&](const auto& raw, int k) {  // (vectors k, k + 1, ... of the thread)
+    constexpr int U = sizeof(raw) / sizeof(raw[0]);
+    float x[U][E::N], m = -INFINITY;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
+      E::unpack(raw[u], x[u]);
       const float vm = vec_max(x[u]);
       if constexpr (TOP) tops.add(vm, k + u);
-      m = fmaxf(m, vm);
+      m = u == 0 ? vm : max3(m, vm, vm);
     }
-    s.m = fmaxf(s.m, m);
+    s.m = max3(s.m, m, m);
     add_batch<ENT>(s, x, m, c);
   };
-  for (int b = 0; b < whole; ++b) {
-    v4u raw[kUnroll];
-    float x[kUnroll][E::N];
+  auto some = [&](auto count, int k) {
+    constexpr int U = decltype(count)::value;
+    v4u raw[U];
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) raw[u] = row.vec((b * kUnroll + u) * NT + tid);
-#pragma unroll
-    for (int u = 0; u < kUnroll; ++u) E::unpack(raw[u], x[u]);
-    batch(x, b * kUnroll);
-  }
-  {
-    v4u raw[kUnroll];
-#pragma unroll
-    for (int u = 0; u < kUnroll; ++u)
-      if ((whole * kUnroll + u) * NT + tid < row.nv) raw[u] = row.vec((whole * kUnroll + u) * NT + tid);
-#pragma unroll
-    for (int u = 0; u < kUnroll; ++u)
-      if ((whole * kUnroll + u) * NT + tid < row.nv) {
-        float x[1][E::N];
-        E::unpack(raw[u], x[0]);
-        batch(x, whole * kUnroll + u);
-      }
-  }
+    for (int u = 0; u < U; ++u) raw[u] = row.vec((k + u) * NT + tid);
+    batch(raw, k);
+  };
+  using std::integral_constant;
+  for (int b = 0; b < whole; ++b) some(integral_constant<int, kUnroll>{}, b * kUnroll);
+  const int left = row.nv / NT - whole * kUnroll;  // vectors that every thread has left, before one that some have
+  if (left == 3) some(integral_constant<int, 3>{}, whole * kUnroll);
+  if (left == 2) some(integral_constant<int, 2>{}, whole * kUnroll);
+  if (left == 1) some(integral_constant<int, 1>{}, whole * kUnroll);
+  if ((whole * kUnroll + left) * NT + tid < row.nv) some(integral_constant<int, 1>{}, whole * kUnroll + left);
   float edge = -INFINITY;
   if (tid < row.edges) {
     edge = E::up(row.x[row.edge_token(tid)]);
@@ -507,9 +499,9 @@ __global__ __launch_bounds__(256) void logprobs_parts_kernel(LogprobArgs a, int 
   if (r >= a.in.rows) return;
   const int lane = threadIdx.x & 63, begin = static_cast<int>(at - r * parts) * 64 * each;
   const Row<E> row = row_at<E>(a.in.x, a.in.stride, r, a.in.V);
-  const float c = a.in.inv_temp * kLog2e;
+  const float c = a.in.c;
   const int end = min(begin + 64 * each, row.nv);
-  Sums s(kFar / c);
+  Sums s(a.in.far);
   for (int v0 = begin + lane; v0 < end; v0 += 64 * kUnroll) {
     v4u raw[kUnroll];
 #pragma unroll
@@ -561,7 +553,7 @@ __global__ __launch_bounds__(kJoinThreads) void logprobs_join_kernel(LogprobArgs
     __syncthreads();
   }
   const Row<E> row = row_at<E>(a.in.x, a.in.stride, r, a.in.V);
-  const float c = a.in.inv_temp * kLog2e;
+  const float c = a.in.c;
   Part p[PER];
   unsigned key[PER];
 #pragma unroll
@@ -609,23 +601,23 @@ __global__ __launch_bounds__(kJoinThreads) void logprobs_join_kernel(LogprobArgs
 // Gradient: p (A + B log2 p) with A = -(G + h H) / T, B = -h ln(2) / T for all tokens, plus what the given ones take.  A
 // workgroup takes kUnroll vectors a thread of one row (a wave, four rows a workgroup, where those hold the row).  The
 // gradients on the given tokens are computed before anything is written and stored behind the rest.
-template <typename E, int NT>
+template <typename E, int NT, bool STREAM>
 __global__ __launch_bounds__(256) void logprobs_backward_kernel(LogprobGradArgs a, int parts) {
   constexpr int ROWS = 256 / NT, PART = NT * kUnroll;
   const int sub = ROWS > 1 ? uniform_i(threadIdx.x / NT) : 0, tid = threadIdx.x % NT;
   const int64_t r = ROWS > 1 ? static_cast<int64_t>(blockIdx.x) * ROWS + sub : blockIdx.x / parts;
   const int part = ROWS > 1 ? 0 : blockIdx.x % parts;
   if (ROWS > 1 && r >= a.in.rows) return;
-  const Row<E> row = row_at<E>(a.in.x, a.in.stride, r, a.in.V);
+  const Row<E> row = row_at<E, 64>(a.in.x, a.in.stride, r, a.in.V);
   typename E::type* out = static_cast<typename E::type*>(a.grad) + r * a.grad_stride;
   v4u raw[kUnroll];
 #pragma unroll
   for (int u = 0; u < kUnroll; ++u)
-    if (part * PART + u * NT + tid < row.nv) raw[u] = row.vec(part * PART + u * NT + tid);
+    if (part * PART + u * NT + tid < row.nv) raw[u] = row.template vec_once<STREAM>(part * PART + u * NT + tid);
   const bool has_edge = part == 0 && tid < row.edges;
   float edge = 0.0f;
   if (has_edge) edge = E::up(row.x[row.edge_token(tid)]);
-  const float inv = a.in.inv_temp, c = inv * kLog2e;
+  const float inv = a.in.inv_temp, c = a.in.c;
   const float m = a.stats[3 * r], logs = a.stats[3 * r + 1], H = a.stats[3 * r + 2];
   const float h = a.grad_entropy ? a.grad_entropy[r] : 0.0f;
   const int lane = threadIdx.x & 63;
@@ -665,7 +657,7 @@ __global__ __launch_bounds__(256) void logprobs_backward_kernel(LogprobGradArgs 
       E::unpack(raw[u], x);
 #pragma unroll
       for (int i = 0; i < E::N; ++i) x[i] = none ? 0.0f : pull(x[i]);
-      store_vector<E>(out + row.token(v, 0), E::pack(x));
+      stream_vector<E>(out + row.token(v, 0), E::pack(x));
     }
   }
   if (has_edge) out[row.edge_token(tid)] = E::down(none ? 0.0f : pull(edge));
@@ -704,14 +696,21 @@ int forward(const LogprobArgs& a, void* workspace, hipStream_t stream) {
   return pick(std::integral_constant<int, 1024>{});
 }
 
+// Logits that with their gradient do not fit in the last cache (256 MB) are not kept there either: 8192 x 32001 bf16 192 -> 188 us,
+// fp32 379 -> 368; 1024 x 32001 bf16, which fits, 21.6 us against 25.2.  The gradient goes past the caches in any case (there 29 -> 22 us).
+constexpr int64_t kStreamBytes = 256ll << 20;
 template <typename E>
 int backward(const LogprobGradArgs& a, hipStream_t stream) {
   const int64_t nv = a.in.V / E::N;
+  const bool large = 2 * static_cast<int64_t>(a.in.rows) * a.in.V * static_cast<int64_t>(sizeof(typename E::type)) > kStreamBytes;
+  const int parts = nv <= 64 * kUnroll ? 1 : static_cast<int>((nv + 256 * kUnroll - 1) / (256 * kUnroll));
+  auto go = [&](auto kernel, int grid) { kernel<<<grid, 256, 0, stream>>>(a, parts); };
   if (nv <= 64 * kUnroll) {
-    logprobs_backward_kernel<E, 64><<<(a.in.rows + 3) / 4, 256, 0, stream>>>(a, 1);
+    if (large) go(logprobs_backward_kernel<E, 64, true>, (a.in.rows + 3) / 4);
+    else go(logprobs_backward_kernel<E, 64, false>, (a.in.rows + 3) / 4);
   } else {
-    const int parts = static_cast<int>((nv + 256 * kUnroll - 1) / (256 * kUnroll));
-    logprobs_backward_kernel<E, 256><<<a.in.rows * parts, 256, 0, stream>>>(a, parts);
+    if (large) go(logprobs_backward_kernel<E, 256, true>, a.in.rows * parts);
+    else go(logprobs_backward_kernel<E, 256, false>, a.in.rows * parts);
   }
   return hipGetLastError() == hipSuccess ? PB_OK : PB_EHIP;
 }
