@@ -215,6 +215,17 @@ __device__ __forceinline__ unsigned bound_of(const unsigned (&key)[PER], int n) 
   return lo;
 }
 
+template <int N>
+__device__ __forceinline__ float element(const float (&x)[N], int i) {  // x[i], in registers
+  float y[N];
+#pragma unroll
+  for (int k = 0; k < N; ++k) y[k] = x[k];
+#pragma unroll
+  for (int n = N / 2; n > 0; n /= 2)
+#pragma unroll
+    for (int k = 0; k < n; ++k) y[k] = i & n ? y[k + n] : y[k];
+  return y[0];
+}
 // Candidates into the list: the elements of vector v that the bound admits.
 template <typename E, int NT>
 __device__ __forceinline__ void push_vector(const Row<E>& row, const float (&x)[E::N], int v, unsigned b, int last, TopLds<NT, E::N>& lds) {
@@ -224,12 +235,11 @@ __device__ __forceinline__ void push_vector(const Row<E>& row, const float (&x)[
   for (int i = 0; i < E::N; ++i) take |= b == 0u || x[i] >= least ? 1u << i : 0u;
   if (take) {
     int at = atomicAdd(&lds.count, __builtin_popcount(take));
-#pragma unroll
-    for (int i = 0; i < E::N; ++i)
-      if ((take >> i) & 1u) {
-        if (at < list_size<E::N>()) lds.list[at] = order64(order32(x[i]), row.token(v, i));
-        ++at;
-      }
+    for (; take; take &= take - 1) {  // (one element as a rule)
+      const int i = __builtin_ctz(take);
+      if (at < list_size<E::N>()) lds.list[at] = order64(order32(element(x, i)), row.token(v, i));
+      ++at;
+    }
   }
 }
 template <typename E, int NT>
@@ -380,16 +390,34 @@ __device__ __forceinline__ void write_alternatives(const Row<E>& row, int tid, c
   }
   row_sync<NT>();
   const int v1 = tops.k1 * NT + tid;
-  if (some && (own > b || (own == b && v1 <= last))) {
+  const bool mine = some && (own > b || (own == b && v1 <= last));
+  if (mine) {
     float x[E::N];
     E::unpack(row.vec(v1), x);
     push_vector<E, NT>(row, x, v1, b, last, lds);
-    if (row.nv > NT && order32(tops.m2) >= b)
+  }
+  // the other vectors of lanes that have more above the bound: of one such lane after the other by the whole wave, or, where
+  // they are many, by all of them at once
+  if (row.nv > NT) {
+    u64 more = __ballot(mine && order32(tops.m2) >= b);
+    if (__builtin_popcountll(more) < row.nv / NT) {
+      for (; more; more &= more - 1) {
+        const int from = wv::first_lane(more), skip = __builtin_amdgcn_readlane(v1, from);
+        for (int v = lane * NT + (tid & ~63) + from; v < row.nv; v += 64 * NT)
+          if (v != skip) {
+            float x[E::N];
+            E::unpack(row.vec(v), x);
+            push_vector<E, NT>(row, x, v, b, last, lds);
+          }
+      }
+    } else if ((more >> lane) & 1u) {
       for (int v = tid; v < row.nv; v += NT)
         if (v != v1) {
+          float x[E::N];
           E::unpack(row.vec(v), x);
           push_vector<E, NT>(row, x, v, b, last, lds);
         }
+    }
   }
   push_edge<E, NT>(row, tid, edge, b, lds);
   write_list<E, NT>(row, tid, edge, out, lds);
