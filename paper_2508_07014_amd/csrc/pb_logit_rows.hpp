@@ -36,6 +36,7 @@ struct F32 {
 #pragma unroll
     for (int i = 0; i < N; ++i) x[i] = __uint_as_float(r[i]);
   }
+  static __device__ __forceinline__ v4u nothing() { return v4u{0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u}; }  // -inf throughout
   static __device__ __forceinline__ v4u pack(const float (&x)[N]) {
     v4u r;
 #pragma unroll
@@ -58,6 +59,7 @@ struct F16 {
       x[2 * i + 1] = static_cast<float>(h.y);
     }
   }
+  static __device__ __forceinline__ v4u nothing() { return v4u{0xfc00fc00u, 0xfc00fc00u, 0xfc00fc00u, 0xfc00fc00u}; }  // -inf throughout
   static __device__ __forceinline__ v4u pack(const float (&x)[N]) {
     v4u r;
 #pragma unroll
@@ -78,6 +80,7 @@ struct BF16 {
       x[2 * i + 1] = __uint_as_float(r[i] & 0xffff0000u);
     }
   }
+  static __device__ __forceinline__ v4u nothing() { return v4u{0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u}; }  // -inf throughout
   static __device__ __forceinline__ v4u pack(const float (&x)[N]) {
     v4u r;
 #pragma unroll

@@ -42,7 +42,7 @@ __device__ __forceinline__ void add_batch(Sums& s, const float (&x)[U][N], float
       s.thr = m;
     }
   }
-  float sum = 0.0f, sum_x = 0.0f;
+  float sum, sum_x;
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     float e[N], ed[N];
@@ -52,8 +52,8 @@ __device__ __forceinline__ void add_batch(Sums& s, const float (&x)[U][N], float
       e[i] = exp2_fast(d);
       if constexpr (ENT) ed[i] = e[i] * fmaxf(d, -1000.0f);  // (-inf: nothing)
     }
-    if constexpr (ENT) sum_x += vec_sum(ed);
-    sum += vec_sum(e);
+    if constexpr (ENT) sum_x = u == 0 ? vec_sum(ed) : sum_x + vec_sum(ed);
+    sum = u == 0 ? vec_sum(e) : sum + vec_sum(e);
   }
   s.P = up ? sum : s.P;
   s.S += up ? 0.0f : sum;
@@ -449,7 +449,8 @@ __device__ __forceinline__ int load_given(const LogprobArgs& a, int64_t r, const
   return t;
 }
 
-// One row.  NT == 64: a wave of its own, kThreads / 64 of them in a workgroup.
+// One row, by a workgroup, or (NT == 64: rows of up to kWaveVectors vectors) by a wave, four in a workgroup.
+static_assert(kWaveVectors == 2 * 64 * kUnroll, "a wave requests its row in two batches");
 template <typename E, int NT, bool ENT, bool TOP>
 __global__ __launch_bounds__(NT == 64 ? 256 : NT) void logprobs_kernel(LogprobArgs a) {
   constexpr int ROWS = NT == 64 ? 4 : 1;
@@ -460,13 +461,27 @@ __global__ __launch_bounds__(NT == 64 ? 256 : NT) void logprobs_kernel(LogprobAr
   if (ROWS > 1 && r >= a.in.rows) return;
   const Row<E> row = row_at<E>(a.in.x, a.in.stride, r, a.in.V);
   const float inv = a.in.inv_temp, c = a.in.c;
-  float given_x;  // (on its way during the pass)
-  const int given = load_given<E>(a, r, row, tid, given_x);
+  // (all that does not depend on other loads is requested before the first wait: the token, the first vectors, the edge)
+  int given = -1;
+  if (tid < a.n_tokens) given = a.tokens[r * a.n_tokens + tid];
+  v4u raw[kUnroll], more[NT == 64 ? kUnroll : 1];
+  auto load = [&](auto& to, int k) {  // vectors k, k + 1, ... of the thread; behind the row's end its last one again
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) to[u] = row.vec(min((k + u) * NT + tid, row.nv - 1));
+  };
+  const bool second = NT == 64 && row.nv > kUnroll * NT;
+  if (row.nv > 0) load(raw, 0);
+  if constexpr (NT == 64)
+    if (second) load(more, kUnroll);
+  float edge = -INFINITY;
+  if (tid < row.edges) edge = E::up(row.x[row.edge_token(tid)]);
+  float given_x = 0.0f;
+  if (static_cast<unsigned>(given) < static_cast<unsigned>(row.V)) given_x = E::up(row.x[given]);
+  else given = -1;
   Sums s(a.in.far);
   Tops tops;
-  const int whole = row.nv / (kUnroll * NT);
-  auto batch = [&](const auto& raw, int k) {  // (vectors k, k + 1, ... of the thread)
-    constexpr int U = sizeof(raw) / sizeof(raw[0]);
+  auto batch = [&](auto count, const auto& raw, int k) {
+    constexpr int U = decltype(count)::value;
     float x[U][E::N], m = -INFINITY;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -478,23 +493,30 @@ __global__ __launch_bounds__(NT == 64 ? 256 : NT) void logprobs_kernel(LogprobAr
     s.m = max3(s.m, m, m);
     add_batch<ENT>(s, x, m, c);
   };
-  auto some = [&](auto count, int k) {
-    constexpr int U = decltype(count)::value;
-    v4u raw[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) raw[u] = row.vec((k + u) * NT + tid);
-    batch(raw, k);
-  };
   using std::integral_constant;
-  for (int b = 0; b < whole; ++b) some(integral_constant<int, kUnroll>{}, b * kUnroll);
-  const int left = row.nv / NT - whole * kUnroll;  // vectors that every thread has left, before one that some have
-  if (left == 3) some(integral_constant<int, 3>{}, whole * kUnroll);
-  if (left == 2) some(integral_constant<int, 2>{}, whole * kUnroll);
-  if (left == 1) some(integral_constant<int, 1>{}, whole * kUnroll);
-  if ((whole * kUnroll + left) * NT + tid < row.nv) some(integral_constant<int, 1>{}, whole * kUnroll + left);
-  float edge = -INFINITY;
+  auto run = [&](auto& raw, int k) {
+    const int left = row.nv - k * NT;  // (uniform, > 0)
+    if (left < kUnroll * NT) {
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u)
+        if ((k + u) * NT + tid >= row.nv) raw[u] = E::nothing();
+    }
+    if (left > 3 * NT) batch(integral_constant<int, 4>{}, raw, k);
+    else if (left > 2 * NT) batch(integral_constant<int, 3>{}, raw, k);
+    else if (left > NT) batch(integral_constant<int, 2>{}, raw, k);
+    else batch(integral_constant<int, 1>{}, raw, k);
+  };
+  static_assert(kUnroll == 4, "run() takes up to four vectors");
+  if constexpr (NT == 64) {
+    if (row.nv > 0) run(raw, 0);
+    if (second) run(more, kUnroll);
+  } else {
+    for (int k = 0; k * NT < row.nv; k += kUnroll) {
+      if (k > 0) load(raw, k);
+      run(raw, k);
+    }
+  }
   if (tid < row.edges) {
-    edge = E::up(row.x[row.edge_token(tid)]);
     const float x[1][1] = {{edge}};
     s.m = fmaxf(s.m, edge);
     add_batch<ENT>(s, x, edge, c);
