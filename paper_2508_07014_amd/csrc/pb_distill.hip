@@ -568,7 +568,7 @@ int distill_split(const DistillArgs& a, const RowSplit& split, void* workspace, 
 
 template <typename E>
 int distill(const DistillArgs& a, void* workspace, hipStream_t stream) {
-  const RowSplit split = row_split(a.in.V / E::N, a.in.rows);
+  const RowSplit split = split_distill(a.in.V / E::N, a.in.rows);
   if (split.parts > 0) return distill_split<E>(a, split, workspace, stream);
   const int nv = a.in.V / E::N, mark_bytes = (a.in.V + 127) / 128 * 16;  // (a bit per element behind the head)
   // (logits of 16 bits that do not fit in the last cache with their gradient, in long rows, are not kept there either:
@@ -600,7 +600,7 @@ int distill(const DistillArgs& a, void* workspace, hipStream_t stream) {
 }  // namespace lr
 
 int64_t distill_topk_workspace(int dtype, int32_t rows, int32_t V) {
-  const RowSplit split = row_split(V / (dtype == PB_F32 ? lr::F32::N : lr::F16::N), rows);
+  const RowSplit split = split_distill(V / (dtype == PB_F32 ? lr::F32::N : lr::F16::N), rows);
   if (split.parts == 0) return 0;
   return static_cast<int64_t>(rows) * (split.parts * static_cast<int64_t>(sizeof(float4)) + sizeof(lr::List) + 2 * 64 * sizeof(float));
 }

@@ -176,6 +176,12 @@ __device__ __forceinline__ float vec_max(const float (&x)[N]) {
   if constexpr (N % 2 == 0) m = max3(m, x[N - 1], x[N - 1]);
   return m;
 }
+// a b, and 0 where a is 0 and b is infinite (or NaN, which the sums of a find anyway).
+__device__ __forceinline__ float mul_0(float a, float b) {
+  float r;
+  asm("v_mul_legacy_f32 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+  return r;
+}
 // log(1 + r), r > -1/2: the logarithm of u = 1 + r, rounded, by what u lacks of r (Kahan).
 __device__ __forceinline__ float log_1p(float r) {
   const float u = 1.0f + r, d = u - 1.0f;

@@ -65,18 +65,28 @@ struct DistillArgs {
 // At most kMaxParts, so that one wave can join them; at least kLeastParts, whose maxima are to bound 64 alternatives; and
 // about kSplitWaves in all, four vectors a lane where there is so much.
 constexpr int kWaveVectors = 512;  // longest row that one wave takes, in vectors
-constexpr int kMaxParts = 256, kLeastParts = 80, kSplitWaves = 4096, kSplitRows = 256;
+constexpr int kMaxParts = 256, kLeastParts = 80, kSplitWaves = 4096;
 constexpr int kMaxEach = 8;  // (the marks of a part's listed tokens lie in LDS)
 static_assert(kMaxEach * 64 * kMaxParts >= kLogitsMaxV / 4, "the widest row is split");
 struct RowSplit {
   int parts, each;
 };
 inline RowSplit row_split(int vectors, int32_t rows) {
-  if (vectors < 64 * kLeastParts || rows >= kSplitRows) return RowSplit{0, 0};
   const int least = (vectors + 64 * kMaxParts - 1) / (64 * kMaxParts), most = vectors / (64 * kLeastParts) < kMaxEach ? vectors / (64 * kLeastParts) : kMaxEach;
   const int64_t want = static_cast<int64_t>(rows) * vectors / (64 * kSplitWaves);
   const int each = static_cast<int>(want < least ? least : want > most ? (most > least ? most : least) : want);
   return RowSplit{(vectors + 64 * each - 1) / (64 * each), each};
+}
+
+// Which calls are split.  us, split / a workgroup a row, log-probs with 20 alternatives: bf16 V = 131072, 1 row 9.7 / 13.2, 16 rows
+// 13.1 / 15.8, 64 rows 18.2 / 16.7; V = 50000, 1 row 9.5 / 9.6, 16 rows 12.3 / 11.7.
+// Distillation: bf16 V = 50000, 16 rows 8.6 / 10.9, 64 rows 10.9 / 11.7, 128 rows 14.8 / 12.8; V = 131072, 128 rows 21.7 / 23.7, 255 rows
+// 36.8 / 33.7.
+inline RowSplit split_logprobs(int vectors, int32_t rows) {
+  return vectors > 8192 && rows <= 32 ? row_split(vectors, rows) : RowSplit{0, 0};
+}
+inline RowSplit split_distill(int vectors, int32_t rows) {
+  return vectors >= 64 * kLeastParts && rows <= (vectors > 8192 ? 160 : 64) ? row_split(vectors, rows) : RowSplit{0, 0};
 }
 
 int64_t token_logprobs_workspace(int dtype, int32_t rows, int32_t V);

@@ -50,7 +50,7 @@ __device__ __forceinline__ void add_batch(Sums& s, const float (&x)[U][N], float
     for (int i = 0; i < N; ++i) {
       const float d = __builtin_fmaf(x[u][i], c, -s.rc);
       e[i] = exp2_fast(d);
-      if constexpr (ENT) ed[i] = e[i] * fmaxf(d, -1000.0f);  // (-inf: nothing)
+      if constexpr (ENT) ed[i] = mul_0(e[i], d);  // (-inf: nothing)
     }
     if constexpr (ENT) sum_x = u == 0 ? vec_sum(ed) : sum_x + vec_sum(ed);
     sum = u == 0 ? vec_sum(e) : sum + vec_sum(e);
@@ -181,9 +181,14 @@ template <int NT, int N>
 struct TopLds {
   unsigned group[NT == 64 ? 1 : NT];
   int first[NT == 64 ? 1 : NT];
-  u64 list[list_size<N>()];
+  __align__(16) u64 list[list_size<N>()];
   u64 best;
+  int rank[NT == 64 ? 1 : 128];
   int count;
+  __device__ __forceinline__ void clear(int tid) {  // (before a barrier)
+    if (tid == 0) count = 0;
+    if (NT > 64 && tid < 128) rank[tid] = 0;
+  }
 };
 
 // The largest b that at least `n` keys of the row's groups reach (0: there are fewer); a wave holds them all, PER per lane.
@@ -194,7 +199,8 @@ __device__ __forceinline__ int how_many(const unsigned (&key)[PER], unsigned b) 
   for (int i = 0; i < PER; ++i) n += __builtin_popcountll(__ballot(key[i] >= b));
   return n;
 }
-// Halving between 0 .. the largest key: about ln2(groups) steps until exactly n reach the middle, 32 at most (equal keys).
+// Between the smallest and the largest key, in quarters (three counts at a time do not wait for each other): four or five steps
+// until exactly n reach one of the three, 16 at most (equal keys).
 template <int PER>
 __device__ __forceinline__ unsigned bound_of(const unsigned (&key)[PER], int n) {
   if (how_many(key, 1u) < n) return 0u;
@@ -206,11 +212,15 @@ __device__ __forceinline__ unsigned bound_of(const unsigned (&key)[PER], int n) 
   }
   unsigned lo = ~wv::wave_max_u(~least) + 1u, hi = wv::wave_max_u(most);  // n keys or more reach lo, fewer reach hi + 1
   while (lo < hi) {
-    const unsigned mid = lo + (hi - lo) / 2 + 1;
-    const int got = how_many(key, mid);
-    if (got == n) return mid;
-    if (got > n) lo = mid;
-    else hi = mid - 1;
+    const unsigned step = (hi - lo) / 4 + 1, t1 = lo + step, t2 = t1 + (hi - t1 < step ? hi - t1 : step), t3 = t2 + (hi - t2 < step ? hi - t2 : step);
+    const int n1 = how_many(key, t1), n2 = how_many(key, t2), n3 = how_many(key, t3);
+    if (n1 == n) return t1;
+    if (n2 == n) return t2;
+    if (n3 == n) return t3;
+    if (n3 > n) lo = t3;
+    else if (n2 > n) lo = t2, hi = t3 - 1;
+    else if (n1 > n) lo = t1, hi = t2 - 1;
+    else hi = t1 - 1;
   }
   return lo;
 }
@@ -226,13 +236,25 @@ __device__ __forceinline__ float element(const float (&x)[N], int i) {  // x[i],
     for (int k = 0; k < n; ++k) y[k] = i & n ? y[k + n] : y[k];
   return y[0];
 }
+// The same, from a lane's largest key alone where there are lanes enough (a bound of 20 from 64 groups instead of 256 admits 24
+// candidates instead of 21, and takes a quarter of the instructions).
+template <int PER>
+__device__ __forceinline__ unsigned some_bound_of(const unsigned (&key)[PER], int n) {
+  if (PER == 1 || n > 24) return bound_of(key, n);
+  unsigned most[1] = {key[0]};
+#pragma unroll
+  for (int i = 1; i < PER; ++i) most[0] = max(most[0], key[i]);
+  const unsigned b = bound_of(most, n);
+  return b != 0u ? b : bound_of(key, n);
+}
+
 // Candidates into the list: the elements of vector v that the bound admits.
 template <typename E, int NT>
 __device__ __forceinline__ void push_vector(const Row<E>& row, const float (&x)[E::N], int v, unsigned b, int last, TopLds<NT, E::N>& lds) {
-  const float least = ukey_val(v <= last ? b : b + 1);  // (an order as good as that of the keys, -0.0 as 0.0)
+  const float least = b == 0u ? -INFINITY : ukey_val(v <= last ? b : b + 1);  // (as good an order as the keys', -0.0 as 0.0)
   unsigned take = 0;
 #pragma unroll
-  for (int i = 0; i < E::N; ++i) take |= b == 0u || x[i] >= least ? 1u << i : 0u;
+  for (int i = 0; i < E::N; ++i) take |= x[i] >= least ? 1u << i : 0u;
   if (take) {
     int at = atomicAdd(&lds.count, __builtin_popcount(take));
     for (; take; take &= take - 1) {  // (one element as a rule)
@@ -308,10 +330,26 @@ __device__ __forceinline__ void write_list(const Row<E>& row, int tid, float edg
   row_sync<NT>();
   const int count = uniform_i(lds.count);
   if (count <= list_size<E::N>()) {
+    constexpr int W = NT / 64;
+    if (W > 1 && count <= 128) {  // (every wave compares all of them with its share of the list)
+      const int share = (count + W - 1) / W, from = share * (tid >> 6), to = min(from + share, count);
+      for (int i = tid & 63; i < count; i += 64) {
+        const u64 k = lds.list[i];
+        int rank = 0;
+        for (int j = from; j < to; ++j) rank += lds.list[j] > k ? 1 : 0;
+        if (rank) atomicAdd(&lds.rank[i], rank);
+      }
+      row_sync<NT>();
+      if (tid < count && lds.rank[tid] < out.n) out.write(lds.rank[tid], lds.list[tid]);
+      return;
+    }
     for (int i = tid; i < count; i += NT) {
       const u64 k = lds.list[i];
       int rank = 0;
-      for (int j = 0; j < count; ++j) rank += lds.list[j] > k ? 1 : 0;
+      for (int j = 0; j < count; j += 2) {
+        const ulonglong2 q = *reinterpret_cast<const ulonglong2*>(lds.list + j);  // (behind the last one: anything)
+        rank += (q.x > k ? 1 : 0) + (j + 1 < count && q.y > k ? 1 : 0);
+      }
       if (rank < out.n) out.write(rank, k);
     }
     return;
@@ -343,11 +381,11 @@ __device__ __forceinline__ void write_list(const Row<E>& row, int tid, float edg
 template <typename E, int NT>
 __device__ __forceinline__ void write_alternatives(const Row<E>& row, int tid, const Tops& tops, float edge, const TopOut& out,
                                                    TopLds<NT, E::N>& lds) {
-  constexpr int PER = NT == 64 ? 1 : kGroups / 64, PARTS = NT == 64 ? 1 : NT / kGroups;
+  constexpr int GROUPS = NT < kGroups ? NT : kGroups, PER = GROUPS / 64, PARTS = NT / GROUPS;
   const int lane = tid & 63;
   const bool some = tid < row.nv;
   const unsigned own = some ? order32(tops.m1) : 0u;
-  if (tid == 0) lds.count = 0;
+  lds.clear(tid);
   unsigned key[PER];
   if constexpr (NT == 64) {
     key[0] = own;
@@ -358,10 +396,10 @@ __device__ __forceinline__ void write_alternatives(const Row<E>& row, int tid, c
     for (int i = 0; i < PER; ++i) {
       key[i] = 0u;
 #pragma unroll
-      for (int p = 0; p < PARTS; ++p) key[i] = max(key[i], lds.group[kGroups * p + 64 * i + lane]);
+      for (int p = 0; p < PARTS; ++p) key[i] = max(key[i], lds.group[GROUPS * p + 64 * i + lane]);
     }
   }
-  const unsigned b = bound_of(key, out.n);
+  const unsigned b = some_bound_of(key, out.n);
   // Elements equal to the bound count in the order of their tokens.  Where many groups have it for their maximum (masked
   // rows with fewer tokens left than alternatives wanted, flat rows), only those up to vector `last` are wanted: the groups
   // above it are not enough by `need`, and the `need` lowest vectors in which a group has its maximum hold so many.
@@ -378,7 +416,7 @@ __device__ __forceinline__ void write_alternatives(const Row<E>& row, int tid, c
         first[i] = INT_MAX;
 #pragma unroll
         for (int p = 0; p < PARTS; ++p) {
-          const int at = kGroups * p + 64 * i + lane;
+          const int at = GROUPS * p + 64 * i + lane;
           if (lds.group[at] == b) first[i] = min(first[i], lds.first[at]);
         }
       }
@@ -464,15 +502,15 @@ __global__ __launch_bounds__(NT == 64 ? 256 : NT) void logprobs_kernel(LogprobAr
   // (all that does not depend on other loads is requested before the first wait: the token, the first vectors, the edge)
   int given = -1;
   if (tid < a.n_tokens) given = a.tokens[r * a.n_tokens + tid];
-  v4u raw[kUnroll], more[NT == 64 ? kUnroll : 1];
+  constexpr bool AHEAD = NT == 64;  // (a wave requests all of its row at once; more waves hide each other's waits)
+  v4u raw[kUnroll], more[AHEAD ? kUnroll : 1];
   auto load = [&](auto& to, int k) {  // vectors k, k + 1, ... of the thread; behind the row's end its last one again
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) to[u] = row.vec(min((k + u) * NT + tid, row.nv - 1));
   };
-  const bool second = NT == 64 && row.nv > kUnroll * NT;
   if (row.nv > 0) load(raw, 0);
-  if constexpr (NT == 64)
-    if (second) load(more, kUnroll);
+  if constexpr (AHEAD)
+    if (row.nv > kUnroll * NT) load(more, kUnroll);
   float edge = -INFINITY;
   if (tid < row.edges) edge = E::up(row.x[row.edge_token(tid)]);
   float given_x = 0.0f;
@@ -507,9 +545,9 @@ __global__ __launch_bounds__(NT == 64 ? 256 : NT) void logprobs_kernel(LogprobAr
     else batch(integral_constant<int, 1>{}, raw, k);
   };
   static_assert(kUnroll == 4, "run() takes up to four vectors");
-  if constexpr (NT == 64) {
+  if constexpr (AHEAD) {
     if (row.nv > 0) run(raw, 0);
-    if (second) run(more, kUnroll);
+    if (row.nv > kUnroll * NT) run(more, kUnroll);
   } else {
     for (int k = 0; k * NT < row.nv; k += kUnroll) {
       if (k > 0) load(raw, k);
@@ -539,11 +577,16 @@ __global__ __launch_bounds__(NT == 64 ? 256 : NT) void logprobs_kernel(LogprobAr
   }
 }
 
-// Few long rows: every wave takes 64 * `each` vectors of a row and leaves their part (the maximum and the sums) in the
-// workspace; a workgroup per row joins them.  The parts' maxima bound the alternatives as the lanes' do above, and the
-// parts that reach the bound are read again.
-template <typename E, bool ENT>
-__global__ __launch_bounds__(256) void logprobs_parts_kernel(LogprobArgs a, int parts, int each, Part* __restrict__ out) {
+// Few long rows: every wave takes 64 * `each` vectors of a row and leaves their part in the workspace, with the largest element
+// of the vectors, its token and the largest of the others; a workgroup per row joins them.  The parts' largest elements bound
+// the alternatives as the lanes' do above, and are candidates themselves; the few parts with a second one are read again.
+struct PartRecord {
+  Part sums;
+  float top, second;
+  int token, unused;
+};
+template <typename E, bool ENT, bool TOP>
+__global__ __launch_bounds__(256) void logprobs_parts_kernel(LogprobArgs a, int parts, int each, PartRecord* __restrict__ out) {
   const int64_t at = static_cast<int64_t>(blockIdx.x) * 4 + uniform_i(threadIdx.x >> 6);
   const int64_t r = at / parts;
   if (r >= a.in.rows) return;
@@ -552,6 +595,7 @@ __global__ __launch_bounds__(256) void logprobs_parts_kernel(LogprobArgs a, int 
   const float c = a.in.c;
   const int end = min(begin + 64 * each, row.nv);
   Sums s(a.in.far);
+  Tops tops;
   for (int v0 = begin + lane; v0 < end; v0 += 64 * kUnroll) {
     v4u raw[kUnroll];
 #pragma unroll
@@ -563,6 +607,7 @@ __global__ __launch_bounds__(256) void logprobs_parts_kernel(LogprobArgs a, int 
         float x[1][E::N];
         E::unpack(raw[u], x[0]);
         const float vm = vec_max(x[0]);
+        if constexpr (TOP) tops.add(vm, v0 + 64 * u);
         s.m = fmaxf(s.m, vm);
         add_batch<ENT>(s, x, vm, c);
       }
@@ -584,14 +629,32 @@ __global__ __launch_bounds__(256) void logprobs_parts_kernel(LogprobArgs a, int 
     }
     if (has_edge) add(edge);
   });
-  if (lane == 0) out[at] = p;
+  PartRecord rec{p, -INFINITY, -INFINITY, 0, 0};
+  if constexpr (TOP) {
+    // (a lane without vectors, or with nothing but -inf in them, keeps its first one in k1)
+    const int own = tops.m1 == -INFINITY ? begin + lane : tops.k1;
+    rec.top = wave_max(tops.m1);
+    const int v = wv::wave_min_nn(tops.m1 == rec.top && own < end ? own : INT_MAX);
+    if (v < end) {
+      float x[E::N], rest = -INFINITY;
+      E::unpack(row.vec(v), x);
+      int i = E::N;
+#pragma unroll
+      for (int k = E::N - 1; k >= 0; --k) i = x[k] == rec.top ? k : i;
+#pragma unroll
+      for (int k = 0; k < E::N; ++k) rest = k == i ? rest : fmaxf(rest, x[k]);
+      rec.token = row.token(v, min(i, E::N - 1));
+      rec.second = fmaxf(rest, wave_max(own == v ? tops.m2 : tops.m1));
+    }
+  }
+  if (lane == 0) out[at] = rec;
 }
 
 // Every wave joins all parts by itself (a few instructions, no barrier); the parts that reach the bound are dealt out to the
 // waves.
 constexpr int kJoinThreads = 512;
 template <typename E, bool ENT, bool TOP>
-__global__ __launch_bounds__(kJoinThreads) void logprobs_join_kernel(LogprobArgs a, int parts, int each, const Part* __restrict__ in) {
+__global__ __launch_bounds__(kJoinThreads) void logprobs_join_kernel(LogprobArgs a, int parts, int each, const PartRecord* __restrict__ in) {
   constexpr int NT = kJoinThreads, W = NT / 64, PER = kMaxParts / 64;
   __shared__ TopLds<TOP ? NT : 64, TOP ? E::N : 1> lds;
   __shared__ int s_found[W];
@@ -599,19 +662,30 @@ __global__ __launch_bounds__(kJoinThreads) void logprobs_join_kernel(LogprobArgs
   const int64_t r = blockIdx.x;
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform_i(tid >> 6);
   if constexpr (TOP) {
-    if (tid == 0) lds.count = 0;
+    lds.clear(tid);
     __syncthreads();
   }
   const Row<E> row = row_at<E>(a.in.x, a.in.stride, r, a.in.V);
   const float c = a.in.c;
   Part p[PER];
   unsigned key[PER];
+  float top[PER], second[PER];
+  int token[PER];
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
     const int at = 64 * i + lane;
-    p[i] = at < parts ? in[r * parts + at] : Part{-INFINITY, 0.0f, 0.0f, 0.0f};
+    p[i] = Part{-INFINITY, 0.0f, 0.0f, 0.0f};
+    top[i] = second[i] = -INFINITY;
+    token[i] = 0;
+    if (at < parts) {
+      const PartRecord rec = in[r * parts + at];
+      p[i] = rec.sums;
+      top[i] = rec.top;
+      second[i] = rec.second;
+      token[i] = rec.token;
+    }
     // (a row's head may leave its last part empty)
-    key[i] = at < parts && (at == 0 || at * 64 * each < row.nv) ? order32(p[i].m) : 0u;
+    key[i] = at < parts && at * 64 * each < row.nv ? order32(top[i]) : 0u;
   }
   float given_x, edge = -INFINITY;
   const int given = load_given<E>(a, r, row, tid, given_x);
@@ -622,23 +696,32 @@ __global__ __launch_bounds__(kJoinThreads) void logprobs_join_kernel(LogprobArgs
   if constexpr (TOP) {
     if (sums.bad) return;
     const TopOut out{a.n_top, sums.base, a.in.inv_temp, sums.log_s, a.top_tokens + r * a.n_top, a.top_logp + r * a.n_top};
-    const unsigned b = bound_of(key, out.n);
+    const unsigned b = some_bound_of(key, out.n);
     const bool ties = b != 0u && how_many(key, b) > out.n + 16;  // (then the elements equal to the bound are looked for in order)
     const int last = ties ? -1 : INT_MAX;
     int n = 0;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
       const bool take = key[i] > b || (key[i] == b && key[i] != 0u && !ties);
-      const u64 who = __ballot(take);
-      if (take) s_part[wave][n + __builtin_amdgcn_mbcnt_hi(static_cast<unsigned>(who >> 32), __builtin_amdgcn_mbcnt_lo(static_cast<unsigned>(who), 0u))] = static_cast<short>(64 * i + lane);
+      if (wave == W - 1 && take) {
+        const int to = atomicAdd(&lds.count, 1);
+        if (to < list_size<E::N>()) lds.list[to] = order64(key[i], token[i]);
+      }
+      const unsigned k2 = order32(second[i]);
+      const bool again = take && (ties ? k2 > b : k2 >= b);
+      const u64 who = __ballot(again);
+      if (again) s_part[wave][n + __builtin_amdgcn_mbcnt_hi(static_cast<unsigned>(who >> 32), __builtin_amdgcn_mbcnt_lo(static_cast<unsigned>(who), 0u))] = static_cast<short>(64 * i + lane);
       n += __builtin_popcountll(who);
     }
     row_sync<64>();
-    for (int i = wave; i < n; i += W) {
-      const int begin = uniform_i(s_part[wave][i]) * 64 * each;
-      for (int v = begin + lane; v < min(begin + 64 * each, row.nv); v += 64) {
+    for (int t0 = wave; t0 < n * each; t0 += W) {  // (64 vectors of a part a turn)
+      const int i = t0 / each, part = uniform_i(s_part[wave][i]), v = part * 64 * each + (t0 - i * each) * 64 + lane;
+      if (v < row.nv) {
         float x[E::N];
         E::unpack(row.vec(v), x);
+        const int skip = in[r * parts + part].token - row.token(v, 0);  // (the part's largest element is a candidate already)
+#pragma unroll
+        for (int k = 0; k < E::N; ++k) x[k] = k == skip ? NAN : x[k];
         push_vector<E, NT>(row, x, v, b, last, lds);
       }
     }
@@ -719,12 +802,15 @@ template <typename E>
 int forward(const LogprobArgs& a, void* workspace, hipStream_t stream) {
   const bool ent = a.entropy || a.stats, top = a.n_top > 0;
   auto done = [] { return hipGetLastError() == hipSuccess ? PB_OK : PB_EHIP; };
-  const RowSplit split = row_split(a.in.V / E::N, a.in.rows);
+  const RowSplit split = split_logprobs(a.in.V / E::N, a.in.rows);
   if (split.parts > 0) {
-    Part* ws = static_cast<Part*>(workspace);
+    PartRecord* ws = static_cast<PartRecord*>(workspace);
     const int grid = static_cast<int>((static_cast<int64_t>(a.in.rows) * split.parts + 3) / 4);
-    if (ent) logprobs_parts_kernel<E, true><<<grid, 256, 0, stream>>>(a, split.parts, split.each, ws);
-    else logprobs_parts_kernel<E, false><<<grid, 256, 0, stream>>>(a, split.parts, split.each, ws);
+    auto begin = [&](auto kernel) { kernel<<<grid, 256, 0, stream>>>(a, split.parts, split.each, ws); };
+    if (ent && top) begin(logprobs_parts_kernel<E, true, true>);
+    else if (ent) begin(logprobs_parts_kernel<E, true, false>);
+    else if (top) begin(logprobs_parts_kernel<E, false, true>);
+    else begin(logprobs_parts_kernel<E, false, false>);
     if (done() != PB_OK) return PB_EHIP;
     auto finish = [&](auto kernel) { kernel<<<a.in.rows, kJoinThreads, 0, stream>>>(a, split.parts, split.each, ws); return done(); };
     if (ent && top) return finish(logprobs_join_kernel<E, true, true>);
@@ -741,9 +827,13 @@ int forward(const LogprobArgs& a, void* workspace, hipStream_t stream) {
     if (top) return go(logprobs_kernel<E, NT, false, true>);
     return go(logprobs_kernel<E, NT, false, false>);
   };
-  if (a.in.V / E::N <= kWaveVectors) return pick(std::integral_constant<int, 64>{});
-  if (a.in.rows >= 1024) return pick(std::integral_constant<int, 256>{});
-  return pick(std::integral_constant<int, 1024>{});
+  // Threads a row, us with 64 / 128 / 256 / 512 / 1024: 16384 x 8192 bf16, 8 alternatives: 58 57 73 143 249; 1024 x 16384, 20 of them:
+  // - 15.8 16.0 21 29; 256 x 16384: - 11.3 9.9 10.2 12.1; 8192 x 32001: - 110 104 122 177; 256 x 131072: - 34 22 19 21.
+  const int nv = a.in.V / E::N;
+  if (nv <= kWaveVectors) return pick(std::integral_constant<int, 64>{});
+  if (nv <= 2048 && a.in.rows >= 1024) return pick(std::integral_constant<int, 128>{});
+  if (nv <= 8192) return pick(std::integral_constant<int, 256>{});
+  return pick(std::integral_constant<int, 512>{});
 }
 
 // Logits that with their gradient do not fit in the last cache (256 MB) are not kept there either: 8192 x 32001 bf16 192 -> 188 us,
@@ -769,7 +859,7 @@ int backward(const LogprobGradArgs& a, hipStream_t stream) {
 }  // namespace lr
 
 int64_t token_logprobs_workspace(int dtype, int32_t rows, int32_t V) {
-  return static_cast<int64_t>(rows) * row_split(V / (dtype == PB_F32 ? lr::F32::N : lr::F16::N), rows).parts * static_cast<int64_t>(sizeof(lr::Part));
+  return static_cast<int64_t>(rows) * split_logprobs(V / (dtype == PB_F32 ? lr::F32::N : lr::F16::N), rows).parts * static_cast<int64_t>(sizeof(lr::PartRecord));
 }
 int launch_token_logprobs(int dtype, const LogprobArgs& a, void* workspace, hipStream_t stream) {
   return dtype == PB_F32   ? lr::forward<lr::F32>(a, workspace, stream)
