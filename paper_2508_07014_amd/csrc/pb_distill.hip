@@ -568,7 +568,7 @@ int distill_split(const DistillArgs& a, const RowSplit& split, void* workspace, 
 
 template <typename E>
 int distill(const DistillArgs& a, void* workspace, hipStream_t stream) {
-  const RowSplit split = split_distill(a.in.V / E::N, a.in.rows);
+  const RowSplit split = split_distill(a.in.V / E::N, a.in.all_rows);
   if (split.parts > 0) return distill_split<E>(a, split, workspace, stream);
   const int nv = a.in.V / E::N, mark_bytes = (a.in.V + 127) / 128 * 16;  // (a bit per element behind the head)
   // (logits of 16 bits that do not fit in the last cache with their gradient, in long rows, are not kept there either:

@@ -16,6 +16,7 @@ struct LogitRows {
   const void* x;       // [rows, stride], enum pb_dtype
   int64_t stride;      // in elements
   int32_t rows, V;
+  int32_t all_rows;    // of the call, of which these are a slice: what decides whether rows are split
   float inv_temp;      // 1 / T
   float c;             // log2(e) / T
   float far;           // logits further from 0 than this: see kFar
@@ -25,7 +26,7 @@ struct LogitRows {
 constexpr float kFar = 1048576.0f;
 inline LogitRows logit_rows(const void* x, int64_t stride, int32_t rows, int32_t V, float temperature) {
   const double c = 1.44269504088896340736 / temperature;
-  return LogitRows{x, stride, rows, V, static_cast<float>(1.0 / temperature), static_cast<float>(c), static_cast<float>(kFar / c)};
+  return LogitRows{x, stride, rows, V, rows, static_cast<float>(1.0 / temperature), static_cast<float>(c), static_cast<float>(kFar / c)};
 }
 
 struct LogprobArgs {
@@ -78,12 +79,12 @@ inline RowSplit row_split(int vectors, int32_t rows) {
   return RowSplit{(vectors + 64 * each - 1) / (64 * each), each};
 }
 
-// Which calls are split.  us, split / a workgroup a row, log-probs with 20 alternatives: bf16 V = 131072, 1 row 9.7 / 13.2, 16 rows
-// 13.1 / 15.8, 64 rows 18.2 / 16.7; V = 50000, 1 row 9.5 / 9.6, 16 rows 12.3 / 11.7.
-// Distillation: bf16 V = 50000, 16 rows 8.6 / 10.9, 64 rows 10.9 / 11.7, 128 rows 14.8 / 12.8; V = 131072, 128 rows 21.7 / 23.7, 255 rows
-// 36.8 / 33.7.
+// Which calls are split.  us, split / a workgroup a row, bf16: log-probs with 20 alternatives, V = 50000, 1 row 8.4 / 9.6, 16 rows
+// 9.9 / 11.4, 64 rows 12.0 / 12.1, 128 rows 14.5 / 13.5; V = 131072, 64 rows 14.9 / 15.9, 128 rows 18.2 / 16.6; without alternatives,
+// 64 rows 8.7 / 10.7.  Distillation: V = 50000, 16 rows 8.6 / 10.9, 64 rows 10.9 / 11.7, 128 rows 14.8 / 12.8; V = 131072, 128 rows
+// 21.7 / 23.7, 255 rows 36.8 / 33.7.
 inline RowSplit split_logprobs(int vectors, int32_t rows) {
-  return vectors > 8192 && rows <= 32 ? row_split(vectors, rows) : RowSplit{0, 0};
+  return vectors >= 64 * kLeastParts && rows <= 64 ? row_split(vectors, rows) : RowSplit{0, 0};
 }
 inline RowSplit split_distill(int vectors, int32_t rows) {
   return vectors >= 64 * kLeastParts && rows <= (vectors > 8192 ? 160 : 64) ? row_split(vectors, rows) : RowSplit{0, 0};

@@ -437,7 +437,8 @@ __device__ __forceinline__ void write_alternatives(const Row<E>& row, int tid, c
   // the other vectors of lanes that have more above the bound: of one such lane after the other by the whole wave, or, where
   // they are many, by all of them at once
   if (row.nv > NT) {
-    u64 more = __ballot(mine && order32(tops.m2) >= b);
+    const unsigned k2 = order32(tops.m2);
+    u64 more = __ballot(mine && (k2 > b || (k2 == b && (v1 == tid ? tid + NT : tid) <= last)));
     if (__builtin_popcountll(more) < row.nv / NT) {
       for (; more; more &= more - 1) {
         const int from = wv::first_lane(more), skip = __builtin_amdgcn_readlane(v1, from);
@@ -802,7 +803,7 @@ template <typename E>
 int forward(const LogprobArgs& a, void* workspace, hipStream_t stream) {
   const bool ent = a.entropy || a.stats, top = a.n_top > 0;
   auto done = [] { return hipGetLastError() == hipSuccess ? PB_OK : PB_EHIP; };
-  const RowSplit split = split_logprobs(a.in.V / E::N, a.in.rows);
+  const RowSplit split = split_logprobs(a.in.V / E::N, a.in.all_rows);
   if (split.parts > 0) {
     PartRecord* ws = static_cast<PartRecord*>(workspace);
     const int grid = static_cast<int>((static_cast<int64_t>(a.in.rows) * split.parts + 3) / 4);

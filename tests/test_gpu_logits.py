@@ -315,6 +315,81 @@ def test_distill_many_rows(rows, V, K, tail, kind):
     check_distill(rng, view, values, kind, V, 1.0, t, l, tail, (rows, V, K, tail, kind))
 
 
+# Rows of every kernel shape, as many as send the call there (the shape is chosen by vectors a row and rows): 8 rows of each
+# call are compared.
+MANY = [(1100, 4104), (1030, 6001), (1025, 16400), (70, 8200), (70, 20001), (70, 30000), (70, 33001), (70, 50000), (70, 70001),
+        (170, 70000), (170, 131072), (300, 33000), (20, 41000), (64, 50001), (160, 70001)]
+
+
+@pytest.mark.parametrize("kind", list(KIND))
+@pytest.mark.parametrize("rows,V", MANY)
+def test_kernel_shapes(rows, V, kind):
+    rng = np.random.default_rng(rows + V)
+    some = np.unique(np.concatenate([[0, rows - 1], rng.integers(0, rows, 6)]))
+    g = torch.Generator(device=DEV)
+    g.manual_seed(rows + V)
+    x = 2.5 * torch.randn((rows, V), generator=g, device=DEV)
+    x[torch.from_numpy(some).to(DEV)] = dev(rows_of(rng, len(some), V, kind).astype(np.float32))
+    shift = int(rng.integers(0, 8))
+    buf = torch.full((shift + rows * V,), JUNK, dtype=KIND[kind][1], device=DEV)
+    view = torch.as_strided(buf, (rows, V), (V, 1), shift)
+    view.copy_(x)
+    at = torch.from_numpy(some).to(DEV)
+    values = host(view[at])
+    tokens = tokens_of(rng, values, 2)
+    all_tokens = rng.integers(0, V, (rows, 2))
+    all_tokens[some] = tokens
+    d_tokens = dev(all_tokens.astype(np.int32))
+    for top, ent in ((0, True), (20, True), (7, False)):
+        o = run_logprobs(view, kind, V, V, 1.0, d_tokens, top, ent, ent)
+        check_logprobs({k: None if v is None else v[at] for k, v in o.items() if k != "ws"}, values, 1.0, tokens, top, (rows, V, kind, top))
+    stats = run_logprobs(view, kind, V, V, 1.0)["stats"]
+    gl, ge = rng.normal(0, 1, (rows, 2)).astype(np.float32), rng.normal(0, 1, rows).astype(np.float32)
+    grad = torch.full_like(buf, JUNK)
+    out = torch.as_strided(grad, (rows, V), (V, 1), shift)
+    run_backward(view, kind, V, V, 1.0, stats, d_tokens, dev(gl), dev(ge), out, V)
+    got = host(out[at])
+    for i, r in enumerate(some):
+        want, err = R.logprobs_grad(values[i], 1.0, tokens[i], gl[r].astype(np.float64), float(ge[r]))
+        R.check(got[i], want, R.rounded(err, want, kind), (rows, V, kind, r))
+    t, l = teacher(rng, values, 17, 1.0, 0.1)
+    all_t, all_l = rng.integers(0, V, (rows, 17)), np.full((rows, 17), -4.0, np.float32)
+    all_t[some], all_l[some] = t, l
+    w = rng.normal(0, 1, rows).astype(np.float32)
+    for tail in (False, True):
+        loss = torch.full((rows,), JUNK, device=DEV)
+        out.fill_(JUNK)
+        run_distill(view, kind, V, V, 1.0, dev(all_t.astype(np.int32)), dev(all_l), tail, dev(w), loss, out, V)
+        got, got_loss = host(out[at]), host(loss[at])
+        for i, r in enumerate(some):
+            want, gr, e, eg = R.distill(values[i], 1.0, t[i], l[i].astype(np.float64), tail, float(w[r]))
+            R.check(got_loss[i], want, e * (1 + 2 ** -20) + R.U * abs(want) + 1e-37, (rows, V, kind, tail, r))
+            R.check(got[i], gr, R.rounded(eg, gr, kind), (rows, V, kind, tail, r))
+        assert not bool((out == JUNK).any())      # every element of every row was written
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+def test_tensors_past_the_last_cache(kind):
+    """Logits and gradients that do not fit in 256 MB together go past the caches: the same results as for a part of the rows."""
+    V, rows = 17001, 4200
+    g = torch.Generator(device=DEV)
+    g.manual_seed(1)
+    view = (2.5 * torch.randn((rows, V), generator=g, device=DEV)).to(KIND[kind][1])
+    rng = np.random.default_rng(8)
+    t = dev(np.stack([rng.permutation(V)[:9] for _ in range(rows)]).astype(np.int32))
+    l = torch.full((rows, 9), -3.0, device=DEV)
+    tok, ones = t[:, :1].contiguous(), torch.ones((rows, 1), device=DEV)
+    stats = run_logprobs(view, kind, V, V, 1.0, tok)["stats"]
+    whole, loss = [torch.empty_like(view) for _ in range(2)], torch.empty(rows, device=DEV)
+    run_backward(view, kind, V, V, 1.0, stats, tok, ones, None, whole[0], V)
+    run_distill(view, kind, V, V, 1.0, t, l, True, None, loss, whole[1], V)
+    for lo, hi in ((0, 500), (3700, 4200)):
+        part, some = [torch.empty_like(view[lo:hi]) for _ in range(2)], torch.empty(hi - lo, device=DEV)
+        run_backward(view[lo:hi], kind, V, V, 1.0, stats[lo:hi], tok[lo:hi], ones, None, part[0], V)
+        run_distill(view[lo:hi], kind, V, V, 1.0, t[lo:hi], l[lo:hi], True, None, some, part[1], V)
+        assert torch.equal(part[0], whole[0][lo:hi]) and torch.equal(part[1], whole[1][lo:hi]) and torch.equal(some, loss[lo:hi])
+
+
 @pytest.mark.parametrize("tail", [False, True])
 def test_lists_that_cover_the_row(tail):
     """Every token listed, every token but one, all tokens with mass listed: nothing, or little, is left for the rest."""
