@@ -169,10 +169,11 @@ __device__ __forceinline__ List load_list(const DistillArgs& a, int64_t r, const
   e = Entry{-1, 0.0f, -INFINITY, 0.0f};
   if (lane < a.K) {
     const int t = a.tokens[r * a.K + lane];
+    const float value = a.logp[r * a.K + lane];
     if (static_cast<unsigned>(t) < static_cast<unsigned>(row.V)) {
       e.token = t;
       e.x = E::up(row.x[t]);
-      e.log_q = a.logp[r * a.K + lane];
+      e.log_q = value;
     }
   }
   List l;
@@ -215,10 +216,10 @@ __device__ __forceinline__ Student student(const RowSums& sums, const List& list
   return s;
 }
 // Sum of q over the entries of the lane's token (it may be listed more than once).  By one wave; `table`, kHashBits bits of
-// LDS, tells whether any two tokens can be the same (6 % of lists of 32 different ones are taken for such), which they
-// hardly ever are: 64 comparisons of every lane took 1.5 us.
+// LDS, finds the few tokens that can be the same as another (in lists of 64 different ones every fifth has such a pair):
+// 64 comparisons of every lane took 3.2 us.
 constexpr int kHashBits = 8192;
-__device__ __forceinline__ float mass_of(const Entry& e, int K, unsigned* table) {
+__device__ __forceinline__ float mass_of(const Entry& e, unsigned* table) {
   const v4u none = {0u, 0u, 0u, 0u};
 #pragma unroll
   for (int i = 0; i < kHashBits / 128; i += 64) reinterpret_cast<v4u*>(table)[i + (threadIdx.x & 63)] = none;
@@ -228,10 +229,16 @@ __device__ __forceinline__ float mass_of(const Entry& e, int K, unsigned* table)
     const unsigned h = static_cast<unsigned>(e.token) * 2654435761u >> 19;
     seen = atomicOr(&table[h >> 5], 1u << (h & 31)) >> (h & 31) & 1u;
   }
-  if (__ballot(seen != 0u) == 0) return e.q;
-  float mass = 0.0f;
-  for (int k = 0; k < K; ++k)
-    if (__builtin_amdgcn_readlane(e.token, k) == e.token) mass += __int_as_float(__builtin_amdgcn_readlane(__float_as_int(e.q), k));
+  float mass = e.q;
+  for (u64 left = __ballot(seen != 0u); left != 0;) {
+    const int token = __builtin_amdgcn_readlane(e.token, wv::first_lane(left));
+    const u64 same = __ballot(e.token == token);
+    if (__builtin_popcountll(same) > 1) {
+      const float sum = wave_sum(e.token == token ? e.q : 0.0f);
+      mass = e.token == token ? sum : mass;
+    }
+    left &= ~same;
+  }
   return mass;
 }
 // By one wave: the row's loss.  Terms that cancel, and log-probs of masked tokens that may pass the fp32 range: in 64 bits.
@@ -290,7 +297,7 @@ __global__ __launch_bounds__(NT == 64 ? 256 : NT) void distill_kernel(DistillArg
   float mass = 0.0f;
   if (lister) {
     list = load_list<E, TAIL>(a, r, row, tid & 63, e);
-    if (a.grad) mass = mass_of(e, a.K, s_table[sub]);
+    if (a.grad) mass = mass_of(e, s_table[sub]);
   }
   if constexpr (NT > 64) {
     if (tid == 0) s_list = list;
@@ -410,18 +417,24 @@ __global__ __launch_bounds__(256) void distill_parts_kernel(DistillArgs a, int p
   const int64_t at = static_cast<int64_t>(blockIdx.x) * 4 + sub;
   const int64_t r = at / (parts + 1);
   if (r >= a.in.rows) return;
-  const int part = static_cast<int>(at - r * (parts + 1)), begin = part * 64 * each;
+  const int part = static_cast<int>(at - r * (parts + 1)) - 1, begin = part * 64 * each;  // (-1: the list, the longest way)
   const Row<E> row = row_at<E>(a.in.x, a.in.stride, r, a.in.V);
   const float c = a.in.c;
   const int end = min(begin + 64 * each, row.nv);
-  if (part == parts) {
+  if (part < 0) {
     Entry e;
     const List l = load_list<E, TAIL>(a, r, row, lane, e);
     if (lane == 0) ws.lists[r] = l;
     ws.x[r * 64 + lane] = e.x;
-    ws.mass[r * 64 + lane] = mass_of(e, a.K, s_table);
+    ws.mass[r * 64 + lane] = mass_of(e, s_table);
     return;
   }
+  v4u raw[kGradUnroll];  // (requested before the list)
+  auto load = [&](int v0) {
+#pragma unroll
+    for (int u = 0; u < kGradUnroll; ++u) raw[u] = row.vec(min(v0 + 64 * u, row.nv - 1));
+  };
+  load(begin + lane);
   if constexpr (TAIL) {
     if (lane < 16 * each) s_marks[sub][lane] = 0u;
     if (16 * each > 64 && lane < 16 * each - 64) s_marks[sub][64 + lane] = 0u;
@@ -441,10 +454,7 @@ __global__ __launch_bounds__(256) void distill_parts_kernel(DistillArgs a, int p
   auto listed = [&](int v) -> unsigned { return TAIL ? reinterpret_cast<const unsigned char*>(s_marks[sub])[v - begin] : 0u; };
   Sums s(a.in.far);
   for (int v0 = begin + lane; v0 < end; v0 += 64 * kGradUnroll) {
-    v4u raw[kGradUnroll];
-#pragma unroll
-    for (int u = 0; u < kGradUnroll; ++u)
-      if (v0 + 64 * u < end) raw[u] = row.vec(v0 + 64 * u);
+    if (v0 > begin + lane) load(v0);
 #pragma unroll
     for (int u = 0; u < kGradUnroll; ++u)
       if (v0 + 64 * u < end) {

@@ -186,7 +186,7 @@ __device__ __forceinline__ float mul_0(float a, float b) {
 __device__ __forceinline__ float log_1p(float r) {
   const float u = 1.0f + r, d = u - 1.0f;
   const float l = __builtin_amdgcn_logf(u) * kLn2;  // (base 2)
-  return d == 0.0f ? r : fabsf(d) < 0.5f ? l * (r / d) : l;
+  return d == 0.0f ? r : fabsf(d) < 0.5f ? l * (r * __builtin_amdgcn_rcpf(d)) : l;
 }
 template <int N>
 __device__ __forceinline__ float vec_sum(float (&x)[N]) {  // (in pairs: fewer roundings in a row)

@@ -63,17 +63,16 @@ struct DistillArgs {
 };
 
 // Few long rows are split over the chip: `parts` waves a row, each with 64 * `each` vectors of 16 bytes (0: not split).
-// At most kMaxParts, so that one wave can join them; at least kLeastParts, whose maxima are to bound 64 alternatives; and
-// about kSplitWaves in all, four vectors a lane where there is so much.
+// At most kMaxParts, so that one wave can join them; at least `few`; and about kSplitWaves in all.
 constexpr int kWaveVectors = 512;  // longest row that one wave takes, in vectors
-constexpr int kMaxParts = 256, kLeastParts = 80, kSplitWaves = 4096;
+constexpr int kMaxParts = 256, kSplitWaves = 4096;
 constexpr int kMaxEach = 8;  // (the marks of a part's listed tokens lie in LDS)
 static_assert(kMaxEach * 64 * kMaxParts >= kLogitsMaxV / 4, "the widest row is split");
 struct RowSplit {
   int parts, each;
 };
-inline RowSplit row_split(int vectors, int32_t rows) {
-  const int least = (vectors + 64 * kMaxParts - 1) / (64 * kMaxParts), most = vectors / (64 * kLeastParts) < kMaxEach ? vectors / (64 * kLeastParts) : kMaxEach;
+inline RowSplit row_split(int vectors, int32_t rows, int few) {
+  const int least = (vectors + 64 * kMaxParts - 1) / (64 * kMaxParts), most = vectors / (64 * few) < kMaxEach ? vectors / (64 * few) : kMaxEach;
   const int64_t want = static_cast<int64_t>(rows) * vectors / (64 * kSplitWaves);
   const int each = static_cast<int>(want < least ? least : want > most ? (most > least ? most : least) : want);
   return RowSplit{(vectors + 64 * each - 1) / (64 * each), each};
@@ -83,11 +82,12 @@ inline RowSplit row_split(int vectors, int32_t rows) {
 // 9.9 / 11.4, 64 rows 12.0 / 12.1, 128 rows 14.5 / 13.5; V = 131072, 64 rows 14.9 / 15.9, 128 rows 18.2 / 16.6; without alternatives,
 // 64 rows 8.7 / 10.7.  Distillation: V = 50000, 16 rows 8.6 / 10.9, 64 rows 10.9 / 11.7, 128 rows 14.8 / 12.8; V = 131072, 128 rows
 // 21.7 / 23.7, 255 rows 36.8 / 33.7.
+constexpr int kSplitVectors = 5120;
 inline RowSplit split_logprobs(int vectors, int32_t rows) {
-  return vectors >= 64 * kLeastParts && rows <= 64 ? row_split(vectors, rows) : RowSplit{0, 0};
+  return vectors >= kSplitVectors && rows <= 64 ? row_split(vectors, rows, 80) : RowSplit{0, 0};  // (the parts are to bound 64 alternatives)
 }
 inline RowSplit split_distill(int vectors, int32_t rows) {
-  return vectors >= 64 * kLeastParts && rows <= (vectors > 8192 ? 160 : 64) ? row_split(vectors, rows) : RowSplit{0, 0};
+  return vectors >= kSplitVectors && rows <= (vectors > 8192 ? 160 : 64) ? row_split(vectors, rows, 16) : RowSplit{0, 0};
 }
 
 int64_t token_logprobs_workspace(int dtype, int32_t rows, int32_t V);

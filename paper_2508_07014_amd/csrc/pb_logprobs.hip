@@ -135,7 +135,7 @@ __device__ __forceinline__ RowSums finish(const Part& p, float c) {
   r.m = r.bad ? NAN : p.m;
   r.base = empty ? 0.0f : p.m;
   r.log_s = r.bad ? NAN : empty ? 0.0f : log_s - rounded * kLn2;
-  r.H = r.bad ? NAN : empty ? 0.0f : log_s - p.X * kLn2 / S;
+  r.H = r.bad ? NAN : empty ? 0.0f : log_s - p.X * kLn2 * __builtin_amdgcn_rcpf(S);
   return r;
 }
 
