@@ -80,8 +80,8 @@ inline RowSplit row_split(int vectors, int32_t rows, int few) {
 
 // Which calls are split.  us, split / a workgroup a row, bf16: log-probs with 20 alternatives, V = 50000, 1 row 8.4 / 9.6, 16 rows
 // 9.9 / 11.4, 64 rows 12.0 / 12.1, 128 rows 14.5 / 13.5; V = 131072, 64 rows 14.9 / 15.9, 128 rows 18.2 / 16.6; without alternatives,
-// 64 rows 8.7 / 10.7.  Distillation: V = 50000, 16 rows 8.6 / 10.9, 64 rows 10.9 / 11.7, 128 rows 14.8 / 12.8; V = 131072, 128 rows
-// 21.7 / 23.7, 255 rows 36.8 / 33.7.
+// 64 rows 8.7 / 10.7.  Distillation: V = 50000, 16 rows 8.4 / 10.8, 64 rows 11.3 / 11.2, 128 rows 13.4 / 12.3; V = 131072, 128 rows
+// 20.5 / 23.4, 200 rows 29.2 / 27.5.
 constexpr int kSplitVectors = 5120;
 inline RowSplit split_logprobs(int vectors, int32_t rows) {
   return vectors >= kSplitVectors && rows <= 64 ? row_split(vectors, rows, 80) : RowSplit{0, 0};  // (the parts are to bound 64 alternatives)
