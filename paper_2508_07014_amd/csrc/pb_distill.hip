@@ -587,7 +587,7 @@ int distill(const DistillArgs& a, void* workspace, hipStream_t stream) {
   const bool large = E::N == 8 && nv > 1024 && 4 * static_cast<int64_t>(a.in.rows) * a.in.V > (256ll << 20);
   auto go = [&](auto nt, auto held) {
     constexpr int NT = decltype(nt)::value, HELD = decltype(held)::value, ROWS = NT == 64 ? 4 : 1, THREADS = NT == 64 ? 256 : NT;
-    constexpr bool CAN = E::N == 8 && NT * HELD > 1024;
+    constexpr bool CAN = E::N == 8 && NT * HELD > 1024 && NT < 1024;  // (too few rows for that)
     const int grid = (a.in.rows + ROWS - 1) / ROWS, lds = a.tail ? ROWS * mark_bytes : 0;
     auto launch = [&](auto kernel) { kernel<<<grid, THREADS, lds, stream>>>(a, a.tail ? mark_bytes : 0); };
     if (a.tail) {
@@ -603,13 +603,14 @@ int distill(const DistillArgs& a, void* workspace, hipStream_t stream) {
   // Threads x vectors held, us at the best and its neighbours: 16384 x 300 bf16 64x4 20.4, 64x8 21.9; 500 x 1025 fp32 64x4 5.2, 64x8 5.8,
   // 16384 x 1025 fp32 37.2 35.4; 16384 x 4096 bf16 64x8 61, 64x16 59, 256x4 70; 16384 x 8192 256x4 103, 256x8 110, 64x16 114;
   // 16384 x 16000 256x8 188, 512x4 191, 512x8 206; 8192 x 32001 256x8 208, 512x8 191, 512x16 204; 4096 x 65000 512x8 216, 512x16 203,
-  // 1024x8 259; 3000 x 32001 fp32 173 149 168.  Longer rows: 1000 x 131072 bf16 512x16 125, 1024x8 130.
+  // 1024x8 259; 3000 x 32001 fp32 173 149 168.  Longer rows: 256 x 131072 bf16 512x16 38, 1024x8 34; 1000 x 90000 75 87.
   if (nv <= 128 || (nv <= 256 && a.in.rows < 4096)) return go(integral_constant<int, 64>{}, integral_constant<int, 4>{});
   if (nv <= 512) return go(integral_constant<int, 64>{}, integral_constant<int, 8>{});
   if (nv <= 1024) return go(integral_constant<int, 256>{}, integral_constant<int, 4>{});
   if (nv <= 2048) return go(integral_constant<int, 256>{}, integral_constant<int, 8>{});
   if (nv <= 4096) return go(integral_constant<int, 512>{}, integral_constant<int, 8>{});
-  return go(integral_constant<int, 512>{}, integral_constant<int, 16>{});
+  if (nv <= 8192 || a.in.rows > 256) return go(integral_constant<int, 512>{}, integral_constant<int, 16>{});
+  return go(integral_constant<int, 1024>{}, integral_constant<int, 8>{});
 }
 
 }  // namespace

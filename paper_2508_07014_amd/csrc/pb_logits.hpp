@@ -80,14 +80,13 @@ inline RowSplit row_split(int vectors, int32_t rows, int few) {
 
 // Which calls are split.  us, split / a workgroup a row, bf16: log-probs with 20 alternatives, V = 50000, 1 row 8.4 / 9.6, 16 rows
 // 9.9 / 11.4, 64 rows 12.0 / 12.1, 128 rows 14.5 / 13.5; V = 131072, 64 rows 14.9 / 15.9, 128 rows 18.2 / 16.6; without alternatives,
-// 64 rows 8.7 / 10.7.  Distillation: V = 50000, 16 rows 8.4 / 10.8, 64 rows 11.3 / 11.2, 128 rows 13.4 / 12.3; V = 131072, 128 rows
-// 20.5 / 23.4, 200 rows 29.2 / 27.5.
-constexpr int kSplitVectors = 5120;
+// 64 rows 8.7 / 10.7.  Distillation: V = 32001, 16 rows 7.9 / 8.4, 64 rows 9.4 / 8.7; V = 50000, 32 rows 9.1 / 10.9, 64 rows 11.4 / 11.1;
+// V = 131072, 64 rows 14.7 / 22, 160 rows 25.5 / 24.7; fp32 V = 131072, 256 rows 66 / 78.
 inline RowSplit split_logprobs(int vectors, int32_t rows) {
-  return vectors >= kSplitVectors && rows <= 64 ? row_split(vectors, rows, 80) : RowSplit{0, 0};  // (the parts are to bound 64 alternatives)
+  return vectors >= 5120 && rows <= 64 ? row_split(vectors, rows, 80) : RowSplit{0, 0};  // (the parts are to bound 64 alternatives)
 }
 inline RowSplit split_distill(int vectors, int32_t rows) {
-  return vectors >= kSplitVectors && rows <= (vectors > 8192 ? 160 : 64) ? row_split(vectors, rows, 16) : RowSplit{0, 0};
+  return vectors >= 3500 && rows <= vectors / 100 ? row_split(vectors, rows, 16) : RowSplit{0, 0};
 }
 
 int64_t token_logprobs_workspace(int dtype, int32_t rows, int32_t V);
