@@ -179,14 +179,14 @@ __device__ __forceinline__ List load_list(const DistillArgs& a, int64_t r, const
   List l;
   if constexpr (TAIL) {
     // (1 - sum q in 64 bits: where the list holds nearly everything, fp32 would leave nothing of it)
-    const double q = exp(static_cast<double>(e.log_q)), left = 1.0 - wave_sum(q);
+    const double q = e.log_q == INFINITY ? NAN : exp(static_cast<double>(e.log_q)), left = 1.0 - wave_sum(q);
     e.q = static_cast<float>(q);
     l.rest = left < 0x1p-20 ? 0.0f : static_cast<float>(left);  // (NaN stays)
     l.any = __ballot(e.token >= 0) != 0 ? 1 : 0;
     l.shift = 0.0f;
   } else {
     const float top = wave_max(e.log_q);
-    l.any = top != -INFINITY ? 1 : 0;
+    l.any = __ballot(e.token >= 0 && e.log_q != -INFINITY) != 0 ? 1 : 0;
     const float part = e.token >= 0 ? exp2_fast((e.log_q - (l.any ? top : 0.0f)) * kLog2e) : 0.0f;
     const float sum = wave_sum(part);
     l.rest = 0.0f;

@@ -315,6 +315,31 @@ def test_distill_many_rows(rows, V, K, tail, kind):
     check_distill(rng, view, values, kind, V, 1.0, t, l, tail, (rows, V, K, tail, kind))
 
 
+@pytest.mark.parametrize("rows,V", [(9, 40), (9, 9000), (9, 70000)])
+def test_entries_that_are_no_numbers(rows, V):
+    """An entry of NaN, of either sign, or +inf: loss and gradient are NaN (in the last case too where nothing else is listed);
+    the rows beside it are what they are without it."""
+    g = torch.Generator(device=DEV)
+    g.manual_seed(V)
+    view = torch.randn((rows, V), generator=g, device=DEV)
+    t = torch.arange(5, dtype=torch.int32, device=DEV).repeat(rows, 1)
+    l = torch.full((rows, 5), -2.0, device=DEV)
+    nans = np.array([0x7fc00000, 0xffc00000, 0x7f800001, 0xff800001, 0x7f800000], np.uint32).view(np.float32)
+    for tail in (False, True):
+        out = []
+        for odd in (False, True):
+            k, listed = l.clone(), t.clone()
+            if odd:
+                k[1:6, 2] = dev(nans)
+                listed[3, :2] = listed[3, 3:] = -1        # (nothing but that entry)
+            loss, grad = torch.empty(rows, device=DEV), torch.empty((rows, V), device=DEV)
+            run_distill(view, "f32", V, V, 1.0, listed, k, tail, None, loss, grad, V)
+            out.append((host(loss), host(grad)))
+        assert np.isnan(out[1][0][1:6]).all() and np.isnan(out[1][1][1:6]).all()
+        for a, b in zip(*out):
+            assert np.array_equal(a[[0, 6, 7, 8]], b[[0, 6, 7, 8]]) and np.isfinite(a).all()
+
+
 # Rows of every kernel shape, as many as send the call there (the shape is chosen by vectors a row and rows): 8 rows of each
 # call are compared.
 MANY = [(1100, 4104), (1030, 6001), (1025, 16400), (70, 8200), (70, 20001), (70, 30000), (70, 33001), (70, 50000), (70, 70001),
