@@ -241,11 +241,35 @@ __device__ __forceinline__ float mass_of(const Entry& e, unsigned* table) {
   }
   return mass;
 }
+// log(v), v a positive number of fp32, to 1e-12: v = 2^k m, m in [sqrt(1/2), sqrt(2)), log m = 2 atanh(t), t = (m - 1) / (m + 1),
+// by its series up to t^15 (the library's takes three times the instructions for the last bits).
+__device__ __forceinline__ double log_64(float v) {
+  int k = static_cast<int>(__float_as_uint(v) >> 23) - 127;
+  float m = __uint_as_float((__float_as_uint(v) & 0x007fffffu) | 0x3f800000u);
+  if (m >= 1.41421356f) {
+    m *= 0.5f;
+    ++k;
+  }
+  const double d = static_cast<double>(m) + 1.0;
+  double r = __builtin_amdgcn_rcp(d);
+  r = __builtin_fma(r, __builtin_fma(-d, r, 1.0), r);
+  r = __builtin_fma(r, __builtin_fma(-d, r, 1.0), r);
+  const double t = (static_cast<double>(m) - 1.0) * r, t2 = t * t;
+  double s = 1.0 / 15.0;
+  s = __builtin_fma(s, t2, 1.0 / 13.0);
+  s = __builtin_fma(s, t2, 1.0 / 11.0);
+  s = __builtin_fma(s, t2, 1.0 / 9.0);
+  s = __builtin_fma(s, t2, 1.0 / 7.0);
+  s = __builtin_fma(s, t2, 1.0 / 5.0);
+  s = __builtin_fma(s, t2, 1.0 / 3.0);
+  s = __builtin_fma(s, t2, 1.0);
+  return __builtin_fma(static_cast<double>(k), 0.69314718055994530942, 2.0 * t * s);
+}
 // By one wave: the row's loss.  Terms that cancel, and log-probs of masked tokens that may pass the fp32 range: in 64 bits.
 template <bool TAIL>
 __device__ __forceinline__ void write_loss(const DistillArgs& a, int64_t r, int lane, const Entry& e, const List& list, const RowSums& sums,
                                            const Student& st, float inv) {
-  const double lp = (static_cast<double>(e.x) - sums.base) * inv - (sums.m == -INFINITY ? 0.0 : log(static_cast<double>(st.S)));
+  const double lp = (static_cast<double>(e.x) - sums.base) * inv - (sums.m == -INFINITY ? 0.0 : log_64(st.S));
   double loss = wave_sum(e.q > 0.0f ? e.q * (e.log_q - lp) : static_cast<double>(e.q));  // (0, or NaN)
   if (TAIL && list.rest != 0.0f) loss += list.rest * static_cast<double>(logf(list.rest / st.p_rest));
   if (lane == 0) a.loss[r] = sums.bad ? NAN : static_cast<float>(loss);
