@@ -201,16 +201,21 @@ __device__ __forceinline__ List load_list(const DistillArgs& a, int64_t r, const
 struct Student {
   float S;       // sum over all tokens
   float p_rest;  // what the student leaves to the tokens that are not listed
-  float A;       // their gradient, a unit of exp((x - base) / T)
+  float A, lift; // their gradient is A exp2((x - base) c + lift)
 };
 template <bool TAIL>
 __device__ __forceinline__ Student student(const RowSums& sums, const List& list, float w, float inv) {
-  Student s{TAIL ? sums.S + sums.X : sums.S, 0.0f, 0.0f};
+  Student s{TAIL ? sums.S + sums.X : sums.S, 0.0f, 0.0f, 0.0f};
   float share = list.Q;
   if constexpr (TAIL) {
     s.p_rest = sums.m == -INFINITY ? 0.0f : sums.S / s.S;
     if (s.p_rest < 0x1p-126f) s.p_rest = 0.0f;  // (NaN stays)
-    if (list.rest > 0.0f && s.p_rest > 0.0f) share -= list.rest / s.p_rest;
+    // (q' / p' may pass the fp32 range together with a row's weight, q' p_j / p' does not: the power of 2 goes into p_j)
+    if (list.rest > 0.0f && s.p_rest > 0.0f) {
+      const int k = 127 - static_cast<int>(__float_as_uint(s.p_rest) >> 23);
+      s.lift = static_cast<float>(k);
+      share = ldexpf(share, -k) - list.rest / ldexpf(s.p_rest, k);
+    }
   }
   s.A = share * w * inv / s.S;
   return s;
@@ -400,7 +405,7 @@ __global__ __launch_bounds__(NT == 64 ? 256 : NT) void distill_kernel(DistillArg
     zeros();
     return;
   }
-  auto grad = [&](float x) { return exp2_fast((x - sums.base) * c) * st.A; };
+  auto grad = [&](float x) { return exp2_fast(__builtin_fmaf(x - sums.base, c, st.lift)) * st.A; };
   auto put = [&](const v4u& raw, int v) {
     float x[E::N];
     E::unpack(raw, x);
@@ -553,6 +558,7 @@ __global__ __launch_bounds__(256) void distill_grad_kernel(DistillArgs a, int pa
       }
     }
   }
+  auto grad = [&](float x) { return exp2_fast(__builtin_fmaf(x - sums.base, c, st.lift)) * st.A; };
   if (out) {
 #pragma unroll
     for (int u = 0; u < kGradUnroll; ++u) {
@@ -561,11 +567,11 @@ __global__ __launch_bounds__(256) void distill_grad_kernel(DistillArgs a, int pa
         float x[E::N];
         E::unpack(raw[u], x);
 #pragma unroll
-        for (int i = 0; i < E::N; ++i) x[i] = none ? 0.0f : exp2_fast((x[i] - sums.base) * c) * st.A;
+        for (int i = 0; i < E::N; ++i) x[i] = none ? 0.0f : grad(x[i]);
         stream_vector<E>(out + row.token(v, 0), E::pack(x));
       }
     }
-    if (has_edge) out[row.edge_token(tid)] = E::down(none ? 0.0f : exp2_fast((edge - sums.base) * c) * st.A);
+    if (has_edge) out[row.edge_token(tid)] = E::down(none ? 0.0f : grad(edge));
   }
   if (block == 0 && tid < 64 && a.loss) {
     if (learn) write_loss<TAIL>(a, r, tid, e, list, sums, st, inv);

@@ -431,6 +431,29 @@ def test_lists_that_cover_the_row(tail):
         check_distill(rng, view, values, "f32", V, 1.0, t, l, tail, (V, masked))
 
 
+@pytest.mark.parametrize("kind", list(KIND))
+@pytest.mark.parametrize("V", [40, 1025, 9000, 70000])
+def test_little_mass_for_the_rest_and_large_weights(V, kind):
+    """A student that leaves e^-80 to the tokens that are not listed, most of them masked, rows weighted by a loss scale: q' / p'
+    times the weight passes the fp32 range, the gradient does not."""
+    rng = np.random.default_rng(V)
+    for T in (1.0, 0.01):
+        x = np.full((5, V), -np.inf)
+        t = np.stack([rng.permutation(V)[:13] for _ in range(5)])
+        for r in range(5):
+            x[r, t[r]] = np.concatenate([rng.normal(0, 1, 8), rng.uniform(-82, -79, 5)]) * T
+        buf, view, values = place(x, kind)
+        t, l = t[:, :8], np.log(rng.dirichlet(np.ones(9), 5)[:, :8]).astype(np.float32)
+        w = np.array([30000.0, -20000.0, 1.0, 0.25, 10000.0], np.float32) * np.float32(T)
+        grad, loss = torch.full((5, V), JUNK, dtype=KIND[kind][1], device=DEV), torch.full((5,), JUNK, device=DEV)
+        run_distill(view, kind, V, V, T, dev(t.astype(np.int32)), dev(l), True, dev(w), loss, grad, V)
+        got, got_loss = host(grad), host(loss)
+        for r in range(5):
+            want, g, e, eg = R.distill(values[r], T, t[r], l[r].astype(np.float64), True, float(w[r]))
+            R.check(got_loss[r], want, e * (1 + 2 ** -20) + R.U * abs(want) + 1e-37, (V, kind, T, r, "loss"))
+            R.check(got[r], g, R.rounded(eg, g, kind), (V, kind, T, r, "grad"))
+
+
 # ---- together ----------------------------------------------------------------------------------------------------------
 
 def test_confidence_of_what_a_decoder_emits_and_a_student_of_the_boosted_rows():
