@@ -369,8 +369,9 @@ int pb_token_logprobs_backward(const void* d_logits, int32_t dtype, int64_t row_
  *   Either output may be null, not both: loss and gradient in one call where the weights of the rows are known, the loss
  *   first and the gradient of the same inputs when they are.  (No factor temperature^2: it belongs in the weights.)
  *   An id outside [0, V) is an absent entry (lists may be shorter than K); a token listed twice counts with the sum of its
- *   q; p' below the smallest normal fp32 number counts as 0.  A row without entries (or, PB_DISTILL_RENORM, with none above -inf) has loss 0 and gradient 0, whatever it holds; a
- *   row of weight 0 has gradient 0.  An entry of NaN or +inf makes the row's loss and gradient NaN.  Where q is positive and p is 0 the loss is +inf, the gradient finite; a student's row of
+ *   q; p' below the smallest normal fp32 number counts as 0.  A row without entries (or, PB_DISTILL_RENORM, with none above
+ *   -inf) has loss 0 and gradient 0, whatever it holds; a row of weight 0 has gradient 0.  An entry of NaN or +inf makes the
+ *   row's loss and gradient NaN.  Where q is positive and p is 0 the loss is +inf, the gradient finite; a student's row of
  *   nothing but -inf has gradient 0.  1 <= K <= 64.  d_grad_logits may be d_logits with the same stride.
  */
 int64_t pb_distill_topk_workspace_bytes(int32_t dtype, int32_t rows, int32_t vocab_size, int32_t K);
