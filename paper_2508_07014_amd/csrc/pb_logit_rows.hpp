@@ -182,10 +182,14 @@ __device__ __forceinline__ float mul_0(float a, float b) {
   asm("v_mul_legacy_f32 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
   return r;
 }
-// log(1 + r), r > -1/2: the logarithm of u = 1 + r, rounded, by what u lacks of r (Kahan).
+// log(1 + r), r > -1/2: the logarithm of u = 1 + r, rounded, by what u lacks of r (Kahan); of u = 2^k m, m in [sqrt(1/2), sqrt(2)),
+// k ln 2 + log m, so that what the hardware's log is off by counts relative to log m (64 rows of 50000: log-probs off by up to
+// 5.2e-8 of themselves without, 3.5e-8 with it, in the same time).
 __device__ __forceinline__ float log_1p(float r) {
   const float u = 1.0f + r, d = u - 1.0f;
-  const float l = __builtin_amdgcn_logf(u) * kLn2;  // (base 2)
+  const int k = (static_cast<int>(__float_as_uint(u)) - 0x3f3504f3) >> 23;
+  const float m = __uint_as_float(__float_as_uint(u) - (static_cast<unsigned>(k) << 23));
+  const float l = __builtin_fmaf(static_cast<float>(k), kLn2, __builtin_amdgcn_logf(m) * kLn2);  // (the hardware's has base 2)
   return d == 0.0f ? r : fabsf(d) < 0.5f ? l * (r * __builtin_amdgcn_rcpf(d)) : l;
 }
 template <int N>
