@@ -199,11 +199,22 @@ __device__ __forceinline__ int how_many(const unsigned (&key)[PER], unsigned b) 
   for (int i = 0; i < PER; ++i) n += __builtin_popcountll(__ballot(key[i] >= b));
   return n;
 }
-// Between the smallest and the largest key, in quarters (three counts at a time do not wait for each other): four or five steps
-// until exactly n reach one of the three, 16 at most (equal keys).
+// For few of 64 keys: one maximum after the other.  Otherwise between the smallest and the largest key, in quarters (three counts
+// at a time do not wait for each other): four or five steps until exactly n reach one of the three, 16 at most (equal keys).
+// (16384 x 1025 fp32 with entropy, 4 / 8 / 12 / 20 alternatives: 17.4 19.4 21.8 26.8 us by maxima, 18.7 20.1 21.5 24.7 in quarters.)
+constexpr int kFewSteps = 8;
 template <int PER>
 __device__ __forceinline__ unsigned bound_of(const unsigned (&key)[PER], int n) {
   if (how_many(key, 1u) < n) return 0u;
+  if (PER == 1 && n <= kFewSteps) {
+    unsigned left = key[0];
+    for (int reached = 0;;) {
+      const unsigned b = wv::wave_max_u(left);
+      reached += __builtin_popcountll(__ballot(left == b));
+      if (reached >= n) return b;
+      left = left == b ? 0u : left;
+    }
+  }
   unsigned most = key[0], least = key[0] - 1u;  // (a key of 0 is none)
 #pragma unroll
   for (int i = 1; i < PER; ++i) {
@@ -211,32 +222,16 @@ __device__ __forceinline__ unsigned bound_of(const unsigned (&key)[PER], int n) 
     least = min(least, key[i] - 1u);
   }
   unsigned lo = ~wv::wave_max_u(~least) + 1u, hi = wv::wave_max_u(most);  // n keys or more reach lo, fewer reach hi + 1
-  if (n == 1) return hi;  // (13540 rows of 704 fp16: 14.4 -> 13.2 us)
   while (lo < hi) {
-    const unsigned step = (hi - lo) / 4 + 1, t1 = lo + step, t2 = t1 + (hi - t1 < step ? hi - t1 : step), t3 = t2 + (hi - t2 < step ? hi - t2 : step);
+    const unsigned step = (hi - lo) / 4 + 1, t1 = lo + step, t2 = t1 + min(hi - t1, step), t3 = t2 + min(hi - t2, step);
     const int n1 = how_many(key, t1), n2 = how_many(key, t2), n3 = how_many(key, t3);
-    if (n1 == n) return t1;
-    if (n2 == n) return t2;
-    if (n3 == n) return t3;
-    if (n3 > n) lo = t3;
-    else if (n2 > n) lo = t2, hi = t3 - 1;
-    else if (n1 > n) lo = t1, hi = t2 - 1;
-    else hi = t1 - 1;
+    hi = n1 < n ? t1 - 1 : n2 < n ? t2 - 1 : n3 < n ? t3 - 1 : hi;
+    lo = n3 >= n ? t3 : n2 >= n ? t2 : n1 >= n ? t1 : lo;
+    if (n3 == n || n2 == n || n1 == n) break;
   }
   return lo;
 }
 
-template <int N>
-__device__ __forceinline__ float element(const float (&x)[N], int i) {  // x[i], in registers
-  float y[N];
-#pragma unroll
-  for (int k = 0; k < N; ++k) y[k] = x[k];
-#pragma unroll
-  for (int n = N / 2; n > 0; n /= 2)
-#pragma unroll
-    for (int k = 0; k < n; ++k) y[k] = i & n ? y[k + n] : y[k];
-  return y[0];
-}
 // The same, from a lane's largest key alone where there are lanes enough (a bound of 20 from 64 groups instead of 256 admits 24
 // candidates instead of 21, and takes a quarter of the instructions).
 template <int PER>
@@ -249,27 +244,37 @@ __device__ __forceinline__ unsigned some_bound_of(const unsigned (&key)[PER], in
   return b != 0u ? b : bound_of(key, n);
 }
 
-// Candidates into the list: the elements of vector v that the bound admits.
+// Candidates into the list: of every lane that calls, the elements of vector v that the bound admits, an element of all lanes
+// after the other (additions of a number of its own by every lane to the count became a loop over the lanes: 13540 x 704 fp16,
+// the largest element 13.4 -> 11.4 us).
+template <int NT, int M>
+__device__ __forceinline__ int places(TopLds<NT, M>& lds, int n) {  // of n candidates of the wave
+  int at = 0;
+  if (__lane_id() == static_cast<unsigned>(wv::first_lane(__ballot(true)))) at = atomicAdd(&lds.count, n);
+  return uniform_i(at);
+}
+__device__ __forceinline__ int lanes_before(u64 who) {
+  return __builtin_amdgcn_mbcnt_hi(static_cast<unsigned>(who >> 32), __builtin_amdgcn_mbcnt_lo(static_cast<unsigned>(who), 0u));
+}
 template <typename E, int NT>
 __device__ __forceinline__ void push_vector(const Row<E>& row, const float (&x)[E::N], int v, unsigned b, int last, TopLds<NT, E::N>& lds) {
   const float least = b == 0u ? -INFINITY : ukey_val(v <= last ? b : b + 1);  // (as good an order as the keys', -0.0 as 0.0)
-  unsigned take = 0;
+  u64 who[E::N];
+  int n = 0;
 #pragma unroll
-  for (int i = 0; i < E::N; ++i) take |= x[i] >= least ? 1u << i : 0u;
-  if (take) {
-    int at = atomicAdd(&lds.count, __builtin_popcount(take));
-    if (__ballot((take & (take - 1)) != 0u) == 0) {  // (one element as a rule)
-      const int i = __builtin_ctz(take);
-      if (at < list_size<E::N>()) lds.list[at] = order64(order32(element(x, i)), row.token(v, i));
-    } else {
-#pragma unroll
-      for (int i = 0; i < E::N; ++i)
-        if ((take >> i) & 1u) {
-          if (at < list_size<E::N>()) lds.list[at] = order64(order32(x[i]), row.token(v, i));
-          ++at;
-        }
-    }
+  for (int i = 0; i < E::N; ++i) {
+    who[i] = __ballot(x[i] >= least);
+    n += __builtin_popcountll(who[i]);
   }
+  if (n == 0) return;
+  int at = places(lds, n);
+#pragma unroll
+  for (int i = 0; i < E::N; ++i)
+    if (who[i] != 0) {
+      const int to = at + lanes_before(who[i]);
+      if (x[i] >= least && to < list_size<E::N>()) lds.list[to] = order64(order32(x[i]), row.token(v, i));
+      at += __builtin_popcountll(who[i]);
+    }
 }
 template <typename E, int NT>
 __device__ __forceinline__ void push_edge(const Row<E>& row, int tid, float edge, unsigned b, TopLds<NT, E::N>& lds) {
