@@ -848,7 +848,7 @@ template <typename E>
 int forward(const LogprobArgs& a, void* workspace, hipStream_t stream) {
   const bool ent = a.entropy || a.stats, top = a.n_top > 0;
   auto done = [] { return hipGetLastError() == hipSuccess ? PB_OK : PB_EHIP; };
-  const RowSplit split = split_logprobs(a.in.V / E::N, a.in.all_rows);
+  const RowSplit split = split_logprobs(a.in.V / E::N, a.in.all_rows, a.in.V);
   if (split.parts > 0) {
     PartRecord* ws = static_cast<PartRecord*>(workspace);
     const int grid = static_cast<int>((static_cast<int64_t>(a.in.rows) * split.parts + 3) / 4);
@@ -905,7 +905,7 @@ int backward(const LogprobGradArgs& a, hipStream_t stream) {
 }  // namespace lr
 
 int64_t token_logprobs_workspace(int dtype, int32_t rows, int32_t V) {
-  return static_cast<int64_t>(rows) * split_logprobs(V / (dtype == PB_F32 ? lr::F32::N : lr::F16::N), rows).parts * static_cast<int64_t>(sizeof(lr::PartRecord));
+  return static_cast<int64_t>(rows) * split_logprobs(V / (dtype == PB_F32 ? lr::F32::N : lr::F16::N), rows, V).parts * static_cast<int64_t>(sizeof(lr::PartRecord));
 }
 int launch_token_logprobs(int dtype, const LogprobArgs& a, void* workspace, hipStream_t stream) {
   return dtype == PB_F32   ? lr::forward<lr::F32>(a, workspace, stream)

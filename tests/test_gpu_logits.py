@@ -343,7 +343,7 @@ def test_entries_that_are_no_numbers(rows, V):
 # Rows of every kernel shape, as many as send the call there (the shape is chosen by vectors a row and rows): 8 rows of each
 # call are compared.
 MANY = [(1100, 4104), (1030, 6001), (1025, 16400), (70, 8200), (70, 20001), (70, 30000), (70, 33001), (70, 50000), (70, 70001),
-        (170, 70000), (170, 131072), (300, 33000), (20, 41000), (64, 50001), (160, 70001), (260, 70001), (5000, 1030), (20, 30001),
+        (170, 70000), (170, 131072), (81, 131072), (82, 131072), (300, 33000), (20, 41000), (64, 50001), (160, 70001), (260, 70001), (5000, 1030), (20, 30001),
         (90, 72000)]
 
 
