@@ -133,20 +133,20 @@ __device__ __forceinline__ RowSums join_waves(Part p, int tid, float c, float* l
   return r;
 }
 
-template <int CTRL, int ROWS>
+template <int CTRL>
 __device__ __forceinline__ double dpp_add(double v) {
   const long long b = __double_as_longlong(v);
-  const unsigned lo = static_cast<unsigned>(__builtin_amdgcn_update_dpp(0, static_cast<int>(b), CTRL, ROWS, 0xf, false));
-  const unsigned hi = static_cast<unsigned>(__builtin_amdgcn_update_dpp(0, static_cast<int>(b >> 32), CTRL, ROWS, 0xf, false));
+  const unsigned lo = static_cast<unsigned>(__builtin_amdgcn_update_dpp(0, static_cast<int>(b), CTRL, 0xf, 0xf, true));
+  const unsigned hi = static_cast<unsigned>(__builtin_amdgcn_update_dpp(0, static_cast<int>(b >> 32), CTRL, 0xf, 0xf, true));
   return v + __longlong_as_double((static_cast<long long>(hi) << 32) | lo);
 }
 __device__ __forceinline__ double wave_sum(double v) {
-  v = dpp_add<0x111, 0xf>(v);
-  v = dpp_add<0x112, 0xf>(v);
-  v = dpp_add<0x114, 0xf>(v);
-  v = dpp_add<0x118, 0xf>(v);
-  v = dpp_add<0x142, 0xa>(v);
-  v = dpp_add<0x143, 0xc>(v);
+  v = dpp_add<0x111>(v);
+  v = dpp_add<0x112>(v);
+  v = dpp_add<0x114>(v);
+  v = dpp_add<0x118>(v);
+  v = dpp_add<0x142>(v);
+  v = dpp_add<0x143>(v);
   const long long b = __double_as_longlong(v);
   const unsigned lo = __builtin_amdgcn_readlane(static_cast<int>(b), 63), hi = __builtin_amdgcn_readlane(static_cast<int>(b >> 32), 63);
   return __longlong_as_double((static_cast<long long>(hi) << 32) | lo);

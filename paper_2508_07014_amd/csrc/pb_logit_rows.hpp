@@ -124,18 +124,20 @@ __device__ __forceinline__ Row<E> row_at(const void* base, int64_t stride, int64
 
 __device__ __forceinline__ float exp2_fast(float v) { return __builtin_amdgcn_exp2f(v); }
 
+// Sum over a wave, in lane 63 of the last step and from there in every lane.  (row_bcast:15 adds a row's sum to the next row's,
+// row_bcast:31 that of the first two to the others': what rows 0 to 2 are left with is not used.  Lanes without a source add 0 by
+// bound_ctrl, so the additions take the moves along.)
 template <int CTRL>
-__device__ __forceinline__ float dpp_f(float v, float none) {
-  return __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(none), __float_as_int(v), CTRL, 0xf, 0xf, false));
+__device__ __forceinline__ float dpp_add(float v) {
+  return v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
 }
 __device__ __forceinline__ float wave_sum(float v) {
-  v += dpp_f<0x111>(v, 0.0f);
-  v += dpp_f<0x112>(v, 0.0f);
-  v += dpp_f<0x114>(v, 0.0f);
-  v += dpp_f<0x118>(v, 0.0f);
-  // (row_bcast writes rows 1 and 3, then 2 and 3, alone: the other rows add their `none`)
-  v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x142, 0xa, 0xf, false));
-  v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x143, 0xc, 0xf, false));
+  v = dpp_add<0x111>(v);
+  v = dpp_add<0x112>(v);
+  v = dpp_add<0x114>(v);
+  v = dpp_add<0x118>(v);
+  v = dpp_add<0x142>(v);
+  v = dpp_add<0x143>(v);
   return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
 }
 __device__ __forceinline__ float wave_max(float v) { return ukey_val(wv::wave_max_u(ukey(v))); }
