@@ -54,23 +54,46 @@ __device__ __forceinline__ void add_vector(Sums& s, const float (&x)[N], float c
   s.S += vec_sum(e);
 }
 
-// Sums of a part of a row, seen from its maximum: d = (x - m) c.  A part of nothing but -inf has sums of 0.
+// Sums of a part of a row, seen from its maximum: d = (x - m) c.  Where less than an eighth of the maximum's term lies beside it,
+// the sums lack that term, so that the rest is not rounded to its unit: `one` says where it belongs, 1: S, 2: X (0: nothing
+// lacks).  A part of nothing but -inf has sums of 0.
 struct Part {
   float m, S, X;
+  int one;
 };
+__device__ __forceinline__ Part whole(const Part& p) { return Part{p.m, p.one == 1 ? p.S + 1.0f : p.S, p.one == 2 ? p.X + 1.0f : p.X, 0}; }
 // The part of a wave from its lanes', the same in every lane.  again(add) goes over the wave's elements a second time, with
 // add(x, listed): where the maximum lies so far from 0 that x c and m c no longer resolve what is between them, the
-// difference does.
-template <bool LISTED, typename Again>
-__device__ __forceinline__ Part wave_part(const Sums& s, float c, Again&& again) {
-  Part p{wave_max(s.m), s.S, s.X};
+// difference does.  lane_again(tid, add) goes over the elements of one lane, by the whole wave.
+template <bool LISTED, typename Again, typename LaneAgain>
+__device__ __forceinline__ Part wave_part(const Sums& s, float c, Again&& again, LaneAgain&& lane_again) {
+  Part p{wave_max(s.m), s.S, s.X, 0};
   const float mc = p.m * c;
   rebase<LISTED>(p.S, p.X, s.rc - mc);
+  const Part own = p;
   p.S = wave_sum(p.S);
   if constexpr (LISTED) p.X = wave_sum(p.X);
-  rebase<LISTED>(p.S, p.X, -__builtin_fmaf(p.m, c, -mc));  // (from the rounded m c to m c)
-  if (!(fabsf(mc) <= kFar) && fabsf(p.m) != INFINITY) {
-    float S = 0.0f, X = 0.0f;
+  const float back = -__builtin_fmaf(p.m, c, -mc);  // (from the rounded m c to m c)
+  rebase<LISTED>(p.S, p.X, back);
+  float S = 0.0f, X = 0.0f;
+  if (fabsf(mc) <= kFar) {
+    if (p.S + p.X < 1.125f) {
+      const int first = wv::first_lane(__ballot(s.m == p.m));
+      bool on_max = false;
+      lane_again(first, [&](float x, bool on) {
+        const float e = x == p.m ? 0.0f : exp2_fast((x - p.m) * c);
+        on_max = on_max || (x == p.m && on);
+        S += LISTED && on ? 0.0f : e;
+        if constexpr (LISTED) X += on ? e : 0.0f;
+      });
+      Part rest = own;  // (of the other lanes)
+      rebase<LISTED>(rest.S, rest.X, back);
+      const bool other = static_cast<int>(threadIdx.x & 63) != first;
+      p.S = wave_sum(S + (other ? rest.S : 0.0f));
+      if constexpr (LISTED) p.X = wave_sum(X + (other ? rest.X : 0.0f));
+      p.one = LISTED && __ballot(on_max) != 0 ? 2 : 1;
+    }
+  } else if (fabsf(p.m) != INFINITY) {
     again([&](float x, bool on) {
       const float d = (x - p.m) * c, e = exp2_fast(d);
       S += LISTED && on ? 0.0f : e;
@@ -81,54 +104,62 @@ __device__ __forceinline__ Part wave_part(const Sums& s, float c, Again&& again)
   }
   return p;
 }
+// Parts seen from the larger of their maxima keep their 1 apart, the others take it along.
 template <bool LISTED>
 __device__ __forceinline__ Part see_from(Part p, float m, float c) {
+  if (p.m == m) return p;
+  p = whole(p);
   rebase<LISTED>(p.S, p.X, (p.m - m) * c);
   p.m = m;
   return p;
 }
-// Two parts, or the parts that the lanes of a wave hold, as one.
+// Two parts, or the parts that the lanes of a wave hold, as one (two that have the same maximum: the second's 1 joins the sums).
 template <bool LISTED>
 __device__ __forceinline__ Part join(const Part& p, const Part& q, float c) {
   const float m = fmaxf(p.m, q.m);
-  const Part a = see_from<LISTED>(p, m, c), b = see_from<LISTED>(q, m, c);
-  return Part{m, a.S + b.S, a.X + b.X};
+  const Part a = see_from<LISTED>(p, m, c);
+  Part b = see_from<LISTED>(q, m, c);
+  if (a.one != 0) b = whole(b);
+  return Part{m, a.S + b.S, a.X + b.X, a.one | b.one};
 }
 template <bool LISTED>
 __device__ __forceinline__ Part join_lanes(const Part& p, float c) {
-  const Part q = see_from<LISTED>(p, wave_max(p.m), c);
-  return Part{q.m, wave_sum(q.S), LISTED ? wave_sum(q.X) : 0.0f};
+  Part q = see_from<LISTED>(p, wave_max(p.m), c);
+  const u64 ones = __ballot(q.one != 0);
+  const int first = wv::first_lane(ones | (1ull << 63)), one = __builtin_amdgcn_readlane(q.one, first);
+  if (static_cast<int>(threadIdx.x & 63) != first) q = whole(q);
+  return Part{q.m, wave_sum(q.S), LISTED ? wave_sum(q.X) : 0.0f, one};
 }
 
 struct RowSums {  // the same in every thread of the row
   float m;        // maximum, -inf for a row of nothing but -inf
   float base;     // m, 0 for such a row
   float S, X;     // the sums, d = (x - base) c
+  double all;     // both sums
   bool bad;       // the row holds a NaN or +inf
 };
-// The row from its waves' parts (`lds`: 3 * NT / 64 floats).
+// The row from its waves' parts (`lds`: NT / 64 of them).
 template <int NT, bool LISTED>
-__device__ __forceinline__ RowSums join_waves(Part p, int tid, float c, float* lds) {
+__device__ __forceinline__ RowSums join_waves(Part p, int tid, float c, Part* lds) {
   constexpr int W = NT / 64;
   if constexpr (W > 1) {
-    if ((tid & 63) == 0) {
-      lds[tid >> 6] = p.m;
-      lds[W + (tid >> 6)] = p.S;
-      lds[2 * W + (tid >> 6)] = p.X;
-    }
+    if ((tid & 63) == 0) lds[tid >> 6] = p;
     __syncthreads();
-    float M = lds[0], S = 0.0f, X = 0.0f;
+    p = lds[0];
+    float M = p.m;
 #pragma unroll
-    for (int w = 1; w < W; ++w) M = fmaxf(M, lds[w]);
+    for (int w = 1; w < W; ++w) M = fmaxf(M, lds[w].m);
+    p = see_from<LISTED>(p, M, c);
 #pragma unroll
-    for (int w = 0; w < W; ++w) {
-      const Part q = see_from<LISTED>(Part{lds[w], lds[W + w], lds[2 * W + w]}, M, c);
-      S += q.S;
-      X += q.X;
+    for (int w = 1; w < W; ++w) {
+      Part q = see_from<LISTED>(lds[w], M, c);
+      if (p.one != 0) q = whole(q);
+      p = Part{M, p.S + q.S, p.X + q.X, p.one | q.one};
     }
-    p = Part{uniform_f(M), uniform_f(S), uniform_f(X)};
+    p = Part{uniform_f(p.m), uniform_f(p.S), uniform_f(p.X), uniform_i(p.one)};
   }
-  RowSums r{p.m, p.m == -INFINITY ? 0.0f : p.m, p.S, p.X, false};
+  const Part w = whole(p);
+  RowSums r{p.m, p.m == -INFINITY ? 0.0f : p.m, w.S, w.X, (p.one != 0 ? 1.0 : 0.0) + (static_cast<double>(p.S) + p.X), false};
   r.bad = r.S != r.S || r.X != r.X || r.m == INFINITY;
   return r;
 }
@@ -179,10 +210,11 @@ __device__ __forceinline__ List load_list(const DistillArgs& a, int64_t r, const
   List l;
   if constexpr (TAIL) {
     // (1 - sum q in 64 bits: where the list holds nearly everything, fp32 would leave nothing of it)
-    const double q = e.log_q == INFINITY ? NAN : exp(static_cast<double>(e.log_q)), left = 1.0 - wave_sum(q);
+    const double q = e.log_q == INFINITY ? NAN : exp(static_cast<double>(e.log_q)), sum = wave_sum(q), left = 1.0 - sum;
     e.q = static_cast<float>(q);
     l.rest = left < 0x1p-20 ? 0.0f : static_cast<float>(left);  // (NaN stays)
     l.any = __ballot(e.token >= 0) != 0 ? 1 : 0;
+    l.Q = l.rest > 0.0f ? 1.0f : static_cast<float>(sum);
     l.shift = 0.0f;
   } else {
     const float top = wave_max(e.log_q);
@@ -193,8 +225,8 @@ __device__ __forceinline__ List load_list(const DistillArgs& a, int64_t r, const
     l.shift = top + logf(sum);
     e.log_q -= l.shift;
     e.q = part / sum;
+    l.Q = sum == sum ? 1.0f : NAN;
   }
-  l.Q = wave_sum(e.q) + l.rest;
   return l;
 }
 
@@ -205,7 +237,7 @@ struct Student {
 };
 template <bool TAIL>
 __device__ __forceinline__ Student student(const RowSums& sums, const List& list, float w, float inv) {
-  Student s{TAIL ? sums.S + sums.X : sums.S, 0.0f, 0.0f, 0.0f};
+  Student s{static_cast<float>(sums.all), 0.0f, 0.0f, 0.0f};
   float share = list.Q;
   if constexpr (TAIL) {
     s.p_rest = sums.m == -INFINITY ? 0.0f : sums.S / s.S;
@@ -246,20 +278,17 @@ __device__ __forceinline__ float mass_of(const Entry& e, unsigned* table) {
   }
   return mass;
 }
-// log(v), v a positive number of fp32, to 1e-12: v = 2^k m, m in [sqrt(1/2), sqrt(2)), log m = 2 atanh(t), t = (m - 1) / (m + 1),
-// by its series up to t^15 (the library's takes three times the instructions for the last bits).
-__device__ __forceinline__ double log_64(float v) {
-  int k = static_cast<int>(__float_as_uint(v) >> 23) - 127;
-  float m = __uint_as_float((__float_as_uint(v) & 0x007fffffu) | 0x3f800000u);
-  if (m >= 1.41421356f) {
-    m *= 0.5f;
-    ++k;
-  }
-  const double d = static_cast<double>(m) + 1.0;
-  double r = __builtin_amdgcn_rcp(d);
-  r = __builtin_fma(r, __builtin_fma(-d, r, 1.0), r);
-  r = __builtin_fma(r, __builtin_fma(-d, r, 1.0), r);
-  const double t = (static_cast<double>(m) - 1.0) * r, t2 = t * t;
+// 1 / v and log(v), v a positive number, to 1e-14: v = 2^k m, m in [sqrt(1/2), sqrt(2)), log m = 2 atanh(t), t = (m - 1) / (m + 1), by
+// its series up to t^15 (the library's takes three times the instructions for the last bits).
+__device__ __forceinline__ double over_64(double v) {
+  double r = __builtin_amdgcn_rcp(v);
+  r = __builtin_fma(r, __builtin_fma(-v, r, 1.0), r);
+  return __builtin_fma(r, __builtin_fma(-v, r, 1.0), r);
+}
+__device__ __forceinline__ double log_64(double v) {
+  const int k = (static_cast<int>(__double_as_longlong(v) >> 32) - 0x3fe6a09e) >> 20;
+  const double m = ldexp(v, -k);
+  const double t = (m - 1.0) * over_64(m + 1.0), t2 = t * t;
   double s = 1.0 / 15.0;
   s = __builtin_fma(s, t2, 1.0 / 13.0);
   s = __builtin_fma(s, t2, 1.0 / 11.0);
@@ -274,14 +303,15 @@ __device__ __forceinline__ double log_64(float v) {
 template <bool TAIL>
 __device__ __forceinline__ void write_loss(const DistillArgs& a, int64_t r, int lane, const Entry& e, const List& list, const RowSums& sums,
                                            const Student& st, float inv) {
-  const double lp = (static_cast<double>(e.x) - sums.base) * inv - (sums.m == -INFINITY ? 0.0 : log_64(st.S));
+  const double lp = (static_cast<double>(e.x) - sums.base) * inv - (sums.m == -INFINITY ? 0.0 : log_64(sums.all));
   double loss = wave_sum(e.q > 0.0f ? e.q * (e.log_q - lp) : static_cast<double>(e.q));  // (0, or NaN)
   if (TAIL && list.rest != 0.0f) loss += list.rest * static_cast<double>(logf(list.rest / st.p_rest));
   if (lane == 0) a.loss[r] = sums.bad ? NAN : static_cast<float>(loss);
 }
-// The gradient on a listed token.
-__device__ __forceinline__ float listed_grad(float x, float mass, const List& list, const RowSums& sums, const Student& st, float c, float w, float inv) {
-  return (exp2_fast((x - sums.base) * c) / st.S * list.Q - mass) * w * inv;
+// The gradient on a listed token: the difference of two probabilities, of which one may be near 1, in 64 bits.
+__device__ __forceinline__ float listed_grad(float x, float mass, const List& list, const RowSums& sums, float c, float w, float inv) {
+  const double p = exp2_fast((x - sums.base) * c) * over_64(sums.all);
+  return static_cast<float>(p * list.Q - mass) * w * inv;
 }
 
 // Has the compiler unpack held vectors again, rather than keep them unpacked in twice the registers.
@@ -299,7 +329,7 @@ template <typename E, int NT, int HELD, bool TAIL, bool STREAM>
 __global__ __launch_bounds__(NT == 64 ? 256 : NT) void distill_kernel(DistillArgs a, int mark_bytes) {
   constexpr int ROWS = NT == 64 ? 4 : 1;
   extern __shared__ __align__(16) unsigned char s_all[];
-  __shared__ float s_sums[ROWS][3 * NT / 64];
+  __shared__ Part s_sums[ROWS][NT / 64];
   __shared__ List s_list;
   __shared__ u64 s_edge[ROWS];
   __shared__ __align__(16) unsigned s_table[ROWS][kHashBits / 32];
@@ -394,6 +424,13 @@ __global__ __launch_bounds__(NT == 64 ? 256 : NT) void distill_kernel(DistillArg
       for (int i = 0; i < E::N; ++i) add(x[i], (on >> i) & 1u);
     }
     if (tid < row.edges) add(edge, edge_listed(tid));
+  }, [&](int lane, auto&& add) {
+    const int me = tid & 63, one = (tid & ~63) + lane;
+    for (int k = me; k < (row.nv - one + NT - 1) / NT * E::N; k += 64) {
+      const int v = one + k / E::N * NT, i = k % E::N;
+      add(E::up(row.x[row.token(v, i)]), (listed(v) >> i) & 1u);
+    }
+    if (me == lane && tid < row.edges) add(edge, edge_listed(tid));
   });
   const RowSums sums = join_waves<NT, TAIL>(part, tid, c, s_sums[sub]);
   const bool empty = sums.m == -INFINITY;
@@ -421,7 +458,7 @@ __global__ __launch_bounds__(NT == 64 ? 256 : NT) void distill_kernel(DistillArg
     if (u * NT + tid < row.nv) put(held[u], u * NT + tid);
   for (int v = HELD * NT + tid; v < row.nv; v += NT) put(row.vec(v), v);
   if (tid < row.edges) out[row.edge_token(tid)] = E::down(grad(edge));
-  const float own = lister ? listed_grad(e.x, mass, list, sums, st, c, w, inv) : 0.0f;
+  const float own = lister ? listed_grad(e.x, mass, list, sums, c, w, inv) : 0.0f;
   row_sync<NT>();
   if (lister && e.token >= 0) out[e.token] = E::down(own);
 }
@@ -511,8 +548,14 @@ __global__ __launch_bounds__(256) void distill_parts_kernel(DistillArgs a, int p
       for (int i = 0; i < E::N; ++i) add(x[i], (on >> i) & 1u);
     }
     if (has_edge) add(edge, on_edge);
+  }, [&](int one, auto&& add) {
+    for (int k = lane; k < (end - begin - one + 63) / 64 * E::N; k += 64) {
+      const int v = begin + one + k / E::N * 64, i = k % E::N;
+      add(E::up(row.x[row.token(v, i)]), (listed(v) >> i) & 1u);
+    }
+    if (lane == one && has_edge) add(edge, on_edge);
   });
-  if (lane == 0) ws.parts[r * parts + part] = make_float4(p.m, p.S, p.X, 0.0f);
+  if (lane == 0) ws.parts[r * parts + part] = make_float4(p.m, p.S, p.X, static_cast<float>(p.one));
 }
 
 template <typename E, bool TAIL>
@@ -532,12 +575,12 @@ __global__ __launch_bounds__(256) void distill_grad_kernel(DistillArgs a, int pa
   if (has_edge) edge = E::up(row.x[row.edge_token(tid)]);
   const float w = a.row_grads ? a.row_grads[r] : 1.0f, inv = a.in.inv_temp, c = a.in.c;
   const List list = ws.lists[r];
-  Part p{-INFINITY, 0.0f, 0.0f};
+  Part p{-INFINITY, 0.0f, 0.0f, 0};
 #pragma unroll
   for (int i = 0; i < kMaxParts / 64; ++i)
     if (64 * i + lane < parts) {
       const float4 q = ws.parts[r * parts + 64 * i + lane];
-      p = join<TAIL>(p, Part{q.x, q.y, q.z}, c);
+      p = join<TAIL>(p, Part{q.x, q.y, q.z, static_cast<int>(q.w)}, c);
     }
   const RowSums sums = join_waves<64, TAIL>(join_lanes<TAIL>(p, c), lane, c, nullptr);
   const Student st = student<TAIL>(sums, list, w, inv);
@@ -579,7 +622,7 @@ __global__ __launch_bounds__(256) void distill_grad_kernel(DistillArgs a, int pa
   }
   if (!out) return;
   __syncthreads();
-  if (mine && !none) out[e.token] = E::down(listed_grad(e.x, mass, list, sums, st, c, w, inv));
+  if (mine && !none) out[e.token] = E::down(listed_grad(e.x, mass, list, sums, c, w, inv));
 }
 
 DistillSpace space_in(void* p, int32_t rows, int parts) {

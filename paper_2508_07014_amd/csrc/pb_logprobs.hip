@@ -15,11 +15,13 @@ constexpr int kGroups = 256;          // parts of a row whose maxima bound the a
 // reference rc = m c, m the largest element that the lane has seen: batch by batch (kUnroll vectors), since a move costs an
 // exponential and a product a sum.  So e <= 1, and the sum X of e d holds no term of the maximum's size that the entropy
 // would have to cancel.  The sum of the batch in which the maximum lies, P, is kept apart from the others', S, down to the
-// logarithm: log(P + S) = log1p((P - 1) + S), so that what lies beside a near-certain token is not rounded to its unit
-// (entropies of such rows: errors of 5e-6 without, 1e-7 with it).  d is rounded once; what rc was rounded by is the same for all terms and
-// comes off at the end.  Elements below -kFar / c are masks of a lowest value: nothing beside any ordinary logit.
+// logarithm: log(P + S) = log1p((P - 1) + S), so that what lies beside a likely token is not rounded to its unit (entropies of
+// such rows: errors of 5e-6 without, 1e-7 with it); where less than an eighth of the maximum's term lies beside it, that batch is
+// summed once more without it.  d is rounded once; what rc was rounded by is the same for all terms and comes off a wave's sums.
+// Elements below -kFar / c are masks of a lowest value: nothing beside any ordinary logit.
 struct Sums {
   float m = -INFINITY, thr, rc = 0.0f, P = 0.0f, S = 0.0f, X = 0.0f;
+  int at = -1;  // first vector of the batch that P is the sum of; -1: the edge
   __device__ __forceinline__ explicit Sums(float far) : thr(-far) {}
 };
 // (S, X) seen from a reference that lies `apart` = rc - new rc higher.
@@ -30,7 +32,7 @@ __device__ __forceinline__ void rebase(float& S, float& X, float apart) {
   S = S == 0.0f ? 0.0f : f * S;
 }
 template <bool ENT, int U, int N>
-__device__ __forceinline__ void add_batch(Sums& s, const float (&x)[U][N], float m, float c) {
+__device__ __forceinline__ void add_batch(Sums& s, const float (&x)[U][N], float m, float c, int at) {
   const bool up = m > s.thr;
   if (__ballot(up) != 0) {
     asm volatile("");  // (a branch: selects would take the move's exponential in every batch)
@@ -40,6 +42,7 @@ __device__ __forceinline__ void add_batch(Sums& s, const float (&x)[U][N], float
       rebase<ENT>(s.S, s.X, s.rc - next);
       s.rc = next;
       s.thr = m;
+      s.at = at;
     }
   }
   float sum, sum_x;
@@ -60,31 +63,53 @@ __device__ __forceinline__ void add_batch(Sums& s, const float (&x)[U][N], float
   if constexpr (ENT) s.X += sum_x;
 }
 
-// Sums of a part of a row, as above, with rc = m c (rounded; where m lies far from 0: d = (x - m) c).  A part of nothing but
-// -inf has sums of 0.
+// Sums of a part of a row, d = (x - m) c.  P is negative where it lacks the maximum's term, 1: then -P is the rest of the batch's.
+// A part of nothing but -inf has sums of 0.
 struct __align__(16) Part {
   float m, P, S, X;
 };
-// The parts that the lanes of a wave hold as one, the same in every lane: one lane's P stays apart.
-template <bool ENT>
-__device__ __forceinline__ Part join_lanes(float m, float rc, float P, float S, float X, float c) {
+__device__ __forceinline__ float whole(float P) { return __float_as_int(P) < 0 ? 1.0f - P : P; }
+// The parts that the lanes of a wave hold as one, the same in every lane: one lane's P stays apart.  `apart(m)`: how far the
+// lane's sums are to move to be seen from m.
+template <bool ENT, typename Apart>
+__device__ __forceinline__ Part join_lanes(float m, float P, float S, float X, Apart&& apart) {
   Part p;
   p.m = wave_max(m);
   const int first = wv::first_lane(__ballot(m == p.m) | (1ull << 63));
   p.P = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(P), first));
   if (static_cast<int>(threadIdx.x & 63) != first) {
-    S += P;
-    rebase<ENT>(S, X, fabsf(p.m) * c <= kFar ? rc - p.m * c : (m - p.m) * c);
+    S += whole(P);
+    rebase<ENT>(S, X, apart(p.m));
   }
   p.S = wave_sum(S);
   p.X = ENT ? wave_sum(X) : 0.0f;
   return p;
 }
-// again(add) goes over the wave's elements a second time, where the maximum lies far from 0.
-template <bool ENT, typename Again>
-__device__ __forceinline__ Part wave_part(const Sums& s, float c, Again&& again) {
-  Part p = join_lanes<ENT>(s.m, s.rc, s.P, s.S, s.X, c);
-  if (!(fabsf(p.m) * c <= kFar) && fabsf(p.m) != INFINITY) {
+template <bool ENT>
+__device__ __forceinline__ Part join_parts(const Part& q, float c) {
+  return join_lanes<ENT>(q.m, q.P, q.S, q.X, [&](float m) { return (q.m - m) * c; });
+}
+// A batch of a lane is of U vectors, `stride` apart, all below `end`.  again(add) goes over the wave's elements a second time, where
+// the maximum lies far from 0.
+template <bool ENT, int U, typename E, typename Again>
+__device__ __forceinline__ Part wave_part(const Row<E>& row, const Sums& s, float c, int stride, int end, Again&& again) {
+  Part p = join_lanes<ENT>(s.m, s.P, s.S, s.X, [&](float m) { return s.rc - m * c; });
+  const float mc = p.m * c;
+  if (fabsf(mc) <= kFar) {
+    const float rounded = __builtin_fmaf(p.m, c, -mc), f = exp2_fast(-rounded);
+    if constexpr (ENT) p.X = f * __builtin_fmaf(-rounded, p.P + p.S, p.X);
+    p.P *= f;
+    p.S *= f;
+    if (p.P + p.S < 1.125f) {
+      const int lane = threadIdx.x & 63, at = __builtin_amdgcn_readlane(s.at, wv::first_lane(__ballot(s.m == p.m)));
+      float rest = 0.0f;
+      if (lane < U * E::N && at >= 0 && at + lane / E::N * stride < end) {
+        const float x = E::up(row.x[row.token(at + lane / E::N * stride, lane % E::N)]);
+        rest = x == p.m ? 0.0f : exp2_fast((x - p.m) * c);
+      }
+      p.P = -wave_sum(rest);
+    }
+  } else if (fabsf(p.m) != INFINITY) {
     float S = 0.0f, X = 0.0f;
     again([&](float x) {
       const float d = (x - p.m) * c, e = exp2_fast(d);
@@ -108,9 +133,9 @@ __device__ __forceinline__ Part join_set(const Part (&q)[W], float c) {
 #pragma unroll
   for (int w = 0; w < W; ++w) {
     const bool top = !taken && q[w].m == p.m;
-    float S = q[w].S + (top ? 0.0f : q[w].P), X = q[w].X;
+    float S = q[w].S + (top ? 0.0f : whole(q[w].P)), X = q[w].X;
     float S1 = S, X1 = X;
-    rebase<ENT>(S1, X1, fabsf(p.m) * c <= kFar ? q[w].m * c - p.m * c : (q[w].m - p.m) * c);
+    rebase<ENT>(S1, X1, (q[w].m - p.m) * c);
     p.P = top ? q[w].P : p.P;
     p.S += top ? S : S1;
     p.X += top ? X : X1;
@@ -126,15 +151,14 @@ struct RowSums {  // the same in every thread of the row
   float H;        // entropy
   bool bad;       // the row holds a NaN or +inf
 };
-__device__ __forceinline__ RowSums finish(const Part& p, float c) {
+__device__ __forceinline__ RowSums finish(const Part& p) {
   const bool empty = p.m == -INFINITY;
-  const float S = p.P + p.S, mc = p.m * c, rounded = fabsf(mc) <= kFar ? __builtin_fmaf(p.m, c, -mc) : 0.0f;
-  const float log_s = log_1p((p.P - 1.0f) + p.S);
+  const float S = whole(p.P) + p.S, log_s = log_1p((__float_as_int(p.P) < 0 ? -p.P : p.P - 1.0f) + p.S);
   RowSums r;
   r.bad = S != S || p.m == INFINITY;
   r.m = r.bad ? NAN : p.m;
   r.base = empty ? 0.0f : p.m;
-  r.log_s = r.bad ? NAN : empty ? 0.0f : log_s - rounded * kLn2;
+  r.log_s = r.bad ? NAN : empty ? 0.0f : log_s;
   r.H = r.bad ? NAN : empty ? 0.0f : log_s - p.X * kLn2 * __builtin_amdgcn_rcpf(S);
   return r;
 }
@@ -143,18 +167,18 @@ __device__ __forceinline__ RowSums finish(const Part& p, float c) {
 template <int NT, bool ENT>
 __device__ __forceinline__ RowSums join_waves(const Part& p, int tid, float c, Part* lds) {
   constexpr int W = NT / 64;
-  if constexpr (W == 1) return finish(p, c);
+  if constexpr (W == 1) return finish(p);
   if ((tid & 63) == 0) lds[tid >> 6] = p;
   __syncthreads();
   if constexpr (W <= 4) {
     Part q[W];
 #pragma unroll
     for (int w = 0; w < W; ++w) q[w] = lds[w];
-    return finish(join_set<ENT, W>(q, c), c);
+    return finish(join_set<ENT, W>(q, c));
   }
   // (a lane each: the waves of one row share a CU, and sixteen joins one after the other took longer than the reductions)
   const Part q = (tid & 63) < W ? lds[tid & 63] : Part{-INFINITY, 0.0f, 0.0f, 0.0f};
-  return finish(join_lanes<ENT>(q.m, q.m * c, q.P, q.S, q.X, c), c);
+  return finish(join_parts<ENT>(q, c));
 }
 
 // The alternatives.  Every lane keeps the largest element of its vectors (m1), the first vector that holds it (k1) and the
@@ -575,7 +599,7 @@ __global__ __launch_bounds__(NT == 64 ? 256 : NT) void logprobs_kernel(LogprobAr
       m = u == 0 ? vm : max3(m, vm, vm);
     }
     s.m = max3(s.m, m, m);
-    add_batch<ENT>(s, x, m, c);
+    add_batch<ENT>(s, x, m, c, k * NT + tid);
   };
   using std::integral_constant;
   auto run = [&](auto& raw, int k) {
@@ -603,9 +627,9 @@ __global__ __launch_bounds__(NT == 64 ? 256 : NT) void logprobs_kernel(LogprobAr
   if (tid < row.edges) {
     const float x[1][1] = {{edge}};
     s.m = fmaxf(s.m, edge);
-    add_batch<ENT>(s, x, edge, c);
+    add_batch<ENT>(s, x, edge, c, -1);
   }
-  const Part part = wave_part<ENT>(s, c, [&](auto&& add) {
+  const Part part = wave_part<ENT, kUnroll>(row, s, c, NT, row.nv, [&](auto&& add) {
     for (int v = tid; v < row.nv; v += NT) {
       float x[E::N];
       E::unpack(row.vec(v), x);
@@ -655,7 +679,7 @@ __global__ __launch_bounds__(256) void logprobs_parts_kernel(LogprobArgs a, int 
         const float vm = vec_max(x[0]);
         if constexpr (TOP) tops.add(vm, v0 + 64 * u);
         s.m = fmaxf(s.m, vm);
-        add_batch<ENT>(s, x, vm, c);
+        add_batch<ENT>(s, x, vm, c, v0 + 64 * u);
       }
   }
   const bool has_edge = begin == 0 && lane < row.edges;  // (the first part has the edge as well)
@@ -664,9 +688,9 @@ __global__ __launch_bounds__(256) void logprobs_parts_kernel(LogprobArgs a, int 
     edge = E::up(row.x[row.edge_token(lane)]);
     const float x[1][1] = {{edge}};
     s.m = fmaxf(s.m, edge);
-    add_batch<ENT>(s, x, edge, c);
+    add_batch<ENT>(s, x, edge, c, -1);
   }
-  const Part p = wave_part<ENT>(s, c, [&](auto&& add) {
+  const Part p = wave_part<ENT, 1>(row, s, c, 64, end, [&](auto&& add) {
     for (int v = begin + lane; v < end; v += 64) {
       float x[E::N];
       E::unpack(row.vec(v), x);
@@ -737,7 +761,7 @@ __global__ __launch_bounds__(kJoinThreads) void logprobs_join_kernel(LogprobArgs
   const int given = load_given<E>(a, r, row, tid, given_x);
   if (tid < row.edges) edge = E::up(row.x[row.edge_token(tid)]);
   const Part all = join_set<ENT, PER>(p, c);
-  const RowSums sums = finish(join_lanes<ENT>(all.m, all.m * c, all.P, all.S, all.X, c), c);
+  const RowSums sums = finish(join_parts<ENT>(all, c));
   if (wave == 0) write_scores(a, r, tid, sums, given, given_x);
   if constexpr (TOP) {
     if (sums.bad) return;

@@ -159,6 +159,30 @@ def test_alternatives_that_crowd(V, kind):
         check_logprobs(o, values, 1.0, None, top, (V, kind, top))
 
 
+@pytest.mark.parametrize("kind", list(KIND))
+@pytest.mark.parametrize("V", [1, 5, 40, 1025, 9000, 40000, 70001, 131072])
+def test_small_log_probs_and_entropies(V, kind):
+    """A token that has all but 1e-3 .. 1e-8 of a row: its log-prob and the entropy are as near, relative to themselves, as the
+    probabilities of the others are (R: their sum, log p = -log(1 + R)), not only relative to 1."""
+    rng = np.random.default_rng(V)
+    x = np.where(rng.random((6, V)) < 30.0 / V, rng.uniform(-21, -10, (6, V)), -np.inf)
+    at = np.array([0, V - 1, *rng.integers(0, V, 4)])
+    x[np.arange(6), at] = np.array([0.0, 3.0, -2.0, 0.0, 5.5, 0.0])
+    buf, view, values = place(x, kind)
+    o = run_logprobs(view, kind, V, V, 1.0, dev(at[:, None].astype(np.int32)), min(V, 3))
+    top = host(o["top_logp"])
+    for r in range(6):
+        d = values[r] - values[r].max()
+        e = np.where(np.arange(V) == at[r], 0.0, np.exp(d))
+        R_, far = e.sum(), np.abs(d[np.isfinite(d)]).max()
+        off = R.U * (R.chain(V) + 16 + 8 * far)      # of every term and their sum, relative to it
+        want = -np.log1p(R_)
+        R.check(host(o["logp"])[r], [want], abs(want) * off, (V, kind, r, "logp"))
+        R.check(top[r, :1], [want], abs(want) * off, (V, kind, r, "top"))
+        H = np.log1p(R_) - (e[e > 0] * d[e > 0]).sum() / (1 + R_)
+        R.check(host(o["entropy"])[r], H, H * 2 * off, (V, kind, r, "entropy"))
+
+
 def test_widest_rows():
     V = 393216
     rng = np.random.default_rng(5)
@@ -452,6 +476,30 @@ def test_little_mass_for_the_rest_and_large_weights(V, kind):
             want, g, e, eg = R.distill(values[r], T, t[r], l[r].astype(np.float64), True, float(w[r]))
             R.check(got_loss[r], want, e * (1 + 2 ** -20) + R.U * abs(want) + 1e-37, (V, kind, T, r, "loss"))
             R.check(got[r], g, R.rounded(eg, g, kind), (V, kind, T, r, "grad"))
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [1, 5, 40, 1025, 9000, 33000, 70001, 131072])
+def test_small_losses_and_gradients(V, kind):
+    """The student has all but 1e-3 .. 1e-8 of a row on the one token that the teacher lists: loss log(1 + R) and gradient
+    -R / (1 + R) on it are as near, relative to themselves, as R, the sum of the others, is."""
+    rng = np.random.default_rng(V)
+    x = np.where(rng.random((6, V)) < 30.0 / V, rng.uniform(-21, -10, (6, V)), -np.inf)
+    at = np.array([0, V - 1, *rng.integers(0, V, 4)])
+    x[np.arange(6), at] = np.array([0.0, 3.0, -2.0, 0.0, 5.5, 0.0])
+    buf, view, values = place(x, kind)
+    for tail in (False, True):
+        loss, grad = torch.full((6,), JUNK, device=DEV), torch.full((6, V), JUNK, dtype=KIND[kind][1], device=DEV)
+        run_distill(view, kind, V, V, 1.0, dev(at[:, None].astype(np.int32)), torch.zeros((6, 1), device=DEV), tail, None, loss, grad, V)
+        for r in range(6):
+            d = values[r] - values[r].max()
+            e = np.where(np.arange(V) == at[r], 0.0, np.exp(d))
+            R_, far = e.sum(), np.abs(d[np.isfinite(d)]).max()
+            off = R.U * (R.chain(V) + 20 + 8 * far)
+            R.check(host(loss)[r], np.log1p(R_), np.log1p(R_) * off, (V, kind, tail, r, "loss"))
+            want = e / (1 + R_)
+            want[at[r]] = -R_ / (1 + R_)
+            R.check(host(grad)[r], want, np.abs(want) * (off + R.HALF_STEP[kind]) + R.TINY[kind], (V, kind, tail, r, "grad"))
 
 
 # ---- together ----------------------------------------------------------------------------------------------------------
