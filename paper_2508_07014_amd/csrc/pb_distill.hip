@@ -183,101 +183,6 @@ __device__ __forceinline__ double wave_sum(double v) {
   return __longlong_as_double((static_cast<long long>(hi) << 32) | lo);
 }
 
-// The teacher's list of a row, an entry a lane.
-struct Entry {
-  int token;    // -1: absent
-  float x;      // the student's logit
-  float log_q, q;
-};
-struct List {   // the same in every lane
-  float rest;   // what the entries leave of 1
-  float Q;      // sum of q and rest
-  float shift;  // log q = l - shift
-  int any;      // there is something to learn from
-};
-template <typename E, bool TAIL>
-__device__ __forceinline__ List load_list(const DistillArgs& a, int64_t r, const Row<E>& row, int lane, Entry& e) {
-  e = Entry{-1, 0.0f, -INFINITY, 0.0f};
-  if (lane < a.K) {
-    const int t = a.tokens[r * a.K + lane];
-    const float value = a.logp[r * a.K + lane];
-    if (static_cast<unsigned>(t) < static_cast<unsigned>(row.V)) {
-      e.token = t;
-      e.x = E::up(row.x[t]);
-      e.log_q = value;
-    }
-  }
-  List l;
-  if constexpr (TAIL) {
-    // (1 - sum q in 64 bits: where the list holds nearly everything, fp32 would leave nothing of it)
-    const double q = e.log_q == INFINITY ? NAN : exp(static_cast<double>(e.log_q)), sum = wave_sum(q), left = 1.0 - sum;
-    e.q = static_cast<float>(q);
-    l.rest = left < 0x1p-20 ? 0.0f : static_cast<float>(left);  // (NaN stays)
-    l.any = __ballot(e.token >= 0) != 0 ? 1 : 0;
-    l.Q = l.rest > 0.0f ? 1.0f : static_cast<float>(sum);
-    l.shift = 0.0f;
-  } else {
-    const float top = wave_max(e.log_q);
-    l.any = __ballot(e.token >= 0 && e.log_q != -INFINITY) != 0 ? 1 : 0;
-    const float part = e.token >= 0 ? exp2_fast((e.log_q - (l.any ? top : 0.0f)) * kLog2e) : 0.0f;
-    const float sum = wave_sum(part);
-    l.rest = 0.0f;
-    l.shift = top + logf(sum);
-    e.log_q -= l.shift;
-    e.q = part / sum;
-    l.Q = sum == sum ? 1.0f : NAN;
-  }
-  return l;
-}
-
-struct Student {
-  float S;       // sum over all tokens
-  float p_rest;  // what the student leaves to the tokens that are not listed
-  float A, lift; // their gradient is A exp2((x - base) c + lift)
-};
-template <bool TAIL>
-__device__ __forceinline__ Student student(const RowSums& sums, const List& list, float w, float inv) {
-  Student s{static_cast<float>(sums.all), 0.0f, 0.0f, 0.0f};
-  float share = list.Q;
-  if constexpr (TAIL) {
-    s.p_rest = sums.m == -INFINITY ? 0.0f : sums.S / s.S;
-    if (s.p_rest < 0x1p-126f) s.p_rest = 0.0f;  // (NaN stays)
-    // (q' / p' may pass the fp32 range together with a row's weight, q' p_j / p' does not: the power of 2 goes into p_j)
-    if (list.rest > 0.0f && s.p_rest > 0.0f) {
-      const int k = 127 - static_cast<int>(__float_as_uint(s.p_rest) >> 23);
-      s.lift = static_cast<float>(k);
-      share = ldexpf(share, -k) - list.rest / ldexpf(s.p_rest, k);
-    }
-  }
-  s.A = share * w * inv / s.S;
-  return s;
-}
-// Sum of q over the entries of the lane's token (it may be listed more than once).  By one wave; `table`, kHashBits bits of
-// LDS, finds the few tokens that can be the same as another (in lists of 64 different ones every fifth has such a pair):
-// 64 comparisons of every lane took 3.2 us.
-constexpr int kHashBits = 8192;
-__device__ __forceinline__ float mass_of(const Entry& e, unsigned* table) {
-  const v4u none = {0u, 0u, 0u, 0u};
-#pragma unroll
-  for (int i = 0; i < kHashBits / 128; i += 64) reinterpret_cast<v4u*>(table)[i + (threadIdx.x & 63)] = none;
-  row_sync<64>();
-  unsigned seen = 0u;
-  if (e.token >= 0) {
-    const unsigned h = static_cast<unsigned>(e.token) * 2654435761u >> 19;
-    seen = atomicOr(&table[h >> 5], 1u << (h & 31)) >> (h & 31) & 1u;
-  }
-  float mass = e.q;
-  for (u64 left = __ballot(seen != 0u); left != 0;) {
-    const int token = __builtin_amdgcn_readlane(e.token, wv::first_lane(left));
-    const u64 same = __ballot(e.token == token);
-    if (__builtin_popcountll(same) > 1) {
-      const float sum = wave_sum(e.token == token ? e.q : 0.0f);
-      mass = e.token == token ? sum : mass;
-    }
-    left &= ~same;
-  }
-  return mass;
-}
 // 1 / v and log(v), v a positive number, to 1e-14: v = 2^k m, m in [sqrt(1/2), sqrt(2)), log m = 2 atanh(t), t = (m - 1) / (m + 1), by
 // its series up to t^15 (the library's takes three times the instructions for the last bits).
 __device__ __forceinline__ double over_64(double v) {
@@ -299,17 +204,113 @@ __device__ __forceinline__ double log_64(double v) {
   s = __builtin_fma(s, t2, 1.0);
   return __builtin_fma(static_cast<double>(k), 0.69314718055994530942, 2.0 * t * s);
 }
+
+// The teacher's list of a row, an entry a lane.
+// (Probabilities of the list and the student's on it in 64 bits: losses and gradients are small differences of them, and fp32 would
+// leave 6e-8 of a probability, as much as 1e-4 of a gradient.)
+struct Entry {
+  int token;    // -1: absent
+  float x;      // the student's logit
+  double log_q, q;
+};
+struct List {   // the same in every lane
+  double rest;  // what the entries leave of 1
+  double shift; // log q = l - shift
+  float Q;      // sum of q and rest
+  int any;      // there is something to learn from
+};
+template <typename E, bool TAIL>
+__device__ __forceinline__ List load_list(const DistillArgs& a, int64_t r, const Row<E>& row, int lane, Entry& e) {
+  e = Entry{-1, 0.0f, -INFINITY, 0.0};
+  if (lane < a.K) {
+    const int t = a.tokens[r * a.K + lane];
+    const float value = a.logp[r * a.K + lane];
+    if (static_cast<unsigned>(t) < static_cast<unsigned>(row.V)) {
+      e.token = t;
+      e.x = E::up(row.x[t]);
+      e.log_q = value;
+    }
+  }
+  List l;
+  if constexpr (TAIL) {
+    e.q = e.log_q == INFINITY ? NAN : exp(e.log_q);
+    const double sum = wave_sum(e.q), left = 1.0 - sum;
+    l.rest = left < 0x1p-20 ? 0.0 : left;  // (NaN stays)
+    l.any = __ballot(e.token >= 0) != 0 ? 1 : 0;
+    l.Q = l.rest > 0.0 ? 1.0f : static_cast<float>(sum);
+    l.shift = 0.0;
+  } else {
+    const float top = wave_max(static_cast<float>(e.log_q));
+    l.any = __ballot(e.token >= 0 && e.log_q != -INFINITY) != 0 ? 1 : 0;
+    const double part = e.token >= 0 ? exp(e.log_q - (l.any ? top : 0.0f)) : 0.0, sum = wave_sum(part);
+    l.rest = 0.0;
+    l.shift = top + log_64(sum);
+    l.Q = sum == sum ? 1.0f : NAN;
+    e.log_q -= l.shift;
+    e.q = part * over_64(sum);
+  }
+  return l;
+}
+
+struct Student {
+  float S;       // sum over all tokens
+  double p_rest; // what the student leaves to the tokens that are not listed
+  float A, lift; // their gradient is A exp2((x - base) c + lift)
+};
+template <bool TAIL>
+__device__ __forceinline__ Student student(const RowSums& sums, const List& list, float w, float inv) {
+  Student s{static_cast<float>(sums.all), 0.0, 0.0f, 0.0f};
+  double share = list.Q;
+  if constexpr (TAIL) {
+    s.p_rest = sums.m == -INFINITY ? 0.0 : sums.S * over_64(sums.all);
+    if (s.p_rest < 0x1p-126) s.p_rest = 0.0;  // (NaN stays)
+    // (q' / p' may pass the fp32 range together with a row's weight, q' p_j / p' does not: the power of 2 goes into p_j)
+    if (list.rest > 0.0 && s.p_rest > 0.0) {
+      const int k = 1023 - static_cast<int>(__double_as_longlong(s.p_rest) >> 52);
+      s.lift = static_cast<float>(k);
+      share = ldexp(share, -k) - list.rest * over_64(ldexp(s.p_rest, k));
+    }
+  }
+  s.A = static_cast<float>(share) * w * inv / s.S;
+  return s;
+}
+// Sum of q over the entries of the lane's token (it may be listed more than once).  By one wave; `table`, kHashBits bits of
+// LDS, finds the few tokens that can be the same as another (in lists of 64 different ones every fifth has such a pair):
+// 64 comparisons of every lane took 3.2 us.
+constexpr int kHashBits = 8192;
+__device__ __forceinline__ double mass_of(const Entry& e, unsigned* table) {
+  const v4u none = {0u, 0u, 0u, 0u};
+#pragma unroll
+  for (int i = 0; i < kHashBits / 128; i += 64) reinterpret_cast<v4u*>(table)[i + (threadIdx.x & 63)] = none;
+  row_sync<64>();
+  unsigned seen = 0u;
+  if (e.token >= 0) {
+    const unsigned h = static_cast<unsigned>(e.token) * 2654435761u >> 19;
+    seen = atomicOr(&table[h >> 5], 1u << (h & 31)) >> (h & 31) & 1u;
+  }
+  double mass = e.q;
+  for (u64 left = __ballot(seen != 0u); left != 0;) {
+    const int token = __builtin_amdgcn_readlane(e.token, wv::first_lane(left));
+    const u64 same = __ballot(e.token == token);
+    if (__builtin_popcountll(same) > 1) {
+      const double sum = wave_sum(e.token == token ? e.q : 0.0);
+      mass = e.token == token ? sum : mass;
+    }
+    left &= ~same;
+  }
+  return mass;
+}
 // By one wave: the row's loss.  Terms that cancel, and log-probs of masked tokens that may pass the fp32 range: in 64 bits.
 template <bool TAIL>
 __device__ __forceinline__ void write_loss(const DistillArgs& a, int64_t r, int lane, const Entry& e, const List& list, const RowSums& sums,
                                            const Student& st, float inv) {
   const double lp = (static_cast<double>(e.x) - sums.base) * inv - (sums.m == -INFINITY ? 0.0 : log_64(sums.all));
-  double loss = wave_sum(e.q > 0.0f ? e.q * (e.log_q - lp) : static_cast<double>(e.q));  // (0, or NaN)
-  if (TAIL && list.rest != 0.0f) loss += list.rest * static_cast<double>(logf(list.rest / st.p_rest));
+  double loss = wave_sum(e.q > 0.0 ? e.q * (e.log_q - lp) : e.q);  // (0, or NaN)
+  if (TAIL && list.rest != 0.0) loss += st.p_rest == 0.0 ? INFINITY : list.rest * (log_64(list.rest) - log_64(st.p_rest));
   if (lane == 0) a.loss[r] = sums.bad ? NAN : static_cast<float>(loss);
 }
 // The gradient on a listed token: the difference of two probabilities, of which one may be near 1, in 64 bits.
-__device__ __forceinline__ float listed_grad(float x, float mass, const List& list, const RowSums& sums, float c, float w, float inv) {
+__device__ __forceinline__ float listed_grad(float x, double mass, const List& list, const RowSums& sums, float c, float w, float inv) {
   const double p = exp2_fast((x - sums.base) * c) * over_64(sums.all);
   return static_cast<float>(p * list.Q - mass) * w * inv;
 }
@@ -351,9 +352,9 @@ __global__ __launch_bounds__(NT == 64 ? 256 : NT) void distill_kernel(DistillArg
     for (int i = tid; i < mark_bytes / 4; i += NT) reinterpret_cast<unsigned*>(marks)[i] = 0u;
     if (tid == 0) s_edge[sub] = 0;
   }
-  Entry e{-1, 0.0f, 0.0f, 0.0f};
-  List list{0.0f, 0.0f, 0.0f, 0};
-  float mass = 0.0f;
+  Entry e{-1, 0.0f, 0.0, 0.0};
+  List list{0.0, 0.0, 0.0f, 0};
+  double mass = 0.0;
   if (lister) {
     list = load_list<E, TAIL>(a, r, row, tid & 63, e);
     if (a.grad) mass = mass_of(e, s_table[sub]);
@@ -471,8 +472,8 @@ constexpr int kGradUnroll = 4;
 struct DistillSpace {
   float4* parts;  // [rows, parts]
   List* lists;    // [rows]
+  double* mass;   // [rows, 64]
   float* x;       // [rows, 64]
-  float* mass;    // [rows, 64]
 };
 template <typename E, bool TAIL>
 __global__ __launch_bounds__(256) void distill_parts_kernel(DistillArgs a, int parts, int each, DistillSpace ws) {
@@ -585,8 +586,8 @@ __global__ __launch_bounds__(256) void distill_grad_kernel(DistillArgs a, int pa
   const RowSums sums = join_waves<64, TAIL>(join_lanes<TAIL>(p, c), lane, c, nullptr);
   const Student st = student<TAIL>(sums, list, w, inv);
   const bool learn = list.any != 0, none = !learn || sums.m == -INFINITY || w == 0.0f;
-  Entry e{-1, 0.0f, -INFINITY, 0.0f};
-  float mass = 0.0f;
+  Entry e{-1, 0.0f, -INFINITY, 0.0};
+  double mass = 0.0;
   bool mine = false;  // the lane's listed token lies in this block, whose first wave writes it after the other stores
   if (tid < 64) {
     if (learn && tid < a.K) {
@@ -596,7 +597,7 @@ __global__ __launch_bounds__(256) void distill_grad_kernel(DistillArgs a, int pa
         e.x = ws.x[r * 64 + tid];
         mass = ws.mass[r * 64 + tid];
         e.log_q = a.logp[r * a.K + tid] - list.shift;
-        e.q = exp2_fast(e.log_q * kLog2e);
+        if (block == 0) e.q = exp(e.log_q);
         mine = block == (t < row.head || t >= row.head + row.nv * E::N ? 0 : (t - row.head) / E::N / BLOCK);
       }
     }
@@ -629,8 +630,8 @@ DistillSpace space_in(void* p, int32_t rows, int parts) {
   DistillSpace ws;
   ws.parts = static_cast<float4*>(p);
   ws.lists = reinterpret_cast<List*>(ws.parts + static_cast<int64_t>(rows) * parts);
-  ws.x = reinterpret_cast<float*>(ws.lists + rows);
-  ws.mass = ws.x + static_cast<int64_t>(rows) * 64;
+  ws.mass = reinterpret_cast<double*>(ws.lists + rows);
+  ws.x = reinterpret_cast<float*>(ws.mass + static_cast<int64_t>(rows) * 64);
   return ws;
 }
 
@@ -692,7 +693,7 @@ int distill(const DistillArgs& a, void* workspace, hipStream_t stream) {
 int64_t distill_topk_workspace(int dtype, int32_t rows, int32_t V) {
   const RowSplit split = split_distill(V / (dtype == PB_F32 ? lr::F32::N : lr::F16::N), rows);
   if (split.parts == 0) return 0;
-  return static_cast<int64_t>(rows) * (split.parts * static_cast<int64_t>(sizeof(float4)) + sizeof(lr::List) + 2 * 64 * sizeof(float));
+  return static_cast<int64_t>(rows) * (split.parts * static_cast<int64_t>(sizeof(float4)) + sizeof(lr::List) + 64 * (sizeof(double) + sizeof(float)));
 }
 int launch_distill_topk(int dtype, const DistillArgs& a, void* workspace, hipStream_t stream) {
   return dtype == PB_F32   ? lr::distill<lr::F32>(a, workspace, stream)
