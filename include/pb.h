@@ -309,8 +309,8 @@ int pb_fuse_step_beam_forest(const pb_forest* forest, const float* d_logp, int64
  * Rows of logits before and after the tree: how sure a model was of the tokens a decoder emitted, what else it had in
  * mind, and the two losses that train on such lists.  Not in the paper.  These calls need no tree.
  *   d_logits: rows x V elements of `dtype` (enum pb_dtype), row r at d_logits + r * row_stride elements (row_stride >= V),
- *   at any alignment of its elements.  Log-probs of the decoders above are logits as well.  Arithmetic is fp32 for every
- *   type.  With z_j = x_j / temperature:
+ *   at any alignment of its elements.  Log-probs of the decoders above are logits as well.  Arithmetic on rows is fp32 for
+ *   every type, on a teacher's list and its loss fp64.  With z_j = x_j / temperature:
  *     log p(t) = z_t - log sum_j exp(z_j),   p_j = exp(log p(j)),   H = -sum_j p_j log p(j)   (p_j = 0 adds nothing).
  *   A logit of -inf is a masked token (p = 0).  A row of nothing but -inf has log p = -inf, H = 0 and gradient 0.  A row
  *   that holds a NaN or +inf is marked: NaN scores, -1 ids.  A token id outside [0, V) is absent: see each call.

@@ -557,7 +557,10 @@ __device__ __forceinline__ int load_given(const LogprobArgs& a, int64_t r, const
   return t;
 }
 
-// One row, by a workgroup, or (NT == 64: rows of up to kWaveVectors vectors) by a wave, four in a workgroup.
+// One row, by a workgroup, or (NT == 64: rows of up to kWaveVectors vectors) by a wave, four in a workgroup.  Large calls of long
+// rows are bound by HBM (8192 x 32001 bf16, 32 alternatives: 100 us, 5.2 TB/s), those of short rows by vector instructions (16000 x
+// 1025 fp32 with entropy: 12.8 us, 5.2 TB/s; with 5 alternatives 17.5 us, 500 instructions a wave, 83 % of the cycles), small ones
+// by the launch and one row's chain of loads and reductions (32 x 1024 fp32: 3.1 us).
 static_assert(kWaveVectors == 2 * 64 * kUnroll, "a wave requests its row in two batches");
 template <typename E, int NT, bool ENT, bool TOP>
 __global__ __launch_bounds__(NT == 64 ? 256 : NT) void logprobs_kernel(LogprobArgs a) {
@@ -650,6 +653,7 @@ __global__ __launch_bounds__(NT == 64 ? 256 : NT) void logprobs_kernel(LogprobAr
 // Few long rows: every wave takes 64 * `each` vectors of a row and leaves their part in the workspace, with the largest element
 // of the vectors, its token and the largest of the others; a workgroup per row joins them.  The parts' largest elements bound
 // the alternatives as the lanes' do above, and are candidates themselves; the few parts with a second one are read again.
+// Both are bound by latency: 1 x 131072 bf16, 20 alternatives, 3.3 us and 5.4 us.
 struct PartRecord {
   Part sums;
   float top, second;
@@ -803,7 +807,8 @@ __global__ __launch_bounds__(kJoinThreads) void logprobs_join_kernel(LogprobArgs
 
 // Gradient: p (A + B log2 p) with A = -(G + h H) / T, B = -h ln(2) / T for all tokens, plus what the given ones take.  A
 // workgroup takes kUnroll vectors a thread of one row (a wave, four rows a workgroup, where those hold the row).  The
-// gradients on the given tokens are computed before anything is written and stored behind the rest.
+// gradients on the given tokens are computed before anything is written and stored behind the rest.  Bound by HBM (4096 x 50000
+// bf16: 134 us, 6.1 TB/s, more than a plain copy's 5.2), small calls by the launch.
 template <typename E, int NT, bool STREAM>
 __global__ __launch_bounds__(256) void logprobs_backward_kernel(LogprobGradArgs a, int parts) {
   constexpr int ROWS = 256 / NT, PART = NT * kUnroll;
@@ -897,8 +902,9 @@ int forward(const LogprobArgs& a, void* workspace, hipStream_t stream) {
     if (top) return go(logprobs_kernel<E, NT, false, true>);
     return go(logprobs_kernel<E, NT, false, false>);
   };
-  // Threads a row, us with 64 / 128 / 256 / 512 / 1024: 16384 x 8192 bf16, 8 alternatives: 58 57 73 143 249; 1024 x 16384, 20 of them:
-  // - 15.8 16.0 21 29; 256 x 16384: - 11.3 9.9 10.2 12.1; 8192 x 32001: - 110 104 122 177; 256 x 131072: - 34 22 19 21.
+  // Threads a row, us with 128 / 256 / 512 / 1024, bf16: 16384 x 8192, 8 alternatives: 59 73 114 312; 5000 x 4104 without: 11.5 12.6 17.4
+  // 29; 1024 x 16384, 20 of them: 14.6 14.9 19.0 35; 256 x 16384: 11.0 10.0 10.1 13.6; 8192 x 32001, 8 of them: 103 99 106 209; 120 x
+  // 33000, 5 of them and entropy: 11.7 8.7 7.7 8.3, 300 x 33000: 14.6 10.8 11.1 15.4; 256 x 131072, 20 of them: 33 22.6 20.0 23.
   const int nv = a.in.V / E::N;
   if (nv <= kWaveVectors) return pick(std::integral_constant<int, 64>{});
   if (nv <= 2048 && a.in.rows >= 1024) return pick(std::integral_constant<int, 128>{});
