@@ -78,15 +78,16 @@ inline RowSplit row_split(int vectors, int32_t rows, int few) {
   return RowSplit{(vectors + 64 * each - 1) / (64 * each), each};
 }
 
-// Which calls are split.  us, split / a workgroup a row: log-probs with entropy and 5 alternatives, bf16, V = 41000, 16 rows 8.3 / 8.7,
-// 32 rows 9.0 / 8.6; V = 50000, 1 row 7.8 / 9.1, 32 rows 9.1 / 9.4, 64 rows 10.5 / 9.7; V = 80000, 32 rows 9.9 / 10.2, 48 rows
-// 11.0 / 10.2; V = 131072, 1 row 8.2 / 12.4, 64 rows 12.4 / 13.5, 96 rows 14.3 / 13.7; fp32 V = 50000, 1 row 7.7 / 8.6, 16 rows 8.7 / 8.8,
-// 32 rows 10.1 / 8.9; bf16 without alternatives, V = 41000 7.3 / 6.6 and V = 131072, 32 rows 6.9 / 10.4.  Distillation, bf16: V = 32001,
-// 16 rows 7.9 / 8.4, 64 rows 9.4 / 8.7; V = 50000, 32 rows 9.1 / 10.9, 64 rows 11.4 / 11.1; V = 131072, 64 rows 14.7 / 22, 160 rows
-// 25.5 / 24.7; fp32 V = 131072, 256 rows 66 / 78.
+// Which calls are split.  us, split / a workgroup a row: log-probs with entropy and 5 alternatives, bf16, V = 50000, 1 row 8.6 / 8.1,
+// 32 rows 9.5 / 8.5; V = 80000, 1 row 8.4 / 9.6, 16 rows 9.2 / 10.0, 48 rows 11.4 / 10.3; V = 131072, 1 row 8.7 / 12.3, 64 rows 12.9 /
+// 13.7, 120 rows 16.0 / 14.0; V = 250000, 1 row 8.8 / 20, 120 rows 20.9 / 22.3; V = 393216, 240 rows 43 / 42; fp32 V = 50000, 1 row
+// 8.5 / 8.6, 16 rows 9.4 / 8.9; bf16 without alternatives, V = 80000, 16 rows 8.8 / 8.0 and V = 131072, 64 rows 9.3 / 11.1.
+// Distillation, bf16: V = 32001, 16 rows 7.9 / 8.4, 64 rows 9.4 / 8.7; V = 50000, 32 rows 9.1 / 10.9, 64 rows 11.4 / 11.1; V = 131072,
+// 64 rows 14.7 / 22, 160 rows 25.5 / 24.7; fp32 V = 131072, 256 rows 66 / 78.
 inline RowSplit split_logprobs(int vectors, int32_t rows, int32_t V) {
-  return vectors >= 5120 && rows <= V / 1600 ? row_split(vectors, rows, 80) : RowSplit{0, 0};  // (the parts are to bound 64 alternatives)
+  return rows <= (V - 70000) / 800 && rows <= V / 1800 ? row_split(vectors, rows, 80) : RowSplit{0, 0};  // (the parts are to bound 64 alternatives)
 }
+static_assert(70000 / 8 >= 80 * 64, "rows that are split have 80 parts of 64 vectors");
 inline RowSplit split_distill(int vectors, int32_t rows) {
   return vectors >= 3500 && rows <= vectors / 100 ? row_split(vectors, rows, 16) : RowSplit{0, 0};
 }

@@ -902,13 +902,14 @@ int forward(const LogprobArgs& a, void* workspace, hipStream_t stream) {
     if (top) return go(logprobs_kernel<E, NT, false, true>);
     return go(logprobs_kernel<E, NT, false, false>);
   };
-  // Threads a row, us with 128 / 256 / 512 / 1024, bf16: 16384 x 8192, 8 alternatives: 59 73 114 312; 5000 x 4104 without: 11.5 12.6 17.4
-  // 29; 1024 x 16384, 20 of them: 14.6 14.9 19.0 35; 256 x 16384: 11.0 10.0 10.1 13.6; 8192 x 32001, 8 of them: 103 99 106 209; 120 x
-  // 33000, 5 of them and entropy: 11.7 8.7 7.7 8.3, 300 x 33000: 14.6 10.8 11.1 15.4; 256 x 131072, 20 of them: 33 22.6 20.0 23.
+  // Threads a row, us with 128 / 256 / 512 / 1024, bf16: 16384 x 8192, 8 alternatives: 59 73 114 312; 5000 x 4104 without: 11.5 12.6
+  // 17.4 29; 1024 x 16384, 20 of them: 14.6 14.9 19.0 35; 8192 x 32001, 8 of them: 103 99 106 209; 400 x 33000, 5 of them and entropy:
+  // 15.1 11.7 11.7 16.6.  A row a CU and fewer, 5 of them and entropy: 200 x 6000 6.4 6.1 6.0 6.3; 64 x 12000 7.0 6.5 6.1 6.8; 256 x 33000
+  // 12.9 10.0 8.7 9.8; 64 x 50000 13.7 9.9 8.7 9.0; 256 x 60000 18.3 12.9 11.1 11.7.
   const int nv = a.in.V / E::N;
   if (nv <= kWaveVectors) return pick(std::integral_constant<int, 64>{});
   if (nv <= 2048 && a.in.rows >= 1024) return pick(std::integral_constant<int, 128>{});
-  if (nv <= 8192) return pick(std::integral_constant<int, 256>{});
+  if (nv <= 1024 || (nv <= 8192 && a.in.rows > 256)) return pick(std::integral_constant<int, 256>{});
   return pick(std::integral_constant<int, 512>{});
 }
 

@@ -339,7 +339,7 @@ def test_distill_many_rows(rows, V, K, tail, kind):
     check_distill(rng, view, values, kind, V, 1.0, t, l, tail, (rows, V, K, tail, kind))
 
 
-@pytest.mark.parametrize("rows,V", [(9, 40), (9, 9000), (9, 70000)])
+@pytest.mark.parametrize("rows,V", [(9, 40), (9, 9000), (9, 70000), (9, 131072)])
 def test_entries_that_are_no_numbers(rows, V):
     """An entry of NaN, of either sign, or +inf: loss and gradient are NaN (in the last case too where nothing else is listed);
     the rows beside it are what they are without it."""
@@ -367,7 +367,7 @@ def test_entries_that_are_no_numbers(rows, V):
 # Rows of every kernel shape, as many as send the call there (the shape is chosen by vectors a row and rows): 8 rows of each
 # call are compared.
 MANY = [(1100, 4104), (1030, 6001), (1025, 16400), (70, 8200), (70, 20001), (70, 30000), (70, 33001), (70, 50000), (70, 70001),
-        (170, 70000), (170, 131072), (81, 131072), (82, 131072), (300, 33000), (20, 41000), (64, 50001), (160, 70001), (260, 70001), (5000, 1030), (20, 30001),
+        (170, 70000), (170, 131072), (72, 131072), (73, 131072), (30, 100001), (9, 300000), (300, 33000), (20, 41000), (64, 50001), (160, 70001), (260, 70001), (5000, 1030), (20, 30001),
         (90, 72000)]
 
 
