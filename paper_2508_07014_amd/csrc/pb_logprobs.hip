@@ -855,7 +855,15 @@ __global__ __launch_bounds__(256) void logprobs_backward_kernel(LogprobGradArgs 
     for (int k = 0; k < a.n_tokens; ++k)
       if (__builtin_amdgcn_readlane(given, k) == given) onto += __int_as_float(__builtin_amdgcn_readlane(__float_as_int(g), k));
   }
-  const float taken = pull(given_x) + onto * inv;
+  // (onto - p G as (onto - G) + (1 - p) G: where p is near 1 the difference would have the rounding of 1, and 1 - p = 1 - e^l comes from
+  // its series, the next term l^6 / 5040 of it)
+  const float l = __builtin_fmaf(given_x - m, inv, -logs), d = fmaxf(__builtin_fmaf(given_x - m, c, -log2s), -1000.0f), p = exp2_fast(d);
+  float series = __builtin_fmaf(l, 1.0f / 6, 1.0f);
+  series = __builtin_fmaf(l * series, 1.0f / 5, 1.0f);
+  series = __builtin_fmaf(l * series, 1.0f / 4, 1.0f);
+  series = __builtin_fmaf(l * series, 1.0f / 3, 1.0f);
+  series = __builtin_fmaf(l * series, 1.0f / 2, 1.0f);
+  const float taken = p * __builtin_fmaf(B, d, -h * H * inv) + ((onto - G) + (l > -0.25f ? -l * series : 1.0f - p) * G) * inv;
   if constexpr (NT > 64) __syncthreads();
 #pragma unroll
   for (int u = 0; u < kUnroll; ++u) {

@@ -183,6 +183,31 @@ def test_small_log_probs_and_entropies(V, kind):
         R.check(host(o["entropy"])[r], H, H * 2 * off, (V, kind, r, "entropy"))
 
 
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [1, 5, 40, 1025, 9000, 33000, 131072])
+def test_small_gradients_of_log_probs(V, kind):
+    """The gradient of such a token's log-prob, R / (1 + R) on it, is as near relative to itself as R is; the others' as their
+    probabilities."""
+    rng = np.random.default_rng(V)
+    x = np.where(rng.random((6, V)) < 30.0 / V, rng.uniform(-21, -10, (6, V)), -np.inf)
+    at = np.array([0, V - 1, *rng.integers(0, V, 4)])
+    x[np.arange(6), at] = np.array([0.0, 3.0, -2.0, 0.0, 5.5, 0.0])
+    buf, view, values = place(x, kind)
+    o = run_logprobs(view, kind, V, V, 1.0)
+    g = np.array([[1.0], [-2.0], [0.5], [1.0], [3.0], [1.0]], np.float32)
+    grad = torch.full((6, V), JUNK, dtype=KIND[kind][1], device=DEV)
+    run_backward(view, kind, V, V, 1.0, o["stats"], dev(at[:, None].astype(np.int32)), dev(g), None, grad, V)
+    for r in range(6):
+        d = values[r] - values[r].max()
+        e = np.where(np.arange(V) == at[r], 0.0, np.exp(d))
+        R_, far = e.sum(), np.abs(d[np.isfinite(d)]).max()
+        off = R.U * (R.chain(V) + 24 + 10 * far)
+        want = -e / (1 + R_)
+        want[at[r]] = R_ / (1 + R_)
+        want *= g[r, 0]
+        R.check(host(grad)[r], want, np.abs(want) * (off + R.HALF_STEP[kind]) + R.TINY[kind], (V, kind, r))
+
+
 def test_widest_rows():
     V = 393216
     rng = np.random.default_rng(5)
