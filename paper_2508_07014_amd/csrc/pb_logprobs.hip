@@ -24,10 +24,12 @@ struct Sums {
   int at = -1;  // first vector of the batch that P is the sum of; -1: the edge
   __device__ __forceinline__ explicit Sums(float far) : thr(-far) {}
 };
-// (S, X) seen from a reference that lies `apart` = rc - new rc higher.
+// (S, X) seen from a reference that lies `apart` = rc - new rc higher.  From further than 2^1000 below nothing is left of either (a
+// wave of nothing but masks of a lowest value beside an ordinary one: apart S would pass the fp32 range, and X be 0 times that).
 template <bool ENT>
 __device__ __forceinline__ void rebase(float& S, float& X, float apart) {
-  const float f = exp2_fast(apart);  // (may be infinite, or none, where the sums are 0)
+  apart = fmaxf(apart, -1000.0f);
+  const float f = exp2_fast(apart);  // (may be infinite where the sums are 0)
   if constexpr (ENT) X = S == 0.0f ? 0.0f : f * __builtin_fmaf(apart, S, X);
   S = S == 0.0f ? 0.0f : f * S;
 }

@@ -1,0 +1,68 @@
+"""Rows of logits of which one part says nothing beside another, and gradients and losses that are small beside the numbers they
+are the difference of, on the GPU against the 64-bit definitions in logit_rows.py."""
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+if not torch.cuda.is_available():
+    pytest.skip("no GPU", allow_module_level=True)
+
+import logit_rows as R  # noqa: E402
+from gpu_helpers import DEV, dev  # noqa: E402
+from test_gpu_logits import JUNK, KIND, check_logprobs, host, place, run_backward, run_distill, run_logprobs, tokens_of  # noqa: E402
+
+
+def masked_rows(rng, rows, V, kind):
+    """Rows of which whole stretches are masked by finite values, in turn: all but the first token, the last, three of them, a
+    run of an eighth, the last few, and ordinary rows with one logit so large that nothing else counts."""
+    low = [-R.LARGEST[kind], -6e4 if kind == "f16" else -1e37, -2e4 if kind == "f16" else -6e35]
+    x = rng.normal(0, 2.5, (rows, V))
+    for r in range(rows):
+        keep = np.zeros(V, bool)
+        sort = r % 6
+        if sort == 0:
+            keep[0] = True
+        elif sort == 1:
+            keep[V - 1] = True
+        elif sort == 2:
+            keep[rng.integers(0, V, 3)] = True
+        elif sort == 3:
+            keep[V // 4:V // 4 + V // 8] = True
+        elif sort == 4:
+            keep[-17:] = True
+        else:
+            keep[:] = True
+            x[r, rng.integers(0, V)] = R.LARGEST[kind] if r // 6 % 2 == 0 else 3e4 if kind == "f16" else 1e36
+        x[r, ~keep] = low[r // 6 % 3]
+    return x
+
+
+@pytest.mark.parametrize("kind", list(KIND))
+@pytest.mark.parametrize("rows,V", [(18, 600), (18, 2100), (18, 9000), (300, 9000), (1030, 9000), (18, 40000), (18, 80000), (18, 131072)])
+def test_finite_masks_of_whole_stretches(rows, V, kind):
+    """A wave, or a part of a split row, that holds nothing but a mask of a lowest value beside one that holds ordinary logits:
+    the entropy counts what is left, and so do the statistics and the gradients that are formed from them."""
+    rng = np.random.default_rng(rows + V)
+    some = 18
+    x = masked_rows(rng, some, V, kind)
+    for T in (1.0, 0.7):
+        buf, view, values = place(np.tile(x, (rows // some + 1, 1))[:rows], kind)
+        tokens = tokens_of(rng, values[:some], 3)
+        tokens[:, 2] = values[:some].argmax(axis=1)
+        all_tokens = np.tile(tokens, (rows // some + 1, 1))[:rows]
+        d_tokens = dev(all_tokens.astype(np.int32))
+        for top in (0, 5):
+            o = run_logprobs(view, kind, V, V, T, d_tokens, top)
+            check_logprobs({k: None if v is None else v[:some] for k, v in o.items() if k != "ws"}, values[:some], T, tokens, top,
+                           (rows, V, kind, T, top))
+            assert not bool(torch.isnan(o["entropy"]).any()) and not bool(torch.isnan(o["stats"]).any())
+        g, h = rng.normal(0, 1, (rows, 3)).astype(np.float32), rng.normal(0, 1, rows).astype(np.float32)
+        for d_h in (None, dev(h)):
+            grad = torch.full((rows, V), JUNK, dtype=KIND[kind][1], device=DEV)
+            run_backward(view, kind, V, V, T, o["stats"], d_tokens, dev(g), d_h, grad, V)
+            got = host(grad[:some])
+            for r in range(some):
+                want, err = R.logprobs_grad(values[r], T, tokens[r], g[r].astype(np.float64), 0.0 if d_h is None else float(h[r]))
+                R.check(got[r], want, R.rounded(err, want, kind), (rows, V, kind, T, r))
