@@ -346,7 +346,8 @@ int pb_token_logprobs(const void* d_logits, int32_t dtype, int64_t row_stride, i
  * pb_token_logprobs left for the same rows and temperature:
  *     d_grad_logits[r * grad_stride + j] = (sum_k g_k ([j = t_k] - p_j) - h p_j (log p(j) + H)) / temperature
  *   in the logits' type, rounded once.  A token id outside [0, V) takes no gradient and its g is not looked at; the same
- *   token several times adds up.  A row whose incoming gradients are all 0 gets zeros, whatever it holds (padding).
+ *   token several times adds up.  A row whose incoming gradients are all 0 gets zeros, whatever it holds (padding); where h is 0
+ *   the H of d_stats is not looked at.
  *   n_tokens == 0 with null d_tokens and d_grad_logp: the entropy alone.  d_grad_logits may be d_logits with the same stride.
  */
 int pb_token_logprobs_backward(const void* d_logits, int32_t dtype, int64_t row_stride, int32_t rows, int32_t vocab_size,

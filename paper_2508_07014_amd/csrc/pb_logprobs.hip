@@ -846,7 +846,8 @@ __global__ __launch_bounds__(256) void logprobs_backward_kernel(LogprobGradArgs 
   }
   const float G = wave_sum(g);
   const bool none = (__ballot(g != 0.0f) == 0 && h == 0.0f) || m == -INFINITY;
-  const float A = none ? 0.0f : m != m ? NAN : -(G + h * H) * inv, B = none ? 0.0f : -h * kLn2 * inv, log2s = logs * kLog2e;
+  const float hH = h == 0.0f ? 0.0f : h * H;  // (H counts for nothing where h does)
+  const float A = none ? 0.0f : m != m ? NAN : -(G + hH) * inv, B = none ? 0.0f : -h * kLn2 * inv, log2s = logs * kLog2e;
   auto pull = [&](float x) {
     const float d = fmaxf(__builtin_fmaf(x - m, c, -log2s), -1000.0f);
     return exp2_fast(d) * __builtin_fmaf(B, d, A);
@@ -865,7 +866,7 @@ __global__ __launch_bounds__(256) void logprobs_backward_kernel(LogprobGradArgs 
   series = __builtin_fmaf(l * series, 1.0f / 4, 1.0f);
   series = __builtin_fmaf(l * series, 1.0f / 3, 1.0f);
   series = __builtin_fmaf(l * series, 1.0f / 2, 1.0f);
-  const float taken = p * __builtin_fmaf(B, d, -h * H * inv) + ((onto - G) + (l > -0.25f ? -l * series : 1.0f - p) * G) * inv;
+  const float taken = m != m ? NAN : p * __builtin_fmaf(B, d, -hH * inv) + ((onto - G) + (l > -0.25f ? -l * series : 1.0f - p) * G) * inv;
   if constexpr (NT > 64) __syncthreads();
 #pragma unroll
   for (int u = 0; u < kUnroll; ++u) {

@@ -66,3 +66,33 @@ def test_finite_masks_of_whole_stretches(rows, V, kind):
             for r in range(some):
                 want, err = R.logprobs_grad(values[r], T, tokens[r], g[r].astype(np.float64), 0.0 if d_h is None else float(h[r]))
                 R.check(got[r], want, R.rounded(err, want, kind), (rows, V, kind, T, r))
+
+
+@pytest.mark.parametrize("kind", list(KIND))
+@pytest.mark.parametrize("V", [5, 600, 1025, 9000, 40000])
+def test_gradient_without_an_entropy_term_does_not_look_at_the_entropy(V, kind):
+    """Where h is 0 or not given, whatever the statistics hold for H: the same bits.  A marked row keeps its mark."""
+    rng = np.random.default_rng(V)
+    x = rng.normal(0, 2.5, (8, V))
+    x[2, :V // 2] = -np.inf
+    x[3, V // 2] = np.nan
+    x[4] = -np.inf
+    buf, view, values = place(x, kind)
+    tokens = dev(rng.integers(0, V, (8, 2)).astype(np.int32))
+    g = dev(rng.normal(0, 1, (8, 2)).astype(np.float32))
+    stats = run_logprobs(view, kind, V, V, 1.0)["stats"]
+    zero = torch.zeros(8, device=DEV)
+    some = zero.clone()
+    some[0] = 0.5        # (a row that does look)
+    want = {}
+    for H in (None, float("nan"), float("inf"), -1e38):
+        s = stats.clone()
+        if H is not None:
+            s[1:, 2] = H
+        for name, h in (("none", None), ("zero", zero), ("some", some)):
+            grad = torch.full((8, V), JUNK, dtype=KIND[kind][1], device=DEV)
+            run_backward(view, kind, V, V, 1.0, s, tokens, g, h, grad, V)
+            got = host(grad)
+            assert np.isnan(got[3]).all() and np.isfinite(np.delete(got, 3, axis=0)).all(), (V, kind, H, name)
+            assert np.array_equal(got, want.setdefault(name, got), equal_nan=True), (V, kind, H, name)
+    assert np.array_equal(want["none"], want["zero"], equal_nan=True)
