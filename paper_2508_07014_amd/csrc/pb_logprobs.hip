@@ -852,21 +852,26 @@ __global__ __launch_bounds__(256) void logprobs_backward_kernel(LogprobGradArgs 
     const float d = fmaxf(__builtin_fmaf(x - m, c, -log2s), -1000.0f);
     return exp2_fast(d) * __builtin_fmaf(B, d, A);
   };
-  float onto = g;  // what the given token takes, listed once or several times
+  float onto = g, rest = 0.0f;  // what the given token takes, listed once or several times, and what the others do
   if (a.n_tokens > 1 && a.grad_logp) {
     onto = 0.0f;
-    for (int k = 0; k < a.n_tokens; ++k)
-      if (__builtin_amdgcn_readlane(given, k) == given) onto += __int_as_float(__builtin_amdgcn_readlane(__float_as_int(g), k));
+    for (int k = 0; k < a.n_tokens; ++k) {
+      const float gk = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(g), k));
+      const bool same = __builtin_amdgcn_readlane(given, k) == given;
+      onto += same ? gk : 0.0f;
+      rest += same ? 0.0f : gk;
+    }
   }
-  // (onto - p G as (onto - G) + (1 - p) G: where p is near 1 the difference would have the rounding of 1, and 1 - p = 1 - e^l comes from
-  // its series, the next term l^6 / 5040 of it)
+  // (onto - p G as (1 - p) onto - p rest: the difference would have the rounding of onto where p is near 1, and of G where p is small and
+  // little falls onto the token; and 1 - p = 1 - e^l comes from its series where p is near 1, the next term l^6 / 5040 of it)
   const float l = __builtin_fmaf(given_x - m, inv, -logs), d = fmaxf(__builtin_fmaf(given_x - m, c, -log2s), -1000.0f), p = exp2_fast(d);
   float series = __builtin_fmaf(l, 1.0f / 6, 1.0f);
   series = __builtin_fmaf(l * series, 1.0f / 5, 1.0f);
   series = __builtin_fmaf(l * series, 1.0f / 4, 1.0f);
   series = __builtin_fmaf(l * series, 1.0f / 3, 1.0f);
   series = __builtin_fmaf(l * series, 1.0f / 2, 1.0f);
-  const float taken = m != m ? NAN : p * __builtin_fmaf(B, d, -hH * inv) + ((onto - G) + (l > -0.25f ? -l * series : 1.0f - p) * G) * inv;
+  const float not_p = l > -0.25f ? -l * series : 1.0f - p;
+  const float taken = m != m ? NAN : p * __builtin_fmaf(B, d, -hH * inv) + __builtin_fmaf(-p, rest, not_p * onto) * inv;
   if constexpr (NT > 64) __syncthreads();
 #pragma unroll
   for (int u = 0; u < kUnroll; ++u) {

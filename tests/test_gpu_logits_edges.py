@@ -96,3 +96,51 @@ def test_gradient_without_an_entropy_term_does_not_look_at_the_entropy(V, kind):
             assert np.isnan(got[3]).all() and np.isfinite(np.delete(got, 3, axis=0)).all(), (V, kind, H, name)
             assert np.array_equal(got, want.setdefault(name, got), equal_nan=True), (V, kind, H, name)
     assert np.array_equal(want["none"], want["zero"], equal_nan=True)
+
+
+def listed_gradient(x, T, tokens, g):
+    """(gradient, bound on its error before the last rounding) of sum g log p(t): on a token t that takes `onto`, the sum of its
+    own g, and leaves `rest`, that of the others, ((1 - p) onto - p rest) / T.  Neither term is a difference of larger ones, so the
+    error is p's, of either term its own: of 1 - p the log-prob's times p and a few roundings of itself, of onto and rest one
+    rounding a term of the sum; 10 U for the products and exponentials."""
+    V = len(x)
+    inside = (tokens >= 0) & (tokens < V)
+    lp, marked = R.row_log_probs(x, T)
+    if marked or not (g[inside] != 0).any() or x.max() == -np.inf:
+        return np.full(V, np.nan if marked and (g[inside] != 0).any() else 0.0), np.zeros(V)
+    p, e, M = np.exp(lp), R.lp_error(x, lp, T), len(g)
+    not_p = np.where(lp > -0.5, -np.expm1(lp), 1 - p)
+    onto, size = np.zeros(V), np.zeros(V)
+    np.add.at(onto, tokens[inside], g[inside])
+    np.add.at(size, tokens[inside], np.abs(g[inside]))
+    rest, others = g[inside].sum() - onto, np.abs(g[inside]).sum() - size
+    for t in set(tokens[inside]):      # (without the rounding of that difference)
+        rest[t], others[t] = g[inside & (tokens != t)].sum(), np.abs(g[inside & (tokens != t)]).sum()
+    grad = (not_p * onto - p * rest) / T
+    return grad, (size * (not_p * (M + 10) * R.U + p * (e + 4 * R.U)) + p * others * (e + (M + 10) * R.U)) / T
+
+
+@pytest.mark.parametrize("kind", list(KIND))
+@pytest.mark.parametrize("V", [2, 7, 129, 1025, 9000, 40000])
+def test_gradients_on_listed_tokens_of_little_weight(V, kind):
+    """Tokens whose own g is 0, or small, beside others of weight: what they get is -p times the others' sum, however small p is;
+    the same where the row is sure of a token, listed or not."""
+    rng = np.random.default_rng(V)
+    for M in (2, 3, 17, 64):
+        rows = 12
+        x = rng.normal(0, 4, (rows, V))
+        x[rows // 2:, rng.integers(0, V)] += 25.0
+        buf, view, values = place(x, kind)
+        tokens = tokens_of(rng, values, M)
+        tokens[::2, 0] = values[::2].argmax(axis=1)
+        g = rng.choice([0.0, 0.0, 1e-6, -1e-9, 1.0, -1.0, 100.0], (rows, M)).astype(np.float32)
+        g[0], g[0, 0] = 0.0, 1.0
+        g[1], g[1, 1] = 0.0, -1.0
+        for T in (1.0, 0.7):
+            grad = torch.full((rows, V), JUNK, dtype=KIND[kind][1], device=DEV)
+            stats = run_logprobs(view, kind, V, V, T)["stats"]
+            run_backward(view, kind, V, V, T, stats, dev(tokens.astype(np.int32)), dev(g), None, grad, V)
+            got = host(grad)
+            for r in range(rows):
+                want, err = listed_gradient(values[r], T, tokens[r], g[r].astype(np.float64))
+                R.check(got[r], want, R.rounded(err, want, kind), (V, kind, M, T, r))
