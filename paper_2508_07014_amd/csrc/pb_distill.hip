@@ -219,6 +219,7 @@ struct List {   // the same in every lane
   float Q;      // sum of q and rest
   int any;      // there is something to learn from
 };
+__device__ __forceinline__ double mass_from(double log_q) { return log_q == INFINITY ? NAN : exp(log_q); }  // (+inf: marked)
 template <typename E, bool TAIL>
 __device__ __forceinline__ List load_list(const DistillArgs& a, int64_t r, const Row<E>& row, int lane, Entry& e) {
   e = Entry{-1, 0.0f, -INFINITY, 0.0};
@@ -233,7 +234,7 @@ __device__ __forceinline__ List load_list(const DistillArgs& a, int64_t r, const
   }
   List l;
   if constexpr (TAIL) {
-    e.q = e.log_q == INFINITY ? NAN : exp(e.log_q);
+    e.q = mass_from(e.log_q);
     const double sum = wave_sum(e.q), left = 1.0 - sum;
     l.rest = left < 0x1p-20 ? 0.0 : left;  // (NaN stays)
     l.any = __ballot(e.token >= 0) != 0 ? 1 : 0;
@@ -600,7 +601,7 @@ __global__ __launch_bounds__(256) void distill_grad_kernel(DistillArgs a, int pa
         e.x = ws.x[r * 64 + tid];
         mass = ws.mass[r * 64 + tid];
         e.log_q = a.logp[r * a.K + tid] - list.shift;
-        if (block == 0) e.q = exp(e.log_q);
+        if (block == 0) e.q = mass_from(e.log_q);
         mine = block == (t < row.head || t >= row.head + row.nv * E::N ? 0 : (t - row.head) / E::N / BLOCK);
       }
     }

@@ -144,3 +144,24 @@ def test_gradients_on_listed_tokens_of_little_weight(V, kind):
             for r in range(rows):
                 want, err = listed_gradient(values[r], T, tokens[r], g[r].astype(np.float64))
                 R.check(got[r], want, R.rounded(err, want, kind), (V, kind, M, T, r))
+
+
+@pytest.mark.parametrize("rows,V", [(6, 40), (6, 9000), (6, 70000), (6, 131072)])
+def test_entries_that_are_no_numbers_where_nothing_is_left(rows, V):
+    """An entry of +inf or NaN where the student leaves nothing to the tokens that are not listed (p' = 0): loss and gradient are
+    NaN, in split rows too.  Without it the loss is +inf where the list leaves something and a number where it does not."""
+    x = torch.full((rows, V), -float("inf"), device=DEV)
+    x[:, :5] = torch.arange(5, device=DEV) / 4.0
+    t = torch.arange(5, dtype=torch.int32, device=DEV).repeat(rows, 1)
+    l = torch.full((rows, 5), -2.0, device=DEV)
+    l[1, 2], l[2, 0], l[3, 4] = float("inf"), float("nan"), float("inf")
+    l[4] = float(np.log(0.2))
+    for tail in (False, True):
+        loss, grad = torch.full((rows,), JUNK, device=DEV), torch.full((rows, V), JUNK, device=DEV)
+        run_distill(x, "f32", V, V, 1.0, t, l, tail, None, loss, grad, V)
+        only = torch.full((rows,), JUNK, device=DEV)
+        run_distill(x, "f32", V, V, 1.0, t, l, tail, None, only, None, 0)
+        got = host(loss)
+        assert np.isnan(got[1:4]).all() and np.isnan(host(only)[1:4]).all() and np.isnan(host(grad)[1:4]).all(), (V, tail)
+        assert np.isfinite(got[4]) and np.isfinite(host(grad)[[0, 4, 5]]).all()
+        assert (got[[0, 5]] == np.inf).all() if tail else np.isfinite(got[[0, 5]]).all()
