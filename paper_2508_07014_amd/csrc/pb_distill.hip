@@ -11,7 +11,7 @@ namespace {
 // Sums of exponentials: every term is e = exp2(d), d = x c - rc with c = log2(e) / T and the reference rc = m c, m the largest
 // element that the lane has seen (a reference below the maximum would add its distance to the rounding of d).  d is rounded
 // once; what rc itself was rounded by is the same for all terms of the lane and is made up for at the end (wave_part).
-// Elements below -kFar / c are masks of a lowest value: nothing beside any ordinary logit.  With LISTED a second sum, X,
+// Elements below -far (see kFar) are masks of a lowest value: nothing beside any ordinary logit.  With LISTED a second sum, X,
 // takes the terms of listed tokens, which S then lacks.
 // (S, X) seen from a reference that lies `apart` = rc - new rc higher:
 template <bool LISTED>

@@ -19,14 +19,16 @@ struct LogitRows {
   int32_t all_rows;    // of the call, of which these are a slice: what decides whether rows are split
   float inv_temp;      // 1 / T
   float c;             // log2(e) / T
-  float far;           // logits further from 0 than this: see kFar
+  float far;           // logits below -far are masks: see kFar
 };
-// Elements further than kFar / c from 0: there x c is too coarse for the differences between them, and a row's sums are
-// formed from (x - max) c instead.
+// Rows whose maximum m lies further than kFar / c from 0, |m c| > kFar as rounded: there x c is too coarse for the differences
+// between elements, and a row's sums are formed from (x - m) c instead.  Elements below -far are left out of the sums of other
+// rows, so far lies beyond every m that |m c| <= kFar takes, whatever c and the product are rounded by (6e-8 each).
 constexpr float kFar = 1048576.0f;
+constexpr double kBeyond = 1.0 + 1e-6;
 inline LogitRows logit_rows(const void* x, int64_t stride, int32_t rows, int32_t V, float temperature) {
   const double c = 1.44269504088896340736 / temperature;
-  return LogitRows{x, stride, rows, V, rows, static_cast<float>(1.0 / temperature), static_cast<float>(c), static_cast<float>(kFar / c)};
+  return LogitRows{x, stride, rows, V, rows, static_cast<float>(1.0 / temperature), static_cast<float>(c), static_cast<float>(kBeyond * kFar / c)};
 }
 
 struct LogprobArgs {

@@ -18,7 +18,7 @@ constexpr int kGroups = 256;          // parts of a row whose maxima bound the a
 // logarithm: log(P + S) = log1p((P - 1) + S), so that what lies beside a likely token is not rounded to its unit (entropies of
 // such rows: errors of 5e-6 without, 1e-7 with it); where less than an eighth of the maximum's term lies beside it, that batch is
 // summed once more without it.  d is rounded once; what rc was rounded by is the same for all terms and comes off a wave's sums.
-// Elements below -kFar / c are masks of a lowest value: nothing beside any ordinary logit.
+// Elements below -far (see kFar) are masks of a lowest value: nothing beside any ordinary logit.
 struct Sums {
   float m = -INFINITY, thr, rc = 0.0f, P = 0.0f, S = 0.0f, X = 0.0f;
   int at = -1;  // first vector of the batch that P is the sum of; -1: the edge

@@ -165,3 +165,43 @@ def test_entries_that_are_no_numbers_where_nothing_is_left(rows, V):
         assert np.isnan(got[1:4]).all() and np.isnan(host(only)[1:4]).all() and np.isnan(host(grad)[1:4]).all(), (V, tail)
         assert np.isfinite(got[4]) and np.isfinite(host(grad)[[0, 4, 5]]).all()
         assert (got[[0, 5]] == np.inf).all() if tail else np.isfinite(got[[0, 5]]).all()
+
+
+# (type, temperature, a): at -a, or just beside it, lies the line past which rows are summed from the differences to their maximum
+FAR = [("f32", 1.0, 726817.5), ("f32", 1.4426950408889634, 1048576.0), ("bf16", 1.4426950408889634, 1048576.0),
+       ("f16", 4096 / 1048576 * 1.4426950408889634, 4096.0), ("bf16", 1.4426950408889634 / 8192, 128.0)]
+
+
+@pytest.mark.parametrize("kind,T,a", FAR)
+@pytest.mark.parametrize("V", [1, 5, 40, 1025, 9000, 131072])
+def test_rows_on_the_line_of_far_logits(V, kind, T, a):
+    """Rows whose maximum is -2^20 T ln 2 exactly, as far from 0 as a row is summed in one pass, or the next number on either side:
+    equal throughout, half of them, one token ahead of others that are as far."""
+    T = float(np.float32(T))
+    step = {"f32": 2.0 ** -23, "f16": 2.0 ** -10, "bf16": 2.0 ** -7}[kind]
+    rng = np.random.default_rng(V)
+    x = np.full((9, V), -np.inf)
+    for r in range(9):
+        m = -a * [1.0, 1.0 + step, 1.0 - step / 2][r // 3]
+        if r % 3 == 0:
+            x[r] = m
+        elif r % 3 == 1:
+            x[r] = np.where(rng.random(V) < 0.5, m, m - a * step * rng.integers(1, 4, V))
+            x[r, rng.integers(0, V)] = m
+        else:
+            x[r] = np.where(rng.random(V) < 0.5, -np.inf, m - 3 * a * step)
+            x[r, rng.integers(0, V)] = m
+    buf, view, values = place(x, kind)
+    tokens = tokens_of(rng, values, 2)
+    o = run_logprobs(view, kind, V, V, T, dev(tokens.astype(np.int32)), min(V, 3))
+    check_logprobs(o, values, T, tokens, min(V, 3), (V, kind, T))
+    t = np.stack([rng.permutation(V)[:min(V, 3)] for _ in range(9)])
+    l = np.log(rng.dirichlet(np.ones(min(V, 3) + 1), 9)[:, :-1]).astype(np.float32)
+    for tail in (False, True):
+        loss, grad = torch.full((9,), JUNK, device=DEV), torch.full((9, V), JUNK, dtype=KIND[kind][1], device=DEV)
+        run_distill(view, kind, V, V, T, dev(t.astype(np.int32)), dev(l), tail, None, loss, grad, V)
+        got, got_loss = host(grad), host(loss)
+        for r in range(9):
+            want, gr, e, eg = R.distill(values[r], T, t[r], l[r].astype(np.float64), tail, 1.0)
+            R.check(got_loss[r], want, e * (1 + 2 ** -20) + R.U * abs(want) + 1e-37, (V, kind, T, tail, r, "loss"))
+            R.check(got[r], gr, R.rounded(eg, gr, kind), (V, kind, T, tail, r, "grad"))
