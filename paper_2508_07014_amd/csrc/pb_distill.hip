@@ -216,7 +216,7 @@ struct Entry {
 struct List {   // the same in every lane
   double rest;  // what the entries leave of 1
   double shift; // log q = l - shift
-  float Q;      // sum of q and rest
+  double Q;     // sum of q and rest
   int any;      // there is something to learn from
 };
 __device__ __forceinline__ double mass_from(double log_q) { return log_q == INFINITY ? NAN : exp(log_q); }  // (+inf: marked)
@@ -238,7 +238,7 @@ __device__ __forceinline__ List load_list(const DistillArgs& a, int64_t r, const
     const double sum = wave_sum(e.q), left = 1.0 - sum;
     l.rest = left < 0x1p-20 ? 0.0 : left;  // (NaN stays)
     l.any = __ballot(e.token >= 0) != 0 ? 1 : 0;
-    l.Q = l.rest > 0.0 ? 1.0f : static_cast<float>(sum);
+    l.Q = l.rest > 0.0 ? 1.0 : sum;  // (NaN stays)
     l.shift = 0.0;
   } else {
     const float top = wave_max(static_cast<float>(e.log_q));
@@ -246,7 +246,7 @@ __device__ __forceinline__ List load_list(const DistillArgs& a, int64_t r, const
     const double part = e.token >= 0 ? exp(e.log_q - (l.any ? top : 0.0f)) : 0.0, sum = wave_sum(part);
     l.rest = 0.0;
     l.shift = top + log_64(sum);
-    l.Q = sum == sum ? 1.0f : NAN;
+    l.Q = sum == sum ? 1.0 : NAN;
     e.log_q -= l.shift;
     e.q = part * over_64(sum);
   }
@@ -356,7 +356,7 @@ __global__ __launch_bounds__(NT == 64 ? 256 : NT) void distill_kernel(DistillArg
     if (tid == 0) s_edge[sub] = 0;
   }
   Entry e{-1, 0.0f, 0.0, 0.0};
-  List list{0.0, 0.0, 0.0f, 0};
+  List list{0.0, 0.0, 0.0, 0};
   double mass = 0.0;
   if (lister) {
     list = load_list<E, TAIL>(a, r, row, tid & 63, e);

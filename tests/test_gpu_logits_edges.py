@@ -205,3 +205,35 @@ def test_rows_on_the_line_of_far_logits(V, kind, T, a):
             want, gr, e, eg = R.distill(values[r], T, t[r], l[r].astype(np.float64), tail, 1.0)
             R.check(got_loss[r], want, e * (1 + 2 ** -20) + R.U * abs(want) + 1e-37, (V, kind, T, tail, r, "loss"))
             R.check(got[r], gr, R.rounded(eg, gr, kind), (V, kind, T, tail, r, "grad"))
+
+
+def near_certain(rng, V, kind):
+    """Six rows with all but 1e-3 .. 1e-8 of their mass on one token; (rows, their values, the tokens, the others' terms seen from
+    the token's, their sums, the bounds on those, relative)."""
+    x = np.where(rng.random((6, V)) < 30.0 / V, rng.uniform(-21, -10, (6, V)), -np.inf)
+    at = np.array([0, V - 1, *rng.integers(0, V, 4)])
+    x[np.arange(6), at] = np.array([0.0, 3.0, -2.0, 0.0, 5.5, 0.0])
+    buf, view, values = place(x, kind)
+    d = values - values.max(axis=1, keepdims=True)
+    e = np.where(np.arange(V) == at[:, None], 0.0, np.exp(d))
+    far = np.abs(np.where(np.isfinite(d), d, 0.0)).max(axis=1)
+    return view, values, at, e, e.sum(axis=1), R.U * (R.chain(V) + 20 + 8 * far)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [5, 40, 1025, 9000, 70001, 131072])
+def test_small_gradient_of_a_list_that_leaves_next_to_nothing(V, kind):
+    """One entry of q = 1 - 5e-7, whose rest counts as 0, and a student that is as sure of it: the gradient q p - q on it, -q R / (1 + R),
+    is as near relative to itself as R is.  (The loss is q (l + log(1 + R)).)"""
+    rng = np.random.default_rng(V)
+    view, values, at, e, R_, off = near_certain(rng, V, kind)
+    l = np.array([-5e-7, -1e-7, -9e-7, -3e-8, 2e-7, -6e-7], np.float32)
+    loss, grad = torch.full((6,), JUNK, device=DEV), torch.full((6, V), JUNK, dtype=KIND[kind][1], device=DEV)
+    run_distill(view, kind, V, V, 1.0, dev(at[:, None].astype(np.int32)), dev(l[:, None]), True, None, loss, grad, V)
+    for r in range(6):
+        q = np.exp(np.float64(l[r]))
+        small = np.log1p(R_[r])
+        R.check(host(loss)[r], q * (l[r] + small), q * small * off[r] + R.U * abs(q * (l[r] + small)) + 1e-13, (V, kind, r, "loss"))
+        want = q * e[r] / (1 + R_[r])
+        want[at[r]] = -q * R_[r] / (1 + R_[r])
+        R.check(host(grad)[r], want, np.abs(want) * (off[r] + R.HALF_STEP[kind]) + 1e-14 + R.TINY[kind], (V, kind, r, "grad"))
