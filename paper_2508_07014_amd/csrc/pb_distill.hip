@@ -134,8 +134,7 @@ __device__ __forceinline__ Part join_lanes(const Part& p, float c) {
 struct RowSums {  // the same in every thread of the row
   float m;        // maximum, -inf for a row of nothing but -inf
   float base;     // m, 0 for such a row
-  float S, X;     // the sums, d = (x - base) c
-  double all;     // both sums
+  double S, all;  // the sum without the listed tokens, and the whole one, d = (x - base) c; 1 + a little, if so, in 64 bits
   bool bad;       // the row holds a NaN or +inf
 };
 // The row from its waves' parts (`lds`: NT / 64 of them).
@@ -158,9 +157,8 @@ __device__ __forceinline__ RowSums join_waves(Part p, int tid, float c, Part* ld
     }
     p = Part{uniform_f(p.m), uniform_f(p.S), uniform_f(p.X), uniform_i(p.one)};
   }
-  const Part w = whole(p);
-  RowSums r{p.m, p.m == -INFINITY ? 0.0f : p.m, w.S, w.X, (p.one != 0 ? 1.0 : 0.0) + (static_cast<double>(p.S) + p.X), false};
-  r.bad = r.S != r.S || r.X != r.X || r.m == INFINITY;
+  RowSums r{p.m, p.m == -INFINITY ? 0.0f : p.m, (p.one == 1 ? 1.0 : 0.0) + p.S, (p.one != 0 ? 1.0 : 0.0) + (static_cast<double>(p.S) + p.X), false};
+  r.bad = r.all != r.all || r.m == INFINITY;
   return r;
 }
 

@@ -237,3 +237,40 @@ def test_small_gradient_of_a_list_that_leaves_next_to_nothing(V, kind):
         want = q * e[r] / (1 + R_[r])
         want[at[r]] = -q * R_[r] / (1 + R_[r])
         R.check(host(grad)[r], want, np.abs(want) * (off[r] + R.HALF_STEP[kind]) + 1e-14 + R.TINY[kind], (V, kind, r, "grad"))
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [40, 1025, 9000, 70001, 131072])
+def test_small_losses_of_a_student_sure_of_a_token_not_listed(V, kind):
+    """Teacher and student leave all but 1e-8 or so to the tokens that are not listed, the student to one of them: log p' =
+    -log(1 + L / (1 + S)) with L and S the sums of the listed and of the other tokens beside that one, and the gradient's share
+    q' / p' - 1, are as near as L is, not as 1 is."""
+    rng = np.random.default_rng(V)
+    view, values, at, e, R_, off = near_certain(rng, V, kind)
+    t, l = np.zeros((6, 2), int), np.zeros((6, 2), np.float32)
+    for r in range(6):
+        some = np.flatnonzero(e[r] > 0)
+        t[r] = rng.choice(some, 2, replace=False)
+        l[r] = np.log(e[r][t[r]]) + rng.normal(0, 1, 2)
+    loss, grad = torch.full((6,), JUNK, device=DEV), torch.full((6, V), JUNK, dtype=KIND[kind][1], device=DEV)
+    run_distill(view, kind, V, V, 1.0, dev(t.astype(np.int32)), dev(l), True, None, loss, grad, V)
+    for r in range(6):
+        where = (V, kind, r)
+        q = np.exp(l[r].astype(np.float64))
+        terms = np.where(np.arange(V) == at[r], 1.0, e[r])
+        L, S = e[r][t[r]].sum(), R_[r] - e[r][t[r]].sum()
+        rest, log_rest = 1 - q.sum(), np.log1p(-q.sum())
+        lp = np.log(e[r][t[r]]) - np.log1p(R_[r])
+        if rest < 0.5:
+            continue
+        log_p = -np.log1p(L / (1 + S))
+        want = (q * (l[r] - lp)).sum() + rest * (log_rest - log_p)
+        bound = (q * off[r]).sum() + L * off[r] + R.U * abs(want) + 1e-13
+        R.check(host(loss)[r], want, bound, where + ("loss",))
+        share = q.sum() - rest * np.expm1(-log_p)      # 1 - q' / p', q' = 1 - sum q, 1 / p' = 1 + L / (1 + S)
+        p = terms / (1 + R_[r])
+        g = p * share
+        g[t[r]] = p[t[r]] - q
+        err = p * (abs(share) * off[r] + L * off[r] + 1e-13)
+        err[t[r]] = (p[t[r]] + q) * off[r]
+        R.check(host(grad)[r], g, R.rounded(err, g, kind), where + ("grad",))
