@@ -24,11 +24,9 @@ struct Sums {
   int at = -1;  // first vector of the batch that P is the sum of; -1: the edge
   __device__ __forceinline__ explicit Sums(float far) : thr(-far) {}
 };
-// (S, X) seen from a reference that lies `apart` = rc - new rc higher.  From further than 2^1000 below nothing is left of either (a
-// wave of nothing but masks of a lowest value beside an ordinary one: apart S would pass the fp32 range, and X be 0 times that).
+// (S, X) seen from a reference that lies `apart` = rc - new rc higher.
 template <bool ENT>
 __device__ __forceinline__ void rebase(float& S, float& X, float apart) {
-  apart = fmaxf(apart, -1000.0f);
   const float f = exp2_fast(apart);  // (may be infinite where the sums are 0)
   if constexpr (ENT) X = S == 0.0f ? 0.0f : f * __builtin_fmaf(apart, S, X);
   S = S == 0.0f ? 0.0f : f * S;
@@ -71,6 +69,10 @@ struct __align__(16) Part {
   float m, P, S, X;
 };
 __device__ __forceinline__ float whole(float P) { return __float_as_int(P) < 0 ? 1.0f - P : P; }
+// How far sums seen from m are to move: from below 2^-1000 nothing is left of them.  (A part of nothing but masks of a lowest value
+// beside an ordinary one: apart S would pass the fp32 range, and X be 0 times that.  Lanes that lie so far apart inside a wave
+// are summed again, see wave_part; the clamp there cost 16384 x 2049 bf16 2 %.)
+__device__ __forceinline__ float parted(float m, float from, float c) { return fmaxf((m - from) * c, -1000.0f); }
 // The parts that the lanes of a wave hold as one, the same in every lane: one lane's P stays apart.  `apart(m)`: how far the
 // lane's sums are to move to be seen from m.
 template <bool ENT, typename Apart>
@@ -89,7 +91,7 @@ __device__ __forceinline__ Part join_lanes(float m, float P, float S, float X, A
 }
 template <bool ENT>
 __device__ __forceinline__ Part join_parts(const Part& q, float c) {
-  return join_lanes<ENT>(q.m, q.P, q.S, q.X, [&](float m) { return (q.m - m) * c; });
+  return join_lanes<ENT>(q.m, q.P, q.S, q.X, [&](float m) { return parted(q.m, m, c); });
 }
 // A batch of a lane is of U vectors, `stride` apart, all below `end`.  again(add) goes over the wave's elements a second time, where
 // the maximum lies far from 0.
@@ -137,7 +139,7 @@ __device__ __forceinline__ Part join_set(const Part (&q)[W], float c) {
     const bool top = !taken && q[w].m == p.m;
     float S = q[w].S + (top ? 0.0f : whole(q[w].P)), X = q[w].X;
     float S1 = S, X1 = X;
-    rebase<ENT>(S1, X1, (q[w].m - p.m) * c);
+    rebase<ENT>(S1, X1, parted(q[w].m, p.m, c));
     p.P = top ? q[w].P : p.P;
     p.S += top ? S : S1;
     p.X += top ? X : X1;
