@@ -132,7 +132,7 @@ __device__ __forceinline__ Part join_lanes(const Part& p, float c) {
 }
 
 struct RowSums {  // the same in every thread of the row
-  float m;        // maximum, -inf for a row of nothing but -inf
+  float m;        // maximum, -inf for a row of nothing but -inf, NaN for a marked one
   float base;     // m, 0 for such a row
   double S, all;  // the sum without the listed tokens, and the whole one, d = (x - base) c; 1 + a little, if so, in 64 bits
   bool bad;       // the row holds a NaN or +inf
@@ -157,8 +157,12 @@ __device__ __forceinline__ RowSums join_waves(Part p, int tid, float c, Part* ld
     }
     p = Part{uniform_f(p.m), uniform_f(p.S), uniform_f(p.X), uniform_i(p.one)};
   }
-  RowSums r{p.m, p.m == -INFINITY ? 0.0f : p.m, (p.one == 1 ? 1.0 : 0.0) + p.S, (p.one != 0 ? 1.0 : 0.0) + (static_cast<double>(p.S) + p.X), false};
-  r.bad = r.all != r.all || r.m == INFINITY;
+  RowSums r;
+  r.S = (p.one == 1 ? 1.0 : 0.0) + p.S;
+  r.all = (p.one != 0 ? 1.0 : 0.0) + (static_cast<double>(p.S) + p.X);
+  r.bad = r.all != r.all || p.m == INFINITY;
+  r.m = r.bad ? NAN : p.m;  // (a row of NaN and -inf has -inf for its largest number, and is no row of nothing but -inf)
+  r.base = r.m == -INFINITY ? 0.0f : r.m;
   return r;
 }
 

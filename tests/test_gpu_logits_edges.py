@@ -274,3 +274,35 @@ def test_small_losses_of_a_student_sure_of_a_token_not_listed(V, kind):
         err = p * (abs(share) * off[r] + L * off[r] + 1e-13)
         err[t[r]] = (p[t[r]] + q) * off[r]
         R.check(host(grad)[r], g, R.rounded(err, g, kind), where + ("grad",))
+
+
+@pytest.mark.parametrize("kind", list(KIND))
+@pytest.mark.parametrize("V", [1, 2, 7, 40, 1025, 9000, 40000, 70000, 131072])
+def test_rows_without_a_number(V, kind):
+    """Rows of nothing but NaN, or of NaN and -inf, are marked throughout, their gradients too: they are no rows of nothing but -inf.
+    A row of weight 0 has gradient 0 all the same."""
+    rng = np.random.default_rng(V)
+    x = np.full((6, V), np.nan)
+    x[1, rng.random(V) < 0.5] = -np.inf
+    x[2] = -np.inf
+    x[3] = -np.inf
+    x[3, rng.integers(0, V)] = np.nan
+    x[4] = rng.normal(0, 1, V)
+    buf, view, values = place(x, kind)
+    marked = np.isnan(values).any(axis=1)
+    tokens = rng.integers(0, V, (6, 2))
+    d_tokens = dev(tokens.astype(np.int32))
+    o = run_logprobs(view, kind, V, V, 1.0, d_tokens, min(V, 3))
+    check_logprobs(o, values, 1.0, tokens, min(V, 3), (V, kind))
+    grad = torch.full((6, V), JUNK, dtype=KIND[kind][1], device=DEV)
+    run_backward(view, kind, V, V, 1.0, o["stats"], d_tokens, torch.ones((6, 2), device=DEV), None, grad, V)
+    assert np.array_equal(np.isnan(host(grad)), np.tile(marked[:, None], (1, V))) and not host(grad)[2].any()
+    l = torch.full((6, 2), -1.0, device=DEV)
+    w = np.array([1.0, -2.0, 1.0, 0.5, 1.0, 0.0], np.float32)
+    for tail in (False, True):
+        loss = torch.full((6,), JUNK, device=DEV)
+        run_distill(view, kind, V, V, 1.0, d_tokens, l, tail, dev(w), loss, grad, V)
+        got = host(grad)
+        assert np.array_equal(np.isnan(host(loss)), marked), (V, kind, tail)
+        assert np.array_equal(np.isnan(got), np.tile((marked & (w != 0))[:, None], (1, V))), (V, kind, tail)
+        assert not got[2].any() and not got[5].any(), (V, kind, tail)
