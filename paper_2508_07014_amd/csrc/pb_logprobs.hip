@@ -353,6 +353,12 @@ __device__ __forceinline__ void push_equal(const Row<E>& row, int tid, unsigned 
   }
 }
 
+// (x - base) / T - log of the sum.  The difference is taken of halves, which changes no bit of it: of the largest and the lowest value
+// of a type it passes the fp32 range, where the quotient need not.
+__device__ __forceinline__ float log_prob(float x, float base, float inv, float logs) {
+  return __builtin_fmaf(__builtin_fmaf(x, 0.5f, -0.5f * base), 2.0f * inv, -logs);
+}
+
 struct TopOut {
   int n;
   float base, inv, logs;
@@ -360,7 +366,7 @@ struct TopOut {
   float* logp;
   __device__ __forceinline__ void write(int rank, u64 k) const {
     tokens[rank] = static_cast<int32_t>(~static_cast<unsigned>(k));
-    logp[rank] = __builtin_fmaf(ukey_val(static_cast<unsigned>(k >> 32)) - base, inv, -logs);
+    logp[rank] = log_prob(ukey_val(static_cast<unsigned>(k >> 32)), base, inv, logs);
   }
 };
 // The list in order.  Where there were more candidates than it holds (the largest values crowd in a few groups): one
@@ -537,7 +543,7 @@ __device__ __forceinline__ void write_alternatives(const Row<E>& row, int tid, c
 
 // What a row's sums say, and the scores of the given tokens.
 __device__ __forceinline__ void write_scores(const LogprobArgs& a, int64_t r, int tid, const RowSums& sums, int given, float given_x) {
-  if (tid < a.n_tokens) a.logp[r * a.n_tokens + tid] = given < 0 ? NAN : __builtin_fmaf(given_x - sums.base, a.in.inv_temp, -sums.log_s);
+  if (tid < a.n_tokens) a.logp[r * a.n_tokens + tid] = given < 0 ? NAN : log_prob(given_x, sums.base, a.in.inv_temp, sums.log_s);
   if (tid == 0) {
     if (a.entropy) a.entropy[r] = sums.H;
     if (a.stats) {

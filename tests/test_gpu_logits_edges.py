@@ -306,3 +306,23 @@ def test_rows_without_a_number(V, kind):
         assert np.array_equal(np.isnan(host(loss)), marked), (V, kind, tail)
         assert np.array_equal(np.isnan(got), np.tile((marked & (w != 0))[:, None], (1, V))), (V, kind, tail)
         assert not got[2].any() and not got[5].any(), (V, kind, tail)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [2, 40, 1025, 9000, 131072])
+def test_log_probs_whose_difference_passes_the_range(V, kind):
+    """The type's largest and lowest value in one row: x - max is -6.8e38, which fp32 does not hold, (x - max) / T is a number for T
+    from 2 on, and so are the log-probs."""
+    rng = np.random.default_rng(V)
+    x = rng.normal(0, 2, (4, V))
+    x[:, 0] = -R.LARGEST[kind]
+    x[0, V - 1], x[1, V - 1], x[2, V // 2] = R.LARGEST[kind], 2e38, 1e38
+    x[3] = np.where(rng.random(V) < 0.5, R.LARGEST[kind], -R.LARGEST[kind])
+    tokens = np.stack([np.zeros(4, int), np.full(4, V - 1), rng.integers(0, V, 4)], axis=1)
+    for T in (1.0, 2.5, 100.0, 1e4):
+        T = float(np.float32(T))
+        buf, view, values = place(x, kind)
+        o = run_logprobs(view, kind, V, V, T, dev(tokens.astype(np.int32)), min(V, 64))
+        check_logprobs(o, values, T, tokens, min(V, 64), (V, kind, T))
+        for r in range(4):
+            assert np.isfinite(host(o["logp"][r])).all() or T == 1.0
