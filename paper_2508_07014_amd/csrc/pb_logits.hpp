@@ -80,12 +80,18 @@ inline RowSplit row_split(int vectors, int32_t rows, int few) {
   return RowSplit{(vectors + 64 * each - 1) / (64 * each), each};
 }
 
-// Which calls are split.  us, split / a workgroup a row: log-probs with entropy and 5 alternatives, bf16, V = 50000, 1 row 8.6 / 8.1,
-// 32 rows 9.5 / 8.5; V = 80000, 1 row 8.4 / 9.6, 16 rows 9.2 / 10.0, 48 rows 11.4 / 10.3; V = 131072, 1 row 8.7 / 12.3, 64 rows 12.9 /
-// 13.7, 120 rows 16.0 / 14.0; V = 250000, 1 row 8.8 / 20, 120 rows 20.9 / 22.3; V = 393216, 240 rows 43 / 42; fp32 V = 50000, 1 row
-// 8.5 / 8.6, 16 rows 9.4 / 8.9; bf16 without alternatives, V = 80000, 16 rows 8.8 / 8.0 and V = 131072, 64 rows 9.3 / 11.1.
-// Distillation, bf16: V = 32001, 16 rows 7.9 / 8.4, 64 rows 9.4 / 8.7; V = 50000, 32 rows 9.1 / 10.9, 64 rows 11.4 / 11.1; V = 131072,
-// 64 rows 14.7 / 22, 160 rows 25.5 / 24.7; fp32 V = 131072, 256 rows 66 / 78.
+// Which calls are split.  us, split / a workgroup a row.  Log-probs with entropy and 5 alternatives, bf16: V = 80000, 1 row 7.6 / 9.3, 12
+// rows 8.3 / 9.7, 32 rows 9.7 / 9.9; V = 131072, 1 row 8.0 / 12.2, 72 rows 12.5 / 13.4, 120 rows 15.3 / 13.7; V = 250000, 1 row 8.3 / 19.8,
+// 138 rows 21.5 / 22.4; V = 393216, 120 rows 25.7 / 34.8, 218 rows 39.4 / 38.0.  fp32: V = 80000, 1 row 7.7 / 10.0, 32 rows 9.8 / 11.6; V =
+// 131072, 72 rows 14.7 / 16.2, 120 rows 18.2 / 17.0; V = 250000, 138 rows 31.7 / 37.6; V = 393216, 218 rows 64.0 / 62.9.  Without
+// alternatives, bf16: V = 80000, 32 rows 6.9 / 7.7; V = 131072, 72 rows 9.0 / 10.8, 120 rows 11.4 / 11.2.  So the line (12 rows at V = 80000, 72
+// at 131072, 138 at 250000, 218 at 393216) lies within 4 % of where both are equal or on the side of one workgroup a row; short of
+// it, V = 80000 with 13 to 32 rows, a split would be 2 to 15 % faster.  At V = 50000 it was slower (bf16 1 row 8.6 / 8.1, 32 rows 9.5 / 8.5; fp32
+// 16 rows 9.4 / 8.9).
+// Distillation, 32 entries and the rest, bf16: V = 32001, 16 rows 8.9 / 9.2, 40 rows 9.5 / 9.5, 64 rows 10.3 / 9.6; V = 50000, 32 rows 10.0 /
+// 11.7, 62 rows 12.0 / 11.9, 100 rows 12.8 / 12.5; V = 131072, 64 rows 14.9 / 24.1, 160 rows 25.4 / 26.5, 200 rows 30.0 / 30.1.  fp32: V =
+// 131072, 64 rows 19.0 / 33.6, 327 rows 84.8 / 123; on the short side the line is drawn for 16 bits, and a workgroup a row would be
+// faster: V = 16001, 40 rows 9.1 / 7.5; V = 32001, 16 rows 9.4 / 9.1, 80 rows 12.1 / 10.7.
 inline RowSplit split_logprobs(int vectors, int32_t rows, int32_t V) {
   return rows <= (V - 70000) / 800 && rows <= V / 1800 ? row_split(vectors, rows, 80) : RowSplit{0, 0};  // (the parts are to bound 64 alternatives)
 }
