@@ -21,14 +21,13 @@ struct LogitRows {
   float c;             // log2(e) / T
   float far;           // logits below -far are masks: see kFar
 };
-// Rows whose maximum m lies further than kFar / c from 0, |m c| > kFar as rounded: there x c is too coarse for the differences
-// between elements, and a row's sums are formed from (x - m) c instead.  Elements below -far are left out of the sums of other
-// rows, so far lies beyond every m that |m c| <= kFar takes, whatever c and the product are rounded by (6e-8 each).
+// Where a wave's largest element m lies further than kFar / c from 0, |m c| > kFar, x c is too coarse for the differences between
+// elements, and its sums are formed from (x - m) c instead.  Other waves leave out the elements below -far, masks of a lowest
+// value.  Those lie as far again below the line, so that beside any m above it they are nothing (2^-kFar of its term).
 constexpr float kFar = 1048576.0f;
-constexpr double kBeyond = 1.0 + 1e-6;
 inline LogitRows logit_rows(const void* x, int64_t stride, int32_t rows, int32_t V, float temperature) {
   const double c = 1.44269504088896340736 / temperature;
-  return LogitRows{x, stride, rows, V, rows, static_cast<float>(1.0 / temperature), static_cast<float>(c), static_cast<float>(kBeyond * kFar / c)};
+  return LogitRows{x, stride, rows, V, rows, static_cast<float>(1.0 / temperature), static_cast<float>(c), static_cast<float>(2 * kFar / c)};
 }
 
 struct LogprobArgs {

@@ -326,3 +326,32 @@ def test_log_probs_whose_difference_passes_the_range(V, kind):
         check_logprobs(o, values, T, tokens, min(V, 64), (V, kind, T))
         for r in range(4):
             assert np.isfinite(host(o["logp"][r])).all() or T == 1.0
+
+
+@pytest.mark.parametrize("T", [1.0, 1.4426950408889634, 0.03, 1e-4, 500.0])
+@pytest.mark.parametrize("V", [3, 40, 300, 1025, 9000, 131072])
+def test_rows_across_the_line_of_far_logits(V, T):
+    """Rows with ordinary logits on either side of -2^20 T ln 2: a lane that has none above it counts beside lanes that have."""
+    T = float(np.float32(T))
+    rng = np.random.default_rng(V)
+    a = 1048576 * T / 1.4426950408889634
+    x = -a + T * rng.uniform(-6, 6, (8, V))
+    x[2:4] = -a + T * rng.uniform(-6, 0, (2, V))
+    x[4:6] = -a + T * np.where(rng.random((2, V)) < 0.9, rng.uniform(-30, -1, (2, V)), rng.uniform(0, 3, (2, V)))
+    x[6] = -a - T * 4.0
+    x[6, V // 2] = -a + T
+    x[7] = -2 * a + T * rng.uniform(-6, 6, V)
+    buf, view, values = place(x, "f32")
+    tokens = tokens_of(rng, values, 3)
+    o = run_logprobs(view, "f32", V, V, T, dev(tokens.astype(np.int32)), min(V, 9))
+    check_logprobs(o, values, T, tokens, min(V, 9), (V, T))
+    t = np.stack([rng.permutation(V)[:3] for _ in range(8)])
+    l = np.log(rng.dirichlet(np.ones(4), 8)[:, :-1]).astype(np.float32)
+    for tail in (False, True):
+        loss, grad = torch.full((8,), JUNK, device=DEV), torch.full((8, V), JUNK, device=DEV)
+        run_distill(view, "f32", V, V, T, dev(t.astype(np.int32)), dev(l), tail, None, loss, grad, V)
+        got, got_loss = host(grad), host(loss)
+        for r in range(8):
+            want, gr, e, eg = R.distill(values[r], T, t[r], l[r].astype(np.float64), tail, 1.0)
+            R.check(got_loss[r], want, e * (1 + 2 ** -20) + R.U * abs(want) + 1e-37, (V, T, tail, r, "loss"))
+            R.check(got[r], gr, R.rounded(eg, gr, "f32"), (V, T, tail, r, "grad"))
