@@ -312,8 +312,9 @@ int pb_fuse_step_beam_forest(const pb_forest* forest, const float* d_logp, int64
  *   at any alignment of its elements.  Log-probs of the decoders above are logits as well.  Arithmetic on rows is fp32 for
  *   every type, on a teacher's list and its loss fp64.  With z_j = x_j / temperature:
  *     log p(t) = z_t - log sum_j exp(z_j),   p_j = exp(log p(j)),   H = -sum_j p_j log p(j)   (p_j = 0 adds nothing).
- *   A logit of -inf is a masked token (p = 0).  A row of nothing but -inf has log p = -inf, H = 0 and gradient 0.  A row
- *   that holds a NaN or +inf is marked: NaN scores, -1 ids.  A token id outside [0, V) is absent: see each call.
+ *   A logit of -inf is a masked token (p = 0); a p below the smallest normal fp32 number counts as 0 in sums and
+ *   gradients.  A row of nothing but -inf has log p = -inf, H = 0 and gradient 0.  A row that holds a NaN or +inf is
+ *   marked: NaN scores, -1 ids, a gradient of NaN.  A token id outside [0, V) is absent: see each call.
  *   The calls take the device that is current and d_logits lies on; they allocate nothing, synchronise nothing and may be
  *   captured.  `d_workspace`: device memory of at least ..._workspace_bytes(...) bytes, 16-byte aligned, used only during
  *   the call (contents before and after mean nothing; calls that may overlap in time, two graphs among them, need one each);

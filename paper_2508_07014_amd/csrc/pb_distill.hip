@@ -330,7 +330,7 @@ __device__ __forceinline__ void reload(v4u (&held)[HELD]) {
 // at work are in between).  With TAIL the tokens that are not listed have a sum of their own, so that little mass does not
 // vanish in a difference: bits in LDS say which elements are listed, and most vectors have none.  Bound by HBM where rows are
 // long (8192 x 32001 bf16, 32 entries: 192 us, 5.5 TB/s), by the 600 instructions a row needs anyway where they are short (13686 x
-// 129 bf16: 16.7 us), by latency where they are few (500 x 1025 fp32: 4.5 us).
+// 129 bf16: 15.4 us with 4 entries, 16.8 with 64), by latency where they are few (500 x 1025 fp32: 4.4 us).
 template <typename E, int NT, int HELD, bool TAIL, bool STREAM>
 __global__ __launch_bounds__(NT == 64 ? 256 : NT) void distill_kernel(DistillArgs a, int mark_bytes) {
   constexpr int ROWS = NT == 64 ? 4 : 1;
@@ -474,7 +474,7 @@ constexpr int kGradUnroll = 4;
 // Few long rows, and rows too long for the registers of a workgroup: every wave takes 64 * `each` vectors of a row and
 // leaves their part of the sums in the workspace, and one more wave the list's (with the student's logits on it, since the
 // gradient may take the logits' place); the second kernel joins the parts and writes the gradient.  64 x 131072 bf16, 64 entries:
-// 7.1 us, the list's wave being the last to end, and 7.4 us.
+// 7.3 us, the list's wave being the last to end, and 8.0 us.
 struct DistillSpace {
   float4* parts;  // [rows, parts]
   List* lists;    // [rows]

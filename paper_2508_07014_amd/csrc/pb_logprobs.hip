@@ -392,7 +392,7 @@ __device__ __forceinline__ void write_list(const Row<E>& row, int tid, float edg
     if (NT == 64 && count > 64) {
       // Few groups for so many alternatives, or fewer tokens left by a mask: a bound of the candidates themselves (the lower
       // tokens among those that equal it), and those that reach it to the front.  (10 x 192 fp32, 56 alternatives: 15.9 us with
-      // each of the 192 compared with all, 8.3 so; 9024 x 769 bf16, 95 % masked, 48 of them: 174 and 64.)
+      // each of the 192 compared with all, 7.2 so; 9024 x 769 bf16, 95 % masked, 48 of them: 174 and 58.)
       constexpr int PER = list_size<E::N>() / 64;
       u64 held[PER];
       unsigned key[PER], place[PER];
@@ -480,7 +480,7 @@ __device__ __forceinline__ void write_alternatives(const Row<E>& row, int tid, c
   // Elements equal to the bound count in the order of their tokens.  Where many groups have it for their maximum (masked
   // rows with fewer tokens left than alternatives wanted, flat rows), only those up to vector `last` are wanted: the groups
   // above it are not enough by `need`, and the `need` lowest vectors in which a group has its maximum hold so many.
-  // (68 x 129 fp16, 95 % of it masked, one alternative: 14.7 us with all of a masked row's elements ranked, 5.7 so; the bound of
+  // (68 x 129 fp16, 95 % of it masked, one alternative: 14.7 us with all of a masked row's elements ranked, 4.6 so; the bound of
   // an ordinary row admits up to some 5 groups more than n and goes without.)
   int last = INT_MAX;
   if (b != 0u && how_many(key, b) > out.n + 8) {
@@ -569,7 +569,7 @@ __device__ __forceinline__ int load_given(const LogprobArgs& a, int64_t r, const
 
 // One row, by a workgroup, or (NT == 64: rows of up to kWaveVectors vectors) by a wave, four in a workgroup.  Large calls of long
 // rows are bound by HBM (8192 x 32001 bf16, 32 alternatives: 100 us, 5.2 TB/s), those of short rows by vector instructions (16000 x
-// 1025 fp32 with entropy: 12.8 us, 5.2 TB/s; with 5 alternatives 17.5 us, 500 instructions a wave, 83 % of the cycles), small ones
+// 1025 fp32 with entropy: 12.5 us, 5.2 TB/s; with 5 alternatives 17.2 us, 509 instructions a wave, 80 % of the cycles), small ones
 // by the launch and one row's chain of loads and reductions (32 x 1024 fp32: 3.1 us).
 static_assert(kWaveVectors == 2 * 64 * kUnroll, "a wave requests its row in two batches");
 template <typename E, int NT, bool ENT, bool TOP>
@@ -663,7 +663,7 @@ __global__ __launch_bounds__(NT == 64 ? 256 : NT) void logprobs_kernel(LogprobAr
 // Few long rows: every wave takes 64 * `each` vectors of a row and leaves their part in the workspace, with the largest element
 // of the vectors, its token and the largest of the others; a workgroup per row joins them.  The parts' largest elements bound
 // the alternatives as the lanes' do above, and are candidates themselves; the few parts with a second one are read again.
-// Both are bound by latency: 1 x 131072 bf16, 20 alternatives, 3.3 us and 5.4 us.
+// Both are bound by latency: 1 x 131072 bf16, 20 alternatives, 3.5 us and 5.6 us.
 struct PartRecord {
   Part sums;
   float top, second;
