@@ -569,7 +569,7 @@ __device__ __forceinline__ int load_given(const LogprobArgs& a, int64_t r, const
 
 // One row, by a workgroup, or (NT == 64: rows of up to kWaveVectors vectors) by a wave, four in a workgroup.  Large calls of long
 // rows are bound by HBM (8192 x 32001 bf16, 32 alternatives: 100 us, 5.2 TB/s), those of short rows by vector instructions (16000 x
-// 1025 fp32 with entropy: 12.5 us, 5.2 TB/s; with 5 alternatives 17.2 us, 509 instructions a wave, 80 % of the cycles), small ones
+// 1025 fp32 with entropy: 12.5 us, 5.2 TB/s; with 5 alternatives 17.2 us, 509 instructions a wave, 79 - 80 % of the cycles), small ones
 // by the launch and one row's chain of loads and reductions (32 x 1024 fp32: 3.1 us).
 static_assert(kWaveVectors == 2 * 64 * kUnroll, "a wave requests its row in two batches");
 template <typename E, int NT, bool ENT, bool TOP>
