@@ -1,0 +1,384 @@
+"""Timed workloads around a student that learns from a teacher's alternatives and then drafts for it.
+
+Its input side: tokens become rows of a table, scaled, and the table's gradient is the sum of the gradients on a token's
+places.  The end of its training step: the norm over all gradients, and their clipping.  What it is for: it drafts some tokens
+a sequence, the teacher's rows for all of them come out of one pass, and each token is accepted or the first refused one drawn
+again so that what is emitted has the teacher's distribution.  Tokens fall like a power of their rank, rows of logits have the
+tails of trained models, in three types, now and then at a round stride; lists of tokens have absent ones, and drafts end early.
+"""
+import math
+
+import torch
+
+own = False  # whether run() makes the framework's calls, or computes the same in elementary operations
+
+DEV = "cuda:0"
+TYPES = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+SIZE = {"f32": 4, "f16": 2, "bf16": 2}
+
+
+def listed():
+    check = dict(op="verify", pad=0, temp=1.0, draft_temp=1.0, drafted=True, ragged=False, masked=0.0)
+    look = dict(op="embed", pad=0, absent=0.0)
+    back = dict(op="embed_grad", pad=0, absent=0.0)
+    return [
+        # The smallest call: one sequence, four tokens drafted by a small head.
+        dict(check, name="verify_step", type="f32", sequences=1, drafts=4, V=1024),
+        # A serving step: 32 sequences, some with fewer drafted tokens, the blank makes rows odd.
+        dict(check, name="verify_serve", type="bf16", sequences=32, drafts=4, V=32001, temp=0.75, draft_temp=0.75, ragged=True),
+        # Tokens proposed without a distribution (continuations of a phrase that has begun) in a constrained search.
+        dict(check, name="verify_phrases", type="f16", sequences=64, drafts=8, V=50000, drafted=False, masked=0.9),
+        # One sequence of a language model's vocabulary, eight tokens: few rows, all of them long.
+        dict(check, name="verify_one", type="bf16", sequences=1, drafts=8, V=131072),
+        # The largest: a full serving batch over the same vocabulary.
+        dict(check, name="verify_batch", type="bf16", sequences=128, drafts=8, V=131072, draft_temp=1.25),
+        # A decoding step looks up what 64 hypotheses have just emitted.
+        dict(look, name="embed_step", table="bf16", out="bf16", tokens=64, V=1024, D=640, scale=1.0),
+        # A training batch from a table held in fp32, scaled by the root of the width.
+        dict(look, name="embed_batch", table="f32", out="bf16", tokens=32768, V=131072, D=2048, scale=math.sqrt(2048)),
+        # The table of a small prediction network: short transcripts, odd vocabulary.
+        dict(back, name="embed_grad_labels", table="f32", grad="f32", tokens=500, V=1025, D=640, scale=1.0, absent=0.2),
+        # A student's batch, gradients in bf16 on a table in fp32.
+        dict(back, name="embed_grad_batch", table="f32", grad="bf16", tokens=16384, V=32001, D=1024, scale=32.0),
+        # A long batch over a language model's vocabulary.
+        dict(back, name="embed_grad_large", table="bf16", grad="bf16", tokens=131072, V=131072, D=2048, scale=1.0),
+        # A small student's gradients: some tens of tensors, all fp32.
+        dict(op="clip", name="clip_small", tensors=30, elements=2000000, mix="f32", packed=False),
+        # A large one's: hundreds, matrices in bf16 and norms in fp32, from one element to tens of millions.
+        dict(op="clip", name="clip_large", tensors=400, elements=400000000, mix="bf16", packed=False),
+    ]
+
+
+MOST_BYTES = 128 * 17 * 131072 * 2  # of a drawn verification
+MOST_GRADS = 400000000
+
+
+def _log_int(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def _vocabulary(rng):
+    V, shape = _log_int(rng, 128, 131072), rng.random()
+    if shape < 0.35:
+        return max(128, V // 64 * 64)      # a tokenizer's round size ...
+    return max(128, V // 64 * 64) + 1 if shape < 0.7 else V  # ... and with the blank
+
+
+def draw(rng):
+    op = rng.choice(["verify", "verify", "verify", "embed", "embed_grad", "embed_grad", "clip"])
+    if op == "clip":
+        mix = rng.choice(["f32", "f16", "bf16"])
+        return dict(op=op, tensors=_log_int(rng, 1, 600), elements=_log_int(rng, 600, MOST_GRADS * 2 // SIZE[mix]), mix=mix,
+                    packed=rng.random() < 0.3)
+    V = _vocabulary(rng)
+    if op == "verify":
+        c = dict(op=op, type=rng.choice(["f32", "f16", "bf16"]), V=V, drafts=rng.choice([0, 1, 2, 3, 4, 5, 8, 15]))
+        c["temp"] = rng.choice([0.5, 0.75, 1.0, 1.0, 1.25])
+        c["draft_temp"] = rng.choice([c["temp"], c["temp"], 1.0])
+        c["pad"] = -V % 64 if rng.random() < 0.3 else 0
+        c["drafted"], c["ragged"] = rng.random() < 0.7, rng.random() < 0.4
+        c["masked"] = rng.choice([0.0, 0.0, 0.5, 0.95])
+        most = MOST_BYTES // ((2 * c["drafts"] + 1) * (V + c["pad"]) * SIZE[c["type"]])
+        c["sequences"] = max(1, min(_log_int(rng, 1, 256), most))
+        return c
+    c = dict(op=op, V=V, D=_log_int(rng, 16, 4096), scale=rng.choice([1.0, 0.5, 11.3125]), table=rng.choice(["f32", "f16", "bf16"]))
+    if rng.random() < 0.6:
+        c["D"] = (c["D"] + 15) // 16 * 16
+    c["pad"] = -c["D"] % 64 if rng.random() < 0.3 else 0
+    c["absent"] = rng.choice([0.0, 0.0, 0.1, 0.5])
+    c["out" if op == "embed" else "grad"] = rng.choice([c["table"], c["table"], "bf16", "f32"])
+    most = (1 << 28) // c["D"]
+    c["tokens"] = max(1, min(_log_int(rng, 1, 131072), most))
+    if op == "embed_grad":
+        c["V"] = max(1, min(V, most))
+    return c
+
+
+# ---- inputs --------------------------------------------------------------------------------------------------------
+
+def _gen(seed, k):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(int(seed) * 1000003 + k)
+    return g
+
+
+def _tokens(g, n, V, absent):
+    """Tokens whose share falls like 1 / rank, the ranks strewn over the vocabulary; some places hold none."""
+    rank = torch.exp(torch.rand(n, generator=g, device=DEV, dtype=torch.float64) * math.log(V + 1)).long() - 1
+    t = (rank.clamp(0, V - 1) * 7919 + 13) % V if V % 7919 else rank.clamp(0, V - 1)
+    return torch.where(torch.rand(n, generator=g, device=DEV) < absent, torch.full_like(t, -1), t).to(torch.int32)
+
+
+def _sequences(c):
+    step = max(1, (1 << 26) // ((c["drafts"] + 1) * c["V"]))
+    return [slice(i, min(c["sequences"], i + step)) for i in range(0, c["sequences"], step)]
+
+
+def _verify_inputs(c, seed):
+    """Rows as heads leave them (see above), the draft's the target's with noise; drafted tokens drawn from the draft's rows.  A
+    masked target bars tokens at random, and one row in 97 as a whole; a draft without rows proposes a likely token."""
+    B, n, V, kind, g = c["sequences"], c["drafts"], c["V"], TYPES[c["type"]], _gen(seed, 1)
+    target = torch.zeros((B, n + 1, V + c["pad"]), dtype=kind, device=DEV)
+    draft = torch.zeros((B, n, V + c["pad"]), dtype=kind, device=DEV) if c["drafted"] else None
+    tokens = torch.zeros((B, n), dtype=torch.int32, device=DEV)
+    for s in _sequences(c):
+        b = s.stop - s.start
+        x = torch.randn((b, n + 1, V), generator=g, device=DEV)
+        x *= 2.5 * torch.randn((b, n + 1, V), generator=g, device=DEV).abs()
+        ahead = torch.randint(0, V, (b, n + 1, 1), generator=g, device=DEV)
+        x.scatter_add_(2, ahead, 8.0 * (torch.rand((b, n + 1, 1), generator=g, device=DEV) < 0.6))
+        if n:
+            y = (0.9 * x[:, :n] + 0.7 * torch.randn((b, n, V), generator=g, device=DEV)).to(kind)
+            race = -torch.log(torch.rand((b, n, V), generator=g, device=DEV).clamp(min=1e-30))
+            tokens[s] = (torch.softmax(y.float() / c["draft_temp"], dim=2) / race).argmax(dim=2).to(torch.int32)
+            if c["drafted"]:
+                draft[s, :, :V] = y
+        if c["masked"]:
+            barred = torch.rand((b, n + 1, V), generator=g, device=DEV) < c["masked"]
+            if n:  # (a drafted token is one of those that are left, most of the time)
+                barred[:, :n].scatter_(2, tokens[s].long()[:, :, None], torch.rand((b, n, 1), generator=g, device=DEV) < 0.1)
+            row = torch.arange(s.start * (n + 1), s.stop * (n + 1), device=DEV).view(b, n + 1, 1)
+            x.masked_fill_(barred | (row % 97 == 41), -math.inf)
+        target[s, :, :V] = x.to(kind)
+    if c["ragged"] and n:
+        size = torch.randint(0, n + 1, (B, 1), generator=g, device=DEV)
+        tokens[torch.arange(n, device=DEV)[None, :] >= size] = -1
+    return {"case": c, "target": target, "draft": draft, "tokens": tokens, "numbers": torch.rand((B, n + 1), generator=g, device=DEV)}
+
+
+def _clip_inputs(c, seed):
+    """Tensors from one element on, sizes spread over their logarithm; gradients of different weights have different scales."""
+    g, n = _gen(seed, 4), c["tensors"]
+    spread = torch.Generator().manual_seed(c["tensors"] * 31 + 7)  # (the sizes belong to the case)
+    part = torch.exp(torch.rand(n, generator=spread, dtype=torch.float64) * math.log(max(2.0, c["elements"] / n)))
+    part *= max(0.0, c["elements"] - n) / float(part.sum())
+    sizes = [1 + int(v) for v in part]
+    types = [TYPES["f32"] if c["mix"] != "f32" and k % 3 == 2 and sizes[k] < 1 << 16 else TYPES[c["mix"]] for k in range(n)]
+    grads = [(torch.randn(s, generator=g, device=DEV) * (1e-3 * 2.0 ** (k % 7))).to(t) for k, (s, t) in enumerate(zip(sizes, types))]
+    return {"case": c, "grads": grads, "max_norm": 1.0 if seed % 3 else 0.125}
+
+
+def _inputs(c, seed):
+    if c["op"] == "verify":
+        return _verify_inputs(c, seed)
+    if c["op"] == "clip":
+        return _clip_inputs(c, seed)
+    d = {"case": c, "tokens": _tokens(_gen(seed, 2), c["tokens"], c["V"], c["absent"]), "scale": torch.tensor(c["scale"]).item()}
+    g = _gen(seed, 3)
+    if c["op"] == "embed":
+        d["table"] = (torch.randn((c["V"], c["D"] + c["pad"]), generator=g, device=DEV) * 0.02).to(TYPES[c["table"]])[:, :c["D"]]
+    else:
+        d["grad"] = (torch.randn((c["tokens"], c["D"] + c["pad"]), generator=g, device=DEV) * 1e-2).to(TYPES[c["grad"]])[:, :c["D"]]
+    return d
+
+
+def _flat(tensors, step):
+    """A buffer per type with room for the tensors one after the other (each at a multiple of `step` elements), and the places."""
+    ends, at = {}, []
+    for x in tensors:
+        at.append(ends.get(x.dtype, 0))
+        ends[x.dtype] = at[-1] + -(-x.numel() // step) * step
+    flat = {t: torch.zeros(n, dtype=t, device=DEV) for t, n in ends.items()}
+    return flat, [flat[x.dtype][a:a + x.numel()] for x, a in zip(tensors, at)]
+
+
+def prepare(c, seed):
+    d = _inputs(c, seed)
+    d["stream"] = int(torch.cuda.current_stream().cuda_stream)
+    d["workspace"] = None
+    if c["op"] == "verify":
+        shape = (c["sequences"], c["drafts"] + 1)
+        d["emitted"] = torch.empty(shape, dtype=torch.int32, device=DEV)
+        d["accepted"] = torch.empty(c["sequences"], dtype=torch.int32, device=DEV)
+        d["logp"] = torch.empty(shape, device=DEV)
+    elif c["op"] == "embed":
+        d["out"] = torch.empty((c["tokens"], c["D"]), dtype=TYPES[c["out"]], device=DEV)
+    elif c["op"] == "embed_grad":
+        d["table_grad"] = torch.empty((c["V"], c["D"]), dtype=TYPES[c["table"]], device=DEV)
+    else:
+        d["norm"] = torch.empty(1, device=DEV)
+        d["flat"], d["clipped"] = _flat(d["grads"], 1 if c["packed"] else 64)
+    return d
+
+
+# ---- one pass ------------------------------------------------------------------------------------------------------
+
+def _softmax(x, temp):
+    """Probabilities and log-probs in 64 bits (drawing among V tokens meets V borders); a row that is -inf throughout: 0, -inf."""
+    m = x.amax(dim=-1, keepdim=True).double()
+    z = (x.double() - torch.where(m == -math.inf, torch.zeros_like(m), m)) / temp
+    e = z.exp()
+    total = e.sum(dim=-1, keepdim=True)
+    some = total > 0
+    return e / torch.where(some, total, torch.ones_like(total)), z - torch.where(some, total, torch.ones_like(total)).log()
+
+
+def _plain_verify(d):
+    c, tokens, n = d["case"], d["tokens"], d["case"]["drafts"]
+    B, V, u = c["sequences"], c["V"], d["numbers"].double()
+    p, lp = _softmax(d["target"][:, :, :V], c["temp"])
+    there = (tokens >= 0).int().cumprod(dim=1)
+    at = tokens.clamp(min=0).long()[:, :, None]
+    q = None
+    if n and c["drafted"]:
+        q, _ = _softmax(d["draft"][:, :, :V], c["draft_temp"])
+    q_at = torch.ones((B, n), dtype=torch.float64, device=DEV) if q is None else q.gather(2, at)[:, :, 0]
+    takes = (u[:, :n] * q_at < p[:, :n].gather(2, at)[:, :, 0]).int() * there
+    k = takes.cumprod(dim=1).sum(dim=1)                       # accepted tokens
+    refused = (k < there.sum(dim=1))[:, None]
+    rows, near = torch.arange(B, device=DEV), k.clamp(max=max(0, n - 1))
+    r = p[rows, k]
+    if n:
+        barred = q[rows, near] if q is not None else torch.zeros((B, V), dtype=torch.float64, device=DEV).scatter_(1, at[rows, near], 1.0)
+        rest = (r - torch.where(refused, barred, torch.zeros_like(barred))).clamp(min=0.0)
+        r = torch.where(rest.sum(dim=1, keepdim=True) > 0, rest, r)
+    upto = r.cumsum(dim=1)
+    drawn = (upto <= u[:, n:] * upto[:, -1:]).sum(dim=1)
+    drawn = torch.where(upto[:, -1] > 0, drawn, torch.full_like(drawn, -1))
+    place = torch.arange(n + 1, device=DEV)[None, :]
+    out = torch.nn.functional.pad(tokens, (0, 1), value=-1).long()
+    out = torch.where(place < k[:, None], out, torch.where(place == k[:, None], drawn[:, None], torch.full_like(out, -1)))
+    logp = lp.gather(2, out.clamp(min=0)[:, :, None])[:, :, 0]
+    logp = torch.where(out >= 0, logp, torch.full_like(logp, math.nan)).float()
+    return {"tokens": out.to(torch.int32), "accepted": k.to(torch.int32), "logp": logp}
+
+
+def _plain_embed(d):
+    c, t = d["case"], d["tokens"].long()
+    rows = d["table"][t.clamp(min=0)].float() * d["scale"]
+    return {"out": torch.where((t >= 0)[:, None], rows, torch.zeros_like(rows)).to(TYPES[c["out"]])}
+
+
+def _plain_embed_grad(d):
+    c, t = d["case"], d["tokens"].long()
+    order = torch.argsort(torch.where(t >= 0, t, torch.full_like(t, c["V"])), stable=True)  # (sorted, so that the sums have an order)
+    t, g = t[order], d["grad"][order].float()
+    t = torch.where(t >= 0, t, torch.full_like(t, c["V"]))
+    first = torch.searchsorted(t, torch.arange(c["V"] + 1, device=DEV))
+    sums = torch.segment_reduce(g, "sum", offsets=first, axis=0, initial=0.0)
+    return {"table_grad": (sums * d["scale"]).to(TYPES[c["table"]])}
+
+
+def _plain_clip(d):
+    """(Squares are summed in 64 bits: long sums.)"""
+    squares = torch.stack([x.double().square().sum() for x in d["grads"]])
+    norm = squares.sum().sqrt().float()
+    by = torch.where(norm > d["max_norm"], d["max_norm"] / norm, torch.ones_like(norm))
+    for x, place in zip(d["grads"], d["clipped"]):
+        place.copy_(x.float() * by)
+    return {"norm": norm.view(1), **{str(t)[6:]: x for t, x in d["flat"].items()}}
+
+
+PLAIN = {"verify": _plain_verify, "embed": _plain_embed, "embed_grad": _plain_embed_grad, "clip": _plain_clip}
+
+
+def run(d):
+    if not own:
+        return PLAIN[d["case"]["op"]](d)
+    import paper_2508_07014_amd as pb
+    c = d["case"]
+    kind = {"f32": pb.PB_F32, "f16": pb.PB_F16, "bf16": pb.PB_BF16}
+    if c["op"] == "embed":
+        pb.pb_embed_tokens(d["table"], kind[c["table"]], c["D"] + c["pad"], c["V"], c["D"], d["scale"], d["tokens"], c["tokens"], d["out"],
+                           kind[c["out"]], c["D"], d["stream"])
+        return {"out": d["out"]}
+    if d["workspace"] is None:
+        if c["op"] == "verify":
+            size = pb.pb_verify_draft_workspace_bytes(kind[c["type"]], c["sequences"], c["drafts"], c["V"])
+        elif c["op"] == "embed_grad":
+            size = pb.pb_embed_tokens_backward_workspace_bytes(c["tokens"], c["V"], c["D"])
+        else:
+            types = {torch.float32: pb.PB_F32, torch.float16: pb.PB_F16, torch.bfloat16: pb.PB_BF16}
+            about = [x.numel() for x in d["grads"]], [types[x.dtype] for x in d["grads"]]
+            d["set"], d["clipped_set"] = pb.pb_tensors_build(d["grads"], *about), pb.pb_tensors_build(d["clipped"], *about)
+            size = pb.pb_grad_norm_workspace_bytes(d["set"])
+        d["workspace"] = torch.empty(max(16, size), dtype=torch.uint8, device=DEV)
+    ws = d["workspace"]
+    if c["op"] == "clip":
+        pb.pb_grad_norm(d["set"], d["norm"], ws, ws.numel(), d["stream"])
+        pb.pb_grad_clip(d["set"], d["norm"], d["max_norm"], d["clipped_set"], d["stream"])
+        return {"norm": d["norm"], **{str(t)[6:]: x for t, x in d["flat"].items()}}
+    if c["op"] == "embed_grad":
+        pb.pb_embed_tokens_backward(d["grad"], kind[c["grad"]], c["D"] + c["pad"], d["tokens"], c["tokens"], c["V"], c["D"], d["scale"], 0,
+                                    d["table_grad"], kind[c["table"]], c["D"], ws, ws.numel(), d["stream"])
+        return {"table_grad": d["table_grad"]}
+    stride, n = c["V"] + c["pad"], c["drafts"]
+    draft = d["draft"] if n else None
+    pb.pb_verify_draft(d["target"], draft, kind[c["type"]], (n + 1) * stride, stride, max(1, n) * stride, stride, c["sequences"], n, c["V"],
+                       c["temp"], c["draft_temp"], d["tokens"] if n else None, d["numbers"], d["emitted"], d["accepted"], d["logp"], ws,
+                       ws.numel(), d["stream"])
+    return {"tokens": d["emitted"], "accepted": d["accepted"], "logp": d["logp"]}
+
+
+def work(c):
+    """Inputs read once, outputs written once (of a table that is looked up, a row a token at most; a gradient is read for the
+    norm, and what clipping reads again is not counted).  A cell of logits: a difference, a product, an exponential, a sum."""
+    if c["op"] == "verify":
+        B, n = float(c["sequences"]), c["drafts"]
+        cells = B * c["V"] * ((2 * n if c["drafted"] else n) + 1)
+        return {"bytes": cells * SIZE[c["type"]] + B * (4 * n + 12 * (n + 1) + 4), "flops": 4 * cells + 8 * B * c["V"]}
+    if c["op"] == "clip":
+        return {"bytes": 2.0 * SIZE[c["mix"]] * c["elements"], "flops": 3.0 * c["elements"]}
+    cells = float(c["tokens"]) * c["D"]
+    if c["op"] == "embed":
+        return {"bytes": min(c["tokens"], c["V"]) * c["D"] * SIZE[c["table"]] + cells * SIZE[c["out"]] + 4 * c["tokens"], "flops": cells}
+    return {"bytes": cells * SIZE[c["grad"]] + float(c["V"]) * c["D"] * SIZE[c["table"]] + 4 * c["tokens"], "flops": cells + float(c["V"]) * c["D"]}
+
+
+# ---- the same in 64 bits, from the definition ----------------------------------------------------------------------
+
+def _exact_sequence(c, d, b):
+    """One sequence, token after token."""
+    V, n, numbers = c["V"], c["drafts"], d["numbers"][b].double().tolist()
+    tokens = d["tokens"][b].tolist()
+    out, logp = [], []
+    for i in range(n + 1):
+        lp = torch.log_softmax(d["target"][b, i, :V].double() / c["temp"], dim=0)
+        lp = torch.where(torch.isnan(lp), torch.full_like(lp, -math.inf), lp)
+        rest = lp.exp()
+        if i < n and tokens[i] >= 0:
+            t = tokens[i]
+            if c["drafted"]:
+                q = torch.log_softmax(d["draft"][b, i, :V].double() / c["draft_temp"], dim=0).exp()
+            else:
+                q = torch.zeros_like(rest)
+                q[t] = 1.0
+            if numbers[i] * float(q[t]) < float(rest[t]):
+                out.append(t)
+                logp.append(float(lp[t]))
+                continue
+            left = torch.relu(rest - q)
+            rest = left if float(left.sum()) > 0 else rest
+        upto = torch.cumsum(rest, dim=0)
+        if float(upto[-1]) > 0:
+            out.append(min(V - 1, int(torch.searchsorted(upto, upto[-1:] * numbers[n], right=True)[0])))
+            logp.append(float(lp[out[-1]]))
+        break
+    return out + [-1] * (n + 1 - len(out)), i, logp + [math.nan] * (n + 1 - len(logp))
+
+
+def exact(c, seed):
+    d = _inputs(c, seed)
+    if c["op"] == "verify":
+        parts = [_exact_sequence(c, d, b) for b in range(c["sequences"])]
+        return {"tokens": torch.tensor([p[0] for p in parts], dtype=torch.int32), "accepted": torch.tensor([p[1] for p in parts], dtype=torch.int32),
+                "logp": torch.tensor([p[2] for p in parts], dtype=torch.float64)}
+    if c["op"] == "clip":
+        norm = math.sqrt(math.fsum(float(torch.dot(x.double(), x.double())) for x in d["grads"]))
+        by = min(1.0, d["max_norm"] / norm)
+        out = {"norm": torch.tensor([norm], dtype=torch.float64)}
+        for kind in dict.fromkeys(x.dtype for x in d["grads"]):
+            some = [torch.nn.functional.pad(x.double() * by, (0, 0 if c["packed"] else -x.numel() % 64)) for x in d["grads"] if x.dtype == kind]
+            out[str(kind)[6:]] = torch.cat(some)
+        return out
+    t, scale = d["tokens"].long(), float(c["scale"])
+    if c["op"] == "embed":
+        out = torch.zeros((c["tokens"], c["D"]), dtype=torch.float64, device=DEV)
+        there = (t >= 0).nonzero()[:, 0]
+        out[there] = d["table"].index_select(0, t[there]).double().mul_(scale)
+        return {"out": out}
+    out = torch.zeros((c["V"] + 1, c["D"]), dtype=torch.float64, device=DEV)
+    for s in range(0, c["tokens"], 16384):
+        some = t[s:s + 16384]
+        out.index_add_(0, some.masked_fill(some < 0, c["V"]), d["grad"][s:s + 16384].double())
+    return {"table_grad": out[:-1] * scale}
