@@ -10,6 +10,7 @@ import math
 
 import torch
 
+NOTHING = 2.0 ** -40  # what a draft leaves of its target counts from here on (two equal rows differ by their roundings)
 own = False  # whether run() makes the framework's calls, or computes the same in elementary operations
 
 DEV = "cuda:0"
@@ -231,7 +232,7 @@ def _plain_verify(d):
     if n:
         barred = q[rows, near] if q is not None else torch.zeros((B, V), dtype=torch.float64, device=DEV).scatter_(1, at[rows, near], 1.0)
         rest = (r - torch.where(refused, barred, torch.zeros_like(barred))).clamp(min=0.0)
-        r = torch.where(rest.sum(dim=1, keepdim=True) > 0, rest, r)
+        r = torch.where(rest.sum(dim=1, keepdim=True) > NOTHING, rest, r)
     upto = r.cumsum(dim=1)
     drawn = (upto <= u[:, n:] * upto[:, -1:]).sum(dim=1)
     drawn = torch.where(upto[:, -1] > 0, drawn, torch.full_like(drawn, -1))
@@ -348,7 +349,7 @@ def _exact_sequence(c, d, b):
                 logp.append(float(lp[t]))
                 continue
             left = torch.relu(rest - q)
-            rest = left if float(left.sum()) > 0 else rest
+            rest = left if float(left.sum()) > NOTHING else rest
         upto = torch.cumsum(rest, dim=0)
         if float(upto[-1]) > 0:
             out.append(min(V - 1, int(torch.searchsorted(upto, upto[-1:] * numbers[n], right=True)[0])))
