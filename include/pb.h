@@ -383,6 +383,84 @@ int pb_distill_topk(const void* d_logits, int32_t dtype, int64_t row_stride, int
                     int64_t workspace_bytes, void* hip_stream);
 
 /*
+ * A student of the teacher whose alternatives pb_distill_topk learns from: what its training step needs around that loss, and
+ * what a small model beside a large one is for.  Not in the paper.  The conventions are those of the calls on rows of logits:
+ * element types enum pb_dtype, strides in elements, any alignment of the elements, the current device, nothing allocated or
+ * synchronised, capturable, `d_workspace` as there, the same bits every time.
+ *
+ * pb_embed_tokens -- rows of a table for tokens:  d_out[i * out_stride + j] = scale * d_table[d_tokens[i] * table_stride + j], j < dim,
+ *   in fp32, rounded once to out_dtype.  A token id outside [0, vocab_size) is absent: its row is 0.
+ * pb_embed_tokens_backward -- the table's gradient from d_grad_out [n_tokens, dim], the gradient on those rows:
+ *     d_grad_table[v * table_stride + j] = scale * sum over i with d_tokens[i] = v of d_grad_out[i * grad_stride + j]
+ *   summed in fp32, by position within 64 places of the order of positions by token and then over those, rounded once to
+ *   table_dtype.  accumulate 0: all vocab_size rows are written, those of tokens that do not occur with 0; accumulate 1: the sum
+ *   is added to what is there, and rows of tokens that do not occur are not touched.  Absent tokens' gradients are not looked at.
+ *   PB_EINVAL: n_tokens < 0, vocab_size < 1, dim < 1, an unknown dtype, a stride below dim, accumulate neither 0 nor 1, a pointer
+ *   that is null but needed or not aligned to its elements, the workspace.  PB_ERANGE: a scale that is not finite.
+ *   PB_EUNSUPPORTED: n_tokens > 2^24, vocab_size > 393216, dim > 65536.  n_tokens == 0: a no-op, but for the gradient that is
+ *   written as 0.  The outputs lie apart from the inputs; d_table may be one matrix with the head that made the logits.
+ */
+int pb_embed_tokens(const void* d_table, int32_t table_dtype, int64_t table_stride, int32_t vocab_size, int32_t dim,
+                    float scale, const int32_t* d_tokens, int32_t n_tokens, void* d_out, int32_t out_dtype,
+                    int64_t out_stride, void* hip_stream);
+int64_t pb_embed_tokens_backward_workspace_bytes(int32_t n_tokens, int32_t vocab_size, int32_t dim);
+int pb_embed_tokens_backward(const void* d_grad_out, int32_t grad_dtype, int64_t grad_stride, const int32_t* d_tokens,
+                             int32_t n_tokens, int32_t vocab_size, int32_t dim, float scale, int32_t accumulate,
+                             void* d_grad_table, int32_t table_dtype, int64_t table_stride, void* d_workspace,
+                             int64_t workspace_bytes, void* hip_stream);
+
+/*
+ * pb_tensors_build -- a set of n >= 1 device buffers (contiguous, sizes[i] >= 0 elements of type dtypes[i]), for instance the
+ *   gradients of a model, as the two calls below take them.  Host-synchronous: a table of their addresses is uploaded to `device`;
+ *   the buffers stay the caller's and have to outlive the calls.  Free with pb_tensors_free (NULL is a no-op) when no call on it
+ *   is under way.  PB_EINVAL: null arguments, n < 1, a negative size, an unknown dtype, a buffer that is null though its size is
+ *   not 0 or not aligned to its elements.  PB_EUNSUPPORTED: a size above 2^40.  PB_EHIP / PB_ENOMEM as in pb_build.
+ * pb_grad_norm -- d_norm[0] = sqrt(sum of x^2 over all elements of all tensors); squares and sums in 64 bits, rounded once to fp32
+ *   (inf above its range; NaN where a tensor holds one).
+ * pb_grad_clip -- x' = x * (max_norm / norm), factor and product each rounded once, where norm = d_norm[0] > max_norm; x' = x where it is not, and where
+ *   it is NaN or +inf (there is no factor: the step is to be skipped).  d_norm is read on the device: pb_grad_norm's, or what
+ *   several devices have made of theirs.  x' goes to the tensors of `out`, a set of the same device, sizes and types whose
+ *   buffers lie apart from those of `grads` or are the same ones; out NULL or grads itself: in place, where nothing is written if nothing is clipped.
+ *   PB_ERANGE: max_norm negative or not finite.  The calls take the device of the set, which must be current.
+ */
+typedef struct pb_tensors pb_tensors; /* opaque; owns its table on the device */
+int pb_tensors_build(const void* const* d_buffers, const int64_t* sizes, const int32_t* dtypes, int32_t n, int32_t device,
+                     pb_tensors** out);
+int pb_tensors_free(pb_tensors* tensors);
+int64_t pb_grad_norm_workspace_bytes(const pb_tensors* grads);
+int pb_grad_norm(const pb_tensors* grads, float* d_norm, void* d_workspace, int64_t workspace_bytes, void* hip_stream);
+int pb_grad_clip(const pb_tensors* grads, const float* d_norm, float max_norm, const pb_tensors* out, void* hip_stream);
+
+/*
+ * pb_verify_draft -- speculative decoding's second half: a small model (or a phrase that has begun) has proposed up to n_draft
+ * tokens t_0, t_1, .. for each sequence, the large one's rows for all of them are there, and what is emitted is to have the
+ * large one's distribution.  Sequence b:
+ *   rows x_i = d_target_logits + b * target_seq_stride + i * target_row_stride, i = 0 .. n_draft, behind token i - 1;
+ *        y_i = d_draft_logits + b * draft_seq_stride + i * draft_row_stride, i < n_draft, that t_i was drawn from
+ *   p_i = softmax(x_i / temperature), q_i = softmax(y_i / draft_temperature); d_draft_logits NULL: q_i is 1 at t_i, 0 elsewhere
+ *   t_i = d_draft_tokens[b, i]; the first id outside [0, V) ends the draft: n tokens (rows behind x_n and y_n-1 are not looked at)
+ *   u_i = d_uniforms[b, i], w = d_uniforms[b, n_draft], numbers in [0, 1) (others count as the nearest such fp32, NaN as 0)
+ *   t_i is accepted if all before it are and u_i q_i(t_i) < p_i(t_i); k = the number of accepted tokens
+ *   then a token is drawn from r = max(p_k - q_k, 0) if k < n, from r = p_n if k = n: the first v with
+ *     sum_{j <= v} r_j > w sum_j r_j, r_v > 0.  Where max(p_k - q_k, 0) sums to no more than 2^-40, r = p_k.
+ * d_accepted[b] = k; d_tokens[b, 0 .. n_draft] = t_0 .. t_k-1, the drawn token, then -1; d_logp (NULL: not wanted) the log p_i of
+ * those tokens, NaN beside -1.  n_draft == 0 draws a token from each row.
+ * Exponentials and sums are in 64 bits, so that a draw from hundreds of thousands of tokens is the definition's; a logit of -inf
+ * has p = 0, as has one that lies 1074 ln 2 T below the largest.  A row of nothing but -inf: p = 0, no token is accepted there, and
+ * none drawn (-1); as a y_i: q = 0.  A row that holds a NaN or +inf accepts nothing; where it decides (x_k, or y_k if k < n) the drawn
+ * token is -1.
+ * PB_EINVAL: as in pb_token_logprobs, n_draft < 0, d_draft_tokens NULL if and only if n_draft > 0, draft rows without drafts, a null
+ *   d_uniforms, d_tokens or d_accepted, a stride below V (where its rows are read).  PB_ERANGE: a temperature outside [1e-4, 1e4].
+ *   PB_EUNSUPPORTED: V > 393216, n_draft > 63.  sequences == 0 is a no-op.  Outputs lie apart from the inputs.
+ */
+int64_t pb_verify_draft_workspace_bytes(int32_t dtype, int32_t sequences, int32_t n_draft, int32_t vocab_size);
+int pb_verify_draft(const void* d_target_logits, const void* d_draft_logits, int32_t dtype, int64_t target_seq_stride,
+                    int64_t target_row_stride, int64_t draft_seq_stride, int64_t draft_row_stride, int32_t sequences,
+                    int32_t n_draft, int32_t vocab_size, float temperature, float draft_temperature,
+                    const int32_t* d_draft_tokens, const float* d_uniforms, int32_t* d_tokens, int32_t* d_accepted,
+                    float* d_logp, void* d_workspace, int64_t workspace_bytes, void* hip_stream);
+
+/*
  * pb_validate -- debug aid (host-side, O(N + V)): bounds-checks every index the kernels follow in the compiled
  * tree -- arc rows tile the arc table and stay inside it, tokens in [0, V) and strictly ascending per row, arc j
  * leads to state j + 1 one level deeper, failure links lead to strictly shallower states, the root row points at

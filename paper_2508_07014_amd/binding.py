@@ -26,7 +26,9 @@ EXPORTS = ["pb_build", "pb_free", "pb_info", "pb_host_arrays", "pb_state_prefix"
            "pb_fuse_frames_ws", "pb_fuse_frames_static", "pb_fuse_step_beam", "pb_forest_build", "pb_forest_free", "pb_score_forest",
            "pb_fuse_step_forest", "pb_fuse_frames_forest", "pb_fuse_step_beam_forest", "pb_validate",
            "pb_validate_states", "pb_strerror", "pb_token_logprobs", "pb_token_logprobs_workspace_bytes",
-           "pb_token_logprobs_backward", "pb_distill_topk", "pb_distill_topk_workspace_bytes"]
+           "pb_token_logprobs_backward", "pb_distill_topk", "pb_distill_topk_workspace_bytes", "pb_embed_tokens",
+           "pb_embed_tokens_backward", "pb_embed_tokens_backward_workspace_bytes", "pb_tensors_build", "pb_tensors_free",
+           "pb_grad_norm", "pb_grad_norm_workspace_bytes", "pb_grad_clip", "pb_verify_draft", "pb_verify_draft_workspace_bytes"]
 
 
 class PbError(RuntimeError):
@@ -61,9 +63,12 @@ HOT = ["pb_score", "pb_fuse_step", "pb_fuse_frames", "pb_fuse_step_select", "pb_
        "pb_fuse_frames_static", "pb_fuse_step_beam", "pb_score_forest", "pb_fuse_step_forest", "pb_fuse_frames_forest",
        "pb_fuse_step_beam_forest"]  # called once per decoding step: they go through _pbcall (see pb_python.cpp)
 ROW_CALLS = ["pb_token_logprobs", "pb_token_logprobs_backward", "pb_distill_topk"]  # the same without a handle
+STUDENT_CALLS = {"pb_embed_tokens": 0, "pb_embed_tokens_backward": 0, "pb_grad_norm": 1, "pb_grad_clip": 1,
+                 "pb_verify_draft": 0}  # and these, with so many handles in front
 
 _lib = None
 _rows = None  # the ROW_CALLS, like _hot
+_student = None  # the STUDENT_CALLS
 _hot = None  # the HOT entry points, taking device buffers as they come and returning a status code
 
 
@@ -148,18 +153,49 @@ def load():
     lib.pb_distill_topk_workspace_bytes.argtypes = [i32, i32, i32, i32]
     lib.pb_distill_topk.restype = C.c_int
     lib.pb_distill_topk.argtypes = [vp, i32, i64, i32, i32, f32, vp, vp, i32, i32, vp, vp, vp, i64, vp, i64, vp]
-    global _hot, _rows
+    lib.pb_embed_tokens.restype = C.c_int
+    lib.pb_embed_tokens.argtypes = [vp, i32, i64, i32, i32, f32, vp, i32, vp, i32, i64, vp]
+    lib.pb_embed_tokens_backward_workspace_bytes.restype = i64
+    lib.pb_embed_tokens_backward_workspace_bytes.argtypes = [i32, i32, i32]
+    lib.pb_embed_tokens_backward.restype = C.c_int
+    lib.pb_embed_tokens_backward.argtypes = [vp, i32, i64, vp, i32, i32, i32, f32, i32, vp, i32, i64, vp, i64, vp]
+    lib.pb_tensors_build.restype = C.c_int
+    lib.pb_tensors_build.argtypes = [C.POINTER(vp), i64p, i32p, i32, i32, C.POINTER(vp)]
+    lib.pb_tensors_free.restype = C.c_int
+    lib.pb_tensors_free.argtypes = [vp]
+    lib.pb_grad_norm_workspace_bytes.restype = i64
+    lib.pb_grad_norm_workspace_bytes.argtypes = [vp]
+    lib.pb_grad_norm.restype = C.c_int
+    lib.pb_grad_norm.argtypes = [vp, vp, vp, i64, vp]
+    lib.pb_grad_clip.restype = C.c_int
+    lib.pb_grad_clip.argtypes = [vp, vp, f32, vp, vp]
+    lib.pb_verify_draft_workspace_bytes.restype = i64
+    lib.pb_verify_draft_workspace_bytes.argtypes = [i32, i32, i32, i32]
+    lib.pb_verify_draft.restype = C.c_int
+    lib.pb_verify_draft.argtypes = [vp, vp, i32, i64, i64, i64, i64, i32, i32, i32, f32, f32, vp, vp, vp, vp, vp, vp, i64, vp]
+    global _hot, _rows, _student
     _hot = _bind_hot(lib)
     _rows = _bind_rows(lib)
+    _student = _bind_student(lib)
     _lib = lib
     return lib
 
 
 def _bind_rows(lib):
-    calls = _CtypesCalls(lib, ROW_CALLS, 0)
+    return _bind_calls(lib, ROW_CALLS, _CtypesCalls(lib, ROW_CALLS, 0))
+
+
+def _bind_student(lib):
+    calls = _CtypesCalls(lib, [])
+    for handles in set(STUDENT_CALLS.values()):
+        vars(calls).update(vars(_CtypesCalls(lib, [n for n, h in STUDENT_CALLS.items() if h == handles], handles)))
+    return _bind_calls(lib, STUDENT_CALLS, calls)
+
+
+def _bind_calls(lib, names, calls):
     try:
         from . import _pbcall
-        for name in ROW_CALLS:
+        for name in names:
             _pbcall.bind(name, C.cast(getattr(lib, name), C.c_void_p).value, getattr(calls, name))
     except (ImportError, ValueError):  # not built (_bind_hot has said so), or built before these calls were there
         return calls
@@ -476,3 +512,87 @@ def pb_distill_topk(d_logits, dtype: int, row_stride: int, rows: int, vocab_size
     _check((_rows or _load_rows()).pb_distill_topk(
         d_logits, dtype, row_stride, rows, vocab_size, temperature, d_teacher_tokens, d_teacher_logp, K, mode, d_row_grads,
         d_loss, d_grad_logits, grad_stride, d_workspace, workspace_bytes, stream), "pb_distill_topk")
+
+
+def _load_student():
+    load()
+    return _student
+
+
+def pb_embed_tokens(d_table, table_dtype: int, table_stride: int, vocab_size: int, dim: int, scale: float, d_tokens,
+                    n_tokens: int, d_out, out_dtype: int, out_stride: int, stream: int = 0):
+    _check((_student or _load_student()).pb_embed_tokens(
+        d_table, table_dtype, table_stride, vocab_size, dim, scale, d_tokens, n_tokens, d_out, out_dtype, out_stride,
+        stream), "pb_embed_tokens")
+
+
+def pb_embed_tokens_backward_workspace_bytes(n_tokens: int, vocab_size: int, dim: int) -> int:
+    return _bytes(int(load().pb_embed_tokens_backward_workspace_bytes(n_tokens, vocab_size, dim)), "pb_embed_tokens_backward_workspace_bytes")
+
+
+def pb_embed_tokens_backward(d_grad_out, grad_dtype: int, grad_stride: int, d_tokens, n_tokens: int, vocab_size: int, dim: int,
+                             scale: float, accumulate: int, d_grad_table, table_dtype: int, table_stride: int, d_workspace,
+                             workspace_bytes: int, stream: int = 0):
+    _check((_student or _load_student()).pb_embed_tokens_backward(
+        d_grad_out, grad_dtype, grad_stride, d_tokens, n_tokens, vocab_size, dim, scale, accumulate, d_grad_table,
+        table_dtype, table_stride, d_workspace, workspace_bytes, stream), "pb_embed_tokens_backward")
+
+
+class Tensors:
+    """Owner of a ``pb_tensors*``; keeps the buffers it was built from alive."""
+
+    def __init__(self, handle: int, buffers):
+        self.handle = handle
+        self.buffers = list(buffers)
+
+    def close(self):
+        if self.handle:
+            load().pb_tensors_free(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def pb_tensors_build(buffers, sizes, dtypes, device: int = 0) -> Tensors:
+    n = len(buffers)
+    if len(sizes) != n or len(dtypes) != n:
+        raise PbError(PB_EINVAL, "pb_tensors_build")
+    ptrs = (C.c_void_p * n)(*[_dptr(b) for b in buffers])
+    out = C.c_void_p()
+    _check(load().pb_tensors_build(ptrs, (C.c_int64 * n)(*sizes), (C.c_int32 * n)(*dtypes), n, device, C.byref(out)), "pb_tensors_build")
+    return Tensors(out.value, buffers)
+
+
+def pb_tensors_free(tensors: Tensors):
+    tensors.close()
+
+
+def pb_grad_norm_workspace_bytes(grads: Tensors) -> int:
+    return _bytes(int(load().pb_grad_norm_workspace_bytes(grads.handle)), "pb_grad_norm_workspace_bytes")
+
+
+def pb_grad_norm(grads: Tensors, d_norm, d_workspace, workspace_bytes: int, stream: int = 0):
+    _check((_student or _load_student()).pb_grad_norm(grads.handle, d_norm, d_workspace, workspace_bytes, stream), "pb_grad_norm")
+
+
+def pb_grad_clip(grads: Tensors, d_norm, max_norm: float, out: Optional[Tensors] = None, stream: int = 0):
+    _check((_student or _load_student()).pb_grad_clip(
+        grads.handle, d_norm, max_norm, None if out is None else out.handle, stream), "pb_grad_clip")
+
+
+def pb_verify_draft_workspace_bytes(dtype: int, sequences: int, n_draft: int, vocab_size: int) -> int:
+    return _bytes(int(load().pb_verify_draft_workspace_bytes(dtype, sequences, n_draft, vocab_size)), "pb_verify_draft_workspace_bytes")
+
+
+def pb_verify_draft(d_target_logits, d_draft_logits, dtype: int, target_seq_stride: int, target_row_stride: int,
+                    draft_seq_stride: int, draft_row_stride: int, sequences: int, n_draft: int, vocab_size: int,
+                    temperature: float, draft_temperature: float, d_draft_tokens, d_uniforms, d_tokens, d_accepted, d_logp,
+                    d_workspace, workspace_bytes: int, stream: int = 0):
+    _check((_student or _load_student()).pb_verify_draft(
+        d_target_logits, d_draft_logits, dtype, target_seq_stride, target_row_stride, draft_seq_stride, draft_row_stride,
+        sequences, n_draft, vocab_size, temperature, draft_temperature, d_draft_tokens, d_uniforms, d_tokens, d_accepted,
+        d_logp, d_workspace, workspace_bytes, stream), "pb_verify_draft")

@@ -14,6 +14,7 @@
 #include "pb.h"
 #include "pb_kernels.hpp"
 #include "pb_logits.hpp"
+#include "pb_student.hpp"
 #include "pb_tree.hpp"
 
 namespace {
@@ -543,6 +544,15 @@ int check_workspace(int64_t need, const void* d_workspace, int64_t bytes) {
   return need > 0 && (!d_workspace || bytes < need || !aligned(d_workspace, 16)) ? PB_EINVAL : PB_OK;
 }
 
+// What both calls on a table of rows for tokens check of their shape.
+int check_embed(int32_t dtype, int32_t other, int32_t n, int32_t V, int32_t dim, float scale) {
+  for (const int32_t t : {dtype, other})
+    if (t != PB_F32 && t != PB_F16 && t != PB_BF16) return PB_EINVAL;
+  if (n < 0 || V < 1 || dim < 1) return PB_EINVAL;
+  if (!std::isfinite(scale)) return PB_ERANGE;
+  return n > pb::kMostTokens || V > pb::kLogitsMaxV || dim > pb::kMostDim ? PB_EUNSUPPORTED : PB_OK;
+}
+
 template <typename T>
 void advance(T*& p, int64_t n) {
   if (p) p += n;
@@ -657,6 +667,159 @@ int pb_distill_topk(const void* d_logits, int32_t dtype, int64_t row_stride, int
     if (a.grad) s.grad = static_cast<char*>(a.grad) + static_cast<int64_t>(at) * grad_stride * es;
     return pb::launch_distill_topk(dtype, s, d_workspace, static_cast<hipStream_t>(hip_stream));
   });
+}
+
+int64_t pb_verify_draft_workspace_bytes(int32_t dtype, int32_t sequences, int32_t n_draft, int32_t vocab_size) {
+  if (n_draft < 0) return PB_EINVAL;
+  const int rc = check_logits(dtype, sequences, vocab_size, 0);
+  if (rc != PB_OK) return rc;
+  if (n_draft > pb::kMaxDrafts) return PB_EUNSUPPORTED;
+  return pb::verify_draft_workspace(dtype, sequences, n_draft, vocab_size);
+}
+
+int pb_verify_draft(const void* d_target_logits, const void* d_draft_logits, int32_t dtype, int64_t target_seq_stride,
+                    int64_t target_row_stride, int64_t draft_seq_stride, int64_t draft_row_stride, int32_t sequences,
+                    int32_t n_draft, int32_t vocab_size, float temperature, float draft_temperature,
+                    const int32_t* d_draft_tokens, const float* d_uniforms, int32_t* d_tokens, int32_t* d_accepted,
+                    float* d_logp, void* d_workspace, int64_t workspace_bytes, void* hip_stream) {
+  if (workspace_bytes < 0) return PB_EINVAL;
+  const int64_t need = pb_verify_draft_workspace_bytes(dtype, sequences, n_draft, vocab_size);
+  if (need < 0) return static_cast<int>(need);
+  if (check_temperature(temperature) != PB_OK || (d_draft_logits && check_temperature(draft_temperature) != PB_OK)) return PB_ERANGE;
+  if (target_seq_stride < vocab_size || target_row_stride < vocab_size) return PB_EINVAL;
+  if (d_draft_logits && (n_draft == 0 || draft_seq_stride < vocab_size || draft_row_stride < vocab_size)) return PB_EINVAL;
+  if (sequences == 0) return PB_OK;
+  const int64_t es = element_bytes(dtype);
+  if (!d_target_logits || !aligned(d_target_logits, es) || !aligned(d_draft_logits, es)) return PB_EINVAL;
+  if ((n_draft > 0) != (d_draft_tokens != nullptr) || !d_uniforms || !d_tokens || !d_accepted) return PB_EINVAL;
+  if (!aligned(d_draft_tokens, 4) || !aligned(d_uniforms, 4) || !aligned(d_tokens, 4) || !aligned(d_accepted, 4) || !aligned(d_logp, 4)) return PB_EINVAL;
+  if (check_workspace(need, d_workspace, workspace_bytes) != PB_OK) return PB_EINVAL;
+  const double log2_e = 1.44269504088896340736;
+  const pb::VerifyArgs a{d_target_logits, d_draft_logits, target_seq_stride, target_row_stride, draft_seq_stride, draft_row_stride, sequences, n_draft, vocab_size,
+                         log2_e / temperature, d_draft_logits ? log2_e / draft_temperature : 0.0, d_draft_tokens, d_uniforms, d_tokens, d_accepted, d_logp};
+  return in_slices(sequences, pb::verify_draft_slice(dtype, n_draft, vocab_size), [&](size_t at, int32_t n) {
+    pb::VerifyArgs s = a;
+    const int64_t from = static_cast<int64_t>(at);
+    s.target = static_cast<const char*>(a.target) + from * target_seq_stride * es;
+    if (a.draft) s.draft = static_cast<const char*>(a.draft) + from * draft_seq_stride * es;
+    s.sequences = n;
+    advance(s.tokens, from * n_draft);
+    advance(s.numbers, from * (n_draft + 1));
+    advance(s.out, from * (n_draft + 1));
+    advance(s.accepted, from);
+    advance(s.logp, from * (n_draft + 1));
+    return pb::launch_verify_draft(dtype, s, d_workspace, static_cast<hipStream_t>(hip_stream));
+  });
+}
+
+int pb_embed_tokens(const void* d_table, int32_t table_dtype, int64_t table_stride, int32_t vocab_size, int32_t dim,
+                    float scale, const int32_t* d_tokens, int32_t n_tokens, void* d_out, int32_t out_dtype,
+                    int64_t out_stride, void* hip_stream) {
+  const int rc = check_embed(table_dtype, out_dtype, n_tokens, vocab_size, dim, scale);
+  if (rc != PB_OK) return rc;
+  if (table_stride < dim || out_stride < dim) return PB_EINVAL;
+  if (n_tokens == 0) return PB_OK;
+  if (!d_table || !d_tokens || !d_out || !aligned(d_tokens, 4)) return PB_EINVAL;
+  if (!aligned(d_table, element_bytes(table_dtype)) || !aligned(d_out, element_bytes(out_dtype))) return PB_EINVAL;
+  const pb::EmbedArgs a{d_table, table_stride, vocab_size, dim, scale, d_tokens, n_tokens, d_out, out_stride};
+  return pb::launch_embed_tokens(table_dtype, out_dtype, a, static_cast<hipStream_t>(hip_stream));
+}
+
+int64_t pb_embed_tokens_backward_workspace_bytes(int32_t n_tokens, int32_t vocab_size, int32_t dim) {
+  const int rc = check_embed(PB_F32, PB_F32, n_tokens, vocab_size, dim, 1.0f);
+  return rc != PB_OK ? rc : pb::embed_tokens_backward_workspace(n_tokens, vocab_size, dim);
+}
+
+int pb_embed_tokens_backward(const void* d_grad_out, int32_t grad_dtype, int64_t grad_stride, const int32_t* d_tokens,
+                             int32_t n_tokens, int32_t vocab_size, int32_t dim, float scale, int32_t accumulate,
+                             void* d_grad_table, int32_t table_dtype, int64_t table_stride, void* d_workspace,
+                             int64_t workspace_bytes, void* hip_stream) {
+  const int rc = check_embed(table_dtype, grad_dtype, n_tokens, vocab_size, dim, scale);
+  if (rc != PB_OK) return rc;
+  if (grad_stride < dim || table_stride < dim || workspace_bytes < 0 || (accumulate != 0 && accumulate != 1)) return PB_EINVAL;
+  if (!d_grad_table || !aligned(d_grad_table, element_bytes(table_dtype))) return PB_EINVAL;
+  if (n_tokens > 0 && (!d_grad_out || !d_tokens || !aligned(d_tokens, 4) || !aligned(d_grad_out, element_bytes(grad_dtype)))) return PB_EINVAL;
+  if (n_tokens == 0 && accumulate) return PB_OK;
+  if (check_workspace(pb_embed_tokens_backward_workspace_bytes(n_tokens, vocab_size, dim), d_workspace, workspace_bytes) != PB_OK) return PB_EINVAL;
+  const pb::EmbedGradArgs a{d_grad_out, grad_stride, d_tokens, n_tokens, vocab_size, dim, scale, accumulate, d_grad_table, table_stride};
+  return pb::launch_embed_tokens_backward(grad_dtype, table_dtype, a, d_workspace, static_cast<hipStream_t>(hip_stream));
+}
+
+int pb_tensors_build(const void* const* d_buffers, const int64_t* sizes, const int32_t* dtypes, int32_t n, int32_t device,
+                     pb_tensors** out) {
+  if (!d_buffers || !sizes || !dtypes || !out || n < 1 || device < 0) return PB_EINVAL;
+  for (int32_t i = 0; i < n; ++i) {
+    if (dtypes[i] != PB_F32 && dtypes[i] != PB_F16 && dtypes[i] != PB_BF16) return PB_EINVAL;
+    if (sizes[i] < 0 || (sizes[i] > 0 && (!d_buffers[i] || !aligned(d_buffers[i], element_bytes(dtypes[i]))))) return PB_EINVAL;
+    if (sizes[i] > (1ll << 40)) return PB_EUNSUPPORTED;
+  }
+  pb_tensors* t = nullptr;
+  std::vector<pb::GradChunk> chunks;
+  try {
+    for (int32_t i = 0; i < n; ++i)
+      for (int64_t at = 0; at < sizes[i]; at += pb::kChunk)
+        chunks.push_back(pb::GradChunk{static_cast<char*>(const_cast<void*>(d_buffers[i])) + at * element_bytes(dtypes[i]),
+                                       static_cast<int32_t>(std::min<int64_t>(pb::kChunk, sizes[i] - at)), dtypes[i]});
+    t = new pb_tensors();
+    t->sizes.assign(sizes, sizes + n);
+    t->dtypes.assign(dtypes, dtypes + n);
+  } catch (const std::bad_alloc&) {
+    delete t;
+    return PB_ENOMEM;
+  }
+  t->device = device;
+  t->count = static_cast<int64_t>(chunks.size());
+  int prev = 0, rc = PB_OK;
+  if (hipGetDevice(&prev) != hipSuccess || hipSetDevice(device) != hipSuccess) {
+    (void)hipGetLastError();
+    delete t;
+    return PB_EHIP;
+  }
+  const size_t bytes = std::max<size_t>(1, chunks.size()) * sizeof(pb::GradChunk);
+  if (hipMalloc(reinterpret_cast<void**>(&t->d_chunks), bytes) != hipSuccess) {
+    (void)hipGetLastError();
+    rc = PB_ENOMEM;
+  } else if (!chunks.empty() && hipMemcpy(t->d_chunks, chunks.data(), bytes, hipMemcpyHostToDevice) != hipSuccess) {
+    (void)hipGetLastError();
+    (void)hipFree(t->d_chunks);
+    rc = PB_EHIP;
+  }
+  (void)hipSetDevice(prev);
+  if (rc != PB_OK) {
+    delete t;
+    return rc;
+  }
+  *out = t;
+  return PB_OK;
+}
+
+int pb_tensors_free(pb_tensors* tensors) {
+  if (!tensors) return PB_OK;
+  int rc = PB_OK, prev = 0;
+  (void)hipGetDevice(&prev);
+  (void)hipSetDevice(tensors->device);
+  if (hipFree(tensors->d_chunks) != hipSuccess) {
+    (void)hipGetLastError();
+    rc = PB_EHIP;
+  }
+  (void)hipSetDevice(prev);
+  delete tensors;
+  return rc;
+}
+
+int64_t pb_grad_norm_workspace_bytes(const pb_tensors* grads) { return grads ? pb::grad_norm_workspace(grads->count) : PB_EINVAL; }
+
+int pb_grad_norm(const pb_tensors* grads, float* d_norm, void* d_workspace, int64_t workspace_bytes, void* hip_stream) {
+  if (!grads || !d_norm || !aligned(d_norm, 4) || workspace_bytes < 0) return PB_EINVAL;
+  if (check_workspace(pb::grad_norm_workspace(grads->count), d_workspace, workspace_bytes) != PB_OK) return PB_EINVAL;
+  return pb::launch_grad_norm(grads->d_chunks, grads->count, d_norm, d_workspace, static_cast<hipStream_t>(hip_stream));
+}
+
+int pb_grad_clip(const pb_tensors* grads, const float* d_norm, float max_norm, const pb_tensors* out, void* hip_stream) {
+  if (!grads || !d_norm || !aligned(d_norm, 4)) return PB_EINVAL;
+  if (!(max_norm >= 0.0f && max_norm <= 3.402823466e+38f)) return PB_ERANGE;
+  if (out && (out->device != grads->device || out->sizes != grads->sizes || out->dtypes != grads->dtypes)) return PB_EINVAL;
+  return pb::launch_grad_clip(grads->d_chunks, out ? out->d_chunks : grads->d_chunks, grads->count, d_norm, max_norm, static_cast<hipStream_t>(hip_stream));
 }
 
 int pb_validate(const pb_tree* tree) {

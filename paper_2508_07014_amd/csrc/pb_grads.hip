@@ -1,0 +1,108 @@
+// The norm over all gradients of a model and their clipping (pb_grad_norm, pb_grad_clip).
+//
+// A set of tensors is a table of pieces of at most kChunk elements on the device; workgroups take them in turn.  Squares are exact in
+// 64 bits and summed there: no scale of gradients overflows or vanishes.
+#include "pb_logit_rows.hpp"
+#include "pb_student.hpp"
+
+namespace pb {
+namespace gr {
+
+using namespace lr;
+
+constexpr int kGroups = 2048;  // workgroups at most: eight a CU
+
+__device__ __forceinline__ double block_sum(double v, double (&shared)[4]) {
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) v += __shfl_xor(v, d, 64);
+  if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = v;
+  __syncthreads();
+  return (shared[0] + shared[1]) + (shared[2] + shared[3]);
+}
+
+template <typename E>
+__device__ __forceinline__ double squares(const GradChunk& c) {
+  const Row<E> row = row_at<E>(c.x, 0, 0, c.n);
+  double s = 0.0;
+  if (static_cast<int>(threadIdx.x) < row.edges) {
+    const double x = E::up(row.x[row.edge_token(threadIdx.x)]);
+    s = x * x;
+  }
+  for (int v = threadIdx.x; v < row.nv; v += 256) {
+    float x[E::N];
+    E::unpack(row.vec(v), x);
+#pragma unroll
+    for (int i = 0; i < E::N; ++i) s = fma(static_cast<double>(x[i]), static_cast<double>(x[i]), s);
+  }
+  return s;
+}
+
+__global__ __launch_bounds__(256) void grad_squares_kernel(const GradChunk* chunks, int64_t n, double* sums) {
+  __shared__ double shared[4];
+  double s = 0.0;
+  for (int64_t c = blockIdx.x; c < n; c += gridDim.x) {
+    const GradChunk chunk = chunks[c];
+    s += chunk.dtype == PB_F32 ? squares<F32>(chunk) : chunk.dtype == PB_F16 ? squares<F16>(chunk) : squares<BF16>(chunk);
+  }
+  s = block_sum(s, shared);
+  if (threadIdx.x == 0) sums[blockIdx.x] = s;
+}
+__global__ __launch_bounds__(256) void grad_norm_kernel(const double* sums, int n, float* norm) {
+  __shared__ double shared[4];
+  double s = 0.0;
+  for (int i = threadIdx.x; i < n; i += 256) s += sums[i];
+  s = block_sum(s, shared);
+  if (threadIdx.x == 0) *norm = static_cast<float>(sqrt(s));
+}
+
+template <typename E>
+__device__ __forceinline__ void scaled(const GradChunk& c, const GradChunk& out, float by) {
+  const Row<E> row = row_at<E>(c.x, 0, 0, c.n);
+  typename E::type* to = static_cast<typename E::type*>(out.x);
+  if (static_cast<int>(threadIdx.x) < row.edges) {
+    const int i = row.edge_token(threadIdx.x);
+    to[i] = E::down(E::up(row.x[i]) * by);
+  }
+  for (int v = threadIdx.x; v < row.nv; v += 256) {
+    float x[E::N];
+    E::unpack(row.vec(v), x);
+#pragma unroll
+    for (int i = 0; i < E::N; ++i) x[i] *= by;
+    store_vector<E>(to + row.token(v, 0), E::pack(x));
+  }
+}
+
+// (A norm that is not finite clips nothing: there is no factor for it.)
+__global__ __launch_bounds__(256) void grad_clip_kernel(const GradChunk* chunks, const GradChunk* out, int64_t n, const float* norm, float max_norm) {
+  const float is = *norm;
+  const bool clips = is > max_norm && is < INFINITY;
+  const float by = clips ? max_norm / is : 1.0f;
+  if (!clips && out == chunks) return;
+  for (int64_t c = blockIdx.x; c < n; c += gridDim.x) {
+    const GradChunk from = chunks[c], to = out[c];
+    if (from.dtype == PB_F32) scaled<F32>(from, to, by);
+    else if (from.dtype == PB_F16) scaled<F16>(from, to, by);
+    else scaled<BF16>(from, to, by);
+  }
+}
+
+int groups_for(int64_t chunks) { return static_cast<int>(chunks < kGroups ? chunks : kGroups); }
+
+}  // namespace gr
+
+int64_t grad_norm_workspace(int64_t chunks) { return gr::groups_for(chunks) * 8; }
+int launch_grad_norm(const GradChunk* chunks, int64_t n, float* norm, void* workspace, hipStream_t stream) {
+  double* sums = static_cast<double*>(workspace);
+  const int groups = gr::groups_for(n);
+  if (groups > 0) gr::grad_squares_kernel<<<groups, 256, 0, stream>>>(chunks, n, sums);
+  if (hipGetLastError() != hipSuccess) return PB_EHIP;
+  gr::grad_norm_kernel<<<1, 256, 0, stream>>>(sums, groups, norm);
+  return hipGetLastError() == hipSuccess ? PB_OK : PB_EHIP;
+}
+int launch_grad_clip(const GradChunk* chunks, const GradChunk* out, int64_t n, const float* norm, float max_norm, hipStream_t stream) {
+  if (n == 0) return PB_OK;
+  gr::grad_clip_kernel<<<gr::groups_for(n), 256, 0, stream>>>(chunks, out, n, norm, max_norm);
+  return hipGetLastError() == hipSuccess ? PB_OK : PB_EHIP;
+}
+
+}  // namespace pb

@@ -163,6 +163,12 @@ __device__ __forceinline__ void store_vector(typename E::type* p, const v4u& r) 
   *reinterpret_cast<typename E::any4*>(p) = r;
 }
 
+// And 16 bytes from any element.
+template <typename E>
+__device__ __forceinline__ v4u any_vector(const typename E::type* p) {
+  return *reinterpret_cast<const typename E::any4*>(p);
+}
+
 // The larger of three (a NaN is passed over, as by fmaxf, which would first quiet each operand by an instruction of its own).
 __device__ __forceinline__ float max3(float a, float b, float c) {
   float r;

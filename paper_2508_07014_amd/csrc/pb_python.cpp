@@ -91,7 +91,8 @@ Entry<ID, A...> entry_of(int (*)(A...));
   X(0, pb_score) X(1, pb_fuse_step) X(2, pb_fuse_frames) X(3, pb_fuse_step_select) X(4, pb_fuse_frames_select) \
   X(5, pb_fuse_frames_ws) X(6, pb_fuse_frames_static) X(7, pb_fuse_step_beam) X(8, pb_score_forest)            \
   X(9, pb_fuse_step_forest) X(10, pb_fuse_frames_forest) X(11, pb_fuse_step_beam_forest)                       \
-  X(12, pb_token_logprobs) X(13, pb_token_logprobs_backward) X(14, pb_distill_topk)
+  X(12, pb_token_logprobs) X(13, pb_token_logprobs_backward) X(14, pb_distill_topk)                            \
+  X(15, pb_embed_tokens) X(16, pb_embed_tokens_backward) X(17, pb_grad_norm) X(18, pb_grad_clip) X(19, pb_verify_draft)
 #define PB_ENTRY(id, name) decltype(entry_of<id>(&name))
 
 // bind(name, address, other): binds an entry point and its ctypes form.
