@@ -392,7 +392,7 @@ int pb_distill_topk(const void* d_logits, int32_t dtype, int64_t row_stride, int
  *   in fp32, rounded once to out_dtype.  A token id outside [0, vocab_size) is absent: its row is 0.
  * pb_embed_tokens_backward -- the table's gradient from d_grad_out [n_tokens, dim], the gradient on those rows:
  *     d_grad_table[v * table_stride + j] = scale * sum over i with d_tokens[i] = v of d_grad_out[i * grad_stride + j]
- *   summed in fp32, by position within 64 places of the order of positions by token and then over those, rounded once to
+ *   summed in fp32, by position within 32 places of the order of positions by token and then over those, rounded once to
  *   table_dtype.  accumulate 0: all vocab_size rows are written, those of tokens that do not occur with 0; accumulate 1: the sum
  *   is added to what is there, and rows of tokens that do not occur are not touched.  Absent tokens' gradients are not looked at.
  *   PB_EINVAL: n_tokens < 0, vocab_size < 1, dim < 1, an unknown dtype, a stride below dim, accumulate neither 0 nor 1, a pointer
@@ -446,7 +446,7 @@ int pb_grad_clip(const pb_tensors* grads, const float* d_norm, float max_norm, c
  * d_accepted[b] = k; d_tokens[b, 0 .. n_draft] = t_0 .. t_k-1, the drawn token, then -1; d_logp (NULL: not wanted) the log p_i of
  * those tokens, NaN beside -1.  n_draft == 0 draws a token from each row.
  * Exponentials and sums are in 64 bits, so that a draw from hundreds of thousands of tokens is the definition's; a logit of -inf
- * has p = 0, as has one that lies 1074 ln 2 T below the largest.  A row of nothing but -inf: p = 0, no token is accepted there, and
+ * has p = 0, as has one whose p / p_max is below 2^-960 (q likewise).  A row of nothing but -inf: p = 0, no token is accepted there, and
  * none drawn (-1); as a y_i: q = 0.  A row that holds a NaN or +inf accepts nothing; where it decides (x_k, or y_k if k < n) the drawn
  * token is -1.
  * PB_EINVAL: as in pb_token_logprobs, n_draft < 0, d_draft_tokens NULL if and only if n_draft > 0, draft rows without drafts, a null

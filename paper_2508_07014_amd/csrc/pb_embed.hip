@@ -1,4 +1,6 @@
 // Rows of a table for tokens, scaled (pb_embed_tokens), and the table's gradient (pb_embed_tokens_backward).
+#include <algorithm>
+
 #include "pb_logit_rows.hpp"
 #include "pb_student.hpp"
 
@@ -8,146 +10,332 @@ namespace em {
 using namespace lr;
 using wv::first_lane;
 
-// Eight elements at p, any alignment of its elements, to and from fp32.
-constexpr int kStep = 8;
-template <typename E>
-__device__ __forceinline__ void load8(const typename E::type* p, float (&x)[kStep]) {
-  if constexpr (E::N == 8) {
+// Elements that a lane takes at once: 16 bytes of the wider type, so that the lanes of an instruction lie next to each other on both
+// sides (two vectors of fp32 a lane, 32 bytes apart: ...).
+template <typename A, typename B>
+constexpr int step_of() { return A::N < B::N ? A::N : B::N; }
+
+// K (4 or 8) elements at p, any alignment of its elements, to and from fp32.
+typedef unsigned v2u __attribute__((ext_vector_type(2)));
+template <typename E, int K>
+__device__ __forceinline__ void load_vector(const typename E::type* p, float (&x)[K]) {
+  if constexpr (E::N == K) {
     E::unpack(any_vector<E>(p), x);
-  } else {
+  } else if constexpr (K == 8) {
     float lo[4], hi[4];
     E::unpack(any_vector<E>(p), lo);
     E::unpack(any_vector<E>(p + 4), hi);
 #pragma unroll
     for (int i = 0; i < 4; ++i) x[i] = lo[i], x[4 + i] = hi[i];
+  } else {
+    typedef unsigned any2 __attribute__((ext_vector_type(2), aligned(2)));
+    const v2u half = *reinterpret_cast<const any2*>(p);
+    float both[8];
+    E::unpack(v4u{half.x, half.y, 0u, 0u}, both);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = both[i];
   }
 }
-template <typename E>
-__device__ __forceinline__ void store8(typename E::type* p, const float (&x)[kStep]) {
-  if constexpr (E::N == 8) {
-    store_vector<E>(p, E::pack(x));
-  } else {
+template <typename E, int K>
+__device__ __forceinline__ void store_vector_of(typename E::type* p, const float (&x)[K]) {
+  if constexpr (E::N == K) {
+    stream_vector<E>(p, E::pack(x));
+  } else if constexpr (K == 8) {
     const float lo[4] = {x[0], x[1], x[2], x[3]}, hi[4] = {x[4], x[5], x[6], x[7]};
     store_vector<E>(p, E::pack(lo));
     store_vector<E>(p + 4, E::pack(hi));
+  } else {
+    typedef unsigned any2 __attribute__((ext_vector_type(2), aligned(2)));
+    const float both[8] = {x[0], x[1], x[2], x[3], 0.0f, 0.0f, 0.0f, 0.0f};
+    const v4u r = E::pack(both);
+    *reinterpret_cast<any2*>(p) = v2u{r.x, r.y};
   }
 }
-// The first n (1 .. 8) of them.
-template <typename E>
-__device__ __forceinline__ void load_some(const typename E::type* p, int n, float (&x)[kStep]) {
-  if (n == kStep) return load8<E>(p, x);
+
+// The columns of a lane: SL vectors of K, `lanes` lanes apart.  The last one of a row is loaded from dim - K on (nothing outside
+// the row is touched), `skip` of it columns of the lane before; NARROW: dim < K, single elements.
+template <int K, int SL, bool NARROW>
+struct Columns {
+  int at[SL], skip[SL], dim;  // skip = K: none
+  __device__ __forceinline__ Columns(int dim_, int first, int lanes, int lane) : dim(dim_) {
 #pragma unroll
-  for (int i = 0; i < kStep; ++i) x[i] = i < n ? E::up(p[i]) : 0.0f;
-}
-template <typename E>
-__device__ __forceinline__ void store_some(typename E::type* p, int n, const float (&x)[kStep]) {
-  if (n == kStep) return store8<E>(p, x);
+    for (int s = 0; s < SL; ++s) {
+      const int d = first + (s * lanes + lane) * K;
+      at[s] = NARROW ? 0 : min(d, dim - K);
+      skip[s] = min(K, NARROW ? (d > 0 ? K : 0) : d - at[s]);
+    }
+  }
+  template <typename E>
+  __device__ __forceinline__ void load(const typename E::type* row, int s, float (&x)[K]) const {
+    if constexpr (NARROW) {
 #pragma unroll
-  for (int i = 0; i < kStep; ++i)
-    if (i < n) p[i] = E::down(x[i]);
+      for (int i = 0; i < K; ++i) x[i] = i < dim ? E::up(row[i]) : 0.0f;
+    } else {
+      load_vector<E>(row + at[s], x);
+    }
+  }
+  template <typename E>
+  __device__ __forceinline__ void store(typename E::type* row, int s, const float (&x)[K]) const {
+    if constexpr (NARROW) {
+#pragma unroll
+      for (int i = 0; i < K; ++i)
+        if (skip[s] == 0 && i < dim) row[i] = E::down(x[i]);
+      return;
+    }
+    if (skip[s] == 0) return store_vector_of<E>(row + at[s], x);
+#pragma unroll
+    for (int i = 1; i < K; ++i)
+      if (i >= skip[s]) row[at[s] + i] = E::down(x[i]);
+  }
+};
+
+// Lanes that take a row: a power of 2, at most a wave.
+int lanes_for(int dim, int step) {
+  int lanes = 1;
+  while (lanes < 64 && lanes * step < dim) lanes *= 2;
+  return lanes;
 }
 
-// `lanes` (a power of 2 up to 64) take a row, 8 elements each a turn.
-template <typename E, typename O>
+// Rows for tokens, SL vectors of a lane at once.
+template <typename E, typename O, int SL, bool NARROW>
 __global__ __launch_bounds__(256) void embed_kernel(EmbedArgs a, int lanes) {
+  constexpr int K = step_of<E, O>();
   const int64_t i = static_cast<int64_t>(blockIdx.x) * (256 / lanes) + threadIdx.x / lanes;
   if (i >= a.n) return;
-  const int t = a.tokens[i], lane = threadIdx.x & (lanes - 1);
+  const int t = a.tokens[i];
   const bool there = static_cast<unsigned>(t) < static_cast<unsigned>(a.V);
   const typename E::type* from = static_cast<const typename E::type*>(a.table) + (there ? t : 0) * a.table_stride;
   typename O::type* to = static_cast<typename O::type*>(a.out) + i * a.out_stride;
-  for (int d = lane * kStep; d < a.dim; d += lanes * kStep) {
-    const int n = min(kStep, a.dim - d);
-    float x[kStep] = {0, 0, 0, 0, 0, 0, 0, 0};
-    if (there) {
-      load_some<E>(from + d, n, x);
+  const Columns<K, SL, NARROW> cols(a.dim, blockIdx.y * lanes * K * SL, lanes, threadIdx.x & (lanes - 1));
+  float x[SL][K] = {};
+  if (there) {
 #pragma unroll
-      for (int k = 0; k < kStep; ++k) x[k] *= a.scale;
-    }
-    store_some<O>(to + d, n, x);
+    for (int u = 0; u < SL; ++u) cols.template load<E>(from, u, x[u]);
+  }
+#pragma unroll
+  for (int u = 0; u < SL; ++u) {
+#pragma unroll
+    for (int k = 0; k < K; ++k) x[u][k] = there ? product(x[u][k], a.scale) : 0.0f;
+    cols.template store<O>(to, u, x[u]);
   }
 }
 
 // The gradient: positions sorted by token, then sums over each token's positions.
 //
-// Sorting.  A workgroup takes a range of the vocabulary and reads all tokens: those of its range it counts, for each wave's share of
-// the positions apart, and places in a second pass; those below its range it counts for the place its range begins at.
-// So the order is that of the positions, without an atomic on memory and with one launch: the workgroups read the tokens
-// as often as there are of them, from the caches (131072 tokens: 128 MB in all).
+// Sorting.  A workgroup takes a range of the vocabulary, 2^shift tokens, and reads all tokens: those of its range it counts, for each
+// wave's share of the positions apart, and places in a second pass; those below its range it counts for the place its range
+// begins at.  So the order is that of the positions, without an atomic on memory and with one launch.  Reading all tokens in every
+// workgroup takes time with their number (16384 of them: 8.8 us, 131072: 42), so from kManyTokens on the positions are
+// split by range first, in chunks: then a workgroup reads its own alone.
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64;
-constexpr int kMostRange = 896;   // tokens of a range: 64 bytes of LDS each
-constexpr int kRanges = 256;      // at least so many workgroups where there are as many tokens
+constexpr int kAhead = 16;      // tokens that a lane requests at once
+constexpr int kMaxShift = 9;    // (ranges of 512 tokens: 32 KiB of counts)
+constexpr int kMaxRanges = (kLogitsMaxV + (1 << kMaxShift) - 1) >> kMaxShift;
+static_assert(kMaxRanges <= kSortThreads, "a thread a range");
+constexpr int kManyTokens = 24576;
+constexpr int kSplit = 4096;    // positions of a chunk: 12 bits beside those of a token in its range
 
-__global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(const int32_t* tokens, int n, int V, int range, int32_t* begin, int32_t* order) {
-  extern __shared__ int counts[];  // [kSortWaves][range]
-  __shared__ int shared_sum[kSortWaves], base;
-  const int tid = threadIdx.x, lane = tid & 63, wave = uniform_i(tid >> 6);
-  const int v0 = blockIdx.x * range, size = min(range, V - v0);
+int shift_for(int V) {  // about as many ranges as there are CUs
+  int shift = 0;
+  while (shift < kMaxShift && ((V - 1) >> shift) >= 256) ++shift;
+  return shift;
+}
+
+// Sums of all threads' values up to each (`total`: of all); s: a place a wave.
+__device__ __forceinline__ int group_upto(int v, int* s, int* total) {
+  const int lane = threadIdx.x & 63, wave = uniform_i(threadIdx.x >> 6);
+  int upto = v;
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const int w = __shfl_up(upto, d, 64);
+    if (lane >= d) upto += w;
+  }
+  __syncthreads();
+  if (lane == 63) s[wave] = upto;
+  __syncthreads();
+  int ahead = 0, all = 0;
+  for (int w = 0; w < kSortWaves; ++w) {
+    if (w < wave) ahead += s[w];
+    all += s[w];
+  }
+  *total = all;
+  return ahead + upto;
+}
+
+// counts[wave][i], i < size: how many of each wave; becomes the place of the wave's first, `base` ahead of them all.  Returns
+// the place of the thread's i (and in *end what follows it).
+__device__ __forceinline__ int places(int* counts, int stride, int size, int base, int* s, int* end) {
+  const int tid = threadIdx.x;
+  int total = 0, all;
+  if (tid < size)
+    for (int w = 0; w < kSortWaves; ++w) total += counts[w * stride + tid];
+  const int first = base + group_upto(total, s, &all) - total;
+  if (tid < size) {
+    int at = first;
+    for (int w = 0; w < kSortWaves; ++w) {
+      const int c = counts[w * stride + tid];
+      counts[w * stride + tid] = at;
+      at += c;
+    }
+  }
+  *end = first + total;
+  __syncthreads();
+  return first;
+}
+
+// Places a wave's keys (of `bits` bits; `in`: the lane has one) at their counters, in the order of the lanes: the lanes with the same key
+// are found bit by bit.
+template <typename Put>
+__device__ __forceinline__ void place_keys(int* counters, unsigned key, bool in, int bits, int lane, Put&& put) {
+  u64 same = __ballot(in);
+  if (same == 0) return;
+  for (int b = 0; b < bits; ++b) {
+    const bool one = (key >> b) & 1u;
+    const u64 ones = __ballot(one);
+    same &= one ? ones : ~ones;
+  }
+  if (in) {
+    const int to = counters[key], rank = __builtin_popcountll(same & ((1ull << lane) - 1));
+    __builtin_amdgcn_wave_barrier();
+    if (rank == 0) counters[key] = to + __builtin_popcountll(same);
+    put(to + rank);
+  }
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+__global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(const int32_t* tokens, int n, int V, int shift, int32_t* begin, int32_t* order) {
+  extern __shared__ int counts[];  // [kSortWaves][2^shift]
+  __shared__ int s[kSortWaves];
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform_i(tid >> 6), range = 1 << shift;
+  const int v0 = blockIdx.x << shift, size = min(range, V - v0);
   for (int i = tid; i < kSortWaves * range; i += kSortThreads) counts[i] = 0;
   __syncthreads();
   const int share = ((n + kSortWaves - 1) / kSortWaves + 63) / 64 * 64, p0 = min(n, wave * share), p1 = min(n, p0 + share);
   int* mine = counts + wave * range;
   int below = 0;
-  for (int p = p0 + lane; p < p1; p += 64) {
-    const int t = tokens[p];
-    if (t >= v0 && t < v0 + size) atomicAdd(&mine[t - v0], 1);
-    below += t >= 0 && t < v0;
-  }
+  auto count = [&](int t) {  // (an id below 0 is a large one without its sign)
+    const unsigned u = static_cast<unsigned>(t) - static_cast<unsigned>(v0);
+    below += static_cast<unsigned>(t) < static_cast<unsigned>(v0);
+    if (u < static_cast<unsigned>(size)) atomicAdd(&mine[u], 1);
+  };
+  int p = p0;
+  for (; p + 64 * kAhead <= p1; p += 64 * kAhead) {
+    int t[kAhead];
 #pragma unroll
-  for (int d = 1; d < 64; d *= 2) below += __shfl_xor(below, d, 64);
-  if (lane == 0) shared_sum[wave] = below;
-  __syncthreads();
-  if (tid == 0) {
-    int s = 0;
-    for (int w = 0; w < kSortWaves; ++w) s += shared_sum[w];
-    base = s;
-  }
-  __syncthreads();
-  // counts[w][v] becomes the place of wave w's first position of token v: sums over tokens, then over the waves before.
-  int total = 0;
-  if (tid < size)
-    for (int w = 0; w < kSortWaves; ++w) total += counts[w * range + tid];
-  int upto = total;
+    for (int k = 0; k < kAhead; ++k) t[k] = tokens[p + 64 * k + lane];
 #pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const int v = __shfl_up(upto, d, 64);
-    if (lane >= d) upto += v;
+    for (int k = 0; k < kAhead; ++k) count(t[k]);
   }
-  __syncthreads();
-  if (lane == 63) shared_sum[wave] = upto;
-  __syncthreads();
-  int at = base + upto - total;
-  for (int w = 0; w < wave; ++w) at += shared_sum[w];
+  for (; p < p1; p += 64)
+    if (p + lane < p1) count(tokens[p + lane]);
+  int base, end;
+  group_upto(below, s, &base);
+  const int at = places(counts, range, size, base, s, &end);
   if (tid < size) {
     begin[v0 + tid] = at;
-    if (v0 + tid == V - 1) begin[V] = at + total;
-    for (int w = 0; w < kSortWaves; ++w) {
-      const int c = counts[w * range + tid];
-      counts[w * range + tid] = at;
-      at += c;
-    }
+    if (v0 + tid == V - 1) begin[V] = end;
   }
+  auto put = [&](int t, int from) {
+    const unsigned u = static_cast<unsigned>(t) - static_cast<unsigned>(v0);
+    place_keys(mine, u, u < static_cast<unsigned>(size), shift, lane, [&](int to) { order[to] = from; });
+  };
+  p = p0;  // (the same in all lanes of a wave)
+  for (; p + 64 * kAhead <= p1; p += 64 * kAhead) {
+    int t[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) t[k] = tokens[p + 64 * k + lane];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) put(t[k], p + 64 * k + lane);
+  }
+  for (; p < p1; p += 64) put(p + lane < p1 ? tokens[p + lane] : -1, p + lane);
+}
+
+// A chunk's positions by the range of their tokens, in order: an entry is the token's place in its range and the position's in the
+// chunk; starts[chunk][range] is where the range's begin in the chunk, starts[chunk][ranges] how many there are.
+__global__ __launch_bounds__(kSortThreads) void embed_split_kernel(const int32_t* tokens, int n, int V, int shift, int ranges, unsigned* entries, int32_t* starts) {
+  __shared__ int counts[kSortWaves * kMaxRanges], s[kSortWaves];
+  constexpr int kTurns = kSplit / kSortThreads;
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform_i(tid >> 6), p0 = blockIdx.x * kSplit, at0 = wave * (kSplit / kSortWaves) + lane;
+  for (int i = tid; i < kSortWaves * ranges; i += kSortThreads) counts[i] = 0;
+  int t[kTurns];
+#pragma unroll
+  for (int k = 0; k < kTurns; ++k) t[k] = p0 + at0 + 64 * k < n ? tokens[p0 + at0 + 64 * k] : -1;
   __syncthreads();
-  for (int p = p0; p < p1; p += 64) {  // (all lanes of a wave: p0 is the wave's)
-    const int t = p + lane < p1 ? tokens[p + lane] : -1;
-    const bool in = t >= v0 && t < v0 + size;
-    u64 left = __ballot(in);
-    while (left) {
-      const int v = __builtin_amdgcn_readlane(t, first_lane(left));
-      const u64 same = __ballot(in && t == v);
-      const int to = mine[v - v0];
-      if (in && t == v) order[to + __builtin_popcountll(same & ((1ull << lane) - 1))] = p + lane;
-      if (lane == 0) mine[v - v0] = to + __builtin_popcountll(same);
-      left &= ~same;
-      __builtin_amdgcn_wave_barrier();
+  int* mine = counts + wave * ranges;
+#pragma unroll
+  for (int k = 0; k < kTurns; ++k)
+    if (static_cast<unsigned>(t[k]) < static_cast<unsigned>(V)) atomicAdd(&mine[t[k] >> shift], 1);
+  __syncthreads();
+  int end;
+  const int at = places(counts, ranges, ranges, 0, s, &end);
+  int32_t* to = starts + static_cast<int64_t>(blockIdx.x) * (ranges + 1);
+  if (tid < ranges) to[tid] = at;
+  if (tid == ranges - 1) to[ranges] = end;
+  int bits = 0;
+  while (((ranges - 1) >> bits) > 0) ++bits;
+#pragma unroll
+  for (int k = 0; k < kTurns; ++k)
+    place_keys(mine, static_cast<unsigned>(t[k]) >> shift, static_cast<unsigned>(t[k]) < static_cast<unsigned>(V), bits, lane, [&](int q) {
+      entries[p0 + q] = static_cast<unsigned>(t[k] & ((1 << shift) - 1)) * kSplit + static_cast<unsigned>(at0 + 64 * k);
+    });
+}
+
+// A range's positions from all chunks: each wave takes some chunks next to each other.
+__global__ __launch_bounds__(kSortThreads) void embed_merge_kernel(const unsigned* entries, const int32_t* starts, int chunks, int V, int shift, int ranges,
+                                                                  int32_t* begin, int32_t* order) {
+  extern __shared__ int counts[];  // [kSortWaves][2^shift]
+  __shared__ int s[kSortWaves];
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform_i(tid >> 6), range = 1 << shift, b = blockIdx.x;
+  const int v0 = b << shift, size = min(range, V - v0);
+  for (int i = tid; i < kSortWaves * range; i += kSortThreads) counts[i] = 0;
+  int below = 0;
+  for (int c = tid; c < chunks; c += kSortThreads) below += starts[static_cast<int64_t>(c) * (ranges + 1) + b];
+  int base, end;
+  group_upto(below, s, &base);  // (waits for the counts to be 0, too)
+  const int share = (chunks + kSortWaves - 1) / kSortWaves, c0 = min(chunks, wave * share), c1 = min(chunks, c0 + share);
+  int* mine = counts + wave * range;
+  // Calls f(entry, is one, chunk) for 64 entries at a time, in order, those of four chunks requested together.
+  auto all = [&](auto&& f) {
+    for (int q = c0; q < c1; q += 64) {
+      const int c = min(q + lane, c1 - 1), from = starts[static_cast<int64_t>(c) * (ranges + 1) + b], to = starts[static_cast<int64_t>(c) * (ranges + 1) + b + 1];
+      const int many = min(64, c1 - q);
+      for (int k0 = 0; k0 < many; k0 += 4) {
+        unsigned e[4];
+        int i0[4], i1[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int from_lane = min(k0 + k, many - 1);
+          i0[k] = __builtin_amdgcn_readlane(from, from_lane);
+          i1[k] = k0 + k < many ? __builtin_amdgcn_readlane(to, from_lane) : i0[k];
+          e[k] = i0[k] + lane < i1[k] ? entries[static_cast<int64_t>(q + k0 + k) * kSplit + i0[k] + lane] : 0u;
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          if (i0[k] < i1[k]) f(e[k], i0[k] + lane < i1[k], q + k0 + k);
+          for (int i = i0[k] + 64; i < i1[k]; i += 64) f(i + lane < i1[k] ? entries[static_cast<int64_t>(q + k0 + k) * kSplit + i + lane] : 0u, i + lane < i1[k], q + k0 + k);
+        }
+      }
     }
+  };
+  all([&](unsigned e, bool is, int) {
+    if (is) atomicAdd(&mine[e / kSplit], 1);
+  });
+  __syncthreads();
+  const int at = places(counts, range, size, base, s, &end);
+  if (tid < size) {
+    begin[v0 + tid] = at;
+    if (v0 + tid == V - 1) begin[V] = end;
   }
+  all([&](unsigned e, bool is, int c) {
+    place_keys(mine, e / kSplit, is, shift, lane, [&](int to) { order[to] = c * kSplit + static_cast<int>(e % kSplit); });
+  });
 }
 
 // Sums.  Tokens with up to kFew positions are summed by `lanes` lanes at once; those with more in pieces, cut at every kFew-th place of
 // the order, which a second launch joins.  A stretch of kFew places holds pieces of two such tokens at most: one that
 // began before it or at its first place, and one that begins later in it.
-constexpr int kFew = 64;
+constexpr int kFew = 32;
 
 struct SumArgs {
   EmbedGradArgs a;
@@ -157,93 +345,152 @@ struct SumArgs {
   int lanes;
 };
 
-// Eight columns from d on over the positions order[i] .. order[j - 1], in that order.
-template <typename G>
-__device__ __forceinline__ void sum_positions(const SumArgs& s, int i, int j, int d, int n, float (&sum)[kStep]) {
-  const typename G::type* g = static_cast<const typename G::type*>(s.a.grad) + d;
-  for (; i + 4 <= j; i += 4) {
-    int p[4];
-    float x[4][kStep];
+// Adds the rows of `U` positions from order[i] on, requested together.
+template <int U, typename G, int K, int SL, bool NARROW>
+__device__ __forceinline__ void add_rows(const SumArgs& s, const Columns<K, SL, NARROW>& cols, int i, float (&sum)[SL][K]) {
+  const typename G::type* g = static_cast<const typename G::type*>(s.a.grad);
+  int p[U];
+  float x[U][SL][K];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) p[k] = s.order[i + k];
+  for (int k = 0; k < U; ++k) p[k] = s.order[i + k];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) load_some<G>(g + p[k] * s.a.grad_stride, n, x[k]);
+  for (int k = 0; k < U; ++k)
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
+    for (int v = 0; v < SL; ++v) cols.template load<G>(g + p[k] * s.a.grad_stride, v, x[k][v]);
 #pragma unroll
-      for (int c = 0; c < kStep; ++c) sum[c] += x[k][c];
+  for (int k = 0; k < U; ++k)
+#pragma unroll
+    for (int v = 0; v < SL; ++v)
+#pragma unroll
+      for (int c = 0; c < K; ++c) sum[v][c] += x[k][v][c];
+}
+template <typename G, int K, int SL, bool NARROW>
+__device__ __forceinline__ void sum_positions(const SumArgs& s, const Columns<K, SL, NARROW>& cols, int i, int j, float (&sum)[SL][K]) {
+  constexpr int U = 64 / (K * SL);
+  for (; i + U <= j; i += U) add_rows<U, G>(s, cols, i, sum);
+  if constexpr (U > 4)
+    for (; i + 4 <= j; i += 4) add_rows<4, G>(s, cols, i, sum);
+  if constexpr (U > 2)
+    if (i + 2 <= j) add_rows<2, G>(s, cols, i, sum), i += 2;
+  for (; i < j; ++i) add_rows<1, G>(s, cols, i, sum);
+}
+template <typename T, int K, int SL, bool NARROW>
+__device__ __forceinline__ void write_columns(const EmbedGradArgs& a, const Columns<K, SL, NARROW>& cols, int v, float (&sum)[SL][K]) {
+  typename T::type* to = static_cast<typename T::type*>(a.table_grad) + v * a.table_stride;
+  float old[SL][K];
+  if (a.accumulate) {
+#pragma unroll
+    for (int u = 0; u < SL; ++u) cols.template load<T>(to, u, old[u]);
   }
-  for (; i < j; ++i) {
-    float x[kStep];
-    load_some<G>(g + s.order[i] * s.a.grad_stride, n, x);
 #pragma unroll
-    for (int c = 0; c < kStep; ++c) sum[c] += x[c];
+  for (int u = 0; u < SL; ++u) {
+#pragma unroll
+    for (int c = 0; c < K; ++c) sum[u][c] = a.accumulate ? product(a.scale, sum[u][c]) + old[u][c] : product(a.scale, sum[u][c]);
+    cols.template store<T>(to, u, sum[u]);
   }
 }
-template <typename T>
-__device__ __forceinline__ void write_columns(const EmbedGradArgs& a, int v, int d, int n, float (&sum)[kStep]) {
-  typename T::type* to = static_cast<typename T::type*>(a.table_grad) + v * a.table_stride + d;
-  float old[kStep];
-  if (a.accumulate) load_some<T>(to, n, old);
+template <int K, int SL, bool NARROW>
+__device__ __forceinline__ void write_piece(float* to, const Columns<K, SL, NARROW>& cols, const float (&sum)[SL][K]) {
 #pragma unroll
-  for (int c = 0; c < kStep; ++c) sum[c] = a.accumulate ? __builtin_fmaf(a.scale, sum[c], old[c]) : a.scale * sum[c];
-  store_some<T>(to, n, sum);
+  for (int u = 0; u < SL; ++u) cols.template store<F32>(to, u, sum[u]);
 }
 
-template <typename G, typename T>
-__global__ __launch_bounds__(256) void embed_sums_kernel(SumArgs s, int rows_blocks, int stretches) {
+// A stretch's pieces, `lanes` lanes a vector of each of its columns.
+template <typename G, int K, bool NARROW>
+__device__ __forceinline__ void sum_stretch(const SumArgs& s, int c, int vector, int end, int lane) {
   const EmbedGradArgs& a = s.a;
-  const int lane = threadIdx.x & (s.lanes - 1), sub = threadIdx.x / s.lanes, each = 256 / s.lanes;
-  const int d = (blockIdx.y * s.lanes + lane) * kStep, n = min(kStep, a.dim - d);
-  if (n <= 0) return;
-  float sum[kStep] = {0, 0, 0, 0, 0, 0, 0, 0};
-  if (static_cast<int>(blockIdx.x) < rows_blocks) {
-    const int64_t v = static_cast<int64_t>(blockIdx.x) * each + sub;
-    if (v >= a.V) return;
-    const int i = s.begin[v], j = s.begin[v + 1];
-    if (j - i > kFew || (j == i && a.accumulate)) return;
-    sum_positions<G>(s, i, j, d, n, sum);
-    write_columns<T>(a, static_cast<int>(v), d, n, sum);
-    return;
-  }
-  const int c = (static_cast<int>(blockIdx.x) - rows_blocks) * each + sub, end = s.begin[a.V];
-  if (c >= stretches || c * kFew >= end) return;
+  const Columns<K, 1, NARROW> cols(a.dim, vector * s.lanes * K, s.lanes, lane);
   const int i0 = c * kFew, i1 = min(end, i0 + kFew);
   const int first = a.tokens[s.order[i0]], last = a.tokens[s.order[i1 - 1]];
+  float* pieces = s.pieces + static_cast<int64_t>(c) * 2 * a.dim;
   if (s.begin[first + 1] - s.begin[first] > kFew) {
-    sum_positions<G>(s, i0, min(i1, s.begin[first + 1]), d, n, sum);
-    store_some<F32>(s.pieces + (static_cast<int64_t>(c) * 2) * a.dim + d, n, sum);
+    float sum[1][K] = {};
+    sum_positions<G>(s, cols, i0, min(i1, s.begin[first + 1]), sum);
+    write_piece(pieces, cols, sum);
   }
   if (last != first && s.begin[last + 1] - s.begin[last] > kFew) {
-    float other[kStep] = {0, 0, 0, 0, 0, 0, 0, 0};
-    sum_positions<G>(s, s.begin[last], i1, d, n, other);
-    store_some<F32>(s.pieces + (static_cast<int64_t>(c) * 2 + 1) * a.dim + d, n, other);
+    float sum[1][K] = {};
+    sum_positions<G>(s, cols, s.begin[last], i1, sum);
+    write_piece(pieces + a.dim, cols, sum);
   }
 }
 
-// Pieces of a token in the order of their stretches, by the workgroup of the stretch in which it begins.
-template <typename T>
-__global__ __launch_bounds__(256) void embed_join_kernel(SumArgs s, int stretches) {
+// The first stretch_blocks * vectors workgroups take stretches (a piece takes longer than other rows), the others `lanes` lanes a token.
+template <typename G, typename T, int SL, bool NARROW>
+__global__ __launch_bounds__(256) void embed_sums_kernel(SumArgs s, int stretch_blocks, int vectors, int row_blocks) {
+  constexpr int K = step_of<G, T>();
   const EmbedGradArgs& a = s.a;
-  const int c = blockIdx.x * (256 / s.lanes) + threadIdx.x / s.lanes, end = s.begin[a.V];
-  const int d = (blockIdx.y * s.lanes + (threadIdx.x & (s.lanes - 1))) * kStep, n = min(kStep, a.dim - d);
-  if (c >= stretches || c * kFew >= end || n <= 0) return;
-  const int v = a.tokens[s.order[min(end, c * kFew + kFew) - 1]], i = s.begin[v], j = s.begin[v + 1];
-  if (j - i <= kFew || i / kFew != c) return;
-  float sum[kStep], x[kStep];
-  load_some<F32>(s.pieces + (static_cast<int64_t>(c) * 2 + (i == c * kFew ? 0 : 1)) * a.dim + d, n, sum);
-  for (int k = c + 1; k * kFew < j; ++k) {
-    load_some<F32>(s.pieces + static_cast<int64_t>(k) * 2 * a.dim + d, n, x);
-#pragma unroll
-    for (int e = 0; e < kStep; ++e) sum[e] += x[e];
+  const int lane = threadIdx.x & (s.lanes - 1), sub = threadIdx.x / s.lanes, each = 256 / s.lanes;
+  int block = blockIdx.x;
+  if (block < stretch_blocks * vectors) {
+    const int c = block % stretch_blocks * each + sub, end = s.begin[a.V];
+    if (c * kFew < end) sum_stretch<G, K, NARROW>(s, c, block / stretch_blocks, end, lane);
+    return;
   }
-  write_columns<T>(a, v, d, n, sum);
+  block -= stretch_blocks * vectors;
+  const int v = block % row_blocks * each + sub;
+  if (v >= a.V) return;
+  const int i = s.begin[v], j = s.begin[v + 1];
+  if (j - i > kFew || (j == i && a.accumulate)) return;
+  const Columns<K, SL, NARROW> cols(a.dim, block / row_blocks * s.lanes * K * SL, s.lanes, lane);
+  float sum[SL][K] = {};
+  sum_positions<G>(s, cols, i, j, sum);
+  write_columns<T>(a, cols, v, sum);
 }
 
-int lanes_for(int dim) {
-  int lanes = 1;
-  while (lanes < 64 && lanes * kStep < dim) lanes *= 2;
-  return lanes;
+// Pieces of a token, in the order of their stretches: a workgroup looks through some stretches for tokens that begin there, and for each
+// its groups of lanes sum a share of the pieces, and one of them those sums.
+constexpr int kJoinThreads = 1024;
+template <typename T, int K, bool NARROW>
+__global__ __launch_bounds__(kJoinThreads) void embed_join_kernel(SumArgs s, int stretches) {
+  __shared__ float shares[kJoinThreads * K];
+  __shared__ int owners[kJoinThreads], n_owners;
+  const EmbedGradArgs& a = s.a;
+  const int tid = threadIdx.x, groups = kJoinThreads / s.lanes, group = tid / s.lanes, lane = tid & (s.lanes - 1), end = s.begin[a.V];
+  if (static_cast<int64_t>(blockIdx.x) * groups * kFew >= end) return;
+  if (tid == 0) n_owners = 0;
+  __syncthreads();
+  const int mine = blockIdx.x * groups + tid;
+  if (tid < groups && mine < stretches && mine * kFew < end) {
+    const int v = a.tokens[s.order[min(end, mine * kFew + kFew) - 1]], i = s.begin[v], j = s.begin[v + 1];
+    if (j - i > kFew && i / kFew == mine) owners[atomicAdd(&n_owners, 1)] = v;
+  }
+  __syncthreads();
+  const Columns<K, 1, NARROW> cols(a.dim, blockIdx.y * s.lanes * K, s.lanes, lane);
+  const int64_t row = 2 * static_cast<int64_t>(a.dim);
+  for (int o = 0; o < n_owners; ++o) {  // (each by itself: their order does not matter)
+    const int v = owners[o], i = s.begin[v], c = i / kFew, last = (s.begin[v + 1] + kFew - 1) / kFew;
+    const int share = (last - c + groups - 1) / groups, k1 = min(last, c + (group + 1) * share);
+    int k = c + group * share;
+    float sum[1][K] = {};
+    auto piece = [&](int q) { return s.pieces + q * row + (q == c && i != c * kFew ? a.dim : 0); };
+    constexpr int U = 8;
+    for (; k + U <= k1; k += U) {
+      float x[U][K];
+#pragma unroll
+      for (int u = 0; u < U; ++u) cols.template load<F32>(piece(k + u), 0, x[u]);
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int e = 0; e < K; ++e) sum[0][e] += x[u][e];
+    }
+    for (; k < k1; ++k) {
+      float x[K];
+      cols.template load<F32>(piece(k), 0, x);
+#pragma unroll
+      for (int e = 0; e < K; ++e) sum[0][e] += x[e];
+    }
+#pragma unroll
+    for (int e = 0; e < K; ++e) shares[e * kJoinThreads + tid] = sum[0][e];
+    __syncthreads();
+    if (group == 0) {
+      for (int q = 1; q < groups && c + q * share < last; ++q)
+#pragma unroll
+        for (int e = 0; e < K; ++e) sum[0][e] += shares[e * kJoinThreads + q * s.lanes + lane];
+      write_columns<T>(a, cols, v, sum);
+    }
+    __syncthreads();
+  }
 }
 
 template <typename Do>
@@ -252,50 +499,95 @@ int with_type(int dtype, Do&& f) {
 }
 int done() { return hipGetLastError() == hipSuccess ? PB_OK : PB_EHIP; }
 
-int sort_range(int V) {
-  const int even = (V + kRanges - 1) / kRanges;
-  return even < kMostRange ? even : kMostRange;
-}
 int64_t padded(int64_t bytes) { return (bytes + 255) / 256 * 256; }
 
 }  // namespace em
 
 int launch_embed_tokens(int table_dtype, int out_dtype, const EmbedArgs& a, hipStream_t stream) {
-  const int lanes = em::lanes_for(a.dim);
-  const unsigned grid = static_cast<unsigned>((static_cast<int64_t>(a.n) * lanes + 255) / 256);
   return em::with_type(table_dtype, [&](auto e) {
     return em::with_type(out_dtype, [&](auto o) {
-      em::embed_kernel<decltype(e), decltype(o)><<<grid, 256, 0, stream>>>(a, lanes);
-      return em::done();
+      using E = decltype(e);
+      using O = decltype(o);
+      constexpr int K = em::step_of<E, O>();
+      const int lanes = em::lanes_for(a.dim, K), vectors = (a.dim + lanes * K - 1) / (lanes * K), groups = (a.n + 256 / lanes - 1) / (256 / lanes);
+      auto go = [&](auto kernel, int sl) {
+        kernel<<<dim3(groups, (vectors + sl - 1) / sl), 256, 0, stream>>>(a, lanes);
+        return em::done();
+      };
+      if (a.dim < K) return go(em::embed_kernel<E, O, 1, true>, 1);
+      if (vectors == 1) return go(em::embed_kernel<E, O, 1, false>, 1);
+      if (vectors == 2) return go(em::embed_kernel<E, O, 2, false>, 2);
+      return go(em::embed_kernel<E, O, 4, false>, 4);
     });
   });
 }
 
-int64_t embed_tokens_backward_workspace(int32_t n, int32_t V, int32_t dim) {
-  const int64_t stretches = (static_cast<int64_t>(n) + em::kFew - 1) / em::kFew;
-  return em::padded((static_cast<int64_t>(V) + 1) * 4) + em::padded(static_cast<int64_t>(n) * 4) + stretches * 2 * dim * 4;
+namespace em {
+// What lies where in the workspace.
+struct Layout {
+  int64_t begin, order, pieces, entries, starts, bytes;
+};
+Layout layout(int32_t n, int32_t V, int32_t dim) {
+  Layout l;
+  l.begin = 0;
+  l.order = padded((static_cast<int64_t>(V) + 1) * 4);
+  l.pieces = l.order + padded(static_cast<int64_t>(n) * 4);
+  l.bytes = l.pieces + (n > kFew ? padded((static_cast<int64_t>(n) + kFew - 1) / kFew * 2 * dim * 4) : 0);
+  l.entries = l.starts = l.pieces;  // (entries and starts are done with before there are pieces)
+  if (n >= kManyTokens) {
+    const int64_t ranges = ((V - 1) >> shift_for(V)) + 1;
+    l.starts = l.entries + padded(static_cast<int64_t>(n) * 4);
+    l.bytes = std::max(l.bytes, l.starts + padded((static_cast<int64_t>(n) + kSplit - 1) / kSplit * (ranges + 1) * 4));
+  }
+  return l;
 }
+}  // namespace em
+
+int64_t embed_tokens_backward_workspace(int32_t n, int32_t V, int32_t dim) { return em::layout(n, V, dim).bytes; }
+
 int launch_embed_tokens_backward(int grad_dtype, int table_dtype, const EmbedGradArgs& a, void* workspace, hipStream_t stream) {
   char* ws = static_cast<char*>(workspace);
-  int32_t* begin = reinterpret_cast<int32_t*>(ws);
-  int32_t* order = reinterpret_cast<int32_t*>(ws + em::padded((static_cast<int64_t>(a.V) + 1) * 4));
-  float* pieces = reinterpret_cast<float*>(ws + em::padded((static_cast<int64_t>(a.V) + 1) * 4) + em::padded(static_cast<int64_t>(a.n) * 4));
-  const int range = em::sort_range(a.V), lanes = em::lanes_for(a.dim), each = 256 / lanes;
-  const int stretches = (a.n + em::kFew - 1) / em::kFew, slices = (a.dim + lanes * em::kStep - 1) / (lanes * em::kStep);
-  em::embed_sort_kernel<<<(a.V + range - 1) / range, em::kSortThreads, static_cast<size_t>(range) * em::kSortWaves * 4, stream>>>(a.tokens, a.n, a.V, range, begin, order);
+  const em::Layout l = em::layout(a.n, a.V, a.dim);
+  int32_t* begin = reinterpret_cast<int32_t*>(ws + l.begin);
+  int32_t* order = reinterpret_cast<int32_t*>(ws + l.order);
+  float* pieces = reinterpret_cast<float*>(ws + l.pieces);
+  const int shift = em::shift_for(a.V), ranges = ((a.V - 1) >> shift) + 1, stretches = (a.n + em::kFew - 1) / em::kFew;
+  const size_t counts = static_cast<size_t>(em::kSortWaves) * 4 << shift;
+  if (a.n >= em::kManyTokens) {
+    unsigned* entries = reinterpret_cast<unsigned*>(ws + l.entries);
+    int32_t* starts = reinterpret_cast<int32_t*>(ws + l.starts);
+    const int chunks = (a.n + em::kSplit - 1) / em::kSplit;
+    em::embed_split_kernel<<<chunks, em::kSortThreads, 0, stream>>>(a.tokens, a.n, a.V, shift, ranges, entries, starts);
+    if (em::done() != PB_OK) return PB_EHIP;
+    em::embed_merge_kernel<<<ranges, em::kSortThreads, counts, stream>>>(entries, starts, chunks, a.V, shift, ranges, begin, order);
+  } else {
+    em::embed_sort_kernel<<<ranges, em::kSortThreads, counts, stream>>>(a.tokens, a.n, a.V, shift, begin, order);
+  }
   if (em::done() != PB_OK) return PB_EHIP;
-  const em::SumArgs s{a, begin, order, pieces, lanes};
-  const int rows_blocks = (a.V + each - 1) / each, stretch_blocks = (stretches + each - 1) / each;
-  const int rc = em::with_type(grad_dtype, [&](auto g) {
+  return em::with_type(grad_dtype, [&](auto g) {
     return em::with_type(table_dtype, [&](auto t) {
-      em::embed_sums_kernel<decltype(g), decltype(t)><<<dim3(rows_blocks + stretch_blocks, slices), 256, 0, stream>>>(s, rows_blocks, stretches);
+      using G = decltype(g);
+      using T = decltype(t);
+      constexpr int K = em::step_of<G, T>();
+      const int lanes = em::lanes_for(a.dim, K), each = 256 / lanes, vectors = (a.dim + lanes * K - 1) / (lanes * K);
+      const em::SumArgs s{a, begin, order, pieces, lanes};
+      const int stretch_blocks = a.n > em::kFew ? (stretches + each - 1) / each : 0, row_blocks = (a.V + each - 1) / each;
+      auto go = [&](auto kernel, int sl) {
+        kernel<<<stretch_blocks * vectors + row_blocks * ((vectors + sl - 1) / sl), 256, 0, stream>>>(s, stretch_blocks, vectors, row_blocks);
+        return em::done();
+      };
+      int rc;
+      if (a.dim < K) rc = go(em::embed_sums_kernel<G, T, 1, true>, 1);
+      else if (vectors == 1 || static_cast<int64_t>(a.V) * vectors < 16384) rc = go(em::embed_sums_kernel<G, T, 1, false>, 1);
+      else if (vectors == 2) rc = go(em::embed_sums_kernel<G, T, 2, false>, 2);
+      else rc = go(em::embed_sums_kernel<G, T, 4, false>, 4);
+      if (rc != PB_OK || a.n <= em::kFew) return rc;
+      const int groups = em::kJoinThreads / lanes;
+      const dim3 grid((stretches + groups - 1) / groups, vectors);
+      if (a.dim < K) em::embed_join_kernel<T, K, true><<<grid, em::kJoinThreads, 0, stream>>>(s, stretches);
+      else em::embed_join_kernel<T, K, false><<<grid, em::kJoinThreads, 0, stream>>>(s, stretches);
       return em::done();
     });
-  });
-  if (rc != PB_OK || a.n <= em::kFew) return rc;
-  return em::with_type(table_dtype, [&](auto t) {
-    em::embed_join_kernel<decltype(t)><<<dim3(stretch_blocks, slices), 256, 0, stream>>>(s, stretches);
-    return em::done();
   });
 }
 

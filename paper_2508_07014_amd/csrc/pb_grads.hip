@@ -61,13 +61,13 @@ __device__ __forceinline__ void scaled(const GradChunk& c, const GradChunk& out,
   typename E::type* to = static_cast<typename E::type*>(out.x);
   if (static_cast<int>(threadIdx.x) < row.edges) {
     const int i = row.edge_token(threadIdx.x);
-    to[i] = E::down(E::up(row.x[i]) * by);
+    to[i] = E::down(product(E::up(row.x[i]), by));
   }
   for (int v = threadIdx.x; v < row.nv; v += 256) {
     float x[E::N];
     E::unpack(row.vec(v), x);
 #pragma unroll
-    for (int i = 0; i < E::N; ++i) x[i] *= by;
+    for (int i = 0; i < E::N; ++i) x[i] = product(x[i], by);
     store_vector<E>(to + row.token(v, 0), E::pack(x));
   }
 }

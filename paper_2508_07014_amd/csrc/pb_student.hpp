@@ -12,6 +12,14 @@
 
 namespace pb {
 
+// A product that is rounded to fp32 by itself: the compiler would fold it into the conversion to fp16 behind it in some places and
+// not in others, and a row's bits would depend on the length of the row.
+__device__ __forceinline__ float product(float a, float b) {
+  float r = a * b;
+  asm("" : "+v"(r));
+  return r;
+}
+
 constexpr int kMaxDrafts = 63;             // drafted tokens a sequence: with the row behind them a lane each
 constexpr int kMostTokens = 1 << 24;       // looked up in a call
 constexpr int kMostDim = 1 << 16;          // columns of a table

@@ -4,7 +4,7 @@ import numpy as np
 
 U = 2.0 ** -24
 BELOW_1 = np.float32(1 - 2.0 ** -24)
-FEW = 64        # places of a token's positions that are summed one after the other, before those sums are
+FEW = 32        # places of a token's positions that are summed one after the other, before those sums are
 
 
 def probabilities(x, T):
