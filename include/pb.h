@@ -392,7 +392,7 @@ int pb_distill_topk(const void* d_logits, int32_t dtype, int64_t row_stride, int
  *   in fp32, rounded once to out_dtype.  A token id outside [0, vocab_size) is absent: its row is 0.
  * pb_embed_tokens_backward -- the table's gradient from d_grad_out [n_tokens, dim], the gradient on those rows:
  *     d_grad_table[v * table_stride + j] = scale * sum over i with d_tokens[i] = v of d_grad_out[i * grad_stride + j]
- *   summed in fp32, by position within 32 places of the order of positions by token and then over those, rounded once to
+ *   summed in fp32 in an order that the sizes of the call and the places of the token among the tokens decide, rounded once to
  *   table_dtype.  accumulate 0: all vocab_size rows are written, those of tokens that do not occur with 0; accumulate 1: the sum
  *   is added to what is there, and rows of tokens that do not occur are not touched.  Absent tokens' gradients are not looked at.
  *   PB_EINVAL: n_tokens < 0, vocab_size < 1, dim < 1, an unknown dtype, a stride below dim, accumulate neither 0 nor 1, a pointer

@@ -48,7 +48,7 @@ __device__ __forceinline__ void store_vector_of(typename E::type* p, const float
     typedef unsigned any2 __attribute__((ext_vector_type(2), aligned(2)));
     const float both[8] = {x[0], x[1], x[2], x[3], 0.0f, 0.0f, 0.0f, 0.0f};
     const v4u r = E::pack(both);
-    *reinterpret_cast<any2*>(p) = v2u{r.x, r.y};
+    __builtin_nontemporal_store(v2u{r.x, r.y}, reinterpret_cast<any2*>(p));
   }
 }
 
@@ -184,11 +184,24 @@ __device__ __forceinline__ int places(int* counts, int stride, int size, int bas
 }
 
 // Places a wave's keys (of `bits` bits; `in`: the lane has one) at their counters, in the order of the lanes: the lanes with the same key
-// are found bit by bit.
+// are found key by key where there are few, bit by bit otherwise.
 template <typename Put>
 __device__ __forceinline__ void place_keys(int* counters, unsigned key, bool in, int bits, int lane, Put&& put) {
   u64 same = __ballot(in);
   if (same == 0) return;
+  if (__builtin_popcountll(same) <= 4) {
+    for (u64 left = same; left;) {
+      const unsigned k = static_cast<unsigned>(__builtin_amdgcn_readlane(static_cast<int>(key), first_lane(left)));
+      const u64 mine = __ballot(in && key == k);
+      const int to = counters[k];
+      if (in && key == k) put(to + __builtin_popcountll(mine & ((1ull << lane) - 1)));
+      if (lane == 0) counters[k] = to + __builtin_popcountll(mine);
+      left &= ~mine;
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+    }
+    return;
+  }
   for (int b = 0; b < bits; ++b) {
     const bool one = (key >> b) & 1u;
     const u64 ones = __ballot(one);
@@ -458,28 +471,35 @@ __global__ __launch_bounds__(kJoinThreads) void embed_join_kernel(SumArgs s, int
   __syncthreads();
   const Columns<K, 1, NARROW> cols(a.dim, blockIdx.y * s.lanes * K, s.lanes, lane);
   const int64_t row = 2 * static_cast<int64_t>(a.dim);
-  for (int o = 0; o < n_owners; ++o) {  // (each by itself: their order does not matter)
-    const int v = owners[o], i = s.begin[v], c = i / kFew, last = (s.begin[v + 1] + kFew - 1) / kFew;
-    const int share = (last - c + groups - 1) / groups, k1 = min(last, c + (group + 1) * share);
-    int k = c + group * share;
-    float sum[1][K] = {};
-    auto piece = [&](int q) { return s.pieces + q * row + (q == c && i != c * kFew ? a.dim : 0); };
-    constexpr int U = 8;
-    for (; k + U <= k1; k += U) {
+  constexpr int U = 8, kFewPieces = 16;
+  auto add = [&](int first_place, int k, int k1, float (&sum)[1][K]) {  // pieces of stretches k .. k1 - 1
+    const int c = first_place / kFew;
+    for (; k < k1; k += U) {
       float x[U][K];
 #pragma unroll
-      for (int u = 0; u < U; ++u) cols.template load<F32>(piece(k + u), 0, x[u]);
+      for (int u = 0; u < U; ++u) {
+        const int q = min(k + u, k1 - 1);
+        cols.template load<F32>(s.pieces + q * row + (q == c && first_place != c * kFew ? a.dim : 0), 0, x[u]);
+      }
 #pragma unroll
       for (int u = 0; u < U; ++u)
 #pragma unroll
-        for (int e = 0; e < K; ++e) sum[0][e] += x[u][e];
+        for (int e = 0; e < K; ++e) sum[0][e] += k + u < k1 ? x[u][e] : 0.0f;
     }
-    for (; k < k1; ++k) {
-      float x[K];
-      cols.template load<F32>(piece(k), 0, x);
-#pragma unroll
-      for (int e = 0; e < K; ++e) sum[0][e] += x[e];
-    }
+  };
+  for (int o = group; o < n_owners; o += groups) {  // (each by itself: their order does not matter)
+    const int v = owners[o], i = s.begin[v], c = i / kFew, last = (s.begin[v + 1] + kFew - 1) / kFew;
+    if (last - c > kFewPieces) continue;
+    float sum[1][K] = {};
+    add(i, c, last, sum);
+    write_columns<T>(a, cols, v, sum);
+  }
+  for (int o = 0; o < n_owners; ++o) {
+    const int v = owners[o], i = s.begin[v], c = i / kFew, last = (s.begin[v + 1] + kFew - 1) / kFew;
+    if (last - c <= kFewPieces) continue;
+    const int share = (last - c + groups - 1) / groups;
+    float sum[1][K] = {};
+    add(i, c + group * share, min(last, c + (group + 1) * share), sum);
 #pragma unroll
     for (int e = 0; e < K; ++e) shares[e * kJoinThreads + tid] = sum[0][e];
     __syncthreads();
@@ -491,6 +511,58 @@ __global__ __launch_bounds__(kJoinThreads) void embed_join_kernel(SumArgs s, int
     }
     __syncthreads();
   }
+}
+
+// Few tokens on a small table, all in one launch: a workgroup a token (and vectors of its columns) looks through the tokens for its
+// positions, waves in their order, its groups of lanes sum a share of those each, and the first of them those sums.
+constexpr int kSmallTokens = 4096;
+template <typename G, typename T, bool NARROW>
+__global__ __launch_bounds__(256) void embed_small_kernel(SumArgs s) {
+  constexpr int K = step_of<G, T>();
+  __shared__ int list[kSmallTokens], found[4];
+  __shared__ float shares[256 * K];
+  const EmbedGradArgs& a = s.a;
+  const int tid = threadIdx.x, v = blockIdx.x, wave = uniform_i(tid >> 6), lane64 = tid & 63;
+  constexpr int kTurns = kSmallTokens / 256;
+  const int turns = (a.n + 255) / 256, p0 = wave * turns * 64 + lane64;
+  u64 here[kTurns];
+  int t[kTurns], count = 0;
+#pragma unroll
+  for (int k = 0; k < kTurns; ++k) t[k] = k < turns && p0 + 64 * k < a.n ? a.tokens[p0 + 64 * k] : -1;
+#pragma unroll
+  for (int k = 0; k < kTurns; ++k) {
+    here[k] = __ballot(t[k] == v);
+    count += __builtin_popcountll(here[k]);
+  }
+  if (lane64 == 0) found[wave] = count;
+  __syncthreads();
+  int at = 0;
+  for (int w = 0; w < wave; ++w) at += found[w];
+#pragma unroll
+  for (int k = 0; k < kTurns; ++k) {
+    if (t[k] == v) list[at + __builtin_popcountll(here[k] & ((1ull << lane64) - 1))] = p0 + 64 * k;
+    at += __builtin_popcountll(here[k]);
+  }
+  count = found[0] + found[1] + found[2] + found[3];
+  if (count == 0 && a.accumulate) return;
+  __syncthreads();
+  const int lane = tid & (s.lanes - 1), group = tid / s.lanes, groups = 256 / s.lanes;
+  const int share = max(8, (count + groups - 1) / groups);
+  const Columns<K, 1, NARROW> cols(a.dim, blockIdx.y * s.lanes * K, s.lanes, lane);
+  float sum[1][K] = {};
+  SumArgs mine = s;
+  mine.order = list;
+  sum_positions<G>(mine, cols, group * share, min(count, (group + 1) * share), sum);
+  if (count > share) {
+#pragma unroll
+    for (int e = 0; e < K; ++e) shares[e * 256 + tid] = sum[0][e];
+    __syncthreads();
+    if (group == 0)
+      for (int q = 1; q * share < count; ++q)
+#pragma unroll
+        for (int e = 0; e < K; ++e) sum[0][e] += shares[e * 256 + q * s.lanes + lane];
+  }
+  if (group == 0) write_columns<T>(a, cols, v, sum);
 }
 
 template <typename Do>
@@ -545,49 +617,64 @@ Layout layout(int32_t n, int32_t V, int32_t dim) {
 
 int64_t embed_tokens_backward_workspace(int32_t n, int32_t V, int32_t dim) { return em::layout(n, V, dim).bytes; }
 
-int launch_embed_tokens_backward(int grad_dtype, int table_dtype, const EmbedGradArgs& a, void* workspace, hipStream_t stream) {
-  char* ws = static_cast<char*>(workspace);
-  const em::Layout l = em::layout(a.n, a.V, a.dim);
+namespace em {
+template <typename G, typename T>
+struct Shape {
+  static constexpr int K = step_of<G, T>();
+  int lanes, vectors;
+  explicit Shape(int dim) : lanes(lanes_for(dim, K)), vectors((dim + lanes * K - 1) / (lanes * K)) {}
+};
+bool small(int64_t n, int64_t V, int vectors) { return n <= kSmallTokens && V * vectors <= 16384; }
+
+template <typename G, typename T>
+int backward(const EmbedGradArgs& a, char* ws, hipStream_t stream) {
+  const Shape<G, T> shape(a.dim);
+  constexpr int K = Shape<G, T>::K;
+  const int lanes = shape.lanes, each = 256 / lanes, vectors = shape.vectors;
+  const Layout l = layout(a.n, a.V, a.dim);
   int32_t* begin = reinterpret_cast<int32_t*>(ws + l.begin);
   int32_t* order = reinterpret_cast<int32_t*>(ws + l.order);
-  float* pieces = reinterpret_cast<float*>(ws + l.pieces);
-  const int shift = em::shift_for(a.V), ranges = ((a.V - 1) >> shift) + 1, stretches = (a.n + em::kFew - 1) / em::kFew;
-  const size_t counts = static_cast<size_t>(em::kSortWaves) * 4 << shift;
-  if (a.n >= em::kManyTokens) {
+  const SumArgs s{a, begin, order, reinterpret_cast<float*>(ws + l.pieces), lanes};
+  if (small(a.n, a.V, vectors)) {
+    if (a.dim < K) embed_small_kernel<G, T, true><<<dim3(a.V, vectors), 256, 0, stream>>>(s);
+    else embed_small_kernel<G, T, false><<<dim3(a.V, vectors), 256, 0, stream>>>(s);
+    return done();
+  }
+  const int shift = shift_for(a.V), ranges = ((a.V - 1) >> shift) + 1, stretches = (a.n + kFew - 1) / kFew;
+  const size_t counts = static_cast<size_t>(kSortWaves) * 4 << shift;
+  if (a.n >= kManyTokens) {
     unsigned* entries = reinterpret_cast<unsigned*>(ws + l.entries);
     int32_t* starts = reinterpret_cast<int32_t*>(ws + l.starts);
-    const int chunks = (a.n + em::kSplit - 1) / em::kSplit;
-    em::embed_split_kernel<<<chunks, em::kSortThreads, 0, stream>>>(a.tokens, a.n, a.V, shift, ranges, entries, starts);
-    if (em::done() != PB_OK) return PB_EHIP;
-    em::embed_merge_kernel<<<ranges, em::kSortThreads, counts, stream>>>(entries, starts, chunks, a.V, shift, ranges, begin, order);
+    const int chunks = (a.n + kSplit - 1) / kSplit;
+    embed_split_kernel<<<chunks, kSortThreads, 0, stream>>>(a.tokens, a.n, a.V, shift, ranges, entries, starts);
+    if (done() != PB_OK) return PB_EHIP;
+    embed_merge_kernel<<<ranges, kSortThreads, counts, stream>>>(entries, starts, chunks, a.V, shift, ranges, begin, order);
   } else {
-    em::embed_sort_kernel<<<ranges, em::kSortThreads, counts, stream>>>(a.tokens, a.n, a.V, shift, begin, order);
+    embed_sort_kernel<<<ranges, kSortThreads, counts, stream>>>(a.tokens, a.n, a.V, shift, begin, order);
   }
-  if (em::done() != PB_OK) return PB_EHIP;
+  if (done() != PB_OK) return PB_EHIP;
+  const int stretch_blocks = a.n > kFew ? (stretches + each - 1) / each : 0, row_blocks = (a.V + each - 1) / each;
+  auto sums = [&](auto kernel, int sl) {
+    kernel<<<stretch_blocks * vectors + row_blocks * ((vectors + sl - 1) / sl), 256, 0, stream>>>(s, stretch_blocks, vectors, row_blocks);
+    return done();
+  };
+  int rc;
+  if (a.dim < K) rc = sums(embed_sums_kernel<G, T, 1, true>, 1);
+  else if (vectors == 1) rc = sums(embed_sums_kernel<G, T, 1, false>, 1);
+  else if (vectors == 2) rc = sums(embed_sums_kernel<G, T, 2, false>, 2);
+  else rc = sums(embed_sums_kernel<G, T, 4, false>, 4);
+  if (rc != PB_OK || stretch_blocks == 0) return rc;
+  const int groups = kJoinThreads / lanes;
+  const dim3 grid((stretches + groups - 1) / groups, vectors);
+  if (a.dim < K) embed_join_kernel<T, K, true><<<grid, kJoinThreads, 0, stream>>>(s, stretches);
+  else embed_join_kernel<T, K, false><<<grid, kJoinThreads, 0, stream>>>(s, stretches);
+  return done();
+}
+}  // namespace em
+
+int launch_embed_tokens_backward(int grad_dtype, int table_dtype, const EmbedGradArgs& a, void* workspace, hipStream_t stream) {
   return em::with_type(grad_dtype, [&](auto g) {
-    return em::with_type(table_dtype, [&](auto t) {
-      using G = decltype(g);
-      using T = decltype(t);
-      constexpr int K = em::step_of<G, T>();
-      const int lanes = em::lanes_for(a.dim, K), each = 256 / lanes, vectors = (a.dim + lanes * K - 1) / (lanes * K);
-      const em::SumArgs s{a, begin, order, pieces, lanes};
-      const int stretch_blocks = a.n > em::kFew ? (stretches + each - 1) / each : 0, row_blocks = (a.V + each - 1) / each;
-      auto go = [&](auto kernel, int sl) {
-        kernel<<<stretch_blocks * vectors + row_blocks * ((vectors + sl - 1) / sl), 256, 0, stream>>>(s, stretch_blocks, vectors, row_blocks);
-        return em::done();
-      };
-      int rc;
-      if (a.dim < K) rc = go(em::embed_sums_kernel<G, T, 1, true>, 1);
-      else if (vectors == 1 || static_cast<int64_t>(a.V) * vectors < 16384) rc = go(em::embed_sums_kernel<G, T, 1, false>, 1);
-      else if (vectors == 2) rc = go(em::embed_sums_kernel<G, T, 2, false>, 2);
-      else rc = go(em::embed_sums_kernel<G, T, 4, false>, 4);
-      if (rc != PB_OK || a.n <= em::kFew) return rc;
-      const int groups = em::kJoinThreads / lanes;
-      const dim3 grid((stretches + groups - 1) / groups, vectors);
-      if (a.dim < K) em::embed_join_kernel<T, K, true><<<grid, em::kJoinThreads, 0, stream>>>(s, stretches);
-      else em::embed_join_kernel<T, K, false><<<grid, em::kJoinThreads, 0, stream>>>(s, stretches);
-      return em::done();
-    });
+    return em::with_type(table_dtype, [&](auto t) { return em::backward<decltype(g), decltype(t)>(a, static_cast<char*>(workspace), stream); });
   });
 }
 

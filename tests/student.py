@@ -71,8 +71,9 @@ def table_gradient(g, tokens, V, scale):
     total, size, count = np.zeros((V, g.shape[1])), np.zeros((V, g.shape[1])), np.bincount(tokens[inside], minlength=V)
     np.add.at(total, tokens[inside], g[inside])
     np.add.at(size, tokens[inside], np.abs(g[inside]))
-    # (a sum of at most FEW terms one after the other, then of a piece each FEW places; the product with the scale)
-    chain = np.minimum(count, FEW) + count // FEW + 3
+    # (a sum of at most FEW terms one after the other, then of a piece each FEW places; or, few tokens on a small table, a quarter of the
+    # terms at most one after the other, then of up to 256 such shares; the product with the scale)
+    chain = np.maximum(np.minimum(count, FEW) + count // FEW, np.minimum(count, count // 4 + 8) + 256 * (len(tokens) <= 4096)) + 3
     return total * scale, size * abs(scale) * U * chain[:, None], count
 
 
