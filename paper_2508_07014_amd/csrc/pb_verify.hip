@@ -5,8 +5,14 @@
 //   v whose sum over all tokens up to it exceeds w times the sum over all.
 //
 // A drawn token is a border between two of V sums: with sums in fp32, off by 1e-7 of the whole, one draw in a hundred from a
-// row of 131072 tokens would be another token than the definition's.  So exponentials and sums are in 64 bits throughout, which
-// the chip's vector units take at the rate of fp32.
+// row of 131072 tokens would be another token than the definition's.  So the row that decides is summed in 64 bits.  The other
+// rows are only compared: their sums in fp32 decide wherever u q lies apart from p by more than those can be off, and where it
+// does not the two rows are summed in 64 bits as well.
+//
+// Long rows take three launches: sums of all rows, a wave a part; then the decision and the deciding row's sums, several workgroups a
+// sequence; then the draw.  max(p - q, 0) needs the ratio of the two rows' sums, which the second launch has in fp32 only:
+// with it, it says which tokens lie above the line e_p = ratio e_q and sums both sides of those, so that the third can put
+// the exact ratio in, and the few slices where a token lies too near to the line are summed again there.
 #include <algorithm>
 
 #include "pb_logit_rows.hpp"
@@ -18,13 +24,14 @@ namespace vd {
 using namespace lr;
 using wv::first_lane;
 
-// Of one row, or of a part of it: the largest element and the sum of 2^((x - m) c); bad: it holds a NaN or +inf.
+// Of a part of a row: the largest element (-inf: nothing) and the sum of 2^((x - m) c) in fp32, NaN where it holds a NaN or +inf.
 struct Sums {
-  float m;
-  int bad;
-  double s;
+  float m, s;
 };
-
+// How far such a sum is off at most, relative to itself: an exponent t by 3 roundings of 2^-24, that is 2.1 |t| 2^-24 of its term, and
+// the mean of |t| over a row of V tokens is log2 V < 19 at most; 2 of the exponential; 18 additions one after the other (8 of vectors, 3
+// in a vector, 6 in a wave, the edge).  60 x 2^-24 < 2^-18; twice that for a ratio of two, and as much again for good measure.
+constexpr double kUnsure = 0x1p-16;
 constexpr double kNothing = 0x1p-40;     // a rest of the target's mass below this is none (equal rows differ by their roundings)
 constexpr double kNoWeight = 0x1p-960;   // weights below this, masked tokens' among them, are none
 
@@ -77,39 +84,35 @@ __device__ __forceinline__ double wave_sum64(double v) { return readlane64(wave_
 
 // Part of a row, by a wave: vectors first .. first + 64 EACH - 1, and the row's edge where `edge`.
 template <typename E, int EACH>
-__device__ __forceinline__ Sums part_sums(const Row<E>& row, int first, bool edge, double c, int lane) {
+__device__ __forceinline__ Sums part_sums(const Row<E>& row, int first, bool edge, double c64, int lane) {
   v4u raw[EACH];
-  float m = -INFINITY, xe = -INFINITY;
+  float xe = -INFINITY;
 #pragma unroll
   for (int u = 0; u < EACH; ++u) {
     const int v = first + 64 * u + lane;
     raw[u] = v < row.nv ? row.vec(v) : E::nothing();
   }
   if (edge && lane < row.edges) xe = E::up(row.x[row.edge_token(lane)]);
-  bool bad = xe != xe;
-  m = fmaxf(m, xe);
+  float m = fmaxf(-INFINITY, xe);
 #pragma unroll
   for (int u = 0; u < EACH; ++u) {
     float x[E::N];
     E::unpack(raw[u], x);
-#pragma unroll
-    for (int i = 0; i < E::N; i += 2) bad |= __builtin_isunordered(x[i], x[i + 1]);
     m = fmaxf(m, vec_max(x));
   }
   m = wave_max(m);
-  bad = __ballot(bad) != 0 || m == INFINITY;
-  if (m == -INFINITY || bad) return Sums{m, bad, 0.0};
-  const Scale k = scale_of(c);
-  double s = edge && lane < row.edges ? weight(xe, m, k) : 0.0;
+  const float c = static_cast<float>(c64), from = m == -INFINITY ? 0.0f : m;  // (inf - inf is a NaN, as is what a NaN leaves)
+  float s = exp2_fast((xe - from) * c);
 #pragma unroll
   for (int u = 0; u < EACH; ++u) {
     if (first + 64 * u >= row.nv) break;
     float x[E::N];
     E::unpack(raw[u], x);
 #pragma unroll
-    for (int i = 0; i < E::N; ++i) s += weight(x[i], m, k);
+    for (int i = 0; i < E::N; ++i) x[i] = exp2_fast((x[i] - from) * c);
+    s += vec_sum(x);
   }
-  return Sums{m, 0, wave_sum64(s)};
+  return Sums{m, wave_sum(s)};
 }
 
 // The rows of a sequence: 0 .. n the target's, n + 1 .. 2 n the draft's.
@@ -153,17 +156,16 @@ __global__ __launch_bounds__(256) void verify_sums_kernel(VerifyArgs a, int rows
 struct Verdict {
   int k;           // accepted tokens
   int none;        // no token is drawn: the target's row there is nothing but -inf, or it, or the draft's, holds a NaN or +inf
-  int refused;     // a drafted token was refused: the draft's row counts
-  int token;       // that one
-  float pm, qm;    // of the rows that decide
-  double pw, qw;   // 1 / their sums (the draft's: 0 for a row of nothing but -inf)
-  double ps;       // the target's sum
+  int refused;     // the token that was refused, -1: none
+  float pm, qm;    // largest elements of the rows that decide; qm = -inf: no draft's row counts
+  double ratio;    // of their sums, about
 };
 
 constexpr int kMaxRows = 2 * kMaxDrafts + 1;
 struct RowSums {
   float m[kMaxRows];
   double s[kMaxRows];
+  double turn[16];  // a place a wave
 };
 
 __device__ __forceinline__ double share(float x, float m, double s, double c) {  // (a row of nothing but -inf: s = 0; a marked one: NaN)
@@ -175,34 +177,75 @@ __device__ __forceinline__ float log_share(float x, float m, double s, double c)
   return static_cast<float>(((static_cast<double>(x) - static_cast<double>(m)) * c - log2(s)) * 0.69314718055994530942);
 }
 
+// Elements v .. v + N - 1 of a row of V; -inf past it.
+template <typename E>
+__device__ __forceinline__ void load_at(const typename E::type* x, int v, int V, float (&xs)[E::N]) {
+  if (v + E::N <= V) {
+    E::unpack(any_vector<E>(x + v), xs);
+  } else {
+#pragma unroll
+    for (int i = 0; i < E::N; ++i) xs[i] = v + i < V ? E::up(x[v + i]) : -INFINITY;
+  }
+}
+// A slice of a row: 64 vectors from a whole number of them on, in a wave.
+template <typename E>
+__host__ __device__ __forceinline__ int slices_of(int V) { return (V + 64 * E::N - 1) / (64 * E::N); }
+template <int N>
+__device__ __forceinline__ double lane_sum(const double (&w)[N]) {
+  double s = w[0];
+#pragma unroll
+  for (int i = 1; i < N; ++i) s += w[i];
+  return s;
+}
+
+// A row's sum in 64 bits, by the whole workgroup.
+template <typename E, int WAVES>
+__device__ __forceinline__ double row_sum(const typename E::type* x, int V, float m, double c, double (&turn)[16]) {
+  const int lane = threadIdx.x & 63, wave = uniform_i(threadIdx.x >> 6);
+  const Scale k = scale_of(c);
+  double s = 0.0;
+  for (int slice = wave; slice < slices_of<E>(V); slice += WAVES) {
+    float xs[E::N];
+    load_at<E>(x, (slice * 64 + lane) * E::N, V, xs);
+#pragma unroll
+    for (int i = 0; i < E::N; ++i) s += weight(xs[i], m, k);
+  }
+  s = wave_sum64(s);
+  __syncthreads();
+  if (lane == 0) turn[wave] = s;
+  __syncthreads();
+  s = 0.0;
+  for (int w = 0; w < WAVES; ++w) s += turn[w];
+  return s;
+}
+
 // Joins the parts of all rows (waves of the workgroup take turns), then decides, the same in every wave.  Writes the accepted tokens
 // if `writes`, in the last wave.
 template <typename E, int WAVES>
 __device__ __forceinline__ Verdict decide(const VerifyArgs& a, int64_t b, const Sums* sums, int rows, int parts, RowSums& joined, bool writes) {
   const int lane = threadIdx.x & 63, wave = uniform_i(threadIdx.x >> 6);
+  const typename E::type* target = static_cast<const typename E::type*>(a.target) + b * a.target_seq;
+  const typename E::type* draft = a.draft ? static_cast<const typename E::type*>(a.draft) + b * a.draft_seq : nullptr;
   int count;
   const int t = drafted_tokens(a, b, lane, &count);
   float xt = 0.0f, yt = 0.0f, u = 0.0f;
   if (lane < count) {
-    xt = E::up((static_cast<const typename E::type*>(a.target) + b * a.target_seq + lane * a.target_row)[t]);
-    if (a.draft) yt = E::up((static_cast<const typename E::type*>(a.draft) + b * a.draft_seq + lane * a.draft_row)[t]);
+    xt = E::up(target[lane * a.target_row + t]);
+    if (draft) yt = E::up(draft[lane * a.draft_row + t]);
     u = fminf(fmaxf(a.numbers[b * (a.n + 1) + lane], 0.0f), 0x1.fffffep-1f);
   }
   for (int j = wave; j < rows; j += WAVES) {
     if (j <= a.n ? j > count : j - a.n - 1 >= count) continue;
     const double c = j <= a.n ? a.target_c : a.draft_c;
     float m = -INFINITY;
-    bool bad = false;
-    for (int p = lane; p < parts; p += 64) {
-      m = fmaxf(m, sums[j * parts + p].m);
-      bad |= sums[j * parts + p].bad != 0;
-    }
+    for (int p = lane; p < parts; p += 64) m = fmaxf(m, sums[j * parts + p].m);
     m = wave_max(m);
     double s = 0.0;
-    if (m != -INFINITY)
-      for (int p = lane; p < parts; p += 64) s += sums[j * parts + p].s * weight(sums[j * parts + p].m, m, scale_of(c));
+    for (int p = lane; p < parts; p += 64) {
+      const Sums part = sums[j * parts + p];
+      s += part.m == -INFINITY ? static_cast<double>(part.s) : static_cast<double>(part.s) * weight(part.m, m, scale_of(c));
+    }
     s = wave_sum64(s);
-    if (__ballot(bad) != 0) s = NAN;
     if (lane == 0) {
       joined.m[j] = m;
       joined.s[j] = s;
@@ -210,25 +253,42 @@ __device__ __forceinline__ Verdict decide(const VerifyArgs& a, int64_t b, const 
   }
   __syncthreads();
   bool takes = false;
-  if (lane < count) {
-    const double p = share(xt, joined.m[lane], joined.s[lane], a.target_c);
-    const double q = a.draft ? share(yt, joined.m[a.n + 1 + lane], joined.s[a.n + 1 + lane], a.draft_c) : 1.0;
-    takes = static_cast<double>(u) * q < p;  // (false for NaN)
+  for (u64 exact = 0;;) {
+    bool unsure = false;
+    takes = false;
+    if (lane < count) {
+      const double p = share(xt, joined.m[lane], joined.s[lane], a.target_c);
+      const double q = draft ? share(yt, joined.m[a.n + 1 + lane], joined.s[a.n + 1 + lane], a.draft_c) : 1.0;
+      const double uq = static_cast<double>(u) * q;
+      takes = uq < p;  // (false for NaN)
+      unsure = p > 0.0 && fabs(uq - p) <= p * kUnsure && !((exact >> lane) & 1u);
+    }
+    const int stop = first_lane(~__ballot(takes || unsure));  // (the first that is refused for sure; lane 63 takes none)
+    const u64 open = __ballot(unsure) & ((1ull << stop) - 1);
+    if (open == 0) break;
+    const int i = first_lane(open);
+    const double ps = row_sum<E, WAVES>(target + i * a.target_row, a.V, joined.m[i], a.target_c, joined.turn);
+    const double qs = draft ? row_sum<E, WAVES>(draft + i * a.draft_row, a.V, joined.m[a.n + 1 + i], a.draft_c, joined.turn) : 0.0;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      if (joined.m[i] != -INFINITY) joined.s[i] = ps;
+      if (draft && joined.m[a.n + 1 + i] != -INFINITY) joined.s[a.n + 1 + i] = qs;
+    }
+    exact |= 1ull << i;
+    __syncthreads();
   }
   Verdict r;
-  r.k = first_lane(~__ballot(takes));  // (lane 63 takes none)
-  r.refused = r.k < count;
-  r.token = __builtin_amdgcn_readlane(t, r.k);
+  r.k = first_lane(~__ballot(takes));
+  r.refused = r.k < count ? __builtin_amdgcn_readlane(t, r.k) : -1;
+  const double ps = joined.s[r.k];
   r.pm = joined.m[r.k];
-  r.ps = joined.s[r.k];
-  r.pw = 1.0 / r.ps;
   r.qm = -INFINITY;
-  r.qw = 0.0;
-  r.none = r.pm == -INFINITY || r.ps != r.ps;
-  if (r.refused && a.draft) {
+  r.ratio = 0.0;
+  r.none = r.pm == -INFINITY || ps != ps;
+  if (r.refused >= 0 && draft) {
     const double qs = joined.s[a.n + 1 + r.k];
     r.qm = joined.m[a.n + 1 + r.k];
-    r.qw = r.qm == -INFINITY ? 0.0 : 1.0 / qs;
+    if (r.qm != -INFINITY) r.ratio = ps / qs;
     r.none |= qs != qs;
   }
   if (writes && wave == WAVES - 1) {
@@ -241,75 +301,52 @@ __device__ __forceinline__ Verdict decide(const VerifyArgs& a, int64_t b, const 
   return r;
 }
 
-// The row that decides, as what a token may be drawn from: max(p - q, 0), or p where `whole`.
+// The rows that decide, as weights.
 template <typename E>
 struct Rest {
   const typename E::type* x;
   const typename E::type* y;  // null: no draft's row counts
   int V, barred;              // the token that a draft without rows was sure of, -1: none
   float pm, qm;
-  double pw, qw;
   Scale pk, qk;
-  // Elements v .. v + N - 1 (0 past the row).
-  __device__ __forceinline__ void at(int v, double (&r)[E::N]) const {
+  __device__ __forceinline__ Rest(const VerifyArgs& a, int64_t b, const Verdict& d)
+      : x(static_cast<const typename E::type*>(a.target) + b * a.target_seq + d.k * a.target_row),
+        y(d.qm == -INFINITY ? nullptr : static_cast<const typename E::type*>(a.draft) + b * a.draft_seq + d.k * a.draft_row),
+        V(a.V), barred(a.draft ? -1 : d.refused), pm(d.pm), qm(d.qm), pk(scale_of(a.target_c)), qk(scale_of(a.draft ? a.draft_c : 1.0)) {}
+  // Of elements v .. v + N - 1 (next to nothing past the row).
+  __device__ __forceinline__ void weights(int v, double (&p)[E::N], double (&q)[E::N]) const {
     float xs[E::N], ys[E::N];
-    if (v + E::N <= V) {
-      E::unpack(any_vector<E>(x + v), xs);
-      if (y) E::unpack(any_vector<E>(y + v), ys);
-    } else {
-#pragma unroll
-      for (int i = 0; i < E::N; ++i) {
-        xs[i] = v + i < V ? E::up(x[v + i]) : -INFINITY;
-        if (y) ys[i] = v + i < V ? E::up(y[v + i]) : -INFINITY;
-      }
-    }
+    load_at<E>(x, v, V, xs);
+    if (y) load_at<E>(y, v, V, ys);
 #pragma unroll
     for (int i = 0; i < E::N; ++i) {
-      double p = weight(xs[i], pm, pk) * pw;
-      if (y) p -= weight(ys[i], qm, qk) * qw;
-      r[i] = p > kNoWeight && v + i != barred ? p : 0.0;
+      p[i] = weight(xs[i], pm, pk);
+      q[i] = y ? weight(ys[i], qm, qk) : 0.0;
+    }
+  }
+  // What a token may be drawn from: p - ratio q where that is more than nothing, in units of the target's largest weight; all of p
+  // where `whole`.
+  __device__ __forceinline__ void rest(int v, const double (&p)[E::N], const double (&q)[E::N], double ratio, bool whole, double (&r)[E::N]) const {
+#pragma unroll
+    for (int i = 0; i < E::N; ++i) {
+      const double d = whole ? p[i] : fma(-ratio, q[i], p[i]);
+      r[i] = d > kNoWeight && (whole || v + i != barred) ? d : 0.0;
     }
   }
 };
-template <typename E>
-__device__ __forceinline__ Rest<E> rest_of(const VerifyArgs& a, int64_t b, const Verdict& d, bool whole) {
-  Rest<E> r;
-  r.x = static_cast<const typename E::type*>(a.target) + b * a.target_seq + d.k * a.target_row;
-  const bool held = d.refused && !whole;
-  r.y = held && a.draft && d.qw > 0.0 ? static_cast<const typename E::type*>(a.draft) + b * a.draft_seq + d.k * a.draft_row : nullptr;
-  r.barred = held && !a.draft ? d.token : -1;
-  r.V = a.V;
-  r.pm = d.pm;
-  r.qm = d.qm;
-  r.pw = d.pw;
-  r.qw = d.qw;
-  r.pk = scale_of(a.target_c);
-  r.qk = scale_of(a.draft ? a.draft_c : 1.0);
-  return r;
-}
-
-// A slice of the row that decides: 64 vectors from a whole number of them on, in a wave.
-template <typename E>
-__host__ __device__ __forceinline__ int slices_of(int V) { return (V + 64 * E::N - 1) / (64 * E::N); }
-template <int N>
-__device__ __forceinline__ double slice_sum(const double (&w)[N]) {
-  double s = w[0];
-#pragma unroll
-  for (int i = 1; i < N; ++i) s += w[i];
-  return wave_sum64(s);
-}
 
 // Where in the sums of the slices the drawn token lies, by any wave (the same in each).
 struct Place {
-  int slice;              // -1: there is no mass
+  int slice;
   double before, target;  // what lies ahead of the slice, what the token's sum is to pass
 };
-__device__ __forceinline__ Place place_of(const double* sums, int slices, float w, double* total, int lane) {
+__device__ __forceinline__ double sum_of(const double* sums, int n, int lane) {
   double all = 0.0;
-  for (int s = lane; s < slices; s += 64) all += sums[s];
-  all = wave_sum64(all);
-  *total = all;
-  Place r{-1, 0.0, static_cast<double>(fminf(fmaxf(w, 0.0f), 0x1.fffffep-1f)) * all};
+  for (int s = lane; s < n; s += 64) all += sums[s];
+  return wave_sum64(all);
+}
+__device__ __forceinline__ Place place_of(const double* sums, int slices, float w, double all, int lane) {
+  Place r{0, 0.0, static_cast<double>(fminf(fmaxf(w, 0.0f), 0x1.fffffep-1f)) * all};
   double ahead = 0.0;
   for (int s0 = 0; s0 < slices; s0 += 64) {
     const double mine = s0 + lane < slices ? sums[s0 + lane] : 0.0;
@@ -330,9 +367,7 @@ __device__ __forceinline__ Place place_of(const double* sums, int slices, float 
 // roundings leave none.
 template <int N>
 __device__ __forceinline__ int find_in_slice(const double (&w)[N], const Place& at, int lane) {
-  double s = w[0];
-#pragma unroll
-  for (int i = 1; i < N; ++i) s += w[i];
+  const double s = lane_sum(w);
   double upto = at.before + (wave_upto64(s) - s);
   int found = -1, any = -1;
   const int v = (at.slice * 64 + lane) * N;
@@ -348,58 +383,81 @@ __device__ __forceinline__ int find_in_slice(const double (&w)[N], const Place& 
 }
 
 template <typename E>
-__device__ __forceinline__ void write_drawn(const VerifyArgs& a, int64_t b, const Verdict& d, int token, int lane) {
+__device__ __forceinline__ void write_drawn(const VerifyArgs& a, int64_t b, const Verdict& d, double ps, int token, int lane) {
   if (lane != 0) return;
   const int64_t at = b * (a.n + 1) + d.k;
   a.out[at] = token;
-  if (a.logp) a.logp[at] = log_share(E::up((static_cast<const typename E::type*>(a.target) + b * a.target_seq + d.k * a.target_row)[token]), d.pm, d.ps, a.target_c);
+  if (a.logp) a.logp[at] = token < 0 ? NAN : log_share(E::up((static_cast<const typename E::type*>(a.target) + b * a.target_seq + d.k * a.target_row)[token]), d.pm, ps, a.target_c);
 }
 
-// Draws for a sequence, by a workgroup that goes through the slices of the row that decides (LDS: slice_sums, again).
+// Rows of up to WAVES * HELD slices: a workgroup a sequence holds the rows that decide in registers.
+constexpr int kHeld = 2;
+template <int WAVES>
+struct DrawShared {
+  double p[WAVES], q[WAVES], slices[WAVES * kHeld];
+};
 template <typename E, int WAVES>
-__device__ __forceinline__ void draw(const VerifyArgs& a, int64_t b, const Verdict& d, bool whole, double* slice_sums) {
+__device__ __forceinline__ void draw_held(const VerifyArgs& a, int64_t b, const Verdict& d, DrawShared<WAVES>& shared) {
   const int lane = threadIdx.x & 63, wave = uniform_i(threadIdx.x >> 6), slices = slices_of<E>(a.V);
   const float number = a.numbers[b * (a.n + 1) + a.n];
-  for (;; whole = true) {
-    const Rest<E> r = rest_of<E>(a, b, d, whole);
-    double w[E::N];
-    for (int s = wave; s < slices; s += WAVES) {
-      r.at((s * 64 + lane) * E::N, w);
-      const double v = slice_sum(w);
-      if (lane == 0) slice_sums[s] = v;
+  const Rest<E> r(a, b, d);
+  double p[kHeld][E::N], q[kHeld][E::N], ps = 0.0, qs = 0.0;
+#pragma unroll
+  for (int h = 0; h < kHeld; ++h) {
+    if (wave + h * WAVES >= slices) break;
+    r.weights(((wave + h * WAVES) * 64 + lane) * E::N, p[h], q[h]);
+    ps += lane_sum(p[h]);
+    qs += lane_sum(q[h]);
+  }
+  ps = wave_sum64(ps);
+  qs = wave_sum64(qs);
+  if (lane == 0) {
+    shared.p[wave] = ps;
+    shared.q[wave] = qs;
+  }
+  __syncthreads();
+  ps = wave_sum64(lane < WAVES ? shared.p[lane] : 0.0);
+  qs = wave_sum64(lane < WAVES ? shared.q[lane] : 0.0);
+  const double ratio = r.y ? ps / qs : 0.0;
+  for (bool whole = d.refused < 0;; whole = true) {
+    double w[kHeld][E::N];
+#pragma unroll
+    for (int h = 0; h < kHeld; ++h) {
+      const int s = wave + h * WAVES;
+      if (s >= slices) break;
+      r.rest((s * 64 + lane) * E::N, p[h], q[h], ratio, whole, w[h]);
+      const double v = wave_sum64(lane_sum(w[h]));
+      if (lane == 0) shared.slices[s] = v;
     }
     __syncthreads();
-    double total;
-    const Place at = place_of(slice_sums, slices, number, &total, lane);
-    if (!whole && !(total > kNothing)) {  // (the same in every wave)
+    const double all = sum_of(shared.slices, slices, lane);
+    if (!whole && !(all > kNothing * ps)) {  // (the same in every wave)
       __syncthreads();
       continue;
     }
-    if (at.slice % WAVES == wave) {  // (some slice has mass: the row's largest element does)
-      if (slices > WAVES) r.at((at.slice * 64 + lane) * E::N, w);  // (otherwise it is the one that it has)
-      write_drawn<E>(a, b, d, find_in_slice(w, at, lane), lane);
-    }
+    const Place at = place_of(shared.slices, slices, number, all, lane);
+#pragma unroll
+    for (int h = 0; h < kHeld; ++h)
+      if (at.slice == wave + h * WAVES) write_drawn<E>(a, b, d, ps, find_in_slice(w[h], at, lane), lane);
     return;
   }
 }
-
-// The rest of a sequence, a workgroup each: decides and draws.
 template <typename E, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void verify_draw_kernel(VerifyArgs a, int rows, int parts, const Sums* sums) {
   __shared__ RowSums joined;
-  __shared__ double slice_sums[kLogitsMaxV / (64 * E::N) + 1];
+  __shared__ DrawShared<WAVES> shared;
   const int64_t b = blockIdx.x;
   const Verdict d = decide<E, WAVES>(a, b, sums + b * rows * parts, rows, parts, joined, true);
-  if (!d.none) draw<E, WAVES>(a, b, d, !d.refused, slice_sums);
+  if (!d.none) draw_held<E, WAVES>(a, b, d, shared);
 }
 
 // All of a sequence in one workgroup, where its rows have few parts.
-constexpr int kSmallItems = 64;
+constexpr int kSmallItems = 32;
 template <typename E, int WAVES, int EACH>
 __global__ __launch_bounds__(64 * WAVES) void verify_small_kernel(VerifyArgs a, int rows, int parts) {
   __shared__ RowSums joined;
   __shared__ Sums sums[kSmallItems];
-  __shared__ double slice_sums[kSmallItems * EACH + 1];
+  __shared__ DrawShared<WAVES> shared;
   const int lane = threadIdx.x & 63, wave = uniform_i(threadIdx.x >> 6);
   const int64_t b = blockIdx.x;
   int count;
@@ -412,42 +470,110 @@ __global__ __launch_bounds__(64 * WAVES) void verify_small_kernel(VerifyArgs a, 
   }
   __syncthreads();
   const Verdict d = decide<E, WAVES>(a, b, sums, rows, parts, joined, true);
-  if (!d.none) draw<E, WAVES>(a, b, d, !d.refused, slice_sums);
+  if (!d.none) draw_held<E, WAVES>(a, b, d, shared);
 }
 
 // Long rows: several workgroups a sequence decide, each for itself, and sum their slices; the first leaves the verdict.
+struct Slice {
+  double p, q;      // sums of the weights
+  double above;     // of p - ratio q over the tokens above the line (the draft's token without rows aside), with the verdict's ratio
+  double above_q;   // of q over those; NaN: a token lies too near to the line
+};
 constexpr int kRestWaves = 16;
 template <typename E>
-__global__ __launch_bounds__(64 * kRestWaves) void verify_rest_kernel(VerifyArgs a, int rows, int parts, const Sums* sums, Verdict* verdicts, double* slice_sums) {
+__global__ __launch_bounds__(64 * kRestWaves) void verify_rest_kernel(VerifyArgs a, int rows, int parts, const Sums* sums, Verdict* verdicts, Slice* out) {
   __shared__ RowSums joined;
   const int lane = threadIdx.x & 63, wave = uniform_i(threadIdx.x >> 6), slices = slices_of<E>(a.V);
   const int64_t b = blockIdx.y;
   const Verdict d = decide<E, kRestWaves>(a, b, sums + b * rows * parts, rows, parts, joined, blockIdx.x == 0);
   if (blockIdx.x == 0 && threadIdx.x == 0) verdicts[b] = d;
   if (d.none) return;
-  const Rest<E> r = rest_of<E>(a, b, d, !d.refused);
+  const Rest<E> r(a, b, d);
   for (int s = blockIdx.x * kRestWaves + wave; s < slices; s += gridDim.x * kRestWaves) {
-    double w[E::N];
-    r.at((s * 64 + lane) * E::N, w);
-    const double v = slice_sum(w);
-    if (lane == 0) slice_sums[b * slices + s] = v;
+    const int v = (s * 64 + lane) * E::N;
+    double p[E::N], q[E::N];
+    r.weights(v, p, q);
+    Slice to{lane_sum(p), 0.0, 0.0, 0.0};
+    if (r.y) {
+      double near = INFINITY;
+      to.q = lane_sum(q);
+#pragma unroll
+      for (int i = 0; i < E::N; ++i) {
+        const double rest = fma(-d.ratio, q[i], p[i]);
+        near = fmin(near, fma(-kUnsure * d.ratio, q[i], fabs(rest)));
+        to.above += fmax(rest, 0.0);
+        to.above_q += rest > 0.0 ? q[i] : 0.0;
+      }
+      to.q = wave_sum64(to.q);
+      to.above = wave_sum64(to.above);
+      to.above_q = wave_sum64(to.above_q);
+      if (__ballot(near <= 0.0) != 0) to.above_q = NAN;
+    } else if (r.barred >= 0) {
+      double w[E::N];
+      r.rest(v, p, q, 0.0, false, w);
+      to.above = wave_sum64(lane_sum(w));
+    }
+    to.p = wave_sum64(to.p);
+    if (lane == 0) out[b * slices + s] = to;
   }
 }
-// And a wave a sequence draws.
+// And a workgroup a sequence draws.
+constexpr int kPickWaves = 4;
 template <typename E>
-__global__ __launch_bounds__(256) void verify_pick_kernel(VerifyArgs a, const Verdict* verdicts, const double* slice_sums) {
-  __shared__ double whole_sums[kLogitsMaxV / (64 * E::N) + 1];
+__global__ __launch_bounds__(64 * kPickWaves) void verify_pick_kernel(VerifyArgs a, const Verdict* verdicts, const Slice* in) {
+  __shared__ double sums[kLogitsMaxV / (64 * E::N) + 1], turn[2 * kPickWaves];
   const int lane = threadIdx.x & 63, wave = uniform_i(threadIdx.x >> 6), slices = slices_of<E>(a.V);
   const int64_t b = blockIdx.x;
   const Verdict d = verdicts[b];
   if (d.none) return;
-  double total;
-  const Place at = place_of(slice_sums + b * slices, slices, a.numbers[b * (a.n + 1) + a.n], &total, lane);
-  if (d.refused && !(total > kNothing)) return draw<E, 4>(a, b, d, true, whole_sums);
-  if (wave != 0) return;
-  double w[E::N];
-  rest_of<E>(a, b, d, !d.refused).at((at.slice * 64 + lane) * E::N, w);
-  write_drawn<E>(a, b, d, find_in_slice(w, at, lane), lane);
+  in += b * slices;
+  const float number = a.numbers[b * (a.n + 1) + a.n];
+  double ps = 0.0, qs = 0.0;
+  for (int s = threadIdx.x; s < slices; s += 64 * kPickWaves) {
+    ps += in[s].p;
+    qs += in[s].q;
+  }
+  ps = wave_sum64(ps);
+  qs = wave_sum64(qs);
+  if (lane == 0) {
+    turn[wave] = ps;
+    turn[kPickWaves + wave] = qs;
+  }
+  __syncthreads();
+  ps = (turn[0] + turn[1]) + (turn[2] + turn[3]);
+  qs = (turn[4] + turn[5]) + (turn[6] + turn[7]);
+  const Rest<E> r(a, b, d);
+  const double ratio = r.y ? ps / qs : 0.0;
+  bool whole = d.refused < 0 || (!r.y && r.barred < 0);  // (a draft's row of nothing but -inf takes nothing away)
+  for (;; whole = true) {
+    for (int s0 = wave * 64; s0 < slices; s0 += 64 * kPickWaves) {
+      double v = 0.0;
+      if (s0 + lane < slices) v = whole ? in[s0 + lane].p : r.y ? fma(d.ratio - ratio, in[s0 + lane].above_q, in[s0 + lane].above) : in[s0 + lane].above;
+      for (u64 left = __ballot(v != v); left; left &= left - 1) {
+        const int at = first_lane(left), from = ((s0 + at) * 64 + lane) * E::N;
+        double p[E::N], q[E::N], w[E::N];
+        r.weights(from, p, q);
+        r.rest(from, p, q, ratio, false, w);
+        const double again = wave_sum64(lane_sum(w));
+        if (lane == at) v = again;
+      }
+      if (s0 + lane < slices) sums[s0 + lane] = v > kNoWeight ? v : 0.0;
+    }
+    __syncthreads();
+    const double all = sum_of(sums, slices, lane);
+    if (!whole && !(all > kNothing * ps)) {
+      __syncthreads();
+      continue;
+    }
+    if (wave != 0) return;
+    const Place at = place_of(sums, slices, number, all, lane);
+    const int v = (at.slice * 64 + lane) * E::N;
+    double p[E::N], q[E::N], w[E::N];
+    r.weights(v, p, q);
+    r.rest(v, p, q, ratio, whole, w);
+    write_drawn<E>(a, b, d, ps, find_in_slice(w, at, lane), lane);
+    return;
+  }
 }
 
 // How a call is laid out.
@@ -463,7 +589,7 @@ Plan plan(int32_t sequences, int32_t n, bool drafted, int32_t V) {
   p.each = 8;
   p.parts = parts_of<E>(V, 8);
   const int slices = slices_of<E>(V);
-  if (p.rows * p.parts <= 32 && slices <= 32) {
+  if (p.rows * p.parts <= kSmallItems && slices <= 16 * kHeld) {
     p.groups = -1;
     p.verdicts = p.slice_sums = p.bytes = 0;
     return p;
@@ -472,10 +598,10 @@ Plan plan(int32_t sequences, int32_t n, bool drafted, int32_t V) {
     p.each = 2;
     p.parts = parts_of<E>(V, 2);
   }
-  p.groups = slices <= 32 ? 0 : static_cast<int>(std::min<int64_t>((slices + kRestWaves - 1) / kRestWaves, std::max<int64_t>(1, 1024 / sequences)));
+  p.groups = slices <= 16 * kHeld ? 0 : static_cast<int>(std::min<int64_t>((slices + kRestWaves - 1) / kRestWaves, std::max<int64_t>(1, 1024 / sequences)));
   p.verdicts = (static_cast<int64_t>(sequences) * p.rows * p.parts * static_cast<int64_t>(sizeof(Sums)) + 15) / 16 * 16;
-  p.slice_sums = p.verdicts + (p.groups > 0 ? static_cast<int64_t>(sequences) * static_cast<int64_t>(sizeof(Verdict)) : 0);
-  p.bytes = p.slice_sums + (p.groups > 0 ? static_cast<int64_t>(sequences) * slices * 8 : 0);
+  p.slice_sums = p.verdicts + (p.groups > 0 ? (static_cast<int64_t>(sequences) * static_cast<int64_t>(sizeof(Verdict)) + 15) / 16 * 16 : 0);
+  p.bytes = p.slice_sums + (p.groups > 0 ? static_cast<int64_t>(sequences) * slices * static_cast<int64_t>(sizeof(Slice)) : 0);
   return p;
 }
 
@@ -498,10 +624,10 @@ int forward(const VerifyArgs& a, void* workspace, hipStream_t stream) {
     return done();
   }
   Verdict* verdicts = reinterpret_cast<Verdict*>(ws + p.verdicts);
-  double* slice_sums = reinterpret_cast<double*>(ws + p.slice_sums);
+  Slice* slice_sums = reinterpret_cast<Slice*>(ws + p.slice_sums);
   verify_rest_kernel<E><<<dim3(p.groups, a.sequences), 64 * kRestWaves, 0, stream>>>(a, p.rows, p.parts, sums, verdicts, slice_sums);
   if (done() != PB_OK) return PB_EHIP;
-  verify_pick_kernel<E><<<a.sequences, 256, 0, stream>>>(a, verdicts, slice_sums);
+  verify_pick_kernel<E><<<a.sequences, 64 * kPickWaves, 0, stream>>>(a, verdicts, slice_sums);
   return done();
 }
 
