@@ -24,14 +24,16 @@ namespace vd {
 using namespace lr;
 using wv::first_lane;
 
-// Of a part of a row: the largest element (-inf: nothing) and the sum of 2^((x - m) c) in fp32, NaN where it holds a NaN or +inf.
+// Of a part of a row: the largest element m (-inf: nothing), the sum of e = 2^t, t = (x - m) c, in fp32 (NaN where it holds a NaN or +inf),
+// and that of e |t|; beside the first part, what the row has of the token drafted there.
 struct Sums {
-  float m, s;
+  float m, s, t, at;
 };
-// How far such a sum is off at most, relative to itself: an exponent t by 3 roundings of 2^-24, that is 2.1 |t| 2^-24 of its term, and
-// the mean of |t| over a row of V tokens is log2 V < 19 at most; 2 of the exponential; 18 additions one after the other (8 of vectors, 3
-// in a vector, 6 in a wave, the edge).  60 x 2^-24 < 2^-18; twice that for a ratio of two, and as much again for good measure.
-constexpr double kUnsure = 0x1p-16;
+// How far a row's sum is off at most, relative to itself: each exponent by three roundings (of the difference, of c, of the product),
+// 3 ln 2 |t| 2^-24 of its term, its exponential by 2 x 2^-24, the sum by 13 additions one after the other (3 in a vector, 3 of vectors, the
+// edge, 6 in a wave; parts are joined in 64 bits).  Told from the row's own mean of |t|, which is some bits where log2 V, the
+// most there can be, is up to 19: the nearer u q may lie to p, and p to q, without a second look.
+__device__ __forceinline__ double off_by(double mean_t) { return (2.1 * mean_t + 16.0) * 0x1p-24; }
 constexpr double kNothing = 0x1p-40;     // a rest of the target's mass below this is none (equal rows differ by their roundings)
 constexpr double kNoWeight = 0x1p-960;   // weights below this, masked tokens' among them, are none
 
@@ -102,17 +104,24 @@ __device__ __forceinline__ Sums part_sums(const Row<E>& row, int first, bool edg
   }
   m = wave_max(m);
   const float c = static_cast<float>(c64), from = m == -INFINITY ? 0.0f : m;  // (inf - inf is a NaN, as is what a NaN leaves)
-  float s = exp2_fast((xe - from) * c);
+  float s[EACH], t = 0.0f;
 #pragma unroll
   for (int u = 0; u < EACH; ++u) {
-    if (first + 64 * u >= row.nv) break;
+    s[u] = 0.0f;
+    if (first + 64 * u >= row.nv) continue;
     float x[E::N];
     E::unpack(raw[u], x);
 #pragma unroll
-    for (int i = 0; i < E::N; ++i) x[i] = exp2_fast((x[i] - from) * c);
-    s += vec_sum(x);
+    for (int i = 0; i < E::N; ++i) {
+      const float d = (x[i] - from) * c;
+      x[i] = exp2_fast(d);
+      t = __builtin_fmaf(x[i], fmaxf(d, -200.0f), t);  // (not 0 times infinity)
+    }
+    s[u] = vec_sum(x);
   }
-  return Sums{m, wave_sum(s)};
+  const float de = (xe - from) * c, e = exp2_fast(de);
+  t = __builtin_fmaf(e, fmaxf(de, -200.0f), t);
+  return Sums{m, wave_sum(vec_sum(s) + e), -wave_sum(t), 0.0f};
 }
 
 // The rows of a sequence: 0 .. n the target's, n + 1 .. 2 n the draft's.
@@ -121,12 +130,27 @@ __device__ __forceinline__ Row<E> row_of(const VerifyArgs& a, int64_t b, int j) 
   return j <= a.n ? row_at<E>(static_cast<const typename E::type*>(a.target) + b * a.target_seq, a.target_row, j, a.V)
                   : row_at<E>(static_cast<const typename E::type*>(a.draft) + b * a.draft_seq, a.draft_row, j - a.n - 1, a.V);
 }
-// Drafted tokens of a sequence, and those of them before the first that is absent.
-__device__ __forceinline__ int drafted_tokens(const VerifyArgs& a, int64_t b, int lane, int* count) {
-  const int t = lane < a.n ? a.tokens[b * a.n + lane] : -1;
-  const u64 none = ~__ballot(static_cast<unsigned>(t) < static_cast<unsigned>(a.V));
-  *count = none ? first_lane(none) : 64;  // (n <= 63: lane 63 holds none)
-  return t;
+// The drafted tokens of a sequence, a lane each, and how many there are before the first that is absent.
+struct Drafted {
+  int t, count;
+  float u;  // their numbers
+};
+__device__ __forceinline__ Drafted drafted_tokens(const VerifyArgs& a, int64_t b, int lane) {
+  Drafted r;
+  r.t = lane < a.n ? a.tokens[b * a.n + lane] : -1;
+  r.u = lane < a.n ? a.numbers[b * (a.n + 1) + lane] : 0.0f;
+  const u64 none = ~__ballot(static_cast<unsigned>(r.t) < static_cast<unsigned>(a.V));
+  r.count = first_lane(none);  // (n <= 63: lane 63 holds none)
+  r.u = fminf(fmaxf(r.u, 0.0f), 0x1.fffffep-1f);
+  return r;
+}
+template <typename E>
+__device__ __forceinline__ float target_at(const VerifyArgs& a, int64_t b, int i, int t) {
+  return E::up((static_cast<const typename E::type*>(a.target) + b * a.target_seq + i * a.target_row)[t]);
+}
+template <typename E>
+__device__ __forceinline__ float draft_at(const VerifyArgs& a, int64_t b, int i, int t) {
+  return E::up((static_cast<const typename E::type*>(a.draft) + b * a.draft_seq + i * a.draft_row)[t]);
 }
 
 // A row is split in parts of 64 EACH vectors, a wave each; at least one.
@@ -144,11 +168,14 @@ __global__ __launch_bounds__(256) void verify_sums_kernel(VerifyArgs a, int rows
   if (item >= static_cast<int64_t>(a.sequences) * rows * parts) return;
   const int part = static_cast<int>(item % parts), j = static_cast<int>(item / parts % rows);
   const int64_t b = item / parts / rows;
-  int count;
-  drafted_tokens(a, b, lane, &count);
-  if (j <= a.n ? j > count : j - a.n - 1 >= count) return;
+  const Drafted tokens = drafted_tokens(a, b, lane);
+  const int i = j <= a.n ? j : j - a.n - 1;
+  if (j <= a.n ? i > tokens.count : i >= tokens.count) return;
   const Row<E> row = row_of<E>(a, b, j);
-  const Sums s = part_sums<E, EACH>(row, part * 64 * EACH, part == 0, j <= a.n ? a.target_c : a.draft_c, lane);
+  float at = 0.0f;
+  if (part == 0 && i < tokens.count) at = E::up(row.x[__builtin_amdgcn_readlane(tokens.t, i)]);
+  Sums s = part_sums<E, EACH>(row, part * 64 * EACH, part == 0, j <= a.n ? a.target_c : a.draft_c, lane);
+  s.at = at;
   if (lane == 0) sums[item] = s;
 }
 
@@ -159,13 +186,15 @@ struct Verdict {
   int refused;     // the token that was refused, -1: none
   float pm, qm;    // largest elements of the rows that decide; qm = -inf: no draft's row counts
   double ratio;    // of their sums, about
+  double near;     // how far that is off at most, relative to itself
 };
 
 constexpr int kMaxRows = 2 * kMaxDrafts + 1;
 struct RowSums {
   float m[kMaxRows];
   double s[kMaxRows];
-  double turn[16];  // a place a wave
+  double off[kMaxRows];  // relative
+  double turn[16];       // a place a wave
 };
 
 __device__ __forceinline__ double share(float x, float m, double s, double c) {  // (a row of nothing but -inf: s = 0; a marked one: NaN)
@@ -222,33 +251,36 @@ __device__ __forceinline__ double row_sum(const typename E::type* x, int V, floa
 // Joins the parts of all rows (waves of the workgroup take turns), then decides, the same in every wave.  Writes the accepted tokens
 // if `writes`, in the last wave.
 template <typename E, int WAVES>
-__device__ __forceinline__ Verdict decide(const VerifyArgs& a, int64_t b, const Sums* sums, int rows, int parts, RowSums& joined, bool writes) {
-  const int lane = threadIdx.x & 63, wave = uniform_i(threadIdx.x >> 6);
+__device__ __forceinline__ Verdict decide(const VerifyArgs& a, int64_t b, const Drafted& tokens, float xt, float yt, const Sums* sums, int rows, int parts,
+                                          RowSums& joined, bool writes) {
+  const int lane = threadIdx.x & 63, wave = uniform_i(threadIdx.x >> 6), t = tokens.t, count = tokens.count;
+  const float u = tokens.u;
   const typename E::type* target = static_cast<const typename E::type*>(a.target) + b * a.target_seq;
   const typename E::type* draft = a.draft ? static_cast<const typename E::type*>(a.draft) + b * a.draft_seq : nullptr;
-  int count;
-  const int t = drafted_tokens(a, b, lane, &count);
-  float xt = 0.0f, yt = 0.0f, u = 0.0f;
-  if (lane < count) {
-    xt = E::up(target[lane * a.target_row + t]);
-    if (draft) yt = E::up(draft[lane * a.draft_row + t]);
-    u = fminf(fmaxf(a.numbers[b * (a.n + 1) + lane], 0.0f), 0x1.fffffep-1f);
-  }
-  for (int j = wave; j < rows; j += WAVES) {
-    if (j <= a.n ? j > count : j - a.n - 1 >= count) continue;
+  for (int j = wave; j < rows; j += WAVES) {  // (rows behind the end of the draft too, whose sums nobody has written and nobody looks at)
     const double c = j <= a.n ? a.target_c : a.draft_c;
-    float m = -INFINITY;
-    for (int p = lane; p < parts; p += 64) m = fmaxf(m, sums[j * parts + p].m);
+    Sums part{-INFINITY, 0.0f, 0.0f, 0.0f};
+    if (lane < parts) part = sums[j * parts + lane];
+    float m = part.m;
+    for (int p = lane + 64; p < parts; p += 64) m = fmaxf(m, sums[j * parts + p].m);
     m = wave_max(m);
-    double s = 0.0;
+    double s = 0.0, t = 0.0;
     for (int p = lane; p < parts; p += 64) {
-      const Sums part = sums[j * parts + p];
-      s += part.m == -INFINITY ? static_cast<double>(part.s) : static_cast<double>(part.s) * weight(part.m, m, scale_of(c));
+      if (p > lane) part = sums[j * parts + p];
+      if (part.m == -INFINITY) {
+        s += static_cast<double>(part.s);  // (0, or NaN)
+      } else {
+        const double w = weight(part.m, m, scale_of(c)), ahead = fmin((static_cast<double>(m) - static_cast<double>(part.m)) * c, 2000.0);
+        s += static_cast<double>(part.s) * w;
+        t += (static_cast<double>(part.t) + static_cast<double>(part.s) * ahead) * w;
+      }
     }
     s = wave_sum64(s);
+    t = wave_sum64(t);
     if (lane == 0) {
       joined.m[j] = m;
       joined.s[j] = s;
+      joined.off[j] = off_by(t / s);
     }
   }
   __syncthreads();
@@ -261,7 +293,7 @@ __device__ __forceinline__ Verdict decide(const VerifyArgs& a, int64_t b, const 
       const double q = draft ? share(yt, joined.m[a.n + 1 + lane], joined.s[a.n + 1 + lane], a.draft_c) : 1.0;
       const double uq = static_cast<double>(u) * q;
       takes = uq < p;  // (false for NaN)
-      unsure = p > 0.0 && fabs(uq - p) <= p * kUnsure && !((exact >> lane) & 1u);
+      unsure = p > 0.0 && fabs(uq - p) <= p * (joined.off[lane] + (draft ? joined.off[a.n + 1 + lane] : 0.0) + 0x1p-40) && !((exact >> lane) & 1u);
     }
     const int stop = first_lane(~__ballot(takes || unsure));  // (the first that is refused for sure; lane 63 takes none)
     const u64 open = __ballot(unsure) & ((1ull << stop) - 1);
@@ -283,12 +315,15 @@ __device__ __forceinline__ Verdict decide(const VerifyArgs& a, int64_t b, const 
   const double ps = joined.s[r.k];
   r.pm = joined.m[r.k];
   r.qm = -INFINITY;
-  r.ratio = 0.0;
+  r.ratio = r.near = 0.0;
   r.none = r.pm == -INFINITY || ps != ps;
   if (r.refused >= 0 && draft) {
     const double qs = joined.s[a.n + 1 + r.k];
     r.qm = joined.m[a.n + 1 + r.k];
-    if (r.qm != -INFINITY) r.ratio = ps / qs;
+    if (r.qm != -INFINITY) {
+      r.ratio = ps / qs;
+      r.near = joined.off[r.k] + joined.off[a.n + 1 + r.k] + 0x1p-40;
+    }
     r.none |= qs != qs;
   }
   if (writes && wave == WAVES - 1) {
@@ -299,6 +334,19 @@ __device__ __forceinline__ Verdict decide(const VerifyArgs& a, int64_t b, const 
     if (lane == 0) a.accepted[b] = r.k;
   }
   return r;
+}
+
+// The same from the sums of a launch before.
+template <typename E, int WAVES>
+__device__ __forceinline__ Verdict decide_rows(const VerifyArgs& a, int64_t b, const Sums* sums, int rows, int parts, RowSums& joined, bool writes) {
+  const int lane = threadIdx.x & 63;
+  sums += b * rows * parts;
+  float xt = 0.0f, yt = 0.0f;
+  if (lane < a.n) {
+    xt = sums[lane * parts].at;
+    if (a.draft) yt = sums[(a.n + 1 + lane) * parts].at;
+  }
+  return decide<E, WAVES>(a, b, drafted_tokens(a, b, lane), xt, yt, sums, rows, parts, joined, writes);
 }
 
 // The rows that decide, as weights.
@@ -387,7 +435,7 @@ __device__ __forceinline__ void write_drawn(const VerifyArgs& a, int64_t b, cons
   if (lane != 0) return;
   const int64_t at = b * (a.n + 1) + d.k;
   a.out[at] = token;
-  if (a.logp) a.logp[at] = token < 0 ? NAN : log_share(E::up((static_cast<const typename E::type*>(a.target) + b * a.target_seq + d.k * a.target_row)[token]), d.pm, ps, a.target_c);
+  if (a.logp) a.logp[at] = token < 0 ? NAN : log_share(target_at<E>(a, b, d.k, token), d.pm, ps, a.target_c);
 }
 
 // Rows of up to WAVES * HELD slices: a workgroup a sequence holds the rows that decide in registers.
@@ -447,7 +495,7 @@ __global__ __launch_bounds__(64 * WAVES) void verify_draw_kernel(VerifyArgs a, i
   __shared__ RowSums joined;
   __shared__ DrawShared<WAVES> shared;
   const int64_t b = blockIdx.x;
-  const Verdict d = decide<E, WAVES>(a, b, sums + b * rows * parts, rows, parts, joined, true);
+  const Verdict d = decide_rows<E, WAVES>(a, b, sums, rows, parts, joined, true);
   if (!d.none) draw_held<E, WAVES>(a, b, d, shared);
 }
 
@@ -460,16 +508,20 @@ __global__ __launch_bounds__(64 * WAVES) void verify_small_kernel(VerifyArgs a, 
   __shared__ DrawShared<WAVES> shared;
   const int lane = threadIdx.x & 63, wave = uniform_i(threadIdx.x >> 6);
   const int64_t b = blockIdx.x;
-  int count;
-  drafted_tokens(a, b, lane, &count);
+  const Drafted tokens = drafted_tokens(a, b, lane);
+  float xt = 0.0f, yt = 0.0f;
+  if (lane < tokens.count) {
+    xt = target_at<E>(a, b, lane, tokens.t);
+    if (a.draft) yt = draft_at<E>(a, b, lane, tokens.t);
+  }
   for (int item = wave; item < rows * parts; item += WAVES) {
     const int j = item / parts, part = item - j * parts;
-    if (j <= a.n ? j > count : j - a.n - 1 >= count) continue;
+    if (j <= a.n ? j > tokens.count : j - a.n - 1 >= tokens.count) continue;
     const Sums s = part_sums<E, EACH>(row_of<E>(a, b, j), part * 64 * EACH, part == 0, j <= a.n ? a.target_c : a.draft_c, lane);
     if (lane == 0) sums[item] = s;
   }
   __syncthreads();
-  const Verdict d = decide<E, WAVES>(a, b, sums, rows, parts, joined, true);
+  const Verdict d = decide<E, WAVES>(a, b, tokens, xt, yt, sums, rows, parts, joined, true);
   if (!d.none) draw_held<E, WAVES>(a, b, d, shared);
 }
 
@@ -485,53 +537,67 @@ __global__ __launch_bounds__(64 * kRestWaves) void verify_rest_kernel(VerifyArgs
   __shared__ RowSums joined;
   const int lane = threadIdx.x & 63, wave = uniform_i(threadIdx.x >> 6), slices = slices_of<E>(a.V);
   const int64_t b = blockIdx.y;
-  const Verdict d = decide<E, kRestWaves>(a, b, sums + b * rows * parts, rows, parts, joined, blockIdx.x == 0);
+  const Verdict d = decide_rows<E, kRestWaves>(a, b, sums, rows, parts, joined, blockIdx.x == 0);
   if (blockIdx.x == 0 && threadIdx.x == 0) verdicts[b] = d;
   if (d.none) return;
   const Rest<E> r(a, b, d);
   for (int s = blockIdx.x * kRestWaves + wave; s < slices; s += gridDim.x * kRestWaves) {
     const int v = (s * 64 + lane) * E::N;
-    double p[E::N], q[E::N];
-    r.weights(v, p, q);
-    Slice to{lane_sum(p), 0.0, 0.0, 0.0};
+    Slice to{0.0, 0.0, 0.0, 0.0};
     if (r.y) {
+      float xs[E::N], ys[E::N];
+      load_at<E>(r.x, v, r.V, xs);
+      load_at<E>(r.y, v, r.V, ys);
       double near = INFINITY;
-      to.q = lane_sum(q);
 #pragma unroll
       for (int i = 0; i < E::N; ++i) {
-        const double rest = fma(-d.ratio, q[i], p[i]);
-        near = fmin(near, fma(-kUnsure * d.ratio, q[i], fabs(rest)));
+        const double p = weight(xs[i], r.pm, r.pk), q = weight(ys[i], r.qm, r.qk), rest = fma(-d.ratio, q, p);
+        near = fmin(near, fma(-d.near * d.ratio, q, fabs(rest)));
+        to.p += p;
+        to.q += q;
         to.above += fmax(rest, 0.0);
-        to.above_q += rest > 0.0 ? q[i] : 0.0;
+        to.above_q += rest > 0.0 ? q : 0.0;
       }
       to.q = wave_sum64(to.q);
       to.above = wave_sum64(to.above);
       to.above_q = wave_sum64(to.above_q);
       if (__ballot(near <= 0.0) != 0) to.above_q = NAN;
-    } else if (r.barred >= 0) {
-      double w[E::N];
-      r.rest(v, p, q, 0.0, false, w);
-      to.above = wave_sum64(lane_sum(w));
+    } else {
+      double p[E::N], q[E::N], w[E::N];
+      r.weights(v, p, q);
+      to.p = lane_sum(p);
+      if (r.barred >= 0) {
+        r.rest(v, p, q, 0.0, false, w);
+        to.above = wave_sum64(lane_sum(w));
+      }
     }
     to.p = wave_sum64(to.p);
     if (lane == 0) out[b * slices + s] = to;
   }
 }
 // And a workgroup a sequence draws.
-constexpr int kPickWaves = 4;
+constexpr int kPickWaves = 8;
 template <typename E>
 __global__ __launch_bounds__(64 * kPickWaves) void verify_pick_kernel(VerifyArgs a, const Verdict* verdicts, const Slice* in) {
-  __shared__ double sums[kLogitsMaxV / (64 * E::N) + 1], turn[2 * kPickWaves];
+  __shared__ double sums[kLogitsMaxV / (64 * E::N)], turn[2 * kPickWaves];
   const int lane = threadIdx.x & 63, wave = uniform_i(threadIdx.x >> 6), slices = slices_of<E>(a.V);
+  constexpr int kEach = (kLogitsMaxV / (64 * E::N) + 64 * kPickWaves - 1) / (64 * kPickWaves);
   const int64_t b = blockIdx.x;
-  const Verdict d = verdicts[b];
-  if (d.none) return;
   in += b * slices;
-  const float number = a.numbers[b * (a.n + 1) + a.n];
+  Slice mine[kEach];
   double ps = 0.0, qs = 0.0;
-  for (int s = threadIdx.x; s < slices; s += 64 * kPickWaves) {
-    ps += in[s].p;
-    qs += in[s].q;
+#pragma unroll
+  for (int k = 0; k < kEach; ++k) {
+    const int s = threadIdx.x + k * 64 * kPickWaves;
+    mine[k] = s < slices ? in[s] : Slice{0.0, 0.0, 0.0, 0.0};
+  }
+  const float number = a.numbers[b * (a.n + 1) + a.n];
+  const Verdict d = verdicts[b];
+  if (d.none) return;  // (and nothing was summed)
+#pragma unroll
+  for (int k = 0; k < kEach; ++k) {
+    ps += mine[k].p;
+    qs += mine[k].q;
   }
   ps = wave_sum64(ps);
   qs = wave_sum64(qs);
@@ -540,24 +606,27 @@ __global__ __launch_bounds__(64 * kPickWaves) void verify_pick_kernel(VerifyArgs
     turn[kPickWaves + wave] = qs;
   }
   __syncthreads();
-  ps = (turn[0] + turn[1]) + (turn[2] + turn[3]);
-  qs = (turn[4] + turn[5]) + (turn[6] + turn[7]);
+  ps = wave_sum64(lane < kPickWaves ? turn[lane] : 0.0);
+  qs = wave_sum64(lane < kPickWaves ? turn[kPickWaves + lane] : 0.0);
   const Rest<E> r(a, b, d);
   const double ratio = r.y ? ps / qs : 0.0;
   bool whole = d.refused < 0 || (!r.y && r.barred < 0);  // (a draft's row of nothing but -inf takes nothing away)
   for (;; whole = true) {
-    for (int s0 = wave * 64; s0 < slices; s0 += 64 * kPickWaves) {
-      double v = 0.0;
-      if (s0 + lane < slices) v = whole ? in[s0 + lane].p : r.y ? fma(d.ratio - ratio, in[s0 + lane].above_q, in[s0 + lane].above) : in[s0 + lane].above;
-      for (u64 left = __ballot(v != v); left; left &= left - 1) {
-        const int at = first_lane(left), from = ((s0 + at) * 64 + lane) * E::N;
-        double p[E::N], q[E::N], w[E::N];
-        r.weights(from, p, q);
-        r.rest(from, p, q, ratio, false, w);
-        const double again = wave_sum64(lane_sum(w));
-        if (lane == at) v = again;
-      }
-      if (s0 + lane < slices) sums[s0 + lane] = v > kNoWeight ? v : 0.0;
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+      const int s = threadIdx.x + k * 64 * kPickWaves;
+      const double v = whole ? mine[k].p : r.y ? fma(d.ratio - ratio, mine[k].above_q, mine[k].above) : mine[k].above;
+      if (s < slices) sums[s] = v != v || v > kNoWeight ? v : 0.0;
+    }
+    __syncthreads();
+    for (int s = wave; s < slices; s += kPickWaves) {
+      if (sums[s] == sums[s]) continue;
+      const int from = (s * 64 + lane) * E::N;
+      double p[E::N], q[E::N], w[E::N];
+      r.weights(from, p, q);
+      r.rest(from, p, q, ratio, false, w);
+      const double again = wave_sum64(lane_sum(w));
+      if (lane == 0) sums[s] = again;
     }
     __syncthreads();
     const double all = sum_of(sums, slices, lane);
@@ -598,7 +667,7 @@ Plan plan(int32_t sequences, int32_t n, bool drafted, int32_t V) {
     p.each = 2;
     p.parts = parts_of<E>(V, 2);
   }
-  p.groups = slices <= 16 * kHeld ? 0 : static_cast<int>(std::min<int64_t>((slices + kRestWaves - 1) / kRestWaves, std::max<int64_t>(1, 1024 / sequences)));
+  p.groups = slices <= 16 * kHeld ? 0 : static_cast<int>(std::min<int64_t>((slices + kRestWaves - 1) / kRestWaves, std::max<int64_t>(1, 256 / sequences)));
   p.verdicts = (static_cast<int64_t>(sequences) * p.rows * p.parts * static_cast<int64_t>(sizeof(Sums)) + 15) / 16 * 16;
   p.slice_sums = p.verdicts + (p.groups > 0 ? (static_cast<int64_t>(sequences) * static_cast<int64_t>(sizeof(Verdict)) + 15) / 16 * 16 : 0);
   p.bytes = p.slice_sums + (p.groups > 0 ? static_cast<int64_t>(sequences) * slices * static_cast<int64_t>(sizeof(Slice)) : 0);
