@@ -755,11 +755,14 @@ int pb_tensors_build(const void* const* d_buffers, const int64_t* sizes, const i
   }
   pb_tensors* t = nullptr;
   std::vector<pb::GradChunk> chunks;
+  int64_t elements = 0;
+  for (int32_t i = 0; i < n; ++i) elements += std::min<int64_t>(sizes[i], 1ll << 30);
+  const int64_t chunk = pb::chunk_for(elements);
   try {
     for (int32_t i = 0; i < n; ++i)
-      for (int64_t at = 0; at < sizes[i]; at += pb::kChunk)
+      for (int64_t at = 0; at < sizes[i]; at += chunk)
         chunks.push_back(pb::GradChunk{static_cast<char*>(const_cast<void*>(d_buffers[i])) + at * element_bytes(dtypes[i]),
-                                       static_cast<int32_t>(std::min<int64_t>(pb::kChunk, sizes[i] - at)), dtypes[i]});
+                                       static_cast<int32_t>(std::min<int64_t>(chunk, sizes[i] - at)), dtypes[i]});
     t = new pb_tensors();
     t->sizes.assign(sizes, sizes + n);
     t->dtypes.assign(dtypes, dtypes + n);

@@ -11,30 +11,43 @@ namespace gr {
 using namespace lr;
 
 constexpr int kGroups = 2048;  // workgroups at most: eight a CU
+constexpr int kAhead = 8;      // vectors that a lane requests at once: a piece of kChunk 16-bit elements in one turn
 
-__device__ __forceinline__ double block_sum(double v, double (&shared)[4]) {
+template <int WAVES>
+__device__ __forceinline__ double block_sum(double v, double (&shared)[WAVES]) {
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) v += __shfl_xor(v, d, 64);
   if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = v;
   __syncthreads();
-  return (shared[0] + shared[1]) + (shared[2] + shared[3]);
+  v = 0.0;
+  for (int w = 0; w < WAVES; ++w) v += shared[w];
+  return v;
 }
 
 template <typename E>
 __device__ __forceinline__ double squares(const GradChunk& c) {
   const Row<E> row = row_at<E>(c.x, 0, 0, c.n);
-  double s = 0.0;
+  double s[4] = {0.0, 0.0, 0.0, 0.0};
+  auto add = [&](const v4u& raw) {
+    float x[E::N];
+    E::unpack(raw, x);
+#pragma unroll
+    for (int i = 0; i < E::N; ++i) s[i % 4] = fma(static_cast<double>(x[i]), static_cast<double>(x[i]), s[i % 4]);
+  };
   if (static_cast<int>(threadIdx.x) < row.edges) {
     const double x = E::up(row.x[row.edge_token(threadIdx.x)]);
-    s = x * x;
+    s[0] = x * x;
   }
-  for (int v = threadIdx.x; v < row.nv; v += 256) {
-    float x[E::N];
-    E::unpack(row.vec(v), x);
+  int v = threadIdx.x;
+  for (; v + 256 * (kAhead - 1) < row.nv; v += 256 * kAhead) {
+    v4u raw[kAhead];
 #pragma unroll
-    for (int i = 0; i < E::N; ++i) s = fma(static_cast<double>(x[i]), static_cast<double>(x[i]), s);
+    for (int k = 0; k < kAhead; ++k) raw[k] = row.vec(v + 256 * k);
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) add(raw[k]);
   }
-  return s;
+  for (; v < row.nv; v += 256) add(row.vec(v));
+  return (s[0] + s[1]) + (s[2] + s[3]);
 }
 
 __global__ __launch_bounds__(256) void grad_squares_kernel(const GradChunk* chunks, int64_t n, double* sums) {
@@ -44,45 +57,57 @@ __global__ __launch_bounds__(256) void grad_squares_kernel(const GradChunk* chun
     const GradChunk chunk = chunks[c];
     s += chunk.dtype == PB_F32 ? squares<F32>(chunk) : chunk.dtype == PB_F16 ? squares<F16>(chunk) : squares<BF16>(chunk);
   }
-  s = block_sum(s, shared);
+  s = block_sum<4>(s, shared);
   if (threadIdx.x == 0) sums[blockIdx.x] = s;
 }
-__global__ __launch_bounds__(256) void grad_norm_kernel(const double* sums, int n, float* norm) {
-  __shared__ double shared[4];
-  double s = 0.0;
-  for (int i = threadIdx.x; i < n; i += 256) s += sums[i];
-  s = block_sum(s, shared);
+__global__ __launch_bounds__(1024) void grad_norm_kernel(const double* sums, int n, float* norm) {
+  __shared__ double shared[16];
+  static_assert(kGroups <= 2048, "two a thread");
+  double s = static_cast<int>(threadIdx.x) < n ? sums[threadIdx.x] : 0.0;
+  if (static_cast<int>(threadIdx.x) + 1024 < n) s += sums[threadIdx.x + 1024];
+  s = block_sum<16>(s, shared);
   if (threadIdx.x == 0) *norm = static_cast<float>(sqrt(s));
 }
 
-template <typename E>
+template <typename E, bool STREAM>
 __device__ __forceinline__ void scaled(const GradChunk& c, const GradChunk& out, float by) {
   const Row<E> row = row_at<E>(c.x, 0, 0, c.n);
   typename E::type* to = static_cast<typename E::type*>(out.x);
+  auto put = [&](int v, const v4u& raw) {
+    float x[E::N];
+    E::unpack(raw, x);
+#pragma unroll
+    for (int i = 0; i < E::N; ++i) x[i] = product(x[i], by);
+    stream_vector<E>(to + row.token(v, 0), E::pack(x));
+  };
   if (static_cast<int>(threadIdx.x) < row.edges) {
     const int i = row.edge_token(threadIdx.x);
     to[i] = E::down(product(E::up(row.x[i]), by));
   }
-  for (int v = threadIdx.x; v < row.nv; v += 256) {
-    float x[E::N];
-    E::unpack(row.vec(v), x);
+  int v = threadIdx.x;
+  for (; v + 256 * (kAhead - 1) < row.nv; v += 256 * kAhead) {
+    v4u raw[kAhead];
 #pragma unroll
-    for (int i = 0; i < E::N; ++i) x[i] = product(x[i], by);
-    store_vector<E>(to + row.token(v, 0), E::pack(x));
+    for (int k = 0; k < kAhead; ++k) raw[k] = row.template vec_once<STREAM>(v + 256 * k);
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) put(v + 256 * k, raw[k]);
   }
+  for (; v < row.nv; v += 256) put(v, row.vec(v));
 }
 
-// (A norm that is not finite clips nothing: there is no factor for it.)
+// (A norm that is not finite clips nothing: there is no factor for it.)  Pieces are taken from the last to the first: the last ones are
+// those that the norm has left in the caches.
+template <bool STREAM>
 __global__ __launch_bounds__(256) void grad_clip_kernel(const GradChunk* chunks, const GradChunk* out, int64_t n, const float* norm, float max_norm) {
   const float is = *norm;
   const bool clips = is > max_norm && is < INFINITY;
   const float by = clips ? max_norm / is : 1.0f;
   if (!clips && out == chunks) return;
-  for (int64_t c = blockIdx.x; c < n; c += gridDim.x) {
+  for (int64_t c = n - 1 - blockIdx.x; c >= 0; c -= gridDim.x) {
     const GradChunk from = chunks[c], to = out[c];
-    if (from.dtype == PB_F32) scaled<F32>(from, to, by);
-    else if (from.dtype == PB_F16) scaled<F16>(from, to, by);
-    else scaled<BF16>(from, to, by);
+    if (from.dtype == PB_F32) scaled<F32, STREAM>(from, to, by);
+    else if (from.dtype == PB_F16) scaled<F16, STREAM>(from, to, by);
+    else scaled<BF16, STREAM>(from, to, by);
   }
 }
 
@@ -96,12 +121,12 @@ int launch_grad_norm(const GradChunk* chunks, int64_t n, float* norm, void* work
   const int groups = gr::groups_for(n);
   if (groups > 0) gr::grad_squares_kernel<<<groups, 256, 0, stream>>>(chunks, n, sums);
   if (hipGetLastError() != hipSuccess) return PB_EHIP;
-  gr::grad_norm_kernel<<<1, 256, 0, stream>>>(sums, groups, norm);
+  gr::grad_norm_kernel<<<1, 1024, 0, stream>>>(sums, groups, norm);
   return hipGetLastError() == hipSuccess ? PB_OK : PB_EHIP;
 }
 int launch_grad_clip(const GradChunk* chunks, const GradChunk* out, int64_t n, const float* norm, float max_norm, hipStream_t stream) {
   if (n == 0) return PB_OK;
-  gr::grad_clip_kernel<<<gr::groups_for(n), 256, 0, stream>>>(chunks, out, n, norm, max_norm);
+  gr::grad_clip_kernel<false><<<gr::groups_for(n), 256, 0, stream>>>(chunks, out, n, norm, max_norm);
   return hipGetLastError() == hipSuccess ? PB_OK : PB_EHIP;
 }
 

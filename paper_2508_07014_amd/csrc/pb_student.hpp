@@ -66,8 +66,13 @@ struct EmbedGradArgs {
 int64_t embed_tokens_backward_workspace(int32_t n, int32_t V, int32_t dim);
 int launch_embed_tokens_backward(int grad_dtype, int table_dtype, const EmbedGradArgs& a, void* workspace, hipStream_t stream);
 
-// A set of tensors as the kernels see it: pieces of at most kChunk elements, in the order of the tensors.
-constexpr int kChunk = 16384;
+// A set of tensors as the kernels see it: pieces of at most kChunk elements, fewer in small sets (which are to fill the chip), in the
+// order of the tensors.
+constexpr int kChunk = 16384, kLeastChunk = 2048;
+inline int64_t chunk_for(int64_t elements) {
+  const int64_t even = (elements / 2048 + kLeastChunk - 1) / kLeastChunk * kLeastChunk;
+  return even < kLeastChunk ? kLeastChunk : even < kChunk ? even : kChunk;
+}
 struct GradChunk {
   void* x;
   int32_t n;
