@@ -772,6 +772,7 @@ int pb_tensors_build(const void* const* d_buffers, const int64_t* sizes, const i
   }
   t->device = device;
   t->count = static_cast<int64_t>(chunks.size());
+  for (int32_t i = 0; i < n; ++i) t->bytes = std::min<int64_t>(1ll << 60, t->bytes + sizes[i] * element_bytes(dtypes[i]));
   int prev = 0, rc = PB_OK;
   if (hipGetDevice(&prev) != hipSuccess || hipSetDevice(device) != hipSuccess) {
     (void)hipGetLastError();
@@ -815,14 +816,14 @@ int64_t pb_grad_norm_workspace_bytes(const pb_tensors* grads) { return grads ? p
 int pb_grad_norm(const pb_tensors* grads, float* d_norm, void* d_workspace, int64_t workspace_bytes, void* hip_stream) {
   if (!grads || !d_norm || !aligned(d_norm, 4) || workspace_bytes < 0) return PB_EINVAL;
   if (check_workspace(pb::grad_norm_workspace(grads->count), d_workspace, workspace_bytes) != PB_OK) return PB_EINVAL;
-  return pb::launch_grad_norm(grads->d_chunks, grads->count, d_norm, d_workspace, static_cast<hipStream_t>(hip_stream));
+  return pb::launch_grad_norm(grads->d_chunks, grads->count, grads->bytes, d_norm, d_workspace, static_cast<hipStream_t>(hip_stream));
 }
 
 int pb_grad_clip(const pb_tensors* grads, const float* d_norm, float max_norm, const pb_tensors* out, void* hip_stream) {
   if (!grads || !d_norm || !aligned(d_norm, 4)) return PB_EINVAL;
   if (!(max_norm >= 0.0f && max_norm <= 3.402823466e+38f)) return PB_ERANGE;
   if (out && (out->device != grads->device || out->sizes != grads->sizes || out->dtypes != grads->dtypes)) return PB_EINVAL;
-  return pb::launch_grad_clip(grads->d_chunks, out ? out->d_chunks : grads->d_chunks, grads->count, d_norm, max_norm, static_cast<hipStream_t>(hip_stream));
+  return pb::launch_grad_clip(grads->d_chunks, out ? out->d_chunks : grads->d_chunks, grads->count, grads->bytes, d_norm, max_norm, static_cast<hipStream_t>(hip_stream));
 }
 
 int pb_validate(const pb_tree* tree) {

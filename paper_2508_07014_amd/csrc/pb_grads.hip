@@ -11,6 +11,9 @@ namespace gr {
 using namespace lr;
 
 constexpr int kGroups = 2048;  // workgroups at most: eight a CU
+// Sets that do not fit in the last cache (256 MB) are read past it, both times: 800 MB of bf16 norm 135 -> 120 us, clipping 295 -> 282; 200
+// MB, which fits, both 99 -> 96 us the other way.
+constexpr int64_t kStreamBytes = 256ll << 20;
 constexpr int kAhead = 8;      // vectors that a lane requests at once: a piece of kChunk 16-bit elements in one turn
 
 template <int WAVES>
@@ -24,7 +27,7 @@ __device__ __forceinline__ double block_sum(double v, double (&shared)[WAVES]) {
   return v;
 }
 
-template <typename E>
+template <typename E, bool STREAM>
 __device__ __forceinline__ double squares(const GradChunk& c) {
   const Row<E> row = row_at<E>(c.x, 0, 0, c.n);
   double s[4] = {0.0, 0.0, 0.0, 0.0};
@@ -42,7 +45,7 @@ __device__ __forceinline__ double squares(const GradChunk& c) {
   for (; v + 256 * (kAhead - 1) < row.nv; v += 256 * kAhead) {
     v4u raw[kAhead];
 #pragma unroll
-    for (int k = 0; k < kAhead; ++k) raw[k] = row.vec(v + 256 * k);
+    for (int k = 0; k < kAhead; ++k) raw[k] = row.template vec_once<STREAM>(v + 256 * k);
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) add(raw[k]);
   }
@@ -50,12 +53,13 @@ __device__ __forceinline__ double squares(const GradChunk& c) {
   return (s[0] + s[1]) + (s[2] + s[3]);
 }
 
+template <bool STREAM>
 __global__ __launch_bounds__(256) void grad_squares_kernel(const GradChunk* chunks, int64_t n, double* sums) {
   __shared__ double shared[4];
   double s = 0.0;
   for (int64_t c = blockIdx.x; c < n; c += gridDim.x) {
     const GradChunk chunk = chunks[c];
-    s += chunk.dtype == PB_F32 ? squares<F32>(chunk) : chunk.dtype == PB_F16 ? squares<F16>(chunk) : squares<BF16>(chunk);
+    s += chunk.dtype == PB_F32 ? squares<F32, STREAM>(chunk) : chunk.dtype == PB_F16 ? squares<F16, STREAM>(chunk) : squares<BF16, STREAM>(chunk);
   }
   s = block_sum<4>(s, shared);
   if (threadIdx.x == 0) sums[blockIdx.x] = s;
@@ -95,15 +99,16 @@ __device__ __forceinline__ void scaled(const GradChunk& c, const GradChunk& out,
   for (; v < row.nv; v += 256) put(v, row.vec(v));
 }
 
-// (A norm that is not finite clips nothing: there is no factor for it.)  Pieces are taken from the last to the first: the last ones are
-// those that the norm has left in the caches.
+// (A norm that is not finite clips nothing: there is no factor for it.)  A workgroup takes the pieces that it has taken for the norm, from
+// the last to the first: the last ones are those that the norm has left in the caches, in that of its own part of the chip.
 template <bool STREAM>
 __global__ __launch_bounds__(256) void grad_clip_kernel(const GradChunk* chunks, const GradChunk* out, int64_t n, const float* norm, float max_norm) {
   const float is = *norm;
   const bool clips = is > max_norm && is < INFINITY;
   const float by = clips ? max_norm / is : 1.0f;
   if (!clips && out == chunks) return;
-  for (int64_t c = n - 1 - blockIdx.x; c >= 0; c -= gridDim.x) {
+  const int64_t grid = gridDim.x, full = grid < kGroups ? 0 : n / kGroups * kGroups;  // (a smaller grid has a piece for each workgroup)
+  for (int64_t c = blockIdx.x + (full + blockIdx.x < n ? full : full - grid); c >= 0; c -= grid) {
     const GradChunk from = chunks[c], to = out[c];
     if (from.dtype == PB_F32) scaled<F32, STREAM>(from, to, by);
     else if (from.dtype == PB_F16) scaled<F16, STREAM>(from, to, by);
@@ -116,17 +121,20 @@ int groups_for(int64_t chunks) { return static_cast<int>(chunks < kGroups ? chun
 }  // namespace gr
 
 int64_t grad_norm_workspace(int64_t chunks) { return gr::groups_for(chunks) * 8; }
-int launch_grad_norm(const GradChunk* chunks, int64_t n, float* norm, void* workspace, hipStream_t stream) {
+int launch_grad_norm(const GradChunk* chunks, int64_t n, int64_t bytes, float* norm, void* workspace, hipStream_t stream) {
   double* sums = static_cast<double*>(workspace);
   const int groups = gr::groups_for(n);
-  if (groups > 0) gr::grad_squares_kernel<<<groups, 256, 0, stream>>>(chunks, n, sums);
+  if (groups > 0 && bytes > gr::kStreamBytes) gr::grad_squares_kernel<true><<<groups, 256, 0, stream>>>(chunks, n, sums);
+  else if (groups > 0) gr::grad_squares_kernel<false><<<groups, 256, 0, stream>>>(chunks, n, sums);
   if (hipGetLastError() != hipSuccess) return PB_EHIP;
   gr::grad_norm_kernel<<<1, 1024, 0, stream>>>(sums, groups, norm);
   return hipGetLastError() == hipSuccess ? PB_OK : PB_EHIP;
 }
-int launch_grad_clip(const GradChunk* chunks, const GradChunk* out, int64_t n, const float* norm, float max_norm, hipStream_t stream) {
+int launch_grad_clip(const GradChunk* chunks, const GradChunk* out, int64_t n, int64_t bytes, const float* norm, float max_norm, hipStream_t stream) {
   if (n == 0) return PB_OK;
-  gr::grad_clip_kernel<false><<<gr::groups_for(n), 256, 0, stream>>>(chunks, out, n, norm, max_norm);
+  const int groups = gr::groups_for(n);
+  if (bytes > gr::kStreamBytes) gr::grad_clip_kernel<true><<<groups, 256, 0, stream>>>(chunks, out, n, norm, max_norm);
+  else gr::grad_clip_kernel<false><<<groups, 256, 0, stream>>>(chunks, out, n, norm, max_norm);
   return hipGetLastError() == hipSuccess ? PB_OK : PB_EHIP;
 }
 

@@ -79,14 +79,15 @@ struct GradChunk {
   int32_t dtype;
 };
 int64_t grad_norm_workspace(int64_t chunks);
-int launch_grad_norm(const GradChunk* chunks, int64_t n, float* norm, void* workspace, hipStream_t stream);
-int launch_grad_clip(const GradChunk* chunks, const GradChunk* out, int64_t n, const float* norm, float max_norm, hipStream_t stream);
+int launch_grad_norm(const GradChunk* chunks, int64_t n, int64_t bytes, float* norm, void* workspace, hipStream_t stream);
+int launch_grad_clip(const GradChunk* chunks, const GradChunk* out, int64_t n, int64_t bytes, const float* norm, float max_norm, hipStream_t stream);
 
 }  // namespace pb
 
 struct pb_tensors {
   pb::GradChunk* d_chunks = nullptr;
   int64_t count = 0;  // pieces
+  int64_t bytes = 0;  // of the tensors
   int device = -1;
   std::vector<int64_t> sizes;
   std::vector<int32_t> dtypes;
