@@ -12,7 +12,7 @@
 // Long rows take three launches: sums of all rows, a wave a part; then the decision and the deciding row's sums, several workgroups a
 // sequence; then the draw.  max(p - q, 0) needs the ratio of the two rows' sums, which the second launch has in fp32 only:
 // with it, it says which tokens lie above the line e_p = ratio e_q and sums both sides of those, so that the third can put
-// the exact ratio in, and the few slices where a token lies too near to the line are summed again there.
+// the exact ratio in; tokens that lie too near to the line for the first ratio are summed apart, with how near they come.
 #include <algorithm>
 
 #include "pb_logit_rows.hpp"
@@ -24,16 +24,19 @@ namespace vd {
 using namespace lr;
 using wv::first_lane;
 
-// Of a part of a row: the largest element m (-inf: nothing), the sum of e = 2^t, t = (x - m) c, in fp32 (NaN where it holds a NaN or +inf),
-// and that of e |t|; beside the first part, what the row has of the token drafted there.
+// Of a part of a row: the largest element m (-inf: nothing) and how many there are of it, the sum of e = 2^t, t = (x - m) c, over the others in fp32
+// (NaN where the part holds a NaN or +inf; beside a near-certain token the others' weight is not lost in its 1); beside the
+// first part, what the row has of the token drafted there.
 struct Sums {
-  float m, s, t, at;
+  float m, ones, s, at;
 };
-// How far a row's sum is off at most, relative to itself: each exponent by three roundings (of the difference, of c, of the product),
+// How far a row's sum s is off at most, relative to itself: each exponent by three roundings (of the difference, of c, of the product),
 // 3 ln 2 |t| 2^-24 of its term, its exponential by 2 x 2^-24, the sum by 13 additions one after the other (3 in a vector, 3 of vectors, the
-// edge, 6 in a wave; parts are joined in 64 bits).  Told from the row's own mean of |t|, which is some bits where log2 V, the
-// most there can be, is up to 19: the nearer u q may lie to p, and p to q, without a second look.
-__device__ __forceinline__ double off_by(double mean_t) { return (2.1 * mean_t + 16.0) * 0x1p-24; }
+// edge, 6 in a wave; parts are joined in 64 bits).  The mean of |t| = log2 (1 / e) over the row's probabilities e / s is at most the
+// logarithm of the mean of 1 / e, which is V / s (s >= 1).
+__device__ __forceinline__ double off_by(double s, int V) {
+  return static_cast<double>((2.1f * __builtin_amdgcn_logf(static_cast<float>(V) / static_cast<float>(s)) + 17.0f) * 0x1p-24f);
+}
 constexpr double kNothing = 0x1p-40;     // a rest of the target's mass below this is none (equal rows differ by their roundings)
 constexpr double kNoWeight = 0x1p-960;   // weights below this, masked tokens' among them, are none
 
@@ -95,16 +98,18 @@ __device__ __forceinline__ Sums part_sums(const Row<E>& row, int first, bool edg
     raw[u] = v < row.nv ? row.vec(v) : E::nothing();
   }
   if (edge && lane < row.edges) xe = E::up(row.x[row.edge_token(lane)]);
-  float m = fmaxf(-INFINITY, xe);
+  float m = fmaxf(-INFINITY, xe), most[EACH];
 #pragma unroll
   for (int u = 0; u < EACH; ++u) {
     float x[E::N];
     E::unpack(raw[u], x);
-    m = fmaxf(m, vec_max(x));
+    most[u] = vec_max(x);
+    m = fmaxf(m, most[u]);
   }
   m = wave_max(m);
-  const float c = static_cast<float>(c64), from = m == -INFINITY ? 0.0f : m;  // (inf - inf is a NaN, as is what a NaN leaves)
-  float s[EACH], t = 0.0f;
+  const float c = static_cast<float>(c64), from = m == -INFINITY ? 0.0f : m;
+  float s[EACH];
+  int ones = 0;
 #pragma unroll
   for (int u = 0; u < EACH; ++u) {
     s[u] = 0.0f;
@@ -112,16 +117,20 @@ __device__ __forceinline__ Sums part_sums(const Row<E>& row, int first, bool edg
     float x[E::N];
     E::unpack(raw[u], x);
 #pragma unroll
+    for (int i = 0; i < E::N; ++i) x[i] = exp2_fast((x[i] - from) * c);
+    s[u] = vec_sum(x);
+    if (__ballot(most[u] == from) == 0) continue;
+    E::unpack(raw[u], x);  // (again, without the largest elements)
+#pragma unroll
     for (int i = 0; i < E::N; ++i) {
-      const float d = (x[i] - from) * c;
-      x[i] = exp2_fast(d);
-      t = __builtin_fmaf(x[i], fmaxf(d, -200.0f), t);  // (not 0 times infinity)
+      ones += __builtin_popcountll(__ballot(x[i] == from));
+      x[i] = x[i] == from ? 0.0f : exp2_fast((x[i] - from) * c);
     }
     s[u] = vec_sum(x);
   }
-  const float de = (xe - from) * c, e = exp2_fast(de);
-  t = __builtin_fmaf(e, fmaxf(de, -200.0f), t);
-  return Sums{m, wave_sum(vec_sum(s) + e), -wave_sum(t), 0.0f};
+  const float e = xe == from ? 0.0f : exp2_fast((xe - from) * c);
+  ones += __builtin_popcountll(__ballot(xe == from));
+  return Sums{m, static_cast<float>(ones), wave_sum(vec_sum(s) + e) + (from - from), 0.0f};  // (inf - inf: NaN)
 }
 
 // The rows of a sequence: 0 .. n the target's, n + 1 .. 2 n the draft's.
@@ -264,23 +273,17 @@ __device__ __forceinline__ Verdict decide(const VerifyArgs& a, int64_t b, const 
     float m = part.m;
     for (int p = lane + 64; p < parts; p += 64) m = fmaxf(m, sums[j * parts + p].m);
     m = wave_max(m);
-    double s = 0.0, t = 0.0;
+    double s = 0.0;
     for (int p = lane; p < parts; p += 64) {
       if (p > lane) part = sums[j * parts + p];
-      if (part.m == -INFINITY) {
-        s += static_cast<double>(part.s);  // (0, or NaN)
-      } else {
-        const double w = weight(part.m, m, scale_of(c)), ahead = fmin((static_cast<double>(m) - static_cast<double>(part.m)) * c, 2000.0);
-        s += static_cast<double>(part.s) * w;
-        t += (static_cast<double>(part.t) + static_cast<double>(part.s) * ahead) * w;
-      }
+      s += part.m == -INFINITY ? static_cast<double>(part.s)  // (0, or NaN)
+                               : (static_cast<double>(part.ones) + static_cast<double>(part.s)) * weight(part.m, m, scale_of(c));
     }
     s = wave_sum64(s);
-    t = wave_sum64(t);
     if (lane == 0) {
       joined.m[j] = m;
       joined.s[j] = s;
-      joined.off[j] = off_by(t / s);
+      joined.off[j] = off_by(s, a.V);
     }
   }
   __syncthreads();
@@ -527,9 +530,11 @@ __global__ __launch_bounds__(64 * WAVES) void verify_small_kernel(VerifyArgs a, 
 
 // Long rows: several workgroups a sequence decide, each for itself, and sum their slices; the first leaves the verdict.
 struct Slice {
-  double p, q;      // sums of the weights
-  double above;     // of p - ratio q over the tokens above the line (the draft's token without rows aside), with the verdict's ratio
-  double above_q;   // of q over those; NaN: a token lies too near to the line
+  double p, q;              // sums of the weights
+  double above;             // of p - ratio q over the tokens above the line (the draft's token without rows aside), with the verdict's ratio
+  double above_q;           // of q over those
+  double near_p, near_q;    // of p and q over tokens that may lie on either side, which are not among those
+  double low, high;         // the least and the largest p / q - ratio of these (none: inf, -inf)
 };
 constexpr int kRestWaves = 16;
 template <typename E>
@@ -543,7 +548,7 @@ __global__ __launch_bounds__(64 * kRestWaves) void verify_rest_kernel(VerifyArgs
   const Rest<E> r(a, b, d);
   for (int s = blockIdx.x * kRestWaves + wave; s < slices; s += gridDim.x * kRestWaves) {
     const int v = (s * 64 + lane) * E::N;
-    Slice to{0.0, 0.0, 0.0, 0.0};
+    Slice to{0.0, 0.0, 0.0, 0.0, 0.0, 0.0, INFINITY, -INFINITY};
     if (r.y) {
       float xs[E::N], ys[E::N];
       load_at<E>(r.x, v, r.V, xs);
@@ -558,10 +563,32 @@ __global__ __launch_bounds__(64 * kRestWaves) void verify_rest_kernel(VerifyArgs
         to.above += fmax(rest, 0.0);
         to.above_q += rest > 0.0 ? q : 0.0;
       }
+      if (__ballot(near <= 0.0) != 0) {
+        to.above = to.above_q = 0.0;
+#pragma unroll 1
+        for (int i = 0; i < E::N; ++i) {
+          const double p = weight(xs[i], r.pm, r.pk), q = weight(ys[i], r.qm, r.qk), rest = fma(-d.ratio, q, p);
+          if (fabs(rest) <= d.near * d.ratio * q) {
+            to.near_p += p;
+            to.near_q += q;
+            to.low = fmin(to.low, rest / q);
+            to.high = fmax(to.high, rest / q);
+          } else if (rest > 0.0) {
+            to.above += rest;
+            to.above_q += q;
+          }
+        }
+        to.near_p = wave_sum64(to.near_p);
+        to.near_q = wave_sum64(to.near_q);
+#pragma unroll
+        for (int l = 1; l < 64; l *= 2) {
+          to.low = fmin(to.low, __shfl_xor(to.low, l, 64));
+          to.high = fmax(to.high, __shfl_xor(to.high, l, 64));
+        }
+      }
       to.q = wave_sum64(to.q);
       to.above = wave_sum64(to.above);
       to.above_q = wave_sum64(to.above_q);
-      if (__ballot(near <= 0.0) != 0) to.above_q = NAN;
     } else {
       double p[E::N], q[E::N], w[E::N];
       r.weights(v, p, q);
@@ -589,7 +616,7 @@ __global__ __launch_bounds__(64 * kPickWaves) void verify_pick_kernel(VerifyArgs
 #pragma unroll
   for (int k = 0; k < kEach; ++k) {
     const int s = threadIdx.x + k * 64 * kPickWaves;
-    mine[k] = s < slices ? in[s] : Slice{0.0, 0.0, 0.0, 0.0};
+    mine[k] = s < slices ? in[s] : Slice{0.0, 0.0, 0.0, 0.0, 0.0, 0.0, INFINITY, -INFINITY};
   }
   const float number = a.numbers[b * (a.n + 1) + a.n];
   const Verdict d = verdicts[b];
@@ -615,7 +642,13 @@ __global__ __launch_bounds__(64 * kPickWaves) void verify_pick_kernel(VerifyArgs
 #pragma unroll
     for (int k = 0; k < kEach; ++k) {
       const int s = threadIdx.x + k * 64 * kPickWaves;
-      const double v = whole ? mine[k].p : r.y ? fma(d.ratio - ratio, mine[k].above_q, mine[k].above) : mine[k].above;
+      double v = whole ? mine[k].p : mine[k].above;
+      if (!whole && r.y) {  // (a slice with tokens on both sides of the ratio that the last bits of their weights decide is summed again)
+        const double further = ratio - d.ratio, bits = ratio * 0x1p-44;
+        v = fma(-further, mine[k].above_q, v);
+        if (mine[k].low > further + bits) v += fma(-ratio, mine[k].near_q, mine[k].near_p);
+        else if (!(mine[k].high < further - bits)) v = NAN;
+      }
       if (s < slices) sums[s] = v != v || v > kNoWeight ? v : 0.0;
     }
     __syncthreads();

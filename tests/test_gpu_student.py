@@ -271,11 +271,15 @@ def check_verify(got, xv, yv, T, Ty, tokens, numbers, where):
     for b in range(len(out)):
         w_out, w_k, w_lp = S.verify(xv[b], None if yv is None else yv[b], T, Ty, tokens[b], numbers[b])
         assert acc[b] == w_k and np.array_equal(out[b], w_out), (where, b, acc[b], w_k, out[b], w_out)
-        if lp is not None:  # (the row's sum is off by 2^-18 of itself at most; 2^-40 of the row's spread is room for what 64 bits round)
-            spread = np.abs(np.where(np.isfinite(xv[b]), xv[b], 0.0)).max() / T + 20.0
+        if lp is not None:  # (what lies beside a row's largest token is off by 2^-18 of itself at most; 2^-50 of its spread for what 64 bits
+            # round; the sum of a row is 1 or more of its largest weight, rounded to 2^-53 of itself here and there, and so its logarithm)
             fin = ~np.isnan(w_lp)
+            room = np.zeros(len(w_lp))
+            for i in np.flatnonzero(fin):
+                p, lps, _ = S.probabilities(xv[b, i], T)
+                room[i] = 2.0 ** -18 * p[p < p.max()].sum() + 2.0 ** -50 * (lps.max() - w_lp[i])
             assert np.array_equal(np.isnan(lp[b]), ~fin), (where, b)
-            assert (np.abs(lp[b][fin] - w_lp[fin]) <= S.U * np.abs(w_lp[fin]) + 2.0 ** -18 + spread * 2.0 ** -40).all(), (where, b, lp[b], w_lp)
+            assert (np.abs(lp[b][fin] - w_lp[fin]) <= S.U * np.abs(w_lp[fin]) + room[fin] + 2.0 ** -51).all(), (where, b, lp[b], w_lp)
 
 
 def rows_for(rng, B, n, V, kind, odd):
@@ -287,7 +291,7 @@ def rows_for(rng, B, n, V, kind, odd):
             for i in range(z.shape[1]):
                 sort = int(rng.integers(0, 16)) if odd else 0
                 if sort == 1:
-                    z[b, i, rng.integers(0, V)] += 30.0
+                    z[b, i, rng.integers(0, V)] += float(rng.choice([12.0, 20.0, 30.0]))
                 elif sort == 2:
                     z[b, i] = 1.5
                 elif sort == 3:
@@ -414,6 +418,72 @@ def test_verify_equal_rows(V, kind):
     got = run_verify(px, py, kind, (V + 1, 3 * (V + 1)), (V, 2 * V + 3), 6, 2, V, 1.0, 1.0, tokens, numbers)
     check_verify(got, xv, yv, 1.0, 1.0, tokens, numbers, V)
     assert list(got[1]) == [2, 2, 2, 1, 1, 1] and (got[0][3:, 1] >= 0).all()
+
+
+def refused(y, x):
+    """A token whose p lies as far below its q as any, and a number that refuses it."""
+    q = np.array([S.probabilities(r, 1.0)[0] for r in y])
+    p = np.array([S.probabilities(r, 1.0)[0] for r in x])
+    return (p / q).argmin(axis=1), S.BELOW_1
+
+
+@pytest.mark.parametrize("V", [700, 5000, 20011, 131072])
+def test_verify_tokens_on_the_line(V):
+    """Draft and target agree on most tokens, and what some have more the others have less, so that p / q is 1 within 1e-8 on the many:
+    on which side they lie is for the last bits of the two sums to say."""
+    rng = np.random.default_rng(V)
+    B = 4
+    y = rng.normal(0, 1.5, (B, 1, V)).astype(np.float32).astype(np.float64)
+    x = np.repeat(y, 2, axis=1)
+    up, down = np.arange(V) % 50 == 3, np.arange(V) % 50 == 7
+    for b in range(B):
+        e = np.exp(y[b, 0])
+        more = (e[up] * (np.e - 1)).sum()
+        if more >= 0.9 * e[down].sum():
+            more, scale = 0.5 * e[down].sum(), np.log1p(0.5 * e[down].sum() / e[up].sum())
+        else:
+            scale = 1.0
+        x[b, 0, up] += np.float32(scale)
+        x[b, 0] = x[b, 0].astype(np.float32)
+        gain = (np.exp(x[b, 0, up]) - e[up]).sum()
+        x[b, 0, down] += np.float32(np.log1p(-gain / e[down].sum()))
+        x[b, 0] = x[b, 0].astype(np.float32)
+        # (both sides of the line, and nearer to it than roundings of the shifted ones allow: one token takes up the rest)
+        at = np.flatnonzero(down)[0]
+        left = np.exp(x[b, 0]).sum() - e.sum() - np.exp(x[b, 0, at])
+        x[b, 0, at] = np.float32(np.log(max(1e-30, -left) * (1 + (1e-6 if b % 2 else -1e-6))))
+    bx, px, xv = block(x, "f32", V, 2 * V)
+    by, py, yv = block(y, "f32", V, V)
+    tokens, u = refused(yv[:, 0], xv[:, 0])
+    for w in (0.0, 0.01, 0.3, 0.999):
+        numbers = np.tile([u, w], (B, 1))
+        got = run_verify(px, py, "f32", (V, 2 * V), (V, V), B, 1, V, 1.0, 1.0, tokens[:, None], numbers)
+        check_verify(got, xv, yv, 1.0, 1.0, tokens[:, None], numbers, (V, w))
+        assert (got[1] == 0).all()
+
+
+@pytest.mark.parametrize("kind", list(KIND))
+@pytest.mark.parametrize("V", [700, 5000, 20011, 131072])
+def test_verify_rows_that_are_all_but_equal(V, kind):
+    """Flat rows but for a few tokens that differ by 1e-5 (1e-2 in one case): numbers next to p / q, a rest of next to nothing."""
+    rng = np.random.default_rng(V + 1)
+    B = 6
+    y = np.zeros((B, 1, V))
+    x = np.zeros((B, 2, V))
+    for b in range(B):
+        size = 1e-2 if b == 5 else 1e-5
+        x[b, 0, rng.integers(0, V, 5)] = size
+        y[b, 0, rng.integers(0, V, 5)] = size * 2
+    bx, px, xv = block(x, kind, V, 2 * V)
+    by, py, yv = block(y, kind, V, V)
+    tokens, u = refused(yv[:, 0], xv[:, 0])
+    p = np.array([S.probabilities(xv[b, 0], 1.0)[0][tokens[b]] / S.probabilities(yv[b, 0], 1.0)[0][tokens[b]] for b in range(B)])
+    for shift in (-2, -1, 1, 2):    # (fp32 numbers on either side of the line, but not on it)
+        number = (np.float32(p) + shift * np.spacing(np.float32(p))).astype(np.float32)
+        numbers = np.stack([number, rng.random(B).astype(np.float32)], axis=1)
+        got = run_verify(px, py, kind, (V, 2 * V), (V, V), B, 1, V, 1.0, 1.0, tokens[:, None], numbers)
+        check_verify(got, xv, yv, 1.0, 1.0, tokens[:, None], numbers, (V, kind, shift))
+        assert (got[1] == (shift < 0)).all()
 
 
 def test_verify_rows_behind_the_end_are_not_read():
