@@ -694,9 +694,9 @@ int pb_verify_draft(const void* d_target_logits, const void* d_draft_logits, int
   if ((n_draft > 0) != (d_draft_tokens != nullptr) || !d_uniforms || !d_tokens || !d_accepted) return PB_EINVAL;
   if (!aligned(d_draft_tokens, 4) || !aligned(d_uniforms, 4) || !aligned(d_tokens, 4) || !aligned(d_accepted, 4) || !aligned(d_logp, 4)) return PB_EINVAL;
   if (check_workspace(need, d_workspace, workspace_bytes) != PB_OK) return PB_EINVAL;
-  const double log2_e = 1.44269504088896340736;
+  auto scale = [](float t) { return pb::VerifyArgs::Scale{1.44269504088896340736 / t, -1000.0 * t / 1.44269504088896340736}; };
   const pb::VerifyArgs a{d_target_logits, d_draft_logits, target_seq_stride, target_row_stride, draft_seq_stride, draft_row_stride, sequences, n_draft, vocab_size,
-                         log2_e / temperature, d_draft_logits ? log2_e / draft_temperature : 0.0, d_draft_tokens, d_uniforms, d_tokens, d_accepted, d_logp};
+                         scale(temperature), scale(d_draft_logits ? draft_temperature : 1.0f), d_draft_tokens, d_uniforms, d_tokens, d_accepted, d_logp};
   return in_slices(sequences, pb::verify_draft_slice(dtype, n_draft, vocab_size), [&](size_t at, int32_t n) {
     pb::VerifyArgs s = a;
     const int64_t from = static_cast<int64_t>(at);

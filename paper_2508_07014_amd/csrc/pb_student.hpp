@@ -30,7 +30,9 @@ struct VerifyArgs {
   const void* draft;   // [sequences, n] rows; null: the draft was sure of its tokens
   int64_t target_seq, target_row, draft_seq, draft_row;  // strides in elements
   int32_t sequences, n, V;
-  double target_c, draft_c;  // log2(e) / T
+  struct Scale {
+    double c, low;  // log2(e) / T, and the difference below which weights do not go (2^-1000)
+  } target_scale, draft_scale;
   const int32_t* tokens;     // [sequences, n]
   const float* numbers;      // [sequences, n + 1]
   int32_t* out;              // [sequences, n + 1]

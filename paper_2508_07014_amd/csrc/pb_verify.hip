@@ -40,11 +40,7 @@ __device__ __forceinline__ double off_by(double s, int V) {
 constexpr double kNothing = 0x1p-40;     // a rest of the target's mass below this is none (equal rows differ by their roundings)
 constexpr double kNoWeight = 0x1p-960;   // weights below this, masked tokens' among them, are none
 
-// What turns x - m into a weight: log2(e) / T, and the difference below which weights do not go (2^-1000).
-struct Scale {
-  double c, low;
-};
-__device__ __forceinline__ Scale scale_of(double c) { return Scale{c, -1000.0 / c}; }
+typedef VerifyArgs::Scale Scale;
 
 // 2^((x - m) c) for x <= m, at least 2^-1000, off by 4e-14 of itself: with n the nearest integer to the exponent (in the low word of
 // the sum with 1.5 2^52) and r what is left, 1 + r P(r), P by interpolation at Chebyshev's nodes, and n added to the exponent.  (16
@@ -183,7 +179,7 @@ __global__ __launch_bounds__(256) void verify_sums_kernel(VerifyArgs a, int rows
   const Row<E> row = row_of<E>(a, b, j);
   float at = 0.0f;
   if (part == 0 && i < tokens.count) at = E::up(row.x[__builtin_amdgcn_readlane(tokens.t, i)]);
-  Sums s = part_sums<E, EACH>(row, part * 64 * EACH, part == 0, j <= a.n ? a.target_c : a.draft_c, lane);
+  Sums s = part_sums<E, EACH>(row, part * 64 * EACH, part == 0, j <= a.n ? a.target_scale.c : a.draft_scale.c, lane);
   s.at = at;
   if (lane == 0) sums[item] = s;
 }
@@ -206,9 +202,9 @@ struct RowSums {
   double turn[16];       // a place a wave
 };
 
-__device__ __forceinline__ double share(float x, float m, double s, double c) {  // (a row of nothing but -inf: s = 0; a marked one: NaN)
+__device__ __forceinline__ double share(float x, float m, double s, const Scale& k) {  // (a row of nothing but -inf: s = 0; a marked one: NaN)
   if (m == -INFINITY) return s;
-  const double w = weight(x, m, scale_of(c));
+  const double w = weight(x, m, k);
   return (w > kNoWeight ? w : 0.0) / s;
 }
 __device__ __forceinline__ float log_share(float x, float m, double s, double c) {
@@ -238,9 +234,8 @@ __device__ __forceinline__ double lane_sum(const double (&w)[N]) {
 
 // A row's sum in 64 bits, by the whole workgroup.
 template <typename E, int WAVES>
-__device__ __forceinline__ double row_sum(const typename E::type* x, int V, float m, double c, double (&turn)[16]) {
+__device__ __forceinline__ double row_sum(const typename E::type* x, int V, float m, const Scale& k, double (&turn)[16]) {
   const int lane = threadIdx.x & 63, wave = uniform_i(threadIdx.x >> 6);
-  const Scale k = scale_of(c);
   double s = 0.0;
   for (int slice = wave; slice < slices_of<E>(V); slice += WAVES) {
     float xs[E::N];
@@ -267,7 +262,7 @@ __device__ __forceinline__ Verdict decide(const VerifyArgs& a, int64_t b, const 
   const typename E::type* target = static_cast<const typename E::type*>(a.target) + b * a.target_seq;
   const typename E::type* draft = a.draft ? static_cast<const typename E::type*>(a.draft) + b * a.draft_seq : nullptr;
   for (int j = wave; j < rows; j += WAVES) {  // (rows behind the end of the draft too, whose sums nobody has written and nobody looks at)
-    const double c = j <= a.n ? a.target_c : a.draft_c;
+    const Scale k = j <= a.n ? a.target_scale : a.draft_scale;
     Sums part{-INFINITY, 0.0f, 0.0f, 0.0f};
     if (lane < parts) part = sums[j * parts + lane];
     float m = part.m;
@@ -277,7 +272,7 @@ __device__ __forceinline__ Verdict decide(const VerifyArgs& a, int64_t b, const 
     for (int p = lane; p < parts; p += 64) {
       if (p > lane) part = sums[j * parts + p];
       s += part.m == -INFINITY ? static_cast<double>(part.s)  // (0, or NaN)
-                               : (static_cast<double>(part.ones) + static_cast<double>(part.s)) * weight(part.m, m, scale_of(c));
+                               : (static_cast<double>(part.ones) + static_cast<double>(part.s)) * weight(part.m, m, k);
     }
     s = wave_sum64(s);
     if (lane == 0) {
@@ -292,8 +287,8 @@ __device__ __forceinline__ Verdict decide(const VerifyArgs& a, int64_t b, const 
     bool unsure = false;
     takes = false;
     if (lane < count) {
-      const double p = share(xt, joined.m[lane], joined.s[lane], a.target_c);
-      const double q = draft ? share(yt, joined.m[a.n + 1 + lane], joined.s[a.n + 1 + lane], a.draft_c) : 1.0;
+      const double p = share(xt, joined.m[lane], joined.s[lane], a.target_scale);
+      const double q = draft ? share(yt, joined.m[a.n + 1 + lane], joined.s[a.n + 1 + lane], a.draft_scale) : 1.0;
       const double uq = static_cast<double>(u) * q;
       takes = uq < p;  // (false for NaN)
       unsure = p > 0.0 && fabs(uq - p) <= p * (joined.off[lane] + (draft ? joined.off[a.n + 1 + lane] : 0.0) + 0x1p-40) && !((exact >> lane) & 1u);
@@ -302,8 +297,8 @@ __device__ __forceinline__ Verdict decide(const VerifyArgs& a, int64_t b, const 
     const u64 open = __ballot(unsure) & ((1ull << stop) - 1);
     if (open == 0) break;
     const int i = first_lane(open);
-    const double ps = row_sum<E, WAVES>(target + i * a.target_row, a.V, joined.m[i], a.target_c, joined.turn);
-    const double qs = draft ? row_sum<E, WAVES>(draft + i * a.draft_row, a.V, joined.m[a.n + 1 + i], a.draft_c, joined.turn) : 0.0;
+    const double ps = row_sum<E, WAVES>(target + i * a.target_row, a.V, joined.m[i], a.target_scale, joined.turn);
+    const double qs = draft ? row_sum<E, WAVES>(draft + i * a.draft_row, a.V, joined.m[a.n + 1 + i], a.draft_scale, joined.turn) : 0.0;
     __syncthreads();
     if (threadIdx.x == 0) {
       if (joined.m[i] != -INFINITY) joined.s[i] = ps;
@@ -332,7 +327,7 @@ __device__ __forceinline__ Verdict decide(const VerifyArgs& a, int64_t b, const 
   if (writes && wave == WAVES - 1) {
     if (lane <= a.n && (lane != r.k || r.none)) {  // (the token at k is drawn later)
       a.out[b * (a.n + 1) + lane] = lane < r.k ? t : -1;
-      if (a.logp) a.logp[b * (a.n + 1) + lane] = lane < r.k ? log_share(xt, joined.m[lane], joined.s[lane], a.target_c) : NAN;
+      if (a.logp) a.logp[b * (a.n + 1) + lane] = lane < r.k ? log_share(xt, joined.m[lane], joined.s[lane], a.target_scale.c) : NAN;
     }
     if (lane == 0) a.accepted[b] = r.k;
   }
@@ -363,7 +358,7 @@ struct Rest {
   __device__ __forceinline__ Rest(const VerifyArgs& a, int64_t b, const Verdict& d)
       : x(static_cast<const typename E::type*>(a.target) + b * a.target_seq + d.k * a.target_row),
         y(d.qm == -INFINITY ? nullptr : static_cast<const typename E::type*>(a.draft) + b * a.draft_seq + d.k * a.draft_row),
-        V(a.V), barred(a.draft ? -1 : d.refused), pm(d.pm), qm(d.qm), pk(scale_of(a.target_c)), qk(scale_of(a.draft ? a.draft_c : 1.0)) {}
+        V(a.V), barred(a.draft ? -1 : d.refused), pm(d.pm), qm(d.qm), pk(a.target_scale), qk(a.draft_scale) {}
   // Of elements v .. v + N - 1 (next to nothing past the row).
   __device__ __forceinline__ void weights(int v, double (&p)[E::N], double (&q)[E::N]) const {
     float xs[E::N], ys[E::N];
@@ -438,23 +433,23 @@ __device__ __forceinline__ void write_drawn(const VerifyArgs& a, int64_t b, cons
   if (lane != 0) return;
   const int64_t at = b * (a.n + 1) + d.k;
   a.out[at] = token;
-  if (a.logp) a.logp[at] = token < 0 ? NAN : log_share(target_at<E>(a, b, d.k, token), d.pm, ps, a.target_c);
+  if (a.logp) a.logp[at] = token < 0 ? NAN : log_share(target_at<E>(a, b, d.k, token), d.pm, ps, a.target_scale.c);
 }
 
 // Rows of up to WAVES * HELD slices: a workgroup a sequence holds the rows that decide in registers.
-constexpr int kHeld = 2;
+constexpr int kHeld = 2;  // at most
 template <int WAVES>
 struct DrawShared {
   double p[WAVES], q[WAVES], slices[WAVES * kHeld];
 };
-template <typename E, int WAVES>
+template <typename E, int WAVES, int HELD>
 __device__ __forceinline__ void draw_held(const VerifyArgs& a, int64_t b, const Verdict& d, DrawShared<WAVES>& shared) {
   const int lane = threadIdx.x & 63, wave = uniform_i(threadIdx.x >> 6), slices = slices_of<E>(a.V);
   const float number = a.numbers[b * (a.n + 1) + a.n];
   const Rest<E> r(a, b, d);
-  double p[kHeld][E::N], q[kHeld][E::N], ps = 0.0, qs = 0.0;
+  double p[HELD][E::N], q[HELD][E::N], ps = 0.0, qs = 0.0;
 #pragma unroll
-  for (int h = 0; h < kHeld; ++h) {
+  for (int h = 0; h < HELD; ++h) {
     if (wave + h * WAVES >= slices) break;
     r.weights(((wave + h * WAVES) * 64 + lane) * E::N, p[h], q[h]);
     ps += lane_sum(p[h]);
@@ -471,9 +466,9 @@ __device__ __forceinline__ void draw_held(const VerifyArgs& a, int64_t b, const 
   qs = wave_sum64(lane < WAVES ? shared.q[lane] : 0.0);
   const double ratio = r.y ? ps / qs : 0.0;
   for (bool whole = d.refused < 0;; whole = true) {
-    double w[kHeld][E::N];
+    double w[HELD][E::N];
 #pragma unroll
-    for (int h = 0; h < kHeld; ++h) {
+    for (int h = 0; h < HELD; ++h) {
       const int s = wave + h * WAVES;
       if (s >= slices) break;
       r.rest((s * 64 + lane) * E::N, p[h], q[h], ratio, whole, w[h]);
@@ -488,23 +483,23 @@ __device__ __forceinline__ void draw_held(const VerifyArgs& a, int64_t b, const 
     }
     const Place at = place_of(shared.slices, slices, number, all, lane);
 #pragma unroll
-    for (int h = 0; h < kHeld; ++h)
+    for (int h = 0; h < HELD; ++h)
       if (at.slice == wave + h * WAVES) write_drawn<E>(a, b, d, ps, find_in_slice(w[h], at, lane), lane);
     return;
   }
 }
-template <typename E, int WAVES>
+template <typename E, int WAVES, int HELD>
 __global__ __launch_bounds__(64 * WAVES) void verify_draw_kernel(VerifyArgs a, int rows, int parts, const Sums* sums) {
   __shared__ RowSums joined;
   __shared__ DrawShared<WAVES> shared;
   const int64_t b = blockIdx.x;
   const Verdict d = decide_rows<E, WAVES>(a, b, sums, rows, parts, joined, true);
-  if (!d.none) draw_held<E, WAVES>(a, b, d, shared);
+  if (!d.none) draw_held<E, WAVES, HELD>(a, b, d, shared);
 }
 
 // All of a sequence in one workgroup, where its rows have few parts.
 constexpr int kSmallItems = 32;
-template <typename E, int WAVES, int EACH>
+template <typename E, int WAVES, int EACH, int HELD>
 __global__ __launch_bounds__(64 * WAVES) void verify_small_kernel(VerifyArgs a, int rows, int parts) {
   __shared__ RowSums joined;
   __shared__ Sums sums[kSmallItems];
@@ -520,12 +515,12 @@ __global__ __launch_bounds__(64 * WAVES) void verify_small_kernel(VerifyArgs a, 
   for (int item = wave; item < rows * parts; item += WAVES) {
     const int j = item / parts, part = item - j * parts;
     if (j <= a.n ? j > tokens.count : j - a.n - 1 >= tokens.count) continue;
-    const Sums s = part_sums<E, EACH>(row_of<E>(a, b, j), part * 64 * EACH, part == 0, j <= a.n ? a.target_c : a.draft_c, lane);
+    const Sums s = part_sums<E, EACH>(row_of<E>(a, b, j), part * 64 * EACH, part == 0, j <= a.n ? a.target_scale.c : a.draft_scale.c, lane);
     if (lane == 0) sums[item] = s;
   }
   __syncthreads();
   const Verdict d = decide<E, WAVES>(a, b, tokens, xt, yt, sums, rows, parts, joined, true);
-  if (!d.none) draw_held<E, WAVES>(a, b, d, shared);
+  if (!d.none) draw_held<E, WAVES, HELD>(a, b, d, shared);
 }
 
 // Long rows: several workgroups a sequence decide, each for itself, and sum their slices; the first leaves the verdict.
@@ -712,7 +707,9 @@ int forward(const VerifyArgs& a, void* workspace, hipStream_t stream) {
   auto done = [] { return hipGetLastError() == hipSuccess ? PB_OK : PB_EHIP; };
   const Plan p = plan<E>(a.sequences, a.n, a.draft != nullptr, a.V);
   if (p.groups < 0) {
-    verify_small_kernel<E, 16, 8><<<a.sequences, 1024, 0, stream>>>(a, p.rows, p.parts);
+    if (a.V <= 4 * 64 * E::N) verify_small_kernel<E, 16, 4, 1><<<a.sequences, 1024, 0, stream>>>(a, p.rows, p.parts);
+    else if (slices_of<E>(a.V) <= 16) verify_small_kernel<E, 16, 8, 1><<<a.sequences, 1024, 0, stream>>>(a, p.rows, p.parts);
+    else verify_small_kernel<E, 16, 8, 2><<<a.sequences, 1024, 0, stream>>>(a, p.rows, p.parts);
     return done();
   }
   char* ws = static_cast<char*>(workspace);
@@ -722,7 +719,8 @@ int forward(const VerifyArgs& a, void* workspace, hipStream_t stream) {
   else verify_sums_kernel<E, 8><<<grid, 256, 0, stream>>>(a, p.rows, p.parts, sums);
   if (done() != PB_OK) return PB_EHIP;
   if (p.groups == 0) {
-    verify_draw_kernel<E, 16><<<a.sequences, 1024, 0, stream>>>(a, p.rows, p.parts, sums);
+    if (slices_of<E>(a.V) <= 16) verify_draw_kernel<E, 16, 1><<<a.sequences, 1024, 0, stream>>>(a, p.rows, p.parts, sums);
+    else verify_draw_kernel<E, 16, 2><<<a.sequences, 1024, 0, stream>>>(a, p.rows, p.parts, sums);
     return done();
   }
   Verdict* verdicts = reinterpret_cast<Verdict*>(ws + p.verdicts);
