@@ -36,10 +36,11 @@ __device__ __forceinline__ void load_vector(const typename E::type* p, float (&x
     for (int i = 0; i < 4; ++i) x[i] = both[i];
   }
 }
-template <typename E, int K>
+template <typename E, bool STREAM, int K>
 __device__ __forceinline__ void store_vector_of(typename E::type* p, const float (&x)[K]) {
   if constexpr (E::N == K) {
-    stream_vector<E>(p, E::pack(x));
+    if constexpr (STREAM) stream_vector<E>(p, E::pack(x));
+    else store_vector<E>(p, E::pack(x));
   } else if constexpr (K == 8) {
     const float lo[4] = {x[0], x[1], x[2], x[3]}, hi[4] = {x[4], x[5], x[6], x[7]};
     store_vector<E>(p, E::pack(lo));
@@ -74,7 +75,7 @@ struct Columns {
       load_vector<E>(row + at[s], x);
     }
   }
-  template <typename E>
+  template <typename E, bool STREAM = true>
   __device__ __forceinline__ void store(typename E::type* row, int s, const float (&x)[K]) const {
     if constexpr (NARROW) {
 #pragma unroll
@@ -82,7 +83,7 @@ struct Columns {
         if (skip[s] == 0 && i < dim) row[i] = E::down(x[i]);
       return;
     }
-    if (skip[s] == 0) return store_vector_of<E>(row + at[s], x);
+    if (skip[s] == 0) return store_vector_of<E, STREAM>(row + at[s], x);
 #pragma unroll
     for (int i = 1; i < K; ++i)
       if (i >= skip[s]) row[at[s] + i] = E::down(x[i]);
@@ -162,6 +163,25 @@ __device__ __forceinline__ int group_upto(int v, int* s, int* total) {
   return ahead + upto;
 }
 
+// Tokens of a range that occur more than kFew times, for the launch that joins their pieces (in any order).
+constexpr int kFew = 32;
+struct Owner {
+  int v, begin, end;
+};
+struct Owners {
+  int32_t* count;  // [ranges]
+  Owner* list;     // [ranges << shift]
+};
+// By all threads of the range's workgroup, the thread's own token with its places (n: a place in LDS).
+__device__ __forceinline__ void write_owners(const Owners& o, int range, int v0, int size, int at, int end, int* n) {
+  const int tid = threadIdx.x;
+  if (tid == 0) *n = 0;
+  __syncthreads();
+  if (tid < size && end - at > kFew) o.list[v0 + atomicAdd(n, 1)] = Owner{v0 + tid, at, end};
+  __syncthreads();
+  if (tid == 0) o.count[range] = *n;
+}
+
 // counts[wave][i], i < size: how many of each wave; becomes the place of the wave's first, `base` ahead of them all.  Returns
 // the place of the thread's i (and in *end what follows it).
 __device__ __forceinline__ int places(int* counts, int stride, int size, int base, int* s, int* end) {
@@ -217,7 +237,7 @@ __device__ __forceinline__ void place_keys(int* counters, unsigned key, bool in,
   __builtin_amdgcn_wave_barrier();
 }
 
-__global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(const int32_t* tokens, int n, int V, int shift, int32_t* begin, int32_t* order) {
+__global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(const int32_t* tokens, int n, int V, int shift, int32_t* begin, int32_t* order, Owners owners) {
   extern __shared__ int counts[];  // [kSortWaves][2^shift]
   __shared__ int s[kSortWaves];
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform_i(tid >> 6), range = 1 << shift;
@@ -249,6 +269,7 @@ __global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(const int32_t*
     begin[v0 + tid] = at;
     if (v0 + tid == V - 1) begin[V] = end;
   }
+  write_owners(owners, blockIdx.x, v0, size, at, end, s);
   auto put = [&](int t, int from) {
     const unsigned u = static_cast<unsigned>(t) - static_cast<unsigned>(v0);
     place_keys(mine, u, u < static_cast<unsigned>(size), shift, lane, [&](int to) { order[to] = from; });
@@ -296,7 +317,7 @@ __global__ __launch_bounds__(kSortThreads) void embed_split_kernel(const int32_t
 
 // A range's positions from all chunks: each wave takes some chunks next to each other.
 __global__ __launch_bounds__(kSortThreads) void embed_merge_kernel(const unsigned* entries, const int32_t* starts, int chunks, int V, int shift, int ranges,
-                                                                  int32_t* begin, int32_t* order) {
+                                                                  int32_t* begin, int32_t* order, Owners owners) {
   extern __shared__ int counts[];  // [kSortWaves][2^shift]
   __shared__ int s[kSortWaves];
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform_i(tid >> 6), range = 1 << shift, b = blockIdx.x;
@@ -326,7 +347,14 @@ __global__ __launch_bounds__(kSortThreads) void embed_merge_kernel(const unsigne
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           if (i0[k] < i1[k]) f(e[k], i0[k] + lane < i1[k], q + k0 + k);
-          for (int i = i0[k] + 64; i < i1[k]; i += 64) f(i + lane < i1[k] ? entries[static_cast<int64_t>(q + k0 + k) * kSplit + i + lane] : 0u, i + lane < i1[k], q + k0 + k);
+          for (int i = i0[k] + 64; i < i1[k]; i += 64 * 8) {
+            unsigned more[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) more[u] = i + 64 * u + lane < i1[k] ? entries[static_cast<int64_t>(q + k0 + k) * kSplit + i + 64 * u + lane] : 0u;
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+              if (i + 64 * u < i1[k]) f(more[u], i + 64 * u + lane < i1[k], q + k0 + k);
+          }
         }
       }
     }
@@ -340,6 +368,7 @@ __global__ __launch_bounds__(kSortThreads) void embed_merge_kernel(const unsigne
     begin[v0 + tid] = at;
     if (v0 + tid == V - 1) begin[V] = end;
   }
+  write_owners(owners, b, v0, size, at, end, s);
   all([&](unsigned e, bool is, int c) {
     place_keys(mine, e / kSplit, is, shift, lane, [&](int to) { order[to] = c * kSplit + static_cast<int>(e % kSplit); });
   });
@@ -348,8 +377,6 @@ __global__ __launch_bounds__(kSortThreads) void embed_merge_kernel(const unsigne
 // Sums.  Tokens with up to kFew positions are summed by `lanes` lanes at once; those with more in pieces, cut at every kFew-th place of
 // the order, which a second launch joins.  A stretch of kFew places holds pieces of two such tokens at most: one that
 // began before it or at its first place, and one that begins later in it.
-constexpr int kFew = 32;
-
 struct SumArgs {
   EmbedGradArgs a;
   const int32_t* begin;  // [V + 1]
@@ -405,7 +432,7 @@ __device__ __forceinline__ void write_columns(const EmbedGradArgs& a, const Colu
 template <int K, int SL, bool NARROW>
 __device__ __forceinline__ void write_piece(float* to, const Columns<K, SL, NARROW>& cols, const float (&sum)[SL][K]) {
 #pragma unroll
-  for (int u = 0; u < SL; ++u) cols.template store<F32>(to, u, sum[u]);
+  for (int u = 0; u < SL; ++u) cols.template store<F32, false>(to, u, sum[u]);
 }
 
 // A stretch's pieces, `lanes` lanes a vector of each of its columns.
@@ -451,24 +478,17 @@ __global__ __launch_bounds__(256) void embed_sums_kernel(SumArgs s, int stretch_
   write_columns<T>(a, cols, v, sum);
 }
 
-// Pieces of a token, in the order of their stretches: a workgroup looks through some stretches for tokens that begin there, and for each
-// its groups of lanes sum a share of the pieces, and one of them those sums.
+// Pieces of a token, in the order of their stretches: a workgroup a range (and vectors of its columns).  Its groups of lanes take the tokens
+// of few pieces one each; of the others, each group sums a share of the pieces, and the first of them those sums.
 constexpr int kJoinThreads = 1024;
 template <typename T, int K, bool NARROW>
-__global__ __launch_bounds__(kJoinThreads) void embed_join_kernel(SumArgs s, int stretches) {
+__global__ __launch_bounds__(kJoinThreads) void embed_join_kernel(SumArgs s, Owners owners, int shift) {
   __shared__ float shares[kJoinThreads * K];
-  __shared__ int owners[kJoinThreads], n_owners;
   const EmbedGradArgs& a = s.a;
-  const int tid = threadIdx.x, groups = kJoinThreads / s.lanes, group = tid / s.lanes, lane = tid & (s.lanes - 1), end = s.begin[a.V];
-  if (static_cast<int64_t>(blockIdx.x) * groups * kFew >= end) return;
-  if (tid == 0) n_owners = 0;
-  __syncthreads();
-  const int mine = blockIdx.x * groups + tid;
-  if (tid < groups && mine < stretches && mine * kFew < end) {
-    const int v = a.tokens[s.order[min(end, mine * kFew + kFew) - 1]], i = s.begin[v], j = s.begin[v + 1];
-    if (j - i > kFew && i / kFew == mine) owners[atomicAdd(&n_owners, 1)] = v;
-  }
-  __syncthreads();
+  const int n_owners = owners.count[blockIdx.x];
+  const Owner* list = owners.list + (static_cast<int64_t>(blockIdx.x) << shift);
+  if (n_owners == 0) return;
+  const int tid = threadIdx.x, groups = kJoinThreads / s.lanes, group = tid / s.lanes, lane = tid & (s.lanes - 1);
   const Columns<K, 1, NARROW> cols(a.dim, blockIdx.y * s.lanes * K, s.lanes, lane);
   const int64_t row = 2 * static_cast<int64_t>(a.dim);
   constexpr int U = 8, kFewPieces = 16;
@@ -487,19 +507,21 @@ __global__ __launch_bounds__(kJoinThreads) void embed_join_kernel(SumArgs s, int
         for (int e = 0; e < K; ++e) sum[0][e] += k + u < k1 ? x[u][e] : 0.0f;
     }
   };
-  for (int o = group; o < n_owners; o += groups) {  // (each by itself: their order does not matter)
-    const int v = owners[o], i = s.begin[v], c = i / kFew, last = (s.begin[v + 1] + kFew - 1) / kFew;
+  for (int o = group; o < n_owners; o += groups) {
+    const Owner w = list[o];
+    const int c = w.begin / kFew, last = (w.end + kFew - 1) / kFew;
     if (last - c > kFewPieces) continue;
     float sum[1][K] = {};
-    add(i, c, last, sum);
-    write_columns<T>(a, cols, v, sum);
+    add(w.begin, c, last, sum);
+    write_columns<T>(a, cols, w.v, sum);
   }
   for (int o = 0; o < n_owners; ++o) {
-    const int v = owners[o], i = s.begin[v], c = i / kFew, last = (s.begin[v + 1] + kFew - 1) / kFew;
+    const Owner w = list[o];
+    const int c = w.begin / kFew, last = (w.end + kFew - 1) / kFew;
     if (last - c <= kFewPieces) continue;
     const int share = (last - c + groups - 1) / groups;
     float sum[1][K] = {};
-    add(i, c + group * share, min(last, c + (group + 1) * share), sum);
+    add(w.begin, c + group * share, min(last, c + (group + 1) * share), sum);
 #pragma unroll
     for (int e = 0; e < K; ++e) shares[e * kJoinThreads + tid] = sum[0][e];
     __syncthreads();
@@ -507,7 +529,7 @@ __global__ __launch_bounds__(kJoinThreads) void embed_join_kernel(SumArgs s, int
       for (int q = 1; q < groups && c + q * share < last; ++q)
 #pragma unroll
         for (int e = 0; e < K; ++e) sum[0][e] += shares[e * kJoinThreads + q * s.lanes + lane];
-      write_columns<T>(a, cols, v, sum);
+      write_columns<T>(a, cols, w.v, sum);
     }
     __syncthreads();
   }
@@ -516,14 +538,13 @@ __global__ __launch_bounds__(kJoinThreads) void embed_join_kernel(SumArgs s, int
 // Few tokens on a small table, all in one launch: a workgroup a token (and vectors of its columns) looks through the tokens for its
 // positions, waves in their order, its groups of lanes sum a share of those each, and the first of them those sums.
 constexpr int kSmallTokens = 4096;
-template <typename G, typename T, bool NARROW>
+template <typename G, typename T, int kTurns, bool NARROW>
 __global__ __launch_bounds__(256) void embed_small_kernel(SumArgs s) {
   constexpr int K = step_of<G, T>();
-  __shared__ int list[kSmallTokens], found[4];
+  __shared__ int list[256 * kTurns], found[4];
   __shared__ float shares[256 * K];
   const EmbedGradArgs& a = s.a;
   const int tid = threadIdx.x, v = blockIdx.x, wave = uniform_i(tid >> 6), lane64 = tid & 63;
-  constexpr int kTurns = kSmallTokens / 256;
   const int turns = (a.n + 255) / 256, p0 = wave * turns * 64 + lane64;
   u64 here[kTurns];
   int t[kTurns], count = 0;
@@ -597,17 +618,19 @@ int launch_embed_tokens(int table_dtype, int out_dtype, const EmbedArgs& a, hipS
 namespace em {
 // What lies where in the workspace.
 struct Layout {
-  int64_t begin, order, pieces, entries, starts, bytes;
+  int64_t begin, order, count, list, pieces, entries, starts, bytes;
 };
 Layout layout(int32_t n, int32_t V, int32_t dim) {
   Layout l;
   l.begin = 0;
   l.order = padded((static_cast<int64_t>(V) + 1) * 4);
-  l.pieces = l.order + padded(static_cast<int64_t>(n) * 4);
+  const int shift = shift_for(V), ranges = ((V - 1) >> shift) + 1;
+  l.count = l.order + padded(static_cast<int64_t>(n) * 4);
+  l.list = l.count + padded(static_cast<int64_t>(ranges) * 4);
+  l.pieces = l.list + padded((static_cast<int64_t>(ranges) << shift) * static_cast<int64_t>(sizeof(Owner)));
   l.bytes = l.pieces + (n > kFew ? padded((static_cast<int64_t>(n) + kFew - 1) / kFew * 2 * dim * 4) : 0);
   l.entries = l.starts = l.pieces;  // (entries and starts are done with before there are pieces)
   if (n >= kManyTokens) {
-    const int64_t ranges = ((V - 1) >> shift_for(V)) + 1;
     l.starts = l.entries + padded(static_cast<int64_t>(n) * 4);
     l.bytes = std::max(l.bytes, l.starts + padded((static_cast<int64_t>(n) + kSplit - 1) / kSplit * (ranges + 1) * 4));
   }
@@ -624,7 +647,9 @@ struct Shape {
   int lanes, vectors;
   explicit Shape(int dim) : lanes(lanes_for(dim, K)), vectors((dim + lanes * K - 1) / (lanes * K)) {}
 };
-bool small(int64_t n, int64_t V, int vectors) { return n <= kSmallTokens && V * vectors <= 16384; }
+// us, in one launch / in three: 4096 tokens, 1025 x 640 fp32 12.7 / 19.2, 100 x 2048 13.5 / 22.4, 8192 x 512 bf16 (8192 workgroups) 21.6 / 16.3;
+// 1000 tokens, 16384 x 256 fp32 (16384 of them) 28.0 / 15.2; 300 tokens of those 26.2 / 13.1.
+bool small(int64_t n, int64_t V, int vectors) { return n <= kSmallTokens && V * vectors <= 6144; }
 
 template <typename G, typename T>
 int backward(const EmbedGradArgs& a, char* ws, hipStream_t stream) {
@@ -636,21 +661,23 @@ int backward(const EmbedGradArgs& a, char* ws, hipStream_t stream) {
   int32_t* order = reinterpret_cast<int32_t*>(ws + l.order);
   const SumArgs s{a, begin, order, reinterpret_cast<float*>(ws + l.pieces), lanes};
   if (small(a.n, a.V, vectors)) {
-    if (a.dim < K) embed_small_kernel<G, T, true><<<dim3(a.V, vectors), 256, 0, stream>>>(s);
-    else embed_small_kernel<G, T, false><<<dim3(a.V, vectors), 256, 0, stream>>>(s);
+    if (a.dim < K) embed_small_kernel<G, T, 16, true><<<dim3(a.V, vectors), 256, 0, stream>>>(s);
+    else if (a.n <= 1024) embed_small_kernel<G, T, 4, false><<<dim3(a.V, vectors), 256, 0, stream>>>(s);
+    else embed_small_kernel<G, T, 16, false><<<dim3(a.V, vectors), 256, 0, stream>>>(s);
     return done();
   }
   const int shift = shift_for(a.V), ranges = ((a.V - 1) >> shift) + 1, stretches = (a.n + kFew - 1) / kFew;
   const size_t counts = static_cast<size_t>(kSortWaves) * 4 << shift;
+  const Owners owners{reinterpret_cast<int32_t*>(ws + l.count), reinterpret_cast<Owner*>(ws + l.list)};
   if (a.n >= kManyTokens) {
     unsigned* entries = reinterpret_cast<unsigned*>(ws + l.entries);
     int32_t* starts = reinterpret_cast<int32_t*>(ws + l.starts);
     const int chunks = (a.n + kSplit - 1) / kSplit;
     embed_split_kernel<<<chunks, kSortThreads, 0, stream>>>(a.tokens, a.n, a.V, shift, ranges, entries, starts);
     if (done() != PB_OK) return PB_EHIP;
-    embed_merge_kernel<<<ranges, kSortThreads, counts, stream>>>(entries, starts, chunks, a.V, shift, ranges, begin, order);
+    embed_merge_kernel<<<ranges, kSortThreads, counts, stream>>>(entries, starts, chunks, a.V, shift, ranges, begin, order, owners);
   } else {
-    embed_sort_kernel<<<ranges, kSortThreads, counts, stream>>>(a.tokens, a.n, a.V, shift, begin, order);
+    embed_sort_kernel<<<ranges, kSortThreads, counts, stream>>>(a.tokens, a.n, a.V, shift, begin, order, owners);
   }
   if (done() != PB_OK) return PB_EHIP;
   const int stretch_blocks = a.n > kFew ? (stretches + each - 1) / each : 0, row_blocks = (a.V + each - 1) / each;
@@ -664,10 +691,9 @@ int backward(const EmbedGradArgs& a, char* ws, hipStream_t stream) {
   else if (vectors == 2) rc = sums(embed_sums_kernel<G, T, 2, false>, 2);
   else rc = sums(embed_sums_kernel<G, T, 4, false>, 4);
   if (rc != PB_OK || stretch_blocks == 0) return rc;
-  const int groups = kJoinThreads / lanes;
-  const dim3 grid((stretches + groups - 1) / groups, vectors);
-  if (a.dim < K) embed_join_kernel<T, K, true><<<grid, kJoinThreads, 0, stream>>>(s, stretches);
-  else embed_join_kernel<T, K, false><<<grid, kJoinThreads, 0, stream>>>(s, stretches);
+  const dim3 grid(ranges, vectors);
+  if (a.dim < K) embed_join_kernel<T, K, true><<<grid, kJoinThreads, 0, stream>>>(s, owners, shift);
+  else embed_join_kernel<T, K, false><<<grid, kJoinThreads, 0, stream>>>(s, owners, shift);
   return done();
 }
 }  // namespace em

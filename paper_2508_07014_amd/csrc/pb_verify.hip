@@ -158,15 +158,16 @@ __device__ __forceinline__ float draft_at(const VerifyArgs& a, int64_t b, int i,
   return E::up((static_cast<const typename E::type*>(a.draft) + b * a.draft_seq + i * a.draft_row)[t]);
 }
 
-// A row is split in parts of 64 EACH vectors, a wave each; at least one.
+// A row is split in parts of 64 kEach vectors, a wave each; at least one.
+constexpr int kEach = 8;
 template <typename E>
-__host__ __device__ __forceinline__ int parts_of(int V, int each) {
-  const int parts = (V / E::N + 64 * each - 1) / (64 * each);
+__host__ __device__ __forceinline__ int parts_of(int V) {
+  const int parts = (V / E::N + 64 * kEach - 1) / (64 * kEach);
   return parts > 0 ? parts : 1;
 }
 
 // A wave a part of a row.  Rows behind the end of a draft are not looked at.
-template <typename E, int EACH>
+template <typename E>
 __global__ __launch_bounds__(256) void verify_sums_kernel(VerifyArgs a, int rows, int parts, Sums* sums) {
   const int lane = threadIdx.x & 63;
   const int64_t item = static_cast<int64_t>(blockIdx.x) * 4 + uniform_i(threadIdx.x >> 6);
@@ -179,7 +180,7 @@ __global__ __launch_bounds__(256) void verify_sums_kernel(VerifyArgs a, int rows
   const Row<E> row = row_of<E>(a, b, j);
   float at = 0.0f;
   if (part == 0 && i < tokens.count) at = E::up(row.x[__builtin_amdgcn_readlane(tokens.t, i)]);
-  Sums s = part_sums<E, EACH>(row, part * 64 * EACH, part == 0, j <= a.n ? a.target_scale.c : a.draft_scale.c, lane);
+  Sums s = part_sums<E, kEach>(row, part * 64 * kEach, part == 0, j <= a.n ? a.target_scale.c : a.draft_scale.c, lane);
   s.at = at;
   if (lane == 0) sums[item] = s;
 }
@@ -603,13 +604,13 @@ template <typename E>
 __global__ __launch_bounds__(64 * kPickWaves) void verify_pick_kernel(VerifyArgs a, const Verdict* verdicts, const Slice* in) {
   __shared__ double sums[kLogitsMaxV / (64 * E::N)], turn[2 * kPickWaves];
   const int lane = threadIdx.x & 63, wave = uniform_i(threadIdx.x >> 6), slices = slices_of<E>(a.V);
-  constexpr int kEach = (kLogitsMaxV / (64 * E::N) + 64 * kPickWaves - 1) / (64 * kPickWaves);
+  constexpr int kMine = (kLogitsMaxV / (64 * E::N) + 64 * kPickWaves - 1) / (64 * kPickWaves);
   const int64_t b = blockIdx.x;
   in += b * slices;
-  Slice mine[kEach];
+  Slice mine[kMine];
   double ps = 0.0, qs = 0.0;
 #pragma unroll
-  for (int k = 0; k < kEach; ++k) {
+  for (int k = 0; k < kMine; ++k) {
     const int s = threadIdx.x + k * 64 * kPickWaves;
     mine[k] = s < slices ? in[s] : Slice{0.0, 0.0, 0.0, 0.0, 0.0, 0.0, INFINITY, -INFINITY};
   }
@@ -617,7 +618,7 @@ __global__ __launch_bounds__(64 * kPickWaves) void verify_pick_kernel(VerifyArgs
   const Verdict d = verdicts[b];
   if (d.none) return;  // (and nothing was summed)
 #pragma unroll
-  for (int k = 0; k < kEach; ++k) {
+  for (int k = 0; k < kMine; ++k) {
     ps += mine[k].p;
     qs += mine[k].q;
   }
@@ -635,7 +636,7 @@ __global__ __launch_bounds__(64 * kPickWaves) void verify_pick_kernel(VerifyArgs
   bool whole = d.refused < 0 || (!r.y && r.barred < 0);  // (a draft's row of nothing but -inf takes nothing away)
   for (;; whole = true) {
 #pragma unroll
-    for (int k = 0; k < kEach; ++k) {
+    for (int k = 0; k < kMine; ++k) {
       const int s = threadIdx.x + k * 64 * kPickWaves;
       double v = whole ? mine[k].p : mine[k].above;
       if (!whole && r.y) {  // (a slice with tokens on both sides of the ratio that the last bits of their weights decide is summed again)
@@ -675,7 +676,7 @@ __global__ __launch_bounds__(64 * kPickWaves) void verify_pick_kernel(VerifyArgs
 
 // How a call is laid out.
 struct Plan {
-  int rows, each, parts;
+  int rows, parts;
   int groups;  // workgroups a sequence that sum the row that decides; 0: one workgroup decides and draws; -1: one does everything
   int64_t verdicts, slice_sums, bytes;  // places in the workspace, its size
 };
@@ -683,17 +684,12 @@ template <typename E>
 Plan plan(int32_t sequences, int32_t n, bool drafted, int32_t V) {
   Plan p;
   p.rows = drafted ? 2 * n + 1 : n + 1;
-  p.each = 8;
-  p.parts = parts_of<E>(V, 8);
+  p.parts = parts_of<E>(V);
   const int slices = slices_of<E>(V);
   if (p.rows * p.parts <= kSmallItems && slices <= 16 * kHeld) {
     p.groups = -1;
     p.verdicts = p.slice_sums = p.bytes = 0;
     return p;
-  }
-  if (static_cast<int64_t>(sequences) * p.rows * p.parts < 2048) {
-    p.each = 2;
-    p.parts = parts_of<E>(V, 2);
   }
   p.groups = slices <= 16 * kHeld ? 0 : static_cast<int>(std::min<int64_t>((slices + kRestWaves - 1) / kRestWaves, std::max<int64_t>(1, 256 / sequences)));
   p.verdicts = (static_cast<int64_t>(sequences) * p.rows * p.parts * static_cast<int64_t>(sizeof(Sums)) + 15) / 16 * 16;
@@ -715,8 +711,7 @@ int forward(const VerifyArgs& a, void* workspace, hipStream_t stream) {
   char* ws = static_cast<char*>(workspace);
   Sums* sums = reinterpret_cast<Sums*>(ws);
   const unsigned grid = static_cast<unsigned>((static_cast<int64_t>(a.sequences) * p.rows * p.parts + 3) / 4);
-  if (p.each == 2) verify_sums_kernel<E, 2><<<grid, 256, 0, stream>>>(a, p.rows, p.parts, sums);
-  else verify_sums_kernel<E, 8><<<grid, 256, 0, stream>>>(a, p.rows, p.parts, sums);
+  verify_sums_kernel<E><<<grid, 256, 0, stream>>>(a, p.rows, p.parts, sums);
   if (done() != PB_OK) return PB_EHIP;
   if (p.groups == 0) {
     if (slices_of<E>(a.V) <= 16) verify_draw_kernel<E, 16, 1><<<a.sequences, 1024, 0, stream>>>(a, p.rows, p.parts, sums);
@@ -735,7 +730,7 @@ int forward(const VerifyArgs& a, void* workspace, hipStream_t stream) {
 
 // (Sequences are the second dimension of a grid, which holds 65535 at most.)
 int32_t verify_draft_slice(int dtype, int32_t n, int32_t V) {
-  const int parts = dtype == PB_F32 ? vd::parts_of<lr::F32>(V, 2) : vd::parts_of<lr::F16>(V, 2);
+  const int parts = dtype == PB_F32 ? vd::parts_of<lr::F32>(V) : vd::parts_of<lr::F16>(V);
   return static_cast<int32_t>(std::min<int64_t>(32768, 4 * kMostGroups / ((2 * n + 1) * static_cast<int64_t>(parts))));
 }
 // (The size is that of the call with rows of the draft, and without them, whichever is larger: it does not depend on them.)
