@@ -137,6 +137,56 @@ def test_table_gradient_of_runs():
         assert torch.equal(out, again)      # the same bits every time
 
 
+def test_rows_past_32_bits():
+    """Tables, gradients and outputs whose rows lie more than 2^32 bytes and 2^31 elements apart."""
+    dim, far = 40, (1 << 31) + 24
+    big = torch.zeros(far + 2 * dim, dtype=torch.bfloat16, device=DEV)
+    two = torch.as_strided(big, (2, dim), (far, 1))
+    two.copy_(torch.randn((2, dim), device=DEV))
+    tokens = dev(np.array([1, 0, 1, -1], np.int32))
+    out = torch.empty((4, dim), dtype=torch.bfloat16, device=DEV)
+    pb.pb_embed_tokens(two, pb.PB_BF16, far, 2, dim, 1.0, tokens, 4, out, pb.PB_BF16, dim, stream_ptr())
+    assert torch.equal(out[0], two[1]) and torch.equal(out[1], two[0]) and torch.equal(out[2], two[1]) and not out[3].any()
+    want = two.clone()
+    grad, ws = torch.empty((3, dim), dtype=torch.bfloat16, device=DEV), workspace(pb.pb_embed_tokens_backward_workspace_bytes(2, 3, dim))
+    pb.pb_embed_tokens_backward(two, pb.PB_BF16, far, dev(np.array([2, 0], np.int32)), 2, 3, dim, 1.0, 0, grad, pb.PB_BF16, dim, ws, ws.numel(), stream_ptr())
+    assert torch.equal(grad[2], want[0]) and torch.equal(grad[0], want[1]) and not grad[1].any()
+    pb.pb_embed_tokens(out, pb.PB_BF16, dim, 4, dim, 1.0, dev(np.array([3, 1], np.int32)), 2, two, pb.PB_BF16, far, stream_ptr())
+    assert not two[0].any() and torch.equal(two[1], out[1])
+    pb.pb_embed_tokens_backward(grad, pb.PB_BF16, dim, dev(np.array([1, 0, 1], np.int32)), 3, 2, dim, 1.0, 0, two, pb.PB_BF16, far, ws, ws.numel(), stream_ptr())
+    assert torch.equal(two[0], grad[1]) and torch.equal(two[1], (grad[0].float() + grad[2].float()).bfloat16())
+    # a verification: row strides and sequence strides
+    x = torch.randn((2, dim), device=DEV)
+    two.copy_(x)
+    numbers = torch.tensor([[0.3], [0.8]], device=DEV)
+    drawn, acc = torch.empty((2, 1), dtype=torch.int32, device=DEV), torch.empty(2, dtype=torch.int32, device=DEV)
+    pb.pb_verify_draft(two, None, pb.PB_BF16, far, dim, 0, 0, 2, 0, dim, 1.0, 1.0, None, numbers, drawn, acc, None, None, 0, stream_ptr())
+    for b in range(2):
+        assert int(drawn[b, 0]) == S.drawn(S.probabilities(host(two[b]), 1.0)[0], float(numbers[b, 0]))
+    pb.pb_verify_draft(two, two, pb.PB_BF16, 2 * far, far, far, dim, 1, 1, dim, 1.0, 1.0, two[0].argmax().view(1, 1).to(torch.int32), numbers, drawn, acc, None, None, 0,
+                       stream_ptr())
+    assert int(acc[0]) == 1 and int(drawn[1, 0]) == S.drawn(S.probabilities(host(two[1]), 1.0)[0], float(numbers[1, 0]))
+
+
+@pytest.mark.parametrize("n,V,hot", [(5_000_000, 1000, 0.0), (4_500_000, 393216, 0.3)])
+def test_table_gradient_of_millions(n, V, hot):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(n)
+    tokens = torch.randint(-1, V, (n,), generator=g, device=DEV, dtype=torch.int32)
+    tokens[torch.rand(n, generator=g, device=DEV) < hot] = 77
+    grad = torch.randn((n, 1), generator=g, device=DEV)
+    out = torch.full((V, 1), JUNK, device=DEV)
+    size = pb.pb_embed_tokens_backward_workspace_bytes(n, V, 1)
+    ws = workspace(size)
+    pb.pb_embed_tokens_backward(grad, pb.PB_F32, 1, tokens, n, V, 1, 0.5, 0, out, pb.PB_F32, 1, ws, size, stream_ptr())
+    assert guard_ok(ws, size)
+    at, x = tokens.cpu().numpy() + 1, host(grad[:, 0]) * 0.5   # (absent ones come first, and are dropped)
+    want, sizes, count = (np.bincount(at, weights=w, minlength=V + 1)[1:] for w in (x, np.abs(x), np.ones(n)))
+    # (as in table_gradient; the pieces' sums once more in up to 1024 shares)
+    bound = sizes * S.U * (np.minimum(count, S.FEW) + count // S.FEW + 1024 + 3) + S.U * np.abs(want)
+    assert (np.abs(host(out[:, 0]) - want) <= bound).all()
+
+
 # ---- norm and clipping -------------------------------------------------------------------------------------------------
 
 def tensors_of(rng, spec, shift=False):
@@ -500,6 +550,64 @@ def test_verify_rows_behind_the_end_are_not_read():
     got = run_verify(px, py, "bf16", (V, (n + 1) * V), (V, n * V), 3, n, V, 1.0, 1.0, tokens, numbers)
     assert list(got[1]) == [0, 1, 3]
     check_verify(got, xv, yv, 1.0, 1.0, tokens, numbers, "ends")
+
+
+@pytest.mark.parametrize("n,V", [(0, 20000), (1, 600)])
+def test_verify_more_sequences_than_a_launch_takes(n, V):
+    B, g = 33000, torch.Generator(device=DEV)
+    g.manual_seed(V)
+    x = torch.empty((B, n + 1, V), dtype=torch.bfloat16, device=DEV)
+    for s in range(0, B, 3000):
+        x[s:s + 3000] = (torch.randn((min(3000, B - s), n + 1, V), generator=g, device=DEV) * 2).bfloat16()
+    tokens = torch.randint(0, V, (B, n), generator=g, device=DEV, dtype=torch.int32)
+    numbers = torch.rand((B, n + 1), generator=g, device=DEV)
+
+    def run(first, count):
+        out, acc = torch.full((count, n + 1), -7, dtype=torch.int32, device=DEV), torch.full((count,), -7, dtype=torch.int32, device=DEV)
+        lp = torch.full((count, n + 1), JUNK, device=DEV)
+        size = pb.pb_verify_draft_workspace_bytes(pb.PB_BF16, count, n, V)
+        ws = workspace(size)
+        pb.pb_verify_draft(x[first:], None, pb.PB_BF16, (n + 1) * V, V, V, V, count, n, V, 1.0, 1.0, tokens[first:] if n else None, numbers[first:], out, acc,
+                           lp, ws, size, stream_ptr())
+        assert guard_ok(ws, size)
+        return out, acc, torch.nan_to_num(lp, nan=9.0)
+    whole = run(0, B)
+    for first in (0, 16500, 32700):
+        for a, b in zip(whole, run(first, 300)):
+            # (log-probs of accepted tokens: sums are the same in any call)
+            assert torch.equal(a[first:first + 300], b)
+    rows = [0, 1, 32767, 32768, B - 1]
+    got = [w[rows].cpu().numpy() for w in whole]
+    check_verify((got[0], got[1], None), host(x[rows]), None, 1.0, 1.0, tokens[rows].cpu().numpy(), numbers[rows].cpu().numpy(), "sequences")
+
+
+def test_verify_two_calls_at_once():
+    """On two streams, a workspace each; equal to one after the other."""
+    rng = np.random.default_rng(8)
+    V, n = 40000, 3
+    calls = []
+    for k in range(2):
+        x = torch.from_numpy(rng.normal(0, 2, (16, n + 1, V)).astype(np.float32)).to(DEV)
+        y = (x[:, :n] + torch.randn((16, n, V), device=DEV)).contiguous()
+        calls.append((x, y, y.argmax(dim=2).to(torch.int32), torch.rand((16, n + 1), device=DEV)))
+    size = pb.pb_verify_draft_workspace_bytes(pb.PB_F32, 16, n, V)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+
+    def go(k, stream, ws):
+        x, y, t, u = calls[k]
+        out, acc = torch.empty((16, n + 1), dtype=torch.int32, device=DEV), torch.empty(16, dtype=torch.int32, device=DEV)
+        pb.pb_verify_draft(x, y, pb.PB_F32, (n + 1) * V, V, n * V, V, 16, n, V, 1.0, 1.0, t, u, out, acc, None, ws, size, stream)
+        return out, acc
+    spaces = [workspace(size) for _ in range(2)]
+    torch.cuda.synchronize()
+    for turn in range(5):
+        at_once = [go(k, int(streams[k].cuda_stream), spaces[k]) for k in range(2)]
+        torch.cuda.synchronize()
+        for k in range(2):
+            one = go(k, stream_ptr(), spaces[0])
+            torch.cuda.synchronize()
+            assert torch.equal(one[0], at_once[k][0]) and torch.equal(one[1], at_once[k][1])
 
 
 # ---- graphs, streams, a run of them ------------------------------------------------------------------------------------
