@@ -455,27 +455,27 @@ __device__ __forceinline__ void sum_stretch(const SumArgs& s, int c, int vector,
   }
 }
 
-// The first stretch_blocks * vectors workgroups take stretches (a piece takes longer than other rows), the others `lanes` lanes a token.
+// The first stretch_blocks workgroups take stretches (a piece takes longer than other rows), the others tokens, `lanes` lanes SL vectors of a
+// row.  What belongs to a row lies next to each other in the grid, so that rows are read whole.
 template <typename G, typename T, int SL, bool NARROW>
-__global__ __launch_bounds__(256) void embed_sums_kernel(SumArgs s, int stretch_blocks, int vectors, int row_blocks) {
+__global__ __launch_bounds__(256) void embed_sums_kernel(SumArgs s, int stretch_blocks, unsigned vectors) {
   constexpr int K = step_of<G, T>();
   const EmbedGradArgs& a = s.a;
-  const int lane = threadIdx.x & (s.lanes - 1), sub = threadIdx.x / s.lanes, each = 256 / s.lanes;
-  int block = blockIdx.x;
-  if (block < stretch_blocks * vectors) {
-    const int c = block % stretch_blocks * each + sub, end = s.begin[a.V];
-    if (c * kFew < end) sum_stretch<G, K, NARROW>(s, c, block / stretch_blocks, end, lane);
+  const int lane = threadIdx.x & (s.lanes - 1), each = 256 / s.lanes;
+  const unsigned unit = (blockIdx.x - (static_cast<int>(blockIdx.x) < stretch_blocks ? 0 : stretch_blocks)) * each + threadIdx.x / s.lanes;
+  if (static_cast<int>(blockIdx.x) < stretch_blocks) {
+    const int c = static_cast<int>(unit / vectors), end = s.begin[a.V];
+    if (static_cast<int64_t>(c) * kFew < end) sum_stretch<G, K, NARROW>(s, c, static_cast<int>(unit % vectors), end, lane);
     return;
   }
-  block -= stretch_blocks * vectors;
-  const int v = block % row_blocks * each + sub;
-  if (v >= a.V) return;
+  const unsigned of_row = (vectors + SL - 1) / SL, v = unit / of_row;
+  if (v >= static_cast<unsigned>(a.V)) return;
   const int i = s.begin[v], j = s.begin[v + 1];
   if (j - i > kFew || (j == i && a.accumulate)) return;
-  const Columns<K, SL, NARROW> cols(a.dim, block / row_blocks * s.lanes * K * SL, s.lanes, lane);
+  const Columns<K, SL, NARROW> cols(a.dim, static_cast<int>(unit % of_row) * s.lanes * K * SL, s.lanes, lane);
   float sum[SL][K] = {};
   sum_positions<G>(s, cols, i, j, sum);
-  write_columns<T>(a, cols, v, sum);
+  write_columns<T>(a, cols, static_cast<int>(v), sum);
 }
 
 // Pieces of a token, in the order of their stretches: a workgroup a range (and vectors of its columns).  Its groups of lanes take the tokens
@@ -680,9 +680,10 @@ int backward(const EmbedGradArgs& a, char* ws, hipStream_t stream) {
     embed_sort_kernel<<<ranges, kSortThreads, counts, stream>>>(a.tokens, a.n, a.V, shift, begin, order, owners);
   }
   if (done() != PB_OK) return PB_EHIP;
-  const int stretch_blocks = a.n > kFew ? (stretches + each - 1) / each : 0, row_blocks = (a.V + each - 1) / each;
+  const int64_t stretch_blocks = a.n > kFew ? (static_cast<int64_t>(stretches) * vectors + each - 1) / each : 0;
   auto sums = [&](auto kernel, int sl) {
-    kernel<<<stretch_blocks * vectors + row_blocks * ((vectors + sl - 1) / sl), 256, 0, stream>>>(s, stretch_blocks, vectors, row_blocks);
+    const int64_t row_blocks = (static_cast<int64_t>(a.V) * ((vectors + sl - 1) / sl) + each - 1) / each;
+    kernel<<<static_cast<unsigned>(stretch_blocks + row_blocks), 256, 0, stream>>>(s, static_cast<int>(stretch_blocks), static_cast<unsigned>(vectors));
     return done();
   };
   int rc;
