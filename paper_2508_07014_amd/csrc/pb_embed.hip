@@ -386,17 +386,17 @@ struct SumArgs {
 };
 
 // Adds the rows of `U` positions from order[i] on, requested together.
-template <int U, typename G, int K, int SL, bool NARROW>
-__device__ __forceinline__ void add_rows(const SumArgs& s, const Columns<K, SL, NARROW>& cols, int i, float (&sum)[SL][K]) {
-  const typename G::type* g = static_cast<const typename G::type*>(s.a.grad);
+template <int U, typename G, typename Order, int K, int SL, bool NARROW>
+__device__ __forceinline__ void add_rows(const EmbedGradArgs& a, const Order* order, const Columns<K, SL, NARROW>& cols, int i, float (&sum)[SL][K]) {
+  const typename G::type* g = static_cast<const typename G::type*>(a.grad);
   int p[U];
   float x[U][SL][K];
 #pragma unroll
-  for (int k = 0; k < U; ++k) p[k] = s.order[i + k];
+  for (int k = 0; k < U; ++k) p[k] = order[i + k];
 #pragma unroll
   for (int k = 0; k < U; ++k)
 #pragma unroll
-    for (int v = 0; v < SL; ++v) cols.template load<G>(g + p[k] * s.a.grad_stride, v, x[k][v]);
+    for (int v = 0; v < SL; ++v) cols.template load<G>(g + p[k] * a.grad_stride, v, x[k][v]);
 #pragma unroll
   for (int k = 0; k < U; ++k)
 #pragma unroll
@@ -404,15 +404,15 @@ __device__ __forceinline__ void add_rows(const SumArgs& s, const Columns<K, SL, 
 #pragma unroll
       for (int c = 0; c < K; ++c) sum[v][c] += x[k][v][c];
 }
-template <typename G, int K, int SL, bool NARROW>
-__device__ __forceinline__ void sum_positions(const SumArgs& s, const Columns<K, SL, NARROW>& cols, int i, int j, float (&sum)[SL][K]) {
+template <typename G, typename Order, int K, int SL, bool NARROW>
+__device__ __forceinline__ void sum_positions(const EmbedGradArgs& a, const Order* order, const Columns<K, SL, NARROW>& cols, int i, int j, float (&sum)[SL][K]) {
   constexpr int U = 64 / (K * SL);
-  for (; i + U <= j; i += U) add_rows<U, G>(s, cols, i, sum);
+  for (; i + U <= j; i += U) add_rows<U, G>(a, order, cols, i, sum);
   if constexpr (U > 4)
-    for (; i + 4 <= j; i += 4) add_rows<4, G>(s, cols, i, sum);
+    for (; i + 4 <= j; i += 4) add_rows<4, G>(a, order, cols, i, sum);
   if constexpr (U > 2)
-    if (i + 2 <= j) add_rows<2, G>(s, cols, i, sum), i += 2;
-  for (; i < j; ++i) add_rows<1, G>(s, cols, i, sum);
+    if (i + 2 <= j) add_rows<2, G>(a, order, cols, i, sum), i += 2;
+  for (; i < j; ++i) add_rows<1, G>(a, order, cols, i, sum);
 }
 template <typename T, int K, int SL, bool NARROW>
 __device__ __forceinline__ void write_columns(const EmbedGradArgs& a, const Columns<K, SL, NARROW>& cols, int v, float (&sum)[SL][K]) {
@@ -445,12 +445,12 @@ __device__ __forceinline__ void sum_stretch(const SumArgs& s, int c, int vector,
   float* pieces = s.pieces + static_cast<int64_t>(c) * 2 * a.dim;
   if (s.begin[first + 1] - s.begin[first] > kFew) {
     float sum[1][K] = {};
-    sum_positions<G>(s, cols, i0, min(i1, s.begin[first + 1]), sum);
+    sum_positions<G>(a, s.order, cols, i0, min(i1, s.begin[first + 1]), sum);
     write_piece(pieces, cols, sum);
   }
   if (last != first && s.begin[last + 1] - s.begin[last] > kFew) {
     float sum[1][K] = {};
-    sum_positions<G>(s, cols, s.begin[last], i1, sum);
+    sum_positions<G>(a, s.order, cols, s.begin[last], i1, sum);
     write_piece(pieces + a.dim, cols, sum);
   }
 }
@@ -474,7 +474,7 @@ __global__ __launch_bounds__(256) void embed_sums_kernel(SumArgs s, int stretch_
   if (j - i > kFew || (j == i && a.accumulate)) return;
   const Columns<K, SL, NARROW> cols(a.dim, static_cast<int>(unit % of_row) * s.lanes * K * SL, s.lanes, lane);
   float sum[SL][K] = {};
-  sum_positions<G>(s, cols, i, j, sum);
+  sum_positions<G>(a, s.order, cols, i, j, sum);
   write_columns<T>(a, cols, static_cast<int>(v), sum);
 }
 
@@ -536,33 +536,43 @@ __global__ __launch_bounds__(kJoinThreads) void embed_join_kernel(SumArgs s, Own
 }
 
 // Few tokens on a small table, all in one launch: a workgroup a token (and vectors of its columns) looks through the tokens for its
-// positions, waves in their order, its groups of lanes sum a share of those each, and the first of them those sums.
-constexpr int kSmallTokens = 4096;
-template <typename G, typename T, int kTurns, bool NARROW>
+// positions, waves in their order, its groups of lanes sum a share of those each, and the first of them those sums.  TURNS: 256 tokens each,
+// held from the count of the positions to their list; LOOP: read again for that, TURNS at a time.
+constexpr int kSmallTokens = 16384;
+static_assert(kSmallTokens <= 65536, "positions in 16 bits");
+template <typename G, typename T, int TURNS, bool LOOP, bool NARROW>
 __global__ __launch_bounds__(256) void embed_small_kernel(SumArgs s) {
   constexpr int K = step_of<G, T>();
-  __shared__ int list[256 * kTurns], found[4];
+  __shared__ unsigned short list[LOOP ? kSmallTokens : 256 * TURNS];
+  __shared__ int found[4];
   __shared__ float shares[256 * K];
   const EmbedGradArgs& a = s.a;
   const int tid = threadIdx.x, v = blockIdx.x, wave = uniform_i(tid >> 6), lane64 = tid & 63;
   const int turns = (a.n + 255) / 256, p0 = wave * turns * 64 + lane64;
-  u64 here[kTurns];
-  int t[kTurns], count = 0;
+  int t[TURNS], count = 0;
+  auto request = [&](int from) {
 #pragma unroll
-  for (int k = 0; k < kTurns; ++k) t[k] = k < turns && p0 + 64 * k < a.n ? a.tokens[p0 + 64 * k] : -1;
+    for (int k = 0; k < TURNS; ++k) t[k] = from + k < turns && p0 + 64 * (from + k) < a.n ? a.tokens[p0 + 64 * (from + k)] : -1;
+  };
+  for (int from = 0; from < (LOOP ? turns : 1); from += TURNS) {
+    request(from);
 #pragma unroll
-  for (int k = 0; k < kTurns; ++k) {
-    here[k] = __ballot(t[k] == v);
-    count += __builtin_popcountll(here[k]);
+    for (int k = 0; k < TURNS; ++k) count += __builtin_popcountll(__ballot(t[k] == v));
   }
   if (lane64 == 0) found[wave] = count;
   __syncthreads();
   int at = 0;
   for (int w = 0; w < wave; ++w) at += found[w];
+  if (count > 0) {
+    for (int from = 0; from < (LOOP ? turns : 1); from += TURNS) {
+      if (LOOP) request(from);
 #pragma unroll
-  for (int k = 0; k < kTurns; ++k) {
-    if (t[k] == v) list[at + __builtin_popcountll(here[k] & ((1ull << lane64) - 1))] = p0 + 64 * k;
-    at += __builtin_popcountll(here[k]);
+      for (int k = 0; k < TURNS; ++k) {
+        const u64 here = __ballot(t[k] == v);
+        if (t[k] == v) list[at + __builtin_popcountll(here & ((1ull << lane64) - 1))] = static_cast<unsigned short>(p0 + 64 * (from + k));
+        at += __builtin_popcountll(here);
+      }
+    }
   }
   count = found[0] + found[1] + found[2] + found[3];
   if (count == 0 && a.accumulate) return;
@@ -571,9 +581,7 @@ __global__ __launch_bounds__(256) void embed_small_kernel(SumArgs s) {
   const int share = max(8, (count + groups - 1) / groups);
   const Columns<K, 1, NARROW> cols(a.dim, blockIdx.y * s.lanes * K, s.lanes, lane);
   float sum[1][K] = {};
-  SumArgs mine = s;
-  mine.order = list;
-  sum_positions<G>(mine, cols, group * share, min(count, (group + 1) * share), sum);
+  sum_positions<G>(a, list, cols, group * share, min(count, (group + 1) * share), sum);
   if (count > share) {
 #pragma unroll
     for (int e = 0; e < K; ++e) shares[e * 256 + tid] = sum[0][e];
@@ -647,9 +655,13 @@ struct Shape {
   int lanes, vectors;
   explicit Shape(int dim) : lanes(lanes_for(dim, K)), vectors((dim + lanes * K - 1) / (lanes * K)) {}
 };
-// us, in one launch / in three: 4096 tokens, 1025 x 640 fp32 12.7 / 19.2, 100 x 2048 13.5 / 22.4, 8192 x 512 bf16 (8192 workgroups) 21.6 / 16.3;
-// 1000 tokens, 16384 x 256 fp32 (16384 of them) 28.0 / 15.2; 300 tokens of those 26.2 / 13.1.
-bool small(int64_t n, int64_t V, int vectors) { return n <= kSmallTokens && V * vectors <= 6144; }
+// us, in one launch / in three, fp32 where not said: 300 tokens, 1025 x 64 3.3 / 10.4, 8192 x 64 10.0 / 9.3; 2000, 4096 x 64 9.2 / 13.8, 8192 x 64 15.2 /
+// 14.1; 4096, 1025 x 640 12.7 / 19.2, 8192 x 512 bf16 21.6 / 16.3; 5000, 4096 x 64 19.7 / 16.7; 8192, 2048 x 64 15.3 / 20.6; 16384, 166 x 64 18.9 / 22.0,
+// 1025 x 64 18.0 / 23.8; and, where a token of many positions has few groups of lanes for them, 8192, 300 x 1024 bf16 27.1 / 23.7; 16384,
+// 166 x 2048 71 / 51.
+bool small(int64_t n, int64_t V, int lanes, int vectors) {
+  return n <= kSmallTokens && n * lanes <= 4096 * 64 && V * vectors <= 6144 && V * vectors * n <= 17 << 20;
+}
 
 template <typename G, typename T>
 int backward(const EmbedGradArgs& a, char* ws, hipStream_t stream) {
@@ -660,11 +672,15 @@ int backward(const EmbedGradArgs& a, char* ws, hipStream_t stream) {
   int32_t* begin = reinterpret_cast<int32_t*>(ws + l.begin);
   int32_t* order = reinterpret_cast<int32_t*>(ws + l.order);
   const SumArgs s{a, begin, order, reinterpret_cast<float*>(ws + l.pieces), lanes};
-  if (small(a.n, a.V, vectors)) {
-    if (a.dim < K) embed_small_kernel<G, T, 16, true><<<dim3(a.V, vectors), 256, 0, stream>>>(s);
-    else if (a.n <= 1024) embed_small_kernel<G, T, 4, false><<<dim3(a.V, vectors), 256, 0, stream>>>(s);
-    else embed_small_kernel<G, T, 16, false><<<dim3(a.V, vectors), 256, 0, stream>>>(s);
-    return done();
+  if (small(a.n, a.V, lanes, vectors)) {
+    auto go = [&](auto kernel) {
+      kernel<<<dim3(a.V, vectors), 256, 0, stream>>>(s);
+      return done();
+    };
+    if (a.dim < K) return go(embed_small_kernel<G, T, 16, true, true>);
+    if (a.n <= 1024) return go(embed_small_kernel<G, T, 4, false, false>);
+    if (a.n <= 4096) return go(embed_small_kernel<G, T, 16, false, false>);
+    return go(embed_small_kernel<G, T, 16, true, false>);
   }
   const int shift = shift_for(a.V), ranges = ((a.V - 1) >> shift) + 1, stretches = (a.n + kFew - 1) / kFew;
   const size_t counts = static_cast<size_t>(kSortWaves) * 4 << shift;

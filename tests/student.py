@@ -73,7 +73,7 @@ def table_gradient(g, tokens, V, scale):
     np.add.at(size, tokens[inside], np.abs(g[inside]))
     # (a sum of at most FEW terms one after the other, then of a piece each FEW places; or, few tokens on a small table, a quarter of the
     # terms at most one after the other, then of up to 256 such shares; the product with the scale)
-    chain = np.maximum(np.minimum(count, FEW) + count // FEW, np.minimum(count, count // 4 + 8) + 256 * (len(tokens) <= 4096)) + 3
+    chain = np.maximum(np.minimum(count, FEW) + count // FEW, np.minimum(count, count // 4 + 8) + 256 * (len(tokens) <= 16384)) + 3
     return total * scale, size * abs(scale) * U * chain[:, None], count
 
 
