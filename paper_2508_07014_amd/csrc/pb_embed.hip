@@ -203,31 +203,42 @@ __device__ __forceinline__ int places(int* counts, int stride, int size, int bas
   return first;
 }
 
-// Places a wave's keys (of `bits` bits; `in`: the lane has one) at their counters, in the order of the lanes: the lanes with the same key
-// are found key by key where there are few, bit by bit otherwise.
-template <typename Put>
-__device__ __forceinline__ void place_keys(int* counters, unsigned key, bool in, int bits, int lane, Put&& put) {
-  u64 same = __ballot(in);
-  if (same == 0) return;
-  if (__builtin_popcountll(same) <= 4) {
-    for (u64 left = same; left;) {
-      const unsigned k = static_cast<unsigned>(__builtin_amdgcn_readlane(static_cast<int>(key), first_lane(left)));
-      const u64 mine = __ballot(in && key == k);
-      const int to = counters[k];
-      if (in && key == k) put(to + __builtin_popcountll(mine & ((1ull << lane) - 1)));
-      if (lane == 0) counters[k] = to + __builtin_popcountll(mine);
-      left &= ~mine;
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-      __builtin_amdgcn_wave_barrier();
-    }
-    return;
+// Counts a wave's keys (`in`: the lane has one) in the wave's own counters.  A token of many positions fills whole waves, whose additions to
+// one place the LDS would take one after the other: the lanes with the first one's key are counted at once.
+template <int ROUNDS>
+__device__ __forceinline__ void count_keys(int* counters, unsigned key, bool in, int lane) {
+  u64 left = __ballot(in);
+  for (int round = 0; round < ROUNDS && left; ++round) {
+    const unsigned k = static_cast<unsigned>(__builtin_amdgcn_readlane(static_cast<int>(key), first_lane(left)));
+    const u64 same = left & __ballot(key == k);
+    if (lane == 0) atomicAdd(&counters[k], __builtin_popcountll(same));
+    left &= ~same;
   }
+  if ((left >> lane) & 1) atomicAdd(&counters[key], 1);
+}
+// Places a wave's keys (of `bits` bits) at their counters, in the order of the lanes: key by key while there are few or one has many
+// lanes, what is left after that bit by bit.
+template <int ROUNDS, typename Put>
+__device__ __forceinline__ void place_keys(int* counters, unsigned key, bool in, int bits, int lane, Put&& put) {
+  u64 left = __ballot(in);
+  for (int round = 0; left && (round < ROUNDS || __builtin_popcountll(left) <= 4); ++round) {
+    const unsigned k = static_cast<unsigned>(__builtin_amdgcn_readlane(static_cast<int>(key), first_lane(left)));
+    const u64 same = left & __ballot(key == k);
+    const int to = counters[k];
+    if ((same >> lane) & 1) put(to + __builtin_popcountll(same & ((1ull << lane) - 1)));
+    if (lane == 0) counters[k] = to + __builtin_popcountll(same);
+    left &= ~same;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  }
+  if (!left) return;
+  u64 same = left;
   for (int b = 0; b < bits; ++b) {
     const bool one = (key >> b) & 1u;
     const u64 ones = __ballot(one);
     same &= one ? ones : ~ones;
   }
-  if (in) {
+  if ((left >> lane) & 1) {
     const int to = counters[key], rank = __builtin_popcountll(same & ((1ull << lane) - 1));
     __builtin_amdgcn_wave_barrier();
     if (rank == 0) counters[key] = to + __builtin_popcountll(same);
@@ -272,7 +283,7 @@ __global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(const int32_t*
   write_owners(owners, blockIdx.x, v0, size, at, end, s);
   auto put = [&](int t, int from) {
     const unsigned u = static_cast<unsigned>(t) - static_cast<unsigned>(v0);
-    place_keys(mine, u, u < static_cast<unsigned>(size), shift, lane, [&](int to) { order[to] = from; });
+    place_keys<1>(mine, u, u < static_cast<unsigned>(size), shift, lane, [&](int to) { order[to] = from; });
   };
   p = p0;  // (the same in all lanes of a wave)
   for (; p + 64 * kAhead <= p1; p += 64 * kAhead) {
@@ -299,7 +310,7 @@ __global__ __launch_bounds__(kSortThreads) void embed_split_kernel(const int32_t
   int* mine = counts + wave * ranges;
 #pragma unroll
   for (int k = 0; k < kTurns; ++k)
-    if (static_cast<unsigned>(t[k]) < static_cast<unsigned>(V)) atomicAdd(&mine[t[k] >> shift], 1);
+    count_keys<1>(mine, static_cast<unsigned>(t[k]) >> shift, static_cast<unsigned>(t[k]) < static_cast<unsigned>(V), lane);
   __syncthreads();
   int end;
   const int at = places(counts, ranges, ranges, 0, s, &end);
@@ -310,7 +321,7 @@ __global__ __launch_bounds__(kSortThreads) void embed_split_kernel(const int32_t
   while (((ranges - 1) >> bits) > 0) ++bits;
 #pragma unroll
   for (int k = 0; k < kTurns; ++k)
-    place_keys(mine, static_cast<unsigned>(t[k]) >> shift, static_cast<unsigned>(t[k]) < static_cast<unsigned>(V), bits, lane, [&](int q) {
+    place_keys<0>(mine, static_cast<unsigned>(t[k]) >> shift, static_cast<unsigned>(t[k]) < static_cast<unsigned>(V), bits, lane, [&](int q) {
       entries[p0 + q] = static_cast<unsigned>(t[k] & ((1 << shift) - 1)) * kSplit + static_cast<unsigned>(at0 + 64 * k);
     });
 }
@@ -359,9 +370,7 @@ __global__ __launch_bounds__(kSortThreads) void embed_merge_kernel(const unsigne
       }
     }
   };
-  all([&](unsigned e, bool is, int) {
-    if (is) atomicAdd(&mine[e / kSplit], 1);
-  });
+  all([&](unsigned e, bool is, int) { count_keys<2>(mine, e / kSplit, is, lane); });
   __syncthreads();
   const int at = places(counts, range, size, base, s, &end);
   if (tid < size) {
@@ -370,7 +379,7 @@ __global__ __launch_bounds__(kSortThreads) void embed_merge_kernel(const unsigne
   }
   write_owners(owners, b, v0, size, at, end, s);
   all([&](unsigned e, bool is, int c) {
-    place_keys(mine, e / kSplit, is, shift, lane, [&](int to) { order[to] = c * kSplit + static_cast<int>(e % kSplit); });
+    place_keys<2>(mine, e / kSplit, is, shift, lane, [&](int to) { order[to] = c * kSplit + static_cast<int>(e % kSplit); });
   });
 }
 
