@@ -392,8 +392,7 @@ int pb_distill_topk(const void* d_logits, int32_t dtype, int64_t row_stride, int
  *   in fp32, rounded once to out_dtype.  A token id outside [0, vocab_size) is absent: its row is 0.
  * pb_embed_tokens_backward -- the table's gradient from d_grad_out [n_tokens, dim], the gradient on those rows:
  *     d_grad_table[v * table_stride + j] = scale * sum over i with d_tokens[i] = v of d_grad_out[i * grad_stride + j]
- *   summed in fp32 in an order that the sizes of the call and the places of the token among the tokens decide, rounded once to
- *   table_dtype.  accumulate 0: all vocab_size rows are written, those of tokens that do not occur with 0; accumulate 1: the sum
+ *   summed in fp32 in an order that the sizes of the call and its tokens decide, rounded once to table_dtype.  accumulate 0: all vocab_size rows are written, those of tokens that do not occur with 0; accumulate 1: the sum
  *   is added to what is there, and rows of tokens that do not occur are not touched.  Absent tokens' gradients are not looked at.
  *   PB_EINVAL: n_tokens < 0, vocab_size < 1, dim < 1, an unknown dtype, a stride below dim, accumulate neither 0 nor 1, a pointer
  *   that is null but needed or not aligned to its elements, the workspace.  PB_ERANGE: a scale that is not finite.
@@ -445,12 +444,13 @@ int pb_grad_clip(const pb_tensors* grads, const float* d_norm, float max_norm, c
  *     sum_{j <= v} r_j > w sum_j r_j, r_v > 0.  Where max(p_k - q_k, 0) sums to no more than 2^-40, r = p_k.
  * d_accepted[b] = k; d_tokens[b, 0 .. n_draft] = t_0 .. t_k-1, the drawn token, then -1; d_logp (NULL: not wanted) the log p_i of
  * those tokens, NaN beside -1.  n_draft == 0 draws a token from each row.
- * Exponentials and sums are in 64 bits, so that a draw from hundreds of thousands of tokens is the definition's; a logit of -inf
+ * What decides is in 64 bits, so that a draw from hundreds of thousands of tokens, or a number next to p / q, is the definition's; the
+ * log p of accepted tokens come from fp32 sums of what lies beside a row's largest logit.  A logit of -inf
  * has p = 0, as has one whose p / p_max is below 2^-960 (q likewise).  A row of nothing but -inf: p = 0, no token is accepted there, and
  * none drawn (-1); as a y_i: q = 0.  A row that holds a NaN or +inf accepts nothing; where it decides (x_k, or y_k if k < n) the drawn
  * token is -1.
- * PB_EINVAL: as in pb_token_logprobs, n_draft < 0, d_draft_tokens NULL if and only if n_draft > 0, draft rows without drafts, a null
- *   d_uniforms, d_tokens or d_accepted, a stride below V (where its rows are read).  PB_ERANGE: a temperature outside [1e-4, 1e4].
+ * PB_EINVAL: as in pb_token_logprobs, n_draft < 0, d_draft_tokens that is null though n_draft > 0 or is not though it is 0, draft
+ *   rows though n_draft is 0, a null d_uniforms, d_tokens or d_accepted, a stride below V (the draft's where it has rows).  PB_ERANGE: a temperature outside [1e-4, 1e4].
  *   PB_EUNSUPPORTED: V > 393216, n_draft > 63.  sequences == 0 is a no-op.  Outputs lie apart from the inputs.
  */
 int64_t pb_verify_draft_workspace_bytes(int32_t dtype, int32_t sequences, int32_t n_draft, int32_t vocab_size);

