@@ -412,15 +412,16 @@ int pb_embed_tokens_backward(const void* d_grad_out, int32_t grad_dtype, int64_t
  * pb_tensors_build -- a set of n >= 1 device buffers (contiguous, sizes[i] >= 0 elements of type dtypes[i]), for instance the
  *   gradients of a model, as the two calls below take them.  Host-synchronous: a table of their addresses is uploaded to `device`;
  *   the buffers stay the caller's and have to outlive the calls.  Free with pb_tensors_free (NULL is a no-op) when no call on it
- *   is under way.  PB_EINVAL: null arguments, n < 1, a negative size, an unknown dtype, a buffer that is null though its size is
- *   not 0 or not aligned to its elements.  PB_EUNSUPPORTED: a size above 2^40.  PB_EHIP / PB_ENOMEM as in pb_build.
+ *   is under way and none that was captured will run again.  PB_EINVAL: null arguments, n < 1, a negative size, an unknown dtype, a buffer that is null though its size is
+ *   not 0 or not aligned to its elements.  PB_EUNSUPPORTED: more than 2^40 elements in all.  PB_EHIP / PB_ENOMEM as in pb_build.
  * pb_grad_norm -- d_norm[0] = sqrt(sum of x^2 over all elements of all tensors); squares and sums in 64 bits, rounded once to fp32
  *   (inf above its range; NaN where a tensor holds one).
  * pb_grad_clip -- x' = x * (max_norm / norm), factor and product each rounded once, where norm = d_norm[0] > max_norm; x' = x where it is not, and where
  *   it is NaN or +inf (there is no factor: the step is to be skipped).  d_norm is read on the device: pb_grad_norm's, or what
- *   several devices have made of theirs.  x' goes to the tensors of `out`, a set of the same device, sizes and types whose
- *   buffers lie apart from those of `grads` or are the same ones; out NULL or grads itself: in place, where nothing is written if nothing is clipped.
- *   PB_ERANGE: max_norm negative or not finite.  The calls take the device of the set, which must be current.
+ *   several devices have made of theirs.  x' goes to the tensors of `out`, a set of the same device, sizes and types, each of
+ *   whose buffers is the one it has in `grads` or lies apart from all of those; out NULL or grads itself: in place, where nothing is written if nothing is clipped.
+ *   PB_ERANGE: max_norm negative or not finite.  PB_EINVAL for both calls: null arguments, a set whose device is not the current one, the workspace; for
+ *   clipping another `out` than that, or buffers to be written that share memory with each other.
  */
 typedef struct pb_tensors pb_tensors; /* opaque; owns its table on the device */
 int pb_tensors_build(const void* const* d_buffers, const int64_t* sizes, const int32_t* dtypes, int32_t n, int32_t device,

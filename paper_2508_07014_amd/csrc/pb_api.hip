@@ -553,6 +553,43 @@ int check_embed(int32_t dtype, int32_t other, int32_t n, int32_t V, int32_t dim,
   return n > pb::kMostTokens || V > pb::kLogitsMaxV || dim > pb::kMostDim ? PB_EUNSUPPORTED : PB_OK;
 }
 
+// Tensors by address, those that share memory as one.
+void find_spans(const void* const* buffers, pb_tensors& t) {
+  for (size_t i = 0; i < t.sizes.size(); ++i) {
+    const uintptr_t begin = reinterpret_cast<uintptr_t>(buffers[i]);
+    if (t.sizes[i] > 0) t.spans.push_back({begin, begin + static_cast<uintptr_t>(t.sizes[i] * element_bytes(t.dtypes[i])), static_cast<int32_t>(i)});
+  }
+  std::sort(t.spans.begin(), t.spans.end(), [](const pb_tensors::Span& a, const pb_tensors::Span& b) { return a.begin < b.begin; });
+  size_t n = 0;
+  for (const pb_tensors::Span& s : t.spans) {
+    if (n > 0 && s.begin < t.spans[n - 1].end) {
+      t.spans[n - 1].end = std::max(t.spans[n - 1].end, s.end);
+      t.spans[n - 1].tensor = -1;
+      t.shares = true;
+    } else {
+      t.spans[n++] = s;
+    }
+  }
+  t.spans.resize(n);
+}
+// Whether each tensor of `out` is the same memory as its own of `in` or apart from all of them.
+bool apart_or_same(const pb_tensors& in, const pb_tensors& out) {
+  for (size_t i = 0, j = 0; i < in.spans.size() && j < out.spans.size();) {
+    const pb_tensors::Span &a = in.spans[i], &b = out.spans[j];
+    if (a.end <= b.begin) ++i;
+    else if (b.end <= a.begin) ++j;
+    else if (a.tensor < 0 || a.tensor != b.tensor || a.begin != b.begin) return false;
+    else ++i, ++j;
+  }
+  return true;
+}
+bool is_current(int device) {
+  int now = -1;
+  if (hipGetDevice(&now) == hipSuccess) return now == device;
+  (void)hipGetLastError();
+  return false;
+}
+
 template <typename T>
 void advance(T*& p, int64_t n) {
   if (p) p += n;
@@ -751,12 +788,14 @@ int pb_tensors_build(const void* const* d_buffers, const int64_t* sizes, const i
   for (int32_t i = 0; i < n; ++i) {
     if (dtypes[i] != PB_F32 && dtypes[i] != PB_F16 && dtypes[i] != PB_BF16) return PB_EINVAL;
     if (sizes[i] < 0 || (sizes[i] > 0 && (!d_buffers[i] || !aligned(d_buffers[i], element_bytes(dtypes[i]))))) return PB_EINVAL;
-    if (sizes[i] > (1ll << 40)) return PB_EUNSUPPORTED;
+  }
+  int64_t elements = 0;
+  for (int32_t i = 0; i < n; ++i) {
+    if (sizes[i] > pb::kMostElements - elements) return PB_EUNSUPPORTED;
+    elements += sizes[i];
   }
   pb_tensors* t = nullptr;
   std::vector<pb::GradChunk> chunks;
-  int64_t elements = 0;
-  for (int32_t i = 0; i < n; ++i) elements += std::min<int64_t>(sizes[i], 1ll << 30);
   const int64_t chunk = pb::chunk_for(elements);
   try {
     for (int32_t i = 0; i < n; ++i)
@@ -766,13 +805,14 @@ int pb_tensors_build(const void* const* d_buffers, const int64_t* sizes, const i
     t = new pb_tensors();
     t->sizes.assign(sizes, sizes + n);
     t->dtypes.assign(dtypes, dtypes + n);
+    find_spans(d_buffers, *t);
   } catch (const std::bad_alloc&) {
     delete t;
     return PB_ENOMEM;
   }
   t->device = device;
   t->count = static_cast<int64_t>(chunks.size());
-  for (int32_t i = 0; i < n; ++i) t->bytes = std::min<int64_t>(1ll << 60, t->bytes + sizes[i] * element_bytes(dtypes[i]));
+  for (int32_t i = 0; i < n; ++i) t->bytes += sizes[i] * element_bytes(dtypes[i]);
   int prev = 0, rc = PB_OK;
   if (hipGetDevice(&prev) != hipSuccess || hipSetDevice(device) != hipSuccess) {
     (void)hipGetLastError();
@@ -814,7 +854,7 @@ int pb_tensors_free(pb_tensors* tensors) {
 int64_t pb_grad_norm_workspace_bytes(const pb_tensors* grads) { return grads ? pb::grad_norm_workspace(grads->count) : PB_EINVAL; }
 
 int pb_grad_norm(const pb_tensors* grads, float* d_norm, void* d_workspace, int64_t workspace_bytes, void* hip_stream) {
-  if (!grads || !d_norm || !aligned(d_norm, 4) || workspace_bytes < 0) return PB_EINVAL;
+  if (!grads || !d_norm || !aligned(d_norm, 4) || workspace_bytes < 0 || !is_current(grads->device)) return PB_EINVAL;
   if (check_workspace(pb::grad_norm_workspace(grads->count), d_workspace, workspace_bytes) != PB_OK) return PB_EINVAL;
   return pb::launch_grad_norm(grads->d_chunks, grads->count, grads->bytes, d_norm, d_workspace, static_cast<hipStream_t>(hip_stream));
 }
@@ -822,7 +862,9 @@ int pb_grad_norm(const pb_tensors* grads, float* d_norm, void* d_workspace, int6
 int pb_grad_clip(const pb_tensors* grads, const float* d_norm, float max_norm, const pb_tensors* out, void* hip_stream) {
   if (!grads || !d_norm || !aligned(d_norm, 4)) return PB_EINVAL;
   if (!(max_norm >= 0.0f && max_norm <= 3.402823466e+38f)) return PB_ERANGE;
-  if (out && (out->device != grads->device || out->sizes != grads->sizes || out->dtypes != grads->dtypes)) return PB_EINVAL;
+  if (!is_current(grads->device) || (out ? out : grads)->shares) return PB_EINVAL;
+  if (out && out != grads && (out->device != grads->device || out->sizes != grads->sizes || out->dtypes != grads->dtypes || !apart_or_same(*grads, *out)))
+    return PB_EINVAL;
   return pb::launch_grad_clip(grads->d_chunks, out ? out->d_chunks : grads->d_chunks, grads->count, grads->bytes, d_norm, max_norm, static_cast<hipStream_t>(hip_stream));
 }
 

@@ -70,6 +70,7 @@ int launch_embed_tokens_backward(int grad_dtype, int table_dtype, const EmbedGra
 
 // A set of tensors as the kernels see it: pieces of at most kChunk elements, fewer in small sets (which are to fill the chip), in the
 // order of the tensors.
+constexpr int64_t kMostElements = 1ll << 40;
 constexpr int kChunk = 16384, kLeastChunk = 2048;
 inline int64_t chunk_for(int64_t elements) {
   const int64_t even = (elements / 2048 + kLeastChunk - 1) / kLeastChunk * kLeastChunk;
@@ -93,4 +94,10 @@ struct pb_tensors {
   int device = -1;
   std::vector<int64_t> sizes;
   std::vector<int32_t> dtypes;
+  struct Span {
+    uintptr_t begin, end;
+    int32_t tensor;  // -1: several that share memory
+  };
+  std::vector<Span> spans;  // by address, apart from each other
+  bool shares = false;      // whether any of them is of several tensors
 };

@@ -37,6 +37,7 @@ struct Sums {
 __device__ __forceinline__ double off_by(double s, int V) {
   return static_cast<double>((2.1f * __builtin_amdgcn_logf(static_cast<float>(V) / static_cast<float>(s)) + 17.0f) * 0x1p-24f);
 }
+constexpr double kBeside = 0x1p-34;      // products of two such bounds, and what the sums in 64 bits are off by
 constexpr double kNothing = 0x1p-40;     // a rest of the target's mass below this is none (equal rows differ by their roundings)
 constexpr double kNoWeight = 0x1p-960;   // weights below this, masked tokens' among them, are none
 
@@ -293,7 +294,7 @@ __device__ __forceinline__ Verdict decide(const VerifyArgs& a, int64_t b, const 
       const double q = draft ? share(yt, joined.m[a.n + 1 + lane], joined.s[a.n + 1 + lane], a.draft_scale) : 1.0;
       const double uq = static_cast<double>(u) * q;
       takes = uq < p;  // (false for NaN)
-      unsure = p > 0.0 && fabs(uq - p) <= p * (joined.off[lane] + (draft ? joined.off[a.n + 1 + lane] : 0.0) + 0x1p-40) && !((exact >> lane) & 1u);
+      unsure = p > 0.0 && fabs(uq - p) <= p * (joined.off[lane] + (draft ? joined.off[a.n + 1 + lane] : 0.0) + kBeside) && !((exact >> lane) & 1u);
     }
     const int stop = first_lane(~__ballot(takes || unsure));  // (the first that is refused for sure; lane 63 takes none)
     const u64 open = __ballot(unsure) & ((1ull << stop) - 1);
@@ -322,7 +323,7 @@ __device__ __forceinline__ Verdict decide(const VerifyArgs& a, int64_t b, const 
     r.qm = joined.m[a.n + 1 + r.k];
     if (r.qm != -INFINITY) {
       r.ratio = ps / qs;
-      r.near = joined.off[r.k] + joined.off[a.n + 1 + r.k] + 0x1p-40;
+      r.near = joined.off[r.k] + joined.off[a.n + 1 + r.k] + kBeside;
     }
     r.none |= qs != qs;
   }

@@ -284,6 +284,32 @@ def test_clip_refuses_another_set():
         assert e.value.code == pb.PB_EINVAL
 
 
+def test_tensors_that_share_memory():
+    x, norm, ws = torch.arange(1.0, 17.0, device=DEV), torch.full((1,), 8.0, device=DEV), workspace(64)
+    f32 = lambda *parts: pb.pb_tensors_build(list(parts), [p.numel() for p in parts], [pb.PB_F32] * len(parts))  # noqa: E731
+    lo, mid, hi, y = x[:4], x[2:6], x[4:8], torch.zeros(8, device=DEV)
+    none = x[:0]
+    for grads, out in ((f32(lo, lo), None), (f32(lo, mid), None), (f32(lo, hi), f32(hi, lo)), (f32(lo, hi), f32(y[:4], y[2:6])), (f32(lo), f32(mid)),
+                       (f32(lo, hi), f32(x[8:12], lo)), (f32(lo, mid), f32(lo, y[:4])), (f32(lo, hi, x[8:12]), f32(lo, hi, x[7:11])),
+                       (f32(x[:8], y), f32(x[1:9], y))):
+        before = x.clone()
+        with pytest.raises(pb.PbError) as e:
+            pb.pb_grad_clip(grads, norm, 1.0, out, stream_ptr())
+        assert e.value.code == pb.PB_EINVAL and torch.equal(x, before)
+    # each counts in the norm; into other buffers, or the same ones by another set, they are clipped
+    got = torch.zeros(1, device=DEV)
+    pb.pb_grad_norm(f32(lo, mid), got, ws, 64, stream_ptr())
+    want = float(torch.cat([lo, mid]).double().square().sum().sqrt())
+    assert abs(float(got) - want) <= 2 * S.U * want
+    pb.pb_grad_clip(f32(lo, mid), norm, 1.0, f32(y[:4], y[4:]), stream_ptr())
+    assert torch.equal(y, torch.cat([lo, mid]) / 8)
+    before = x.clone()
+    pb.pb_grad_clip(f32(hi, none, lo), norm, 1.0, f32(hi, y[:0], lo), stream_ptr())
+    assert torch.equal(x[:8], before[:8] / 8) and torch.equal(x[8:], before[8:])
+    pb.pb_grad_clip(f32(x[8:12], hi, lo), norm, 1.0, f32(x[8:12], y[:4], lo), stream_ptr())
+    assert torch.equal(x[8:12], before[8:12] / 8) and torch.equal(y[:4], before[4:8] / 64) and torch.equal(x[4:8], before[4:8] / 8)
+
+
 # ---- verification ------------------------------------------------------------------------------------------------------
 
 def block(x, kind, row_stride, seq_stride, shift=0):

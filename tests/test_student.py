@@ -79,6 +79,7 @@ def test_sets_of_tensors_refused():
     assert lib.pb_tensors_build(*one, 1, 0, None) == pb.PB_EINVAL
     for buffers, sizes, kinds, want in (([None], [1], [0], pb.PB_EINVAL), ([P], [-1], [0], pb.PB_EINVAL), ([P], [1], [3], pb.PB_EINVAL),
                                         ([P + 2], [1], [0], pb.PB_EINVAL), ([P + 1], [1], [2], pb.PB_EINVAL), ([P], [1 << 41], [0], pb.PB_EUNSUPPORTED),
+                                        ([P, 2 * P], [1 << 39, (1 << 39) + 1], [2, 2], pb.PB_EUNSUPPORTED),
                                         ([], [], [], pb.PB_EINVAL), ([P], [1, 2], [0], pb.PB_EINVAL)):
         with pytest.raises(pb.PbError) as e:
             pb.pb_tensors_build(buffers, sizes, kinds)
