@@ -128,20 +128,24 @@ __global__ __launch_bounds__(256) void embed_kernel(EmbedArgs a, int lanes) {
 // Sorting.  A workgroup takes a range of the vocabulary, 2^shift tokens, and reads all tokens: those of its range it counts, for each
 // wave's share of the positions apart, and places in a second pass; those below its range it counts for the place its range
 // begins at.  So the order is that of the positions, without an atomic on memory and with one launch.  Reading all tokens in every
-// workgroup takes time with their number (16384 of them: 11 us, 131072: 42), so from kManyTokens on the positions are
+// workgroup takes time with their number (16384 of them: 9 us, 131072: 42), so from kManyTokens on the positions are
 // split by range first, in chunks: then a workgroup reads its own alone (131072: 7 and 16 us).  Gradients of 32001 x 256 fp32, split / not:
-// 20000 tokens 36.0 / 33.0 us, 32768 38.5 / 35.6, 65536 45.2 / 49.4.
+// 24000 tokens 32.9 / 28.5 us, 36000 36.2 / 32.6, 48000 37.9 / 37.8, 64000 41.4 / 42.2, 90000 58.5 / 61.3.
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64;
-constexpr int kAhead = 16;      // tokens that a lane requests at once
+constexpr int kAhead = 16, kTail = 4;  // tokens that a lane requests at once, and of the last ones
 constexpr int kMaxShift = 9;    // (ranges of 512 tokens: 32 KiB of counts)
 constexpr int kMaxRanges = (kLogitsMaxV + (1 << kMaxShift) - 1) >> kMaxShift;
 static_assert(kMaxRanges <= kSortThreads, "a thread a range");
 constexpr int kManyTokens = 40960;
 constexpr int kSplit = 4096;    // positions of a chunk: 12 bits beside those of a token in its range
 
-int shift_for(int V) {  // about as many ranges as there are CUs
+// Workgroups a range: the one with the most frequent token takes longest, and two of them place half the positions each (they count all).  Two /
+// one: 8000 x 640 fp32 on 8192 rows 22.9 / 24.4 us, 40000 x 128 on 4097 28.8 / 31.2; where the ranges are as many as CUs already 16000 x 64 on
+// 131072 26.9 / 25.3.
+int parts_for(int n, int V) { return n >= 4096 && n < kManyTokens && V <= 128 << kMaxShift ? 2 : 1; }
+int shift_for(int n, int V) {  // about as many workgroups as there are CUs
   int shift = 0;
-  while (shift < kMaxShift && ((V - 1) >> shift) >= 256) ++shift;
+  while (shift < kMaxShift && ((V - 1) >> shift) >= 256 / parts_for(n, V)) ++shift;
   return shift;
 }
 
@@ -186,19 +190,28 @@ __device__ __forceinline__ void write_owners(const Owners& o, int range, int v0,
 }
 
 // counts[wave][i], i < size: how many of each wave; becomes the place of the wave's first, `base` ahead of them all.  Returns
-// the place of the thread's i (and in *end what follows it).
+// the place of the thread's i (and in *end what follows it).  PARTS: two more rows of counts, of what lies ahead of all waves' and behind.
+template <bool PARTS = false>
 __device__ __forceinline__ int places(int* counts, int stride, int size, int base, int* s, int* end) {
   const int tid = threadIdx.x;
-  int total = 0, all;
-  if (tid < size)
-    for (int w = 0; w < kSortWaves; ++w) total += counts[w * stride + tid];
+  int total = 0, all, ahead = 0, each[kSortWaves];
+  if (tid < size) {
+    if (PARTS) {
+      ahead = counts[kSortWaves * stride + tid];
+      total = ahead + counts[(kSortWaves + 1) * stride + tid];
+    }
+#pragma unroll
+    for (int w = 0; w < kSortWaves; ++w) each[w] = counts[w * stride + tid];
+#pragma unroll
+    for (int w = 0; w < kSortWaves; ++w) total += each[w];
+  }
   const int first = base + group_upto(total, s, &all) - total;
   if (tid < size) {
-    int at = first;
+    int at = first + ahead;
+#pragma unroll
     for (int w = 0; w < kSortWaves; ++w) {
-      const int c = counts[w * stride + tid];
       counts[w * stride + tid] = at;
-      at += c;
+      at += each[w];
     }
   }
   *end = first + total;
@@ -219,29 +232,28 @@ __device__ __forceinline__ void count_keys(int* counters, unsigned key, bool in,
   }
   if ((left >> lane) & 1) atomicAdd(&counters[key], 1);
 }
-// Places a wave's keys (of `bits` bits) at their counters, in the order of the lanes: key by key while there are few or one has many
-// lanes, what is left after that bit by bit.
+// Places a wave's keys (of `bits` bits) at their counters, in the order of the lanes.  Which lanes have the same key is found key by key
+// while there are few or one has many lanes, for what is left after that bit by bit; the counters are read and moved on once for all.
 template <int ROUNDS, typename Put>
 __device__ __forceinline__ void place_keys(int* counters, unsigned key, bool in, int bits, int lane, Put&& put) {
-  u64 left = __ballot(in);
+  u64 left = __ballot(in), same = 0;
+  if (!left) return;
   for (int round = 0; left && (round < ROUNDS || __builtin_popcountll(left) <= 4); ++round) {
     const unsigned k = static_cast<unsigned>(__builtin_amdgcn_readlane(static_cast<int>(key), first_lane(left)));
-    const u64 same = left & __ballot(key == k);
-    const int to = counters[k];
-    if ((same >> lane) & 1) put(to + __builtin_popcountll(same & ((1ull << lane) - 1)));
-    if (lane == 0) counters[k] = to + __builtin_popcountll(same);
-    left &= ~same;
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
+    const u64 these = left & __ballot(key == k);
+    if ((these >> lane) & 1) same = these;
+    left &= ~these;
   }
-  if (!left) return;
-  u64 same = left;
-  for (int b = 0; b < bits; ++b) {
-    const bool one = (key >> b) & 1u;
-    const u64 ones = __ballot(one);
-    same &= one ? ones : ~ones;
+  if (left) {
+    u64 those = left;
+    for (int b = 0; b < bits; ++b) {
+      const bool one = (key >> b) & 1u;
+      const u64 ones = __ballot(one);
+      those &= one ? ones : ~ones;
+    }
+    if ((left >> lane) & 1) same = those;
   }
-  if ((left >> lane) & 1) {
+  if (in) {
     const int to = counters[key], rank = __builtin_popcountll(same & ((1ull << lane) - 1));
     __builtin_amdgcn_wave_barrier();
     if (rank == 0) counters[key] = to + __builtin_popcountll(same);
@@ -252,43 +264,56 @@ __device__ __forceinline__ void place_keys(int* counters, unsigned key, bool in,
 }
 
 __global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(const int32_t* tokens, int n, int V, int shift, int32_t* begin, int32_t* order, Owners owners) {
-  extern __shared__ int counts[];  // [kSortWaves][2^shift]
+  extern __shared__ int counts[];  // [kSortWaves + 2][2^shift]
   __shared__ int s[kSortWaves];
-  const int tid = threadIdx.x, lane = tid & 63, wave = uniform_i(tid >> 6), range = 1 << shift;
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform_i(tid >> 6), range = 1 << shift, part = blockIdx.y, parts = gridDim.y;
   const int v0 = blockIdx.x << shift, size = min(range, V - v0);
-  for (int i = tid; i < kSortWaves * range; i += kSortThreads) counts[i] = 0;
+  for (int i = tid; i < (kSortWaves + 2) * range; i += kSortThreads) counts[i] = 0;
   __syncthreads();
-  const int share = ((n + kSortWaves - 1) / kSortWaves + 63) / 64 * 64, p0 = min(n, wave * share), p1 = min(n, p0 + share);
+  const int shares = kSortWaves * parts, share = ((n + shares - 1) / shares + 63) / 64 * 64;
+  const int p0 = min(n, (part * kSortWaves + wave) * share), p1 = min(n, p0 + share);
   int* mine = counts + wave * range;
   int below = 0;
-  auto count = [&](int t) {  // (an id below 0 is a large one without its sign)
+  auto count = [&](int* to, int t) {  // (an id below 0 is a large one without its sign)
     const unsigned u = static_cast<unsigned>(t) - static_cast<unsigned>(v0);
     below += static_cast<unsigned>(t) < static_cast<unsigned>(v0);
-    if (u < static_cast<unsigned>(size)) atomicAdd(&mine[u], 1);
+    if (u < static_cast<unsigned>(size)) atomicAdd(&to[u], 1);
   };
-  int p = p0;
-  for (; p + 64 * kAhead <= p1; p += 64 * kAhead) {
-    int t[kAhead];
+  auto count_share = [&](int* to, int p, int end) {
+    for (; p + 64 * kAhead <= end; p += 64 * kAhead) {
+      int t[kAhead];
 #pragma unroll
-    for (int k = 0; k < kAhead; ++k) t[k] = tokens[p + 64 * k + lane];
+      for (int k = 0; k < kAhead; ++k) t[k] = tokens[p + 64 * k + lane];
 #pragma unroll
-    for (int k = 0; k < kAhead; ++k) count(t[k]);
+      for (int k = 0; k < kAhead; ++k) count(to, t[k]);
+    }
+    for (; p < end; p += 64 * kTail) {
+      int t[kTail];
+#pragma unroll
+      for (int k = 0; k < kTail; ++k) t[k] = p + 64 * k + lane < end ? tokens[p + 64 * k + lane] : -1;
+#pragma unroll
+      for (int k = 0; k < kTail; ++k) count(to, t[k]);
+    }
+  };
+  for (int q = 0; q < parts; ++q) {
+    const int from = min(n, (q * kSortWaves + wave) * share);
+    count_share(q == part ? mine : counts + (q < part ? kSortWaves : kSortWaves + 1) * range, from, min(n, from + share));
   }
-  for (; p < p1; p += 64)
-    if (p + lane < p1) count(tokens[p + lane]);
   int base, end;
   group_upto(below, s, &base);
-  const int at = places(counts, range, size, base, s, &end);
-  if (tid < size) {
-    begin[v0 + tid] = at;
-    if (v0 + tid == V - 1) begin[V] = end;
+  const int at = places<true>(counts, range, size, base, s, &end);
+  if (part == 0) {
+    if (tid < size) {
+      begin[v0 + tid] = at;
+      if (v0 + tid == V - 1) begin[V] = end;
+    }
+    write_owners(owners, blockIdx.x, v0, size, at, end, s);
   }
-  write_owners(owners, blockIdx.x, v0, size, at, end, s);
   auto put = [&](int t, int from) {
     const unsigned u = static_cast<unsigned>(t) - static_cast<unsigned>(v0);
     place_keys<1>(mine, u, u < static_cast<unsigned>(size), shift, lane, [&](int to) { order[to] = from; });
   };
-  p = p0;  // (the same in all lanes of a wave)
+  int p = p0;  // (the same in all lanes of a wave)
   for (; p + 64 * kAhead <= p1; p += 64 * kAhead) {
     int t[kAhead];
 #pragma unroll
@@ -296,7 +321,13 @@ __global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(const int32_t*
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) put(t[k], p + 64 * k + lane);
   }
-  for (; p < p1; p += 64) put(p + lane < p1 ? tokens[p + lane] : -1, p + lane);
+  for (; p < p1; p += 64 * kTail) {
+    int t[kTail];
+#pragma unroll
+    for (int k = 0; k < kTail; ++k) t[k] = p + 64 * k + lane < p1 ? tokens[p + 64 * k + lane] : -1;
+#pragma unroll
+    for (int k = 0; k < kTail; ++k) put(t[k], p + 64 * k + lane);
+  }
 }
 
 // A chunk's positions by the range of their tokens, in order: an entry is the token's place in its range and the position's in the
@@ -471,7 +502,10 @@ __device__ __forceinline__ void sum_stretch(const SumArgs& s, int c, int vector,
 // The first stretch_blocks workgroups take stretches (a piece takes longer than other rows), the others tokens, `lanes` lanes SL vectors of a
 // row.  What belongs to a row lies next to each other in the grid, so that rows are read whole (131072 x 2048 bf16 285 -> 262 us).  The gradient is
 // written past the caches (262 us and, 16384 x 1024 on fp32 rows, 40; otherwise 283 and 66).  Bound by HBM: 1.07 GB in 215 us of those 262.
-template <typename G, typename T, int SL, bool NARROW>
+// ROWS: rows that lanes take one after the other, where a row is one vector of each lane and there are more rows than the chip holds at
+// once twice over: where they begin is read at once (60000 x 512 bf16 on 50000 49.3 -> 44.2 us, 100000 x 200 on 131072 fp32 rows 74 -> 61; two rows
+// 45.6 and 63; few rows lose by it: 40000 x 128 on 4097 rows 28.6 -> 32.3, longer ones as well: 8000 x 640 22.5 -> 24.5).
+template <typename G, typename T, int SL, int ROWS, bool NARROW>
 __global__ __launch_bounds__(256) void embed_sums_kernel(SumArgs s, int stretch_blocks, unsigned vectors) {
   constexpr int K = step_of<G, T>();
   const EmbedGradArgs& a = s.a;
@@ -482,19 +516,29 @@ __global__ __launch_bounds__(256) void embed_sums_kernel(SumArgs s, int stretch_
     if (static_cast<int64_t>(c) * kFew < end) sum_stretch<G, K, NARROW>(s, c, static_cast<int>(unit % vectors), end, lane);
     return;
   }
-  const unsigned of_row = (vectors + SL - 1) / SL, v = unit / of_row;
-  if (v >= static_cast<unsigned>(a.V)) return;
-  const int i = s.begin[v], j = s.begin[v + 1];
-  if (j - i > kFew || (j == i && a.accumulate)) return;
-  const Columns<K, SL, NARROW> cols(a.dim, static_cast<int>(unit % of_row) * s.lanes * K * SL, s.lanes, lane);
-  float sum[SL][K] = {};
-  sum_positions<G>(a, s.order, cols, i, j, sum);
-  write_columns<T>(a, cols, static_cast<int>(v), sum);
+  const unsigned of_row = SL == 1 ? 1 : (vectors + SL - 1) / SL, first = (blockIdx.x - stretch_blocks) * (each * ROWS) + threadIdx.x / s.lanes;
+  int from[ROWS], to[ROWS];
+#pragma unroll
+  for (int r = 0; r < ROWS; ++r) {
+    const unsigned v = min((first + r * each) / of_row, static_cast<unsigned>(a.V) - 1);
+    from[r] = s.begin[v];
+    to[r] = s.begin[v + 1];
+  }
+#pragma unroll
+  for (int r = 0; r < ROWS; ++r) {
+    const unsigned v = (first + r * each) / of_row;
+    if (v >= static_cast<unsigned>(a.V)) return;
+    if (to[r] - from[r] > kFew || (to[r] == from[r] && a.accumulate)) continue;
+    const Columns<K, SL, NARROW> cols(a.dim, static_cast<int>((first + r * each) % of_row) * s.lanes * K * SL, s.lanes, lane);
+    float sum[SL][K] = {};
+    sum_positions<G>(a, s.order, cols, from[r], to[r], sum);
+    write_columns<T>(a, cols, static_cast<int>(v), sum);
+  }
 }
 
 // Pieces of a token, in the order of their stretches: a workgroup a range (and vectors of its columns).  Its groups of lanes take the tokens
 // of few pieces one each; of the others, each group sums a share of the pieces, and the first of them those sums.
-constexpr int kJoinThreads = 1024;
+constexpr int kJoinThreads = 512;  // (1024 / 512 / 256: 131072 x 2048 bf16 259 / 256 / 285 us, 8000 x 640 fp32 27.5 / 26.7 / 25.7, 40000 x 128 34.8 / 32.9 / 32.7)
 template <typename T, int K, bool NARROW>
 __global__ __launch_bounds__(kJoinThreads) void embed_join_kernel(SumArgs s, Owners owners, int shift) {
   __shared__ float shares[kJoinThreads * K];
@@ -505,7 +549,7 @@ __global__ __launch_bounds__(kJoinThreads) void embed_join_kernel(SumArgs s, Own
   const int tid = threadIdx.x, groups = kJoinThreads / s.lanes, group = tid / s.lanes, lane = tid & (s.lanes - 1);
   const Columns<K, 1, NARROW> cols(a.dim, blockIdx.y * s.lanes * K, s.lanes, lane);
   const int64_t row = 2 * static_cast<int64_t>(a.dim);
-  constexpr int U = 8, kFewPieces = 16;
+  constexpr int U = 2 * K, kFewPieces = 16;
   auto add = [&](int first_place, int k, int k1, float (&sum)[1][K]) {  // pieces of stretches k .. k1 - 1
     const int c = first_place / kFew;
     for (; k < k1; k += U) {
@@ -646,7 +690,7 @@ Layout layout(int32_t n, int32_t V, int32_t dim) {
   Layout l;
   l.begin = 0;
   l.order = padded((static_cast<int64_t>(V) + 1) * 4);
-  const int shift = shift_for(V), ranges = ((V - 1) >> shift) + 1;
+  const int shift = shift_for(n, V), ranges = ((V - 1) >> shift) + 1;
   l.count = l.order + padded(static_cast<int64_t>(n) * 4);
   l.list = l.count + padded(static_cast<int64_t>(ranges) * 4);
   l.pieces = l.list + padded((static_cast<int64_t>(ranges) << shift) * static_cast<int64_t>(sizeof(Owner)));
@@ -669,10 +713,10 @@ struct Shape {
   int lanes, vectors;
   explicit Shape(int dim) : lanes(lanes_for(dim, K)), vectors((dim + lanes * K - 1) / (lanes * K)) {}
 };
-// us, in one launch / in three, fp32 where not said: 300 tokens, 1025 x 64 3.3 / 10.4, 8192 x 64 10.0 / 9.3; 2000, 4096 x 64 9.2 / 13.8, 8192 x 64 15.2 /
-// 14.1; 4096, 1025 x 640 12.7 / 19.2, 8192 x 512 bf16 21.6 / 16.3; 5000, 4096 x 64 19.7 / 16.7; 8192, 2048 x 64 15.3 / 20.6; 16384, 166 x 64 18.9 / 22.0,
-// 1025 x 64 18.0 / 23.8; and, where a token of many positions has few groups of lanes for them, 8192, 300 x 1024 bf16 27.1 / 23.7; 16384,
-// 166 x 2048 71 / 51.
+// us, in one launch / in three, fp32 where not said: 500 tokens, 1025 x 640 5.7 / 12.4; 2000, 4096 x 64 9.1 / 14.0, 8192 x 64 15.2 / 14.1; 2900, 6000 x 64
+// 12.2 / 13.9; 4096, 4096 x 64 10.0 / 14.8, 1025 x 640 12.7 / 17.0, 8192 x 512 bf16 21.6 / 16.3; 5000, 4096 x 64 19.7 / 16.7; 8192, 2048 x 64 15.1 / 17.7;
+// 16384, 166 x 64 18.4 / 21.3, 1025 x 64 17.4 / 20.1; and, where a token of many positions has few groups of lanes for them, 8192, 300 x 512 bf16
+// 17.4 / 17.8, 300 x 1024 bf16 27.1 / 23.7; 16384, 166 x 2048 71 / 51.
 bool small(int64_t n, int64_t V, int lanes, int vectors) {
   return n <= kSmallTokens && n * lanes <= 4096 * 64 && V * vectors <= 6144 && V * vectors * n <= 17 << 20;
 }
@@ -696,7 +740,7 @@ int backward(const EmbedGradArgs& a, char* ws, hipStream_t stream) {
     if (a.n <= 4096) return go(embed_small_kernel<G, T, 16, false, false>);
     return go(embed_small_kernel<G, T, 16, true, false>);
   }
-  const int shift = shift_for(a.V), ranges = ((a.V - 1) >> shift) + 1, stretches = (a.n + kFew - 1) / kFew;
+  const int shift = shift_for(a.n, a.V), ranges = ((a.V - 1) >> shift) + 1, stretches = (a.n + kFew - 1) / kFew;
   const size_t counts = static_cast<size_t>(kSortWaves) * 4 << shift;
   const Owners owners{reinterpret_cast<int32_t*>(ws + l.count), reinterpret_cast<Owner*>(ws + l.list)};
   if (a.n >= kManyTokens) {
@@ -707,20 +751,22 @@ int backward(const EmbedGradArgs& a, char* ws, hipStream_t stream) {
     if (done() != PB_OK) return PB_EHIP;
     embed_merge_kernel<<<ranges, kSortThreads, counts, stream>>>(entries, starts, chunks, a.V, shift, ranges, begin, order, owners);
   } else {
-    embed_sort_kernel<<<ranges, kSortThreads, counts, stream>>>(a.tokens, a.n, a.V, shift, begin, order, owners);
+    embed_sort_kernel<<<dim3(ranges, parts_for(a.n, a.V)), kSortThreads, counts + (static_cast<size_t>(8) << shift), stream>>>(a.tokens, a.n, a.V, shift, begin, order, owners);
   }
   if (done() != PB_OK) return PB_EHIP;
   const int64_t stretch_blocks = a.n > kFew ? (static_cast<int64_t>(stretches) * vectors + each - 1) / each : 0;
-  auto sums = [&](auto kernel, int sl) {
-    const int64_t row_blocks = (static_cast<int64_t>(a.V) * ((vectors + sl - 1) / sl) + each - 1) / each;
+  auto sums = [&](auto kernel, int sl, int rows) {
+    const int64_t of_block = static_cast<int64_t>(each) * rows, row_blocks = (static_cast<int64_t>(a.V) * ((vectors + sl - 1) / sl) + of_block - 1) / of_block;
     kernel<<<static_cast<unsigned>(stretch_blocks + row_blocks), 256, 0, stream>>>(s, static_cast<int>(stretch_blocks), static_cast<unsigned>(vectors));
     return done();
   };
   int rc;
-  if (a.dim < K) rc = sums(embed_sums_kernel<G, T, 1, true>, 1);
-  else if (vectors == 1) rc = sums(embed_sums_kernel<G, T, 1, false>, 1);
-  else if (vectors == 2) rc = sums(embed_sums_kernel<G, T, 2, false>, 2);
-  else rc = sums(embed_sums_kernel<G, T, 4, false>, 4);
+  const bool many = static_cast<int64_t>(a.V) * lanes > 64 * 16384;  // (waves of 64 lanes)
+  if (a.dim < K) rc = sums(embed_sums_kernel<G, T, 1, 1, true>, 1, 1);
+  else if (vectors == 1 && many) rc = sums(embed_sums_kernel<G, T, 1, 4, false>, 1, 4);
+  else if (vectors == 1) rc = sums(embed_sums_kernel<G, T, 1, 1, false>, 1, 1);
+  else if (vectors == 2) rc = sums(embed_sums_kernel<G, T, 2, 1, false>, 2, 1);
+  else rc = sums(embed_sums_kernel<G, T, 4, 1, false>, 4, 1);
   if (rc != PB_OK || stretch_blocks == 0) return rc;
   const dim3 grid(ranges, vectors);
   if (a.dim < K) embed_join_kernel<T, K, true><<<grid, kJoinThreads, 0, stream>>>(s, owners, shift);

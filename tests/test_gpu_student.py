@@ -122,6 +122,16 @@ def test_table_gradient_sizes(n, V, dim, hot):
         check_backward(rng, n, V, dim, kind, tkind, 0.1, hot, accumulate, (n, V, dim, kind))
 
 
+@pytest.mark.parametrize("n,V,dim,hot", [(4095, 65536, 5, 0.1), (4096, 65536, 5, 0.1), (4096, 65537, 4, 0.1), (20000, 32001, 250, 0.05), (300, 70001, 200, 0.2), (40959, 20001, 256, 0.3),
+                                         (9000, 200001, 22, 0.2), (7000, 33001, 300, 0.0), (41000, 16385, 511, 0.1), (4096, 16385, 256, 0.9), (1, 16385, 255, 0.0), (0, 16385, 256, 0.0),
+                                         (33000, 6145, 3, 0.02), (16385, 129, 3, 0.5), (32768, 65536, 2, 0.9)])
+def test_table_gradient_of_large_tables(n, V, dim, hot):
+    """Positions that two workgroups a range place, rows that lanes take several of."""
+    rng = np.random.default_rng(n + V)
+    for kind, tkind, accumulate in (("f32", "f32", 1), ("bf16", "f32", 0), ("f16", "bf16", 0), ("bf16", "bf16", 1)):
+        check_backward(rng, n, V, dim, kind, tkind, 0.1, hot, accumulate, (n, V, dim, kind))
+
+
 def test_table_gradient_of_runs():
     """Tokens in runs whose lengths lie around the lengths that are summed at once: ends of runs on and beside every border."""
     rng = np.random.default_rng(9)
