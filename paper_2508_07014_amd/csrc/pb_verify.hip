@@ -681,8 +681,9 @@ __global__ __launch_bounds__(64 * kPickWaves) void verify_pick_kernel(VerifyArgs
 // How a call is laid out.  us, one launch / two, 16 waves a sequence: 1 x 9 rows of 1024 fp32 8.1 / 9.8, 64 x 17 of 1025 bf16 10.1 / 11.6, 256 x 31 of
 // 1025 12.9 / 17.5, 1 x 17 of 4096 13.1 / 11.9, 256 x 17 of 4096 16.5 / 19.0, 1 x 9 of 8192 14.4 / 13.2, 256 x 9 of 8192 18.7 / 20.9, 64 x 3 of 16384 17.2 /
 // 18.0.  Two launches / three: 8 x 9 rows of 16000 bf16 18.5 / 18.0, 256 x 9 30.5 / 34.1, 64 x 9 of 8000 fp32 18.0 / 19.2; past what the
-// registers of a workgroup hold there are three.  Workgroups a sequence for 128 / 256 / 512 in all: 128 x 17 of 131072 bf16 197 / 154 / 148,
-// 64 x 1 29.4 / 23.4 / 24.3, 64 x 9 of 50000 without rows of the draft 29.4 / 27.3 / 29.4.
+// registers of a workgroup hold there are three.  Workgroups a sequence for 256 / 512 in all: 128 x 17 of 131072 bf16 155 /
+// 149, 200 x 3 of 131072 fp32 139.5 / 134.5, 64 x 3 of 131072 bf16 40.0 / 41.4, 64 x 9 of 50000 without rows of the draft 27.0 / 29.2, 128 x 9 of 50000 51.0 /
+// 52.1, 256 x 5 of 65536 72.0 / 73.6, 128 x 17 of 32001 fp32 70.7 / 73.7.
 struct Plan {
   int rows, parts;
   int groups;  // workgroups a sequence that sum the row that decides; 0: one workgroup decides and draws; -1: one does everything
@@ -699,7 +700,9 @@ Plan plan(int32_t sequences, int32_t n, bool drafted, int32_t V) {
     p.verdicts = p.slice_sums = p.bytes = 0;
     return p;
   }
-  p.groups = slices <= 16 * kHeld ? 0 : static_cast<int>(std::min<int64_t>((slices + kRestWaves - 1) / kRestWaves, std::max<int64_t>(1, 256 / sequences)));
+  int64_t groups = 256 / sequences;
+  if (slices >= 256) groups = std::max<int64_t>(groups, std::min(512 / sequences, slices / (4 * kRestWaves)));  // (four slices a wave)
+  p.groups = slices <= 16 * kHeld ? 0 : static_cast<int>(std::min<int64_t>((slices + kRestWaves - 1) / kRestWaves, std::max<int64_t>(1, groups)));
   p.verdicts = (static_cast<int64_t>(sequences) * p.rows * p.parts * static_cast<int64_t>(sizeof(Sums)) + 15) / 16 * 16;
   p.slice_sums = p.verdicts + (p.groups > 0 ? (static_cast<int64_t>(sequences) * static_cast<int64_t>(sizeof(Verdict)) + 15) / 16 * 16 : 0);
   p.bytes = p.slice_sums + (p.groups > 0 ? static_cast<int64_t>(sequences) * slices * static_cast<int64_t>(sizeof(Slice)) : 0);
