@@ -137,7 +137,13 @@ constexpr int kMaxShift = 9;    // (ranges of 512 tokens: 32 KiB of counts)
 constexpr int kMaxRanges = (kLogitsMaxV + (1 << kMaxShift) - 1) >> kMaxShift;
 static_assert(kMaxRanges <= kSortThreads, "a thread a range");
 constexpr int kManyTokens = 40960;
-constexpr int kSplit = 4096;    // positions of a chunk: 12 bits beside those of a token in its range
+constexpr int kSplit = 4096;    // positions of a chunk at most: 12 bits beside those of a token in its range
+// Positions of a chunk, so that the waves that merge them have as many each (67251 x 40 on 193 rows 47.0 -> 41.8 us, 200000 x 64 on
+// 32001 51.6 -> 48.3; always kSplit of them before).
+int span_for(int n) {
+  const int64_t turns = (static_cast<int64_t>(n) + kSortWaves * kSplit - 1) / (kSortWaves * kSplit);
+  return static_cast<int>(((n + kSortWaves * turns - 1) / (kSortWaves * turns) + 63) / 64 * 64);
+}
 
 // Workgroups a range: the one with the most frequent token takes longest, and two of them place half the positions each (they count all).  Two /
 // one: 8000 x 640 fp32 on 8192 rows 22.9 / 24.4 us, 40000 x 128 on 4097 28.8 / 31.2; where the ranges are as many as CUs already 16000 x 64 on
@@ -332,14 +338,14 @@ __global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(const int32_t*
 
 // A chunk's positions by the range of their tokens, in order: an entry is the token's place in its range and the position's in the
 // chunk; starts[chunk][range] is where the range's begin in the chunk, starts[chunk][ranges] how many there are.
-__global__ __launch_bounds__(kSortThreads) void embed_split_kernel(const int32_t* tokens, int n, int V, int shift, int ranges, unsigned* entries, int32_t* starts) {
+__global__ __launch_bounds__(kSortThreads) void embed_split_kernel(const int32_t* tokens, int n, int V, int shift, int ranges, int span, unsigned* entries, int32_t* starts) {
   __shared__ int counts[kSortWaves * kMaxRanges], s[kSortWaves];
   constexpr int kTurns = kSplit / kSortThreads;
-  const int tid = threadIdx.x, lane = tid & 63, wave = uniform_i(tid >> 6), p0 = blockIdx.x * kSplit, at0 = wave * (kSplit / kSortWaves) + lane;
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform_i(tid >> 6), p0 = blockIdx.x * span, p1 = min(n, p0 + span), at0 = wave * (kSplit / kSortWaves) + lane;
   for (int i = tid; i < kSortWaves * ranges; i += kSortThreads) counts[i] = 0;
   int t[kTurns];
 #pragma unroll
-  for (int k = 0; k < kTurns; ++k) t[k] = p0 + at0 + 64 * k < n ? tokens[p0 + at0 + 64 * k] : -1;
+  for (int k = 0; k < kTurns; ++k) t[k] = p0 + at0 + 64 * k < p1 ? tokens[p0 + at0 + 64 * k] : -1;
   __syncthreads();
   int* mine = counts + wave * ranges;
 #pragma unroll
@@ -361,7 +367,7 @@ __global__ __launch_bounds__(kSortThreads) void embed_split_kernel(const int32_t
 }
 
 // A range's positions from all chunks: each wave takes some chunks next to each other.
-__global__ __launch_bounds__(kSortThreads) void embed_merge_kernel(const unsigned* entries, const int32_t* starts, int chunks, int V, int shift, int ranges,
+__global__ __launch_bounds__(kSortThreads) void embed_merge_kernel(const unsigned* entries, const int32_t* starts, int chunks, int span, int V, int shift, int ranges,
                                                                   int32_t* begin, int32_t* order, Owners owners) {
   extern __shared__ int counts[];  // [kSortWaves][2^shift]
   __shared__ int s[kSortWaves];
@@ -387,7 +393,7 @@ __global__ __launch_bounds__(kSortThreads) void embed_merge_kernel(const unsigne
           const int from_lane = min(k0 + k, many - 1);
           i0[k] = __builtin_amdgcn_readlane(from, from_lane);
           i1[k] = k0 + k < many ? __builtin_amdgcn_readlane(to, from_lane) : i0[k];
-          e[k] = i0[k] + lane < i1[k] ? entries[static_cast<int64_t>(q + k0 + k) * kSplit + i0[k] + lane] : 0u;
+          e[k] = i0[k] + lane < i1[k] ? entries[static_cast<int64_t>(q + k0 + k) * span + i0[k] + lane] : 0u;
         }
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
@@ -395,7 +401,7 @@ __global__ __launch_bounds__(kSortThreads) void embed_merge_kernel(const unsigne
           for (int i = i0[k] + 64; i < i1[k]; i += 64 * 8) {
             unsigned more[8];
 #pragma unroll
-            for (int u = 0; u < 8; ++u) more[u] = i + 64 * u + lane < i1[k] ? entries[static_cast<int64_t>(q + k0 + k) * kSplit + i + 64 * u + lane] : 0u;
+            for (int u = 0; u < 8; ++u) more[u] = i + 64 * u + lane < i1[k] ? entries[static_cast<int64_t>(q + k0 + k) * span + i + 64 * u + lane] : 0u;
 #pragma unroll
             for (int u = 0; u < 8; ++u)
               if (i + 64 * u < i1[k]) f(more[u], i + 64 * u + lane < i1[k], q + k0 + k);
@@ -413,7 +419,7 @@ __global__ __launch_bounds__(kSortThreads) void embed_merge_kernel(const unsigne
   }
   write_owners(owners, b, v0, size, at, end, s);
   all([&](unsigned e, bool is, int c) {
-    place_keys<2>(mine, e / kSplit, is, shift, lane, [&](int to) { order[to] = c * kSplit + static_cast<int>(e % kSplit); });
+    place_keys<2>(mine, e / kSplit, is, shift, lane, [&](int to) { order[to] = c * span + static_cast<int>(e % kSplit); });
   });
 }
 
@@ -698,7 +704,7 @@ Layout layout(int32_t n, int32_t V, int32_t dim) {
   l.entries = l.starts = l.pieces;  // (entries and starts are done with before there are pieces)
   if (n >= kManyTokens) {
     l.starts = l.entries + padded(static_cast<int64_t>(n) * 4);
-    l.bytes = std::max(l.bytes, l.starts + padded((static_cast<int64_t>(n) + kSplit - 1) / kSplit * (ranges + 1) * 4));
+    l.bytes = std::max(l.bytes, l.starts + padded((static_cast<int64_t>(n) + span_for(n) - 1) / span_for(n) * (ranges + 1) * 4));
   }
   return l;
 }
@@ -746,10 +752,10 @@ int backward(const EmbedGradArgs& a, char* ws, hipStream_t stream) {
   if (a.n >= kManyTokens) {
     unsigned* entries = reinterpret_cast<unsigned*>(ws + l.entries);
     int32_t* starts = reinterpret_cast<int32_t*>(ws + l.starts);
-    const int chunks = (a.n + kSplit - 1) / kSplit;
-    embed_split_kernel<<<chunks, kSortThreads, 0, stream>>>(a.tokens, a.n, a.V, shift, ranges, entries, starts);
+    const int span = span_for(a.n), chunks = (a.n + span - 1) / span;
+    embed_split_kernel<<<chunks, kSortThreads, 0, stream>>>(a.tokens, a.n, a.V, shift, ranges, span, entries, starts);
     if (done() != PB_OK) return PB_EHIP;
-    embed_merge_kernel<<<ranges, kSortThreads, counts, stream>>>(entries, starts, chunks, a.V, shift, ranges, begin, order, owners);
+    embed_merge_kernel<<<ranges, kSortThreads, counts, stream>>>(entries, starts, chunks, span, a.V, shift, ranges, begin, order, owners);
   } else {
     embed_sort_kernel<<<dim3(ranges, parts_for(a.n, a.V)), kSortThreads, counts + (static_cast<size_t>(8) << shift), stream>>>(a.tokens, a.n, a.V, shift, begin, order, owners);
   }
