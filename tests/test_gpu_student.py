@@ -225,7 +225,8 @@ def run_norm(grads, stream=None):
 
 SPECS = [[(1, "f32")], [(5, "bf16"), (0, "f16"), (9, "f16"), (3, "f32")], [(16384, "f32"), (16385, "bf16"), (16383, "f16"), (1, "bf16")],
          [(100000, "bf16"), (7, "f32"), (300001, "f32"), (77777, "f16")], [(n, k) for n in range(1, 40) for k in KIND], [(0, "f32")],
-         [(50_000_000, "bf16"), (3, "f32")]]
+         [(50_000_000, "bf16"), (3, "f32")], [(1 + k, "f16") for k in range(64)], [(1, "f32")] * 65, [(2048 * 64, "bf16")], [(2048 * 63 + 1, "f32"), (1, "bf16")],
+         [(2047, k) for k in KIND] * 16 + [(2049, "f32")] * 8]
 
 
 @pytest.mark.parametrize("spec", SPECS, ids=range(len(SPECS)))
