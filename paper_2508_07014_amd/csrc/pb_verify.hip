@@ -255,15 +255,10 @@ __device__ __forceinline__ double row_sum(const typename E::type* x, int V, floa
   return s;
 }
 
-// Joins the parts of all rows (waves of the workgroup take turns), then decides, the same in every wave.  Writes the accepted tokens
-// if `writes`, in the last wave.
-template <typename E, int WAVES>
-__device__ __forceinline__ Verdict decide(const VerifyArgs& a, int64_t b, const Drafted& tokens, float xt, float yt, const Sums* sums, int rows, int parts,
-                                          RowSums& joined, bool writes) {
-  const int lane = threadIdx.x & 63, wave = uniform_i(threadIdx.x >> 6), t = tokens.t, count = tokens.count;
-  const float u = tokens.u;
-  const typename E::type* target = static_cast<const typename E::type*>(a.target) + b * a.target_seq;
-  const typename E::type* draft = a.draft ? static_cast<const typename E::type*>(a.draft) + b * a.draft_seq : nullptr;
+// Joins the parts of all rows (waves of the workgroup take turns).
+template <int WAVES>
+__device__ __forceinline__ void join_rows(const VerifyArgs& a, const Sums* sums, int rows, int parts, RowSums& joined) {
+  const int lane = threadIdx.x & 63, wave = uniform_i(threadIdx.x >> 6);
   for (int j = wave; j < rows; j += WAVES) {  // (rows behind the end of the draft too, whose sums nobody has written and nobody looks at)
     const Scale k = j <= a.n ? a.target_scale : a.draft_scale;
     Sums part{-INFINITY, 0.0f, 0.0f, 0.0f};
@@ -284,6 +279,15 @@ __device__ __forceinline__ Verdict decide(const VerifyArgs& a, int64_t b, const 
       joined.off[j] = off_by(s, a.V);
     }
   }
+}
+
+// Decides from the rows' sums, the same in every wave.  Writes the accepted tokens if `writes`, in the last wave.
+template <typename E, int WAVES>
+__device__ __forceinline__ Verdict decide(const VerifyArgs& a, int64_t b, const Drafted& tokens, float xt, float yt, RowSums& joined, bool writes) {
+  const int lane = threadIdx.x & 63, wave = uniform_i(threadIdx.x >> 6), t = tokens.t, count = tokens.count;
+  const float u = tokens.u;
+  const typename E::type* target = static_cast<const typename E::type*>(a.target) + b * a.target_seq;
+  const typename E::type* draft = a.draft ? static_cast<const typename E::type*>(a.draft) + b * a.draft_seq : nullptr;
   __syncthreads();
   bool takes = false;
   for (u64 exact = 0;;) {
@@ -347,7 +351,9 @@ __device__ __forceinline__ Verdict decide_rows(const VerifyArgs& a, int64_t b, c
     xt = sums[lane * parts].at;
     if (a.draft) yt = sums[(a.n + 1 + lane) * parts].at;
   }
-  return decide<E, WAVES>(a, b, drafted_tokens(a, b, lane), xt, yt, sums, rows, parts, joined, writes);
+  const Drafted tokens = drafted_tokens(a, b, lane);
+  join_rows<WAVES>(a, sums, rows, parts, joined);
+  return decide<E, WAVES>(a, b, tokens, xt, yt, joined, writes);
 }
 
 // The rows that decide, as weights.
@@ -522,7 +528,8 @@ __global__ __launch_bounds__(64 * WAVES) void verify_small_kernel(VerifyArgs a, 
     if (lane == 0) sums[item] = s;
   }
   __syncthreads();
-  const Verdict d = decide<E, WAVES>(a, b, tokens, xt, yt, sums, rows, parts, joined, true);
+  join_rows<WAVES>(a, sums, rows, parts, joined);
+  const Verdict d = decide<E, WAVES>(a, b, tokens, xt, yt, joined, true);
   if (!d.none) draw_held<E, WAVES, HELD>(a, b, d, shared);
 }
 
@@ -602,6 +609,26 @@ __global__ __launch_bounds__(64 * kRestWaves) void verify_rest_kernel(VerifyArgs
     if (lane == 0) out[b * slices + s] = to;
   }
 }
+// Draws from the slices' sums (in LDS), by a wave.
+template <typename E>
+__device__ __forceinline__ void draw_from(const VerifyArgs& a, int64_t b, const Verdict& d, const Rest<E>& r, double* sums, int slices, float number, double ratio,
+                                          bool whole, double ps, double all, int lane) {
+  for (;;) {
+    const Place at = place_of(sums, slices, number, all, lane);
+    const int v = (at.slice * 64 + lane) * E::N;
+    double p[E::N], q[E::N], w[E::N];
+    r.weights(v, p, q);
+    r.rest(v, p, q, ratio, whole, w);
+    const int token = find_in_slice(w, at, lane);
+    if (token >= 0 || !(sums[at.slice] > 0.0)) return write_drawn<E>(a, b, d, ps, token, lane);
+    // (nothing but weights that are none each, and together are one: not a slice to draw from)
+    __builtin_amdgcn_wave_barrier();
+    if (lane == 0) sums[at.slice] = 0.0;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    all = sum_of(sums, slices, lane);
+  }
+}
 // And a workgroup a sequence draws.
 constexpr int kPickWaves = 8;
 template <typename E>
@@ -667,13 +694,120 @@ __global__ __launch_bounds__(64 * kPickWaves) void verify_pick_kernel(VerifyArgs
       __syncthreads();
       continue;
     }
-    if (wave != 0) return;
-    const Place at = place_of(sums, slices, number, all, lane);
-    const int v = (at.slice * 64 + lane) * E::N;
-    double p[E::N], q[E::N], w[E::N];
-    r.weights(v, p, q);
-    r.rest(v, p, q, ratio, whole, w);
-    write_drawn<E>(a, b, d, ps, find_in_slice(w, at, lane), lane);
+    if (wave == 0) draw_from(a, b, d, r, sums, slices, number, ratio, whole, ps, all, lane);
+    return;
+  }
+}
+
+// Rows without a draft, and a few of one that was sure of its tokens, need no ratio: all are summed in 64 bits, slice by slice, and one launch more
+// decides and draws from those sums.  us, this way / in three launches, bf16 where not said: 1 x 1 row of 131072 11.2 / 14.8, 70 x 1 of 89793 16.5 / 22.3,
+// 254 x 1 of 34124 17.3 / 22.4, 64 x 1 of 131072 fp32 20.0 / 30.1, 256 x 1 of 131072 34.7 / 50.4; 1 x 5 of 131072 13.8 / 16.5, 22 x 5 of 42561 16.5 / 17.3,
+// 10 x 16 of 41282 fp32 19.1 / 18.9, 98 x 5 of 39809 27.1 / 26.4, 64 x 9 of 50000 32.7 / 27.2.
+constexpr int64_t kSureElements = 5 << 20;  // of rows of a draft
+struct SliceSum {
+  float m;     // the largest element of the slices that a wave has summed
+  float ones;  // how many of them the slice has
+  double s;    // of the others' weights, in units of its own (NaN where one of these slices holds a NaN or +inf)
+  __device__ __forceinline__ double in_units_of(float most, const Scale& k) const { return m == -INFINITY ? s : (ones + s) * weight(m, most, k); }
+};
+constexpr int kSureSlices = 4;  // a wave
+template <typename E>
+__global__ __launch_bounds__(256) void verify_slices_kernel(VerifyArgs a, int parts, SliceSum* out) {
+  const int lane = threadIdx.x & 63, rows = a.n + 1, slices = slices_of<E>(a.V);
+  const unsigned item = blockIdx.x * 4 + uniform_i(threadIdx.x >> 6), of_seq = static_cast<unsigned>(rows) * parts;
+  const unsigned b = item / of_seq, within = item - b * of_seq;
+  if (b >= static_cast<unsigned>(a.sequences)) return;
+  const int j = static_cast<int>(within / parts), first = (static_cast<int>(within) - j * parts) * kSureSlices;
+  const typename E::type* row = static_cast<const typename E::type*>(a.target) + b * a.target_seq + j * a.target_row;
+  float x[kSureSlices][E::N], most[kSureSlices], m = -INFINITY;
+  const int t = lane < j ? a.tokens[static_cast<int64_t>(b) * a.n + lane] : 0;
+  if (__ballot(static_cast<unsigned>(t) >= static_cast<unsigned>(a.V))) return;  // (a row behind the end of the draft)
+#pragma unroll
+  for (int k = 0; k < kSureSlices; ++k) load_at<E>(row, ((first + k) * 64 + lane) * E::N, a.V, x[k]);
+  bool marked = false;
+#pragma unroll
+  for (int k = 0; k < kSureSlices; ++k) {
+    most[k] = vec_max(x[k]);
+    m = fmaxf(m, most[k]);
+#pragma unroll
+    for (int i = 0; i < E::N; ++i) marked |= !(x[k][i] < INFINITY);
+  }
+  m = wave_max(m);
+  const bool none = __ballot(marked) != 0;
+  const float from = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+  for (int k = 0; k < kSureSlices; ++k) {
+    double s = 0.0;
+    int ones = 0;
+#pragma unroll
+    for (int i = 0; i < E::N; ++i) s += weight(x[k][i], from, a.target_scale);
+    if (__ballot(most[k] == from) != 0) {  // (again, without the largest elements)
+      s = 0.0;
+#pragma unroll
+      for (int i = 0; i < E::N; ++i) {
+        const double w = weight(x[k][i], from, a.target_scale);
+        s += x[k][i] == from ? 0.0 : w;
+        ones += __builtin_popcountll(__ballot(x[k][i] == from));
+      }
+    }
+    s = wave_sum64(s);
+    if (lane == 0 && first + k < slices)
+      out[(static_cast<int64_t>(b) * rows + j) * slices + first + k] = SliceSum{m, static_cast<float>(ones), none ? NAN : m == -INFINITY ? 0.0 : s};
+  }
+}
+constexpr int kSureWaves = 16;
+template <typename E>
+__global__ __launch_bounds__(64 * kSureWaves) void verify_sure_kernel(VerifyArgs a, const SliceSum* in) {
+  __shared__ RowSums joined;
+  __shared__ double sums[kLogitsMaxV / (64 * E::N)];
+  const int lane = threadIdx.x & 63, wave = uniform_i(threadIdx.x >> 6), slices = slices_of<E>(a.V);
+  const int64_t b = blockIdx.x;
+  in += b * (a.n + 1) * slices;
+  const Drafted tokens = drafted_tokens(a, b, lane);
+  const float xt = lane < tokens.count ? target_at<E>(a, b, lane, tokens.t) : 0.0f, number = a.numbers[b * (a.n + 1) + a.n];
+  for (int j = wave; j <= tokens.count; j += kSureWaves) {
+    float m = -INFINITY;
+    for (int s = lane; s < slices; s += 64) m = fmaxf(m, in[j * slices + s].m);
+    m = wave_max(m);
+    double all = 0.0, ones = 0.0;  // (apart, so that what lies beside a near-certain token is not lost in its 1)
+    for (int s = lane; s < slices; s += 64) {
+      const SliceSum part = in[j * slices + s];
+      all += part.m == m ? part.s : part.in_units_of(m, a.target_scale);
+      ones += part.m == m ? part.ones : 0.0f;
+    }
+    all = wave_sum64(all);
+    ones = wave_sum64(ones);
+    if (lane == 0) {
+      joined.m[j] = m;
+      joined.s[j] = ones + all;
+      joined.off[j] = 0.0;
+    }
+  }
+  const Verdict d = decide<E, kSureWaves>(a, b, tokens, xt, 0.0f, joined, true);
+  if (d.none) return;
+  const Rest<E> r(a, b, d);
+  const int own = d.refused < 0 ? -1 : d.refused / (64 * E::N);  // the slice of the token that may not be drawn
+  const double ps = joined.s[d.k];
+  for (bool whole = d.refused < 0;; whole = true) {
+    for (int s = threadIdx.x; s < slices; s += 64 * kSureWaves) {
+      const SliceSum part = in[d.k * slices + s];
+      const double v = part.in_units_of(d.pm, a.target_scale);
+      if (whole || s != own) sums[s] = v > kNoWeight ? v : 0.0;
+    }
+    if (!whole && wave == kSureWaves - 1) {
+      double p[E::N], q[E::N], w[E::N];
+      r.weights((own * 64 + lane) * E::N, p, q);
+      r.rest((own * 64 + lane) * E::N, p, q, 0.0, false, w);
+      const double v = wave_sum64(lane_sum(w));
+      if (lane == 0) sums[own] = v;
+    }
+    __syncthreads();
+    const double all = sum_of(sums, slices, lane);
+    if (!whole && !(all > kNothing * ps)) {  // (the same in every wave)
+      __syncthreads();
+      continue;
+    }
+    if (wave == 0) draw_from(a, b, d, r, sums, slices, number, 0.0, whole, ps, all, lane);
     return;
   }
 }
@@ -686,7 +820,8 @@ __global__ __launch_bounds__(64 * kPickWaves) void verify_pick_kernel(VerifyArgs
 // 52.1, 256 x 5 of 65536 72.0 / 73.6, 128 x 17 of 32001 fp32 70.7 / 73.7.
 struct Plan {
   int rows, parts;
-  int groups;  // workgroups a sequence that sum the row that decides; 0: one workgroup decides and draws; -1: one does everything
+  int groups;  // workgroups a sequence that sum the row that decides; 0: one workgroup decides and draws; -1: one does everything; -2: from sums of all
+               // slices in 64 bits, one decides and draws
   int64_t verdicts, slice_sums, bytes;  // places in the workspace, its size
 };
 template <typename E>
@@ -698,6 +833,12 @@ Plan plan(int32_t sequences, int32_t n, bool drafted, int32_t V) {
   if (p.rows * p.parts <= kSmallItems && slices <= 16 * kHeld) {
     p.groups = -1;
     p.verdicts = p.slice_sums = p.bytes = 0;
+    return p;
+  }
+  if (!drafted && slices > 16 * kHeld && (n == 0 || static_cast<int64_t>(sequences) * p.rows * V <= kSureElements)) {
+    p.groups = -2;
+    p.verdicts = p.slice_sums = 0;
+    p.bytes = static_cast<int64_t>(sequences) * p.rows * slices * static_cast<int64_t>(sizeof(SliceSum));
     return p;
   }
   int64_t groups = 256 / sequences;
@@ -713,10 +854,18 @@ template <typename E>
 int forward(const VerifyArgs& a, void* workspace, hipStream_t stream) {
   auto done = [] { return hipGetLastError() == hipSuccess ? PB_OK : PB_EHIP; };
   const Plan p = plan<E>(a.sequences, a.n, a.draft != nullptr, a.V);
-  if (p.groups < 0) {
+  if (p.groups == -1) {
     if (a.V <= 4 * 64 * E::N) verify_small_kernel<E, 16, 4, 1><<<a.sequences, 1024, 0, stream>>>(a, p.rows, p.parts);
     else if (slices_of<E>(a.V) <= 16) verify_small_kernel<E, 16, 8, 1><<<a.sequences, 1024, 0, stream>>>(a, p.rows, p.parts);
     else verify_small_kernel<E, 16, 8, 2><<<a.sequences, 1024, 0, stream>>>(a, p.rows, p.parts);
+    return done();
+  }
+  if (p.groups == -2) {
+    const int parts = (slices_of<E>(a.V) + kSureSlices - 1) / kSureSlices;
+    SliceSum* slices = static_cast<SliceSum*>(workspace);
+    verify_slices_kernel<E><<<static_cast<unsigned>((static_cast<int64_t>(a.sequences) * p.rows * parts + 3) / 4), 256, 0, stream>>>(a, parts, slices);
+    if (done() != PB_OK) return PB_EHIP;
+    verify_sure_kernel<E><<<a.sequences, 64 * kSureWaves, 0, stream>>>(a, slices);
     return done();
   }
   char* ws = static_cast<char*>(workspace);

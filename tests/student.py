@@ -17,7 +17,8 @@ def probabilities(x, T):
     with np.errstate(over="ignore", under="ignore"):
         z = (x - m) / T
         e = np.exp(z)
-    return e / e.sum(), z - np.log(e.sum()), False
+    ones, rest = (e == 1.0).sum(), e[e < 1.0].sum()  # (apart: a sum of 150000 of them with the 1 among them loses 2^-53 at each of its steps)
+    return e / (ones + rest), z - (np.log(ones) + np.log1p(rest / ones)), False
 
 
 def number(u):
@@ -26,10 +27,12 @@ def number(u):
 
 
 def drawn(r, w):
-    """The first token whose sum up to it passes w times the whole; -1 where there is no mass."""
-    upto = np.cumsum(r)
-    if not upto[-1] > 0:
+    """The first token whose sum up to it passes w times the whole; -1 where there is no mass.  In units of the largest one, so that the sums of
+    equal weights, 1 each, are exact: 75000 of 150000 tokens are not more than 0.5 of them, but 75000 times p, p = 1 / 150000 rounded and the
+    sums rounded 75000 times, may come out as more."""
+    if not r.max() > 0:
         return -1
+    upto = np.cumsum(r / r.max())
     has = (upto > w * upto[-1]) & (r > 0)
     return int(np.argmax(has)) if has.any() else int(np.flatnonzero(r > 0)[-1])
 

@@ -590,6 +590,44 @@ def test_verify_rows_behind_the_end_are_not_read():
     check_verify(got, xv, yv, 1.0, 1.0, tokens, numbers, "ends")
 
 
+@pytest.mark.parametrize("kind", list(KIND))
+@pytest.mark.parametrize("B,n,V", [(1, 0, 393216), (3, 0, 16385), (40, 0, 50001), (2, 1, 131072), (5, 2, 33000), (2, 63, 16390), (1, 4, 393215), (5, 9, 150001), (6, 9, 150001), (300, 0, 17000)])
+def test_verify_long_rows_without_a_draft(kind, B, n, V):
+    """Rows without a draft's, few elements and many: summed in 64 bits at once, or in three steps."""
+    rng = np.random.default_rng(V + n)
+    x, y = rows_for(rng, B, n, V, kind, True)
+    tokens, numbers = tokens_of(rng, x, x[:, :n], True), numbers_of(rng, B, n, True)
+    if n:  # (a token that has all of its row: nothing is left beside it)
+        x[0, 0], tokens[0, 0], numbers[0, 0] = -np.inf, V // 2, 1.0
+        x[0, 0, V // 2] = 1.0
+        x[-1, 0, V // 3], tokens[-1, 0], numbers[-1, 0] = 40.0, V // 3, np.nan
+    T, pad = float(rng.choice([0.5, 1.0, 1.25])), int(rng.choice([0, 3]))
+    bx, px, xv = block(x, kind, V + pad, (n + 1) * (V + pad), int(rng.choice([0, 1])))
+    got = run_verify(px, None, kind, (V + pad, (n + 1) * (V + pad)), (0, 0), B, n, V, T, 1.0, tokens, numbers)
+    check_verify(got, xv, None, T, 1.0, tokens, numbers, (kind, B, n, V))
+
+
+@pytest.mark.parametrize("kind", list(KIND))
+@pytest.mark.parametrize("V", [600, 6000, 40000, 131072])
+@pytest.mark.parametrize("drafted", [False, True, None])
+def test_weights_that_are_none_each(kind, V, drafted):
+    """Thousands of tokens with weights just below those that count, in front of the one that has all: not drawn at a number of 0."""
+    n = 0 if drafted is None else 1
+    x, y = np.full((2, n + 1, V), -np.inf), np.full((2, n, V), -np.inf)
+    x[:, :, :V - 100] = -668.0
+    x[:, :, V - 50] = 0.0
+    x[1, :, V - 70] = -664.0  # (this one counts)
+    if n:
+        y[:, :, V - 10] = 0.0
+    tokens, numbers = np.full((2, n), V - 10), np.zeros((2, n + 1))
+    bx, px, xv = block(x, kind, V, (n + 1) * V)
+    py, yv = None, None
+    if drafted:
+        by, py, yv = block(y, kind, V, n * V)
+    got = run_verify(px, py, kind, (V, (n + 1) * V), (V, n * V), 2, n, V, 1.0, 1.0, tokens, numbers)
+    assert list(got[1]) == [0, 0] and list(got[0][:, 0]) == [V - 50, V - 70]
+
+
 @pytest.mark.parametrize("n,V", [(0, 20000), (1, 600)])
 def test_verify_more_sequences_than_a_launch_takes(n, V):
     B, g = 33000, torch.Generator(device=DEV)
