@@ -259,10 +259,12 @@ __device__ __forceinline__ double row_sum(const typename E::type* x, int V, floa
 template <int WAVES>
 __device__ __forceinline__ void join_rows(const VerifyArgs& a, const Sums* sums, int rows, int parts, RowSums& joined) {
   const int lane = threadIdx.x & 63, wave = uniform_i(threadIdx.x >> 6);
+  const Sums none{-INFINITY, 0.0f, 0.0f, 0.0f};
+  Sums next = wave < rows && lane < parts ? sums[wave * parts + lane] : none;
   for (int j = wave; j < rows; j += WAVES) {  // (rows behind the end of the draft too, whose sums nobody has written and nobody looks at)
     const Scale k = j <= a.n ? a.target_scale : a.draft_scale;
-    Sums part{-INFINITY, 0.0f, 0.0f, 0.0f};
-    if (lane < parts) part = sums[j * parts + lane];
+    Sums part = next;
+    if (j + WAVES < rows && lane < parts) next = sums[(j + WAVES) * parts + lane];
     float m = part.m;
     for (int p = lane + 64; p < parts; p += 64) m = fmaxf(m, sums[j * parts + p].m);
     m = wave_max(m);
@@ -634,6 +636,7 @@ constexpr int kPickWaves = 8;
 template <typename E>
 __global__ __launch_bounds__(64 * kPickWaves) void verify_pick_kernel(VerifyArgs a, const Verdict* verdicts, const Slice* in) {
   __shared__ double sums[kLogitsMaxV / (64 * E::N)], turn[2 * kPickWaves];
+  __shared__ int again;
   const int lane = threadIdx.x & 63, wave = uniform_i(threadIdx.x >> 6), slices = slices_of<E>(a.V);
   constexpr int kMine = (kLogitsMaxV / (64 * E::N) + 64 * kPickWaves - 1) / (64 * kPickWaves);
   const int64_t b = blockIdx.x;
@@ -659,6 +662,7 @@ __global__ __launch_bounds__(64 * kPickWaves) void verify_pick_kernel(VerifyArgs
     turn[wave] = ps;
     turn[kPickWaves + wave] = qs;
   }
+  if (threadIdx.x == 0) again = 0;
   __syncthreads();
   ps = wave_sum64(lane < kPickWaves ? turn[lane] : 0.0);
   qs = wave_sum64(lane < kPickWaves ? turn[kPickWaves + lane] : 0.0);
@@ -677,9 +681,10 @@ __global__ __launch_bounds__(64 * kPickWaves) void verify_pick_kernel(VerifyArgs
         else if (!(mine[k].high < further - bits)) v = NAN;
       }
       if (s < slices) sums[s] = v != v || v > kNoWeight ? v : 0.0;
+      if (s < slices && v != v) again = 1;
     }
     __syncthreads();
-    for (int s = wave; s < slices; s += kPickWaves) {
+    for (int s = wave; s < slices && !whole && again; s += kPickWaves) {
       if (sums[s] == sums[s]) continue;
       const int from = (s * 64 + lane) * E::N;
       double p[E::N], q[E::N], w[E::N];
