@@ -386,7 +386,7 @@ int pb_distill_topk(const void* d_logits, int32_t dtype, int64_t row_stride, int
  * A student of the teacher whose alternatives pb_distill_topk learns from: what its training step needs around that loss, and
  * what a small model beside a large one is for.  Not in the paper.  The conventions are those of the calls on rows of logits:
  * element types enum pb_dtype, strides in elements, any alignment of the elements, the current device, nothing allocated or
- * synchronised, capturable, `d_workspace` as there, the same bits every time.
+ * synchronised, capturable, `d_workspace` as there (what suffices for some tokens or sequences does for fewer), the same bits every time.
  *
  * pb_embed_tokens -- rows of a table for tokens:  d_out[i * out_stride + j] = scale * d_table[d_tokens[i] * table_stride + j], j < dim,
  *   in fp32, rounded once to out_dtype.  A token id outside [0, vocab_size) is absent: its row is 0.

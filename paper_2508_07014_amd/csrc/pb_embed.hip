@@ -140,9 +140,10 @@ constexpr int kManyTokens = 40960;
 constexpr int kSplit = 4096;    // positions of a chunk at most: 12 bits beside those of a token in its range
 // Positions of a chunk, so that the waves that merge them have as many each (67251 x 40 on 193 rows 47.0 -> 41.8 us, 200000 x 64 on
 // 32001 51.6 -> 48.3; always kSplit of them before).
+int64_t turns_for(int n) { return (static_cast<int64_t>(n) + kSortWaves * kSplit - 1) / (kSortWaves * kSplit); }
 int span_for(int n) {
-  const int64_t turns = (static_cast<int64_t>(n) + kSortWaves * kSplit - 1) / (kSortWaves * kSplit);
-  return static_cast<int>(((n + kSortWaves * turns - 1) / (kSortWaves * turns) + 63) / 64 * 64);
+  const int64_t chunks = kSortWaves * turns_for(n);
+  return static_cast<int>(((n + chunks - 1) / chunks + 63) / 64 * 64);
 }
 
 // Workgroups a range: the one with the most frequent token takes longest, and two of them place half the positions each (they count all).  Two /
@@ -688,7 +689,7 @@ int launch_embed_tokens(int table_dtype, int out_dtype, const EmbedArgs& a, hipS
 }
 
 namespace em {
-// What lies where in the workspace.
+// What lies where in the workspace.  Its size does not fall with n: one for many tokens does for fewer.
 struct Layout {
   int64_t begin, order, count, list, pieces, entries, starts, bytes;
 };
@@ -696,15 +697,14 @@ Layout layout(int32_t n, int32_t V, int32_t dim) {
   Layout l;
   l.begin = 0;
   l.order = padded((static_cast<int64_t>(V) + 1) * 4);
-  const int shift = shift_for(n, V), ranges = ((V - 1) >> shift) + 1;
   l.count = l.order + padded(static_cast<int64_t>(n) * 4);
-  l.list = l.count + padded(static_cast<int64_t>(ranges) * 4);
-  l.pieces = l.list + padded((static_cast<int64_t>(ranges) << shift) * static_cast<int64_t>(sizeof(Owner)));
+  l.list = l.count + kMaxRanges * 4;
+  l.pieces = l.list + padded((static_cast<int64_t>(V) + (1 << kMaxShift)) * static_cast<int64_t>(sizeof(Owner)));
   l.bytes = l.pieces + (n > kFew ? padded((static_cast<int64_t>(n) + kFew - 1) / kFew * 2 * dim * 4) : 0);
   l.entries = l.starts = l.pieces;  // (entries and starts are done with before there are pieces)
   if (n >= kManyTokens) {
     l.starts = l.entries + padded(static_cast<int64_t>(n) * 4);
-    l.bytes = std::max(l.bytes, l.starts + padded((static_cast<int64_t>(n) + span_for(n) - 1) / span_for(n) * (ranges + 1) * 4));
+    l.bytes = std::max(l.bytes, l.starts + turns_for(n) * kSortWaves * ((((V - 1) >> shift_for(n, V)) + 2) * 4));
   }
   return l;
 }

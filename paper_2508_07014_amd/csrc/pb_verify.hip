@@ -709,6 +709,7 @@ __global__ __launch_bounds__(64 * kPickWaves) void verify_pick_kernel(VerifyArgs
 // 254 x 1 of 34124 17.3 / 22.4, 64 x 1 of 131072 fp32 20.0 / 30.1, 256 x 1 of 131072 34.7 / 50.4; 1 x 5 of 131072 13.8 / 16.5, 22 x 5 of 42561 16.5 / 17.3,
 // 10 x 16 of 41282 fp32 19.1 / 18.9, 98 x 5 of 39809 27.1 / 26.4, 64 x 9 of 50000 32.7 / 27.2.
 constexpr int64_t kSureElements = 5 << 20;  // of rows of a draft
+constexpr int32_t kHeldTwice = 128;         // sequences up to which no workgroup holds two slices of 16-bit rows a wave
 struct SliceSum {
   float m;     // the largest element of the slices that a wave has summed
   float ones;  // how many of them the slice has
@@ -819,8 +820,8 @@ __global__ __launch_bounds__(64 * kSureWaves) void verify_sure_kernel(VerifyArgs
 
 // How a call is laid out.  us, one launch / two, 16 waves a sequence: 1 x 9 rows of 1024 fp32 8.1 / 9.8, 64 x 17 of 1025 bf16 10.1 / 11.6, 256 x 31 of
 // 1025 12.9 / 17.5, 1 x 17 of 4096 13.1 / 11.9, 256 x 17 of 4096 16.5 / 19.0, 1 x 9 of 8192 14.4 / 13.2, 256 x 9 of 8192 18.7 / 20.9, 64 x 3 of 16384 17.2 /
-// 18.0.  Two launches / three: 8 x 9 rows of 16000 bf16 18.5 / 18.0, 256 x 9 30.5 / 34.1, 64 x 9 of 8000 fp32 18.0 / 19.2; past what the
-// registers of a workgroup hold there are three.  Workgroups a sequence for 256 / 512 in all: 128 x 17 of 131072 bf16 155 /
+// 18.0.  Two launches / three: 1 x 9 rows of 16000 bf16 18.8 / 17.7, 64 x 9 27.6 / 27.3, 128 x 9 30.0 / 29.9, 256 x 9 42.3 / 48.3, 64 x 9 of 8000
+// 18.8 / 22.7, 1 x 9 of 8000 fp32 14.9 / 15.3, 256 x 5 25.2 / 28.2; past what the registers of a workgroup hold there are three.  Workgroups a sequence for 256 / 512 in all: 128 x 17 of 131072 bf16 155 /
 // 149, 200 x 3 of 131072 fp32 139.5 / 134.5, 64 x 3 of 131072 bf16 40.0 / 41.4, 64 x 9 of 50000 without rows of the draft 27.0 / 29.2, 128 x 9 of 50000 51.0 /
 // 52.1, 256 x 5 of 65536 72.0 / 73.6, 128 x 17 of 32001 fp32 70.7 / 73.7.
 struct Plan {
@@ -840,7 +841,8 @@ Plan plan(int32_t sequences, int32_t n, bool drafted, int32_t V) {
     p.verdicts = p.slice_sums = p.bytes = 0;
     return p;
   }
-  if (!drafted && slices > 16 * kHeld && (n == 0 || static_cast<int64_t>(sequences) * p.rows * V <= kSureElements)) {
+  const int held = E::N == 8 && sequences <= kHeldTwice ? 16 : 16 * kHeld;  // slices that one workgroup decides and draws from
+  if (!drafted && slices > held && (n == 0 || static_cast<int64_t>(sequences) * p.rows * V <= kSureElements)) {
     p.groups = -2;
     p.verdicts = p.slice_sums = 0;
     p.bytes = static_cast<int64_t>(sequences) * p.rows * slices * static_cast<int64_t>(sizeof(SliceSum));
@@ -848,7 +850,7 @@ Plan plan(int32_t sequences, int32_t n, bool drafted, int32_t V) {
   }
   int64_t groups = 256 / sequences;
   if (slices >= 256) groups = std::max<int64_t>(groups, std::min(512 / sequences, slices / (4 * kRestWaves)));  // (four slices a wave)
-  p.groups = slices <= 16 * kHeld ? 0 : static_cast<int>(std::min<int64_t>((slices + kRestWaves - 1) / kRestWaves, std::max<int64_t>(1, groups)));
+  p.groups = slices <= held ? 0 : static_cast<int>(std::min<int64_t>((slices + kRestWaves - 1) / kRestWaves, std::max<int64_t>(1, groups)));
   p.verdicts = (static_cast<int64_t>(sequences) * p.rows * p.parts * static_cast<int64_t>(sizeof(Sums)) + 15) / 16 * 16;
   p.slice_sums = p.verdicts + (p.groups > 0 ? (static_cast<int64_t>(sequences) * static_cast<int64_t>(sizeof(Verdict)) + 15) / 16 * 16 : 0);
   p.bytes = p.slice_sums + (p.groups > 0 ? static_cast<int64_t>(sequences) * slices * static_cast<int64_t>(sizeof(Slice)) : 0);
@@ -898,14 +900,16 @@ int32_t verify_draft_slice(int dtype, int32_t n, int32_t V) {
   const int parts = dtype == PB_F32 ? vd::parts_of<lr::F32>(V) : vd::parts_of<lr::F16>(V);
   return static_cast<int32_t>(std::min<int64_t>(32768, 4 * kMostGroups / ((2 * n + 1) * static_cast<int64_t>(parts))));
 }
-// (The size is that of the call with rows of the draft, and without them, whichever is larger: it does not depend on them.)
+// (The size is that of the call with rows of the draft and of that without, whichever is larger, and no less than that of fewer sequences: those
+// that a rule of plan() ends at are asked for too.)
 int64_t verify_draft_workspace(int dtype, int32_t sequences, int32_t n, int32_t V) {
-  const int32_t some = std::min(sequences, verify_draft_slice(dtype, n, V)), last = sequences % std::max(1, some);
-  int64_t most = 0;
-  for (const int32_t count : {some, last})
+  const int32_t most = std::min(sequences, verify_draft_slice(dtype, n, V));
+  const int32_t sure = static_cast<int32_t>(std::min<int64_t>(most, vd::kSureElements / ((n + 1) * static_cast<int64_t>(V))));
+  int64_t bytes = 0;
+  for (const int32_t count : {most, std::min(most, vd::kHeldTwice), sure})
     for (const bool drafted : {false, true})
-      if (count > 0) most = std::max(most, (dtype == PB_F32 ? vd::plan<lr::F32>(count, n, drafted, V) : vd::plan<lr::F16>(count, n, drafted, V)).bytes);
-  return most;
+      if (count > 0) bytes = std::max(bytes, (dtype == PB_F32 ? vd::plan<lr::F32>(count, n, drafted, V) : vd::plan<lr::F16>(count, n, drafted, V)).bytes);
+  return bytes;
 }
 int launch_verify_draft(int dtype, const VerifyArgs& a, void* workspace, hipStream_t stream) {
   return dtype == PB_F32   ? vd::forward<lr::F32>(a, workspace, stream)

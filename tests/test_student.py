@@ -118,6 +118,19 @@ def test_workspaces():
         assert e.value.code == want
 
 
+@pytest.mark.parametrize("V", [1, 129, 1025, 6145, 16000, 32001, 65536, 65537, 131072, 393216])
+def test_workspaces_for_more_do_for_fewer(V):
+    for dim in (1, 64, 2048):
+        counts = sorted({*range(0, 200, 7), *range(4000, 4200, 3), *range(40900, 41100, 3), *range(65400, 65700, 5), *range(130900, 131200, 5), 70000, 200000, 1 << 20, 1 << 24})
+        sizes = [pb.pb_embed_tokens_backward_workspace_bytes(n, V, dim) for n in counts]
+        assert sizes == sorted(sizes), dim
+    for kind in (pb.PB_F32, pb.PB_F16, pb.PB_BF16):
+        for n in (0, 1, 3, 8, 15, 63):
+            sizes = [pb.pb_verify_draft_workspace_bytes(kind, B, n, V) for B in [*range(0, 1400), 5000, 32768, 32769, 40000, 70000]]
+            assert sizes == sorted(sizes), (kind, n)
+
+
+
 # p: pointer, h: handle, l: 64-bit, i: 32-bit, f: float -- the C declarations, written out a second time
 SIGNATURES = dict(pb_embed_tokens="piliifpipil" + "p", pb_embed_tokens_backward="pilpiiifipilpl" + "p", pb_grad_norm="hppl" + "p",
                   pb_grad_clip="hpfh" + "p", pb_verify_draft="ppilllliiiffppppppl" + "p")
