@@ -31,7 +31,7 @@ struct Sums {
   float m, ones, s, at;
 };
 // How far a row's sum s is off at most, relative to itself: each exponent by three roundings (of the difference, of c, of the product),
-// 3 ln 2 |t| 2^-24 of its term, its exponential by 2 x 2^-24, the sum by 13 additions one after the other (3 in a vector, 3 of vectors, the
+// 3 ln 2 |t| 2^-24 of its term, its exponential by 2 x 2^-24, the sum by 13 additions one after the other at most (3 in a vector, 3 of vectors, the
 // edge, 6 in a wave; parts are joined in 64 bits).  The mean of |t| = log2 (1 / e) over the row's probabilities e / s is at most the
 // logarithm of the mean of 1 / e, which is V / s (s >= 1).
 __device__ __forceinline__ double off_by(double s, int V) {
@@ -159,11 +159,15 @@ __device__ __forceinline__ float draft_at(const VerifyArgs& a, int64_t b, int i,
   return E::up((static_cast<const typename E::type*>(a.draft) + b * a.draft_seq + i * a.draft_row)[t]);
 }
 
-// A row is split in parts of 64 kEach vectors, a wave each; at least one.
-constexpr int kEach = 8;
+// A row is split in parts of 64 EACH vectors, a wave each; at least one.  Of 2048 elements (16-bit rows 4096 / 2048 / 1024 us: 32 x 9 of 32001 22.0 / 21.0 /
+// 21.6, 64 x 9 of 50000 without rows of the draft 26.3 / 25.4 / 26.7, 128 x 17 of 131072 146 / 145 / 173; fp32 2048 / 1024: 8 x 9 of 131072 22.7 /
+// 23.1); 64 kSmallEach vectors where one workgroup takes all of a sequence.
 template <typename E>
-__host__ __device__ __forceinline__ int parts_of(int V) {
-  const int parts = (V / E::N + 64 * kEach - 1) / (64 * kEach);
+constexpr int kEach = 32 / E::N;
+constexpr int kSmallEach = 8;
+template <typename E>
+__host__ __device__ __forceinline__ int parts_of(int V, int each) {
+  const int parts = (V / E::N + 64 * each - 1) / (64 * each);
   return parts > 0 ? parts : 1;
 }
 
@@ -182,7 +186,7 @@ __global__ __launch_bounds__(256) void verify_sums_kernel(VerifyArgs a, int rows
   const Row<E> row = row_of<E>(a, b, j);
   float at = 0.0f;
   if (part == 0 && i < tokens.count) at = E::up(row.x[__builtin_amdgcn_readlane(tokens.t, i)]);
-  Sums s = part_sums<E, kEach>(row, part * 64 * kEach, part == 0, j <= a.n ? a.target_scale.c : a.draft_scale.c, lane);
+  Sums s = part_sums<E, kEach<E>>(row, part * 64 * kEach<E>, part == 0, j <= a.n ? a.target_scale.c : a.draft_scale.c, lane);
   s.at = at;
   if (lane == 0) sums[item] = s;
 }
@@ -834,13 +838,14 @@ template <typename E>
 Plan plan(int32_t sequences, int32_t n, bool drafted, int32_t V) {
   Plan p;
   p.rows = drafted ? 2 * n + 1 : n + 1;
-  p.parts = parts_of<E>(V);
+  p.parts = parts_of<E>(V, kSmallEach);
   const int slices = slices_of<E>(V);
   if (p.rows * p.parts <= kSmallItems && slices <= 16 * kHeld) {
     p.groups = -1;
     p.verdicts = p.slice_sums = p.bytes = 0;
     return p;
   }
+  p.parts = parts_of<E>(V, kEach<E>);
   const int held = E::N == 8 && sequences <= kHeldTwice ? 16 : 16 * kHeld;  // slices that one workgroup decides and draws from
   if (!drafted && slices > held && (n == 0 || static_cast<int64_t>(sequences) * p.rows * V <= kSureElements)) {
     p.groups = -2;
@@ -863,8 +868,8 @@ int forward(const VerifyArgs& a, void* workspace, hipStream_t stream) {
   const Plan p = plan<E>(a.sequences, a.n, a.draft != nullptr, a.V);
   if (p.groups == -1) {
     if (a.V <= 4 * 64 * E::N) verify_small_kernel<E, 16, 4, 1><<<a.sequences, 1024, 0, stream>>>(a, p.rows, p.parts);
-    else if (slices_of<E>(a.V) <= 16) verify_small_kernel<E, 16, 8, 1><<<a.sequences, 1024, 0, stream>>>(a, p.rows, p.parts);
-    else verify_small_kernel<E, 16, 8, 2><<<a.sequences, 1024, 0, stream>>>(a, p.rows, p.parts);
+    else if (slices_of<E>(a.V) <= 16) verify_small_kernel<E, 16, kSmallEach, 1><<<a.sequences, 1024, 0, stream>>>(a, p.rows, p.parts);
+    else verify_small_kernel<E, 16, kSmallEach, 2><<<a.sequences, 1024, 0, stream>>>(a, p.rows, p.parts);
     return done();
   }
   if (p.groups == -2) {
@@ -897,7 +902,7 @@ int forward(const VerifyArgs& a, void* workspace, hipStream_t stream) {
 
 // (Sequences are the second dimension of a grid, which holds 65535 at most.)
 int32_t verify_draft_slice(int dtype, int32_t n, int32_t V) {
-  const int parts = dtype == PB_F32 ? vd::parts_of<lr::F32>(V) : vd::parts_of<lr::F16>(V);
+  const int parts = dtype == PB_F32 ? vd::parts_of<lr::F32>(V, vd::kEach<lr::F32>) : vd::parts_of<lr::F16>(V, vd::kEach<lr::F16>);
   return static_cast<int32_t>(std::min<int64_t>(32768, 4 * kMostGroups / ((2 * n + 1) * static_cast<int64_t>(parts))));
 }
 // (The size is that of the call with rows of the draft and of that without, whichever is larger, and no less than that of fewer sequences: those
