@@ -46,7 +46,7 @@ typedef VerifyArgs::Scale Scale;
 // 2^((x - m) c) for x <= m, at least 2^-1000, off by 4e-14 of itself: with n the nearest integer to the exponent (in the low word of
 // the sum with 1.5 2^52) and r what is left, 1 + r P(r), P by interpolation at Chebyshev's nodes, and n added to the exponent: 16
 // instructions in 64 bits, 4 cycles each like those in fp32.  (With rounding, conversion and ldexp as instructions of their own it is 19;
-// all rows of 128 x 17 of 131072 bf16 in these weights took 209 us and 190; in fp32 they take 90.)
+// all rows of 128 x 17 of 131072 bf16 in these weights took 209 us and 190; in fp32 they take 89.)
 __device__ __forceinline__ double weight(float x, float m, const Scale& k) {
   const double d = fmax(static_cast<double>(x) - static_cast<double>(m), k.low);
   const double s = fma(d, k.c, 0x1.8p52), r = fma(d, k.c, -(s - 0x1.8p52));
@@ -171,8 +171,8 @@ __host__ __device__ __forceinline__ int parts_of(int V, int each) {
   return parts > 0 ? parts : 1;
 }
 
-// A wave a part of a row.  Rows behind the end of a draft are not looked at.  Bound by HBM where there are many (128 x 17 rows of 131072 bf16: 90 us,
-// 6.3 TB/s), at 7 instructions an element.
+// A wave a part of a row.  Rows behind the end of a draft are not looked at.  Bound by HBM where there are many (128 x 17 rows of 131072 bf16: 89 us,
+// 6.4 TB/s), at 9 instructions an element.
 template <typename E>
 __global__ __launch_bounds__(256) void verify_sums_kernel(VerifyArgs a, int rows, int parts, Sums* sums) {
   const int lane = threadIdx.x & 63;
@@ -547,7 +547,7 @@ struct Slice {
   double near_p, near_q;    // of p and q over tokens that may lie on either side, which are not among those
   double low, high;         // the least and the largest p / q - ratio of these (none: inf, -inf)
 };
-// Bound by instructions in 64 bits, 46 an element of both rows (128 sequences of 131072: 39 us); few sequences by the chain of reads up to the
+// Bound by instructions in 64 bits, 46 an element of both rows (128 sequences of 131072: 42 us); few sequences by the chain of reads up to the
 // decision and the row behind it (9 us).
 constexpr int kRestWaves = 16;
 template <typename E>
