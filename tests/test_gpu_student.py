@@ -688,24 +688,26 @@ def test_verify_two_calls_at_once():
 
 # ---- graphs, streams, a run of them ------------------------------------------------------------------------------------
 
-def test_captured_and_replayed():
+@pytest.mark.parametrize("n,V,N,rows,dim", [(3, 5000, 3000, 700, 96), (0, 40001, 9000, 9000, 96), (2, 30000, 50000, 70001, 40), (3, 9001, 5000, 20001, 200), (1, 600, 100, 30, 1)])
+def test_captured_and_replayed(n, V, N, rows, dim):
     """Two graphs with a workspace each, replayed in turn with eager calls between them; every replay equals the eager result."""
     rng = np.random.default_rng(2)
-    B, n, V, dim, N = 4, 3, 5000, 96, 3000
+    B = 4
     x, y = rng.normal(0, 2, (B, n + 1, V)), rng.normal(0, 2, (B, n, V))
     X, Y = (torch.from_numpy(a.astype(np.float32)).to(DEV) for a in (x, y))
-    tokens, numbers = dev(y.argmax(axis=2).astype(np.int32)), dev(rng.random((B, n + 1)).astype(np.float32))
-    toks = dev(tokens_for(rng, N, 700, 0.1, 0.2).astype(np.int32))
-    table, grad = torch.randn((700, dim), device=DEV), torch.randn((N, dim), device=DEV)
+    Y = Y if n else None
+    tokens, numbers = dev(y.argmax(axis=2).astype(np.int32)) if n else None, dev(rng.random((B, n + 1)).astype(np.float32))
+    toks = dev(tokens_for(rng, N, rows, 0.1, 0.2).astype(np.int32))
+    table, grad = torch.randn((rows, dim), device=DEV), torch.randn((N, dim), device=DEV)
 
     class Run:
         def __init__(self):
             self.out = torch.zeros((B, n + 1), dtype=torch.int32, device=DEV)
             self.acc, self.lp = torch.zeros(B, dtype=torch.int32, device=DEV), torch.zeros((B, n + 1), device=DEV)
-            self.rows, self.tg, self.norm = torch.zeros((N, dim), device=DEV), torch.zeros((700, dim), device=DEV), torch.zeros(1, device=DEV)
-            self.clipped = torch.zeros((700, dim), device=DEV)
+            self.looked, self.tg, self.norm = torch.zeros((N, dim), device=DEV), torch.zeros((rows, dim), device=DEV), torch.zeros(1, device=DEV)
+            self.clipped = torch.zeros((rows, dim), device=DEV)
             self.set, self.to = (pb.pb_tensors_build([t], [t.numel()], [pb.PB_F32]) for t in (self.tg, self.clipped))
-            sizes = (pb.pb_verify_draft_workspace_bytes(pb.PB_F32, B, n, V), pb.pb_embed_tokens_backward_workspace_bytes(N, 700, dim),
+            sizes = (pb.pb_verify_draft_workspace_bytes(pb.PB_F32, B, n, V), pb.pb_embed_tokens_backward_workspace_bytes(N, rows, dim),
                      pb.pb_grad_norm_workspace_bytes(self.set))
             self.ws = [workspace(s, 0) for s in sizes]
 
@@ -713,13 +715,13 @@ def test_captured_and_replayed():
             s = int(torch.cuda.current_stream().cuda_stream)
             pb.pb_verify_draft(X, Y, pb.PB_F32, (n + 1) * V, V, n * V, V, B, n, V, 1.0, 1.0, tokens, numbers, self.out, self.acc, self.lp, self.ws[0],
                                self.ws[0].numel(), s)
-            pb.pb_embed_tokens(table, pb.PB_F32, dim, 700, dim, 0.5, toks, N, self.rows, pb.PB_F32, dim, s)
-            pb.pb_embed_tokens_backward(grad, pb.PB_F32, dim, toks, N, 700, dim, 0.5, 0, self.tg, pb.PB_F32, dim, self.ws[1], self.ws[1].numel(), s)
+            pb.pb_embed_tokens(table, pb.PB_F32, dim, rows, dim, 0.5, toks, N, self.looked, pb.PB_F32, dim, s)
+            pb.pb_embed_tokens_backward(grad, pb.PB_F32, dim, toks, N, rows, dim, 0.5, 0, self.tg, pb.PB_F32, dim, self.ws[1], self.ws[1].numel(), s)
             pb.pb_grad_norm(self.set, self.norm, self.ws[2], self.ws[2].numel(), s)
             pb.pb_grad_clip(self.set, self.norm, 1.0, self.to, s)
 
         def results(self):
-            return [t.clone() for t in (self.out, self.acc, self.lp, self.rows, self.tg, self.norm, self.clipped)]
+            return [t.clone() for t in (self.out, self.acc, self.lp, self.looked, self.tg, self.norm, self.clipped)]
 
     eager, runs, graphs = Run(), [Run(), Run()], []
     for r in runs:
