@@ -605,58 +605,110 @@ __global__ __launch_bounds__(kJoinThreads) void embed_join_kernel(SumArgs s, Own
 // held from the count of the positions to their list; LOOP: read again for that, TURNS at a time.
 constexpr int kSmallTokens = 16384;
 static_assert(kSmallTokens <= 65536, "positions in 16 bits");
-template <typename G, typename T, int TURNS, bool LOOP, bool NARROW>
-__global__ __launch_bounds__(256) void embed_small_kernel(SumArgs s) {
-  constexpr int K = step_of<G, T>();
-  __shared__ unsigned short list[LOOP ? kSmallTokens : 256 * TURNS];
-  __shared__ int found[4];
-  __shared__ float shares[256 * K];
-  const EmbedGradArgs& a = s.a;
-  const int tid = threadIdx.x, v = blockIdx.x, wave = uniform_i(tid >> 6), lane64 = tid & 63;
-  const int turns = (a.n + 255) / 256, p0 = wave * turns * 64 + lane64;
-  int t[TURNS], count = 0;
-  auto request = [&](int from) {
+template <int K, int TURNS, bool LOOP>
+struct SmallShared {
+  unsigned short list[LOOP ? kSmallTokens : 256 * TURNS];
+  int found[4];
+  float shares[256 * K];
+};
+// A wave's tokens from turn `from` on.
+template <int TURNS>
+__device__ __forceinline__ void request_tokens(const EmbedGradArgs& a, int turns, int p0, int from, int (&t)[TURNS]) {
 #pragma unroll
-    for (int k = 0; k < TURNS; ++k) t[k] = from + k < turns && p0 + 64 * (from + k) < a.n ? a.tokens[p0 + 64 * (from + k)] : -1;
-  };
+  for (int k = 0; k < TURNS; ++k) t[k] = from + k < turns && p0 + 64 * (from + k) < a.n ? a.tokens[p0 + 64 * (from + k)] : -1;
+}
+// Token v's row of the gradient, by the workgroup; t: its tokens (of the first turns, where there are more than TURNS of them).
+template <typename G, typename T, int TURNS, bool LOOP, int K, bool NARROW>
+__device__ __forceinline__ void sum_token(const SumArgs& s, int v, const Columns<K, 1, NARROW>& cols, int (&t)[TURNS], int turns, int p0, SmallShared<K, TURNS, LOOP>& sh) {
+  const EmbedGradArgs& a = s.a;
+  const int tid = threadIdx.x, wave = uniform_i(tid >> 6), lane64 = tid & 63;
+  int count = 0;
   for (int from = 0; from < (LOOP ? turns : 1); from += TURNS) {
-    request(from);
+    if (LOOP && from > 0) request_tokens(a, turns, p0, from, t);
 #pragma unroll
     for (int k = 0; k < TURNS; ++k) count += __builtin_popcountll(__ballot(t[k] == v));
   }
-  if (lane64 == 0) found[wave] = count;
+  if (lane64 == 0) sh.found[wave] = count;
   __syncthreads();
   int at = 0;
-  for (int w = 0; w < wave; ++w) at += found[w];
+  for (int w = 0; w < wave; ++w) at += sh.found[w];
   if (count > 0) {
     for (int from = 0; from < (LOOP ? turns : 1); from += TURNS) {
-      if (LOOP) request(from);
+      if (LOOP) request_tokens(a, turns, p0, from, t);
 #pragma unroll
       for (int k = 0; k < TURNS; ++k) {
         const u64 here = __ballot(t[k] == v);
-        if (t[k] == v) list[at + __builtin_popcountll(here & ((1ull << lane64) - 1))] = static_cast<unsigned short>(p0 + 64 * (from + k));
+        if (t[k] == v) sh.list[at + __builtin_popcountll(here & ((1ull << lane64) - 1))] = static_cast<unsigned short>(p0 + 64 * (from + k));
         at += __builtin_popcountll(here);
       }
     }
   }
-  count = found[0] + found[1] + found[2] + found[3];
+  count = sh.found[0] + sh.found[1] + sh.found[2] + sh.found[3];
   if (count == 0 && a.accumulate) return;
   __syncthreads();
   const int lane = tid & (s.lanes - 1), group = tid / s.lanes, groups = 256 / s.lanes;
   const int share = max(8, (count + groups - 1) / groups);
-  const Columns<K, 1, NARROW> cols(a.dim, blockIdx.y * s.lanes * K, s.lanes, lane);
   float sum[1][K] = {};
-  sum_positions<G>(a, list, cols, group * share, min(count, (group + 1) * share), sum);
+  sum_positions<G>(a, sh.list, cols, group * share, min(count, (group + 1) * share), sum);
   if (count > share) {
 #pragma unroll
-    for (int e = 0; e < K; ++e) shares[e * 256 + tid] = sum[0][e];
+    for (int e = 0; e < K; ++e) sh.shares[e * 256 + tid] = sum[0][e];
     __syncthreads();
     if (group == 0)
       for (int q = 1; q * share < count; ++q)
 #pragma unroll
-        for (int e = 0; e < K; ++e) sum[0][e] += shares[e * 256 + q * s.lanes + lane];
+        for (int e = 0; e < K; ++e) sum[0][e] += sh.shares[e * 256 + q * s.lanes + lane];
   }
   if (group == 0) write_columns<T>(a, cols, v, sum);
+}
+template <typename G, typename T, int TURNS, bool LOOP, bool NARROW>
+__global__ __launch_bounds__(256) void embed_small_kernel(SumArgs s) {
+  constexpr int K = step_of<G, T>();
+  __shared__ SmallShared<K, TURNS, LOOP> sh;
+  const int turns = (s.a.n + 255) / 256, p0 = uniform_i(threadIdx.x >> 6) * turns * 64 + (threadIdx.x & 63);
+  int t[TURNS];
+  request_tokens(s.a, turns, p0, 0, t);
+  const Columns<K, 1, NARROW> cols(s.a.dim, blockIdx.y * s.lanes * K, s.lanes, threadIdx.x & (s.lanes - 1));
+  sum_token<G, T, TURNS, LOOP>(s, blockIdx.x, cols, t, turns, p0, sh);
+}
+
+// Few tokens on a large table, all in one launch: a workgroup takes some rows (and a vector of their columns), most of which no token has.  us, so / in
+// three launches, fp32: 88 tokens, 44224 x 320 bf16 8.9 / 17.4; 500, 32001 x 640 18.3 / 23.2; 1000, 8192 x 256 7.9 / 12.4, 32001 x 256 9.1 / 16.1, 65000 x 256
+// 13.8 / 21.5, 131072 x 64 10.5 / 17.1; all of them one token, 32001 x 256 16.0 / 17.4.  2000: 32001 x 256 11.9 / 16.6, but where they are one
+// token 29 / 16.  Rows a workgroup, 8 / 16 / 32: 1000, 8192 x 256 7.9 / 10.1 / -, 32001 x 256 10.1 / 9.1 / 9.2, 131072 x 64 19.9 / 13.6 / 10.5.
+constexpr int kFewTokens = 1024;
+int few_rows(int V) { return V <= 8 * 2048 ? 8 : V <= 16 * 2048 ? 16 : 32; }
+template <typename G, typename T>
+__global__ __launch_bounds__(256) void embed_few_kernel(SumArgs s, int rows) {
+  constexpr int K = step_of<G, T>(), TURNS = kFewTokens / 256;
+  __shared__ SmallShared<K, TURNS, false> sh;
+  __shared__ unsigned occur;
+  const EmbedGradArgs& a = s.a;
+  const int turns = (a.n + 255) / 256, p0 = uniform_i(threadIdx.x >> 6) * turns * 64 + (threadIdx.x & 63);
+  const int v0 = blockIdx.x * rows, size = min(rows, a.V - v0);
+  int t[TURNS];
+  request_tokens(a, turns, p0, 0, t);
+  if (threadIdx.x == 0) occur = 0;
+  __syncthreads();
+  unsigned mine = 0;
+#pragma unroll
+  for (int k = 0; k < TURNS; ++k) {
+    const unsigned u = static_cast<unsigned>(t[k]) - static_cast<unsigned>(v0);
+    mine |= u < static_cast<unsigned>(size) ? 1u << u : 0u;
+  }
+  if (mine != 0) atomicOr(&occur, mine);
+  __syncthreads();
+  const unsigned has = occur;
+  const Columns<K, 1, false> cols(a.dim, blockIdx.y * s.lanes * K, s.lanes, threadIdx.x & (s.lanes - 1));
+  if (!a.accumulate) {
+    const float zero[K] = {};
+    for (int r = threadIdx.x / s.lanes; r < size; r += 256 / s.lanes)
+      if (!((has >> r) & 1u)) cols.template store<T>(static_cast<typename T::type*>(a.table_grad) + (v0 + r) * a.table_stride, 0, zero);
+  }
+  for (unsigned left = has; left != 0; left &= left - 1) {
+    sum_token<G, T, TURNS, false>(s, v0 + __builtin_ctz(left), cols, t, turns, p0, sh);
+    __syncthreads();
+  }
 }
 
 template <typename Do>
@@ -719,12 +771,13 @@ struct Shape {
   int lanes, vectors;
   explicit Shape(int dim) : lanes(lanes_for(dim, K)), vectors((dim + lanes * K - 1) / (lanes * K)) {}
 };
-// us, in one launch / in three, fp32 where not said: 500 tokens, 1025 x 640 5.7 / 12.4; 2000, 4096 x 64 9.1 / 14.0, 8192 x 64 15.2 / 14.1; 2900, 6000 x 64
-// 12.2 / 13.9; 4096, 4096 x 64 10.0 / 14.8, 1025 x 640 12.7 / 17.0, 8192 x 512 bf16 21.6 / 16.3; 5000, 4096 x 64 19.7 / 16.7; 8192, 2048 x 64 15.1 / 17.7;
-// 16384, 166 x 64 18.4 / 21.3, 1025 x 64 17.4 / 20.1; and, where a token of many positions has few groups of lanes for them, 8192, 300 x 512 bf16
-// 17.4 / 17.8, 300 x 1024 bf16 27.1 / 23.7; 16384, 166 x 2048 71 / 51.
+// us, a workgroup a token / in three launches, fp32 where not said: 500 tokens, 1025 x 640 5.7 / 12.4; 2000, 4096 x 64 9.1 / 14.0, 8192 x 64 15.2 / 14.1;
+// 2900, 6000 x 64 12.2 / 13.9; 4096, 4096 x 64 10.0 / 14.8, 1025 x 640 12.7 / 17.0, 8192 x 512 bf16 21.6 / 16.3; 5000, 4096 x 64 19.7 / 16.7; 8192, 2048 x 64
+// 15.1 / 17.7; 16384, 166 x 64 18.4 / 21.3, 1025 x 64 17.4 / 20.1; and, where a token of many positions has few groups of lanes for them, 8192, 300 x 512
+// bf16 17.4 / 17.8, 300 x 1024 bf16 27.1 / 23.7; 16384, 166 x 2048 71 / 51.  Few tokens, a workgroup a token / some rows: 1000, 2048 x 64 4.7 / 9.9, 4096 x 64
+// 6.6 / 10.2, 3000 x 512 8.9 / 7.1, 6000 x 64 8.6 / 6.3; 300, 6000 x 64 7.8 / 4.6.
 bool small(int64_t n, int64_t V, int lanes, int vectors) {
-  return n <= kSmallTokens && n * lanes <= 4096 * 64 && V * vectors <= 6144 && V * vectors * n <= 17 << 20;
+  return n <= kSmallTokens && n * lanes <= 4096 * 64 && V * vectors <= (n <= kFewTokens ? 4608 : 6144) && V * vectors * n <= 17 << 20;
 }
 
 template <typename G, typename T>
@@ -745,6 +798,11 @@ int backward(const EmbedGradArgs& a, char* ws, hipStream_t stream) {
     if (a.n <= 1024) return go(embed_small_kernel<G, T, 4, false, false>);
     if (a.n <= 4096) return go(embed_small_kernel<G, T, 16, false, false>);
     return go(embed_small_kernel<G, T, 16, true, false>);
+  }
+  if (a.n <= kFewTokens && a.dim >= K) {  // (narrower rows are seldom: three launches)
+    const int rows = few_rows(a.V);
+    embed_few_kernel<G, T><<<dim3((a.V + rows - 1) / rows, vectors), 256, 0, stream>>>(s, rows);
+    return done();
   }
   const int shift = shift_for(a.n, a.V), ranges = ((a.V - 1) >> shift) + 1, stretches = (a.n + kFew - 1) / kFew;
   const size_t counts = static_cast<size_t>(kSortWaves) * 4 << shift;

@@ -132,6 +132,15 @@ def test_table_gradient_of_large_tables(n, V, dim, hot):
         check_backward(rng, n, V, dim, kind, tkind, 0.1, hot, accumulate, (n, V, dim, kind))
 
 
+@pytest.mark.parametrize("n,V,dim,hot", [(1024, 4609, 64, 0.1), (1025, 4609, 64, 0.1), (1024, 6145, 8, 1.0), (1, 32769, 130, 0.0), (0, 20000, 9, 0.0), (1000, 16384, 257, 0.0), (1000, 16385, 12, 0.3),
+                                         (700, 32768, 300, 0.05), (257, 40007, 1030, 0.0), (256, 131072, 8, 0.9), (1023, 393216, 16, 0.0), (300, 2400, 700, 0.2), (64, 9001, 7, 0.0), (64, 9001, 3, 0.0)])
+def test_table_gradient_of_few_tokens(n, V, dim, hot):
+    """One launch whose workgroups take some rows each."""
+    rng = np.random.default_rng(n + V)
+    for kind, tkind, accumulate in (("f32", "f32", 1), ("bf16", "f32", 0), ("f16", "bf16", 0), ("bf16", "bf16", 1)):
+        check_backward(rng, n, V, dim, kind, tkind, 0.1, hot, accumulate, (n, V, dim, kind))
+
+
 def test_table_gradient_of_runs():
     """Tokens in runs whose lengths lie around the lengths that are summed at once: ends of runs on and beside every border."""
     rng = np.random.default_rng(9)
