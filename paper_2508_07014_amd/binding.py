@@ -580,6 +580,8 @@ def pb_grad_norm(grads: Tensors, d_norm, d_workspace, workspace_bytes: int, stre
 
 
 def pb_grad_clip(grads: Tensors, d_norm, max_norm: float, out: Optional[Tensors] = None, stream: int = 0):
+    if out is not None and not out.handle:  # (closed: without an address the call would clip in place)
+        raise PbError(PB_EINVAL, "pb_grad_clip")
     _check((_student or _load_student()).pb_grad_clip(
         grads.handle, d_norm, max_norm, None if out is None else out.handle, stream), "pb_grad_clip")
 
