@@ -446,9 +446,10 @@ int pb_grad_clip(const pb_tensors* grads, const float* d_norm, float max_norm, c
  * d_accepted[b] = k; d_tokens[b, 0 .. n_draft] = t_0 .. t_k-1, the drawn token, then -1; d_logp (NULL: not wanted) the log p_i of
  * those tokens, NaN beside -1.  n_draft == 0 draws a token from each row.
  * What decides is in 64 bits, so that a draw from hundreds of thousands of tokens, or a number next to p / q, is the definition's; the
- * log p of accepted tokens come from sums in fp32 or better of what lies beside a row's largest logit.  A logit of -inf
- * has p = 0, as has one whose p / p_max is below 2^-960 (q likewise).  A row of nothing but -inf: p = 0, no token is accepted there, and
- * none drawn (-1); as a y_i: q = 0.  A row that holds a NaN or +inf accepts nothing; where it decides (x_k, or y_k if k < n) the drawn
+ * log p come from sums in fp32 or better of what lies beside a row's largest logit, apart from its own 1, so that a near-certain
+ * token's is as near relative to itself (in fp32 weights below 2^-126 of the largest are none).  A logit of -inf has p = 0, as has one
+ * whose p / p_max is below 2^-960 (q likewise).  A row of nothing but -inf: p = 0, no token is accepted there, and none
+ * drawn (-1); as a y_i: q = 0.  A row that holds a NaN or +inf accepts nothing; where it decides (x_k, or y_k if k < n) the drawn
  * token is -1.
  * PB_EINVAL: as in pb_token_logprobs, n_draft < 0, d_draft_tokens that is null though n_draft > 0 or is not though it is 0, draft
  *   rows though n_draft is 0, a null d_uniforms, d_tokens or d_accepted, a stride below V (the draft's where it has rows).  PB_ERANGE: a temperature outside [1e-4, 1e4].

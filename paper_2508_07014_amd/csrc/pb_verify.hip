@@ -38,6 +38,7 @@ __device__ __forceinline__ double off_by(double s, int V) {
   return static_cast<double>((2.1f * __builtin_amdgcn_logf(static_cast<float>(V) / static_cast<float>(s)) + 17.0f) * 0x1p-24f);
 }
 constexpr double kBeside = 0x1p-34;      // products of two such bounds, and what the sums in 64 bits are off by
+constexpr double kSmallBeside = 0x1p-20; // of a row's weight beside its largest element, apart from which it is kept below this
 constexpr double kNothing = 0x1p-40;     // a rest of the target's mass below this is none (equal rows differ by their roundings)
 constexpr double kNoWeight = 0x1p-960;   // weights below this, masked tokens' among them, are none
 
@@ -200,13 +201,20 @@ struct Verdict {
   double ratio;    // of their sums, about
   double near;     // how far that is off at most, relative to itself
 };
+struct LeftVerdict {  // for the next launch
+  Verdict d;
+  double beside;  // of the target's row, as in RowSums
+};
 
 constexpr int kMaxRows = 2 * kMaxDrafts + 1;
 struct RowSums {
   float m[kMaxRows];
   double s[kMaxRows];
-  double off[kMaxRows];  // relative
-  double turn[16];       // a place a wave
+  double off[kMaxRows];     // how far s is off at most, relative to itself
+  double turn[16];          // a place a wave
+  // Where s is 1 and less than kSmallBeside, this; else no less than that.  (Behind the others: decide() takes 8 registers more with it among them,
+  // and a workgroup of 1024 threads then leaves no room for the next one's first waves: 128 x 17 rows of 131072 bf16 137 -> 140 us.)
+  double beside[kMaxRows];
 };
 
 __device__ __forceinline__ double share(float x, float m, double s, const Scale& k) {  // (a row of nothing but -inf: s = 0; a marked one: NaN)
@@ -214,8 +222,11 @@ __device__ __forceinline__ double share(float x, float m, double s, const Scale&
   const double w = weight(x, m, k);
   return (w > kNoWeight ? w : 0.0) / s;
 }
-__device__ __forceinline__ float log_share(float x, float m, double s, double c) {
-  return static_cast<float>(((static_cast<double>(x) - static_cast<double>(m)) * c - log2(s)) * 0.69314718055994530942);
+// (Next to a near-certain token, the others' weight is all of the logarithm, and would be lost in a sum with its 1: log(1 + r) is r - r^2 / 2
+// within 2^-40 of itself.  From kSmallBeside on what a sum in 64 bits keeps of it is nearer than the fp32 sums of long rows' parts.)
+__device__ __forceinline__ float log_share(float x, float m, double s, double beside, double c) {
+  const double all = beside < kSmallBeside ? fma(-0.5 * beside, beside, beside) : log2(s) * 0.69314718055994530942;
+  return static_cast<float>((static_cast<double>(x) - static_cast<double>(m)) * c * 0.69314718055994530942 - all);
 }
 
 // Elements v .. v + N - 1 of a row of V; -inf past it.
@@ -279,8 +290,18 @@ __device__ __forceinline__ void join_rows(const VerifyArgs& a, const Sums* sums,
                                : (static_cast<double>(part.ones) + static_cast<double>(part.s)) * weight(part.m, m, k);
     }
     s = wave_sum64(s);
+    double beside = s;
+    if (s < kSmallBeside + 1.0) {  // (again, without the largest element)
+      beside = 0.0;
+      for (int p = lane; p < parts; p += 64) {
+        part = sums[j * parts + p];
+        beside += part.m == m || part.m == -INFINITY ? static_cast<double>(part.s) : (static_cast<double>(part.ones) + static_cast<double>(part.s)) * weight(part.m, m, k);
+      }
+      beside = wave_sum64(beside);
+    }
     if (lane == 0) {
       joined.m[j] = m;
+      joined.beside[j] = beside;
       joined.s[j] = s;
       joined.off[j] = off_by(s, a.V);
     }
@@ -340,7 +361,7 @@ __device__ __forceinline__ Verdict decide(const VerifyArgs& a, int64_t b, const 
   if (writes && wave == WAVES - 1) {
     if (lane <= a.n && (lane != r.k || r.none)) {  // (the token at k is drawn later)
       a.out[b * (a.n + 1) + lane] = lane < r.k ? t : -1;
-      if (a.logp) a.logp[b * (a.n + 1) + lane] = lane < r.k ? log_share(xt, joined.m[lane], joined.s[lane], a.target_scale.c) : NAN;
+      if (a.logp) a.logp[b * (a.n + 1) + lane] = lane < r.k ? log_share(xt, joined.m[lane], joined.s[lane], joined.beside[lane], a.target_scale.c) : NAN;
     }
     if (lane == 0) a.accepted[b] = r.k;
   }
@@ -444,11 +465,11 @@ __device__ __forceinline__ int find_in_slice(const double (&w)[N], const Place& 
 }
 
 template <typename E>
-__device__ __forceinline__ void write_drawn(const VerifyArgs& a, int64_t b, const Verdict& d, double ps, int token, int lane) {
+__device__ __forceinline__ void write_drawn(const VerifyArgs& a, int64_t b, const Verdict& d, double ps, double beside, int token, int lane) {
   if (lane != 0) return;
   const int64_t at = b * (a.n + 1) + d.k;
   a.out[at] = token;
-  if (a.logp) a.logp[at] = token < 0 ? NAN : log_share(target_at<E>(a, b, d.k, token), d.pm, ps, a.target_scale.c);
+  if (a.logp) a.logp[at] = token < 0 ? NAN : log_share(target_at<E>(a, b, d.k, token), d.pm, ps, beside, a.target_scale.c);
 }
 
 // Rows of up to WAVES * HELD slices: a workgroup a sequence holds the rows that decide in registers.
@@ -458,7 +479,7 @@ struct DrawShared {
   double p[WAVES], q[WAVES], slices[WAVES * kHeld];
 };
 template <typename E, int WAVES, int HELD>
-__device__ __forceinline__ void draw_held(const VerifyArgs& a, int64_t b, const Verdict& d, DrawShared<WAVES>& shared) {
+__device__ __forceinline__ void draw_held(const VerifyArgs& a, int64_t b, const Verdict& d, const RowSums& joined, DrawShared<WAVES>& shared) {
   const int lane = threadIdx.x & 63, wave = uniform_i(threadIdx.x >> 6), slices = slices_of<E>(a.V);
   const float number = a.numbers[b * (a.n + 1) + a.n];
   const Rest<E> r(a, b, d);
@@ -499,7 +520,7 @@ __device__ __forceinline__ void draw_held(const VerifyArgs& a, int64_t b, const 
     const Place at = place_of(shared.slices, slices, number, all, lane);
 #pragma unroll
     for (int h = 0; h < HELD; ++h)
-      if (at.slice == wave + h * WAVES) write_drawn<E>(a, b, d, ps, find_in_slice(w[h], at, lane), lane);
+      if (at.slice == wave + h * WAVES) write_drawn<E>(a, b, d, ps, joined.beside[d.k], find_in_slice(w[h], at, lane), lane);
     return;
   }
 }
@@ -509,7 +530,7 @@ __global__ __launch_bounds__(64 * WAVES) void verify_draw_kernel(VerifyArgs a, i
   __shared__ DrawShared<WAVES> shared;
   const int64_t b = blockIdx.x;
   const Verdict d = decide_rows<E, WAVES>(a, b, sums, rows, parts, joined, true);
-  if (!d.none) draw_held<E, WAVES, HELD>(a, b, d, shared);
+  if (!d.none) draw_held<E, WAVES, HELD>(a, b, d, joined, shared);
 }
 
 // All of a sequence in one workgroup, where its rows have few parts.
@@ -536,7 +557,7 @@ __global__ __launch_bounds__(64 * WAVES) void verify_small_kernel(VerifyArgs a, 
   __syncthreads();
   join_rows<WAVES>(a, sums, rows, parts, joined);
   const Verdict d = decide<E, WAVES>(a, b, tokens, xt, yt, joined, true);
-  if (!d.none) draw_held<E, WAVES, HELD>(a, b, d, shared);
+  if (!d.none) draw_held<E, WAVES, HELD>(a, b, d, joined, shared);
 }
 
 // Long rows: several workgroups a sequence decide, each for itself, and sum their slices; the first leaves the verdict.
@@ -551,12 +572,12 @@ struct Slice {
 // decision and the row behind it (9 us).
 constexpr int kRestWaves = 16;
 template <typename E>
-__global__ __launch_bounds__(64 * kRestWaves) void verify_rest_kernel(VerifyArgs a, int rows, int parts, const Sums* sums, Verdict* verdicts, Slice* out) {
+__global__ __launch_bounds__(64 * kRestWaves) void verify_rest_kernel(VerifyArgs a, int rows, int parts, const Sums* sums, LeftVerdict* verdicts, Slice* out) {
   __shared__ RowSums joined;
   const int lane = threadIdx.x & 63, wave = uniform_i(threadIdx.x >> 6), slices = slices_of<E>(a.V);
   const int64_t b = blockIdx.y;
   const Verdict d = decide_rows<E, kRestWaves>(a, b, sums, rows, parts, joined, blockIdx.x == 0);
-  if (blockIdx.x == 0 && threadIdx.x == 0) verdicts[b] = d;
+  if (blockIdx.x == 0 && threadIdx.x == 0) verdicts[b] = LeftVerdict{d, joined.beside[d.k]};
   if (d.none) return;
   const Rest<E> r(a, b, d);
   for (int s = blockIdx.x * kRestWaves + wave; s < slices; s += gridDim.x * kRestWaves) {
@@ -618,7 +639,7 @@ __global__ __launch_bounds__(64 * kRestWaves) void verify_rest_kernel(VerifyArgs
 // Draws from the slices' sums (in LDS), by a wave.
 template <typename E>
 __device__ __forceinline__ void draw_from(const VerifyArgs& a, int64_t b, const Verdict& d, const Rest<E>& r, double* sums, int slices, float number, double ratio,
-                                          bool whole, double ps, double all, int lane) {
+                                          bool whole, double ps, double beside, double all, int lane) {
   for (;;) {
     const Place at = place_of(sums, slices, number, all, lane);
     const int v = (at.slice * 64 + lane) * E::N;
@@ -626,7 +647,7 @@ __device__ __forceinline__ void draw_from(const VerifyArgs& a, int64_t b, const 
     r.weights(v, p, q);
     r.rest(v, p, q, ratio, whole, w);
     const int token = find_in_slice(w, at, lane);
-    if (token >= 0 || !(sums[at.slice] > 0.0)) return write_drawn<E>(a, b, d, ps, token, lane);
+    if (token >= 0 || !(sums[at.slice] > 0.0)) return write_drawn<E>(a, b, d, ps, beside, token, lane);
     // (nothing but weights that are none each, and together are one: not a slice to draw from)
     __builtin_amdgcn_wave_barrier();
     if (lane == 0) sums[at.slice] = 0.0;
@@ -638,7 +659,7 @@ __device__ __forceinline__ void draw_from(const VerifyArgs& a, int64_t b, const 
 // And a workgroup a sequence draws.
 constexpr int kPickWaves = 8;
 template <typename E>
-__global__ __launch_bounds__(64 * kPickWaves) void verify_pick_kernel(VerifyArgs a, const Verdict* verdicts, const Slice* in) {
+__global__ __launch_bounds__(64 * kPickWaves) void verify_pick_kernel(VerifyArgs a, const LeftVerdict* verdicts, const Slice* in) {
   __shared__ double sums[kLogitsMaxV / (64 * E::N)], turn[2 * kPickWaves];
   __shared__ int again;
   const int lane = threadIdx.x & 63, wave = uniform_i(threadIdx.x >> 6), slices = slices_of<E>(a.V);
@@ -653,7 +674,7 @@ __global__ __launch_bounds__(64 * kPickWaves) void verify_pick_kernel(VerifyArgs
     mine[k] = s < slices ? in[s] : Slice{0.0, 0.0, 0.0, 0.0, 0.0, 0.0, INFINITY, -INFINITY};
   }
   const float number = a.numbers[b * (a.n + 1) + a.n];
-  const Verdict d = verdicts[b];
+  const Verdict d = verdicts[b].d;
   if (d.none) return;  // (and nothing was summed)
 #pragma unroll
   for (int k = 0; k < kMine; ++k) {
@@ -703,7 +724,7 @@ __global__ __launch_bounds__(64 * kPickWaves) void verify_pick_kernel(VerifyArgs
       __syncthreads();
       continue;
     }
-    if (wave == 0) draw_from(a, b, d, r, sums, slices, number, ratio, whole, ps, all, lane);
+    if (wave == 0) draw_from(a, b, d, r, sums, slices, number, ratio, whole, ps, verdicts[b].beside, all, lane);
     return;
   }
 }
@@ -779,7 +800,7 @@ __global__ __launch_bounds__(64 * kSureWaves) void verify_sure_kernel(VerifyArgs
     float m = -INFINITY;
     for (int s = lane; s < slices; s += 64) m = fmaxf(m, in[j * slices + s].m);
     m = wave_max(m);
-    double all = 0.0, ones = 0.0;  // (apart, so that what lies beside a near-certain token is not lost in its 1)
+    double all = 0.0, ones = 0.0;  // (see log_share)
     for (int s = lane; s < slices; s += 64) {
       const SliceSum part = in[j * slices + s];
       all += part.m == m ? part.s : part.in_units_of(m, a.target_scale);
@@ -789,6 +810,7 @@ __global__ __launch_bounds__(64 * kSureWaves) void verify_sure_kernel(VerifyArgs
     ones = wave_sum64(ones);
     if (lane == 0) {
       joined.m[j] = m;
+      joined.beside[j] = ones > 1.0 ? ones : all;
       joined.s[j] = ones + all;
       joined.off[j] = 0.0;
     }
@@ -817,7 +839,7 @@ __global__ __launch_bounds__(64 * kSureWaves) void verify_sure_kernel(VerifyArgs
       __syncthreads();
       continue;
     }
-    if (wave == 0) draw_from(a, b, d, r, sums, slices, number, 0.0, whole, ps, all, lane);
+    if (wave == 0) draw_from(a, b, d, r, sums, slices, number, 0.0, whole, ps, joined.beside[d.k], all, lane);
     return;
   }
 }
@@ -857,7 +879,7 @@ Plan plan(int32_t sequences, int32_t n, bool drafted, int32_t V) {
   if (slices >= 256) groups = std::max<int64_t>(groups, std::min(512 / sequences, slices / (4 * kRestWaves)));  // (four slices a wave)
   p.groups = slices <= held ? 0 : static_cast<int>(std::min<int64_t>((slices + kRestWaves - 1) / kRestWaves, std::max<int64_t>(1, groups)));
   p.verdicts = (static_cast<int64_t>(sequences) * p.rows * p.parts * static_cast<int64_t>(sizeof(Sums)) + 15) / 16 * 16;
-  p.slice_sums = p.verdicts + (p.groups > 0 ? (static_cast<int64_t>(sequences) * static_cast<int64_t>(sizeof(Verdict)) + 15) / 16 * 16 : 0);
+  p.slice_sums = p.verdicts + (p.groups > 0 ? (static_cast<int64_t>(sequences) * static_cast<int64_t>(sizeof(LeftVerdict)) + 15) / 16 * 16 : 0);
   p.bytes = p.slice_sums + (p.groups > 0 ? static_cast<int64_t>(sequences) * slices * static_cast<int64_t>(sizeof(Slice)) : 0);
   return p;
 }
@@ -890,7 +912,7 @@ int forward(const VerifyArgs& a, void* workspace, hipStream_t stream) {
     else verify_draw_kernel<E, 16, 2><<<a.sequences, 1024, 0, stream>>>(a, p.rows, p.parts, sums);
     return done();
   }
-  Verdict* verdicts = reinterpret_cast<Verdict*>(ws + p.verdicts);
+  LeftVerdict* verdicts = reinterpret_cast<LeftVerdict*>(ws + p.verdicts);
   Slice* slice_sums = reinterpret_cast<Slice*>(ws + p.slice_sums);
   verify_rest_kernel<E><<<dim3(p.groups, a.sequences), 64 * kRestWaves, 0, stream>>>(a, p.rows, p.parts, sums, verdicts, slice_sums);
   if (done() != PB_OK) return PB_EHIP;
