@@ -442,7 +442,8 @@ int pb_grad_clip(const pb_tensors* grads, const float* d_norm, float max_norm, c
  *   u_i = d_uniforms[b, i], w = d_uniforms[b, n_draft], numbers in [0, 1) (others count as the nearest such fp32, NaN as 0)
  *   t_i is accepted if all before it are and u_i q_i(t_i) < p_i(t_i); k = the number of accepted tokens
  *   then a token is drawn from r = max(p_k - q_k, 0) if k < n, from r = p_n if k = n: the first v with
- *     sum_{j <= v} r_j > w sum_j r_j, r_v > 0.  Where max(p_k - q_k, 0) sums to no more than 2^-40, r = p_k.
+ *     sum_{j <= v} r_j > w sum_j r_j, r_v > 0.  Where max(p_k - q_k, 0) sums to no more than 2^-40, r = p_k.  (A difference below 2^-46 of p_k
+ *   is none.)
  * d_accepted[b] = k; d_tokens[b, 0 .. n_draft] = t_0 .. t_k-1, the drawn token, then -1; d_logp (NULL: not wanted) the log p_i of
  * those tokens, NaN beside -1.  n_draft == 0 draws a token from each row.
  * What decides is in 64 bits, so that a draw from hundreds of thousands of tokens, or a number next to p / q, is the definition's; the

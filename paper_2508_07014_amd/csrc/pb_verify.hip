@@ -40,6 +40,9 @@ __device__ __forceinline__ double off_by(double s, int V) {
 constexpr double kBeside = 0x1p-34;      // products of two such bounds, and what the sums in 64 bits are off by
 constexpr double kSmallBeside = 0x1p-20; // of a row's weight beside its largest element, apart from which it is kept below this
 constexpr double kNothing = 0x1p-40;     // a rest of the target's mass below this is none (equal rows differ by their roundings)
+// p - ratio q below this, relative to p, is none: the ratio of two sums in 64 bits, of at most 30 additions one after the other each, is off by up to
+// 2^-47 of itself, and a token of p = q would be drawn for it.
+constexpr double kEven = 0x1p-46;
 constexpr double kNoWeight = 0x1p-960;   // weights below this, masked tokens' among them, are none
 
 typedef VerifyArgs::Scale Scale;
@@ -412,7 +415,7 @@ struct Rest {
 #pragma unroll
     for (int i = 0; i < E::N; ++i) {
       const double d = whole ? p[i] : fma(-ratio, q[i], p[i]);
-      r[i] = d > kNoWeight && (whole || v + i != barred) ? d : 0.0;
+      r[i] = d > fmax(kNoWeight, kEven * p[i]) && (whole || v + i != barred) ? d : 0.0;
     }
   }
 };

@@ -1,4 +1,5 @@
-"""More of the calls around a student on the GPU: handles that are gone, log-probs of near-certain tokens."""
+"""More of the calls around a student on the GPU: handles that are gone, log-probs of near-certain tokens, what
+is left of rows that differ in two places."""
 import numpy as np
 import pytest
 
@@ -72,3 +73,25 @@ def test_log_probs_of_near_certain_tokens(V, n, sure, kind):
             # (beside that the last rounding, and 64 bits' of the difference from the largest and of the logarithm of how many there are)
             room = S.U * abs(want_lp[i]) + beside_error(xv[b, i], T) + 2.0 ** -50 * (abs(xv[b, i, want[i]]) + (xv[b, i] == 0).sum() - 1)
             assert abs(lp[b, i] - want_lp[i]) <= room, (b, i, lp[b, i], want_lp[i], room)
+
+
+@pytest.mark.parametrize("kind", list(KIND))
+@pytest.mark.parametrize("V", [40, 600, 5000, 20011, 131072])
+def test_rows_that_differ_in_two_places(V, kind):
+    """A draft's row is the target's with two logits exchanged: p = q but for these, and nothing but the one that has more of the target's is left,
+    though the two sums are of other orders and differ in their last bits.  A number of 0, at which the first token with any rest is drawn, finds it too."""
+    rng = np.random.default_rng(V)
+    B = 12
+    x = rng.normal(0, 2, (B, 2, V))
+    at = np.array([rng.permutation(np.arange(V // 2, V))[:2] for _ in range(B)])
+    for b in range(B):
+        x[b, 0, at[b]] = [3.0, 1.5]
+    y = x[:, :1].copy()
+    for b in range(B):
+        y[b, 0, at[b]] = [1.5, 3.0]
+    bx, px, xv = block(x, kind, V, 2 * V)
+    by, py, yv = block(y, kind, V + 3, V + 3, 1)
+    for w in (0.0, 0.5, S.BELOW_1):
+        numbers = np.tile([0.5, w], (B, 1))  # (p / q = e^-1.5)
+        out, acc, lp = run_verify(px, py, kind, (V, 2 * V), (V + 3, V + 3), B, 1, V, 1.0, 1.0, at[:, 1:], numbers)
+        assert not acc.any() and np.array_equal(out[:, 0], at[:, 0]), (w, out[:, 0], at[:, 0])
