@@ -1,5 +1,5 @@
 """More of the calls around a student on the GPU: handles that are gone, log-probs of near-certain tokens, what
-is left of rows that differ in two places."""
+is left of rows that differ in two places, sums that are exact, sums of few terms, the largest layouts of the verification, sets past the last cache."""
 import numpy as np
 import pytest
 
@@ -11,9 +11,9 @@ if not torch.cuda.is_available():
 
 import paper_2508_07014_amd as pb  # noqa: E402
 import student as S  # noqa: E402
-from gpu_helpers import DEV, stream_ptr  # noqa: E402
-from test_gpu_logits import KIND  # noqa: E402
-from test_gpu_student import block, run_verify  # noqa: E402
+from gpu_helpers import DEV, dev, stream_ptr  # noqa: E402
+from test_gpu_logits import JUNK, KIND, host, place  # noqa: E402
+from test_gpu_student import block, check_verify, numbers_of, rows_for, run_backward, run_norm, run_verify, set_of, tokens_for, tokens_of  # noqa: E402
 
 
 def test_a_closed_set_to_write_to_is_refused():
@@ -95,3 +95,146 @@ def test_rows_that_differ_in_two_places(V, kind):
         numbers = np.tile([0.5, w], (B, 1))  # (p / q = e^-1.5)
         out, acc, lp = run_verify(px, py, kind, (V, 2 * V), (V + 3, V + 3), B, 1, V, 1.0, 1.0, at[:, 1:], numbers)
         assert not acc.any() and np.array_equal(out[:, 0], at[:, 0]), (w, out[:, 0], at[:, 0])
+
+
+@pytest.mark.parametrize("n,V,dim,hot", [(500, 1025, 640, 0.9), (1000, 3000, 64, 0.5), (4096, 4096, 64, 0.9), (16384, 1000, 64, 0.9), (16384, 166, 3, 0.5),   # a workgroup a token
+                                         (1024, 32001, 320, 0.9), (1000, 131072, 24, 0.5), (90, 9001, 1030, 0.6),                                            # some rows a workgroup
+                                         (8192, 300, 512, 0.9), (20000, 32001, 256, 0.6), (40959, 4097, 128, 0.7), (24000, 131072, 24, 0.9), (5000, 70001, 3, 0.3),  # sorted at once
+                                         (131072, 5000, 4, 0.3), (40960, 300, 100, 0.5), (70000, 32001, 256, 0.35), (131072, 131072, 40, 0.2), (131073, 193, 17, 0.0),  # split first
+                                         (60000, 50000, 512, 0.4), (5000000, 1000, 1, 0.3)])
+def test_table_gradient_of_whole_numbers(n, V, dim, hot):
+    """Every sum of small whole numbers is exact in fp32, in any order: a position that is lost, or counted twice, shows however many a token has."""
+    rng = np.random.default_rng(n + V + dim)
+    tokens = tokens_for(rng, n, V, 0.1, hot)
+    inside = (tokens >= 0) & (tokens < V)
+    g = rng.integers(-3, 4, (n, dim), dtype=np.int8)
+    # (float32: no sum passes 3 n < 2^24)
+    want = torch.zeros((V, dim)).index_add_(0, torch.from_numpy(tokens[inside]), torch.from_numpy(g[inside]).float()).to(DEV)
+    occurs = torch.from_numpy(np.bincount(tokens[inside], minlength=V) > 0).to(DEV)
+    for kind, tkind, accumulate in (("f32", "f32", 0), ("bf16", "f32", 1), ("f16", "bf16", 0), ("bf16", "bf16", 0)):
+        grad = torch.from_numpy(g).to(DEV).to(KIND[kind][1])
+        out = torch.full((V, dim), 5.0 if accumulate else JUNK, dtype=KIND[tkind][1], device=DEV)
+        run_backward(grad, kind, dim, tokens, V, dim, 0.5, accumulate, out, tkind, dim)
+        ref = want * 0.5
+        if accumulate:
+            ref = torch.where(occurs[:, None], ref + 5.0, torch.full_like(ref, 5.0))
+        assert torch.equal(out, ref.to(KIND[tkind][1])), (kind, tkind, accumulate)
+
+
+@pytest.mark.parametrize("n,V,dim", [(64, 1000, 65), (900, 700, 130), (1000, 40000, 96), (4000, 3000, 33), (9000, 9000, 200), (39000, 30000, 24), (50000, 70000, 40), (16000, 40, 3)])
+def test_table_gradient_of_few_terms(n, V, dim):
+    """c terms are summed by c - 1 additions, in any order, and one product: off by c U of their absolute values' sum at most (2^-10 more for products
+    of roundings).  That leaves next to nothing where a token occurs once or twice."""
+    rng = np.random.default_rng(n)
+    tokens = tokens_for(rng, n, V)
+    buf, view, values = place(rng.normal(0, 1, (n, dim)), "f32")
+    out = torch.full((V, dim), JUNK, device=DEV)
+    scale = float(np.float32(0.3))
+    run_backward(view, "f32", dim, tokens, V, dim, scale, 0, out, "f32", dim)
+    inside = (tokens >= 0) & (tokens < V)
+    total, size = np.zeros((V, dim)), np.zeros((V, dim))
+    np.add.at(total, tokens[inside], values[inside])
+    np.add.at(size, tokens[inside], np.abs(values[inside]))
+    count = np.bincount(tokens[inside], minlength=V)
+    assert (np.abs(host(out) - total * scale) <= size * scale * S.U * count[:, None] * (1 + 2.0 ** -10)).all()
+
+
+def some_of(x, sequences):
+    return None if x is None else x[torch.from_numpy(np.asarray(sequences)).to(x.device)]
+
+
+def verify_on_device(x, y, kind, T, tokens, numbers):
+    """run_verify of contiguous rows that are on the device already."""
+    B, n1, V = x.shape
+    return run_verify(x, y, kind, (V, n1 * V), (V, (n1 - 1) * V), B, n1 - 1, V, T, T, tokens, numbers)
+
+
+@pytest.mark.parametrize("kind", list(KIND))
+def test_verify_rows_that_few_workgroups_sum(kind):
+    """140 sequences of long rows: the workgroups of a sequence take slices several times over.  As calls of ten sequences, bit for bit."""
+    rng = np.random.default_rng(14)
+    B, V = 140, 65537
+    g = torch.Generator(device=DEV)
+    g.manual_seed(7)
+    x = (torch.randn((B, 2, V), generator=g, device=DEV) * 2).to(KIND[kind][1])
+    y = (0.9 * x[:, :1].float() + 0.7 * torch.randn((B, 1, V), generator=g, device=DEV)).to(KIND[kind][1])
+    tokens = y.float().argmax(dim=2).cpu().numpy()
+    numbers = rng.random((B, 2)).astype(np.float32)
+    tokens[::3] = (y[::3].float() - x[::3, :1].float()).argmax(dim=2).cpu().numpy()  # (refused)
+    numbers[::3, 0] = S.BELOW_1
+    out, acc, lp = verify_on_device(x, y, kind, 1.0, tokens, numbers)
+    assert 0 < acc.sum() < B
+    for b in range(0, B, 10):
+        few = verify_on_device(x[b:b + 10], y[b:b + 10], kind, 1.0, tokens[b:b + 10], numbers[b:b + 10])
+        for whole, part in zip((out, acc, lp), few):
+            assert np.array_equal(whole[b:b + 10], part, equal_nan=part.dtype.kind == "f")
+    rows = [0, 1, 69, 138, 139]
+    check_verify((out[rows], acc[rows], lp[rows]), host(some_of(x, rows)), host(some_of(y, rows)), 1.0, 1.0, tokens[rows], numbers[rows], kind)
+
+
+@pytest.mark.parametrize("kind", list(KIND))
+@pytest.mark.parametrize("V", [9001, 16000, 16384])
+def test_verify_more_sequences_of_middling_rows(V, kind):
+    """130 sequences are decided and drawn from in one launch where 16-bit rows of 128 take two; both draw the same tokens."""
+    rng = np.random.default_rng(V)
+    B, n = 130, 8
+    g = torch.Generator(device=DEV)
+    g.manual_seed(V)
+    x = (torch.randn((B, n + 1, V), generator=g, device=DEV) * 2).to(KIND[kind][1])
+    y = (0.95 * x[:, :n].float() + 0.3 * torch.randn((B, n, V), generator=g, device=DEV)).to(KIND[kind][1])
+    tokens = y.float().argmax(dim=2).cpu().numpy()
+    tokens[rng.random((B, n)) < 0.03] = -1
+    numbers = numbers_of(rng, B, n, True)
+    out, acc, lp = verify_on_device(x, y, kind, 0.75, tokens, numbers)
+    two = verify_on_device(x[:128], y[:128], kind, 0.75, tokens[:128], numbers[:128])
+    assert np.array_equal(out[:128], two[0]) and np.array_equal(acc[:128], two[1])
+    # (the rows' sums are of the same terms in two orders, 64 bits: a last rounding may fall to either side)
+    some = ~np.isnan(two[2])
+    assert np.array_equal(~np.isnan(lp[:128]), some) and (np.abs(lp[:128][some] - two[2][some]) <= 2 * S.U * np.abs(two[2][some]) + 2.0 ** -45).all()
+    rows = [0, 63, 127, 128, 129]
+    check_verify((out[rows], acc[rows], lp[rows]), host(some_of(x, rows)), host(some_of(y, rows)), 0.75, 0.75, tokens[rows], numbers[rows], (V, kind))
+
+
+@pytest.mark.parametrize("kind", list(KIND))
+@pytest.mark.parametrize("n,V", [(15, 500), (16, 500), (31, 1025), (63, 40), (63, 3001), (63, 9001), (40, 20011)])
+def test_verify_long_drafts(n, V, kind):
+    rng = np.random.default_rng(V + n)
+    for B in (1, 3):
+        x, y = rows_for(rng, B, n, V, kind, True)
+        y[0] = x[0, :n]   # (a draft that is its target: all are accepted but where a row is marked)
+        bx, px, xv = block(x, kind, V + 1, (n + 1) * (V + 1))
+        by, py, yv = block(y, kind, V, n * V)
+        tokens, numbers = tokens_of(rng, xv, yv, B > 1), numbers_of(rng, B, n, True)
+        check_verify(run_verify(px, py, kind, (V + 1, (n + 1) * (V + 1)), (V, n * V), B, n, V, 1.0, 1.0, tokens, numbers), xv, yv, 1.0, 1.0, tokens, numbers, (n, V, kind, B))
+
+
+@pytest.mark.parametrize("kind,size", [("bf16", 140_000_001), ("f16", 134_300_000), ("f32", 70_000_003)])
+def test_sets_past_the_last_cache(kind, size):
+    """More than 256 MiB, odd tensors that begin at any element among them: read past the caches; clipped into other buffers and in place."""
+    g = torch.Generator(device=DEV)
+    g.manual_seed(size)
+    spec = [(77, "f32"), (size, kind), (1, "bf16"), (16385, "f16"), (3_000_001, "bf16")]
+
+    def buffers():
+        bufs = [torch.full((n + 8,), JUNK, dtype=KIND[k][1], device=DEV) for n, k in spec]
+        return bufs, [b[at:at + n] for at, (b, (n, _)) in enumerate(zip(bufs, spec), 1)]
+    bufs, views = buffers()
+    for v in views:
+        v.copy_(torch.randn(v.numel(), generator=g, device=DEV))
+    grads = set_of([(None, v, k) for v, (_, k) in zip(views, spec)])
+    norm = run_norm(grads)
+    want = float(torch.sqrt(sum((v[i:i + (1 << 26)].double().square().sum() for v in views for i in range(0, v.numel(), 1 << 26)))))
+    # (sums in 64 bits: what is left is the last rounding; 2^-30 is room for n 2^-53)
+    assert abs(float(norm) - want) <= want * (S.U + 2.0 ** -30)
+    max_norm = want / 3
+    by = torch.tensor(np.float32(max_norm) / np.float32(float(norm)), device=DEV)
+    obufs, outs = buffers()
+    pb.pb_grad_clip(grads, norm, max_norm, set_of([(None, v, k) for v, (_, k) in zip(outs, spec)]), stream_ptr())
+    torch.cuda.synchronize()
+    for v, o, b in zip(views, outs, obufs):
+        assert torch.equal(o, (v.float() * by).to(v.dtype)) and bool((b[:o.storage_offset()] == JUNK).all()) and bool((b[o.storage_offset() + o.numel():] == JUNK).all())
+    pb.pb_grad_clip(grads, norm, 2 * want, None, stream_ptr())   # (not clipped: nothing changes)
+    pb.pb_grad_clip(grads, norm, max_norm, None, stream_ptr())
+    torch.cuda.synchronize()
+    for v, o, b in zip(views, outs, bufs):
+        assert torch.equal(v, o) and bool((b[:v.storage_offset()] == JUNK).all()) and bool((b[v.storage_offset() + v.numel():] == JUNK).all())
