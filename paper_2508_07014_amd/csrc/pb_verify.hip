@@ -413,9 +413,9 @@ struct Rest {
   // where `whole`.
   __device__ __forceinline__ void rest(int v, const double (&p)[E::N], const double (&q)[E::N], double ratio, bool whole, double (&r)[E::N]) const {
 #pragma unroll
-    for (int i = 0; i < E::N; ++i) {
+    for (int i = 0; i < E::N; ++i) {  // (what is compared hangs on d: kEven p alone is taken out of draw_held()'s loop, into registers that it does not have)
       const double d = whole ? p[i] : fma(-ratio, q[i], p[i]);
-      r[i] = d > fmax(kNoWeight, kEven * p[i]) && (whole || v + i != barred) ? d : 0.0;
+      r[i] = fma(-kEven, p[i], d) > kNoWeight && (whole || v + i != barred) ? d : 0.0;
     }
   }
 };
