@@ -550,6 +550,7 @@ __global__ __launch_bounds__(256) void embed_sums_kernel(SumArgs s, int stretch_
 
 // Pieces of a token, in the order of their stretches: a workgroup a range (and vectors of its columns).  Its groups of lanes take the tokens
 // of few pieces one each; of the others, each group sums a share of the pieces, and the first of them those sums.
+// (Shares are added one after the other in fp32: of a token with 131072 positions 512 pieces by each of 8 groups of 64 lanes.)
 constexpr int kJoinThreads = 512;  // (1024 / 512 / 256: 131072 x 2048 bf16 259 / 256 / 285 us, 8000 x 640 fp32 27.5 / 26.7 / 25.7, 40000 x 128 34.8 / 32.9 / 32.7)
 template <typename T, int K, bool NARROW>
 __global__ __launch_bounds__(kJoinThreads) void embed_join_kernel(SumArgs s, Owners owners, int shift) {
@@ -623,6 +624,7 @@ __device__ __forceinline__ void request_tokens(const EmbedGradArgs& a, int turns
   for (int k = 0; k < TURNS; ++k) t[k] = from + k < turns && p0 + 64 * (from + k) < a.n ? a.tokens[p0 + 64 * (from + k)] : -1;
 }
 // Token v's row of the gradient, by the workgroup; t: its tokens (of the first turns, where there are more than TURNS of them).
+// A group of lanes adds its share one after the other in fp32: up to 1024 of them where small() ends (4096 positions of one token, 64 lanes; 16384, 16).
 template <typename G, typename T, int TURNS, bool LOOP, int K, bool NARROW>
 __device__ __forceinline__ void sum_token(const SumArgs& s, int v, const Columns<K, 1, NARROW>& cols, int (&t)[TURNS], int turns, int p0, SmallShared<K, TURNS, LOOP>& sh) {
   const EmbedGradArgs& a = s.a;

@@ -571,7 +571,7 @@ struct Slice {
   double near_p, near_q;    // of p and q over tokens that may lie on either side, which are not among those
   double low, high;         // the least and the largest p / q - ratio of these (none: inf, -inf)
 };
-// Bound by instructions in 64 bits, 46 an element of both rows (128 sequences of 131072: 42 us); few sequences by the chain of reads up to the
+// Bound by instructions in 64 bits, 46 an element of both rows (128 sequences of 131072: 43 us); few sequences by the chain of reads up to the
 // decision and the row behind it (9 us).
 constexpr int kRestWaves = 16;
 template <typename E>
@@ -733,9 +733,10 @@ __global__ __launch_bounds__(64 * kPickWaves) void verify_pick_kernel(VerifyArgs
 }
 
 // Rows without a draft, and a few of one that was sure of its tokens, need no ratio: all are summed in 64 bits, slice by slice, and one launch more
-// decides and draws from those sums.  us, this way / in three launches, bf16 where not said: 1 x 1 row of 131072 11.2 / 14.8, 70 x 1 of 89793 16.5 / 22.3,
-// 254 x 1 of 34124 17.3 / 22.4, 64 x 1 of 131072 fp32 20.0 / 30.1, 256 x 1 of 131072 34.7 / 50.4; 1 x 5 of 131072 13.8 / 16.5, 22 x 5 of 42561 16.5 / 17.3,
-// 10 x 16 of 41282 fp32 19.1 / 18.9, 98 x 5 of 39809 27.1 / 26.4, 64 x 9 of 50000 32.7 / 27.2.
+// decides and draws from those sums.  us, this way / in three launches, bf16 where not said: 1 x 1 row of 131072 11.7 / 12.6, 70 x 1 of 89793 16.5 / 20.1,
+// 254 x 1 of 34124 17.4 / 20.6, 64 x 1 of 131072 fp32 19.8 / 26.6, 256 x 1 of 131072 34.8 / 46.3; 1 x 5 of 131072 13.9 / 14.4, 22 x 5 of 42561 16.9 / 16.6,
+// 10 x 16 of 41282 fp32 19.0 / 18.3, 98 x 5 of 39809 28.3 / 25.3, 64 x 9 of 50000 34.5 / 25.9.  (256 x 1 of 131072: 32 and 8 us, the first bound by its 16
+// instructions in 64 bits an element, where reading takes 10.)
 constexpr int64_t kSureElements = 5 << 20;  // of rows of a draft
 constexpr int32_t kHeldTwice = 128;         // sequences up to which no workgroup holds two slices of 16-bit rows a wave
 struct SliceSum {
@@ -847,10 +848,10 @@ __global__ __launch_bounds__(64 * kSureWaves) void verify_sure_kernel(VerifyArgs
   }
 }
 
-// How a call is laid out.  us, one launch / two, 16 waves a sequence: 1 x 9 rows of 1024 fp32 8.1 / 9.8, 64 x 17 of 1025 bf16 10.1 / 11.6, 256 x 31 of
-// 1025 12.9 / 17.5, 1 x 17 of 4096 13.1 / 11.9, 256 x 17 of 4096 16.5 / 19.0, 1 x 9 of 8192 14.4 / 13.2, 256 x 9 of 8192 18.7 / 20.9, 64 x 3 of 16384 17.2 /
-// 18.0.  Two launches / three: 1 x 9 rows of 16000 bf16 18.8 / 17.7, 64 x 9 27.6 / 27.3, 128 x 9 30.0 / 29.9, 256 x 9 42.3 / 48.3, 64 x 9 of 8000
-// 18.8 / 22.7, 1 x 9 of 8000 fp32 14.9 / 15.3, 256 x 5 25.2 / 28.2; past what the registers of a workgroup hold there are three.  Workgroups a sequence for 256 / 512 in all: 128 x 17 of 131072 bf16 155 /
+// How a call is laid out.  us, one launch / two, 16 waves a sequence: 1 x 9 rows of 1024 fp32 8.3 / 10.0, 64 x 17 of 1025 bf16 10.4 / 11.8, 256 x 31 of
+// 1025 13.2 / 15.9, 1 x 17 of 4096 12.8 / 11.8, 256 x 17 of 4096 16.7 / 18.5, 1 x 9 of 8192 13.9 / 13.0, 256 x 9 of 8192 18.7 / 20.8, 64 x 3 of 16384 17.3 /
+// 18.1.  Two launches / three: 1 x 9 rows of 16000 bf16 16.5 / 15.4, 64 x 9 22.0 / 21.2, 128 x 9 24.6 / 24.1, 256 x 9 29.5 / 32.4, 64 x 9 of 8000
+// 15.9 / 20.2, 1 x 9 of 8000 fp32 13.7 / 14.3, 256 x 5 20.7 / 23.6; past what the registers of a workgroup hold there are three.  Workgroups a sequence for 256 / 512 in all: 128 x 17 of 131072 bf16 155 /
 // 149, 200 x 3 of 131072 fp32 139.5 / 134.5, 64 x 3 of 131072 bf16 40.0 / 41.4, 64 x 9 of 50000 without rows of the draft 27.0 / 29.2, 128 x 9 of 50000 51.0 /
 // 52.1, 256 x 5 of 65536 72.0 / 73.6, 128 x 17 of 32001 fp32 70.7 / 73.7.
 struct Plan {
