@@ -1,5 +1,6 @@
 """More of the calls around a student on the GPU: handles that are gone, log-probs of near-certain tokens, what
-is left of rows that differ in two places, sums that are exact, sums of few terms, the largest layouts of the verification, sets past the last cache."""
+is left of rows that differ in two places, sums that are exact, sums of few terms, the largest layouts of the verification, sets past the last cache,
+subnormal numbers, temperatures at their ends, gradients that are not finite, nothing but absent tokens."""
 import numpy as np
 import pytest
 
@@ -238,3 +239,97 @@ def test_sets_past_the_last_cache(kind, size):
     torch.cuda.synchronize()
     for v, o, b in zip(views, outs, bufs):
         assert torch.equal(v, o) and bool((b[:v.storage_offset()] == JUNK).all()) and bool((b[v.storage_offset() + v.numel():] == JUNK).all())
+
+
+PATHS = [(500, 1025, 40), (9000, 300, 12), (300, 3, 2), (1000, 20000, 65), (20000, 32001, 9), (6000, 70001, 130), (50000, 3000, 33), (41000, 393216, 3)]
+
+
+@pytest.mark.parametrize("n,V,dim", PATHS)
+@pytest.mark.parametrize("kind,tkind", [("f32", "f32"), ("bf16", "bf16"), ("f16", "f32")])
+def test_table_gradient_of_absent_tokens_alone(n, V, dim, kind, tkind):
+    tokens = np.random.default_rng(n).choice([-1, V, 2 ** 31 - 1, -2 ** 31], n)
+    grad = torch.full((n, dim), float("nan"), dtype=KIND[kind][1], device=DEV)
+    for accumulate in (0, 1):
+        out = torch.full((V, dim), 3.0, dtype=KIND[tkind][1], device=DEV)
+        run_backward(grad, kind, dim, tokens, V, dim, 2.0, accumulate, out, tkind, dim)
+        assert bool((out == (3.0 if accumulate else 0.0)).all())
+
+
+@pytest.mark.parametrize("n,V,dim", PATHS)
+@pytest.mark.parametrize("kind,tkind", [("f32", "f32"), ("bf16", "f32"), ("f16", "bf16")])
+def test_table_gradient_that_is_not_finite(n, V, dim, kind, tkind):
+    """An infinity or a NaN in a column of a gradient is one in that column of its token's row, and nowhere else."""
+    rng = np.random.default_rng(V)
+    tokens = tokens_for(rng, n, V, 0.1, 0.2)
+    g = rng.integers(-3, 4, (n, dim)).astype(np.float32)
+    for value in (np.inf, -np.inf, np.nan):
+        g[rng.integers(0, n, 4), rng.integers(0, dim, 4)] = value
+    inside = (tokens >= 0) & (tokens < V)
+    want = torch.zeros((V, dim)).index_add_(0, torch.from_numpy(tokens[inside]), torch.from_numpy(g[inside]))
+    out = torch.full((V, dim), JUNK, dtype=KIND[tkind][1], device=DEV)
+    run_backward(torch.from_numpy(g).to(DEV).to(KIND[kind][1]), kind, dim, tokens, V, dim, 1.0, 0, out, tkind, dim)
+    want = want.to(KIND[tkind][1]).float()
+    assert not torch.isfinite(want).all() and torch.equal(torch.nan_to_num(out.float().cpu(), nan=-12345.0, posinf=1e30, neginf=-1e30), torch.nan_to_num(want, nan=-12345.0, posinf=1e30, neginf=-1e30))
+
+
+@pytest.mark.parametrize("kind", list(KIND))
+def test_subnormal_numbers(kind):
+    """Values, products and sums below the smallest normal number of their type keep what the type holds of them."""
+    low = {"f32": 2.0 ** -149, "f16": 2.0 ** -24, "bf16": 2.0 ** -133}[kind]  # the type's smallest
+    dim, V = 37, 5
+    table = (torch.arange(V * dim, device=DEV, dtype=torch.float64).view(V, dim) * low).to(torch.float32).to(KIND[kind][1])
+    assert int((table != 0).sum()) == V * dim - 1
+    tokens, out = np.array([4, 0, 3, 3, 1]), torch.full((5, dim), JUNK, dtype=KIND[kind][1], device=DEV)
+    for scale in (1.0, 0.5, 3.0):
+        pb.pb_embed_tokens(table, KIND[kind][0], dim, V, dim, scale, dev(tokens.astype(np.int32)), 5, out, KIND[kind][0], dim, stream_ptr())
+        want = (table.double().cpu() * scale)[torch.from_numpy(tokens)].to(KIND[kind][1])  # (whole multiples of half the smallest: no second rounding)
+        assert torch.equal(out.cpu(), want), scale
+        grad = torch.full((V, dim), JUNK, dtype=KIND[kind][1], device=DEV)
+        run_backward(table, kind, dim, tokens, V, dim, scale, 0, grad, kind, dim)
+        sums = torch.zeros((V, dim), dtype=torch.float64).index_add_(0, torch.from_numpy(tokens), table.double().cpu())
+        assert torch.equal(grad.cpu(), (sums * scale).to(KIND[kind][1])), scale
+    grads = set_of([(None, table.view(-1), kind)])
+    norm = run_norm(grads)
+    want = float(table.double().square().sum().sqrt())
+    assert abs(float(norm) - want) <= want * S.U + 2.0 ** -150  # (half a step of fp32's own)
+    by = torch.full((1,), 4.0, device=DEV)
+    pb.pb_grad_clip(grads, by, 1.0, set_of([(None, out.view(-1), kind)]), stream_ptr())
+    assert torch.equal(out.cpu(), (table.double().cpu() / 4).to(KIND[kind][1]))
+
+
+@pytest.mark.parametrize("kind", list(KIND))
+@pytest.mark.parametrize("T", [1e-4, 1e4])
+@pytest.mark.parametrize("V,n,sure", [(900, 3, False), (7000, 2, False), (40000, 2, False), (40000, 2, True), (40000, 0, True)])
+def test_verify_at_the_ends_of_temperature(V, n, sure, T, kind):
+    rng = np.random.default_rng(V + n)
+    B, T = 6, float(np.float32(T))
+    for size in (1.0, 1e-4, 1e3):
+        x, y = rows_for(rng, B, n, V, kind, True)
+        bx, px, xv = block(x * size, kind, V, (n + 1) * V)
+        py, yv = None, None
+        if n and not sure:
+            by, py, yv = block(y * size, kind, V, n * V)
+        tokens, numbers = tokens_of(rng, xv, xv[:, :n], True), numbers_of(rng, B, n, False)
+        tokens[::2] = xv[::2, :n].argmax(axis=2)
+        out, acc, lp = run_verify(px, py, kind, (V, (n + 1) * V), (V, n * V), B, n, V, T, T, tokens, numbers)
+        check_verify((out, acc, None), xv, yv, T, T, tokens, numbers, (V, T, kind, size))
+
+
+def test_verify_more_sequences_than_a_launch_takes_with_a_draft():
+    """Rows of both models, of middling length and long, in two slices; sequences on both sides as calls of their own."""
+    for V in (9001, 20001):
+        B, n, g = 32900, 1, torch.Generator(device=DEV)
+        g.manual_seed(V)
+        x, y = torch.empty((B, 2, V), dtype=torch.bfloat16, device=DEV), torch.empty((B, 1, V), dtype=torch.bfloat16, device=DEV)
+        for s in range(0, B, 3000):
+            some = torch.randn((min(3000, B - s), 2, V), generator=g, device=DEV) * 2
+            x[s:s + 3000] = some
+            y[s:s + 3000] = 0.9 * some[:, :1] + 0.7 * torch.randn((min(3000, B - s), 1, V), generator=g, device=DEV)
+        tokens, numbers = y.argmax(dim=2).cpu().numpy(), torch.rand((B, 2), generator=g, device=DEV).cpu().numpy()
+        out, acc, lp = verify_on_device(x, y, "bf16", 1.0, tokens, numbers)
+        for first in (0, 32700):  # (200 sequences: laid out as all of them are)
+            s = slice(first, first + 200)
+            for whole, part in zip((out, acc, lp), verify_on_device(x[s], y[s], "bf16", 1.0, tokens[s], numbers[s])):
+                assert np.array_equal(whole[s], part, equal_nan=part.dtype.kind == "f"), (V, first)
+        rows = [0, 32767, 32768, B - 1]
+        check_verify((out[rows], acc[rows], lp[rows]), host(some_of(x, rows)), host(some_of(y, rows)), 1.0, 1.0, tokens[rows], numbers[rows], V)
