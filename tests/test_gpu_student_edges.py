@@ -10,6 +10,7 @@ torch = pytest.importorskip("torch")
 if not torch.cuda.is_available():
     pytest.skip("no GPU", allow_module_level=True)
 
+import logit_rows as R  # noqa: E402
 import paper_2508_07014_amd as pb  # noqa: E402
 import student as S  # noqa: E402
 from gpu_helpers import DEV, dev, stream_ptr  # noqa: E402
@@ -304,11 +305,12 @@ def test_verify_at_the_ends_of_temperature(V, n, sure, T, kind):
     rng = np.random.default_rng(V + n)
     B, T = 6, float(np.float32(T))
     for size in (1.0, 1e-4, 1e3):
-        x, y = rows_for(rng, B, n, V, kind, True)
-        bx, px, xv = block(x * size, kind, V, (n + 1) * V)
+        # (the types' lowest values, as masks, stay what they are or become -inf)
+        x, y = (np.where(np.isfinite(r), np.maximum(r * size, -R.LARGEST["f32"]), r) for r in rows_for(rng, B, n, V, kind, True))
+        bx, px, xv = block(x, kind, V, (n + 1) * V)
         py, yv = None, None
         if n and not sure:
-            by, py, yv = block(y * size, kind, V, n * V)
+            by, py, yv = block(y, kind, V, n * V)
         tokens, numbers = tokens_of(rng, xv, xv[:, :n], True), numbers_of(rng, B, n, False)
         tokens[::2] = xv[::2, :n].argmax(axis=2)
         out, acc, lp = run_verify(px, py, kind, (V, (n + 1) * V), (V, n * V), B, n, V, T, T, tokens, numbers)
